@@ -292,6 +292,128 @@ int topkv_repage_layer(int layer, const void* src_pool, const topkv_layout* src_
                        const topkv_layout* dst_layout, const topkv_batch* dst_batch,
                        topkv_stream_t stream);
 
+/* ---- attention of one new token over the paged cache ------------------------------------------
+ * What a decode worker does with the cache it has received: one layer's attention of ONE new token
+ * per request over the tokens that the block table holds for it (batch->seq_lens counts them, the
+ * new token included: topkv_unpack_layer with window_tokens = 1 writes its K/V, one wire row per
+ * request, and topkv_extend_requests gives it a page). For request r, query head a, KV head
+ * h = a / (num_q_heads / H), over the visible tokens i:
+ *     x_i = scale * k_scale * sum_d q[r][a][d] * K[i][h][d]
+ *     out[r][a][:] = v_scale * sum_i exp(x_i) V[i][h][:] / sum_i exp(x_i)
+ *     lse[r][a] = ln sum_i exp(x_i)
+ * Visible: all s_r tokens, or in a windowed layer (batch->window_tokens = W > 0) the last
+ * min(s_r, W) and the first sink_tokens. A request with no visible token (s_r = 0) gives zeros and
+ * lse = -infinity. Table columns that hold no visible token are ignored; what lies in masked places
+ * (a page's tail, tokens outside the window) is never read.
+ *   kv_factor 2: K and V planes, head_dim at most 256 and a multiple of 8 (16 for 8-bit elements).
+ *   kv_factor 1 with one head: multi-head latent attention in its absorbed form (§5.3). A row is key
+ *     and value at once: K[i] = the row (head_dim at most 576, a multiple of 8), V[i] = its first
+ *     value_dim elements (a multiple of 16, at most 512), shared by all query heads.
+ * Scores, sums and accumulated values are kept in 32 bits; the weights are rounded to 16 bits for
+ * the second product (bf16 for a bf16 cache, else fp16) and the result once to io_type.
+ * Long requests are split between CTAs and joined in a fixed order, through d_workspace: the same
+ * arguments give the same bits. At most two kernels are enqueued on `stream`; no allocation, no
+ * synchronisation, capturable. The workspace holds nothing between calls and needs no
+ * initialisation; calls that may run at the same time (other streams, two captured graphs) need
+ * one each. TOPKV_FLAG_TABLES_SETTLED is honoured; TOPKV_FLAG_OVERLAP_PREVIOUS is ignored (the call
+ * always waits for the kernels before it). cu_seq_lens and total_tokens are optional; a stated
+ * total only bounds the lengths. out and lse must not overlap the inputs. A length outside
+ * [0, max_pages_per_req * P] is cut to that range and a page id outside the pool is skipped
+ * (as if its tokens were not visible); both raise error bit 2. */
+enum { TOPKV_TYPE_BF16 = 1, TOPKV_TYPE_FP16 = 2, TOPKV_TYPE_E4M3 = 3 };
+typedef struct topkv_attention {
+  uint32_t struct_size;       /* = sizeof(topkv_attention)                                         */
+  uint32_t cache_type;        /* TOPKV_TYPE_*: what the cache's elements are (elem_bytes 2, 2, 1).  */
+                              /* E4M3 for kv_factor 2 only                                         */
+  uint32_t io_type;           /* of q and out: BF16 or FP16; the cache's own type when it has 16   */
+                              /* bits                                                              */
+  uint32_t num_q_heads;       /* a multiple of num_kv_heads                                        */
+  uint32_t value_dim;         /* kv_factor 1: leading elements of a row that are the value;        */
+                              /* kv_factor 2: 0 or head_dim                                        */
+  uint32_t sink_tokens;       /* first tokens that stay visible in a windowed layer                */
+  float scale;                /* of the scores, usually 1 / sqrt(head_dim); finite                 */
+  float k_scale, v_scale;     /* what an 8-bit element of K, V is multiplied by; 1 for 16 bits     */
+  uint32_t reserved;          /* must be 0                                                         */
+  int64_t q_request_stride;   /* bytes, multiples of 16; the elements of a head are contiguous.    */
+  int64_t q_head_stride;      /* q may be broadcast (stride 0), rows of out must not overlap       */
+  int64_t out_request_stride;
+  int64_t out_head_stride;
+  float* lse;                 /* DEVICE float [R][num_q_heads] or NULL                             */
+} topkv_attention;
+/* Bytes of d_workspace that topkv_attend_layer needs for these descriptors, whatever the lengths
+ * (0 when no request can be long enough to be split), or a negative topkv_status. */
+int64_t topkv_attend_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                     const topkv_attention* attention);
+/* d_q [R][num_q_heads][head_dim], d_out [R][num_q_heads][value_dim or head_dim], both strided as
+ * described; pool, q, out and workspace bases are multiples of 16 bytes. */
+int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout,
+                       const topkv_batch* batch, const topkv_attention* attention, const void* d_q,
+                       void* d_out, void* d_workspace, int64_t workspace_bytes,
+                       topkv_stream_t stream);
+
+/* ---- pages of the cache: extend, fork, free, compact, copy --------------------------------------
+ * The device-side bookkeeping of a paged cache whose pages may be shared: ref_counts[p] counts the
+ * block-table entries (and whatever else a caller keeps) that use page p, 0 = free. A page id is the
+ * same slot in every layer, so every call below works on all layers of the layout at once (except
+ * topkv_copy_pages, which takes a range). Pages are always given out lowest free id first: a call
+ * has exactly one possible result. The tables are read from batch->block_table, batch->seq_lens and
+ * tables->ref_counts and written whole to the three *_out arrays; an out array may be its in array
+ * (updated in place) and must otherwise not overlap it. batch->window_tokens must be 0;
+ * cu_seq_lens, total_tokens and flags are ignored (a call always waits for the kernels before it).
+ * num_pool_pages must fit an int32. Everything is enqueued on `stream`, one to three kernels; no
+ * allocation, no synchronisation, capturable. Calls that may run at the same time need their own
+ * workspace. What a request cannot be given leaves that request unchanged and raises an error bit:
+ * 2 for unusable arguments found on the device, 8 when there is no free page left for it. An empty
+ * batch (num_requests or max_pages_per_req 0) does nothing, except for topkv_compact_pages. */
+typedef struct topkv_page_tables {
+  uint32_t struct_size;        /* = sizeof(topkv_page_tables)                  */
+  uint32_t reserved;           /* must be 0                                    */
+  const int32_t* ref_counts;   /* DEVICE int32 [num_pool_pages]                */
+  int32_t* block_table_out;    /* DEVICE int32 [R][max_pages_per_req]          */
+  int32_t* seq_lens_out;       /* DEVICE int32 [R]                             */
+  int32_t* ref_counts_out;     /* DEVICE int32 [num_pool_pages]                */
+} topkv_page_tables;
+/* Bytes that the calls below need in d_workspace (16-byte aligned, no initialisation) for this
+ * pool and batch and at most num_forks forks, or a negative topkv_status. */
+int64_t topkv_page_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                   int32_t num_forks);
+/* seq_lens[r] += d_new_tokens[r] (DEVICE int32 [R], >= 0), with the pages that takes. Requests are
+ * served in order: r gets its pages if the free ones suffice for it and for every request before
+ * it (a request that needs no new page always succeeds). */
+int topkv_extend_requests(const topkv_layout* layout, const topkv_batch* batch,
+                          const topkv_page_tables* tables, const int32_t* d_new_tokens,
+                          void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream);
+/* Row d_children[i] becomes a copy of row d_parents[i] (DEVICE int32 [num_forks]) as the rows are
+ * before the call: full pages are shared (their counts go up), the tokens of a last page that is
+ * only partly filled are copied to a page of the child's own, in every layer, so that parent and
+ * child can both be extended. A child row must be empty (length 0) and differ from its parent; of
+ * two forks into one row the first is done. */
+int topkv_fork_requests(void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                        const topkv_page_tables* tables, const int32_t* d_parents,
+                        const int32_t* d_children, int32_t num_forks, void* d_workspace,
+                        int64_t workspace_bytes, topkv_stream_t stream);
+/* The rows d_rows[i] (DEVICE int32 [num_rows]) give back their pages (each count goes down by one),
+ * their table entries become -1 and their lengths 0. Empty rows, and a row's second mention, are
+ * left alone; a count never goes below 0 (error bit 2). */
+int topkv_free_requests(const topkv_layout* layout, const topkv_batch* batch,
+                        const topkv_page_tables* tables, const int32_t* d_rows, int32_t num_rows,
+                        topkv_stream_t stream);
+/* Moves the pages in use to ids 0 .. n-1, n = *d_num_used (DEVICE int32 [1]) of them, so that the
+ * rest of the pool is one free range: the k-th page in use at or above n goes to the k-th free page
+ * below n, with its contents in all layers, its count and every table entry that names it.
+ * d_page_map (DEVICE int32 [num_pool_pages]) gets the new id of every page, -1 for free ones, for
+ * ids that the caller keeps elsewhere. */
+int topkv_compact_pages(void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                        const topkv_page_tables* tables, int32_t* d_num_used, int32_t* d_page_map,
+                        void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream);
+/* Copies page d_src_pages[k] to page d_dst_pages[k] (DEVICE int32 [num_pages]) in the layers
+ * first_layer .. first_layer + num_layers - 1: all page_tokens tokens, planes and heads; padding
+ * between them keeps its value. Precondition (unchecked on the device): no page is the destination
+ * of two copies, or the destination of one and the source of another. */
+int topkv_copy_pages(int first_layer, int num_layers, void* pool, const topkv_layout* layout,
+                     const int32_t* d_src_pages, const int32_t* d_dst_pages, int32_t num_pages,
+                     topkv_stream_t stream);
+
 /* ---- integrity: wire header and CRC-64 (§3.4) ------------------------------------------------ */
 
 /* The fixed 128-byte header of §3.4, one per request: magic, request ID, model ID, tensor
@@ -645,6 +767,7 @@ int topkv_last_cuda_error(void);
  *      those pages were skipped, nothing outside the pool was touched
  *   4  the lengths found on the device did not fit the wire slab (N_layer when total_tokens is
  *      known, else the capacity passed): that work was skipped, nothing outside was touched
+ *   8  a page operator found no free page for a request: that request was left as it was
  * topkv_device_error_flags() waits for ALL work on the current device (cudaDeviceSynchronize:
  * every stream, non-blocking ones included; not a hot-path call) and returns the bits raised on
  * it since the library was loaded or the flags were last reset (0 = none), or a negative

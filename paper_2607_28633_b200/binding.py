@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_double, c_int, c_int32, c_int64, c_uint32, c_void_p
+from ctypes import c_double, c_float, c_int, c_int32, c_int64, c_uint32, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtopkv.so")
@@ -31,6 +31,7 @@ TOPKV_FLAG_OVERLAP_PREVIOUS = 1
 TOPKV_FLAG_TABLES_SETTLED = 2
 TOPKV_LINK_WAIT_PREVIOUS = 1
 TOPKV_NOALLOC_STAGING_BYTES = 8 * 1024 * 1024
+TOPKV_TYPE_BF16, TOPKV_TYPE_FP16, TOPKV_TYPE_E4M3 = 1, 2, 3
 
 # every symbol include/topkv.h declares
 EXPORTS = (
@@ -52,7 +53,9 @@ EXPORTS = (
     "topkv_unpack_model_layers_from_host_pipelined", "topkv_span_link_words",
     "topkv_pack_layer_linked", "topkv_unpack_layer_linked",
     "topkv_pack_layers_to_host_two_lanes", "topkv_unpack_layers_from_host_two_lanes",
-    "topkv_relay_layers_linked",
+    "topkv_relay_layers_linked", "topkv_attend_workspace_bytes", "topkv_attend_layer",
+    "topkv_page_workspace_bytes", "topkv_extend_requests", "topkv_fork_requests",
+    "topkv_free_requests", "topkv_compact_pages", "topkv_copy_pages",
 )
 
 
@@ -126,6 +129,56 @@ def make_layer_table(specs, h_seq_lens, state_pool=None, state_slots=None, state
     t.num_state_slots = num_state_slots
     t._keepalive = (arr, lens, state_pool, state_slots)
     return t
+
+
+class topkv_attention(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", c_uint32), ("cache_type", c_uint32), ("io_type", c_uint32),
+        ("num_q_heads", c_uint32), ("value_dim", c_uint32), ("sink_tokens", c_uint32),
+        ("scale", c_float), ("k_scale", c_float), ("v_scale", c_float), ("reserved", c_uint32),
+        ("q_request_stride", c_int64), ("q_head_stride", c_int64),
+        ("out_request_stride", c_int64), ("out_head_stride", c_int64), ("lse", c_void_p),
+    ]
+
+
+def make_attention(q, out, cache_type: int, io_type: int, scale: float, value_dim: int = 0,
+                   sink_tokens: int = 0, k_scale: float = 1.0, v_scale: float = 1.0,
+                   lse=None) -> topkv_attention:
+    """q [R][num_q_heads][head_dim] and out [R][num_q_heads][value_dim or head_dim]: device tensors
+    of 16-bit elements, whose strides the descriptor takes (the last axis must be contiguous)."""
+    for t in (q, out):
+        if t.ndim != 3 or t.element_size() != 2 or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError("q and out are [requests][heads][elements] of 16-bit elements, the last axis contiguous")
+    if q.shape[:2] != out.shape[:2]:
+        raise ValueError("q and out differ in requests or heads")
+    if lse is not None and (tuple(lse.shape) != tuple(q.shape[:2]) or lse.element_size() != 4 or not lse.is_contiguous()):
+        raise ValueError("lse is a contiguous float32 [requests][heads]")
+    a = topkv_attention()
+    a.struct_size = ctypes.sizeof(topkv_attention)
+    a.cache_type, a.io_type, a.num_q_heads, a.value_dim = cache_type, io_type, q.shape[1], value_dim
+    a.sink_tokens, a.scale, a.k_scale, a.v_scale = sink_tokens, scale, k_scale, v_scale
+    a.q_request_stride, a.q_head_stride = 2 * q.stride(0), 2 * q.stride(1)
+    a.out_request_stride, a.out_head_stride = 2 * out.stride(0), 2 * out.stride(1)
+    a.lse = _ptr(lse)
+    a._keepalive = lse
+    return a
+
+
+class topkv_page_tables(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("reserved", c_uint32), ("ref_counts", c_void_p),
+                ("block_table_out", c_void_p), ("seq_lens_out", c_void_p), ("ref_counts_out", c_void_p)]
+
+
+def make_page_tables(ref_counts, block_table_out, seq_lens_out, ref_counts_out) -> topkv_page_tables:
+    """Device int32 tensors; an out tensor may be the one it is read from (in place)."""
+    t = topkv_page_tables()
+    t.struct_size = ctypes.sizeof(topkv_page_tables)
+    t.ref_counts, t.block_table_out = _ptr(ref_counts), _ptr(block_table_out)
+    t.seq_lens_out, t.ref_counts_out = _ptr(seq_lens_out), _ptr(ref_counts_out)
+    t._keepalive = (ref_counts, block_table_out, seq_lens_out, ref_counts_out)
+    return t
+
+
 TOPKV_TRANSPORT_NVLINK, TOPKV_TRANSPORT_PCIE, TOPKV_TRANSPORT_RDMA, TOPKV_TRANSPORT_TCP = 1, 2, 3, 4
 
 
@@ -242,6 +295,19 @@ def lib() -> ctypes.CDLL:
                    L.topkv_unpack_model_layers_from_host_pipelined):
             fn.argtypes = [c_int, c_int, c_void_p, lp, bp, tp, c_void_p, c_int64, c_void_p, c_int64,
                            c_void_p, c_void_p, c_void_p]
+        ap, pp = ctypes.POINTER(topkv_attention), ctypes.POINTER(topkv_page_tables)
+        L.topkv_attend_workspace_bytes.argtypes = [lp, bp, ap]
+        L.topkv_attend_workspace_bytes.restype = c_int64
+        L.topkv_attend_layer.argtypes = [c_int, c_void_p, lp, bp, ap, c_void_p, c_void_p, c_void_p, c_int64,
+                                         c_void_p]
+        L.topkv_page_workspace_bytes.argtypes = [lp, bp, c_int32]
+        L.topkv_page_workspace_bytes.restype = c_int64
+        L.topkv_extend_requests.argtypes = [lp, bp, pp, c_void_p, c_void_p, c_int64, c_void_p]
+        L.topkv_fork_requests.argtypes = [c_void_p, lp, bp, pp, c_void_p, c_void_p, c_int32, c_void_p, c_int64,
+                                          c_void_p]
+        L.topkv_free_requests.argtypes = [lp, bp, pp, c_void_p, c_int32, c_void_p]
+        L.topkv_compact_pages.argtypes = [c_void_p, lp, bp, pp, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
+        L.topkv_copy_pages.argtypes = [c_int, c_int, c_void_p, lp, c_void_p, c_void_p, c_int32, c_void_p]
         ep = ctypes.POINTER(topkv_endpoint)
         L.topkv_select_transport.argtypes = [ep, ep, c_int, c_int]
         L.topkv_planning_rate.argtypes = [c_int]
@@ -520,6 +586,53 @@ def topkv_repage_layer(layer, src_pool, src_layout, src_batch, dst_pool, dst_lay
                                     ctypes.byref(src_batch), _ptr(dst_pool),
                                     ctypes.byref(dst_layout), ctypes.byref(dst_batch),
                                     _stream(stream))
+
+
+def topkv_attend_workspace_bytes(layout, batch, attention):
+    return lib().topkv_attend_workspace_bytes(ctypes.byref(layout), ctypes.byref(batch),
+                                              ctypes.byref(attention))
+
+
+def topkv_attend_layer(layer, pool, layout, batch, attention, d_q, d_out, d_workspace, workspace_bytes,
+                       stream=None):
+    return lib().topkv_attend_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
+                                    ctypes.byref(attention), _ptr(d_q), _ptr(d_out), _ptr(d_workspace),
+                                    workspace_bytes, _stream(stream))
+
+
+def topkv_page_workspace_bytes(layout, batch, num_forks=0):
+    return lib().topkv_page_workspace_bytes(ctypes.byref(layout), ctypes.byref(batch), num_forks)
+
+
+def topkv_extend_requests(layout, batch, tables, d_new_tokens, d_workspace, workspace_bytes, stream=None):
+    return lib().topkv_extend_requests(ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(tables),
+                                       _ptr(d_new_tokens), _ptr(d_workspace), workspace_bytes,
+                                       _stream(stream))
+
+
+def topkv_fork_requests(pool, layout, batch, tables, d_parents, d_children, num_forks, d_workspace,
+                        workspace_bytes, stream=None):
+    return lib().topkv_fork_requests(_ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
+                                     ctypes.byref(tables), _ptr(d_parents), _ptr(d_children), num_forks,
+                                     _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def topkv_free_requests(layout, batch, tables, d_rows, num_rows, stream=None):
+    return lib().topkv_free_requests(ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(tables),
+                                     _ptr(d_rows), num_rows, _stream(stream))
+
+
+def topkv_compact_pages(pool, layout, batch, tables, d_num_used, d_page_map, d_workspace,
+                        workspace_bytes, stream=None):
+    return lib().topkv_compact_pages(_ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
+                                     ctypes.byref(tables), _ptr(d_num_used), _ptr(d_page_map),
+                                     _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def topkv_copy_pages(first_layer, num_layers, pool, layout, d_src_pages, d_dst_pages, num_pages,
+                     stream=None):
+    return lib().topkv_copy_pages(first_layer, num_layers, _ptr(pool), ctypes.byref(layout),
+                                  _ptr(d_src_pages), _ptr(d_dst_pages), num_pages, _stream(stream))
 
 
 def topkv_header_fill(header, request_id, model_id, layout, seq_len, crc_k, crc_v):

@@ -5,7 +5,9 @@
 // This file holds the host side: argument checks, launch geometry and the extern "C" entry
 // points declared and documented in include/topkv.h. The kernels live in the .cuh files next
 // to it (topkv_vec: vectorised page copy and plan; topkv_bulk: bulk-async ring; topkv_repage:
-// pool to pool; topkv_crc: checksummed copy); topkv_host.cpp holds the CUDA-free helpers.
+// pool to pool; topkv_crc: checksummed copy; topkv_attend: attention over the paged cache;
+// topkv_pages: page operators; the host side of these two is topkv_decode_host.cuh);
+// topkv_host.cpp holds the CUDA-free helpers.
 // Nothing here ever calls the CPU oracle.
 #include "topkv.h"
 
@@ -19,6 +21,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <mutex>
@@ -1690,3 +1693,5 @@ int topkv_set_kernel_variant(int variant) {
 }
 
 }  // extern "C"
+
+#include "topkv_decode_host.cuh"

@@ -1,0 +1,577 @@
+// Attention of one new token per request over one layer of a paged cache with K and V planes.
+//
+//   x_i = scale * k_scale * q . K[i]      m = max x_i      l = sum exp(x_i - m)
+//   out = v_scale * sum exp(x_i - m) V[i] / l              lse = m + ln l
+// over the visible tokens i of the request. A window with first tokens that stay visible leaves two
+// ranges, [0, ns) and [lo, s): the kernel numbers the visible tokens 0 .. n-1 straight through, so
+// nothing that is masked is ever loaded, and a NaN left behind there cannot reach the result.
+//
+// What bounds it: every K and V byte is read once and used for G query heads, 2 G flops a byte at 16
+// bits, so for the usual G <= 16 it is memory, far below the tensor rate; the matrix instructions
+// are warp-wide m16n8k16 ones with the G query heads as rows (padded to 16), which need no shared
+// staging of accumulators and leave 85 % of the issue slots free. Layout of the work:
+//  * a CTA has 4 warps and one KV head; each warp takes its own 16 tokens of every 64 and runs its
+//    own ring of cp.async stages, running maximum and sum, so the loop has no CTA barrier at all;
+//  * the visible tokens of all requests, cut into tiles of 64, are shared out evenly between
+//    `teams` of CTAs (one CTA per KV head and group of 16 query heads in a team, so that a team
+//    reads whole token rows at about the same time), whatever the lengths: a long request is
+//    split between teams, and several short ones may fall to one;
+//  * a request that lies inside one team is finished by it. Of one that is cut, each team leaves
+//    its (m, l, sum) in the workspace and topkv_attend_join_kernel joins the parts in their
+//    order, so the result does not depend on which CTA ran when.
+// Scores, maxima, sums and the accumulated values are 32-bit; the weights exp(x - m) are rounded to
+// the 16-bit type of the values for the second product (to fp16 for an 8-bit cache): half a step of
+// 2^-8 (bf16) or 2^-11 of each weight, which averages out over the tokens and stays below the
+// rounding of the output.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "topkv_bulk.cuh"
+#include "topkv_common.cuh"
+
+namespace topkv {
+
+constexpr int kAttendWarps = 4;
+constexpr int kAttendThreads = kAttendWarps * 32;
+constexpr int kWarpTokens = 16;
+constexpr int kTileTokens = kAttendWarps * kWarpTokens;
+constexpr int kAttendRows = 16;      // query heads per CTA (rows of the matrix instruction)
+constexpr int kUncutTiles = 4;       // requests of at most this many tiles are not cut
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+enum AttendType { kBf16 = 1, kFp16 = 2, kE4m3 = 3 };
+
+struct AttendParams {
+  const uint8_t* pool;  // this layer's slab
+  const int32_t* bt;
+  const int32_t* sl;
+  const uint8_t* q;
+  uint8_t* out;
+  float* lse;           // [R][Hq] or nullptr
+  int64_t S_page, S_kv, S_tok, S_head;
+  int64_t q_req, q_head, o_req, o_head;  // bytes
+  int64_t num_pages;
+  int R, maxp, P;
+  int H, G, gtiles;     // KV heads, query heads per KV head, groups of 16 query heads per KV head
+  int D, Dv;            // elements
+  int window, sinks;
+  float qk_scale;       // scale * k_scale * log2(e): scores are kept in powers of two
+  float v_scale;
+  int io_bf16;
+  int teams;            // CTAs along x; 0 tiles of a request cross a team when uncut
+  int uncut;            // 1: team t is request t
+  int late_wait;        // tables are settled
+  int rows;             // rows of a partial result, min(G, 16)
+  // workspace
+  int2* cuts;           // [teams]: the request that the team's range begins inside of, or -1; and whether that
+                        // request begins behind the start of the range before (its part there is slot 1)
+  float2* ml;           // [teams][2][H * gtiles][rows]
+  float* part;          // [teams][2][H * gtiles][rows][Dv]
+};
+
+// Visible tokens of a request: 0 .. n-1 stand for tokens 0 .. ns-1 and lo, lo+1, ..
+struct Visible {
+  int n, ns, lo;
+};
+__device__ __forceinline__ Visible visible_tokens(const AttendParams& p, int r, bool complain) {
+  int s = p.sl[r];
+  const int64_t row = (int64_t)p.maxp * p.P;
+  if (s < 0 || s > row) {
+    if (complain) raise_error(kErrTable);
+    s = s < 0 ? 0 : (int)row;
+  }
+  Visible v;
+  v.lo = p.window > 0 ? max(s - p.window, 0) : 0;
+  v.ns = min(p.sinks, v.lo);
+  v.n = v.ns + s - v.lo;
+  return v;
+}
+__device__ __forceinline__ int attend_tiles(int n) { return n / kTileTokens + (n % kTileTokens != 0); }
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  const int n = valid ? 16 : 0;  // 0: nothing is read, the 16 bytes become zero
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+// Two 8-bit values (low 16 bits) to two fp16 values; exact.
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
+  uint32_t r;
+  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ float load_io(const uint8_t* p, bool bf16) {
+  return bf16 ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(p))
+              : __half2float(*reinterpret_cast<const __half*>(p));
+}
+__device__ __forceinline__ void store_io(uint8_t* p, float v, bool bf16) {
+  if (bf16)
+    *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v);
+  else
+    *reinterpret_cast<__half*>(p) = __float2half_rn(v);
+}
+
+// Shared memory: per warp a ring of stages, each 16 rows of K and 16 rows of V of DP elements.
+// Rows are swizzled in 16-byte chunks so that the eight rows of a matrix load hit all banks.
+template <int DP, int TYPE>
+struct AttendShape {
+  static constexpr int kElem = TYPE == kE4m3 ? 1 : 2;
+  static constexpr int kRow = DP * kElem;                    // bytes of a row
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kStage = 2 * kWarpTokens * kRow;      // K rows, then V rows
+  static constexpr int kStages = kStage >= 16384 ? 3 : (kStage <= 2048 ? 8 : 24576 / kStage);
+  static constexpr int kSmem = kAttendWarps * kStages * kStage;
+  static_assert(kSmem >= kAttendWarps * kAttendRows * (DP + 2) * 4, "the epilogue reuses the ring");
+  static __device__ __forceinline__ uint32_t at(int token, int chunk) {
+    const int s = kChunks >= 8 ? (token & 7) : ((token >> 1) & 3);
+    return (uint32_t)(token * kRow + ((chunk ^ s) << 4));
+  }
+};
+
+template <int DP, int TYPE>
+__global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const AttendParams p) {
+  using S = AttendShape<DP, TYPE>;
+  constexpr bool kMmaBf16 = TYPE == kBf16;
+  constexpr float kShift = kMmaBf16 ? 0.f : 15.f;
+  constexpr int kSteps = DP / 16;  // k-steps of the first product, pairs of n-tiles of the second
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int64_t s_scan[kAttendWarps];
+  __shared__ int s_start[2];
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
+  const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * kAttendRows;
+  const int rows = min(p.G - g0, kAttendRows);
+  if (!p.late_wait) pdl_wait_prior_grid();
+  pdl_release_next_grid();
+
+  // ---- which tiles are this team's: [a, b) of all requests' tiles laid end to end -------------
+  int64_t a = 0, b = 0, prev = 0;
+  int r = team, t0 = 0;  // first request, and the tile in it to begin with
+  if (!p.uncut) {
+    const int per = (p.R + kAttendThreads - 1) / kAttendThreads;
+    const int r0 = min(tid * per, p.R), r1 = min(r0 + per, p.R);
+    int64_t mine = 0;
+    for (int i = r0; i < r1; ++i) mine += attend_tiles(visible_tokens(p, i, false).n);
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    if (tid == 0) s_start[0] = -1;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < kAttendWarps; ++w) {
+      if (w < warp) incl += s_scan[w];
+      total += s_scan[w];
+    }
+    const int teams = (int)min((int64_t)p.teams, total);  // no team between two others is without tiles
+    if (team < teams) {
+      a = total * team / teams;
+      b = total * (team + 1) / teams;
+      prev = team > 0 ? total * (team - 1) / teams : 0;
+    }
+    if (a < b && a >= incl - mine && a < incl) {  // exactly one thread
+      int64_t at = incl - mine;
+      for (int i = r0; i < r1; ++i) {
+        const int n = attend_tiles(visible_tokens(p, i, false).n);
+        if (a < at + n) {
+          s_start[0] = i;
+          s_start[1] = (int)(a - at);
+          break;
+        }
+        at += n;
+      }
+    }
+    __syncthreads();
+    r = s_start[0];
+    t0 = s_start[1];
+  }
+  if (p.late_wait) pdl_wait_prior_grid();
+  if (!p.uncut && unit == 0 && tid == 0)
+    p.cuts[team] = a < b && t0 > 0 ? make_int2(r, a - t0 > prev) : make_int2(-1, 0);
+
+  const int64_t q_head0 = (int64_t)h * p.G + g0;
+  // requests with nothing to see: zeros, and a log-sum-exp of minus infinity
+  for (int e = team; e < p.R; e += p.teams) {
+    if (visible_tokens(p, e, unit == 0 && tid == 0).n > 0) continue;
+    for (int i = tid; i < rows * p.Dv; i += kAttendThreads) {
+      const int g = i / p.Dv, d = i - g * p.Dv;
+      store_io(p.out + e * p.o_req + (q_head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
+    }
+    if (p.lse != nullptr && tid < rows)
+      p.lse[(int64_t)e * p.H * p.G + q_head0 + tid] = -INFINITY;
+  }
+  if (!p.uncut && a >= b) return;
+
+  uint8_t* ring = smem + warp * S::kStages * S::kStage;
+  const uint32_t ring_a = smem_addr(ring);
+  if (p.D < DP) {  // columns past the head dimension stay zero
+    for (int i = lane; i < S::kStages * S::kStage / 16; i += 32)
+      reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
+  }
+  const int chunks = p.D * S::kElem / 16;
+  const uint8_t* k_base = p.pool + (int64_t)h * p.S_head;
+  int64_t left = p.uncut ? 1 : b - a;
+  const int gr = lane >> 2, gc = lane & 3;  // row and column group of this thread in a matrix fragment
+
+  for (bool first = true; left > 0 && r < p.R; first = false, t0 = 0, ++r) {
+    const Visible vis = visible_tokens(p, r, false);
+    const int tiles = attend_tiles(vis.n);
+    if (tiles == 0) {
+      if (p.uncut) return;
+      continue;
+    }
+    const int t1 = p.uncut ? tiles : (int)min((int64_t)tiles, t0 + left);
+    left -= p.uncut ? 1 : t1 - t0;
+
+    // ---- the query rows as fragments ----------------------------------------------------------
+    uint32_t qf[kSteps][4];
+    float row_scale[2] = {p.qk_scale, p.qk_scale};
+    {
+      const uint8_t* qp = p.q + r * p.q_req + q_head0 * p.q_head;
+      float top[2] = {0.f, 0.f};
+      // For an 8-bit cache a thread's four consecutive elements take the places (2c, 2c+1, 2c+8, 2c+9)
+      // of a k-step, in Q and in K alike: that is how four 8-bit values of K arrive in one register.
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int row = gr + (j & 1) * 8;
+          const int col = k * 16 + (TYPE == kE4m3 ? gc * 4 + (j >> 1) * 2 : gc * 2 + (j >> 1) * 8);
+          uint32_t v = 0;
+          if (row < rows && col < p.D) v = *reinterpret_cast<const uint32_t*>(qp + row * p.q_head + col * 2);
+          qf[k][j] = v;
+          if (TYPE == kE4m3 && p.io_bf16)
+            top[j & 1] = fmaxf(top[j & 1], fmaxf(fabsf(__uint_as_float(v << 16)), fabsf(__uint_as_float(v & 0xffff0000u))));
+        }
+      if (TYPE == kE4m3 && p.io_bf16) {
+        // bf16 queries become fp16 ones: exact after a power of two per row, except for elements
+        // below 2^-14 of the row's largest, which keep an absolute error of 2^-25 of it
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+          int e = 0;
+          if (top[i] > 0.f && top[i] < INFINITY) e = ilogbf(top[i]);
+          // in two steps: a single factor of 2^-e may itself leave the range of a float
+          const float half_up = exp2f((float)(-(e / 2))), rest_up = exp2f((float)(-(e - e / 2)));
+          row_scale[i] = p.qk_scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if ((j & 1) == i) {
+                const uint32_t v = qf[k][j];
+                qf[k][j] = pack2<false>(__uint_as_float(v << 16) * half_up * rest_up,
+                                        __uint_as_float(v & 0xffff0000u) * half_up * rest_up);
+              }
+        }
+      }
+    }
+
+    float o[2 * kSteps][4];
+#pragma unroll
+    for (int i = 0; i < 2 * kSteps; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+    // ---- this warp's 16 tokens of every tile ---------------------------------------------------
+    // byte offset of the row of visible token v, or -1: past the end, or a page outside the pool
+    auto locate = [&](int t) -> int64_t {
+      const int v = t * kTileTokens + warp * kWarpTokens + (lane & 15);
+      if (t >= t1 || v >= vis.n) return -1;
+      const int i = v < vis.ns ? v : v - vis.ns + vis.lo;
+      const int j = i / p.P;
+      const int pg = p.bt[(int64_t)r * p.maxp + j];
+      if (pg < 0 || pg >= p.num_pages) {
+        raise_error(kErrTable);
+        return -1;
+      }
+      return (int64_t)pg * p.S_page + (int64_t)(i - j * p.P) * p.S_tok;
+    };
+    uint32_t stage_mask[S::kStages];  // which of a stage's 16 tokens count
+    auto issue = [&](int stage, int64_t off) {
+      const uint32_t dst = ring_a + stage * S::kStage;
+#pragma unroll
+      for (int i = 0; i < kWarpTokens * S::kChunks / 32; ++i) {
+        const int idx = i * 32 + lane;
+        const int token = idx / S::kChunks, chunk = idx % S::kChunks;
+        const int64_t row = __shfl_sync(0xffffffffu, off, token);
+        if (chunk < chunks) {
+          const uint8_t* src = k_base + (row < 0 ? 0 : row) + chunk * 16;
+          const uint32_t to = dst + S::at(token, chunk);
+          cp_async16(to, src, row >= 0);
+          cp_async16(to + kWarpTokens * S::kRow, src + (row < 0 ? 0 : p.S_kv), row >= 0);
+        }
+      }
+      return __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
+    };
+    int64_t next = locate(t0);
+#pragma unroll
+    for (int s = 0; s < S::kStages - 1; ++s) {
+      const int64_t off = next;
+      next = locate(t0 + s + 1);
+      stage_mask[s] = issue(s, off);
+      cp_async_commit();
+    }
+    int stage = 0;
+    for (int t = t0; t < t1; ++t) {
+      {
+        const int64_t off = next;
+        next = locate(t + S::kStages);
+        int fill = stage + S::kStages - 1;
+        if (fill >= S::kStages) fill -= S::kStages;
+        const uint32_t mask = issue(fill, off);
+        cp_async_commit();
+#pragma unroll
+        for (int s = 0; s < S::kStages; ++s)
+          if (s == fill) stage_mask[s] = mask;
+      }
+      uint32_t mask = 0;
+#pragma unroll
+      for (int s = 0; s < S::kStages; ++s)
+        if (s == stage) mask = stage_mask[s];
+      cp_async_wait<S::kStages - 1>();
+      __syncwarp();
+      const uint32_t k_a = ring_a + stage * S::kStage, v_a = k_a + kWarpTokens * S::kRow;
+      if (mask != 0) {
+        float s[2][4] = {};
+        if constexpr (TYPE == kE4m3) {
+#pragma unroll
+          for (int k = 0; k < kSteps; k += 2) {
+            uint32_t b4[4];
+            ldmatrix4(b4, k_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k + (lane >> 4)));
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                mma16816<false>(s[j], qf[k + u], e4m3x2_to_f16x2(b4[u * 2 + j] & 0xffffu),
+                                e4m3x2_to_f16x2(b4[u * 2 + j] >> 16));
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) {
+            uint32_t b4[4];
+            ldmatrix4(b4, k_a + S::at((lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)));
+            mma16816<kMmaBf16>(s[0], qf[k], b4[0], b4[1]);
+            mma16816<kMmaBf16>(s[1], qf[k], b4[2], b4[3]);
+          }
+        }
+        // scores of rows gr and gr + 8 at tokens gc*2, +1, +8, +9
+        float top[2] = {m[0], m[1]};
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool seen = (mask >> (j * 8 + gc * 2 + (e & 1))) & 1;
+            s[j][e] = seen ? s[j][e] * row_scale[e >> 1] : -INFINITY;
+            top[e >> 1] = fmaxf(top[e >> 1], s[j][e]);
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+        }
+        if (__any_sync(0xffffffffu, top[0] != m[0] || top[1] != m[1])) {
+          float alpha[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            alpha[i] = top[i] == m[i] ? 1.f : exp2f(m[i] - top[i]);
+            l[i] *= alpha[i];
+            m[i] = top[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 2 * kSteps; ++i) {
+            o[i][0] *= alpha[0];
+            o[i][1] *= alpha[0];
+            o[i][2] *= alpha[1];
+            o[i][3] *= alpha[1];
+          }
+        }
+        // the sums are kept relative to m - kShift: fp16 weights then run up to 2^15, so that one
+        // of them is exact to 2^-11 down to 2^-29 of the largest instead of 2^-14
+        const float base[2] = {m[0] == -INFINITY ? 0.f : m[0] - kShift, m[1] == -INFINITY ? 0.f : m[1] - kShift};
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[j][e] = exp2f(s[j][e] - base[e >> 1]);
+            l[e >> 1] += s[j][e];
+          }
+        uint32_t pf[4];
+        pf[0] = pack2<kMmaBf16>(s[0][0], s[0][1]);
+        pf[1] = pack2<kMmaBf16>(s[0][2], s[0][3]);
+        pf[2] = pack2<kMmaBf16>(s[1][0], s[1][1]);
+        pf[3] = pack2<kMmaBf16>(s[1][2], s[1][3]);
+        if constexpr (TYPE == kE4m3) {
+          // a transposed load of 16-bit units brings two neighbouring columns of two tokens: the
+          // even columns of a 16-byte chunk form one n-tile, the odd ones the other
+#pragma unroll
+          for (int k = 0; k < kSteps; k += 2) {
+            uint32_t b4[4];
+            ldmatrix4_trans(b4, v_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k + (lane >> 4)));
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t e0 = __byte_perm(b4[u * 2], b4[u * 2], 0x3120), e1 = __byte_perm(b4[u * 2 + 1], b4[u * 2 + 1], 0x3120);
+              mma16816<false>(o[(k + u) * 2], pf, e4m3x2_to_f16x2(e0 & 0xffffu), e4m3x2_to_f16x2(e1 & 0xffffu));
+              mma16816<false>(o[(k + u) * 2 + 1], pf, e4m3x2_to_f16x2(e0 >> 16), e4m3x2_to_f16x2(e1 >> 16));
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) {
+            uint32_t b4[4];
+            ldmatrix4_trans(b4, v_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k * 2 + (lane >> 4)));
+            mma16816<kMmaBf16>(o[k * 2], pf, b4[0], b4[1]);
+            mma16816<kMmaBf16>(o[k * 2 + 1], pf, b4[2], b4[3]);
+          }
+        }
+      }
+      __syncwarp();
+      if (++stage == S::kStages) stage = 0;
+    }
+    cp_async_wait<0>();
+    __syncthreads();
+
+    // ---- the four warps' results joined, through the ring's memory ------------------------------
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+    }
+    float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][DP]
+    float* s_m = s_o + kAttendWarps * kAttendRows * DP;                       // [warp][row]
+    float* s_l = s_m + kAttendWarps * kAttendRows;
+    if (gc == 0) {
+      s_m[warp * kAttendRows + gr] = m[0] - kShift;
+      s_m[warp * kAttendRows + gr + 8] = m[1] - kShift;
+      s_l[warp * kAttendRows + gr] = l[0];
+      s_l[warp * kAttendRows + gr + 8] = l[1];
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * kSteps; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = gr + (e >> 1) * 8, c = gc * 2 + (e & 1);
+        const int col = TYPE == kE4m3 ? (i >> 1) * 16 + c * 2 + (i & 1) : i * 8 + c;
+        if (row < rows) s_o[(warp * kAttendRows + row) * DP + col] = o[i][e];
+      }
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == tiles;
+    const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
+    for (int i = tid; i < rows * p.Dv; i += kAttendThreads) {
+      const int g = i / p.Dv, d = i - g * p.Dv;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) top = fmaxf(top, s_m[w * kAttendRows + g]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) {
+        const float f = exp2f(s_m[w * kAttendRows + g] - base);
+        sum += f * s_l[w * kAttendRows + g];
+        acc += f * s_o[(w * kAttendRows + g) * DP + d];
+      }
+      if (whole) {
+        store_io(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc / sum * p.v_scale, p.io_bf16);
+        if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+      } else {
+        p.part[(slot * p.rows + g) * p.Dv + d] = acc;
+        if (d == 0) p.ml[slot * p.rows + g] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();
+    if (p.D < DP && left > 0) {  // the epilogue has written over the zero columns
+      for (int i = lane; i < S::kStages * S::kStage / 16; i += 32)
+        reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+      __syncwarp();
+    }
+    if (p.uncut) return;
+  }
+}
+
+// Joins the parts of the requests that were cut: the CTA of the first cut inside a request takes
+// it. Parts are added in the order of the tokens.
+constexpr int kJoinThreads = 128;
+__global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const AttendParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int team = blockIdx.x + 1, unit = blockIdx.y;
+  const int2 cut = p.cuts[team];
+  if (cut.x < 0 || p.cuts[team - 1].x == cut.x) return;  // no cut here, or not the request's first
+  int last = team - 1;  // the last team that holds a part: those that begin inside the request follow each other
+  for (int base = team; base < p.teams; base += kJoinThreads) {
+    const int t = base + threadIdx.x;
+    const int n = __syncthreads_count(t < p.teams && p.cuts[t].x == cut.x);
+    last += n;
+    if (n < kJoinThreads) break;
+  }
+  const int r = cut.x, units = gridDim.y;
+  const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * kAttendRows;
+  const int rows = min(p.G - g0, kAttendRows);
+  const int64_t q_head0 = (int64_t)h * p.G + g0;
+  for (int i = blockIdx.z * kJoinThreads + threadIdx.x; i < rows * p.Dv; i += kJoinThreads * gridDim.z) {
+    const int g = i / p.Dv, d = i - g * p.Dv;
+    auto slot = [&](int t) -> int64_t { return (((int64_t)t * 2 + (t == team - 1 ? cut.y : 0)) * units + unit) * p.rows + g; };
+    float top = -INFINITY;
+    for (int t = team - 1; t <= last; ++t) top = fmaxf(top, p.ml[slot(t)].x);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, acc = 0.f;
+    for (int t = team - 1; t <= last; ++t) {
+      const float2 ml = p.ml[slot(t)];
+      const float f = exp2f(ml.x - base);
+      sum += f * ml.y;
+      acc += f * p.part[slot(t) * p.Dv + d];
+    }
+    store_io(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc / sum * p.v_scale, p.io_bf16);
+    if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+  }
+}
+
+}  // namespace topkv

@@ -54,8 +54,9 @@ struct KParams {
 //   2  a table entry was unusable (page id outside the pool, or a length longer than its
 //      block-table row): the affected pages were skipped
 //   4  the lengths found on the device do not fit the wire slab: the affected work was skipped
+//   8  a page operator needed more free pages than the pool has: the requests it names were left out
 __device__ int g_device_error_flags = 0;
-constexpr int kErrWait = 1, kErrTable = 2, kErrWire = 4;
+constexpr int kErrWait = 1, kErrTable = 2, kErrWire = 4, kErrPages = 8;
 __device__ __forceinline__ void raise_error(int bit) {
   if ((*(volatile int*)&g_device_error_flags & bit) == 0) atomicOr(&g_device_error_flags, bit);
 }
@@ -171,9 +172,9 @@ struct Vec<32> {
 };
 
 // Launch with programmatic stream serialisation allowed (see pdl_prologue above).
-template <typename P>
-cudaError_t launch_pdl(void (*kernel)(const P), dim3 grid, dim3 block, size_t smem,
-                       cudaStream_t stream, const P& params) {
+template <typename... K, typename... P>
+cudaError_t launch_pdl(void (*kernel)(K...), dim3 grid, dim3 block, size_t smem,
+                       cudaStream_t stream, const P&... params) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -184,7 +185,7 @@ cudaError_t launch_pdl(void (*kernel)(const P), dim3 grid, dim3 block, size_t sm
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, params);
+  return cudaLaunchKernelEx(&cfg, kernel, params...);
 }
 
 }  // namespace topkv

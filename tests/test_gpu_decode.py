@@ -1,0 +1,534 @@
+"""GPU tests of the decode side: attention of one new token over the paged cache against the oracle
+in 64 bits (tolerances derived in oracle.decode.attend), and the page operators against the
+oracle's loops, integer for integer and byte for byte."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import oracle
+from oracle import Geom, decode as od
+from paper_2607_28633_b200 import binding as tk
+
+pytestmark = pytest.mark.gpu
+
+TYPE = {"bf16": tk.TOPKV_TYPE_BF16, "fp16": tk.TOPKV_TYPE_FP16, "e4m3": tk.TOPKV_TYPE_E4M3}
+TORCH = {"bf16": torch.bfloat16, "fp16": torch.float16}
+NAN = {"bf16": (0xC1, 0x7F), "fp16": (0x01, 0x7E), "e4m3": (0x7F, 0xFF)}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    import __graft_entry__ as entry
+    entry.build()
+    return torch.device("cuda:0")
+
+
+@pytest.fixture(autouse=True)
+def clean(dev):
+    tk.check(tk.topkv_reset_device_error_flags())
+    yield
+    assert tk.topkv_device_error_flags() == 0
+
+
+def _layout(g: Geom):
+    lo = tk.make_layout(g.L, g.F, g.h_kv, g.d_h, g.b_p, g.P, g.num_pages, kind=tk.TOPKV_KIND_GQA)
+    lo.pool_layer_stride, lo.pool_page_stride, lo.pool_kv_stride = g.S_layer, g.S_page, g.S_kv
+    lo.pool_token_stride, lo.pool_head_stride = g.S_tok, g.S_head
+    return lo
+
+
+def _geom(F, H, D, E, P, pages, style="page", L=1, window=0):
+    g = Geom(L=L, F=F, h_kv=H, d_h=D, b_p=E, P=P, num_pages=pages)
+    if style == "padded":
+        g.S_tok = H * D * E + 32
+        g.S_kv = P * g.S_tok
+        g.S_page = F * g.S_kv + 16
+        g.S_layer = pages * g.S_page
+    elif style == "head":
+        g.S_tok = D * E
+        g.S_head = P * g.S_tok
+        g.S_kv = H * g.S_head
+        g.S_page = F * g.S_kv
+        g.S_layer = pages * g.S_page
+    elif style == "plane":
+        g.S_page = P * g.S_tok
+        g.S_kv = pages * g.S_page
+        g.S_layer = F * g.S_kv + 16
+    g.window = window
+    return g
+
+
+def _table(sl, P, spare, extra_cols, rng):
+    pages = -(-np.asarray(sl) // P)
+    n = int(pages.sum()) + spare
+    bt = np.full((len(sl), max(int(pages.max()), 1) + extra_cols), -1, np.int32)
+    perm, pos = rng.permutation(n), 0
+    for r, k in enumerate(pages):
+        bt[r, :k] = perm[pos:pos + k]
+        pos += k
+    return bt, n
+
+
+def _run(dev, g, lo, pool, bt, sl, q, kind, io, scale, Dv=0, sinks=0, ks=1.0, vs=1.0, T=-1, layer=0, stream=None,
+         out_order="rh", flags=0, batch_window=None):
+    """One call; returns out float64 and lse, with guard rows around out checked."""
+    R, Hq, D = q.shape
+    dv = Dv or D
+    d_q = torch.from_numpy(q).to(dev).to(TORCH[io])
+    if out_order == "rh":
+        whole = torch.full((R + 2, Hq, dv), 7.0, dtype=TORCH[io], device=dev)
+        out = whole[1:R + 1]
+    else:
+        whole = torch.full((Hq + 2, R, dv), 7.0, dtype=TORCH[io], device=dev)
+        out = whole[1:Hq + 1].transpose(0, 1)
+    lse = torch.full((R, Hq), 3.0, device=dev)
+    b = tk.make_batch(torch.from_numpy(np.ascontiguousarray(bt)).to(dev), torch.from_numpy(np.asarray(sl, np.int32)).to(dev), T,
+                      window_tokens=g.window if batch_window is None else batch_window, flags=flags)
+    att = tk.make_attention(d_q, out, TYPE[kind], TYPE[io], scale, value_dim=Dv, sink_tokens=sinks, k_scale=ks,
+                            v_scale=vs, lse=lse)
+    n = tk.check(tk.topkv_attend_workspace_bytes(lo, b, att))
+    ws = torch.full((n + 32,), 0xFF, dtype=torch.uint8, device=dev)           # NaN patterns: nothing is assumed
+    torch.cuda.synchronize()
+    tk.check(tk.topkv_attend_layer(layer, pool, lo, b, att, d_q, out, ws, n, stream))
+    torch.cuda.synchronize()
+    assert (whole[0] == 7).all() and (whole[-1] == 7).all() and (ws[n:] == 0xFF).all()
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+def _cache(g, bt, sl, kind, sinks, rng, layer=0):
+    """A pool of NaN patterns in which only what the new tokens see holds numbers."""
+    pool = np.empty(g.L * g.S_layer, dtype=np.uint8)
+    pool[0::2], pool[1::2] = NAN[kind]
+    n = g.d_h * g.b_p
+    for r, s in enumerate(sl):
+        for i in od.visible(int(s), g.window, sinks):
+            for c in range(g.F):
+                for h in range(g.h_kv):
+                    a = od.row_offset(g, layer, int(bt[r, i // g.P]), c, int(i % g.P), h)
+                    pool[a:a + n] = od.encode_elements(rng.normal(size=g.d_h), kind)
+    return pool
+
+
+def _check(got, want):
+    out, lse = got
+    ref, ref_lse, tol, tol_lse = want
+    assert np.isfinite(out).all()
+    bad = np.abs(out - ref) > tol
+    assert not bad.any(), (np.argwhere(bad)[:5], out[bad][:5], ref[bad][:5], tol[bad][:5])
+    empty = ref_lse == -np.inf
+    assert (lse[empty] == -np.inf).all() and (out[empty] == 0).all()
+    assert (np.abs(lse - ref_lse)[~empty] <= tol_lse[~empty]).all()
+
+
+def _case(dev, F, H, G, D, P, sl, kind="bf16", io=None, Dv=0, window=0, sinks=0, style="page", seed=0, layer=0, L=1,
+          extra_cols=1, ks=1.0, vs=1.0, **kw):
+    rng = np.random.default_rng(seed)
+    io = io or (kind if kind != "e4m3" else "bf16")
+    bt, pages = _table(sl, P, 2, extra_cols, rng)
+    g = _geom(F, H, D, 1 if kind == "e4m3" else 2, P, pages, style, L, window)
+    pool_h = _cache(g, bt, sl, kind, sinks, rng, layer)
+    pool = torch.from_numpy(pool_h).to(dev)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=(len(sl), H * G, D)).reshape(-1), io), io).reshape(len(sl), H * G, D)
+    scale = D ** -0.5
+    got = _run(dev, g, _layout(g), pool, bt, sl, q, kind, io, scale, Dv, sinks, ks, vs, layer=layer, **kw)
+    _check(got, od.attend(g, layer, pool_h, bt, sl, q, kind, io, scale, Dv, sinks, ks, vs))
+    assert np.array_equal(pool.cpu().numpy(), pool_h)
+    return got
+
+
+# ------------------------------------------------------------------------- grouped heads
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "e4m3"])
+@pytest.mark.parametrize("D", [16, 64, 80, 128, 192, 256])
+def test_attend_head_dims_and_types(dev, kind, D):
+    _case(dev, 2, 2, 4, D, 16, [1, 17, 64, 130], kind, ks=0.5 if kind == "e4m3" else 1.0, vs=2.0 if kind == "e4m3" else 1.0)
+
+
+@pytest.mark.parametrize("sl", [[1], [0, 5, 0], [16, 15, 33, 64, 65], [255, 256], [0, 0], [257, 3, 900, 0, 64]])
+def test_attend_lengths(dev, sl):
+    _case(dev, 2, 2, 3, 64, 16, sl, seed=len(sl))
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (1, 16), (1, 17), (3, 5), (8, 8), (2, 40), (16, 1), (5, 7)])
+def test_attend_head_layouts(dev, H, G):
+    _case(dev, 2, H, G, 64, 16, [70, 1, 333], seed=H * 100 + G)
+
+
+@pytest.mark.parametrize("style", ["page", "padded", "head", "plane"])
+@pytest.mark.parametrize("P", [1, 3, 16, 48, 512])
+def test_attend_pools_and_pages(dev, style, P):
+    _case(dev, 2, 2, 2, 72, P, [100, 500, 7], "fp16", style=style, seed=P, layer=1, L=2)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (64, 0), (100, 5), (128, 128), (300, 4), (5000, 3)])
+def test_attend_window_and_sinks(dev, window, sinks):
+    _case(dev, 2, 2, 4, 64, 16, [1, 2, 16, 64, 120, 257, 700, 0], "fp16", window=window, sinks=sinks, seed=window)
+
+
+@pytest.mark.parametrize("kind,io", [("e4m3", "bf16"), ("e4m3", "fp16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("H,sl", [(1, [4000]), (2, [3000, 17, 999, 2048]), (8, [1500, 1, 0, 400])])
+def test_attend_split_requests(dev, kind, io, H, sl):
+    """Lengths that are cut between CTAs, from one request over all of them to several in one."""
+    _case(dev, 2, H, 2, 64, 16, sl, kind, io, seed=sum(sl))
+
+
+def test_attend_many_requests(dev):
+    """More requests than threads look at, most of them short, a long one in the middle; the
+    cut and the uncut way of sharing out the work give results within the same bound."""
+    rng = np.random.default_rng(1)
+    sl = rng.integers(0, 40, size=1500)
+    sl[700] = 600
+    _case(dev, 2, 1, 2, 16, 16, sl, "fp16", seed=9)
+    _case(dev, 2, 1, 2, 16, 16, np.minimum(sl, 60), "fp16", seed=9)
+
+
+def test_attend_same_bits_every_time_and_out_layouts(dev):
+    kw = dict(kind="bf16", seed=4)
+    a = _case(dev, 2, 2, 4, 128, 16, [2000, 30, 700], **kw)
+    b = _case(dev, 2, 2, 4, 128, 16, [2000, 30, 700], out_order="hr", stream=torch.cuda.Stream(dev), **kw)
+    c = _case(dev, 2, 2, 4, 128, 16, [2000, 30, 700], T=2730, flags=tk.TOPKV_FLAG_TABLES_SETTLED, **kw)
+    for x in (b, c):
+        assert np.array_equal(a[0], x[0]) and np.array_equal(a[1], x[1])
+
+
+def _values_case(dev, k_rows, v_rows, q, kind="fp16", **kw):
+    """One request, one head, D = 8 columns used of 16: explicit K, V and q."""
+    n, D = len(k_rows), 16
+    bt, pages = _table([n], 16, 1, 0, np.random.default_rng(3))
+    g = _geom(2, 1, D, 2, 16, pages)
+    pool = np.zeros(g.pool_bytes(), np.uint8)
+    for i in range(n):
+        for c, rows in ((0, k_rows), (1, v_rows)):
+            a = od.row_offset(g, 0, int(bt[0, i // 16]), c, i % 16, 0)
+            row = np.zeros(D)
+            row[:len(rows[i])] = rows[i]
+            pool[a:a + 2 * D] = od.encode_elements(row, kind)
+    qq = np.zeros((1, 1, D))
+    qq[0, 0, :len(q)] = q
+    return g, pool, bt, [n], qq, _run(dev, g, _layout(g), torch.from_numpy(pool).to(dev), bt, [n], qq, kind, kind, 1.0, **kw)
+
+
+def test_attend_extreme_values(dev):
+    # one token far above many others whose weights are far below the largest: they still count
+    n = 6000
+    k = np.zeros((n, 1)); k[17] = 16.0
+    v = np.ones((n, 1)); v[17] = 0.0
+    g, pool, bt, sl, q, got = _values_case(dev, k, v, [1.0])
+    _check(got, od.attend(g, 0, pool, bt, sl, q, "fp16", "fp16", 1.0))
+    # the type's lowest value as a key, one token and all of them
+    for n, rows in ((70, [3]), (70, range(70))):
+        k = np.full((n, 1), 0.25)
+        k[list(rows)] = -65504.0
+        g, pool, bt, sl, q, got = _values_case(dev, k, np.arange(n)[:, None] / 8, [2.0])
+        _check(got, od.attend(g, 0, pool, bt, sl, q, "fp16", "fp16", 1.0))
+    # infinities and NaN in visible places act as in the formula
+    k = np.full((70, 1), 0.25); k[5] = -np.inf
+    *_, (out, lse) = _values_case(dev, k, np.ones((70, 1)), [2.0])
+    assert abs(out[0, 0, 0] - 1) < 1e-3 and abs(lse[0, 0] - (0.5 + np.log(69))) < 1e-5
+    k = np.full((70, 1), -np.inf)
+    *_, (out, lse) = _values_case(dev, k, np.ones((70, 1)), [2.0])
+    assert np.isnan(out[0, 0, 0])
+    for bad in (np.inf, np.nan):
+        k = np.zeros((400, 1)); k[333] = bad
+        *_, (out, lse) = _values_case(dev, k, np.ones((400, 1)), [2.0])
+        assert np.isnan(out[0, 0, 0]) and np.isnan(lse[0, 0])
+        v = np.zeros((400, 1)); v[2] = bad
+        *_, (out, lse) = _values_case(dev, np.zeros((400, 1)), v, [2.0])
+        assert not np.isfinite(out[0, 0, 0]) and abs(lse[0, 0] - np.log(400)) < 1e-5
+
+
+@pytest.mark.parametrize("big", [1e-30, 1e30])
+def test_attend_8bit_cache_with_queries_beyond_fp16(dev, big):
+    """bf16 queries of any magnitude over an 8-bit cache."""
+    rng = np.random.default_rng(5)
+    bt, pages = _table([90], 16, 1, 0, rng)
+    g = _geom(2, 1, 64, 1, 16, pages)
+    pool = _cache(g, bt, [90], "e4m3", 0, rng)
+    q = rng.normal(size=(1, 3, 64)) * big
+    q[0, 2] = 0
+    q = od.decode_elements(od.encode_elements(q.reshape(-1), "bf16"), "bf16").reshape(q.shape)
+    got = _run(dev, g, _layout(g), torch.from_numpy(pool).to(dev), bt, [90], q, "e4m3", "bf16", 0.1 / big)
+    _check(got, od.attend(g, 0, pool, bt, [90], q, "e4m3", "bf16", 0.1 / big))
+
+
+def test_attend_unusable_tables(dev):
+    """Page ids outside the pool are skipped, lengths outside the row cut; both raise bit 2."""
+    rng = np.random.default_rng(6)
+    sl = [90, 40]
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(2, 1, 64, 2, 16, pages)
+    pool_h = _cache(g, bt, sl, "bf16", 0, rng)
+    pool = torch.from_numpy(pool_h).to(dev)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=2 * 64), "bf16"), "bf16").reshape(2, 1, 64)
+    for bad in (pages, -1, 1 << 30):
+        broken = bt.copy()
+        broken[0, 2] = bad
+        out, lse = _run(dev, g, _layout(g), pool, broken, sl, q, "bf16", "bf16", 0.125)
+        assert tk.topkv_device_error_flags() == 2
+        tk.check(tk.topkv_reset_device_error_flags())
+        rows = [i for i in range(90) if i // 16 != 2]           # what is left of request 0
+        k, v = (od.rows_of(g, 0, pool_h, bt[0], np.array(rows), c, 0, "bf16") for c in (0, 1))
+        w = np.exp(0.125 * k @ q[0, 0])
+        assert np.abs(out[0, 0] - w @ v / w.sum()).max() < 2.0 ** -6 and abs(lse[0, 0] - np.log(w.sum())) < 1e-4
+    out, lse = _run(dev, g, _layout(g), pool, bt[:, :3], [48, 1000], q, "bf16", "bf16", 0.125)
+    assert tk.topkv_device_error_flags() == 2 and np.isfinite(lse).sum() >= 1
+    tk.check(tk.topkv_reset_device_error_flags())
+    out, lse = _run(dev, g, _layout(g), pool, bt, [90, -3], q, "bf16", "bf16", 0.125)
+    assert tk.topkv_device_error_flags() == 2 and lse[1, 0] == -np.inf and (out[1] == 0).all()
+    tk.check(tk.topkv_reset_device_error_flags())
+
+
+def test_attend_rows_past_two_gigabytes(dev):
+    """Offsets beyond 32 bits: the pages in use lie at the end of a 6 GiB pool."""
+    g = _geom(2, 8, 128, 2, 16, 6 * (1 << 30) // 65536)
+    pool = torch.zeros(g.pool_bytes(), dtype=torch.uint8, device=dev)
+    rng = np.random.default_rng(8)
+    sl = [40, 300]
+    bt = np.full((2, 20), -1, np.int32)
+    bt[0, :3] = [g.num_pages - 1, 5, g.num_pages - 7]
+    bt[1, :19] = g.num_pages - 100 + np.arange(19)
+    want = {}
+    for p in {int(x) for x in bt.reshape(-1) if x >= 0}:
+        want[p] = od.encode_elements(rng.normal(size=32768), "bf16")
+        pool[p * 65536:(p + 1) * 65536] = torch.from_numpy(want[p]).to(dev)
+    small = _geom(2, 8, 128, 2, 16, len(want))
+    order = {p: i for i, p in enumerate(want)}
+    pool_h = np.concatenate(list(want.values()))
+    bt_h = np.array([[order.get(int(x), -1) for x in row] for row in bt], np.int32)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=2 * 16 * 128), "bf16"), "bf16").reshape(2, 16, 128)
+    got = _run(dev, g, _layout(g), pool, bt, sl, q, "bf16", "bf16", 0.09)
+    _check(got, od.attend(small, 0, pool_h, bt_h, sl, q, "bf16", "bf16", 0.09))
+
+
+def test_attend_in_a_graph_and_on_two_streams(dev):
+    """Captured and replayed with other contents; two calls at the same time with a workspace each."""
+    rng = np.random.default_rng(11)
+    sl = [1500, 40]
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(2, 2, 64, 2, 16, pages)
+    lo = _layout(g)
+    pool = torch.zeros(g.pool_bytes(), dtype=torch.uint8, device=dev)
+    b = tk.make_batch(torch.from_numpy(bt).to(dev), torch.tensor(sl, dtype=torch.int32, device=dev))
+    q = torch.zeros(2, 8, 64, dtype=torch.bfloat16, device=dev)
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    lses = [torch.zeros(2, 8, device=dev) for _ in range(2)]
+    T = tk.TOPKV_TYPE_BF16
+    atts = [tk.make_attention(q, o, T, T, 0.125, lse=l) for o, l in zip(outs, lses)]
+    n = tk.check(tk.topkv_attend_workspace_bytes(lo, b, atts[0]))
+    assert n > 0
+    ws = [torch.empty(n, dtype=torch.uint8, device=dev) for _ in range(2)]
+    call = lambda i, s: tk.check(tk.topkv_attend_layer(0, pool, lo, b, atts[i], q, outs[i], ws[i], n, s))
+    call(0, torch.cuda.current_stream())                      # shared-memory limit raised outside the capture
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(dev)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(0, torch.cuda.current_stream())
+    for seed in (1, 2):
+        r2 = np.random.default_rng(seed)
+        pool_h = _cache(g, bt, sl, "bf16", 0, r2)
+        pool.copy_(torch.from_numpy(pool_h))
+        q_h = od.decode_elements(od.encode_elements(r2.normal(size=2 * 8 * 64), "bf16"), "bf16").reshape(2, 8, 64)
+        q.copy_(torch.from_numpy(q_h).to(torch.bfloat16))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            graph.replay()
+            call(1, side)
+        torch.cuda.synchronize()
+        want = od.attend(g, 0, pool_h, bt, sl, q_h, "bf16", "bf16", 0.125)
+        for o, l in zip(outs, lses):
+            _check((o.double().cpu().numpy(), l.double().cpu().numpy()), want)
+
+
+# ------------------------------------------------------------------------- page operators
+
+def _page_case(seed, L=2, F=2, H=2, D=8, E=2, P=4, R=7, style="page", spare=5, maxlen=20):
+    rng = np.random.default_rng(seed)
+    sl = rng.integers(0, maxlen + 1, size=R).astype(np.int32)
+    bt, pages = _table(sl, P, spare, 2, rng)
+    g = _geom(F, H, D, E, P, pages, style, L)
+    ref = np.zeros(pages, np.int32)
+    for p in bt[bt >= 0]:
+        ref[p] += 1
+    pool = rng.integers(0, 256, g.L * g.S_layer, dtype=np.uint8)
+    return rng, g, sl, bt, ref, pool
+
+
+class _State:
+    """Device copies of the tables and the pool, an out set apart or in place."""
+
+    def __init__(self, dev, g, sl, bt, ref, pool, in_place, skew=0):
+        self.g, self.lo = g, _layout(g)
+        put = lambda x: torch.from_numpy(np.ascontiguousarray(x).copy()).to(dev)
+        buf = torch.zeros(len(pool) + skew, dtype=torch.uint8, device=dev)
+        self.pool = buf[skew:]
+        self.pool.copy_(put(pool))
+        self.first = (put(bt), put(sl), put(ref))
+        self.out = self.first if in_place else tuple(torch.full_like(x, -77) for x in self.first)
+        self.batch = tk.make_batch(self.first[0], self.first[1])
+        self.tables = tk.make_page_tables(self.first[2], *self.out)
+        self.put = put
+        n = tk.check(tk.topkv_page_workspace_bytes(self.lo, self.batch, 64))
+        self.ws = torch.full((n,), 0x55, dtype=torch.uint8, device=dev)
+        self.n = n
+
+    def check(self, bt, sl, ref, pool, err):
+        torch.cuda.synchronize()
+        assert tk.topkv_device_error_flags() == err
+        tk.check(tk.topkv_reset_device_error_flags())
+        for got, want in zip(self.out, (bt, sl, ref)):
+            assert np.array_equal(got.cpu().numpy(), want)
+        assert np.array_equal(self.pool.cpu().numpy(), pool)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("seed", range(6))
+def test_extend(dev, seed, in_place):
+    rng, g, sl, bt, ref, pool = _page_case(seed, spare=[5, 0, 3, 40, 6, 2][seed], P=[4, 1, 16, 3, 4, 8][seed])
+    s = _State(dev, g, sl, bt, ref, pool, in_place)
+    new = rng.integers(0, 6, size=len(sl)).astype(np.int32)
+    if seed == 4:
+        new[2], new[5] = -1, 1 << 30
+    d_new = s.put(new)
+    tk.check(tk.topkv_extend_requests(s.lo, s.batch, s.tables, d_new, s.ws, s.n))
+    err = od.extend_requests(g.P, bt, sl, ref, new)
+    s.check(bt, sl, ref, pool, err)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("seed", range(4))
+def test_free(dev, seed, in_place):
+    rng, g, sl, bt, ref, pool = _page_case(seed, R=9)
+    ref[bt[0, 0]] += 2                                       # a page that others use too
+    if seed == 3:
+        ref[bt[1, 0]] = 0                                    # a count that is wrong already
+        bt[2, 0], sl[2] = len(ref), max(int(sl[2]), 1)
+        sl[3] = bt.shape[1] * g.P + 1
+    s = _State(dev, g, sl, bt, ref, pool, in_place)
+    rows = np.array([3, 0, 3, 1, 2] if seed != 1 else [0, 9, -1, 0], np.int32)
+    tk.check(tk.topkv_free_requests(s.lo, s.batch, s.tables, s.put(rows), len(rows)))
+    err = od.free_requests(g.P, bt, sl, ref, rows)
+    s.check(bt, sl, ref, pool, err)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("style,E,P,skew", [("page", 2, 4, 0), ("padded", 2, 4, 0), ("head", 2, 5, 16), ("plane", 2, 1, 0),
+                                            ("page", 2, 200, 16)])
+def test_fork(dev, style, E, P, skew, in_place):
+    for seed in range(3):
+        rng, g, sl, bt, ref, pool = _page_case(seed, E=E, P=P, R=9, style=style, D=64 if P == 200 else 8, maxlen=5 * P,
+                                               spare=[4, 2, 0][seed])
+        sl[[1, 4, 6]], kept = 0, bt.copy()
+        for r in (1, 4, 6):
+            for p in kept[r][kept[r] >= 0]:
+                ref[p] -= 1
+            bt[r] = -1
+        ref[bt[0][bt[0] >= 0]] += seed                       # shared already
+        s = _State(dev, g, sl, bt, ref, pool, in_place, skew)
+        parents = np.array([0, 0, 2, 0, 3, 5, 20], np.int32)
+        children = np.array([4, 1, 4, 6, 3, -1, 6], np.int32)  # a row named twice, itself, outside
+        if seed == 0:
+            parents, children = parents[:2], children[:2]
+        tk.check(tk.topkv_fork_requests(s.pool, s.lo, s.batch, s.tables, s.put(parents), s.put(children), len(parents),
+                                        s.ws, s.n))
+        err = od.fork_requests(g, pool, bt, sl, ref, parents, children)
+        s.check(bt, sl, ref, pool, err)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("style,P,skew,pages", [("page", 4, 0, 5), ("padded", 4, 0, 60), ("head", 3, 16, 9), ("plane", 16, 0, 5),
+                                                ("page", 1, 0, 9000)])
+def test_compact(dev, style, P, skew, pages, in_place):
+    for seed in range(3):
+        rng, g, sl, bt, ref, pool = _page_case(seed, P=P, R=8, style=style, spare=pages, L=1 if pages > 1000 else 2, maxlen=9 * P)
+        ref[bt[3][bt[3] >= 0]] -= 1                          # a request that ended
+        bt[3], sl[3] = -1, 0
+        ref[rng.integers(0, len(ref), size=3)] += 2          # pages that somebody holds outside the table
+        if seed == 2 and sl[5] > 0:
+            bt[5, 0] = len(ref) + 3
+        s = _State(dev, g, sl, bt, ref, pool, in_place, skew)
+        used = torch.full((1,), -5, dtype=torch.int32, device=dev)
+        to = torch.full((g.num_pages,), -5, dtype=torch.int32, device=dev)
+        tk.check(tk.topkv_compact_pages(s.pool, s.lo, s.batch, s.tables, used, to, s.ws, s.n))
+        err, n, want_to = od.compact_pages(g, pool, bt, sl, ref)
+        s.check(bt, sl, ref, pool, err)
+        assert used.item() == n and np.array_equal(to.cpu().numpy(), want_to)
+        ids = np.flatnonzero(ref > 0)
+        assert np.array_equal(ids, np.arange(n))
+
+
+def test_compact_without_requests_and_when_there_is_nothing_to_do(dev):
+    _, g, sl, bt, ref, pool = _page_case(3)
+    ref[:] = 0
+    ref[[2, 3, len(ref) - 1]] = 4
+    lo = _layout(g)
+    d = torch.from_numpy(pool).to(dev)
+    d_ref = torch.from_numpy(ref.copy()).to(dev)
+    empty = torch.empty((0, 4), dtype=torch.int32, device=dev)
+    none = torch.empty((0,), dtype=torch.int32, device=dev)
+    b, t = tk.make_batch(empty, none), tk.make_page_tables(d_ref, empty, none, d_ref)
+    n = tk.check(tk.topkv_page_workspace_bytes(lo, b, 0))
+    ws, used = torch.empty(n, dtype=torch.uint8, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    to = torch.zeros(len(ref), dtype=torch.int32, device=dev)
+    bt0, sl0 = np.zeros((0, 4), np.int32), np.zeros(0, np.int32)
+    for _ in range(2):                                       # the second time nothing moves
+        tk.check(tk.topkv_compact_pages(d, lo, b, t, used, to, ws, n))
+        _, want, want_to = od.compact_pages(g, pool, bt0, sl0, ref)
+        assert used.item() == want == 3 and np.array_equal(to.cpu().numpy(), want_to)
+        assert np.array_equal(d_ref.cpu().numpy(), ref) and np.array_equal(d.cpu().numpy(), pool)
+
+
+@pytest.mark.parametrize("style,P,D,skew", [("page", 4, 8, 0), ("padded", 4, 8, 16), ("head", 3, 16, 0), ("plane", 1, 64, 0),
+                                            ("page", 300, 64, 0), ("padded", 130, 64, 0)])
+def test_copy_pages(dev, style, P, D, skew):
+    rng, g, sl, bt, ref, pool = _page_case(1, P=P, D=D, L=3, style=style, spare=12)
+    ids = rng.permutation(g.num_pages)[:9].astype(np.int32)
+    src, dst = ids[:4].copy(), ids[4:8].copy()
+    buf = torch.zeros(len(pool) + skew, dtype=torch.uint8, device=dev)
+    d = buf[skew:]
+    d.copy_(torch.from_numpy(pool))
+    lo = _layout(g)
+    put = lambda x: torch.from_numpy(x).to(dev)
+    tk.check(tk.topkv_copy_pages(1, 2, d, lo, put(src), put(dst), 4))
+    od.copy_pages(g, pool, 1, 2, src, dst)
+    assert np.array_equal(d.cpu().numpy(), pool)
+    # unusable entries are skipped, a page onto itself is left alone
+    src = np.array([ids[0], -1, ids[8], ids[1]], np.int32)
+    dst = np.array([g.num_pages, ids[2], ids[8], ids[3]], np.int32)
+    tk.check(tk.topkv_copy_pages(0, 1, d, lo, put(src), put(dst), 4))
+    assert od.copy_pages(g, pool, 0, 1, src, dst) == 2 == tk.topkv_device_error_flags()
+    tk.check(tk.topkv_reset_device_error_flags())
+    assert np.array_equal(d.cpu().numpy(), pool)
+
+
+def test_a_random_run_of_page_operators(dev):
+    """Thirty calls in a row, in place, against the oracle's loops; then a compaction."""
+    rng, g, sl, bt, ref, pool = _page_case(21, R=12, P=4, spare=40, maxlen=16)
+    s = _State(dev, g, sl, bt, ref, pool, True)
+    err = 0
+    for _ in range(30):
+        op = rng.integers(0, 3)
+        if op == 0:
+            new = rng.integers(0, 4, size=12).astype(np.int32)
+            new[sl == 0] = 0
+            tk.check(tk.topkv_extend_requests(s.lo, s.batch, s.tables, s.put(new), s.ws, s.n))
+            err |= od.extend_requests(g.P, bt, sl, ref, new)
+        elif op == 1:
+            rows = rng.integers(0, 12, size=3).astype(np.int32)
+            tk.check(tk.topkv_free_requests(s.lo, s.batch, s.tables, s.put(rows), 3))
+            err |= od.free_requests(g.P, bt, sl, ref, rows)
+        else:
+            parents, children = rng.integers(0, 12, size=4).astype(np.int32), rng.integers(0, 12, size=4).astype(np.int32)
+            tk.check(tk.topkv_fork_requests(s.pool, s.lo, s.batch, s.tables, s.put(parents), s.put(children), 4, s.ws, s.n))
+            err |= od.fork_requests(g, pool, bt, sl, ref, parents, children)
+    used, to = torch.zeros(1, dtype=torch.int32, device=dev), torch.zeros(g.num_pages, dtype=torch.int32, device=dev)
+    tk.check(tk.topkv_compact_pages(s.pool, s.lo, s.batch, s.tables, used, to, s.ws, s.n))
+    err |= od.compact_pages(g, pool, bt, sl, ref)[0]
+    counts = np.zeros_like(ref)
+    for r in range(12):
+        np.add.at(counts, bt[r, :-(-int(sl[r]) // g.P)], 1)
+    assert np.array_equal(counts, ref)                       # the counts are the table's
+    s.check(bt, sl, ref, pool, err)
