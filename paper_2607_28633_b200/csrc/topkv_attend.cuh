@@ -56,7 +56,7 @@ struct AttendParams {
   int64_t q_req, q_head, o_req, o_head;  // bytes
   int64_t num_pages;
   int R, maxp, P;
-  int H, G, gtiles;     // KV heads, query heads per KV head, groups of 16 query heads per KV head
+  int H, G, gtiles;     // KV heads, query heads per KV head, groups of row_tile query heads per KV head
   int D, Dv;            // elements
   int window, sinks;
   float qk_scale;       // scale * k_scale * log2(e): scores are kept in powers of two
@@ -65,7 +65,8 @@ struct AttendParams {
   int teams;            // CTAs along x; 0 tiles of a request cross a team when uncut
   int uncut;            // 1: team t is request t
   int late_wait;        // tables are settled
-  int rows;             // rows of a partial result, min(G, 16)
+  int rows;             // rows of a partial result, min(G, row_tile)
+  int row_tile;         // query heads per CTA
   // workspace
   int2* cuts;           // [teams]: the request that the team's range begins inside of, or -1; and whether that
                         // request begins behind the start of the range before (its part there is slot 1)
@@ -91,6 +92,77 @@ __device__ __forceinline__ Visible visible_tokens(const AttendParams& p, int r, 
   return v;
 }
 __device__ __forceinline__ int attend_tiles(int n) { return n / kTileTokens + (n % kTileTokens != 0); }
+
+// Which tiles are a team's. The tiles of all requests, laid end to end, are cut into equal ranges;
+// in an uncut launch team t takes request t. Every CTA works it out from the lengths.
+struct TeamRange {
+  int r, t0;      // first request, and the tile in it to begin with
+  int64_t left;   // tiles (uncut: 1, the request)
+  int cut;        // the range begins inside the request
+  int cut_slot;   // ... which begins behind the start of the range before
+};
+struct TeamStart {
+  int64_t scan[16];
+  int r, t0;
+};
+template <int THREADS>
+__device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team, TeamStart* s) {
+  TeamRange out = {team, 0, 1, 0, 0};
+  if (p.uncut) return out;
+  constexpr int kWarps = THREADS / 32;
+  static_assert(kWarps <= 16, "scan holds 16 warps");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (p.R + THREADS - 1) / THREADS;
+  const int r0 = (int)min((int64_t)tid * per, (int64_t)p.R), r1 = min(r0 + per, p.R);
+  int64_t mine = 0;
+  for (int i = r0; i < r1; ++i) mine += attend_tiles(visible_tokens(p, i, false).n);
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) s->scan[warp] = incl;
+  if (tid == 0) s->r = -1;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) incl += s->scan[w];
+    total += s->scan[w];
+  }
+  const int teams = (int)min((int64_t)p.teams, total);  // no team between two others is without tiles
+  int64_t a = 0, b = 0, prev = 0;
+  if (team < teams) {
+    a = total * team / teams;
+    b = total * (team + 1) / teams;
+    prev = team > 0 ? total * (team - 1) / teams : 0;
+  }
+  if (a < b && a >= incl - mine && a < incl) {  // exactly one thread
+    int64_t at = incl - mine;
+    for (int i = r0; i < r1; ++i) {
+      const int n = attend_tiles(visible_tokens(p, i, false).n);
+      if (a < at + n) {
+        s->r = i;
+        s->t0 = (int)(a - at);
+        break;
+      }
+      at += n;
+    }
+  }
+  __syncthreads();
+  out.r = s->r;
+  out.t0 = s->t0;
+  out.left = out.r < 0 ? 0 : b - a;
+  out.cut = out.left > 0 && out.t0 > 0;
+  out.cut_slot = a - out.t0 > prev;
+  return out;
+}
+// What the joining kernel needs to know of the range's start. Behind the wait for earlier kernels:
+// the join of the call before may still read the workspace until then.
+__device__ __forceinline__ void note_cut(const AttendParams& p, int team, const TeamRange& t) {
+  if (!p.uncut) p.cuts[team] = t.cut ? make_int2(t.r, t.cut_slot) : make_int2(-1, 0);
+}
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
   const int n = valid ? 16 : 0;  // 0: nothing is read, the 16 bytes become zero
@@ -134,16 +206,6 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
   }
 }
-// Two 8-bit values (low 16 bits) to two fp16 values; exact.
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
-  uint32_t r;
-  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(v));
-  return r;
-}
-__device__ __forceinline__ float load_io(const uint8_t* p, bool bf16) {
-  return bf16 ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(p))
-              : __half2float(*reinterpret_cast<const __half*>(p));
-}
 __device__ __forceinline__ void store_io(uint8_t* p, float v, bool bf16) {
   if (bf16)
     *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v);
@@ -151,6 +213,25 @@ __device__ __forceinline__ void store_io(uint8_t* p, float v, bool bf16) {
     *reinterpret_cast<__half*>(p) = __float2half_rn(v);
 }
 
+// Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0.
+template <int THREADS>
+__device__ __forceinline__ void empty_requests(const AttendParams& p, int team, int64_t head0, int rows, bool complain) {
+  for (int e = team; e < p.R; e += p.teams) {
+    if (visible_tokens(p, e, complain && threadIdx.x == 0).n > 0) continue;
+    for (int i = threadIdx.x; i < rows * p.Dv; i += THREADS) {
+      const int g = i / p.Dv, d = i - g * p.Dv;
+      store_io(p.out + e * p.o_req + (head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
+    }
+    if (p.lse != nullptr)
+      for (int g = threadIdx.x; g < rows; g += THREADS) p.lse[(int64_t)e * p.H * p.G + head0 + g] = -INFINITY;
+  }
+}
+// Two 8-bit values (low 16 bits) to two fp16 values; exact.
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
+  uint32_t r;
+  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(v));
+  return r;
+}
 // Shared memory: per warp a ring of stages, each 16 rows of K and 16 rows of V of DP elements.
 // Rows are swizzled in 16-byte chunks so that the eight rows of a matrix load hit all banks.
 template <int DP, int TYPE>
@@ -175,8 +256,7 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
   constexpr float kShift = kMmaBf16 ? 0.f : 15.f;
   constexpr int kSteps = DP / 16;  // k-steps of the first product, pairs of n-tiles of the second
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t s_scan[kAttendWarps];
-  __shared__ int s_start[2];
+  __shared__ TeamStart s_team;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
@@ -185,67 +265,12 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
   if (!p.late_wait) pdl_wait_prior_grid();
   pdl_release_next_grid();
 
-  // ---- which tiles are this team's: [a, b) of all requests' tiles laid end to end -------------
-  int64_t a = 0, b = 0, prev = 0;
-  int r = team, t0 = 0;  // first request, and the tile in it to begin with
-  if (!p.uncut) {
-    const int per = (p.R + kAttendThreads - 1) / kAttendThreads;
-    const int r0 = min(tid * per, p.R), r1 = min(r0 + per, p.R);
-    int64_t mine = 0;
-    for (int i = r0; i < r1; ++i) mine += attend_tiles(visible_tokens(p, i, false).n);
-    int64_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
-    }
-    if (lane == 31) s_scan[warp] = incl;
-    if (tid == 0) s_start[0] = -1;
-    __syncthreads();
-    int64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < kAttendWarps; ++w) {
-      if (w < warp) incl += s_scan[w];
-      total += s_scan[w];
-    }
-    const int teams = (int)min((int64_t)p.teams, total);  // no team between two others is without tiles
-    if (team < teams) {
-      a = total * team / teams;
-      b = total * (team + 1) / teams;
-      prev = team > 0 ? total * (team - 1) / teams : 0;
-    }
-    if (a < b && a >= incl - mine && a < incl) {  // exactly one thread
-      int64_t at = incl - mine;
-      for (int i = r0; i < r1; ++i) {
-        const int n = attend_tiles(visible_tokens(p, i, false).n);
-        if (a < at + n) {
-          s_start[0] = i;
-          s_start[1] = (int)(a - at);
-          break;
-        }
-        at += n;
-      }
-    }
-    __syncthreads();
-    r = s_start[0];
-    t0 = s_start[1];
-  }
+  const TeamRange mine = team_range<kAttendThreads>(p, team, &s_team);
   if (p.late_wait) pdl_wait_prior_grid();
-  if (!p.uncut && unit == 0 && tid == 0)
-    p.cuts[team] = a < b && t0 > 0 ? make_int2(r, a - t0 > prev) : make_int2(-1, 0);
-
+  if (unit == 0 && tid == 0) note_cut(p, team, mine);
   const int64_t q_head0 = (int64_t)h * p.G + g0;
-  // requests with nothing to see: zeros, and a log-sum-exp of minus infinity
-  for (int e = team; e < p.R; e += p.teams) {
-    if (visible_tokens(p, e, unit == 0 && tid == 0).n > 0) continue;
-    for (int i = tid; i < rows * p.Dv; i += kAttendThreads) {
-      const int g = i / p.Dv, d = i - g * p.Dv;
-      store_io(p.out + e * p.o_req + (q_head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
-    }
-    if (p.lse != nullptr && tid < rows)
-      p.lse[(int64_t)e * p.H * p.G + q_head0 + tid] = -INFINITY;
-  }
-  if (!p.uncut && a >= b) return;
+  empty_requests<kAttendThreads>(p, team, q_head0, rows, unit == 0);
+  if (mine.left == 0) return;
 
   uint8_t* ring = smem + warp * S::kStages * S::kStage;
   const uint32_t ring_a = smem_addr(ring);
@@ -256,7 +281,8 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
   }
   const int chunks = p.D * S::kElem / 16;
   const uint8_t* k_base = p.pool + (int64_t)h * p.S_head;
-  int64_t left = p.uncut ? 1 : b - a;
+  int64_t left = mine.left;
+  int r = mine.r, t0 = mine.t0;
   const int gr = lane >> 2, gc = lane & 3;  // row and column group of this thread in a matrix fragment
 
   for (bool first = true; left > 0 && r < p.R; first = false, t0 = 0, ++r) {
@@ -553,8 +579,8 @@ __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const A
     if (n < kJoinThreads) break;
   }
   const int r = cut.x, units = gridDim.y;
-  const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * kAttendRows;
-  const int rows = min(p.G - g0, kAttendRows);
+  const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * p.row_tile;
+  const int rows = min(p.G - g0, p.row_tile);
   const int64_t q_head0 = (int64_t)h * p.G + g0;
   for (int i = blockIdx.z * kJoinThreads + threadIdx.x; i < rows * p.Dv; i += kJoinThreads * gridDim.z) {
     const int g = i / p.Dv, d = i - g * p.Dv;

@@ -2,6 +2,7 @@
 // operators. Included by topkv.cu, whose argument checks, launch counter and error state it shares.
 #pragma once
 #include "topkv_attend.cuh"
+#include "topkv_latent.cuh"
 #include "topkv_pages.cuh"
 
 namespace {
@@ -58,6 +59,7 @@ constexpr int kAttendCtas = 2 * 148;  // CTAs that are resident together (two pe
 
 struct AttendPlan {
   int units;        // CTAs per team
+  int row_tile;     // query heads per CTA
   int rows;         // rows of a partial result
   int dv;
   int teams;
@@ -91,7 +93,10 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
     if (lo->num_kv_heads > 1 && !mult16(lo->pool_head_stride)) return TOPKV_ERR_ALIGNMENT;
     plan->dv = D;
   } else {
-    return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+    if (lo->num_kv_heads != 1 || narrow || D > kLatentMaxD) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+    if (at->value_dim == 0 || at->value_dim > lo->head_dim || at->value_dim % 16 != 0) return TOPKV_ERR_INVALID_ARG;
+    if (at->value_dim > (uint32_t)kLatentMaxDv) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+    plan->dv = (int)at->value_dim;
   }
   const int64_t q_row = 2ll * D, o_row = 2ll * plan->dv;
   if (at->q_request_stride < 0 || at->q_head_stride < 0 || at->out_request_stride < 0 || at->out_head_stride < 0)
@@ -109,15 +114,18 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
 
   // How the work is shared out. A request can have at most `most` visible tokens.
   const int G = (int)(at->num_q_heads / lo->num_kv_heads);
-  const int gtiles = (G + kAttendRows - 1) / kAttendRows;
+  // query heads per CTA: latent rows take 16, 32 or 64 as columns of one product, whichever holds
+  // them all, so that few heads do not pay for empty columns
+  plan->row_tile = lo->kv_factor == 2 ? kAttendRows : G <= 16 ? 16 : G <= 32 ? 32 : 64;
+  const int gtiles = (G + plan->row_tile - 1) / plan->row_tile;
   plan->units = (int)lo->num_kv_heads * gtiles;
-  plan->rows = std::min(G, kAttendRows);
+  plan->rows = std::min(G, plan->row_tile);
   if (plan->units > 65535) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   int64_t most = (int64_t)b->max_pages_per_req * lo->page_tokens;
   if (b->window_tokens > 0) most = std::min(most, (int64_t)b->window_tokens + at->sink_tokens);
   if (b->total_tokens >= 0) most = std::min(most, b->total_tokens);
   const int64_t tiles = (most + kTileTokens - 1) / kTileTokens;
-  const int64_t resident = D > 128 ? kAttendCtas / 2 : kAttendCtas;
+  const int64_t resident = D > 128 || lo->kv_factor == 1 ? kAttendCtas / 2 : kAttendCtas;
   int64_t teams = std::max<int64_t>(1, resident / plan->units);
   // units that do not divide the resident CTAs would leave some of them idle: two rounds then
   if (teams * plan->units * 8 < resident * 7) teams = std::max<int64_t>(1, 2 * resident / plan->units);
@@ -147,6 +155,22 @@ int launch_attend_dim(const AttendParams& p, int units, cudaStream_t s) {
   if (p.D <= 128) return launch_attend<128, TYPE>(p, units, s);
   return launch_attend<256, TYPE>(p, units, s);
 }
+
+template <int N, bool BF16>
+int launch_latent2(const AttendParams& p, int units, cudaStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const int st = raise_smem(topkv_latent_kernel<N, BF16>, (int)latent_smem(N, kLatentMaxD, kLatentMaxDv).total, &done);
+  if (st != TOPKV_OK) return st;
+  return launched(launch_pdl(topkv_latent_kernel<N, BF16>, dim3(p.teams, units), dim3(kLatentThreads),
+                             latent_smem(N, p.D, p.Dv).total, s, p), 1);
+}
+template <bool BF16>
+int launch_latent(const AttendParams& p, int units, cudaStream_t s) {
+  if (p.row_tile == 16) return launch_latent2<16, BF16>(p, units, s);
+  if (p.row_tile == 32) return launch_latent2<32, BF16>(p, units, s);
+  return launch_latent2<64, BF16>(p, units, s);
+}
+static_assert(sizeof(LatentControl) <= 3072, "the largest layout leaves this much of 227 KiB");
 
 // ---- page operators -------------------------------------------------------------------------------
 int check_pages(const topkv_layout* lo, const topkv_batch* b, Resolved* rs) {
@@ -295,6 +319,7 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   p.uncut = plan.uncut;
   p.late_wait = (batch->flags & TOPKV_FLAG_TABLES_SETTLED) ? 1 : 0;
   p.rows = plan.rows;
+  p.row_tile = plan.row_tile;
   if (!plan.uncut) {
     uint8_t* w = static_cast<uint8_t*>(d_workspace);
     const int64_t slots = 2ll * plan.teams * plan.units * plan.rows;
@@ -304,7 +329,9 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
     p.part = reinterpret_cast<float*>(w + slots * 8);
   }
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (attention->cache_type == TOPKV_TYPE_BF16)
+  if (layout->kv_factor == 1)
+    st = p.io_bf16 ? launch_latent<true>(p, plan.units, s) : launch_latent<false>(p, plan.units, s);
+  else if (attention->cache_type == TOPKV_TYPE_BF16)
     st = launch_attend_dim<kBf16>(p, plan.units, s);
   else if (attention->cache_type == TOPKV_TYPE_FP16)
     st = launch_attend_dim<kFp16>(p, plan.units, s);

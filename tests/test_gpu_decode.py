@@ -532,3 +532,76 @@ def test_a_random_run_of_page_operators(dev):
         np.add.at(counts, bt[r, :-(-int(sl[r]) // g.P)], 1)
     assert np.array_equal(counts, ref)                       # the counts are the table's
     s.check(bt, sl, ref, pool, err)
+
+
+# ------------------------------------------------------------------------- latent rows
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq", [1, 16, 17, 32, 40, 64, 128])
+def test_latent_heads(dev, kind, Hq):
+    _case(dev, 1, 1, Hq, 576, 64, [100, 1, 64], kind, Dv=512, seed=Hq)
+
+
+@pytest.mark.parametrize("D,Dv", [(576, 512), (288, 256), (192, 128), (320, 320), (64, 16), (24, 16), (72, 48), (512, 512), (576, 400)])
+def test_latent_dims(dev, D, Dv):
+    _case(dev, 1, 1, 20, D, 16, [130, 7, 0], "bf16", Dv=Dv, seed=D)
+
+
+@pytest.mark.parametrize("P,style", [(1, "page"), (3, "padded"), (16, "padded"), (64, "page"), (100, "page"), (512, "padded")])
+def test_latent_pages(dev, P, style):
+    _case(dev, 1, 1, 8, 192, P, [300, 65, 1, 64], "fp16", Dv=128, style=style, seed=P, layer=1, L=2)
+
+
+@pytest.mark.parametrize("sl", [[1], [0, 0], [0, 257, 1, 0, 900, 64], [4000], [700, 3000, 63]])
+def test_latent_lengths(dev, sl):
+    for Hq in (3, 70):
+        _case(dev, 1, 1, Hq, 128, 16, sl, "bf16", Dv=64, seed=sum(sl))
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (64, 4), (100, 0), (700, 65)])
+def test_latent_window_and_sinks(dev, window, sinks):
+    _case(dev, 1, 1, 16, 128, 16, [1, 64, 257, 1400, 0], "fp16", Dv=128, window=window, sinks=sinks, seed=window)
+
+
+def test_latent_growing_scores(dev):
+    """Each tile's scores lie far above the ones before: the running maximum moves every time, by
+    little and by much, up to weights that vanish."""
+    for step in (0.5, 3.0, 9.0, 40.0):
+        for kind in ("bf16", "fp16"):
+            rng = np.random.default_rng(17)
+            sl = [900]
+            bt, pages = _table(sl, 64, 1, 0, rng)
+            g = _geom(1, 1, 64, 2, 64, pages)
+            pool = np.zeros(g.pool_bytes(), np.uint8)
+            for i in range(900):
+                row = rng.normal(size=64)
+                row[0] = (i // 64) * step if i % 3 else -(i // 64) * step
+                a = od.row_offset(g, 0, int(bt[0, i // 64]), 0, i % 64, 0)
+                pool[a:a + 128] = od.encode_elements(row, kind)
+            q = np.zeros((1, 18, 64))
+            q[0, :, 0] = np.linspace(-2, 2, 18)
+            q[0, :, 1:] = 0.1 * rng.normal(size=(18, 63))
+            q = od.decode_elements(od.encode_elements(q.reshape(-1), kind), kind).reshape(q.shape)
+            got = _run(dev, g, _layout(g), torch.from_numpy(pool).to(dev), bt, sl, q, kind, kind, 1.0, 64)
+            _check(got, od.attend(g, 0, pool, bt, sl, q, kind, kind, 1.0, 64))
+
+
+def test_latent_same_bits_graph_and_unusable_tables(dev):
+    rng = np.random.default_rng(12)
+    sl = [1500, 40, 700]
+    a = _case(dev, 1, 1, 33, 192, 16, sl, "bf16", Dv=128, seed=2)
+    b = _case(dev, 1, 1, 33, 192, 16, sl, "bf16", Dv=128, seed=2, T=2240, flags=tk.TOPKV_FLAG_TABLES_SETTLED, out_order="hr")
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(1, 1, 192, 2, 16, pages)
+    pool_h = _cache(g, bt, sl, "bf16", 0, rng)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=3 * 4 * 192), "bf16"), "bf16").reshape(3, 4, 192)
+    broken = bt.copy()
+    broken[1, :] = -1
+    broken[2, 1] = 1 << 29
+    out, lse = _run(dev, g, _layout(g), torch.from_numpy(pool_h).to(dev), broken, sl, q, "bf16", "bf16", 0.07, 128)
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
+    want = od.attend(g, 0, pool_h, bt, sl, q, "bf16", "bf16", 0.07, 128)
+    assert (np.abs(out[0] - want[0][0]) <= want[2][0]).all()
+    assert np.isfinite(out[2]).all() and (lse[1] == -np.inf).all()
