@@ -41,6 +41,7 @@ constexpr int kWarpTokens = 16;
 constexpr int kTileTokens = kAttendWarps * kWarpTokens;
 constexpr int kAttendRows = 16;      // query heads per CTA (rows of the matrix instruction)
 constexpr int kUncutTiles = 4;       // requests of at most this many tiles are not cut
+constexpr float kLazy = 8.f;         // a running maximum moves when it is exceeded by more than this (powers of two)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum AttendType { kBf16 = 1, kFp16 = 2, kE4m3 = 3 };
@@ -56,6 +57,7 @@ struct AttendParams {
   int64_t q_req, q_head, o_req, o_head;  // bytes
   int64_t num_pages;
   int R, maxp, P;
+  int page_shift;       // log2 of P, or -1 if P is no power of two
   int H, G, gtiles;     // KV heads, query heads per KV head, groups of row_tile query heads per KV head
   int D, Dv;            // elements
   int window, sinks;
@@ -213,6 +215,9 @@ __device__ __forceinline__ void store_io(uint8_t* p, float v, bool bf16) {
     *reinterpret_cast<__half*>(p) = __float2half_rn(v);
 }
 
+__device__ __forceinline__ void store_io2(uint8_t* p, float a, float b, bool bf16) {
+  *reinterpret_cast<uint32_t*>(p) = bf16 ? pack2<true>(a, b) : pack2<false>(a, b);
+}
 // Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0.
 template <int THREADS>
 __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, int64_t head0, int rows, bool complain) {
@@ -226,6 +231,12 @@ __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, 
       for (int g = threadIdx.x; g < rows; g += THREADS) p.lse[(int64_t)e * p.H * p.G + head0 + g] = -INFINITY;
   }
 }
+// 2^x by the hardware's approximation (2 ulp; results below 2^-126 become 0).
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // Two 8-bit values (low 16 bits) to two fp16 values; exact.
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
   uint32_t r;
@@ -233,27 +244,33 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
   return r;
 }
 // Shared memory: per warp a ring of stages, each 16 rows of K and 16 rows of V of DP elements.
-// Rows are swizzled in 16-byte chunks so that the eight rows of a matrix load hit all banks.
+// Rows are swizzled in 16-byte chunks so that the eight rows of a matrix load hit all banks. Stages
+// and registers are set for several CTAs per SM: a warp works through a tile in a chain of dependent
+// steps, so it takes 12 to 16 warps an SM to keep enough loads in flight.
 template <int DP, int TYPE>
 struct AttendShape {
   static constexpr int kElem = TYPE == kE4m3 ? 1 : 2;
   static constexpr int kRow = DP * kElem;                    // bytes of a row
   static constexpr int kChunks = kRow / 16;
   static constexpr int kStage = 2 * kWarpTokens * kRow;      // K rows, then V rows
-  static constexpr int kStages = kStage >= 16384 ? 3 : (kStage <= 2048 ? 8 : 24576 / kStage);
+  static constexpr int kCtas = DP == 64 ? 4 : DP == 128 ? 3 : TYPE == kE4m3 ? 2 : 1;  // per SM
+  static constexpr int kStages = (kCtas == 4 ? 12288 : kCtas == 3 ? 16384 : kCtas == 2 ? 24576 : 49152) / kStage;
   static constexpr int kSmem = kAttendWarps * kStages * kStage;
   static_assert(kSmem >= kAttendWarps * kAttendRows * (DP + 2) * 4, "the epilogue reuses the ring");
-  static __device__ __forceinline__ uint32_t at(int token, int chunk) {
+  static __device__ __forceinline__ uint32_t swizzle(int token, int chunk) {
     const int s = kChunks >= 8 ? (token & 7) : ((token >> 1) & 3);
-    return (uint32_t)(token * kRow + ((chunk ^ s) << 4));
+    return (uint32_t)((chunk ^ s) << 4);
   }
 };
+__host__ __device__ inline int attend_ctas_per_sm(int D, int type) {
+  return D <= 64 ? 4 : D <= 128 ? 3 : type == kE4m3 ? 2 : 1;
+}
 
 template <int DP, int TYPE>
-__global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) topkv_attend_kernel(const AttendParams p) {
   using S = AttendShape<DP, TYPE>;
   constexpr bool kMmaBf16 = TYPE == kBf16;
-  constexpr float kShift = kMmaBf16 ? 0.f : 15.f;
+  constexpr float kShift = kMmaBf16 ? 0.f : 7.f;
   constexpr int kSteps = DP / 16;  // k-steps of the first product, pairs of n-tiles of the second
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TeamStart s_team;
@@ -345,59 +362,101 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
     for (int i = 0; i < 2 * kSteps; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, base[2] = {0.f, 0.f};
 
     // ---- this warp's 16 tokens of every tile ---------------------------------------------------
-    // byte offset of the row of visible token v, or -1: past the end, or a page outside the pool
-    auto locate = [&](int t) -> int64_t {
-      const int v = t * kTileTokens + warp * kWarpTokens + (lane & 15);
-      if (t >= t1 || v >= vis.n) return -1;
-      const int i = v < vis.ns ? v : v - vis.ns + vis.lo;
-      const int j = i / p.P;
-      const int pg = p.bt[(int64_t)r * p.maxp + j];
-      if (pg < 0 || pg >= p.num_pages) {
-        raise_error(kErrTable);
-        return -1;
-      }
-      return (int64_t)pg * p.S_page + (int64_t)(i - j * p.P) * p.S_tok;
+    // Token of the lane's row (lane % 16) in tile t, or -1 past the end.
+    auto token_of = [&](int t, int row) {
+      const int v = t * kTileTokens + warp * kWarpTokens + row;
+      return t >= t1 || v >= vis.n ? -1 : v < vis.ns ? v : v - vis.ns + vis.lo;
     };
-    uint32_t stage_mask[S::kStages];  // which of a stage's 16 tokens count
-    auto issue = [&](int stage, int64_t off) {
+    auto column_of_page = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
+    // The page id comes one tile ahead of its use.
+    auto page_of = [&](int t) {
+      const int i = token_of(t, lane & 15);
+      return i < 0 ? -1 : p.bt[(int64_t)r * p.maxp + column_of_page(i)];
+    };
+    constexpr int kRows = 32 / S::kChunks;   // rows that one warp-wide copy brings
+    static_assert(kRows >= 1, "a row is at most 512 bytes");
+    constexpr int kCopies = kWarpTokens * S::kChunks / 32;
+    const int my_row = lane / S::kChunks, my_chunk = lane % S::kChunks;
+    auto issue = [&](int stage, int t, int pg) -> uint32_t {
       const uint32_t dst = ring_a + stage * S::kStage;
+      const int i0 = token_of(t, 0), i15 = token_of(t, 15);
+      if (i0 < 0) return 0;  // nothing left: the stage is not read
+      const int j0 = column_of_page(i0);
+      if (i15 == i0 + 15 && column_of_page(i15) == j0) {
+        // all 16 tokens follow each other in one page: rows at a constant stride, every lane has the id
+        if (pg < 0 || pg >= p.num_pages) {
+          if (lane == 0) raise_error(kErrTable);
+          return 0;
+        }
+        const uint8_t* src = k_base + (int64_t)pg * p.S_page + (int64_t)(i0 - j0 * p.P + my_row) * p.S_tok + my_chunk * 16;
 #pragma unroll
-      for (int i = 0; i < kWarpTokens * S::kChunks / 32; ++i) {
-        const int idx = i * 32 + lane;
-        const int token = idx / S::kChunks, chunk = idx % S::kChunks;
+        for (int i = 0; i < kCopies; ++i) {
+          const int token = i * kRows + my_row;
+          const uint32_t to = dst + token * S::kRow + S::swizzle(token, my_chunk);
+          if (my_chunk < chunks) {
+            cp_async16(to, src, true);
+            cp_async16(to + kWarpTokens * S::kRow, src + p.S_kv, true);
+          }
+          src += kRows * p.S_tok;
+        }
+        return 0xffffu;
+      }
+      int64_t off = -1;
+      const int i = token_of(t, lane & 15);
+      if (i >= 0) {
+        if (pg < 0 || pg >= p.num_pages)
+          raise_error(kErrTable);
+        else
+          off = (int64_t)pg * p.S_page + (int64_t)(i - column_of_page(i) * p.P) * p.S_tok;
+      }
+#pragma unroll
+      for (int k = 0; k < kCopies; ++k) {
+        const int token = k * kRows + my_row;
         const int64_t row = __shfl_sync(0xffffffffu, off, token);
-        if (chunk < chunks) {
-          const uint8_t* src = k_base + (row < 0 ? 0 : row) + chunk * 16;
-          const uint32_t to = dst + S::at(token, chunk);
+        if (my_chunk < chunks) {
+          const uint8_t* src = k_base + (row < 0 ? 0 : row) + my_chunk * 16;
+          const uint32_t to = dst + token * S::kRow + S::swizzle(token, my_chunk);
           cp_async16(to, src, row >= 0);
           cp_async16(to + kWarpTokens * S::kRow, src + (row < 0 ? 0 : p.S_kv), row >= 0);
         }
       }
       return __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
     };
-    int64_t next = locate(t0);
+    uint32_t stage_mask[S::kStages];  // which of a stage's 16 tokens count
+    int next = page_of(t0);
 #pragma unroll
     for (int s = 0; s < S::kStages - 1; ++s) {
-      const int64_t off = next;
-      next = locate(t0 + s + 1);
-      stage_mask[s] = issue(s, off);
+      const int pg = next;
+      next = page_of(t0 + s + 1);
+      stage_mask[s] = issue(s, t0 + s, pg);
       cp_async_commit();
+    }
+    // matrix loads: row and first chunk of this lane, K as it lies and V transposed
+    const int k_row = TYPE == kE4m3 ? (lane & 7) + ((lane >> 3) & 1) * 8 : (lane & 7) + (lane >> 4) * 8;
+    const int k_chunk = TYPE == kE4m3 ? lane >> 4 : (lane >> 3) & 1;
+    const int v_row = (lane & 7) + ((lane >> 3) & 1) * 8, v_chunk = lane >> 4;
+    constexpr int kOffsets = S::kChunks >= 8 ? 4 : 2;  // the swizzle repeats after 128 bytes (a row, if shorter)
+    uint32_t k_off[kOffsets], v_off[kOffsets];
+#pragma unroll
+    for (int i = 0; i < kOffsets; ++i) {
+      k_off[i] = ring_a + k_row * S::kRow + S::swizzle(k_row, 2 * i + k_chunk);
+      v_off[i] = ring_a + (kWarpTokens + v_row) * S::kRow + S::swizzle(v_row, 2 * i + v_chunk);
     }
     int stage = 0;
     for (int t = t0; t < t1; ++t) {
       {
-        const int64_t off = next;
-        next = locate(t + S::kStages);
+        const int pg = next;
+        next = page_of(t + S::kStages);
         int fill = stage + S::kStages - 1;
         if (fill >= S::kStages) fill -= S::kStages;
-        const uint32_t mask = issue(fill, off);
+        const uint32_t filled = issue(fill, t + S::kStages - 1, pg);
         cp_async_commit();
 #pragma unroll
         for (int s = 0; s < S::kStages; ++s)
-          if (s == fill) stage_mask[s] = mask;
+          if (s == fill) stage_mask[s] = filled;
       }
       uint32_t mask = 0;
 #pragma unroll
@@ -405,14 +464,14 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
         if (s == stage) mask = stage_mask[s];
       cp_async_wait<S::kStages - 1>();
       __syncwarp();
-      const uint32_t k_a = ring_a + stage * S::kStage, v_a = k_a + kWarpTokens * S::kRow;
+      const uint32_t at = stage * S::kStage;
       if (mask != 0) {
         float s[2][4] = {};
         if constexpr (TYPE == kE4m3) {
 #pragma unroll
           for (int k = 0; k < kSteps; k += 2) {
             uint32_t b4[4];
-            ldmatrix4(b4, k_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k + (lane >> 4)));
+            ldmatrix4(b4, k_off[(k / 2) % kOffsets] + at + (k / 2 / kOffsets) * (kOffsets * 32));
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -424,33 +483,39 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) {
             uint32_t b4[4];
-            ldmatrix4(b4, k_a + S::at((lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)));
+            ldmatrix4(b4, k_off[k % kOffsets] + at + (k / kOffsets) * (kOffsets * 32));
             mma16816<kMmaBf16>(s[0], qf[k], b4[0], b4[1]);
             mma16816<kMmaBf16>(s[1], qf[k], b4[2], b4[3]);
           }
         }
         // scores of rows gr and gr + 8 at tokens gc*2, +1, +8, +9
-        float top[2] = {m[0], m[1]};
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool seen = (mask >> (j * 8 + gc * 2 + (e & 1))) & 1;
-            s[j][e] = seen ? s[j][e] * row_scale[e >> 1] : -INFINITY;
-            top[e >> 1] = fmaxf(top[e >> 1], s[j][e]);
-          }
+          for (int e = 0; e < 4; ++e) s[j][e] *= row_scale[e >> 1];
+        if (mask != 0xffffu) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!((mask >> (j * 8 + gc * 2 + (e & 1))) & 1)) s[j][e] = -INFINITY;
         }
-        if (__any_sync(0xffffffffu, top[0] != m[0] || top[1] != m[1])) {
+        float top[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) top[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
+        // The reference of a row moves only when a score exceeds it by more than 2^kLazy: most tiles
+        // need one vote here, no exchange and no rescaling. Weights are at most 2^(kLazy + kShift).
+        if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
           float alpha[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            alpha[i] = top[i] == m[i] ? 1.f : exp2f(m[i] - top[i]);
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            top[i] = fmaxf(top[i], m[i]);
+            alpha[i] = top[i] == m[i] ? 1.f : exp2_approx(m[i] - top[i]);
             l[i] *= alpha[i];
             m[i] = top[i];
+            base[i] = m[i] == -INFINITY ? 0.f : m[i] - kShift;
           }
 #pragma unroll
           for (int i = 0; i < 2 * kSteps; ++i) {
@@ -460,14 +525,11 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
             o[i][3] *= alpha[1];
           }
         }
-        // the sums are kept relative to m - kShift: fp16 weights then run up to 2^15, so that one
-        // of them is exact to 2^-11 down to 2^-29 of the largest instead of 2^-14
-        const float base[2] = {m[0] == -INFINITY ? 0.f : m[0] - kShift, m[1] == -INFINITY ? 0.f : m[1] - kShift};
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            s[j][e] = exp2f(s[j][e] - base[e >> 1]);
+            s[j][e] = exp2_approx(s[j][e] - base[e >> 1]);
             l[e >> 1] += s[j][e];
           }
         uint32_t pf[4];
@@ -481,7 +543,7 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
 #pragma unroll
           for (int k = 0; k < kSteps; k += 2) {
             uint32_t b4[4];
-            ldmatrix4_trans(b4, v_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k + (lane >> 4)));
+            ldmatrix4_trans(b4, v_off[(k / 2) % kOffsets] + at + (k / 2 / kOffsets) * (kOffsets * 32));
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const uint32_t e0 = __byte_perm(b4[u * 2], b4[u * 2], 0x3120), e1 = __byte_perm(b4[u * 2 + 1], b4[u * 2 + 1], 0x3120);
@@ -493,7 +555,7 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) {
             uint32_t b4[4];
-            ldmatrix4_trans(b4, v_a + S::at((lane & 7) + ((lane >> 3) & 1) * 8, k * 2 + (lane >> 4)));
+            ldmatrix4_trans(b4, v_off[k % kOffsets] + at + (k / kOffsets) * (kOffsets * 32));
             mma16816<kMmaBf16>(o[k * 2], pf, b4[0], b4[1]);
             mma16816<kMmaBf16>(o[k * 2 + 1], pf, b4[2], b4[3]);
           }
@@ -531,24 +593,31 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
     __syncthreads();
     const bool whole = t0 == 0 && t1 == tiles;
     const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
-    for (int i = tid; i < rows * p.Dv; i += kAttendThreads) {
-      const int g = i / p.Dv, d = i - g * p.Dv;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kAttendWarps; ++w) top = fmaxf(top, s_m[w * kAttendRows + g]);
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, acc = 0.f;
+    // a thread takes neighbouring pairs of columns of one row after the other
+    const int pairs = p.Dv / 2;
+    for (int i = tid; i < rows * pairs; i += kAttendThreads) {
+      const int g = i / pairs, d = (i - g * pairs) * 2;
+      float f[kAttendWarps], top = -INFINITY, sum = 0.f, a0 = 0.f, a1 = 0.f;
 #pragma unroll
       for (int w = 0; w < kAttendWarps; ++w) {
-        const float f = exp2f(s_m[w * kAttendRows + g] - base);
-        sum += f * s_l[w * kAttendRows + g];
-        acc += f * s_o[(w * kAttendRows + g) * DP + d];
+        f[w] = s_m[w * kAttendRows + g];
+        top = fmaxf(top, f[w]);
+      }
+      const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) {
+        const float c = exp2_approx(f[w] - from);
+        const float2 v = *reinterpret_cast<const float2*>(&s_o[(w * kAttendRows + g) * DP + d]);
+        sum += c * s_l[w * kAttendRows + g];
+        a0 += c * v.x;
+        a1 += c * v.y;
       }
       if (whole) {
-        store_io(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc / sum * p.v_scale, p.io_bf16);
+        const float inv = p.v_scale / sum;
+        store_io2(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, a0 * inv, a1 * inv, p.io_bf16);
         if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
       } else {
-        p.part[(slot * p.rows + g) * p.Dv + d] = acc;
+        *reinterpret_cast<float2*>(&p.part[(slot * p.rows + g) * p.Dv + d]) = make_float2(a0, a1);
         if (d == 0) p.ml[slot * p.rows + g] = make_float2(top, sum);
       }
     }
@@ -562,41 +631,91 @@ __global__ void __launch_bounds__(kAttendThreads) topkv_attend_kernel(const Atte
   }
 }
 
-// Joins the parts of the requests that were cut: the CTA of the first cut inside a request takes
-// it. Parts are added in the order of the tokens.
-constexpr int kJoinThreads = 128;
+// Joins the parts of the requests that were cut: the CTAs of the first cut inside a request take it,
+// blockIdx.z of them row by row. Groups of threads take every other part and are added up at the end,
+// always in the same order.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinParts = 640;  // more teams than a launch has
 __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const AttendParams p) {
+  __shared__ float s_w[kJoinParts];
+  __shared__ float s_red[kJoinThreads / 32][2];
+  __shared__ float4 s_acc[kJoinThreads];
   pdl_wait_prior_grid();
   pdl_release_next_grid();
-  const int team = blockIdx.x + 1, unit = blockIdx.y;
+  const int team = blockIdx.x + 1, unit = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int2 cut = p.cuts[team];
   if (cut.x < 0 || p.cuts[team - 1].x == cut.x) return;  // no cut here, or not the request's first
-  int last = team - 1;  // the last team that holds a part: those that begin inside the request follow each other
+  int parts = 1;  // the part before the cut, and the ranges that begin inside the request, which follow each other
   for (int base = team; base < p.teams; base += kJoinThreads) {
-    const int t = base + threadIdx.x;
+    const int t = base + tid;
     const int n = __syncthreads_count(t < p.teams && p.cuts[t].x == cut.x);
-    last += n;
+    parts += n;
     if (n < kJoinThreads) break;
   }
   const int r = cut.x, units = gridDim.y;
   const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * p.row_tile;
   const int rows = min(p.G - g0, p.row_tile);
   const int64_t q_head0 = (int64_t)h * p.G + g0;
-  for (int i = blockIdx.z * kJoinThreads + threadIdx.x; i < rows * p.Dv; i += kJoinThreads * gridDim.z) {
-    const int g = i / p.Dv, d = i - g * p.Dv;
-    auto slot = [&](int t) -> int64_t { return (((int64_t)t * 2 + (t == team - 1 ? cut.y : 0)) * units + unit) * p.rows + g; };
+  const int quads = p.Dv / 4;                      // at most 128
+  const int groups = kJoinThreads / quads;
+  const int group = tid / quads, quad = tid - group * quads;
+  for (int g = blockIdx.z; g < rows; g += gridDim.z) {
+    auto slot = [&](int k) -> int64_t {
+      return (((int64_t)(team - 1 + k) * 2 + (k == 0 ? cut.y : 0)) * units + unit) * p.rows + g;
+    };
+    // the parts' weights
     float top = -INFINITY;
-    for (int t = team - 1; t <= last; ++t) top = fmaxf(top, p.ml[slot(t)].x);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, acc = 0.f;
-    for (int t = team - 1; t <= last; ++t) {
-      const float2 ml = p.ml[slot(t)];
-      const float f = exp2f(ml.x - base);
+    for (int k = tid; k < parts; k += kJoinThreads) top = fmaxf(top, p.ml[slot(k)].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) s_red[warp][0] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[w][0]);
+    const float from = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (int k = tid; k < parts; k += kJoinThreads) {
+      const float2 ml = p.ml[slot(k)];
+      const float f = exp2_approx(ml.x - from);
+      s_w[k] = f;
       sum += f * ml.y;
-      acc += f * p.part[slot(t) * p.Dv + d];
     }
-    store_io(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc / sum * p.v_scale, p.io_bf16);
-    if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_red[warp][1] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_red[w][1];
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (group < groups) {
+#pragma unroll 4
+      for (int k = group; k < parts; k += groups) {
+        const float4 v = *reinterpret_cast<const float4*>(&p.part[slot(k) * p.Dv + quad * 4]);
+        const float f = s_w[k];
+        acc.x += f * v.x;
+        acc.y += f * v.y;
+        acc.z += f * v.z;
+        acc.w += f * v.w;
+      }
+      s_acc[tid] = acc;
+    }
+    __syncthreads();
+    if (group == 0) {
+      for (int k = 1; k < groups; ++k) {
+        const float4 v = s_acc[k * quads + quad];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+      }
+      const float inv = p.v_scale / sum;
+      uint8_t* to = p.out + r * p.o_req + (q_head0 + g) * p.o_head + quad * 8;
+      store_io2(to, acc.x * inv, acc.y * inv, p.io_bf16);
+      store_io2(to + 4, acc.z * inv, acc.w * inv, p.io_bf16);
+      if (quad == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+    }
+    __syncthreads();
   }
 }
 

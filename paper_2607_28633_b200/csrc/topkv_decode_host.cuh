@@ -55,7 +55,6 @@ int raise_smem(K kernel, int bytes, std::atomic<uint64_t>* done) {
 }
 
 // ---- attention ----------------------------------------------------------------------------------
-constexpr int kAttendCtas = 2 * 148;  // CTAs that are resident together (two per SM up to 128 columns)
 
 struct AttendPlan {
   int units;        // CTAs per team
@@ -125,10 +124,11 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   if (b->window_tokens > 0) most = std::min(most, (int64_t)b->window_tokens + at->sink_tokens);
   if (b->total_tokens >= 0) most = std::min(most, b->total_tokens);
   const int64_t tiles = (most + kTileTokens - 1) / kTileTokens;
-  const int64_t resident = D > 128 || lo->kv_factor == 1 ? kAttendCtas / 2 : kAttendCtas;
+  const int64_t resident = 148 * (lo->kv_factor == 1 ? 1 : attend_ctas_per_sm(D, (int)at->cache_type));
   int64_t teams = std::max<int64_t>(1, resident / plan->units);
   // units that do not divide the resident CTAs would leave some of them idle: two rounds then
   if (teams * plan->units * 8 < resident * 7) teams = std::max<int64_t>(1, 2 * resident / plan->units);
+  teams = std::min<int64_t>(teams, kJoinParts);
   teams = std::min(teams, std::max<int64_t>(1, b->num_requests) * std::max<int64_t>(1, tiles));
   plan->uncut = tiles <= kUncutTiles || (teams == 1 && b->num_requests == 1);
   plan->teams = plan->uncut ? b->num_requests : (int)teams;
@@ -305,6 +305,7 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   p.R = batch->num_requests;
   p.maxp = batch->max_pages_per_req;
   p.P = (int)layout->page_tokens;
+  p.page_shift = (p.P & (p.P - 1)) == 0 ? __builtin_ctz((unsigned)p.P) : -1;
   p.H = (int)layout->num_kv_heads;
   p.G = (int)(attention->num_q_heads / layout->num_kv_heads);
   p.gtiles = plan.units / p.H;
@@ -338,7 +339,9 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   else
     st = launch_attend_dim<kE4m3>(p, plan.units, s);
   if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
-  const unsigned z = (unsigned)((plan.rows * plan.dv + 2 * kJoinThreads - 1) / (2 * kJoinThreads));
+  // about eight CTAs per SM if every team cuts a request
+  const int cuts = (plan.teams - 1) * plan.units;
+  const unsigned z = (unsigned)std::max(1, std::min(plan.rows, 8 * 148 / cuts));
   return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.teams - 1, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
 }
 

@@ -43,7 +43,7 @@ constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;
 constexpr int kLatentThreads = (kSoftmaxWarps + kLoadWarps + 1) * 32;
 constexpr int kLatentBlock = kLatentTile * 128;  // bytes of 64 columns of a tile
 constexpr int kLatentMaxD = 576, kLatentMaxDv = 512;
-constexpr float kLazy = 8.f;                     // a maximum moves when it is exceeded by more than this (powers of two)
+constexpr long long kWaitClocks = 1000000000ll;  // about half a second
 
 template <int N>
 __device__ __forceinline__ void tmem_load(uint32_t (&v)[N], uint32_t a);
@@ -88,6 +88,30 @@ __device__ __forceinline__ void tmem_store<32>(uint32_t a, const uint32_t (&v)[3
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
 
+// The 16 lanes of a quarter that hold scores, over all 32 threads: thread t gets, of columns
+// 8 i + 2 (t % 4) and the next, row t / 4 in v[4 i], v[4 i + 1] and row t / 4 + 8 in v[4 i + 2], v[4 i + 3].
+template <int N>
+__device__ __forceinline__ void tmem_load_half(uint32_t (&v)[N], uint32_t a);
+template <>
+__device__ __forceinline__ void tmem_load_half<4>(uint32_t (&v)[4], uint32_t a) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(a));
+}
+template <>
+__device__ __forceinline__ void tmem_load_half<8>(uint32_t (&v)[8], uint32_t a) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(a));
+}
+template <>
+__device__ __forceinline__ void tmem_load_half<16>(uint32_t (&v)[16], uint32_t a) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
+                 "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
+                 "=r"(v[14]), "=r"(v[15])
+               : "r"(a));
+}
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -105,10 +129,45 @@ __device__ __forceinline__ void proxy_fence_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ float redux_max(float v) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity)
+               : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+  return p != 0;
+}
+// Joins C values of each thread over the eight threads t, t ^ 4, t ^ 8, ... of a warp: as long as a
+// thread holds several columns, each step hands half of them over and joins the others. What is left
+// is one column per thread, number `column_of` of the thread's own.
+template <int C, typename Op>
+__device__ __forceinline__ float join_rows(float (&v)[C], int lane, Op op) {
+  int bit = 4;
+#pragma unroll
+  for (int n = C / 2; n >= 1; n /= 2, bit *= 2) {
+    const bool up = lane & bit;
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+      const float give = up ? v[j] : v[j + n];
+      const float keep = up ? v[j + n] : v[j];
+      v[j] = op(keep, __shfl_xor_sync(0xffffffffu, give, bit));
+    }
+  }
+#pragma unroll
+  for (; bit < 32; bit *= 2) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], bit));
+  return v[0];
+}
+template <int C>
+__device__ __forceinline__ int column_of(int lane) {  // 2 i + e, of column 8 i + 2 (lane % 4) + e
+  int j = 0, bit = 4;
+#pragma unroll
+  for (int n = C / 2; n >= 1; n /= 2, bit *= 2) j |= (lane & bit) ? n : 0;
+  return (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
 }
 // Shared-memory operand, 128-byte swizzle: `lead` and `stride` in bytes.
 __device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t lead, uint32_t stride) {
@@ -144,6 +203,7 @@ __host__ __device__ inline LatentSmem latent_smem(int N, int D, int Dv) {
 template <int N, bool BF16>
 __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const AttendParams p) {
   constexpr int NC = N / 2;                       // heads per softmax warp
+  constexpr int C = NC / 4;                       // ... per thread of it
   constexpr float kShift = BF16 ? 0.f : 7.f;
   constexpr uint32_t kCols = N == 64 ? 512 : N * 8;  // TMEM columns: 2 N for S^T, 4 N for O^T, a power of two
   extern __shared__ __align__(128) uint8_t smem[];
@@ -196,7 +256,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     const long long began = clock64();
     while (!mbar_try_wait(bar, phase & 1)) {
       if (s_dead) break;
-      if (clock64() - began > 1000000000ll) {  // about half a second
+      if (clock64() - began > kWaitClocks) {
         s_dead = 1;
         raise_error(kErrWait);
         break;
@@ -227,6 +287,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       // ---- load: pair `g` of warps takes the stages g of its own parity ---------------------------
       const int g = (warp - kSoftmaxWarps) >> 1, half = (warp - kSoftmaxWarps) & 1;
       const int chunks = p.D / 8, padded = ksteps * 2;  // 16-byte chunks of a row, and up to the last k-step
+      const int full = chunks / 8;                      // blocks that a row fills
       for (int i = (g - (int)(n & 1)) & 1; i < count; i += 2) {
         const uint32_t k = n + i;
         const int v = (t0 + i) * kLatentTile + half * 32 + lane;
@@ -243,22 +304,19 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         const uint32_t valid = __ballot_sync(0xffffffffu, off >= 0);
         if (k >= 2) wait(b_free + 8 * g, (k >> 1) - 1);
         if (lane == 0) ctl.valid[g][half] = valid;
+        // a warp-wide copy brings 128 bytes of four rows, so source and destination advance by a
+        // constant from one block of 64 columns to the next
+        const int c = lane & 7, sub = lane >> 3;
         const uint32_t dst = base + lay.kv + g * lay.stage + half * 32 * 128;
-        int row = 0, chunk = lane;
-        while (chunk >= padded) {
-          chunk -= padded;
-          ++row;
-        }
-        for (int e = lane; e < 32 * padded; e += 32) {
+#pragma unroll 2
+        for (int rg = 0; rg < 8; ++rg) {
+          const int row = rg * 4 + sub;
           const int64_t o = __shfl_sync(0xffffffffu, off, row);
-          const bool ok = o >= 0 && chunk < chunks;
-          cp_async16(dst + (chunk >> 3) * kLatentBlock + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
-                     p.pool + (ok ? o + chunk * 16 : 0), ok);
-          chunk += 32;
-          while (chunk >= padded) {
-            chunk -= padded;
-            ++row;
-          }
+          const uint8_t* src = p.pool + (o < 0 ? 0 : o) + c * 16;
+          uint32_t to = dst + row * 128 + ((c ^ (row & 7)) << 4);
+#pragma unroll 3
+          for (int b = 0; b < full; ++b, src += 128, to += kLatentBlock) cp_async16(to, src, o >= 0);
+          if (full * 8 + c < padded) cp_async16(to, full * 8 + c < chunks ? src : p.pool, o >= 0 && full * 8 + c < chunks);
         }
         cp_async_commit();
         cp_async_wait<0>();
@@ -267,46 +325,65 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       }
     } else if (warp == kSoftmaxWarps + kLoadWarps) {
       // ---- matrix instructions ----------------------------------------------------------------------
-      if (lane == 0) {
-        constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
-        constexpr uint32_t kScore = kType | 4u << 24;                        // M = 64, both K-major
-        constexpr uint32_t kValue = kType | 1u << 15 | 1u << 16 | 8u << 24;  // M = 128, M- and N-major
-        wait(b_query, seg);
-        for (int i = 0; i <= count; ++i) {
-          if (i < count) {
-            const uint32_t k = n + i, st = k & 1;
-            wait(b_full + 8 * st, k >> 1);
-            tcgen05_after_sync();
-            const uint32_t kv = base + lay.kv + st * lay.stage;
-            if (!s_dead) {
-              for (int s = 0; s < ksteps; ++s)
-                tcgen05_mma(tmem + st * N, smem_operand(kv + (s >> 2) * kLatentBlock + (s & 3) * 32, 16, 1024),
-                            smem_operand(base + lay.q + (s >> 2) * (N * 128) + (s & 3) * 32, 16, 1024), kScore, s > 0);
-              tcgen05_commit(b_score + 8 * st);
-            }
-          }
-          if (i > 0) {
-            const uint32_t k = n + i - 1, st = k & 1;
-            wait(b_weight, k);
-            tcgen05_after_sync();
-            const uint32_t kv = base + lay.kv + st * lay.stage;
-            if (!s_dead) {
-              for (int b = 0; b < vblocks; ++b)
+      // Scores of the next tile as soon as it is there, values of the one before as soon as its
+      // weights are: whichever comes first, so that a late load never holds up the tile whose rows
+      // have to be used before the next load can start. The descriptors are formed by the whole warp
+      // and one thread issues: from inside a branch of one thread each instruction took 70 cycles to
+      // issue, where the tensor core needs 35 (64 x 64) to 51 (128 x 64) for it.
+      constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
+      constexpr uint32_t kScore = kType | 4u << 24;                        // M = 64, both K-major
+      constexpr uint32_t kValue = kType | 1u << 15 | 1u << 16 | 8u << 24;  // M = 128, M- and N-major
+      wait(b_query, seg);
+      const uint64_t q0 = smem_operand(base + lay.q, 16, 1024), p0 = smem_operand(base + lay.p, kLatentBlock, 1024);
+      const long long began = clock64();
+      for (int is = 0, iv = 0; iv < count;) {
+        const uint32_t ks = n + is, kv = n + iv;
+        if (is < count && is < iv + 2 && __all_sync(0xffffffffu, mbar_test(b_full + 8 * (ks & 1), ks >> 1 & 1))) {
+          const uint32_t st = ks & 1;
+          tcgen05_after_sync();
+          const uint64_t a0 = smem_operand(base + lay.kv + st * lay.stage, 16, 1024);
+          const uint32_t d = tmem + st * N;
+          if (elect_one()) {
+#pragma unroll 3
+            for (int b = 0; b < ksteps / 4; ++b)
 #pragma unroll
-                for (int s = 0; s < kLatentTile / 16; ++s)
-                  tcgen05_mma(tmem + 2 * N + b * N, smem_operand(kv + 2 * b * kLatentBlock + s * 2048, kLatentBlock, 1024),
-                              smem_operand(base + lay.p + s * 2048, kLatentBlock, 1024), kValue, i > 1 || s > 0);
-              tcgen05_commit(b_free + 8 * st);
-            }
+              for (int u = 0; u < 4; ++u)
+                tcgen05_mma(d, a0 + (uint32_t)(b * (kLatentBlock >> 4) + 2 * u), q0 + (uint32_t)(b * (N * 128 >> 4) + 2 * u), kScore,
+                            b + u > 0);
+            for (int s = ksteps & ~3; s < ksteps; ++s)
+              tcgen05_mma(d, a0 + (uint32_t)((s >> 2) * (kLatentBlock >> 4) + 2 * (s & 3)),
+                          q0 + (uint32_t)((s >> 2) * (N * 128 >> 4) + 2 * (s & 3)), kScore, s > 0);
+            tcgen05_commit(b_score + 8 * st);
           }
+          __syncwarp();
+          ++is;
+        } else if (iv < is && __all_sync(0xffffffffu, mbar_test(b_weight, kv & 1))) {
+          const uint32_t st = kv & 1;
+          tcgen05_after_sync();
+          const uint64_t a0 = smem_operand(base + lay.kv + st * lay.stage, kLatentBlock, 1024);
+          if (elect_one()) {
+#pragma unroll 4
+            for (int v = 0; v < vblocks; ++v)
+#pragma unroll
+              for (int u = 0; u < kLatentTile / 16; ++u)
+                tcgen05_mma(tmem + 2 * N + v * N, a0 + (uint32_t)(v * (2 * kLatentBlock >> 4) + 128 * u), p0 + (uint32_t)(128 * u), kValue,
+                            iv + u > 0);
+            tcgen05_commit(b_free + 8 * st);
+          }
+          __syncwarp();
+          ++iv;
+        } else if (__any_sync(0xffffffffu, s_dead || clock64() - began > kWaitClocks * (int64_t)(count + 1))) {
+          if (lane == 0 && !s_dead) {
+            s_dead = 1;
+            raise_error(kErrWait);
+          }
+          break;
         }
       }
-      __syncwarp();
     } else {
       // ---- softmax ------------------------------------------------------------------------------------
       const int quarter = warp & 3, half = warp >> 2;
       const uint32_t lanes = (uint32_t)quarter << 21;  // first TMEM lane of this warp's quarter, in an address
-      const int token = quarter * 16 + lane;           // of a tile; lanes 16-31 of a quarter hold no scores
       const int c0 = half * NC;
       // Q: N rows of D elements, zero past the last head and column
       {
@@ -314,37 +391,44 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         const int padded = ksteps * 2;
         for (int e = tid; e < N * padded; e += kSoftmaxWarps * 32) {
           const int row = e / padded, chunk = e - row * padded;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (row < rows && chunk < p.D / 8) v = *reinterpret_cast<const uint4*>(src + row * p.q_head + chunk * 16);
-          *reinterpret_cast<uint4*>(smem + lay.q + (chunk >> 3) * (N * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = v;
+          const bool ok = row < rows && chunk < p.D / 8;
+          cp_async16(base + lay.q + (chunk >> 3) * (N * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4),
+                     ok ? src + row * p.q_head + chunk * 16 : src, ok);
         }
+        cp_async_commit();
+        cp_async_wait<0>();
         proxy_fence_smem();
         tcgen05_before_sync();  // the accumulator of the segment before has been read
         bar_arrive(b_query);
       }
-      float sum[NC];
+      // A thread's scores: columns c0 + 8 i + 2 (lane % 4) + e of tokens row and row + 8.
+      const int row = quarter * 16 + (lane >> 2);
+      const int mine_col = column_of<C>(lane);
+      float sum[C];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) sum[c] = 0.f;
+      for (int j = 0; j < C; ++j) sum[j] = 0.f;
       float top = -INFINITY;  // of head c0 + lane (lane < NC)
       for (int i = 0; i < count; ++i) {
         const uint32_t k = n + i, st = k & 1;
         wait(b_full + 8 * st, k >> 1);   // for ctl.valid
         wait(b_score + 8 * st, k >> 1);
         tcgen05_after_sync();
-        uint32_t raw[NC];
-        tmem_load<NC>(raw, tmem + lanes + st * N + c0);
-        const bool seen = lane < 16 && (ctl.valid[st][quarter >> 1] >> ((quarter & 1) * 16 + (lane & 15)) & 1);
+        uint32_t raw[2 * C];
+        tmem_load_half<2 * C>(raw, tmem + lanes + st * N + c0);
+        const uint32_t valid = ctl.valid[st][quarter >> 1] >> ((quarter & 1) * 16 + (lane >> 2));
+        const bool seen0 = valid & 1, seen1 = valid >> 8 & 1;
         tmem_wait_load();
-        float x[NC], most = -INFINITY;
+        float x[2 * C], most[C];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          x[c] = seen ? __uint_as_float(raw[c]) * p.qk_scale : -INFINITY;
-          const float m = redux_max(x[c]);
-          if (lane == c) most = m;
+        for (int j = 0; j < C; ++j) {  // j = 2 i + e; x[2 j] and x[2 j + 1] are the two tokens
+          x[2 * j] = seen0 ? __uint_as_float(raw[(j >> 1) * 4 + (j & 1)]) * p.qk_scale : -INFINITY;
+          x[2 * j + 1] = seen1 ? __uint_as_float(raw[(j >> 1) * 4 + (j & 1) + 2]) * p.qk_scale : -INFINITY;
+          most[j] = fmaxf(x[2 * j], x[2 * j + 1]);
         }
+        const float tile_top = join_rows<C>(most, lane, [](float a, float b) { return fmaxf(a, b); });
         float* const red = s_red + (k & 1) * 4 * N;
-        if (lane < NC) red[quarter * N + c0 + lane] = most;
-        asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+        red[quarter * N + c0 + mine_col] = tile_top;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");  // the four warps of these heads
         bool moved = false;
         float alpha = 1.f;
         if (lane < NC) {
@@ -352,33 +436,36 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
           const float m = fmaxf(fmaxf(red[c], red[N + c]), fmaxf(red[2 * N + c], red[3 * N + c]));
           if (m > top + kLazy) {
             moved = true;
-            alpha = exp2f(top - m);
+            alpha = exp2_approx(top - m);
             top = m;
           }
         }
         const bool rescale = __any_sync(0xffffffffu, moved);
         const float from = top == -INFINITY ? 0.f : top - kShift;
-        uint32_t w[NC / 2];
         if (rescale) {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) sum[c] *= __shfl_sync(0xffffffffu, alpha, c);
+          for (int j = 0; j < C; ++j) sum[j] *= __shfl_sync(0xffffffffu, alpha, (j >> 1) * 8 + (lane & 3) * 2 + (j & 1));
+        }
+        uint32_t w[C];  // w[2 i], w[2 i + 1]: the pair of columns, of the two tokens
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          const float f = __shfl_sync(0xffffffffu, from, (j >> 1) * 8 + (lane & 3) * 2 + (j & 1));
+          x[2 * j] = exp2_approx(x[2 * j] - f);
+          x[2 * j + 1] = exp2_approx(x[2 * j + 1] - f);
+          sum[j] += x[2 * j] + x[2 * j + 1];
         }
 #pragma unroll
-        for (int c = 0; c < NC; c += 2) {
-          x[c] = exp2f(x[c] - __shfl_sync(0xffffffffu, from, c));
-          x[c + 1] = exp2f(x[c + 1] - __shfl_sync(0xffffffffu, from, c + 1));
-          w[c / 2] = pack2<BF16>(x[c], x[c + 1]);
-          sum[c] += x[c];
-          sum[c + 1] += x[c + 1];
+        for (int j = 0; j < C; j += 2) {
+          w[j] = pack2<BF16>(x[2 * j], x[2 * j + 2]);
+          w[j + 1] = pack2<BF16>(x[2 * j + 1], x[2 * j + 3]);
         }
         // the second product of the tile before has to be done with the weights and the accumulator
         if (k > 0) wait(b_free + 8 * (st ^ 1), (k - 1) >> 1);
-        if (lane < 16) {
-          uint8_t* row = smem + lay.p + token * 128;
 #pragma unroll
-          for (int c = 0; c < NC / 8; ++c)
-            *reinterpret_cast<uint4*>(row + (((half * (NC / 8) + c) ^ (token & 7)) << 4)) =
-                make_uint4(w[c * 4], w[c * 4 + 1], w[c * 4 + 2], w[c * 4 + 3]);
+        for (int j = 0; j < C; j += 2) {
+          uint8_t* to = smem + lay.p + row * 128 + (((half * (NC / 8) + j / 2) ^ (row & 7)) << 4) + (lane & 3) * 4;
+          *reinterpret_cast<uint32_t*>(to) = w[j];
+          *reinterpret_cast<uint32_t*>(to + 8 * 128) = w[j + 1];  // row + 8: the same place of its swizzle
         }
         if (rescale && i > 0) {
           tcgen05_after_sync();
@@ -400,27 +487,20 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       // ---- the segment's result -----------------------------------------------------------------------
       wait(b_free + 8 * ((n + count - 1) & 1), (n + count - 1) >> 1);
       tcgen05_after_sync();
-      float total = 0.f;  // of head c0 + lane
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float v = sum[c];
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        v = __shfl_sync(0xffffffffu, v, 0);  // lanes 0-15 hold the tokens
-        if (lane == c) total = v;
-      }
+      float total = join_rows<C>(sum, lane, [](float a, float b) { return a + b; });
       // the turn after the last tile's: its readers have passed the last tile's barrier, and the next
       // tile's writers wait for scores that need every warp's arrival behind this read
       float* const red = s_red + ((n + count) & 1) * 4 * N;
-      if (lane < NC) red[quarter * N + c0 + lane] = total;
-      asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
-      if (lane < NC) {
+      red[quarter * N + c0 + mine_col] = total;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");
+      if (lane < NC) {  // from here on: of head c0 + lane
         const int c = c0 + lane;
         total = (red[c] + red[N + c]) + (red[2 * N + c] + red[3 * N + c]);
       }
       const bool whole = t0 == 0 && t1 == tiles;
       const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
       const int head = c0 + lane;
+      const float inv = 1.f / total;
       if (quarter == 0 && lane < NC && head < rows) {
         if (!whole)
           p.ml[slot * p.rows + head] = make_float2(top - kShift, total);
@@ -432,15 +512,18 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         tmem_load<NC>(o, tmem + lanes + 2 * N + b * N + c0);
         tmem_wait_load();
         const int d = b * 128 + quarter * 32 + lane;
+        if (whole) {
+          uint8_t* to = p.out + r * p.o_req + (int64_t)(g0 + c0) * p.o_head + d * 2;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const float l = __shfl_sync(0xffffffffu, total, c);
-          if (c0 + c < rows && d < p.Dv) {
-            if (whole)
-              store_io(p.out + r * p.o_req + (g0 + c0 + c) * p.o_head + d * 2, __uint_as_float(o[c]) / l, BF16);
-            else
-              p.part[(slot * p.rows + c0 + c) * p.Dv + d] = __uint_as_float(o[c]);
+          for (int c = 0; c < NC; ++c, to += p.o_head) {
+            const float f = __shfl_sync(0xffffffffu, inv, c);
+            if (c0 + c < rows && d < p.Dv) store_io(to, __uint_as_float(o[c]) * f, BF16);
           }
+        } else {
+          float* to = p.part + (slot * p.rows + c0) * p.Dv + d;
+#pragma unroll
+          for (int c = 0; c < NC; ++c, to += p.Dv)
+            if (c0 + c < rows && d < p.Dv) *to = __uint_as_float(o[c]);
         }
       }
     }
