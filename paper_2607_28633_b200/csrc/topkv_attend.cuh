@@ -67,6 +67,8 @@ struct AttendParams {
   int teams;            // CTAs along x; 0 tiles of a request cross a team when uncut
   int uncut;            // 1: team t is request t
   int late_wait;        // tables are settled
+  int box;              // latent rows: tokens of a tensor copy (divides the page and 64), 0 = none are used
+  int q_box;            // latent rows: 1 = Q comes by tensor copies too
   int rows;             // rows of a partial result, min(G, row_tile)
   int row_tile;         // query heads per CTA
   // workspace
@@ -632,13 +634,15 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
 }
 
 // Joins the parts of the requests that were cut: the CTAs of the first cut inside a request take it,
-// blockIdx.z of them row by row. Groups of threads take every other part and are added up at the end,
+// each up to eight of its rows. First a warp per row turns the parts' maxima and sums into weights,
+// then every thread adds up four neighbouring columns of a row over the parts; where rows and
+// columns do not fill the CTA, groups of threads take every other part and are added up at the end,
 // always in the same order.
 constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 8;
 constexpr int kJoinParts = 640;  // more teams than a launch has
 __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const AttendParams p) {
-  __shared__ float s_w[kJoinParts];
-  __shared__ float s_red[kJoinThreads / 32][2];
+  __shared__ float s_w[kJoinRows][kJoinParts];
   __shared__ float4 s_acc[kJoinThreads];
   pdl_wait_prior_grid();
   pdl_release_next_grid();
@@ -654,68 +658,78 @@ __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const A
   }
   const int r = cut.x, units = gridDim.y;
   const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * p.row_tile;
-  const int rows = min(p.G - g0, p.row_tile);
-  const int64_t q_head0 = (int64_t)h * p.G + g0;
-  const int quads = p.Dv / 4;                      // at most 128
-  const int groups = kJoinThreads / quads;
-  const int group = tid / quads, quad = tid - group * quads;
-  for (int g = blockIdx.z; g < rows; g += gridDim.z) {
-    auto slot = [&](int k) -> int64_t {
-      return (((int64_t)(team - 1 + k) * 2 + (k == 0 ? cut.y : 0)) * units + unit) * p.rows + g;
-    };
-    // the parts' weights
+  const int all_rows = min(p.G - g0, p.row_tile);
+  const int per = (p.rows + gridDim.z - 1) / gridDim.z;  // at most kJoinRows
+  const int row0 = blockIdx.z * per, rows = min(per, all_rows - row0);
+  if (rows <= 0) return;
+  const int64_t q_head0 = (int64_t)h * p.G + g0 + row0;
+  // row `row0` of part k; the parts but the first lie at a constant stride
+  const int64_t slot0 = (((int64_t)(team - 1) * 2 + cut.y) * units + unit) * p.rows + row0;
+  const int64_t slot1 = ((int64_t)team * 2 * units + unit) * p.rows + row0, step = 2ll * units * p.rows;
+  auto slot = [&](int k) -> int64_t { return k == 0 ? slot0 : slot1 + (k - 1) * step; };
+
+  for (int g = warp; g < rows; g += kJoinThreads / 32) {
     float top = -INFINITY;
-    for (int k = tid; k < parts; k += kJoinThreads) top = fmaxf(top, p.ml[slot(k)].x);
+    for (int k = lane; k < parts; k += 32) top = fmaxf(top, p.ml[slot(k) + g].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) s_red[warp][0] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[w][0]);
     const float from = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
-    for (int k = tid; k < parts; k += kJoinThreads) {
-      const float2 ml = p.ml[slot(k)];
+    for (int k = lane; k < parts; k += 32) {
+      const float2 ml = p.ml[slot(k) + g];
       const float f = exp2_approx(ml.x - from);
-      s_w[k] = f;
+      s_w[g][k] = f;
       sum += f * ml.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s_red[warp][1] = sum;
-    __syncthreads();
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) sum += s_red[w][1];
+    const float inv = p.v_scale / sum;
+    __syncwarp();
+    for (int k = lane; k < parts; k += 32) s_w[g][k] *= inv;
+    if (lane == 0 && p.lse != nullptr)
+      p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+  }
+  __syncthreads();
+
+  const int quads = p.Dv / 4, items = rows * quads;  // quads: at most 128
+  auto add_parts = [&](int i, int first, int by) {
+    const int g = i / quads, quad = i - g * quads;
+    const float* from = p.part + (int64_t)g * p.Dv + quad * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (group < groups) {
 #pragma unroll 4
-      for (int k = group; k < parts; k += groups) {
-        const float4 v = *reinterpret_cast<const float4*>(&p.part[slot(k) * p.Dv + quad * 4]);
-        const float f = s_w[k];
-        acc.x += f * v.x;
-        acc.y += f * v.y;
-        acc.z += f * v.z;
-        acc.w += f * v.w;
-      }
-      s_acc[tid] = acc;
+    for (int k = first; k < parts; k += by) {
+      const float4 v = *reinterpret_cast<const float4*>(from + slot(k) * p.Dv);
+      const float f = s_w[g][k];
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
     }
-    __syncthreads();
-    if (group == 0) {
-      for (int k = 1; k < groups; ++k) {
-        const float4 v = s_acc[k * quads + quad];
-        acc.x += v.x;
-        acc.y += v.y;
-        acc.z += v.z;
-        acc.w += v.w;
-      }
-      const float inv = p.v_scale / sum;
-      uint8_t* to = p.out + r * p.o_req + (q_head0 + g) * p.o_head + quad * 8;
-      store_io2(to, acc.x * inv, acc.y * inv, p.io_bf16);
-      store_io2(to + 4, acc.z * inv, acc.w * inv, p.io_bf16);
-      if (quad == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
+    return acc;
+  };
+  auto finish = [&](int i, float4 acc) {
+    const int g = i / quads, quad = i - g * quads;
+    uint8_t* to = p.out + r * p.o_req + (q_head0 + g) * p.o_head + quad * 8;
+    store_io2(to, acc.x, acc.y, p.io_bf16);
+    store_io2(to + 4, acc.z, acc.w, p.io_bf16);
+  };
+  if (items >= kJoinThreads) {
+    for (int i = tid; i < items; i += kJoinThreads) finish(i, add_parts(i, 0, 1));
+    return;
+  }
+  const int groups = kJoinThreads / items, group = tid / items;
+  if (group < groups) s_acc[tid] = add_parts(tid - group * items, group, groups);
+  __syncthreads();
+  if (group == 0) {
+    float4 acc = s_acc[tid];
+    for (int k = 1; k < groups; ++k) {
+      const float4 v = s_acc[k * items + tid];
+      acc.x += v.x;
+      acc.y += v.y;
+      acc.z += v.z;
+      acc.w += v.w;
     }
-    __syncthreads();
+    finish(tid, acc);
   }
 }
 

@@ -156,13 +156,67 @@ int launch_attend_dim(const AttendParams& p, int units, cudaStream_t s) {
   return launch_attend<256, TYPE>(p, units, s);
 }
 
+// Tensor map of one layer's rows, [page][token][column], for boxes of p->box tokens x 64 columns in the
+// swizzled order of the operands. Pieces of 8 to 64 tokens that never straddle a page: the page size
+// must be a multiple of 8 and tiles must begin at multiples of 8 tokens, so windowed layers, whose
+// first token is anywhere, do without (box 0), as does a layout that a tensor map cannot describe.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) cudaGetLastError();
+    return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(f) : nullptr;
+  }();
+  return fn;
+}
+CUtensorMap latent_map(AttendParams* p) {
+  CUtensorMap map = {};
+  p->box = 0;
+  const int box = std::min(kLatentTile, p->P & -p->P);
+  const int64_t tok = p->P > 1 ? p->S_tok : 16;
+  if (p->window > 0 || box < 8 || p->S_page >= (1ll << 40) || tok >= (1ll << 40) || p->num_pages > 0x7fffffffll) return map;
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return map;
+  const cuuint64_t dims[3] = {(cuuint64_t)p->D, (cuuint64_t)p->P, (cuuint64_t)p->num_pages};
+  const cuuint64_t strides[2] = {(cuuint64_t)tok, (cuuint64_t)p->S_page};
+  const cuuint32_t sizes[3] = {64, (cuuint32_t)box, 1}, steps[3] = {1, 1, 1};
+  const CUresult r = encode(&map, p->io_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                            const_cast<uint8_t*>(p->pool), dims, strides, sizes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) p->box = box;
+  return map;
+}
+
+// ... and of the queries, [request][head][column], for boxes of one request's heads_per_box heads.
+CUtensorMap query_map(AttendParams* p, int heads_per_box) {
+  CUtensorMap map = {};
+  p->q_box = 0;
+  if ((p->G > 1 && p->q_head < 2ll * p->D) || p->q_head >= (1ll << 40) || p->q_req >= (1ll << 40)) return map;
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return map;
+  const bool shared = p->q_req == 0;  // one query for all requests
+  const cuuint64_t dims[3] = {(cuuint64_t)p->D, (cuuint64_t)p->G, (cuuint64_t)(shared ? 1 : p->R)};
+  const cuuint64_t strides[2] = {(cuuint64_t)(p->G > 1 ? p->q_head : 16), (cuuint64_t)(shared ? 16 : p->q_req)};
+  const cuuint32_t sizes[3] = {64, (cuuint32_t)heads_per_box, 1}, steps[3] = {1, 1, 1};
+  const CUresult r = encode(&map, p->io_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                            const_cast<uint8_t*>(p->q), dims, strides, sizes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) p->q_box = 1;
+  return map;
+}
+
 template <int N, bool BF16>
-int launch_latent2(const AttendParams& p, int units, cudaStream_t s) {
+int launch_latent2(AttendParams p, int units, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   const int st = raise_smem(topkv_latent_kernel<N, BF16>, (int)latent_smem(N, kLatentMaxD, kLatentMaxDv).total, &done);
   if (st != TOPKV_OK) return st;
+  const CUtensorMap map = latent_map(&p), q_map = query_map(&p, N);
   return launched(launch_pdl(topkv_latent_kernel<N, BF16>, dim3(p.teams, units), dim3(kLatentThreads),
-                             latent_smem(N, p.D, p.Dv).total, s, p), 1);
+                             latent_smem(N, p.D, p.Dv).total, s, p, map, q_map), 1);
 }
 template <bool BF16>
 int launch_latent(const AttendParams& p, int units, cudaStream_t s) {
@@ -339,9 +393,9 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   else
     st = launch_attend_dim<kE4m3>(p, plan.units, s);
   if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
-  // about eight CTAs per SM if every team cuts a request
-  const int cuts = (plan.teams - 1) * plan.units;
-  const unsigned z = (unsigned)std::max(1, std::min(plan.rows, 8 * 148 / cuts));
+  // about eight CTAs per SM for the requests that can be cut
+  const int64_t cuts = (int64_t)std::min(plan.teams - 1, p.R) * plan.units;
+  const unsigned z = (unsigned)std::max((plan.rows + kJoinRows - 1) / kJoinRows, (int)std::min<int64_t>(plan.rows, 8 * 148 / cuts));
   return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.teams - 1, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
 }
 

@@ -20,14 +20,16 @@
 // the same rows at about the same time, from L2. Roles:
 //   warps 0-7   softmax: two warps per 32-lane quarter of TMEM, each with half of the heads; also
 //               load Q, rescale and write out the accumulator
-//   warps 8-11  load: two stages of 64 rows, one pair of warps each, 16-byte asynchronous copies
-//               through the block table (any page size and stride; what is masked becomes zero)
+//   warps 8-11  load: two stages of 64 rows, one pair of warps each, through the block table: tensor
+//               copies for full tiles, 16-byte copies for the rest (any page size and stride;
+//               what is masked becomes zero)
 //   warp 12     one thread issues the matrix instructions
 // Running maxima move only when a tile exceeds them by more than 2^8, so the accumulator is rescaled
 // a few times per request and not once per tile; the weights are at most 2^8 (fp16: scaled by
 // 2^7, to stay below 2^15), which costs no precision in a floating type.
 // Every wait is bounded; one that runs out raises error bit 1 and lets the CTA finish.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -119,10 +121,13 @@ __device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fen
 __device__ __forceinline__ void tcgen05_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tcgen05_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+// Operand descriptors are two words; only the low one (address, leading stride) differs between the
+// steps of a product, so the steps cost one addition each.
+__device__ __forceinline__ void tcgen05_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool accumulate) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      "{ .reg .pred p; .reg .b64 da, db; mov.b64 da, {%1, %3}; mov.b64 db, {%2, %3}; setp.ne.u32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)accumulate)
       : "memory");
 }
 __device__ __forceinline__ void proxy_fence_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -136,6 +141,17 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
                : "r"(bar), "r"(parity)
                : "memory");
   return ok != 0;
+}
+// Box of the tensor map at (x, y, z) into shared memory (bytes counted by the barrier), or into L2 only.
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map, int x, int y, int z) {
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z)
+               : "memory");
 }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -169,16 +185,14 @@ __device__ __forceinline__ int column_of(int lane) {  // 2 i + e, of column 8 i 
   for (int n = C / 2; n >= 1; n /= 2, bit *= 2) j |= (lane & bit) ? n : 0;
   return (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
 }
-// Shared-memory operand, 128-byte swizzle: `lead` and `stride` in bytes.
-__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t lead, uint32_t stride) {
-  return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 |
-         2ull << 61;
-}
+// Shared-memory operand, 128-byte swizzle, 1,024 bytes from eight rows to the next eight; `lead` in bytes.
+__device__ __forceinline__ uint32_t operand_lo(uint32_t addr, uint32_t lead) { return (addr & 0x3ffff) >> 4 | lead >> 4 << 16; }
+constexpr uint32_t kOperandHi = 1024 >> 4 | 1u << 14 | 2u << 29;
 
 // Layout of the dynamic shared memory. All operand blocks are multiples of 1,024 bytes.
 struct LatentControl {
   float red[2 * 4 * 64];  // maxima and sums per quarter of TMEM and head, by turns
-  uint64_t bar[8];
+  uint64_t bar[14];
   TeamStart team;
   uint32_t valid[2][2];   // which of a stage's tokens count
   uint32_t tmem;
@@ -201,7 +215,7 @@ __host__ __device__ inline LatentSmem latent_smem(int N, int D, int Dv) {
 }
 
 template <int N, bool BF16>
-__global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const AttendParams p, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
   constexpr int NC = N / 2;                       // heads per softmax warp
   constexpr int C = NC / 4;                       // ... per thread of it
   constexpr float kShift = BF16 ? 0.f : 7.f;
@@ -221,18 +235,24 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
   volatile int& s_dead = ctl.dead;
   float* const s_red = ctl.red;  // [2][quarter][head]
 
-  // barriers: rows loaded [2], rows used [2], scores ready [2], weights written, Q written
+  const int ksteps = (p.D + 15) / 16, vblocks = (p.Dv + 127) / 128;
+  const int blocks = (p.D + 63) / 64;
+  // Barriers. The blocks of a stage are given up in groups, one per 128 value columns (the blocks
+  // behind the values belong to the first): a group is loaded again while the products of the next
+  // one still run.
+  //   rows loaded [2], rows used [2][4], scores ready [2], weights written, Q written
   const uint32_t bar0 = smem_addr(ctl.bar);
-  const uint32_t b_full = bar0, b_free = bar0 + 16, b_score = bar0 + 32, b_weight = bar0 + 48, b_query = bar0 + 56;
+  const uint32_t b_full = bar0, b_free = bar0 + 16, b_score = bar0 + 80, b_weight = bar0 + 96, b_query = bar0 + 104;
+  const int last = vblocks - 1;  // the group whose products come last
   if (tid == 0) {
     s_dead = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(b_full + 8 * i, 64);
-      mbar_init(b_free + 8 * i, 1);
       mbar_init(b_score + 8 * i, 1);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(b_free + 8 * i, 1);
     mbar_init(b_weight, kSoftmaxWarps * 32);
-    mbar_init(b_query, kSoftmaxWarps * 32);
+    mbar_init(b_query, p.q_box ? 1 : kSoftmaxWarps * 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kSoftmaxWarps + kLoadWarps) {
@@ -253,6 +273,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
 
   // Waits until the barrier has completed its phase number `phase` (0, 1, 2, ...).
   auto wait = [&](uint32_t bar, uint32_t phase) {
+    if (mbar_try_wait(bar, phase & 1)) return;
     const long long began = clock64();
     while (!mbar_try_wait(bar, phase & 1)) {
       if (s_dead) break;
@@ -264,7 +285,6 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     }
   };
 
-  const int ksteps = (p.D + 15) / 16, vblocks = (p.Dv + 127) / 128;
   uint32_t n = 0;    // tiles before the current segment, in this CTA: they number the phases
   uint32_t seg = 0;  // segments before
   int64_t left = mine.left;  // 0: no tiles
@@ -288,21 +308,80 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       const int g = (warp - kSoftmaxWarps) >> 1, half = (warp - kSoftmaxWarps) & 1;
       const int chunks = p.D / 8, padded = ksteps * 2;  // 16-byte chunks of a row, and up to the last k-step
       const int full = chunks / 8;                      // blocks that a row fills
-      for (int i = (g - (int)(n & 1)) & 1; i < count; i += 2) {
+      // A full tile of whole page pieces comes by tensor copies, one instruction per piece and block
+      // of 64 columns, and its successor is brought to L2 meanwhile; any other tile comes by copies of
+      // 16 bytes per thread. (Those alone: 43 cycles each to issue, 3,100 a tile, 95 us for the
+      // 134k tokens x 128 heads that take 60 us with tensor copies.)
+      const int boxes = p.box > 0 ? kLatentTile / p.box : 0;  // pieces of a tile
+      auto page_column = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
+      // Page and token of piece `lane` of tile i (tensor copies: no window, so token and place agree).
+      auto piece = [&](int i, int* at) {
+        *at = 0;
+        const int v = (t0 + i) * kLatentTile + lane * p.box;
+        if (i >= count || lane >= boxes || (t0 + i + 1) * kLatentTile > vis.n) return -1;
+        const int j = page_column(v);
+        *at = v - j * p.P;
+        return p.bt[(int64_t)r * p.maxp + j];
+      };
+      int i = (g - (int)(n & 1)) & 1;
+      int at, pg = piece(i, &at);
+      for (; i < count; i += 2) {
         const uint32_t k = n + i;
-        const int v = (t0 + i) * kLatentTile + half * 32 + lane;
+        const bool pieces = boxes > 0 && __all_sync(0xffffffffu, lane >= boxes || (pg >= 0 && pg < p.num_pages));
+        if (pieces) {
+          // ctl.valid of the tile before has been read when its products begin
+          if (k >= 2) wait(b_free + 32 * g, (k >> 1) - 1);
+          // both warps come to the same answer; each takes every other group
+          int own = half == 0 ? max(blocks - 2 * vblocks, 0) : 0;  // blocks that this warp brings
+          for (int v = half; v < vblocks; v += 2) own += min(2, blocks - 2 * v);
+          if (lane == 0) {
+            ctl.valid[g][half] = 0xffffffffu;
+            mbar_expect_tx(b_full + 8 * g, (uint32_t)(own * kLatentBlock));
+          } else {
+            bar_arrive(b_full + 8 * g);
+          }
+          __syncwarp();
+          const uint32_t dst = base + lay.kv + g * lay.stage;
+          for (int v = half; v < vblocks; v += 2) {
+            if (k >= 2) wait(b_free + 32 * g + 8 * v, (k >> 1) - 1);
+            for (int e = 0; e < boxes; ++e) {
+              const int z = __shfl_sync(0xffffffffu, pg, e), y = __shfl_sync(0xffffffffu, at, e);
+              if (elect_one()) {
+                auto bring = [&](int b) {
+                  tma_load(dst + b * kLatentBlock + e * p.box * 128, &map, b * 64, y, z, b_full + 8 * g);
+                };
+                bring(2 * v);
+                if (2 * v + 1 < blocks) bring(2 * v + 1);
+                if (v == 0)
+                  for (int b = 2 * vblocks; b < blocks; ++b) bring(b);
+              }
+              __syncwarp();
+            }
+          }
+          pg = piece(i + 2, &at);
+          if (__all_sync(0xffffffffu, lane >= boxes || (pg >= 0 && pg < p.num_pages))) {
+            for (int e = 0; e < boxes; ++e) {
+              const int z = __shfl_sync(0xffffffffu, pg, e), y = __shfl_sync(0xffffffffu, at, e);
+              if (elect_one())
+                for (int b = half; b < blocks; b += 2) tma_prefetch(&map, b * 64, y, z);
+              __syncwarp();
+            }
+          }
+          continue;
+        }
+        pg = piece(i + 2, &at);
         int64_t off = -1;
-        if (v < vis.n) {
-          const int tok = v < vis.ns ? v : v - vis.ns + vis.lo;
-          const int j = tok / p.P;
-          const int pg = p.bt[(int64_t)r * p.maxp + j];
-          if (pg < 0 || pg >= p.num_pages)
+        const int place = (t0 + i) * kLatentTile + half * 32 + lane;
+        if (place < vis.n) {
+          const int tok = place < vis.ns ? place : place - vis.ns + vis.lo;
+          const int j = page_column(tok), page = p.bt[(int64_t)r * p.maxp + j];
+          if (page < 0 || page >= p.num_pages)
             raise_error(kErrTable);
           else
-            off = (int64_t)pg * p.S_page + (int64_t)(tok - j * p.P) * p.S_tok;
+            off = (int64_t)page * p.S_page + (int64_t)(tok - j * p.P) * p.S_tok;
         }
         const uint32_t valid = __ballot_sync(0xffffffffu, off >= 0);
-        if (k >= 2) wait(b_free + 8 * g, (k >> 1) - 1);
+        if (k >= 2) wait(b_free + 32 * g + 8 * last, (k >> 1) - 1);
         if (lane == 0) ctl.valid[g][half] = valid;
         // a warp-wide copy brings 128 bytes of four rows, so source and destination advance by a
         // constant from one block of 64 columns to the next
@@ -333,26 +412,34 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
       constexpr uint32_t kScore = kType | 4u << 24;                        // M = 64, both K-major
       constexpr uint32_t kValue = kType | 1u << 15 | 1u << 16 | 8u << 24;  // M = 128, M- and N-major
+      // Every score product of the segment before has been waited for, through its weights.
+      if (p.q_box) {
+        if (elect_one()) {
+          mbar_expect_tx(b_query, (uint32_t)(blocks * N * 128));
+          for (int b = 0; b < blocks; ++b) tma_load(base + lay.q + b * (N * 128), &q_map, b * 64, g0, p.q_req > 0 ? r : 0, b_query);
+        }
+        __syncwarp();
+      }
       wait(b_query, seg);
-      const uint64_t q0 = smem_operand(base + lay.q, 16, 1024), p0 = smem_operand(base + lay.p, kLatentBlock, 1024);
+      const uint32_t q0 = operand_lo(base + lay.q, 16), p0 = operand_lo(base + lay.p, kLatentBlock);
       const long long began = clock64();
+      uint32_t polls = 0;
       for (int is = 0, iv = 0; iv < count;) {
         const uint32_t ks = n + is, kv = n + iv;
         if (is < count && is < iv + 2 && __all_sync(0xffffffffu, mbar_test(b_full + 8 * (ks & 1), ks >> 1 & 1))) {
           const uint32_t st = ks & 1;
           tcgen05_after_sync();
-          const uint64_t a0 = smem_operand(base + lay.kv + st * lay.stage, 16, 1024);
+          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, 16);
           const uint32_t d = tmem + st * N;
           if (elect_one()) {
 #pragma unroll 3
             for (int b = 0; b < ksteps / 4; ++b)
 #pragma unroll
               for (int u = 0; u < 4; ++u)
-                tcgen05_mma(d, a0 + (uint32_t)(b * (kLatentBlock >> 4) + 2 * u), q0 + (uint32_t)(b * (N * 128 >> 4) + 2 * u), kScore,
-                            b + u > 0);
+                tcgen05_mma(d, a0 + b * (kLatentBlock >> 4) + 2 * u, q0 + b * (N * 128 >> 4) + 2 * u, kOperandHi, kScore, b + u > 0);
             for (int s = ksteps & ~3; s < ksteps; ++s)
-              tcgen05_mma(d, a0 + (uint32_t)((s >> 2) * (kLatentBlock >> 4) + 2 * (s & 3)),
-                          q0 + (uint32_t)((s >> 2) * (N * 128 >> 4) + 2 * (s & 3)), kScore, s > 0);
+              tcgen05_mma(d, a0 + (s >> 2) * (kLatentBlock >> 4) + 2 * (s & 3), q0 + (s >> 2) * (N * 128 >> 4) + 2 * (s & 3), kOperandHi,
+                          kScore, s > 0);
             tcgen05_commit(b_score + 8 * st);
           }
           __syncwarp();
@@ -360,19 +447,20 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         } else if (iv < is && __all_sync(0xffffffffu, mbar_test(b_weight, kv & 1))) {
           const uint32_t st = kv & 1;
           tcgen05_after_sync();
-          const uint64_t a0 = smem_operand(base + lay.kv + st * lay.stage, kLatentBlock, 1024);
+          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, kLatentBlock);
           if (elect_one()) {
 #pragma unroll 4
-            for (int v = 0; v < vblocks; ++v)
+            for (int v = 0; v < vblocks; ++v) {
 #pragma unroll
               for (int u = 0; u < kLatentTile / 16; ++u)
-                tcgen05_mma(tmem + 2 * N + v * N, a0 + (uint32_t)(v * (2 * kLatentBlock >> 4) + 128 * u), p0 + (uint32_t)(128 * u), kValue,
-                            iv + u > 0);
-            tcgen05_commit(b_free + 8 * st);
+                tcgen05_mma(tmem + 2 * N + v * N, a0 + v * (2 * kLatentBlock >> 4) + 128 * u, p0 + 128 * u, kOperandHi, kValue,
+                            iv > 0 || u > 0);
+              tcgen05_commit(b_free + 32 * st + 8 * v);
+            }
           }
           __syncwarp();
           ++iv;
-        } else if (__any_sync(0xffffffffu, s_dead || clock64() - began > kWaitClocks * (int64_t)(count + 1))) {
+        } else if ((++polls & 255) == 0 && __any_sync(0xffffffffu, s_dead || clock64() - began > kWaitClocks * (count + 1))) {
           if (lane == 0 && !s_dead) {
             s_dead = 1;
             raise_error(kErrWait);
@@ -385,8 +473,8 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       const int quarter = warp & 3, half = warp >> 2;
       const uint32_t lanes = (uint32_t)quarter << 21;  // first TMEM lane of this warp's quarter, in an address
       const int c0 = half * NC;
-      // Q: N rows of D elements, zero past the last head and column
-      {
+      // Q: N rows of D elements, zero past the last head and column (where no tensor copy can bring it)
+      if (!p.q_box) {
         const uint8_t* src = p.q + r * p.q_req + g0 * p.q_head;
         const int padded = ksteps * 2;
         for (int e = tid; e < N * padded; e += kSoftmaxWarps * 32) {
@@ -410,7 +498,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       float top = -INFINITY;  // of head c0 + lane (lane < NC)
       for (int i = 0; i < count; ++i) {
         const uint32_t k = n + i, st = k & 1;
-        wait(b_full + 8 * st, k >> 1);   // for ctl.valid
+        wait(b_full + 8 * st, k >> 1);  // for ctl.valid
         wait(b_score + 8 * st, k >> 1);
         tcgen05_after_sync();
         uint32_t raw[2 * C];
@@ -460,7 +548,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
           w[j + 1] = pack2<BF16>(x[2 * j + 1], x[2 * j + 3]);
         }
         // the second product of the tile before has to be done with the weights and the accumulator
-        if (k > 0) wait(b_free + 8 * (st ^ 1), (k - 1) >> 1);
+        if (k > 0) wait(b_free + 32 * (st ^ 1) + 8 * last, (k - 1) >> 1);
 #pragma unroll
         for (int j = 0; j < C; j += 2) {
           uint8_t* to = smem + lay.p + row * 128 + (((half * (NC / 8) + j / 2) ^ (row & 7)) << 4) + (lane & 3) * 4;
@@ -485,11 +573,11 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         bar_arrive(b_weight);
       }
       // ---- the segment's result -----------------------------------------------------------------------
-      wait(b_free + 8 * ((n + count - 1) & 1), (n + count - 1) >> 1);
+      wait(b_free + 32 * ((n + count - 1) & 1) + 8 * last, (n + count - 1) >> 1);
       tcgen05_after_sync();
       float total = join_rows<C>(sum, lane, [](float a, float b) { return a + b; });
-      // the turn after the last tile's: its readers have passed the last tile's barrier, and the next
-      // tile's writers wait for scores that need every warp's arrival behind this read
+      // the turn after the last tile's: its readers have passed the last tile's barrier; the next
+      // tile's writers wait below until this turn has been read
       float* const red = s_red + ((n + count) & 1) * 4 * N;
       red[quarter * N + c0 + mine_col] = total;
       asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");
@@ -497,6 +585,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         const int c = c0 + lane;
         total = (red[c] + red[N + c]) + (red[2 * N + c] + red[3 * N + c]);
       }
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");
       const bool whole = t0 == 0 && t1 == tiles;
       const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
       const int head = c0 + lane;
