@@ -239,11 +239,11 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Two 8-bit values (low 16 bits) to two fp16 values; exact.
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
-  uint32_t r;
-  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(v));
-  return r;
+// Four 8-bit values to two pairs of fp16 values; exact.
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t v, uint32_t* lo, uint32_t* hi) {
+  asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b; }"
+      : "=r"(*lo), "=r"(*hi)
+      : "r"(v));
 }
 // Shared memory: per warp a ring of stages, each 16 rows of K and 16 rows of V of DP elements.
 // Rows are swizzled in 16-byte chunks so that the eight rows of a matrix load hit all banks. Stages
@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   constexpr int kSteps = DP / 16;  // k-steps of the first product, pairs of n-tiles of the second
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TeamStart s_team;
+  __shared__ uint32_t s_mask[kAttendWarps][AttendShape<DP, TYPE>::kStages];
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
@@ -366,74 +367,71 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, base[2] = {0.f, 0.f};
 
-    // ---- this warp's 16 tokens of every tile ---------------------------------------------------
-    // Token of the lane's row (lane % 16) in tile t, or -1 past the end.
-    auto token_of = [&](int t, int row) {
-      const int v = t * kTileTokens + warp * kWarpTokens + row;
-      return t >= t1 || v >= vis.n ? -1 : v < vis.ns ? v : v - vis.ns + vis.lo;
-    };
-    auto column_of_page = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
-    // The page id comes one tile ahead of its use.
-    auto page_of = [&](int t) {
-      const int i = token_of(t, lane & 15);
-      return i < 0 ? -1 : p.bt[(int64_t)r * p.maxp + column_of_page(i)];
-    };
+    // ---- this warp's 16 tokens of every tile: visible tokens v .. v + 15, 64 further each time -----
+    const int end = min(vis.n, t1 * kTileTokens);
+    const int32_t* bt_row = p.bt + (int64_t)r * p.maxp;
+    auto token = [&](int v) { return v < vis.ns ? v : v + (vis.lo - vis.ns); };
+    auto page_column = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
+    // The page of the tile's first token, one tile ahead of its use.
+    auto page_of = [&](int v) { return v < end ? bt_row[page_column(token(v))] : 0; };
     constexpr int kRows = 32 / S::kChunks;   // rows that one warp-wide copy brings
     static_assert(kRows >= 1, "a row is at most 512 bytes");
     constexpr int kCopies = kWarpTokens * S::kChunks / 32;
     const int my_row = lane / S::kChunks, my_chunk = lane % S::kChunks;
-    auto issue = [&](int stage, int t, int pg) -> uint32_t {
+    uint32_t slow = 0;  // bit s: stage s holds a tile whose s_mask says which tokens count
+    auto issue = [&](int stage, int v, int pg) {
       const uint32_t dst = ring_a + stage * S::kStage;
-      const int i0 = token_of(t, 0), i15 = token_of(t, 15);
-      if (i0 < 0) return 0;  // nothing left: the stage is not read
-      const int j0 = column_of_page(i0);
-      if (i15 == i0 + 15 && column_of_page(i15) == j0) {
-        // all 16 tokens follow each other in one page: rows at a constant stride, every lane has the id
-        if (pg < 0 || pg >= p.num_pages) {
-          if (lane == 0) raise_error(kErrTable);
-          return 0;
-        }
-        const uint8_t* src = k_base + (int64_t)pg * p.S_page + (int64_t)(i0 - j0 * p.P + my_row) * p.S_tok + my_chunk * 16;
+      if (v >= end) return;  // nothing left: the stage is not read
+      const int i0 = token(v), x0 = i0 - page_column(i0) * p.P;
+      if (v + kWarpTokens <= end && (v >= vis.ns || v + kWarpTokens <= vis.ns) && x0 + kWarpTokens <= p.P && pg >= 0 &&
+          pg < p.num_pages) {
+        // all 16 tokens follow each other in one page: rows at a constant stride
+        const uint8_t* src = k_base + (int64_t)pg * p.S_page + (int64_t)(x0 + my_row) * p.S_tok + my_chunk * 16;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-          const int token = i * kRows + my_row;
-          const uint32_t to = dst + token * S::kRow + S::swizzle(token, my_chunk);
+          const int row = i * kRows + my_row;
+          const uint32_t to = dst + row * S::kRow + S::swizzle(row, my_chunk);
           if (my_chunk < chunks) {
             cp_async16(to, src, true);
             cp_async16(to + kWarpTokens * S::kRow, src + p.S_kv, true);
           }
           src += kRows * p.S_tok;
         }
-        return 0xffffu;
+        slow &= ~(1u << stage);
+        return;
       }
+      // the end of a request, pages of fewer than 16 tokens, a tile across pages or across the gap of
+      // a window, a page outside the pool: every row for itself
       int64_t off = -1;
-      const int i = token_of(t, lane & 15);
-      if (i >= 0) {
-        if (pg < 0 || pg >= p.num_pages)
+      if (v + (lane & 15) < end) {
+        const int i = token(v + (lane & 15)), j = page_column(i), page = bt_row[j];
+        if (page < 0 || page >= p.num_pages)
           raise_error(kErrTable);
         else
-          off = (int64_t)pg * p.S_page + (int64_t)(i - column_of_page(i) * p.P) * p.S_tok;
+          off = (int64_t)page * p.S_page + (int64_t)(i - j * p.P) * p.S_tok;
       }
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < kCopies; ++k) {
-        const int token = k * kRows + my_row;
-        const int64_t row = __shfl_sync(0xffffffffu, off, token);
+        const int row = k * kRows + my_row;
+        const int64_t o = __shfl_sync(0xffffffffu, off, row);
         if (my_chunk < chunks) {
-          const uint8_t* src = k_base + (row < 0 ? 0 : row) + my_chunk * 16;
-          const uint32_t to = dst + token * S::kRow + S::swizzle(token, my_chunk);
-          cp_async16(to, src, row >= 0);
-          cp_async16(to + kWarpTokens * S::kRow, src + (row < 0 ? 0 : p.S_kv), row >= 0);
+          const uint8_t* src = k_base + (o < 0 ? 0 : o) + my_chunk * 16;
+          const uint32_t to = dst + row * S::kRow + S::swizzle(row, my_chunk);
+          cp_async16(to, src, o >= 0);
+          cp_async16(to + kWarpTokens * S::kRow, src + (o < 0 ? 0 : p.S_kv), o >= 0);
         }
       }
-      return __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
+      const uint32_t mask = __ballot_sync(0xffffffffu, off >= 0) & 0xffffu;
+      if (lane == 0) s_mask[warp][stage] = mask;
+      slow |= 1u << stage;
     };
-    uint32_t stage_mask[S::kStages];  // which of a stage's 16 tokens count
-    int next = page_of(t0);
+    int v = t0 * kTileTokens + warp * kWarpTokens;
+    int next = page_of(v);
 #pragma unroll
     for (int s = 0; s < S::kStages - 1; ++s) {
       const int pg = next;
-      next = page_of(t0 + s + 1);
-      stage_mask[s] = issue(s, t0 + s, pg);
+      next = page_of(v + (s + 1) * kTileTokens);
+      issue(s, v + s * kTileTokens, pg);
       cp_async_commit();
     }
     // matrix loads: row and first chunk of this lane, K as it lies and V transposed
@@ -448,25 +446,17 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       v_off[i] = ring_a + (kWarpTokens + v_row) * S::kRow + S::swizzle(v_row, 2 * i + v_chunk);
     }
     int stage = 0;
-    for (int t = t0; t < t1; ++t) {
+    for (; v < end; v += kTileTokens) {
       {
         const int pg = next;
-        next = page_of(t + S::kStages);
-        int fill = stage + S::kStages - 1;
-        if (fill >= S::kStages) fill -= S::kStages;
-        const uint32_t filled = issue(fill, t + S::kStages - 1, pg);
+        next = page_of(v + S::kStages * kTileTokens);
+        issue(stage == 0 ? S::kStages - 1 : stage - 1, v + (S::kStages - 1) * kTileTokens, pg);
         cp_async_commit();
-#pragma unroll
-        for (int s = 0; s < S::kStages; ++s)
-          if (s == fill) stage_mask[s] = filled;
       }
-      uint32_t mask = 0;
-#pragma unroll
-      for (int s = 0; s < S::kStages; ++s)
-        if (s == stage) mask = stage_mask[s];
       cp_async_wait<S::kStages - 1>();
       __syncwarp();
       const uint32_t at = stage * S::kStage;
+      const uint32_t mask = slow >> stage & 1 ? s_mask[warp][stage] : 0xffffu;
       if (mask != 0) {
         float s[2][4] = {};
         if constexpr (TYPE == kE4m3) {
@@ -477,9 +467,11 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int j = 0; j < 2; ++j)
-                mma16816<false>(s[j], qf[k + u], e4m3x2_to_f16x2(b4[u * 2 + j] & 0xffffu),
-                                e4m3x2_to_f16x2(b4[u * 2 + j] >> 16));
+              for (int j = 0; j < 2; ++j) {
+                uint32_t lo, hi;
+                e4m3x4_to_f16(b4[u * 2 + j], &lo, &hi);
+                mma16816<false>(s[j], qf[k + u], lo, hi);
+              }
           }
         } else {
 #pragma unroll
@@ -548,9 +540,12 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
             ldmatrix4_trans(b4, v_off[(k / 2) % kOffsets] + at + (k / 2 / kOffsets) * (kOffsets * 32));
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const uint32_t e0 = __byte_perm(b4[u * 2], b4[u * 2], 0x3120), e1 = __byte_perm(b4[u * 2 + 1], b4[u * 2 + 1], 0x3120);
-              mma16816<false>(o[(k + u) * 2], pf, e4m3x2_to_f16x2(e0 & 0xffffu), e4m3x2_to_f16x2(e1 & 0xffffu));
-              mma16816<false>(o[(k + u) * 2 + 1], pf, e4m3x2_to_f16x2(e0 >> 16), e4m3x2_to_f16x2(e1 >> 16));
+              // bytes: token 0 (even, odd column), token 1 (even, odd) -> both tokens' even, both odd
+              uint32_t even0, odd0, even1, odd1;
+              e4m3x4_to_f16(__byte_perm(b4[u * 2], 0, 0x3120), &even0, &odd0);
+              e4m3x4_to_f16(__byte_perm(b4[u * 2 + 1], 0, 0x3120), &even1, &odd1);
+              mma16816<false>(o[(k + u) * 2], pf, even0, even1);
+              mma16816<false>(o[(k + u) * 2 + 1], pf, odd0, odd1);
             }
           }
         } else {
