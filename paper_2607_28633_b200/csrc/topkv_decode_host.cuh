@@ -266,8 +266,8 @@ PageTables page_tables(const topkv_layout* lo, const topkv_batch* b, const topkv
                     (int)lo->page_tokens, (int)lo->num_pool_pages};
 }
 
-// Brings the tables into the out arrays, where the operator then works in place.
-int copy_tables(const topkv_layout* lo, const topkv_batch* b, const topkv_page_tables* t, cudaStream_t s) {
+// The copy that brings the tables into the out arrays, where the operator then works in place.
+TablesCopyParams tables_copy(const topkv_layout* lo, const topkv_batch* b, const topkv_page_tables* t, int64_t* most) {
   TablesCopyParams p = {};
   p.src[0] = b->block_table;
   p.src[1] = b->seq_lens;
@@ -278,14 +278,19 @@ int copy_tables(const topkv_layout* lo, const topkv_batch* b, const topkv_page_t
   p.n[0] = (int64_t)b->num_requests * b->max_pages_per_req;
   p.n[1] = b->num_requests;
   p.n[2] = lo->num_pool_pages;
-  int64_t most = 0;
+  *most = 0;
   for (int i = 0; i < 3; ++i) {
     if (p.src[i] == p.dst[i]) p.n[i] = 0;
-    most = std::max(most, p.n[i]);
+    *most = std::max(*most, p.n[i]);
   }
+  return p;
+}
+unsigned copy_ctas(int64_t most, int threads) { return (unsigned)std::min<int64_t>((most + threads - 1) / threads, 2 * 148); }
+int copy_tables(const topkv_layout* lo, const topkv_batch* b, const topkv_page_tables* t, cudaStream_t s) {
+  int64_t most;
+  const TablesCopyParams p = tables_copy(lo, b, t, &most);
   if (most == 0) return TOPKV_OK;
-  const unsigned blocks = (unsigned)std::min<int64_t>((most + 255) / 256, 4 * 148);
-  return launched(launch_pdl(topkv_tables_copy_kernel, dim3(blocks), dim3(256), 0, s, p), 1);
+  return launched(launch_pdl(topkv_tables_copy_kernel, dim3(copy_ctas(most, 256)), dim3(256), 0, s, p), 1);
 }
 
 // How the contents of a page are moved; *vec = bytes per access.
@@ -303,8 +308,10 @@ PageGeom page_geometry(int first_layer, int num_layers, void* pool, const topkv_
   g.S_unit = g.U > 1 ? lo->pool_head_stride : 0;
   g.unit_bytes = rs.unit_bytes;
   g.linear = g.S_tok == rs.unit_bytes;
-  const int64_t tok_bytes = g.F * rs.row_bytes;
-  g.tps = (int)std::max<int64_t>(1, std::min<int64_t>(g.P, kSpanTargetBytes / tok_bytes));
+  // equal parts of about 64 KiB (a page of 72 KiB stays whole: as 56 + 16 KiB its copy took 20 % longer)
+  const int64_t page_bytes = g.P * g.F * rs.row_bytes;
+  const int64_t parts = std::min<int64_t>(g.P, std::max<int64_t>(1, (page_bytes + kSpanTargetBytes / 2) / kSpanTargetBytes));
+  g.tps = (int)((g.P + parts - 1) / parts);
   g.cpp = (g.P + g.tps - 1) / g.tps;
   const uintptr_t m = reinterpret_cast<uintptr_t>(g.pool) | (uintptr_t)g.S_layer | (uintptr_t)g.S_page |
                       (uintptr_t)g.S_kv | (uintptr_t)g.S_tok | (uintptr_t)g.S_unit | (uintptr_t)g.unit_bytes;
@@ -455,8 +462,9 @@ int topkv_fork_requests(void* pool, const topkv_layout* layout, const topkv_batc
     p.g.cpp = 1;
     if (p.g.layers > 65534) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   }
-  st = copy_tables(layout, batch, tables, s);
-  if (st != TOPKV_OK || num_forks == 0) return st;
+  if (num_forks == 0) return copy_tables(layout, batch, tables, s);
+  int64_t most;
+  p.copy = tables_copy(layout, batch, tables, &most);
   p.t = page_tables(layout, batch, tables);
   p.parents = d_parents;
   p.children = d_children;
@@ -464,7 +472,7 @@ int topkv_fork_requests(void* pool, const topkv_layout* layout, const topkv_batc
   p.rec = static_cast<ForkRecord*>(d_workspace);
   p.claim = reinterpret_cast<int32_t*>(p.rec + num_forks);
   p.list = p.claim + p.t.R;
-  st = launched(launch_pdl(topkv_fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p), 1);
+  st = launched(launch_pdl(topkv_fork_plan_kernel, dim3(1 + copy_ctas(most, kPlanThreads)), dim3(kPlanThreads), 0, s, p), 1);
   if (st != TOPKV_OK) return st;
   const dim3 grid((unsigned)num_forks, (unsigned)(1 + p.g.layers * p.g.cpp));
   return launched(vec == 32 ? launch_pdl(topkv_fork_apply_kernel<32>, grid, dim3(kMoveThreads), 0, s, p)
@@ -501,11 +509,11 @@ int topkv_compact_pages(void* pool, const topkv_layout* layout, const topkv_batc
   st = check_page_workspace(layout, batch, 0, d_workspace, workspace_bytes);
   if (st != TOPKV_OK) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  st = copy_tables(layout, batch, tables, s);
-  if (st != TOPKV_OK) return st;
   int vec;
   const PageGeom g = page_geometry(0, (int)layout->num_layers, pool, layout, rs, &vec);
   CompactParams p;
+  int64_t most;
+  p.copy = tables_copy(layout, batch, tables, &most);
   p.t = page_tables(layout, batch, tables);
   const int64_t N = p.t.num_pages;
   p.code = static_cast<int32_t*>(d_workspace);
@@ -515,7 +523,8 @@ int topkv_compact_pages(void* pool, const topkv_layout* layout, const topkv_batc
   p.num_used = d_num_used;
   p.map = d_page_map;
   const int block = kPlanThreads * kPlanPages;
-  st = launched(launch_pdl(topkv_compact_plan_kernel, dim3((unsigned)((N + block - 1) / block)), dim3(kPlanThreads), 0, s, p), 1);
+  p.blocks = (int)((N + block - 1) / block);
+  st = launched(launch_pdl(topkv_compact_plan_kernel, dim3(p.blocks + copy_ctas(most, kPlanThreads)), dim3(kPlanThreads), 0, s, p), 1);
   if (st != TOPKV_OK) return st;
   return launched(vec == 32 ? launch_pdl(topkv_compact_apply_kernel<32>, dim3(kMoveCtas), dim3(kMoveThreads), 0, s, p, g)
                             : launch_pdl(topkv_compact_apply_kernel<16>, dim3(kMoveCtas), dim3(kMoveThreads), 0, s, p, g), 1);
@@ -541,7 +550,7 @@ int topkv_copy_pages(int first_layer, int num_layers, void* pool, const topkv_la
   p.n = num_pages;
   p.num_pages = (int)layout->num_pool_pages;
   const int64_t items = p.n * p.g.layers * p.g.cpp;
-  const dim3 grid((unsigned)std::min<int64_t>(items, kMoveCtas));
+  const dim3 grid((unsigned)std::min<int64_t>(items, 0x7fffffffll));  // one CTA per part
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   return launched(vec == 32 ? launch_pdl(topkv_page_move_kernel<32>, grid, dim3(kMoveThreads), 0, s, p)
                             : launch_pdl(topkv_page_move_kernel<16>, grid, dim3(kMoveThreads), 0, s, p), 1);

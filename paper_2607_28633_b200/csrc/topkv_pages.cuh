@@ -3,7 +3,7 @@
 // The tables (block table, lengths, reference counts) are integers and every rule that picks a
 // page takes the lowest free id first, so a call has one possible result whatever the order in
 // which its CTAs run. Each call is one to three launches: the tables are copied when the caller
-// wants them in other buffers (topkv_tables_copy_kernel), one CTA works out who gets which page
+// wants them in other buffers (beside the planning, or before), one CTA works out who gets which page
 // (fork, extend: prefix sums over the requests, then one walk over the reference counts up to the
 // last page that is needed), and a wide grid rewrites rows and moves page contents.
 //
@@ -109,12 +109,15 @@ struct TablesCopyParams {
   int32_t* dst[3];
   int64_t n[3];  // 0: stays where it is
 };
-__global__ void __launch_bounds__(256) topkv_tables_copy_kernel(const TablesCopyParams p) {
-  pdl_prologue(0);
-  const int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
+__device__ __forceinline__ void copy_tables(const TablesCopyParams& p, int cta, int ctas) {
+  const int64_t t = (int64_t)cta * blockDim.x + threadIdx.x, step = (int64_t)ctas * blockDim.x;
 #pragma unroll
   for (int a = 0; a < 3; ++a)
     for (int64_t i = t; i < p.n[a]; i += step) p.dst[a][i] = p.src[a][i];
+}
+__global__ void __launch_bounds__(256) topkv_tables_copy_kernel(const TablesCopyParams p) {
+  pdl_prologue(0);
+  copy_tables(p, blockIdx.x, gridDim.x);
 }
 
 // ---- free ---------------------------------------------------------------------------------------
@@ -298,6 +301,7 @@ struct ForkRecord {
 };
 struct ForkParams {
   PageTables t;
+  TablesCopyParams copy;
   PageGeom g;
   const int32_t* parents;
   const int32_t* children;
@@ -311,7 +315,12 @@ struct ForkParams {
 __global__ void __launch_bounds__(kPlanThreads) topkv_fork_plan_kernel(const ForkParams p) {
   __shared__ int s_scan[33];
   pdl_prologue(0);
+  if (blockIdx.x > 0) {  // the other CTAs copy the tables; this one reads them where they were
+    copy_tables(p.copy, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
   const int tid = threadIdx.x;
+  const int32_t *bt = p.copy.src[0], *sl = p.copy.src[1], *ref = p.copy.src[2];
   for (int i = tid; i < p.n; i += kPlanThreads) {  // only the rows that are named have to be cleared
     const int c = p.children[i];
     if (c >= 0 && c < p.t.R) p.claim[c] = 0x7fffffff;
@@ -331,11 +340,11 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_fork_plan_kernel(const For
     if (i < p.n) {
       const int a = p.parents[i], c = p.children[i];
       bool ok = a >= 0 && a < p.t.R && c >= 0 && c < p.t.R && a != c;
-      if (ok) ok = *(volatile int32_t*)(p.claim + c) == i && p.t.sl[c] == 0;
-      const int len = ok ? p.t.sl[a] : 0;
+      if (ok) ok = *(volatile int32_t*)(p.claim + c) == i && sl[c] == 0;
+      const int len = ok ? sl[a] : 0;
       if (ok) ok = len >= 0 && len <= row;
       if (ok && len % p.t.P != 0) {  // the page that is shared in part must be a page of the pool
-        const int pg = p.t.bt[(int64_t)a * p.t.maxp + len / p.t.P];
+        const int pg = bt[(int64_t)a * p.t.maxp + len / p.t.P];
         ok = pg >= 0 && pg < p.t.num_pages;
         need = ok;
       }
@@ -354,7 +363,7 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_fork_plan_kernel(const For
     carry += total;
   }
   const int wanted = min(carry, p.t.num_pages);
-  const int found = wanted > 0 ? list_free_pages(p.t.ref, p.t.num_pages, wanted, p.list, s_scan) : 0;
+  const int found = wanted > 0 ? list_free_pages(ref, p.t.num_pages, wanted, p.list, s_scan) : 0;
   for (int i = tid; i < p.n; i += kPlanThreads) {  // this thread wrote these records itself
     const int rank = p.rec[i].fresh;
     if (rank < 0) continue;
@@ -402,6 +411,8 @@ __global__ void __launch_bounds__(kMoveThreads, 3) topkv_fork_apply_kernel(const
 // ---- compact ------------------------------------------------------------------------------------
 struct CompactParams {
   PageTables t;
+  TablesCopyParams copy;
+  int blocks;       // CTAs that plan; the others copy the tables
   int32_t* code;    // workspace [num_pages]: -1 free, p stays, -2 - k moves to holes[k]
   int32_t* holes;   // workspace [num_pages / 2 + 1]: free pages below the number in use, ascending
   int32_t* movers;  // workspace [num_pages / 2 + 1]: pages in use at or above it, ascending
@@ -414,12 +425,17 @@ struct CompactParams {
 __global__ void __launch_bounds__(kPlanThreads) topkv_compact_plan_kernel(const CompactParams p) {
   __shared__ int s_scan[33];
   pdl_prologue(0);
+  if (blockIdx.x >= p.blocks) {
+    copy_tables(p.copy, blockIdx.x - p.blocks, gridDim.x - p.blocks);
+    return;
+  }
+  const int32_t* ref = p.copy.src[2];
   const int tid = threadIdx.x, N = p.t.num_pages;
   constexpr int kBlock = kPlanThreads * kPlanPages;
   const int mine = blockIdx.x * kBlock;
   int all = 0, before = 0;
   for (int64_t i = tid; i < N; i += kPlanThreads) {
-    const int u = p.t.ref[i] > 0;
+    const int u = ref[i] > 0;
     all += u;
     before += i < mine ? u : 0;
   }
@@ -427,7 +443,7 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_compact_plan_kernel(const 
   block_exclusive_sum(all, s_scan, &used);
   block_exclusive_sum(before, s_scan, &used_before);
   int low = 0;
-  for (int i = tid; i < used; i += kPlanThreads) low += p.t.ref[i] > 0;
+  for (int i = tid; i < used; i += kPlanThreads) low += ref[i] > 0;
   int used_low;  // pages in use that stay
   block_exclusive_sum(low, s_scan, &used_low);
   int n = 0;
@@ -435,7 +451,7 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_compact_plan_kernel(const 
   const int64_t p0 = (int64_t)mine + (int64_t)tid * kPlanPages;
 #pragma unroll
   for (int k = 0; k < kPlanPages; ++k) {
-    u[k] = p0 + k < N && p.t.ref[p0 + k] > 0;
+    u[k] = p0 + k < N && ref[p0 + k] > 0;
     n += u[k];
   }
   int rank = used_before + block_exclusive_sum(n, s_scan, &dummy);  // pages in use below p0
