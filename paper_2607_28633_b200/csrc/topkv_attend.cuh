@@ -66,14 +66,14 @@ struct AttendParams {
   int io_bf16;
   int teams;            // CTAs along x; 0 tiles of a request cross a team when uncut
   int uncut;            // 1: team t is request t
+  int by_request;       // how the join records are indexed
   int late_wait;        // tables are settled
   int box;              // latent rows: tokens of a tensor copy (divides the page and 64), 0 = none are used
   int q_box;            // latent rows: 1 = Q comes by tensor copies too
   int rows;             // rows of a partial result, min(G, row_tile)
   int row_tile;         // query heads per CTA
   // workspace
-  int2* cuts;           // [teams]: the request that the team's range begins inside of, or -1; and whether that
-                        // request begins behind the start of the range before (its part there is slot 1)
+  int4* joins;          // which requests were cut, see JoinRecord: [R] if by_request, else [teams]
   float2* ml;           // [teams][2][H * gtiles][rows]
   float* part;          // [teams][2][H * gtiles][rows][Dv]
 };
@@ -102,16 +102,22 @@ __device__ __forceinline__ int attend_tiles(int n) { return n / kTileTokens + (n
 struct TeamRange {
   int r, t0;      // first request, and the tile in it to begin with
   int64_t left;   // tiles (uncut: 1, the request)
-  int cut;        // the range begins inside the request
-  int cut_slot;   // ... which begins behind the start of the range before
 };
-struct TeamStart {
+struct TeamStart {  // in shared memory
   int64_t scan[16];
+  int64_t pos;    // the range's start among all tiles
+  int64_t each;   // tiles of a range ...
+  int more;       // ... and how many ranges have one more
   int r, t0;
 };
+// The team whose range holds tile x.
+__device__ __forceinline__ int team_of(const TeamStart& t, int64_t x) {
+  const int64_t wide = t.more * (t.each + 1);
+  return x < wide ? (int)(x / (t.each + 1)) : t.more + (int)((x - wide) / t.each);
+}
 template <int THREADS>
 __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team, TeamStart* s) {
-  TeamRange out = {team, 0, 1, 0, 0};
+  TeamRange out = {team, 0, 1};
   if (p.uncut) return out;
   constexpr int kWarps = THREADS / 32;
   static_assert(kWarps <= 16, "scan holds 16 warps");
@@ -136,11 +142,18 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
     total += s->scan[w];
   }
   const int teams = (int)min((int64_t)p.teams, total);  // no team between two others is without tiles
-  int64_t a = 0, b = 0, prev = 0;
+  int64_t a = 0, b = 0;
   if (team < teams) {
-    a = total * team / teams;
-    b = total * (team + 1) / teams;
-    prev = team > 0 ? total * (team - 1) / teams : 0;
+    const bool narrow = total <= 0xffffffffll;  // a 32-bit division where that will do
+    const int64_t each = narrow ? (uint32_t)total / (uint32_t)teams : total / teams;
+    const int more = (int)(total - each * teams);
+    a = each * team + min(team, more);
+    b = a + each + (team < more ? 1 : 0);
+    if (tid == 0) {
+      s->pos = a;
+      s->each = each;
+      s->more = more;
+    }
   }
   if (a < b && a >= incl - mine && a < incl) {  // exactly one thread
     int64_t at = incl - mine;
@@ -158,16 +171,20 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
   out.r = s->r;
   out.t0 = s->t0;
   out.left = out.r < 0 ? 0 : b - a;
-  out.cut = out.left > 0 && out.t0 > 0;
-  out.cut_slot = a - out.t0 > prev;
   return out;
 }
-// What the joining kernel needs to know of the range's start. Behind the wait for earlier kernels:
-// the join of the call before may still read the workspace until then.
-__device__ __forceinline__ void note_cut(const AttendParams& p, int team, const TeamRange& t) {
-  if (!p.uncut) p.cuts[team] = t.cut ? make_int2(t.r, t.cut_slot) : make_int2(-1, 0);
+// What the joining kernel needs to know of a request that does not end in the team that begins it: its
+// number, that team, which of the team's segments it is (0 the first, else 1), and how many teams hold
+// a part (0: nothing to join). Written by the team that begins the request, behind the wait for earlier
+// kernels: the join of the call before reads the records until then. Indexed by team, a record says
+// what holds for the last request that the team begins: no other can be cut.
+__device__ __forceinline__ void write_join(const AttendParams& p, int r, int team, int slot, int parts) {
+  p.joins[p.by_request ? r : team] = make_int4(r, team, slot, parts);
 }
-
+__device__ __forceinline__ void request_begins(const AttendParams& p, const TeamStart& s, int team, int r, bool first, int64_t done,
+                                               int tiles, bool whole) {
+  write_join(p, r, team, first ? 0 : 1, whole ? 0 : team_of(s, s.pos + done + tiles - 1) - team + 1);
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
   const int n = valid ? 16 : 0;  // 0: nothing is read, the 16 bytes become zero
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -217,14 +234,17 @@ __device__ __forceinline__ void store_io(uint8_t* p, float v, bool bf16) {
     *reinterpret_cast<__half*>(p) = __float2half_rn(v);
 }
 
-__device__ __forceinline__ void store_io2(uint8_t* p, float a, float b, bool bf16) {
-  *reinterpret_cast<uint32_t*>(p) = bf16 ? pack2<true>(a, b) : pack2<false>(a, b);
+__device__ __forceinline__ void store_io4(uint8_t* p, const float4& v, float f, bool bf16) {
+  const uint2 w = bf16 ? make_uint2(pack2<true>(v.x * f, v.y * f), pack2<true>(v.z * f, v.w * f))
+                       : make_uint2(pack2<false>(v.x * f, v.y * f), pack2<false>(v.z * f, v.w * f));
+  *reinterpret_cast<uint2*>(p) = w;
 }
 // Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0.
 template <int THREADS>
 __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, int64_t head0, int rows, bool complain) {
   for (int e = team; e < p.R; e += p.teams) {
     if (visible_tokens(p, e, complain && threadIdx.x == 0).n > 0) continue;
+    if (complain && threadIdx.x == 0 && !p.uncut && p.by_request) write_join(p, e, 0, 0, 0);
     for (int i = threadIdx.x; i < rows * p.Dv; i += THREADS) {
       const int g = i / p.Dv, d = i - g * p.Dv;
       store_io(p.out + e * p.o_req + (head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
@@ -258,7 +278,7 @@ struct AttendShape {
   static constexpr int kCtas = DP == 64 ? 4 : DP == 128 ? 3 : TYPE == kE4m3 ? 2 : 1;  // per SM
   static constexpr int kStages = (kCtas == 4 ? 12288 : kCtas == 3 ? 16384 : kCtas == 2 ? 24576 : 49152) / kStage;
   static constexpr int kSmem = kAttendWarps * kStages * kStage;
-  static_assert(kSmem >= kAttendWarps * kAttendRows * (DP + 2) * 4, "the epilogue reuses the ring");
+  static_assert(kSmem >= kAttendWarps * kAttendRows * (DP + 8 + 2) * 4, "the epilogue reuses the ring");
   static __device__ __forceinline__ uint32_t swizzle(int token, int chunk) {
     const int s = kChunks >= 8 ? (token & 7) : ((token >> 1) & 3);
     return (uint32_t)((chunk ^ s) << 4);
@@ -287,9 +307,10 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
 
   const TeamRange mine = team_range<kAttendThreads>(p, team, &s_team);
   if (p.late_wait) pdl_wait_prior_grid();
-  if (unit == 0 && tid == 0) note_cut(p, team, mine);
   const int64_t q_head0 = (int64_t)h * p.G + g0;
   empty_requests<kAttendThreads>(p, team, q_head0, rows, unit == 0);
+  const bool records = !p.uncut && unit == 0 && tid == 0;
+  if (records && !p.by_request) write_join(p, 0, team, 0, 0);
   if (mine.left == 0) return;
 
   uint8_t* ring = smem + warp * S::kStages * S::kStage;
@@ -314,6 +335,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     }
     const int t1 = p.uncut ? tiles : (int)min((int64_t)tiles, t0 + left);
     left -= p.uncut ? 1 : t1 - t0;
+    if (records && t0 == 0) request_begins(p, s_team, team, r, first, mine.left - left - t1, tiles, t1 == tiles);
 
     // ---- the query rows as fragments ----------------------------------------------------------
     uint32_t qf[kSteps][4];
@@ -570,8 +592,9 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     }
-    float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][DP]
-    float* s_m = s_o + kAttendWarps * kAttendRows * DP;                       // [warp][row]
+    constexpr int kPitch = DP + 8;  // floats: the eight rows of a warp's store start in different banks
+    float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][kPitch]
+    float* s_m = s_o + kAttendWarps * kAttendRows * kPitch;                   // [warp][row]
     float* s_l = s_m + kAttendWarps * kAttendRows;
     if (gc == 0) {
       s_m[warp * kAttendRows + gr] = m[0] - kShift;
@@ -580,21 +603,26 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       s_l[warp * kAttendRows + gr + 8] = l[1];
     }
 #pragma unroll
-    for (int i = 0; i < 2 * kSteps; ++i)
+    for (int i = 0; i < 2; ++i) {
+      if (gr + i * 8 >= rows) continue;
+      float* to = s_o + (warp * kAttendRows + gr + i * 8) * kPitch;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = gr + (e >> 1) * 8, c = gc * 2 + (e & 1);
-        const int col = TYPE == kE4m3 ? (i >> 1) * 16 + c * 2 + (i & 1) : i * 8 + c;
-        if (row < rows) s_o[(warp * kAttendRows + row) * DP + col] = o[i][e];
+      for (int k = 0; k < 2 * kSteps; k += TYPE == kE4m3 ? 2 : 1) {
+        if constexpr (TYPE == kE4m3)  // the tiles of even and of odd columns
+          *reinterpret_cast<float4*>(to + k * 8 + gc * 4) =
+              make_float4(o[k][2 * i], o[k + 1][2 * i], o[k][2 * i + 1], o[k + 1][2 * i + 1]);
+        else
+          *reinterpret_cast<float2*>(to + k * 8 + gc * 2) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
       }
+    }
     __syncthreads();
     const bool whole = t0 == 0 && t1 == tiles;
     const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
-    // a thread takes neighbouring pairs of columns of one row after the other
-    const int pairs = p.Dv / 2;
-    for (int i = tid; i < rows * pairs; i += kAttendThreads) {
-      const int g = i / pairs, d = (i - g * pairs) * 2;
-      float f[kAttendWarps], top = -INFINITY, sum = 0.f, a0 = 0.f, a1 = 0.f;
+    const int quads = p.Dv / 4;
+    for (int i = tid; i < rows * quads; i += kAttendThreads) {
+      const int g = i / quads, d = (i - g * quads) * 4;
+      float f[kAttendWarps], top = -INFINITY, sum = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kAttendWarps; ++w) {
         f[w] = s_m[w * kAttendRows + g];
@@ -604,17 +632,19 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
 #pragma unroll
       for (int w = 0; w < kAttendWarps; ++w) {
         const float c = exp2_approx(f[w] - from);
-        const float2 v = *reinterpret_cast<const float2*>(&s_o[(w * kAttendRows + g) * DP + d]);
+        const float4 v = *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]);
         sum += c * s_l[w * kAttendRows + g];
-        a0 += c * v.x;
-        a1 += c * v.y;
+        acc.x += c * v.x;
+        acc.y += c * v.y;
+        acc.z += c * v.z;
+        acc.w += c * v.w;
       }
       if (whole) {
-        const float inv = p.v_scale / sum;
-        store_io2(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, a0 * inv, a1 * inv, p.io_bf16);
+        const float inv = __fdividef(p.v_scale, sum);
+        store_io4(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc, inv, p.io_bf16);
         if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
       } else {
-        *reinterpret_cast<float2*>(&p.part[(slot * p.rows + g) * p.Dv + d]) = make_float2(a0, a1);
+        *reinterpret_cast<float4*>(&p.part[(slot * p.rows + g) * p.Dv + d]) = acc;
         if (d == 0) p.ml[slot * p.rows + g] = make_float2(top, sum);
       }
     }
@@ -628,30 +658,22 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   }
 }
 
-// Joins the parts of the requests that were cut: the CTAs of the first cut inside a request take it,
-// each up to eight of its rows. First a warp per row turns the parts' maxima and sums into weights,
+// Joins the parts of the requests that were cut, a CTA up to eight rows of one of them. First a warp per row turns the parts' maxima and sums into weights,
 // then every thread adds up four neighbouring columns of a row over the parts; where rows and
 // columns do not fill the CTA, groups of threads take every other part and are added up at the end,
 // always in the same order.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 8;
 constexpr int kJoinParts = 640;  // more teams than a launch has
-__global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(const AttendParams p) {
   __shared__ float s_w[kJoinRows][kJoinParts];
   __shared__ float4 s_acc[kJoinThreads];
   pdl_wait_prior_grid();
   pdl_release_next_grid();
-  const int team = blockIdx.x + 1, unit = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int2 cut = p.cuts[team];
-  if (cut.x < 0 || p.cuts[team - 1].x == cut.x) return;  // no cut here, or not the request's first
-  int parts = 1;  // the part before the cut, and the ranges that begin inside the request, which follow each other
-  for (int base = team; base < p.teams; base += kJoinThreads) {
-    const int t = base + tid;
-    const int n = __syncthreads_count(t < p.teams && p.cuts[t].x == cut.x);
-    parts += n;
-    if (n < kJoinThreads) break;
-  }
-  const int r = cut.x, units = gridDim.y;
+  const int unit = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int4 rec = p.joins[blockIdx.x];  // JoinRecord
+  const int r = rec.x, team = rec.y, parts = rec.w, units = gridDim.y;
+  if (parts == 0) return;
   const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * p.row_tile;
   const int all_rows = min(p.G - g0, p.row_tile);
   const int per = (p.rows + gridDim.z - 1) / gridDim.z;  // at most kJoinRows
@@ -659,10 +681,23 @@ __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const A
   if (rows <= 0) return;
   const int64_t q_head0 = (int64_t)h * p.G + g0 + row0;
   // row `row0` of part k; the parts but the first lie at a constant stride
-  const int64_t slot0 = (((int64_t)(team - 1) * 2 + cut.y) * units + unit) * p.rows + row0;
-  const int64_t slot1 = ((int64_t)team * 2 * units + unit) * p.rows + row0, step = 2ll * units * p.rows;
+  const int64_t slot0 = (((int64_t)team * 2 + rec.z) * units + unit) * p.rows + row0;
+  const int64_t slot1 = ((int64_t)(team + 1) * 2 * units + unit) * p.rows + row0, step = 2ll * units * p.rows;
   auto slot = [&](int k) -> int64_t { return k == 0 ? slot0 : slot1 + (k - 1) * step; };
 
+  const int quads = p.Dv / 4, items = rows * quads;  // quads: at most 128
+  const int groups = max(kJoinThreads / items, 1), group = groups > 1 ? tid / items : 0;
+  // Item i: columns 4 quad .. of row g; a thread's first item is loaded while the weights are formed.
+  auto part_of = [&](int i) { return p.part + (int64_t)(i / quads) * p.Dv + (i % quads) * 4; };
+  constexpr int kAhead = 4;
+  float4 ahead[kAhead];
+  const int item0 = tid - group * items;
+  const bool mine = group < groups && item0 < items;
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const int k = group + j * groups;
+    if (mine && k < parts) ahead[j] = *reinterpret_cast<const float4*>(part_of(item0) + slot(k) * p.Dv);
+  }
   for (int g = warp; g < rows; g += kJoinThreads / 32) {
     float top = -INFINITY;
     for (int k = lane; k < parts; k += 32) top = fmaxf(top, p.ml[slot(k) + g].x);
@@ -686,45 +721,34 @@ __global__ void __launch_bounds__(kJoinThreads) topkv_attend_join_kernel(const A
   }
   __syncthreads();
 
-  const int quads = p.Dv / 4, items = rows * quads;  // quads: at most 128
-  auto add_parts = [&](int i, int first, int by) {
-    const int g = i / quads, quad = i - g * quads;
-    const float* from = p.part + (int64_t)g * p.Dv + quad * 4;
+  auto add = [](float4& acc, const float4& v, float f) {
+    acc.x += f * v.x;
+    acc.y += f * v.y;
+    acc.z += f * v.z;
+    acc.w += f * v.w;
+  };
+  for (int i = item0; mine && i < items; i += kJoinThreads) {
+    const int g = i / quads;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    int k = group;
+    if (i == item0) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j, k += groups)
+        if (k < parts) add(acc, ahead[j], s_w[g][k]);
+    }
 #pragma unroll 4
-    for (int k = first; k < parts; k += by) {
-      const float4 v = *reinterpret_cast<const float4*>(from + slot(k) * p.Dv);
-      const float f = s_w[g][k];
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
-    }
-    return acc;
-  };
-  auto finish = [&](int i, float4 acc) {
-    const int g = i / quads, quad = i - g * quads;
-    uint8_t* to = p.out + r * p.o_req + (q_head0 + g) * p.o_head + quad * 8;
-    store_io2(to, acc.x, acc.y, p.io_bf16);
-    store_io2(to + 4, acc.z, acc.w, p.io_bf16);
-  };
-  if (items >= kJoinThreads) {
-    for (int i = tid; i < items; i += kJoinThreads) finish(i, add_parts(i, 0, 1));
-    return;
+    for (; k < parts; k += groups) add(acc, *reinterpret_cast<const float4*>(part_of(i) + slot(k) * p.Dv), s_w[g][k]);
+    if (groups > 1)
+      s_acc[tid] = acc;
+    else
+      store_io4(p.out + r * p.o_req + (q_head0 + g) * p.o_head + (i % quads) * 8, acc, 1.f, p.io_bf16);
   }
-  const int groups = kJoinThreads / items, group = tid / items;
-  if (group < groups) s_acc[tid] = add_parts(tid - group * items, group, groups);
+  if (groups == 1) return;
   __syncthreads();
-  if (group == 0) {
+  if (tid < items) {
     float4 acc = s_acc[tid];
-    for (int k = 1; k < groups; ++k) {
-      const float4 v = s_acc[k * items + tid];
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
-    }
-    finish(tid, acc);
+    for (int k = 1; k < groups; ++k) add(acc, s_acc[k * items + tid], 1.f);
+    store_io4(p.out + r * p.o_req + (q_head0 + tid / quads) * p.o_head + (tid % quads) * 8, acc, 1.f, p.io_bf16);
   }
 }
 

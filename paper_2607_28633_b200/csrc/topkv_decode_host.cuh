@@ -62,6 +62,7 @@ struct AttendPlan {
   int rows;         // rows of a partial result
   int dv;
   int teams;
+  int joins;        // join records: one per request or per team, whichever are fewer
   bool uncut;
   int64_t bytes;    // of the workspace
 };
@@ -135,7 +136,8 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   plan->bytes = 0;
   if (!plan->uncut) {
     const int64_t slots = 2ll * plan->teams * plan->units * plan->rows;
-    plan->bytes = ((int64_t)plan->teams * 8 + 15) / 16 * 16 + slots * 8 + slots * plan->dv * 4;
+    plan->joins = std::min(plan->teams, b->num_requests);
+    plan->bytes = (int64_t)plan->joins * 16 + slots * 8 + slots * plan->dv * 4;
     plan->bytes = (plan->bytes + 255) / 256 * 256;
   }
   return TOPKV_OK;
@@ -385,8 +387,9 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   if (!plan.uncut) {
     uint8_t* w = static_cast<uint8_t*>(d_workspace);
     const int64_t slots = 2ll * plan.teams * plan.units * plan.rows;
-    p.cuts = reinterpret_cast<int2*>(w);
-    w += ((int64_t)plan.teams * 8 + 15) / 16 * 16;
+    p.joins = reinterpret_cast<int4*>(w);
+    p.by_request = plan.joins == p.R;
+    w += (int64_t)plan.joins * 16;
     p.ml = reinterpret_cast<float2*>(w);
     p.part = reinterpret_cast<float*>(w + slots * 8);
   }
@@ -401,9 +404,9 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
     st = launch_attend_dim<kE4m3>(p, plan.units, s);
   if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
   // about eight CTAs per SM for the requests that can be cut
-  const int64_t cuts = (int64_t)std::min(plan.teams - 1, p.R) * plan.units;
+  const int64_t cuts = (int64_t)plan.joins * plan.units;
   const unsigned z = (unsigned)std::max((plan.rows + kJoinRows - 1) / kJoinRows, (int)std::min<int64_t>(plan.rows, 8 * 148 / cuts));
-  return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.teams - 1, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
+  return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.joins, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
 }
 
 int64_t topkv_page_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch, int32_t num_forks) {

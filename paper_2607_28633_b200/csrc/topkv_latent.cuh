@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = ctl.tmem;
-  if (unit == 0 && tid == 0) note_cut(p, team, mine);
+  const bool records = !p.uncut && unit == 0 && tid == 0;
+  if (records && !p.by_request) write_join(p, 0, team, 0, 0);
   empty_requests<kLatentThreads>(p, team, (int64_t)g0, rows, unit == 0);
 
   // Waits until the barrier has completed its phase number `phase` (0, 1, 2, ...).
@@ -302,6 +303,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     const int t1 = p.uncut ? tiles : (int)min((int64_t)tiles, t0 + left);
     const int count = t1 - t0;
     left -= p.uncut ? 1 : count;
+    if (records && t0 == 0) request_begins(p, ctl.team, team, r, first, n, tiles, t1 == tiles);
 
     if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoadWarps) {
       // ---- load: pair `g` of warps takes the stages g of its own parity ---------------------------
