@@ -134,6 +134,15 @@ __device__ __forceinline__ void proxy_fence_smem() { asm volatile("fence.proxy.a
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Barrier `id` of `threads` threads; whether the predicate holds for any of them.
+__device__ __forceinline__ bool bar_any(int id, int threads, bool pred) {
+  uint32_t r;
+  asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %3, 0; bar.red.or.pred q, %1, %2, p; selp.u32 %0, 1, 0, q; }"
+               : "=r"(r)
+               : "r"(id), "r"(threads), "r"((uint32_t)pred)
+               : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
@@ -192,15 +201,16 @@ constexpr uint32_t kOperandHi = 1024 >> 4 | 1u << 14 | 2u << 29;
 // Layout of the dynamic shared memory. All operand blocks are multiples of 1,024 bytes.
 struct LatentControl {
   float red[2 * 4 * 64];  // maxima and sums per quarter of TMEM and head, by turns
-  uint64_t bar[14];
+  uint64_t bar[15];
   TeamStart team;
   uint32_t valid[2][2];   // which of a stage's tokens count
   uint32_t tmem;
   volatile int dead;      // a wait ran out
 };
 struct LatentSmem {
-  uint32_t q, kv, p, control, total;
-  uint32_t stage;  // bytes of a stage
+  uint32_t q, kv, control, total;
+  uint32_t p, p_step;  // weights of the first stage's tile, and from there to the second's
+  uint32_t stage;      // bytes of a stage
 };
 __host__ __device__ inline LatentSmem latent_smem(int N, int D, int Dv) {
   const int blocks = (D + 63) / 64, vblocks = (Dv + 127) / 128 * 2;
@@ -208,8 +218,12 @@ __host__ __device__ inline LatentSmem latent_smem(int N, int D, int Dv) {
   s.stage = (uint32_t)((blocks > vblocks ? blocks : vblocks) * kLatentBlock);
   s.q = 0;
   s.kv = (uint32_t)(blocks * N * 128);
-  s.p = s.kv + 2 * s.stage;
-  s.control = s.p + kLatentTile * 128;
+  // The weights of a tile (64 tokens x 128 bytes) take the place of its first block behind the values,
+  // which only the scores need; rows without such a block get two buffers.
+  const bool inside = blocks > vblocks;
+  s.p = s.kv + (inside ? (uint32_t)(vblocks * kLatentBlock) : 2 * s.stage);
+  s.p_step = inside ? s.stage : (uint32_t)kLatentBlock;
+  s.control = s.kv + 2 * s.stage + (inside ? 0 : 2 * kLatentBlock);
   s.total = s.control + (uint32_t)sizeof(LatentControl);
   return s;
 }
@@ -238,20 +252,20 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
   const int ksteps = (p.D + 15) / 16, vblocks = (p.Dv + 127) / 128;
   const int blocks = (p.D + 63) / 64;
   // Barriers. The blocks of a stage are given up in groups, one per 128 value columns (the blocks
-  // behind the values belong to the first): a group is loaded again while the products of the next
-  // one still run.
-  //   rows loaded [2], rows used [2][4], scores ready [2], weights written, Q written
+  // behind the values, which hold the weights by then, belong to the last): a group is loaded again
+  // while the products of the next one still run.
+  //   rows loaded [2], rows used [2][4], scores ready [2], weights written [2], Q written
   const uint32_t bar0 = smem_addr(ctl.bar);
-  const uint32_t b_full = bar0, b_free = bar0 + 16, b_score = bar0 + 80, b_weight = bar0 + 96, b_query = bar0 + 104;
+  const uint32_t b_full = bar0, b_free = bar0 + 16, b_score = bar0 + 80, b_weight = bar0 + 96, b_query = bar0 + 112;
   const int last = vblocks - 1;  // the group whose products come last
   if (tid == 0) {
     s_dead = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(b_full + 8 * i, 64);
       mbar_init(b_score + 8 * i, 1);
+      mbar_init(b_weight + 8 * i, kSoftmaxWarps * 32);
     }
     for (int i = 0; i < 8; ++i) mbar_init(b_free + 8 * i, 1);
-    mbar_init(b_weight, kSoftmaxWarps * 32);
     mbar_init(b_query, p.q_box ? 1 : kSoftmaxWarps * 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -334,7 +348,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
           // ctl.valid of the tile before has been read when its products begin
           if (k >= 2) wait(b_free + 32 * g, (k >> 1) - 1);
           // both warps come to the same answer; each takes every other group
-          int own = half == 0 ? max(blocks - 2 * vblocks, 0) : 0;  // blocks that this warp brings
+          int own = half == (last & 1) ? max(blocks - 2 * vblocks, 0) : 0;  // blocks that this warp brings
           for (int v = half; v < vblocks; v += 2) own += min(2, blocks - 2 * v);
           if (lane == 0) {
             ctl.valid[g][half] = 0xffffffffu;
@@ -354,7 +368,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
                 };
                 bring(2 * v);
                 if (2 * v + 1 < blocks) bring(2 * v + 1);
-                if (v == 0)
+                if (v == last)
                   for (int b = 2 * vblocks; b < blocks; ++b) bring(b);
               }
               __syncwarp();
@@ -423,7 +437,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         __syncwarp();
       }
       wait(b_query, seg);
-      const uint32_t q0 = operand_lo(base + lay.q, 16), p0 = operand_lo(base + lay.p, kLatentBlock);
+      const uint32_t q0 = operand_lo(base + lay.q, 16), p00 = operand_lo(base + lay.p, kLatentBlock);
       const long long began = clock64();
       uint32_t polls = 0;
       for (int is = 0, iv = 0; iv < count;) {
@@ -446,10 +460,10 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
           }
           __syncwarp();
           ++is;
-        } else if (iv < is && __all_sync(0xffffffffu, mbar_test(b_weight, kv & 1))) {
+        } else if (iv < is && __all_sync(0xffffffffu, mbar_test(b_weight + 8 * (kv & 1), kv >> 1 & 1))) {
           const uint32_t st = kv & 1;
           tcgen05_after_sync();
-          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, kLatentBlock);
+          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, kLatentBlock), p0 = p00 + st * (lay.p_step >> 4);
           if (elect_one()) {
 #pragma unroll 4
             for (int v = 0; v < vblocks; ++v) {
@@ -494,9 +508,12 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       // A thread's scores: columns c0 + 8 i + 2 (lane % 4) + e of tokens row and row + 8.
       const int row = quarter * 16 + (lane >> 2);
       const int mine_col = column_of<C>(lane);
-      float sum[C];
+      float sum[C], from[C], limit[C];  // per column: what is subtracted, and up to where that will do
 #pragma unroll
-      for (int j = 0; j < C; ++j) sum[j] = 0.f;
+      for (int j = 0; j < C; ++j) {
+        sum[j] = from[j] = 0.f;
+        limit[j] = -INFINITY;
+      }
       float top = -INFINITY;  // of head c0 + lane (lane < NC)
       for (int i = 0; i < count; ++i) {
         const uint32_t k = n + i, st = k & 1;
@@ -508,56 +525,66 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         const uint32_t valid = ctl.valid[st][quarter >> 1] >> ((quarter & 1) * 16 + (lane >> 2));
         const bool seen0 = valid & 1, seen1 = valid >> 8 & 1;
         tmem_wait_load();
-        float x[2 * C], most[C];
+        float x[2 * C], e[2 * C];
+        bool over = false;
 #pragma unroll
         for (int j = 0; j < C; ++j) {  // j = 2 i + e; x[2 j] and x[2 j + 1] are the two tokens
           x[2 * j] = seen0 ? __uint_as_float(raw[(j >> 1) * 4 + (j & 1)]) * p.qk_scale : -INFINITY;
           x[2 * j + 1] = seen1 ? __uint_as_float(raw[(j >> 1) * 4 + (j & 1) + 2]) * p.qk_scale : -INFINITY;
-          most[j] = fmaxf(x[2 * j], x[2 * j + 1]);
+          over |= fmaxf(x[2 * j], x[2 * j + 1]) > limit[j];
+          e[2 * j] = exp2_approx(x[2 * j] - from[j]);
+          e[2 * j + 1] = exp2_approx(x[2 * j + 1] - from[j]);
         }
-        const float tile_top = join_rows<C>(most, lane, [](float a, float b) { return fmaxf(a, b); });
-        float* const red = s_red + (k & 1) * 4 * N;
-        red[quarter * N + c0 + mine_col] = tile_top;
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");  // the four warps of these heads
-        bool moved = false;
+        // Most tiles stay below the limits: one vote of the four warps that share these heads, and
+        // nothing is exchanged. Otherwise they find the new maxima together.
+        bool rescale = false;
         float alpha = 1.f;
-        if (lane < NC) {
-          const int c = c0 + lane;
-          const float m = fmaxf(fmaxf(red[c], red[N + c]), fmaxf(red[2 * N + c], red[3 * N + c]));
-          if (m > top + kLazy) {
-            moved = true;
-            alpha = exp2_approx(top - m);
-            top = m;
-          }
-        }
-        const bool rescale = __any_sync(0xffffffffu, moved);
-        const float from = top == -INFINITY ? 0.f : top - kShift;
-        if (rescale) {
+        if (bar_any(1 + half, kSoftmaxWarps * 16, over)) {
+          float most[C];
 #pragma unroll
-          for (int j = 0; j < C; ++j) sum[j] *= __shfl_sync(0xffffffffu, alpha, (j >> 1) * 8 + (lane & 3) * 2 + (j & 1));
+          for (int j = 0; j < C; ++j) most[j] = fmaxf(x[2 * j], x[2 * j + 1]);
+          const float tile_top = join_rows<C>(most, lane, [](float a, float b) { return fmaxf(a, b); });
+          float* const red = s_red + (k & 1) * 4 * N;
+          red[quarter * N + c0 + mine_col] = tile_top;
+          asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");
+          bool moved = false;
+          if (lane < NC) {
+            const int c = c0 + lane;
+            const float m = fmaxf(fmaxf(red[c], red[N + c]), fmaxf(red[2 * N + c], red[3 * N + c]));
+            if (m > top + kLazy) {
+              moved = true;
+              alpha = exp2_approx(top - m);
+              top = m;
+            }
+          }
+          rescale = __any_sync(0xffffffffu, moved);
+          const float lane_from = top == -INFINITY ? 0.f : top - kShift;
+#pragma unroll
+          for (int j = 0; j < C; ++j) {
+            const int col = (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
+            sum[j] *= __shfl_sync(0xffffffffu, alpha, col);
+            from[j] = __shfl_sync(0xffffffffu, lane_from, col);
+            limit[j] = __shfl_sync(0xffffffffu, top, col) + kLazy;
+            e[2 * j] = exp2_approx(x[2 * j] - from[j]);
+            e[2 * j + 1] = exp2_approx(x[2 * j + 1] - from[j]);
+          }
         }
         uint32_t w[C];  // w[2 i], w[2 i + 1]: the pair of columns, of the two tokens
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-          const float f = __shfl_sync(0xffffffffu, from, (j >> 1) * 8 + (lane & 3) * 2 + (j & 1));
-          x[2 * j] = exp2_approx(x[2 * j] - f);
-          x[2 * j + 1] = exp2_approx(x[2 * j + 1] - f);
-          sum[j] += x[2 * j] + x[2 * j + 1];
+        for (int j = 0; j < C; ++j) sum[j] += e[2 * j] + e[2 * j + 1];
+#pragma unroll
+        for (int j = 0; j < C; j += 2) {
+          w[j] = pack2<BF16>(e[2 * j], e[2 * j + 2]);
+          w[j + 1] = pack2<BF16>(e[2 * j + 1], e[2 * j + 3]);
         }
 #pragma unroll
         for (int j = 0; j < C; j += 2) {
-          w[j] = pack2<BF16>(x[2 * j], x[2 * j + 2]);
-          w[j + 1] = pack2<BF16>(x[2 * j + 1], x[2 * j + 3]);
-        }
-        // the second product of the tile before has to be done with the weights and the accumulator
-        if (k > 0) wait(b_free + 32 * (st ^ 1) + 8 * last, (k - 1) >> 1);
-#pragma unroll
-        for (int j = 0; j < C; j += 2) {
-          uint8_t* to = smem + lay.p + row * 128 + (((half * (NC / 8) + j / 2) ^ (row & 7)) << 4) + (lane & 3) * 4;
+          uint8_t* to = smem + lay.p + st * lay.p_step + row * 128 + (((half * (NC / 8) + j / 2) ^ (row & 7)) << 4) + (lane & 3) * 4;
           *reinterpret_cast<uint32_t*>(to) = w[j];
           *reinterpret_cast<uint32_t*>(to + 8 * 128) = w[j + 1];  // row + 8: the same place of its swizzle
         }
         if (rescale && i > 0) {
+          wait(b_free + 32 * (st ^ 1) + 8 * last, (k - 1) >> 1);  // the products of the tile before are in
           tcgen05_after_sync();
           for (int b = 0; b < vblocks; ++b) {
             uint32_t o[NC];
@@ -572,7 +599,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         }
         proxy_fence_smem();
         tcgen05_before_sync();
-        bar_arrive(b_weight);
+        bar_arrive(b_weight + 8 * st);
       }
       // ---- the segment's result -----------------------------------------------------------------------
       wait(b_free + 32 * ((n + count - 1) & 1) + 8 * last, (n + count - 1) >> 1);
