@@ -23,7 +23,7 @@
 //   warps 8-11  load: two stages of 64 rows, one pair of warps each, through the block table: tensor
 //               copies for full tiles, 16-byte copies for the rest (any page size and stride;
 //               what is masked becomes zero)
-//   warp 12     one thread issues the matrix instructions
+//   warps 12, 13 one thread each issues the matrix instructions of the first and of the second product
 // Running maxima move only when a tile exceeds them by more than 2^8, so the accumulator is rescaled
 // a few times per request and not once per tile; the weights are at most 2^8 (fp16: scaled by
 // 2^7, to stay below 2^15), which costs no precision in a floating type.
@@ -42,7 +42,8 @@ namespace topkv {
 constexpr int kLatentTile = 64;                  // tokens per tile
 static_assert(kLatentTile == kTileTokens, "both kernels share out tiles of the same size");
 constexpr int kSoftmaxWarps = 8, kLoadWarps = 4;
-constexpr int kLatentThreads = (kSoftmaxWarps + kLoadWarps + 1) * 32;
+constexpr int kScoreWarp = kSoftmaxWarps + kLoadWarps, kValueWarp = kScoreWarp + 1;
+constexpr int kLatentThreads = (kValueWarp + 1) * 32;
 constexpr int kLatentBlock = kLatentTile * 128;  // bytes of 64 columns of a tile
 constexpr int kLatentMaxD = 576, kLatentMaxDv = 512;
 constexpr long long kWaitClocks = 1000000000ll;  // about half a second
@@ -142,14 +143,6 @@ __device__ __forceinline__ bool bar_any(int id, int threads, bool pred) {
                : "r"(id), "r"(threads), "r"((uint32_t)pred)
                : "memory");
   return r != 0;
-}
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
-               : "=r"(ok)
-               : "r"(bar), "r"(parity)
-               : "memory");
-  return ok != 0;
 }
 // Box of the tensor map at (x, y, z) into shared memory (bytes counted by the barrier), or into L2 only.
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -269,7 +262,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     mbar_init(b_query, p.q_box ? 1 : kSoftmaxWarps * 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kSoftmaxWarps + kLoadWarps) {
+  if (warp == kScoreWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "n"(kCols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -300,6 +293,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     }
   };
 
+  constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
   uint32_t n = 0;    // tiles before the current segment, in this CTA: they number the phases
   uint32_t seg = 0;  // segments before
   int64_t left = mine.left;  // 0: no tiles
@@ -418,18 +412,15 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         proxy_fence_smem();
         bar_arrive(b_full + 8 * g);
       }
-    } else if (warp == kSoftmaxWarps + kLoadWarps) {
-      // ---- matrix instructions ----------------------------------------------------------------------
-      // Scores of the next tile as soon as it is there, values of the one before as soon as its
-      // weights are: whichever comes first, so that a late load never holds up the tile whose rows
-      // have to be used before the next load can start. The descriptors are formed by the whole warp
-      // and one thread issues: from inside a branch of one thread each instruction took 70 cycles to
-      // issue, where the tensor core needs 35 (64 x 64) to 51 (128 x 64) for it.
-      constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
-      constexpr uint32_t kScore = kType | 4u << 24;                        // M = 64, both K-major
-      constexpr uint32_t kValue = kType | 1u << 15 | 1u << 16 | 8u << 24;  // M = 128, M- and N-major
-      // Every score product of the segment before has been waited for, through its weights.
+    } else if (warp == kScoreWarp) {
+      // ---- scores -------------------------------------------------------------------------------------
+      // The descriptors are formed by the whole warp and one elected thread issues: from inside a branch
+      // of one thread each instruction took 70 cycles to issue, where the tensor core needs 35
+      // (64 x 64) to 51 (128 x 64) for it. Two warps, one per product: one warp that takes whichever is
+      // ready next lost 350 cycles from one product to the other.
+      constexpr uint32_t kScore = kType | 4u << 24;  // M = 64, both K-major
       if (p.q_box) {
+        if (n > 0) wait(b_score + 8 * ((n - 1) & 1), (n - 1) >> 1);  // Q of the segment before is done with
         if (elect_one()) {
           mbar_expect_tx(b_query, (uint32_t)(blocks * N * 128));
           for (int b = 0; b < blocks; ++b) tma_load(base + lay.q + b * (N * 128), &q_map, b * 64, g0, p.q_req > 0 ? r : 0, b_query);
@@ -437,52 +428,49 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         __syncwarp();
       }
       wait(b_query, seg);
-      const uint32_t q0 = operand_lo(base + lay.q, 16), p00 = operand_lo(base + lay.p, kLatentBlock);
-      const long long began = clock64();
-      uint32_t polls = 0;
-      for (int is = 0, iv = 0; iv < count;) {
-        const uint32_t ks = n + is, kv = n + iv;
-        if (is < count && is < iv + 2 && __all_sync(0xffffffffu, mbar_test(b_full + 8 * (ks & 1), ks >> 1 & 1))) {
-          const uint32_t st = ks & 1;
-          tcgen05_after_sync();
-          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, 16);
-          const uint32_t d = tmem + st * N;
-          if (elect_one()) {
+      const uint32_t q0 = operand_lo(base + lay.q, 16);
+      for (int i = 0; i < count; ++i) {
+        const uint32_t k = n + i, st = k & 1;
+        if (k >= 2) wait(b_weight + 8 * st, (k >> 1) - 1);  // the scores two tiles before have been read
+        wait(b_full + 8 * st, k >> 1);
+        if (s_dead) break;
+        tcgen05_after_sync();
+        const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, 16);
+        const uint32_t d = tmem + st * N;
+        if (elect_one()) {
 #pragma unroll 3
-            for (int b = 0; b < ksteps / 4; ++b)
+          for (int b = 0; b < ksteps / 4; ++b)
 #pragma unroll
-              for (int u = 0; u < 4; ++u)
-                tcgen05_mma(d, a0 + b * (kLatentBlock >> 4) + 2 * u, q0 + b * (N * 128 >> 4) + 2 * u, kOperandHi, kScore, b + u > 0);
-            for (int s = ksteps & ~3; s < ksteps; ++s)
-              tcgen05_mma(d, a0 + (s >> 2) * (kLatentBlock >> 4) + 2 * (s & 3), q0 + (s >> 2) * (N * 128 >> 4) + 2 * (s & 3), kOperandHi,
-                          kScore, s > 0);
-            tcgen05_commit(b_score + 8 * st);
-          }
-          __syncwarp();
-          ++is;
-        } else if (iv < is && __all_sync(0xffffffffu, mbar_test(b_weight + 8 * (kv & 1), kv >> 1 & 1))) {
-          const uint32_t st = kv & 1;
-          tcgen05_after_sync();
-          const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, kLatentBlock), p0 = p00 + st * (lay.p_step >> 4);
-          if (elect_one()) {
-#pragma unroll 4
-            for (int v = 0; v < vblocks; ++v) {
-#pragma unroll
-              for (int u = 0; u < kLatentTile / 16; ++u)
-                tcgen05_mma(tmem + 2 * N + v * N, a0 + v * (2 * kLatentBlock >> 4) + 128 * u, p0 + 128 * u, kOperandHi, kValue,
-                            iv > 0 || u > 0);
-              tcgen05_commit(b_free + 32 * st + 8 * v);
-            }
-          }
-          __syncwarp();
-          ++iv;
-        } else if ((++polls & 255) == 0 && __any_sync(0xffffffffu, s_dead || clock64() - began > kWaitClocks * (count + 1))) {
-          if (lane == 0 && !s_dead) {
-            s_dead = 1;
-            raise_error(kErrWait);
-          }
-          break;
+            for (int u = 0; u < 4; ++u)
+              tcgen05_mma(d, a0 + b * (kLatentBlock >> 4) + 2 * u, q0 + b * (N * 128 >> 4) + 2 * u, kOperandHi, kScore, b + u > 0);
+          for (int s = ksteps & ~3; s < ksteps; ++s)
+            tcgen05_mma(d, a0 + (s >> 2) * (kLatentBlock >> 4) + 2 * (s & 3), q0 + (s >> 2) * (N * 128 >> 4) + 2 * (s & 3), kOperandHi,
+                        kScore, s > 0);
+          tcgen05_commit(b_score + 8 * st);
         }
+        __syncwarp();
+      }
+    } else if (warp == kValueWarp) {
+      // ---- values -------------------------------------------------------------------------------------
+      constexpr uint32_t kValue = kType | 1u << 15 | 1u << 16 | 8u << 24;  // M = 128, M- and N-major
+      const uint32_t p00 = operand_lo(base + lay.p, kLatentBlock);
+      for (int i = 0; i < count; ++i) {
+        const uint32_t k = n + i, st = k & 1;
+        wait(b_weight + 8 * st, k >> 1);
+        if (s_dead) break;
+        tcgen05_after_sync();
+        const uint32_t a0 = operand_lo(base + lay.kv + st * lay.stage, kLatentBlock), p0 = p00 + st * (lay.p_step >> 4);
+        if (elect_one()) {
+#pragma unroll 4
+          for (int v = 0; v < vblocks; ++v) {
+#pragma unroll
+            for (int u = 0; u < kLatentTile / 16; ++u)
+              tcgen05_mma(tmem + 2 * N + v * N, a0 + v * (2 * kLatentBlock >> 4) + 128 * u, p0 + 128 * u, kOperandHi, kValue,
+                          i > 0 || u > 0);
+            tcgen05_commit(b_free + 32 * st + 8 * v);
+          }
+        }
+        __syncwarp();
       }
     } else {
       // ---- softmax ------------------------------------------------------------------------------------
@@ -653,7 +641,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
   }
   tcgen05_before_sync();
   __syncthreads();
-  if (warp == kSoftmaxWarps + kLoadWarps)
+  if (warp == kScoreWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols) : "memory");
 }
 
