@@ -5,8 +5,10 @@ layer's slab to pinned host memory with the checksummed host leg, and at the end
 128-byte header per request (§3.4). ``TransferReceiver`` is the decode side: it places every
 layer from the host slab into its own paged pool, checksumming as it goes, and checks the
 headers when the last layer is in; a mismatch is reported per request so that the caller can
-retry (§3.1). Both only issue library calls on the streams they are given: no pack / unpack
-arithmetic happens in Python, and nothing here touches the CPU oracle.
+retry (§3.1). ``DecodeCache`` is what the decode side does next with the pool it has received:
+it gives new tokens their pages, writes their K/V, attends to the cache, forks and frees
+requests and compacts the pool. All of them only issue library calls on the streams they are
+given: no pack / unpack arithmetic happens in Python, and nothing here touches the CPU oracle.
 """
 from __future__ import annotations
 
@@ -102,6 +104,82 @@ class TransferReceiver(Endpoint):
             crc_v = int(crc[r, 1]) if self.layout.kv_factor == 2 else 0
             out.append(tk.topkv_header_check(h, self.layout, int(h_seq_lens[r]), int(crc[r, 0]), crc_v))
         return out
+
+
+class DecodeCache:
+    """The paged cache of a decode worker, from the tables of a receiver (or any pool and tables):
+    ``rows`` request slots of ``max_pages`` pages each, of which the first ones hold the requests
+    that have arrived. All tables live on the device and are changed in place by the calls below,
+    which only enqueue work on ``stream``; calls are ordered by the stream they are given, and one
+    object's calls must not run at the same time (they share a workspace). ``max_forks`` bounds
+    the forks of one call."""
+
+    def __init__(self, pool: torch.Tensor, layout: tk.topkv_layout, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                 rows: int | None = None, max_pages: int | None = None, max_forks: int = 64):
+        dev = pool.device
+        R, maxp = block_table.shape
+        rows, max_pages = R if rows is None else rows, maxp if max_pages is None else max_pages
+        if rows < R or max_pages < maxp:
+            raise ValueError("rows and max_pages must hold the tables that are taken over")
+        self.pool, self.layout, self.max_forks = pool, layout, max_forks
+        self.block_table = torch.full((rows, max_pages), -1, dtype=torch.int32, device=dev)
+        self.block_table[:R, :maxp] = block_table
+        self.seq_lens = torch.zeros(rows, dtype=torch.int32, device=dev)
+        self.seq_lens[:R] = seq_lens
+        used = torch.arange(max_pages, device=dev)[None, :] * layout.page_tokens < self.seq_lens[:, None]
+        self.block_table.masked_fill_(~used, -1)
+        self.ref_counts = torch.bincount(self.block_table[used].long(), minlength=layout.num_pool_pages).to(torch.int32)
+        self.batch = tk.make_batch(self.block_table, self.seq_lens)
+        self.tables = tk.make_page_tables(self.ref_counts, self.block_table, self.seq_lens, self.ref_counts)
+        n = tk.check(tk.topkv_page_workspace_bytes(layout, self.batch, max_forks))
+        self.workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+        self.num_used = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.page_map = torch.zeros(layout.num_pool_pages, dtype=torch.int32, device=dev)
+        self._attend_ws = None
+        torch.cuda.current_stream(dev).synchronize()
+
+    def extend(self, new_tokens: torch.Tensor, stream):
+        """Room for new_tokens[r] (device int32 [rows]) more tokens of every request."""
+        tk.check(tk.topkv_extend_requests(self.layout, self.batch, self.tables, new_tokens, self.workspace,
+                                          self.workspace.numel(), stream))
+
+    def append(self, layer: int, kv: torch.Tensor, stream, tokens: int = 1):
+        """Writes the K/V of the last ``tokens`` tokens of every request: ``kv`` is a wire slab of
+        min(length, tokens) tokens per request, in request order (empty rows contribute none)."""
+        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens)
+        at = layer * self.layout.wire_layer_stride  # the call adds it: kv is this layer's slab alone
+        tk.check(tk.topkv_unpack_layer(layer, self.pool, self.layout, b, kv.data_ptr() - at, kv.numel() * kv.element_size() + at,
+                                       stream))
+
+    def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
+               window_tokens: int = 0, **attention):
+        """Attention of the newest token of every request; see topkv_attend_layer. ``attention`` goes
+        to make_attention (value_dim, sink_tokens, k_scale, v_scale, lse)."""
+        io = tk.TOPKV_TYPE_BF16 if q.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
+        att = tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
+        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=window_tokens)
+        n = tk.check(tk.topkv_attend_workspace_bytes(self.layout, b, att))
+        if self._attend_ws is None or self._attend_ws.numel() < n:
+            # on its stream, so that the buffer it replaces is not handed out while a call still uses it
+            with torch.cuda.stream(stream):
+                self._attend_ws = torch.empty(max(n, 16), dtype=torch.uint8, device=self.pool.device)
+        tk.check(tk.topkv_attend_layer(layer, self.pool, self.layout, b, att, q, out, self._attend_ws,
+                                       self._attend_ws.numel(), stream))
+
+    def fork(self, parents: torch.Tensor, children: torch.Tensor, stream):
+        """Row children[i] becomes a copy of row parents[i] that shares its full pages."""
+        if parents.numel() != children.numel() or parents.numel() > self.max_forks:
+            raise ValueError("as many parents as children, at most max_forks")
+        tk.check(tk.topkv_fork_requests(self.pool, self.layout, self.batch, self.tables, parents, children, parents.numel(),
+                                        self.workspace, self.workspace.numel(), stream))
+
+    def free(self, rows: torch.Tensor, stream):
+        tk.check(tk.topkv_free_requests(self.layout, self.batch, self.tables, rows, rows.numel(), stream))
+
+    def compact(self, stream):
+        """Afterwards pages 0 .. num_used - 1 are the ones in use; page_map has every page's new id."""
+        tk.check(tk.topkv_compact_pages(self.pool, self.layout, self.batch, self.tables, self.num_used, self.page_map,
+                                        self.workspace, self.workspace.numel(), stream))
 
 
 def transfer(sender: TransferSender, receiver: TransferReceiver, h_wire: torch.Tensor,

@@ -605,3 +605,73 @@ def test_latent_same_bits_graph_and_unusable_tables(dev):
     want = od.attend(g, 0, pool_h, bt, sl, q, "bf16", "bf16", 0.07, 128)
     assert (np.abs(out[0] - want[0][0]) <= want[2][0]).all()
     assert np.isfinite(out[2]).all() and (lse[1] == -np.inf).all()
+
+
+# ------------------------------------------------------------------------- all of it together
+
+@pytest.mark.parametrize("F,H,G,D,Dv", [(2, 2, 4, 64, 0), (1, 1, 24, 192, 128)])
+def test_received_cache_is_decoded(dev, F, H, G, D, Dv):
+    """A transfer through pinned host memory, then a decode worker's life on the cache it received:
+    tokens appended and attended to, a request forked, another one freed, the pool compacted."""
+    from paper_2607_28633_b200 import harness, session, workloads as wl
+    spec = wl.WorkloadSpec("decode", L=2, F=F, H=H, D=D, E=2, P=8, R=3, lengths=("fixed", (16, 33, 290)), pool_factor=2.0, seed=40)
+    w = harness.setup(spec, dev, need_wire=False)
+    tx = session.TransferSender(w.src_pool, w.layout, w.src_bt, w.seq_lens, w.batch.total_tokens)
+    rx = session.TransferReceiver(w.dst_pool, w.layout, w.dst_bt, w.seq_lens, w.batch.total_tokens)
+    h_wire = torch.zeros(spec.L * w.n_layer, dtype=torch.uint8).pin_memory()
+    _, status = session.transfer(tx, rx, h_wire, [1, 2, 3], 7, w.batch.seq_lens)
+    assert status == [tk.TOPKV_OK] * 3
+    g = Geom(L=2, F=F, h_kv=H, d_h=D, b_p=2, P=8, num_pages=w.batch.num_pool_pages)
+    cache = session.DecodeCache(w.dst_pool, w.layout, w.dst_bt, w.seq_lens, rows=5, max_pages=w.dst_bt.shape[1] + 2)
+    # the oracle's copies
+    pool = w.dst_pool.cpu().numpy()
+    bt, sl, ref = (x.cpu().numpy().copy() for x in (cache.block_table, cache.seq_lens, cache.ref_counts))
+    rng = np.random.default_rng(3)
+    s = torch.cuda.Stream(dev)
+    put = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    keep = []
+
+    def step(live):
+        new = np.array([1 if r in live else 0 for r in range(5)], np.int32)
+        d_new = put(new)
+        s.wait_stream(torch.cuda.current_stream(dev))
+        cache.extend(d_new, s)
+        assert od.extend_requests(g.P, bt, sl, ref, new) == 0
+        for layer in range(2):
+            rows = od.encode_elements(rng.normal(size=len(live) * F * H * D), "bf16")
+            kv = torch.from_numpy(rows).to(dev)
+            q = torch.from_numpy(rng.normal(size=(5, H * G, D))).to(dev).to(torch.bfloat16)
+            out = torch.zeros((5, H * G, Dv or D), dtype=torch.bfloat16, device=dev)
+            s.wait_stream(torch.cuda.current_stream(dev))
+            cache.append(layer, kv, s)
+            keep.append((kv, q, out, d_new))
+            rows = rows.reshape(len(live), F, H, D * 2)
+            for k, r in enumerate(live):
+                i = int(sl[r]) - 1
+                for c in range(F):
+                    for h in range(H):
+                        a = od.row_offset(g, layer, int(bt[r, i // g.P]), c, i % g.P, h)
+                        pool[a:a + 2 * D] = rows[k, c, h]
+            cache.attend(layer, q, out, D ** -0.5, s, value_dim=Dv)
+            s.synchronize()
+            want, _, tol, _ = od.attend(g, layer, pool, bt, sl, q.double().cpu().numpy(), "bf16", "bf16", D ** -0.5, Dv)
+            assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+
+    step([0, 1, 2])
+    parents, children = put([2, 1]), put([3, 4])
+    s.wait_stream(torch.cuda.current_stream(dev))
+    cache.fork(parents, children, s)
+    assert od.fork_requests(g, pool, bt, sl, ref, [2, 1], [3, 4]) == 0
+    step([0, 1, 2, 3, 4])
+    ended = put([2, 0])
+    s.wait_stream(torch.cuda.current_stream(dev))
+    cache.free(ended, s)
+    assert od.free_requests(g.P, bt, sl, ref, [2, 0]) == 0
+    step([1, 3, 4])
+    cache.compact(s)
+    err, n, to = od.compact_pages(g, pool, bt, sl, ref)
+    step([1, 3, 4])
+    s.synchronize()
+    assert err == 0 and cache.num_used.item() == n
+    for got, want in ((cache.block_table, bt), (cache.seq_lens, sl), (cache.ref_counts, ref), (w.dst_pool, pool)):
+        assert np.array_equal(got.cpu().numpy(), want)
