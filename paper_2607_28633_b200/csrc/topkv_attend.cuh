@@ -680,15 +680,16 @@ __global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(cons
   const int row0 = blockIdx.z * per, rows = min(per, all_rows - row0);
   if (rows <= 0) return;
   const int64_t q_head0 = (int64_t)h * p.G + g0 + row0;
-  // row `row0` of part k; the parts but the first lie at a constant stride
-  const int64_t slot0 = (((int64_t)team * 2 + rec.z) * units + unit) * p.rows + row0;
-  const int64_t slot1 = ((int64_t)(team + 1) * 2 * units + unit) * p.rows + row0, step = 2ll * units * p.rows;
-  auto slot = [&](int k) -> int64_t { return k == 0 ? slot0 : slot1 + (k - 1) * step; };
+  // row `row0` of part k; the parts but the first lie at a constant stride (the host has checked that
+  // the workspace's elements can be counted in 32 bits)
+  const int slot0 = ((team * 2 + rec.z) * units + unit) * p.rows + row0;
+  const int step = 2 * units * p.rows, slot1 = ((team + 1) * 2 * units + unit) * p.rows + row0 - step;
+  auto slot = [&](int k) -> int { return k == 0 ? slot0 : slot1 + k * step; };
 
   const int quads = p.Dv / 4, items = rows * quads;  // quads: at most 128
   const int groups = max(kJoinThreads / items, 1), group = groups > 1 ? tid / items : 0;
   // Item i: columns 4 quad .. of row g; a thread's first item is loaded while the weights are formed.
-  auto part_of = [&](int i) { return p.part + (int64_t)(i / quads) * p.Dv + (i % quads) * 4; };
+  auto part_of = [&](int i) { return i / quads * p.Dv + (i % quads) * 4; };
   constexpr int kAhead = 4;
   float4 ahead[kAhead];
   const int item0 = tid - group * items;
@@ -696,26 +697,40 @@ __global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(cons
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) {
     const int k = group + j * groups;
-    if (mine && k < parts) ahead[j] = *reinterpret_cast<const float4*>(part_of(item0) + slot(k) * p.Dv);
+    if (mine && k < parts) ahead[j] = *reinterpret_cast<const float4*>(&p.part[part_of(item0) + slot(k) * p.Dv]);
   }
   for (int g = warp; g < rows; g += kJoinThreads / 32) {
-    float top = -INFINITY;
-    for (int k = lane; k < parts; k += 32) top = fmaxf(top, p.ml[slot(k) + g].x);
+    // up to 64 parts are held by the warp's lanes, so that they are loaded once and all together
+    constexpr int kHeld = 2;
+    float2 held[kHeld];
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      const int k = lane + 32 * j;
+      held[j] = k < parts ? p.ml[slot(k) + g] : make_float2(-INFINITY, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) top = fmaxf(top, held[j].x);
+    for (int k = lane + 32 * kHeld; k < parts; k += 32) top = fmaxf(top, p.ml[slot(k) + g].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float from = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (int k = lane; k < parts; k += 32) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      held[j].x = exp2_approx(held[j].x - from);
+      sum += held[j].x * held[j].y;
+    }
+    for (int k = lane + 32 * kHeld; k < parts; k += 32) {
       const float2 ml = p.ml[slot(k) + g];
-      const float f = exp2_approx(ml.x - from);
-      s_w[g][k] = f;
-      sum += f * ml.y;
+      sum += exp2_approx(ml.x - from) * ml.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float inv = p.v_scale / sum;
-    __syncwarp();
-    for (int k = lane; k < parts; k += 32) s_w[g][k] *= inv;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (lane + 32 * j < parts) s_w[g][lane + 32 * j] = held[j].x * inv;
+    for (int k = lane + 32 * kHeld; k < parts; k += 32) s_w[g][k] = exp2_approx(p.ml[slot(k) + g].x - from) * inv;
     if (lane == 0 && p.lse != nullptr)
       p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
   }
@@ -737,7 +752,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(cons
         if (k < parts) add(acc, ahead[j], s_w[g][k]);
     }
 #pragma unroll 4
-    for (; k < parts; k += groups) add(acc, *reinterpret_cast<const float4*>(part_of(i) + slot(k) * p.Dv), s_w[g][k]);
+    for (; k < parts; k += groups) add(acc, *reinterpret_cast<const float4*>(&p.part[part_of(i) + slot(k) * p.Dv]), s_w[g][k]);
     if (groups > 1)
       s_acc[tid] = acc;
     else

@@ -136,6 +136,7 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   plan->bytes = 0;
   if (!plan->uncut) {
     const int64_t slots = 2ll * plan->teams * plan->units * plan->rows;
+    if (slots * plan->dv > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
     plan->joins = std::min(plan->teams, b->num_requests);
     plan->bytes = (int64_t)plan->joins * 16 + slots * 8 + slots * plan->dv * 4;
     plan->bytes = (plan->bytes + 255) / 256 * 256;
