@@ -67,6 +67,7 @@ struct AttendParams {
   int teams;            // CTAs along x; 0 tiles of a request cross a team when uncut
   int uncut;            // 1: team t is request t
   int by_request;       // how the join records are indexed
+  int start_cost;       // of a request, in tiles
   int late_wait;        // tables are settled
   int box;              // latent rows: tokens of a tensor copy (divides the page and 64), 0 = none are used
   int q_box;            // latent rows: 1 = Q comes by tensor copies too
@@ -97,27 +98,40 @@ __device__ __forceinline__ Visible visible_tokens(const AttendParams& p, int r, 
 }
 __device__ __forceinline__ int attend_tiles(int n) { return n / kTileTokens + (n % kTileTokens != 0); }
 
-// Which tiles are a team's. The tiles of all requests, laid end to end, are cut into equal ranges;
-// in an uncut launch team t takes request t. Every CTA works it out from the lengths.
+// Which tiles are a team's. The requests are laid end to end, each `p.start_cost` + its tiles long (what
+// it costs to begin with a request and to write its result, in tiles; an empty one 0), and cut into
+// ranges of equal length; a range has the tiles that lie in it. In an uncut launch team t takes request
+// t. Every CTA works it out from the lengths.
 struct TeamRange {
-  int r, t0;      // first request, and the tile in it to begin with
-  int64_t left;   // tiles (uncut: 1, the request)
+  int r;          // first request
+  int64_t off;    // where in it the range begins
+  int64_t left;   // length of the range (uncut: the request)
 };
 struct TeamStart {  // in shared memory
   int64_t scan[16];
-  int64_t pos;    // the range's start among all tiles
-  int64_t each;   // tiles of a range ...
-  int more;       // ... and how many ranges have one more
-  int r, t0;
+  int64_t pos;    // the range's start
+  int64_t off;
+  int64_t each;   // length of a range ...
+  int more;       // ... and how many ranges are one longer
+  int r;
 };
-// The team whose range holds tile x.
+// The tiles [t0, t1) of a request of n tiles that a range has which begins `off` into it and is `left` long;
+// the return value is how much of the range the request takes.
+__device__ __forceinline__ int64_t tiles_in_range(const AttendParams& p, int n, int64_t off, int64_t left, int* t0, int* t1) {
+  const int c = p.uncut ? 0 : p.start_cost;
+  const int64_t end = min(off + left, (int64_t)c + n);
+  *t0 = (int)max(off - c, (int64_t)0);
+  *t1 = (int)max(end - c, (int64_t)0);
+  return end - off;
+}
+// The team whose range holds position x.
 __device__ __forceinline__ int team_of(const TeamStart& t, int64_t x) {
   const int64_t wide = t.more * (t.each + 1);
   return x < wide ? (int)(x / (t.each + 1)) : t.more + (int)((x - wide) / t.each);
 }
 template <int THREADS>
 __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team, TeamStart* s) {
-  TeamRange out = {team, 0, 1};
+  TeamRange out = {team, 0, 0x7fffffff};
   if (p.uncut) return out;
   constexpr int kWarps = THREADS / 32;
   static_assert(kWarps <= 16, "scan holds 16 warps");
@@ -125,7 +139,11 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
   const int per = (p.R + THREADS - 1) / THREADS;
   const int r0 = (int)min((int64_t)tid * per, (int64_t)p.R), r1 = min(r0 + per, p.R);
   int64_t mine = 0;
-  for (int i = r0; i < r1; ++i) mine += attend_tiles(visible_tokens(p, i, false).n);
+  auto length = [&](int i) {
+    const int n = attend_tiles(visible_tokens(p, i, false).n);
+    return n > 0 ? n + p.start_cost : 0;
+  };
+  for (int i = r0; i < r1; ++i) mine += length(i);
   int64_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -141,7 +159,7 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
     if (w < warp) incl += s->scan[w];
     total += s->scan[w];
   }
-  const int teams = (int)min((int64_t)p.teams, total);  // no team between two others is without tiles
+  const int teams = (int)min((int64_t)p.teams, total);  // no range is empty
   int64_t a = 0, b = 0;
   if (team < teams) {
     const bool narrow = total <= 0xffffffffll;  // a 32-bit division where that will do
@@ -158,10 +176,10 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
   if (a < b && a >= incl - mine && a < incl) {  // exactly one thread
     int64_t at = incl - mine;
     for (int i = r0; i < r1; ++i) {
-      const int n = attend_tiles(visible_tokens(p, i, false).n);
+      const int n = length(i);
       if (a < at + n) {
         s->r = i;
-        s->t0 = (int)(a - at);
+        s->off = a - at;
         break;
       }
       at += n;
@@ -169,7 +187,7 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
   }
   __syncthreads();
   out.r = s->r;
-  out.t0 = s->t0;
+  out.off = s->off;
   out.left = out.r < 0 ? 0 : b - a;
   return out;
 }
@@ -181,9 +199,10 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
 __device__ __forceinline__ void write_join(const AttendParams& p, int r, int team, int slot, int parts) {
   p.joins[p.by_request ? r : team] = make_int4(r, team, slot, parts);
 }
-__device__ __forceinline__ void request_begins(const AttendParams& p, const TeamStart& s, int team, int r, bool first, int64_t done,
+// `begin`: where the request begins, from the start of the team's range (before it, if negative).
+__device__ __forceinline__ void request_begins(const AttendParams& p, const TeamStart& s, int team, int r, bool first, int64_t begin,
                                                int tiles, bool whole) {
-  write_join(p, r, team, first ? 0 : 1, whole ? 0 : team_of(s, s.pos + done + tiles - 1) - team + 1);
+  write_join(p, r, team, first ? 0 : 1, whole ? 0 : team_of(s, s.pos + begin + p.start_cost + tiles - 1) - team + 1);
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
   const int n = valid ? 16 : 0;  // 0: nothing is read, the 16 bytes become zero
@@ -322,20 +341,23 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   }
   const int chunks = p.D * S::kElem / 16;
   const uint8_t* k_base = p.pool + (int64_t)h * p.S_head;
-  int64_t left = mine.left;
-  int r = mine.r, t0 = mine.t0;
+  int64_t left = mine.left, off = mine.off;
+  int r = mine.r;
   const int gr = lane >> 2, gc = lane & 3;  // row and column group of this thread in a matrix fragment
 
-  for (bool first = true; left > 0 && r < p.R; first = false, t0 = 0, ++r) {
+  for (bool first = true; left > 0 && r < p.R; ++r) {
     const Visible vis = visible_tokens(p, r, false);
     const int tiles = attend_tiles(vis.n);
     if (tiles == 0) {
       if (p.uncut) return;
       continue;
     }
-    const int t1 = p.uncut ? tiles : (int)min((int64_t)tiles, t0 + left);
-    left -= p.uncut ? 1 : t1 - t0;
-    if (records && t0 == 0) request_begins(p, s_team, team, r, first, mine.left - left - t1, tiles, t1 == tiles);
+    int t0, t1;
+    const int64_t taken = tiles_in_range(p, tiles, off, left, &t0, &t1);
+    if (records && t0 == 0 && t1 > 0) request_begins(p, s_team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
+    left -= taken;
+    off = 0;
+    if (t0 == t1) continue;
 
     // ---- the query rows as fragments ----------------------------------------------------------
     uint32_t qf[kSteps][4];
@@ -390,7 +412,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, base[2] = {0.f, 0.f};
 
     // ---- this warp's 16 tokens of every tile: visible tokens v .. v + 15, 64 further each time -----
-    const int end = min(vis.n, t1 * kTileTokens);
+    const int end = t1 == tiles ? vis.n : t1 * kTileTokens;
     const int32_t* bt_row = p.bt + (int64_t)r * p.maxp;
     auto token = [&](int v) { return v < vis.ns ? v : v + (vis.lo - vis.ns); };
     auto page_column = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
@@ -655,6 +677,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       __syncwarp();
     }
     if (p.uncut) return;
+    first = false;
   }
 }
 

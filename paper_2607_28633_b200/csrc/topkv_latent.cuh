@@ -296,22 +296,22 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
   constexpr uint32_t kType = 1u << 4 | (BF16 ? 1u : 0u) << 7 | (BF16 ? 1u : 0u) << 10 | (uint32_t)(N >> 3) << 17;
   uint32_t n = 0;    // tiles before the current segment, in this CTA: they number the phases
   uint32_t seg = 0;  // segments before
-  int64_t left = mine.left;  // 0: no tiles
-  int t0 = mine.t0;
+  int64_t left = mine.left, off = mine.off;  // left 0: no tiles
   bool first = true;
   for (int r = mine.r; left > 0 && r < p.R; ++r) {
     const Visible vis = visible_tokens(p, r, false);
     const int tiles = attend_tiles(vis.n);
     if (tiles == 0) {
       if (p.uncut) break;
-      t0 = 0;
-      first = false;
       continue;
     }
-    const int t1 = p.uncut ? tiles : (int)min((int64_t)tiles, t0 + left);
+    int t0, t1;
+    const int64_t taken = tiles_in_range(p, tiles, off, left, &t0, &t1);
+    if (records && t0 == 0 && t1 > 0) request_begins(p, ctl.team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
+    left -= taken;
+    off = 0;
     const int count = t1 - t0;
-    left -= p.uncut ? 1 : count;
-    if (records && t0 == 0) request_begins(p, ctl.team, team, r, first, n, tiles, t1 == tiles);
+    if (count == 0) continue;
 
     if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kLoadWarps) {
       // ---- load: pair `g` of warps takes the stages g of its own parity ---------------------------
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       auto piece = [&](int i, int* at) {
         *at = 0;
         const int v = (t0 + i) * kLatentTile + lane * p.box;
-        if (i >= count || lane >= boxes || (t0 + i + 1) * kLatentTile > vis.n) return -1;
+        if (i >= count || lane >= boxes || (int64_t)(t0 + i + 1) * kLatentTile > vis.n) return -1;
         const int j = page_column(v);
         *at = v - j * p.P;
         return p.bt[(int64_t)r * p.maxp + j];
@@ -636,7 +636,6 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     n += count;
     ++seg;
     first = false;
-    t0 = 0;
     if (p.uncut) break;
   }
   tcgen05_before_sync();
