@@ -126,7 +126,7 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   if (b->window_tokens > 0) most = std::min(most, (int64_t)b->window_tokens + at->sink_tokens);
   if (b->total_tokens >= 0) most = std::min(most, b->total_tokens);
   const int64_t tiles = (most + kTileTokens - 1) / kTileTokens;
-  const int64_t resident = 148 * (lo->kv_factor == 1 ? 1 : attend_ctas_per_sm(D, (int)at->cache_type));
+  const int64_t resident = lo->kv_factor == 1 ? 148 : 148 * attend_ctas_per_sm(D, (int)at->cache_type) - 4;
   int64_t teams = std::max<int64_t>(1, resident / plan->units);
   // units that do not divide the resident CTAs would leave some of them idle: two rounds then
   if (teams * plan->units * 8 < resident * 7) teams = std::max<int64_t>(1, 2 * resident / plan->units);
