@@ -313,7 +313,8 @@ int topkv_repage_layer(int layer, const void* src_pool, const topkv_layout* src_
  * the second product (bf16 for a bf16 cache, else fp16) and the result once to io_type.
  * Long requests are split between CTAs and joined in a fixed order, through d_workspace: the same
  * arguments give the same bits. At most two kernels are enqueued on `stream`; no allocation, no
- * synchronisation, capturable. The workspace holds nothing between calls and needs no
+ * synchronisation, capturable (the first call for a head size and type on a device raises that
+ * kernel's shared-memory limit: make it outside a capture). The workspace holds nothing between calls and needs no
  * initialisation; calls that may run at the same time (other streams, two captured graphs) need
  * one each. TOPKV_FLAG_TABLES_SETTLED is honoured; TOPKV_FLAG_OVERLAP_PREVIOUS is ignored (the call
  * always waits for the kernels before it). cu_seq_lens and total_tokens are optional; a stated

@@ -258,18 +258,24 @@ __device__ __forceinline__ void store_io4(uint8_t* p, const float4& v, float f, 
                        : make_uint2(pack2<false>(v.x * f, v.y * f), pack2<false>(v.z * f, v.w * f));
   *reinterpret_cast<uint2*>(p) = w;
 }
-// Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0.
+// Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0. Every
+// lane looks at one request of the team's share, a warp writes what it finds.
 template <int THREADS>
 __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, int64_t head0, int rows, bool complain) {
-  for (int e = team; e < p.R; e += p.teams) {
-    if (visible_tokens(p, e, complain && threadIdx.x == 0).n > 0) continue;
-    if (complain && threadIdx.x == 0 && !p.uncut && p.by_request) write_join(p, e, 0, 0, 0);
-    for (int i = threadIdx.x; i < rows * p.Dv; i += THREADS) {
-      const int g = i / p.Dv, d = i - g * p.Dv;
-      store_io(p.out + e * p.o_req + (head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int64_t first = team + (int64_t)p.teams * 32 * warp; first < p.R; first += (int64_t)p.teams * THREADS) {
+    const int64_t e = first + (int64_t)p.teams * lane;
+    const bool empty = e < p.R && visible_tokens(p, (int)e, complain).n == 0;
+    if (empty && complain && !p.uncut && p.by_request) write_join(p, (int)e, 0, 0, 0);
+    for (uint32_t left = __ballot_sync(0xffffffffu, empty); left != 0; left &= left - 1) {
+      const int64_t r = first + (int64_t)p.teams * (__ffs(left) - 1);
+      for (int i = lane; i < rows * p.Dv; i += 32) {
+        const int g = i / p.Dv, d = i - g * p.Dv;
+        store_io(p.out + r * p.o_req + (head0 + g) * p.o_head + d * 2, 0.f, p.io_bf16);
+      }
+      if (p.lse != nullptr)
+        for (int g = lane; g < rows; g += 32) p.lse[r * p.H * p.G + head0 + g] = -INFINITY;
     }
-    if (p.lse != nullptr)
-      for (int g = threadIdx.x; g < rows; g += THREADS) p.lse[(int64_t)e * p.H * p.G + head0 + g] = -INFINITY;
   }
 }
 // 2^x by the hardware's approximation (2 ulp; results below 2^-126 become 0).

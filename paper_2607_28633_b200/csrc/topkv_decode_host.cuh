@@ -12,6 +12,7 @@ inline bool mult4p(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) 
 // The parts of a batch that these calls use: unlike the copies they need no prefix sums, so any
 // number of requests is fine without cu_seq_lens.
 int check_tables_batch(const topkv_layout* lo, const topkv_batch* b) {
+  if (lo->page_tokens > 0x7fffffffu) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   if (b == nullptr || b->struct_size != sizeof(topkv_batch) ||
       (b->flags & ~(uint32_t)(TOPKV_FLAG_OVERLAP_PREVIOUS | TOPKV_FLAG_TABLES_SETTLED)) != 0)
     return TOPKV_ERR_INVALID_ARG;
@@ -135,7 +136,7 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   plan->uncut = tiles <= kUncutTiles || (teams == 1 && b->num_requests == 1);
   plan->teams = plan->uncut ? b->num_requests : (int)teams;
   plan->bytes = 0;
-  if (!plan->uncut) {
+  if (!plan->uncut && b->num_requests > 0) {
     const int64_t slots = 2ll * plan->teams * plan->units * plan->rows;
     if (slots * plan->dv > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
     plan->joins = std::min(plan->teams, b->num_requests);
@@ -544,7 +545,7 @@ int topkv_copy_pages(int first_layer, int num_layers, void* pool, const topkv_la
   Resolved rs;
   const int st = check_layout(layout, &rs);
   if (st != TOPKV_OK) return st;
-  if (layout->num_pool_pages > 0x7ffffff0ll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (layout->num_pool_pages > 0x7ffffff0ll || layout->page_tokens > 0x7fffffffu) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   if (first_layer < 0 || num_layers < 0 || (int64_t)first_layer + num_layers > (int64_t)layout->num_layers)
     return TOPKV_ERR_LAYER_RANGE;
   if (pool == nullptr || num_pages < 0) return TOPKV_ERR_INVALID_ARG;

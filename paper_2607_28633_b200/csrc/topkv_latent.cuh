@@ -336,6 +336,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       int i = (g - (int)(n & 1)) & 1;
       int at, pg = piece(i, &at);
       for (; i < count; i += 2) {
+        if (s_dead) break;
         const uint32_t k = n + i;
         const bool pieces = boxes > 0 && __all_sync(0xffffffffu, lane >= boxes || (pg >= 0 && pg < p.num_pages));
         if (pieces) {
@@ -637,6 +638,10 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     ++seg;
     first = false;
     if (p.uncut) break;
+  }
+  if (s_dead) {  // give the copies and products that are in flight a millisecond to end
+    const long long began = clock64();
+    while (clock64() - began < 2000000) __nanosleep(1000);
   }
   tcgen05_before_sync();
   __syncthreads();

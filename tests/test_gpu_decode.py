@@ -675,3 +675,139 @@ def test_received_cache_is_decoded(dev, F, H, G, D, Dv):
     assert err == 0 and cache.num_used.item() == n
     for got, want in ((cache.block_table, bt), (cache.seq_lens, sl), (cache.ref_counts, ref), (w.dst_pool, pool)):
         assert np.array_equal(got.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------------- calls at the edges
+
+@pytest.mark.parametrize("D,kind", [(8, "bf16"), (24, "fp16"), (248, "bf16"), (48, "e4m3"), (144, "e4m3")])
+def test_attend_odd_head_dims(dev, D, kind):
+    _case(dev, 2, 3, 2, D, 16, [33, 600, 1], kind, seed=D)
+
+
+@pytest.mark.parametrize("F", [1, 2])
+def test_attend_broadcast_queries(dev, F):
+    """One query for all requests, and one for all heads (strides of 0)."""
+    rng = np.random.default_rng(2)
+    sl, D, Dv, Hq = [400, 20, 1500], 64, 48 if F == 1 else 0, 6
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(F, 1, D, 2, 16, pages)
+    pool_h = _cache(g, bt, sl, "bf16", 0, rng)
+    pool, lo = torch.from_numpy(pool_h).to(dev), _layout(g)
+    b = tk.make_batch(torch.from_numpy(bt).to(dev), torch.tensor(sl, dtype=torch.int32, device=dev))
+    base = torch.from_numpy(rng.normal(size=(3, Hq, D))).to(dev).to(torch.bfloat16)
+    for q in (base[:1].expand(3, Hq, D), base[:, :1].expand(3, Hq, D), base[:1, :1].expand(3, Hq, D)):
+        out = torch.zeros(3, Hq, Dv or D, dtype=torch.bfloat16, device=dev)
+        lse = torch.zeros(3, Hq, device=dev)
+        att = tk.make_attention(q, out, 1, 1, 0.125, value_dim=Dv, lse=lse)
+        n = tk.check(tk.topkv_attend_workspace_bytes(lo, b, att))
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        tk.check(tk.topkv_attend_layer(0, pool, lo, b, att, q, out, ws, n))
+        torch.cuda.synchronize()
+        _check((out.double().cpu().numpy(), lse.double().cpu().numpy()),
+               od.attend(g, 0, pool_h, bt, sl, q.double().cpu().numpy(), "bf16", "bf16", 0.125, Dv))
+
+
+@pytest.mark.parametrize("F,Hq,Dv", [(2, 2, 0), (1, 5, 16)])
+def test_attend_mostly_empty_batches(dev, F, Hq, Dv):
+    """A padded batch: far more rows than CTAs, nearly all of them empty, lengths of 0 at both ends."""
+    sl = np.zeros(3000, np.int64)
+    sl[[5, 1234, 2998]] = [700, 1, 330]
+    _case(dev, F, 1, Hq, 32, 16, sl, "bf16", Dv=Dv)
+    _case(dev, F, 1, Hq, 32, 16, np.minimum(sl, 200), "bf16", Dv=Dv)
+    _case(dev, F, 1, Hq, 32, 16, np.zeros(2000, np.int64), "bf16", Dv=Dv, extra_cols=100)
+
+
+@pytest.mark.parametrize("P", [8, 24, 40, 64, 192])
+def test_latent_tensor_copies_with_a_bad_page(dev, P):
+    """Pages of several pieces and of odd multiples of 8; the tile with the bad page comes row by row."""
+    rng = np.random.default_rng(P)
+    sl = [1000, 129]
+    bt, pages = _table(sl, P, 2, 1, rng)
+    g = _geom(1, 1, 128, 2, P, pages)
+    pool_h = _cache(g, bt, sl, "bf16", 0, rng)
+    pool = torch.from_numpy(pool_h).to(dev)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=2 * 17 * 128), "bf16"), "bf16").reshape(2, 17, 128)
+    got = _run(dev, g, _layout(g), pool, bt, sl, q, "bf16", "bf16", 0.09, 64)
+    _check(got, od.attend(g, 0, pool_h, bt, sl, q, "bf16", "bf16", 0.09, 64))
+    broken = bt.copy()
+    broken[0, 3] = pages + 7
+    out, lse = _run(dev, g, _layout(g), pool, broken, sl, q, "bf16", "bf16", 0.09, 64)
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
+    rows = np.array([i for i in range(1000) if i // P != 3])
+    k = od.rows_of(g, 0, pool_h, bt[0], rows, 0, 0, "bf16")
+    for a in range(17):
+        w = np.exp(0.09 * k @ q[0, a])
+        assert np.abs(out[0, a] - w @ k[:, :64] / w.sum()).max() < 2.0 ** -6 and abs(lse[0, a] - np.log(w.sum())) < 1e-4
+    _, want_lse, _, _ = od.attend(g, 0, pool_h, bt, sl, q, "bf16", "bf16", 0.09, 64)
+    assert np.abs(lse[1] - want_lse[1]).max() < 1e-4
+
+
+def test_latent_rows_past_two_gigabytes_and_graphs_on_two_streams(dev):
+    g = _geom(1, 1, 576, 2, 64, 6 * (1 << 30) // 73728)
+    pool = torch.zeros(g.pool_bytes(), dtype=torch.uint8, device=dev)
+    rng = np.random.default_rng(8)
+    sl = [100, 700]
+    bt = np.full((2, 12), -1, np.int32)
+    bt[0, :2] = [g.num_pages - 1, 5]
+    bt[1, :11] = g.num_pages - 100 + np.arange(11)
+    want = {int(p): od.encode_elements(rng.normal(size=36864), "bf16") for p in bt.reshape(-1) if p >= 0}
+    for p, raw in want.items():
+        pool[p * 73728:(p + 1) * 73728] = torch.from_numpy(raw).to(dev)
+    small = _geom(1, 1, 576, 2, 64, len(want))
+    order = {p: i for i, p in enumerate(want)}
+    pool_h = np.concatenate(list(want.values()))
+    bt_h = np.array([[order.get(int(x), -1) for x in row] for row in bt], np.int32)
+    lo = _layout(g)
+    b = tk.make_batch(torch.from_numpy(bt).to(dev), torch.tensor(sl, dtype=torch.int32, device=dev))
+    q = torch.zeros(2, 70, 576, dtype=torch.bfloat16, device=dev)
+    outs = [torch.zeros(2, 70, 512, dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    lses = [torch.zeros(2, 70, device=dev) for _ in range(2)]
+    atts = [tk.make_attention(q, o, 1, 1, 0.04, value_dim=512, lse=l) for o, l in zip(outs, lses)]
+    n = tk.check(tk.topkv_attend_workspace_bytes(lo, b, atts[0]))
+    ws = [torch.empty(n, dtype=torch.uint8, device=dev) for _ in range(2)]
+    call = lambda i, s: tk.check(tk.topkv_attend_layer(0, pool, lo, b, atts[i], q, outs[i], ws[i], n, s))
+    call(0, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(dev)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(0, torch.cuda.current_stream())
+    for seed in (1, 2):
+        q_h = od.decode_elements(od.encode_elements(np.random.default_rng(seed).normal(size=2 * 70 * 576), "bf16"), "bf16").reshape(2, 70, 576)
+        q.copy_(torch.from_numpy(q_h).to(torch.bfloat16))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            graph.replay()
+            call(1, side)
+        torch.cuda.synchronize()
+        exact = od.attend(small, 0, pool_h, bt_h, sl, q_h, "bf16", "bf16", 0.04, 512)
+        for o, l in zip(outs, lses):
+            _check((o.double().cpu().numpy(), l.double().cpu().numpy()), exact)
+
+
+def test_page_operators_in_a_graph(dev):
+    """A captured turn (free, fork, extend) replayed from restored tables gives the same tables."""
+    rng, g, sl, bt, ref, pool = _page_case(5, R=8, P=4, spare=20, maxlen=14)
+    sl[1] = max(int(sl[1]), 1)
+    s = _State(dev, g, sl, bt, ref, pool, False)
+    in_place = tk.make_page_tables(s.out[2], *s.out)
+    b2 = tk.make_batch(s.out[0], s.out[1])
+    rows, parents, children = s.put(np.array([0, 3], np.int32)), s.put(np.array([1, 1], np.int32)), s.put(np.array([0, 3], np.int32))
+    new = s.put(np.ones(8, np.int32))
+
+    def turn(st):
+        tk.check(tk.topkv_free_requests(s.lo, s.batch, s.tables, rows, 2, st))
+        tk.check(tk.topkv_fork_requests(s.pool, s.lo, b2, in_place, parents, children, 2, s.ws, s.n, st))
+        tk.check(tk.topkv_extend_requests(s.lo, b2, in_place, new, s.ws, s.n, st))
+    side = torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        turn(torch.cuda.current_stream())
+    err = od.free_requests(g.P, bt, sl, ref, [0, 3])
+    err |= od.fork_requests(g, pool, bt, sl, ref, [1, 1], [0, 3])
+    err |= od.extend_requests(g.P, bt, sl, ref, [1] * 8)
+    for _ in range(3):
+        graph.replay()
+    s.check(bt, sl, ref, pool, err)
