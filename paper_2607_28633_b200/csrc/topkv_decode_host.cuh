@@ -298,6 +298,16 @@ int copy_tables(const topkv_layout* lo, const topkv_batch* b, const topkv_page_t
   return launched(launch_pdl(topkv_tables_copy_kernel, dim3(copy_ctas(most, 256)), dim3(256), 0, s, p), 1);
 }
 
+// Small tables (128 KiB: what one CTA copies in the time of a launch, 2 us) are left to the operator's own
+// kernel, larger ones copied by a launch before it.
+int copy_or_pass(const topkv_layout* lo, const topkv_batch* b, const topkv_page_tables* t, TablesCopyParams* pass, cudaStream_t s) {
+  int64_t most;
+  *pass = tables_copy(lo, b, t, &most);
+  if (pass->n[0] + pass->n[1] + pass->n[2] <= 32768) return TOPKV_OK;
+  *pass = TablesCopyParams{};
+  return copy_tables(lo, b, t, s);
+}
+
 // How the contents of a page are moved; *vec = bytes per access.
 PageGeom page_geometry(int first_layer, int num_layers, void* pool, const topkv_layout* lo, const Resolved& rs, int* vec) {
   PageGeom g;
@@ -437,9 +447,9 @@ int topkv_extend_requests(const topkv_layout* layout, const topkv_batch* batch, 
   st = check_page_workspace(layout, batch, 0, d_workspace, workspace_bytes);
   if (st != TOPKV_OK) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  st = copy_tables(layout, batch, tables, s);
-  if (st != TOPKV_OK) return st;
   ExtendParams p;
+  st = copy_or_pass(layout, batch, tables, &p.copy, s);
+  if (st != TOPKV_OK) return st;
   p.t = page_tables(layout, batch, tables);
   p.add = d_new_tokens;
   p.prefix = static_cast<int32_t*>(d_workspace);
@@ -499,12 +509,17 @@ int topkv_free_requests(const topkv_layout* layout, const topkv_batch* batch, co
   if (!mult4p(d_rows)) return TOPKV_ERR_ALIGNMENT;
   if (batch->num_requests == 0 || batch->max_pages_per_req == 0) return TOPKV_OK;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  st = copy_tables(layout, batch, tables, s);
-  if (st != TOPKV_OK || num_rows == 0) return st;
+  if (num_rows == 0) return copy_tables(layout, batch, tables, s);
   FreeParams p;
+  st = copy_or_pass(layout, batch, tables, &p.copy, s);
+  if (st != TOPKV_OK) return st;
   p.t = page_tables(layout, batch, tables);
   p.rows = d_rows;
-  return launched(launch_pdl(topkv_free_kernel, dim3((unsigned)num_rows), dim3(256), 0, s, p), 1);
+  p.n = num_rows;
+  // one CTA if it has the tables to copy or little to do, else 32 rows each
+  const bool passed = p.copy.n[0] + p.copy.n[1] + p.copy.n[2] > 0;
+  const unsigned ctas = passed ? 1 : (unsigned)std::min<int64_t>(((int64_t)num_rows + 31) / 32, 2 * 148);
+  return launched(launch_pdl(topkv_free_kernel, dim3(ctas), dim3(kPlanThreads), 0, s, p), 1);
 }
 
 int topkv_compact_pages(void* pool, const topkv_layout* layout, const topkv_batch* batch,

@@ -123,49 +123,59 @@ __global__ void __launch_bounds__(256) topkv_tables_copy_kernel(const TablesCopy
 // ---- free ---------------------------------------------------------------------------------------
 struct FreeParams {
   PageTables t;
+  TablesCopyParams copy;  // done by the kernel itself (one CTA, small tables)
   const int32_t* rows;
+  int n;
 };
-// One CTA per listed row. Whoever takes the row's length (an exchange with 0) frees its pages, so a
+// A warp per listed row. Whoever takes the row's length (an exchange with 0) frees its pages, so a
 // row that is listed twice is freed once; reference counts go down by integer atomics, whose order
 // does not show in the result.
-__global__ void __launch_bounds__(256) topkv_free_kernel(const FreeParams p) {
-  __shared__ int s_len;
+__global__ void __launch_bounds__(kPlanThreads) topkv_free_kernel(const FreeParams p) {
   pdl_prologue(0);
-  const int r = p.rows[blockIdx.x];
-  if (r < 0 || r >= p.t.R) {
-    if (threadIdx.x == 0) raise_error(kErrTable);
-    return;
+  if (gridDim.x == 1) {
+    copy_tables(p.copy, 0, 1);
+    __syncthreads();
   }
-  if (threadIdx.x == 0) s_len = atomicExch(p.t.sl + r, 0);
-  __syncthreads();
-  const int len = s_len;
-  if (len <= 0) {
-    if (threadIdx.x == 0 && len < 0) raise_error(kErrTable);
-    return;
-  }
-  int pages = ceil_div(len, p.t.P);
-  if (pages > p.t.maxp) {
-    pages = p.t.maxp;
-    if (threadIdx.x == 0) raise_error(kErrTable);
-  }
-  int32_t* row = p.t.bt + (int64_t)r * p.t.maxp;
-  for (int j = threadIdx.x; j < p.t.maxp; j += blockDim.x) {
-    if (j < pages) {
-      const int pg = row[j];
-      if (pg < 0 || pg >= p.t.num_pages) {
-        raise_error(kErrTable);
-      } else if (atomicSub(p.t.ref + pg, 1) <= 0) {  // it was free already: the count stays at 0
-        atomicAdd(p.t.ref + pg, 1);
-        raise_error(kErrTable);
-      }
+  const int lane = threadIdx.x & 31;
+  const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  for (int64_t i = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); i < p.n; i += warps) {
+    const int r = p.rows[i];
+    if (r < 0 || r >= p.t.R) {
+      if (lane == 0) raise_error(kErrTable);
+      continue;
     }
-    row[j] = -1;
+    int len = 0;
+    if (lane == 0) len = atomicExch(p.t.sl + r, 0);
+    len = __shfl_sync(0xffffffffu, len, 0);
+    if (len <= 0) {
+      if (lane == 0 && len < 0) raise_error(kErrTable);
+      continue;
+    }
+    int pages = ceil_div(len, p.t.P);
+    if (pages > p.t.maxp) {
+      pages = p.t.maxp;
+      if (lane == 0) raise_error(kErrTable);
+    }
+    int32_t* row = p.t.bt + (int64_t)r * p.t.maxp;
+    for (int j = lane; j < p.t.maxp; j += 32) {
+      if (j < pages) {
+        const int pg = row[j];
+        if (pg < 0 || pg >= p.t.num_pages) {
+          raise_error(kErrTable);
+        } else if (atomicSub(p.t.ref + pg, 1) <= 0) {  // it was free already: the count stays at 0
+          atomicAdd(p.t.ref + pg, 1);
+          raise_error(kErrTable);
+        }
+      }
+      row[j] = -1;
+    }
   }
 }
 
 // ---- extend -------------------------------------------------------------------------------------
 struct ExtendParams {
   PageTables t;
+  TablesCopyParams copy;  // done by the kernel itself
   const int32_t* add;  // [R]
   int32_t* prefix;     // workspace [R + 1]: pages wanted by the requests before r (cut off at num_pages + 1)
   int32_t* list;       // workspace [num_pages]
@@ -184,6 +194,8 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_extend_kernel(const Extend
   __shared__ int s_scan[33];
   pdl_prologue(0);
   const int tid = threadIdx.x;
+  copy_tables(p.copy, 0, 1);
+  __syncthreads();
   const int64_t cap = (int64_t)p.t.num_pages + 1;  // more than this is never there
   int64_t carry = 0;
   for (int64_t base = 0; base < p.t.R; base += kPlanThreads) {
@@ -325,7 +337,8 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_fork_plan_kernel(const For
     const int c = p.children[i];
     if (c >= 0 && c < p.t.R) p.claim[c] = 0x7fffffff;
   }
-  __syncthreads();
+  // as many free pages as the forks could want, whichever of them are done (its barriers serve the claims)
+  const int found = list_free_pages(ref, p.t.num_pages, min(p.n, p.t.num_pages), p.list, s_scan);
   for (int i = tid; i < p.n; i += kPlanThreads) {
     const int c = p.children[i];
     if (c >= 0 && c < p.t.R) atomicMin(p.claim + c, i);
@@ -362,8 +375,6 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_fork_plan_kernel(const For
     if (i < p.n) p.rec[i] = rec;
     carry += total;
   }
-  const int wanted = min(carry, p.t.num_pages);
-  const int found = wanted > 0 ? list_free_pages(ref, p.t.num_pages, wanted, p.list, s_scan) : 0;
   for (int i = tid; i < p.n; i += kPlanThreads) {  // this thread wrote these records itself
     const int rank = p.rec[i].fresh;
     if (rank < 0) continue;

@@ -811,3 +811,24 @@ def test_page_operators_in_a_graph(dev):
     for _ in range(3):
         graph.replay()
     s.check(bt, sl, ref, pool, err)
+
+
+def test_page_operators_on_large_tables(dev):
+    """Tables that are copied by a launch of their own, and more rows than one CTA takes."""
+    rng, g, sl, bt, ref, pool = _page_case(2, L=1, F=1, H=1, P=1, R=400, spare=40000, maxlen=30)
+    s = _State(dev, g, sl, bt, ref, pool, False)
+    rows = rng.permutation(400)[:150].astype(np.int32)
+    tk.check(tk.topkv_free_requests(s.lo, s.batch, s.tables, s.put(rows), len(rows)))
+    err = od.free_requests(g.P, bt, sl, ref, rows)
+    s.check(bt, sl, ref, pool, err)
+    s = _State(dev, g, sl, bt, ref, pool, False)
+    new = rng.integers(0, 3, size=400).astype(np.int32)
+    new[sl + new > bt.shape[1]] = 0
+    tk.check(tk.topkv_extend_requests(s.lo, s.batch, s.tables, s.put(new), s.ws, s.n))
+    err = od.extend_requests(g.P, bt, sl, ref, new)
+    s.check(bt, sl, ref, pool, err)
+    s = _State(dev, g, sl, bt, ref, pool, True)
+    tk.check(tk.topkv_free_requests(s.lo, s.batch, s.tables, s.put(np.arange(400, dtype=np.int32)), 400))
+    err = od.free_requests(g.P, bt, sl, ref, range(400))
+    s.check(bt, sl, ref, pool, err)
+    assert (ref == 0).all()
