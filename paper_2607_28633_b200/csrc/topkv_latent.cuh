@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
             for (int e = 0; e < boxes; ++e) {
               const int z = __shfl_sync(0xffffffffu, pg, e), y = __shfl_sync(0xffffffffu, at, e);
               if (elect_one())
-                for (int b = half; b < blocks; b += 2) tma_prefetch(&map, b * 64, y, z);
+                for (int b = 2 * unit + half; b < blocks; b += 2 * gridDim.y) tma_prefetch(&map, b * 64, y, z);  // the team shares it
               __syncwarp();
             }
           }
