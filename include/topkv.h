@@ -310,13 +310,14 @@ int topkv_repage_layer(int layer, const void* src_pool, const topkv_layout* src_
  *     and value at once: K[i] = the row (head_dim at most 576, a multiple of 8), V[i] = its first
  *     value_dim elements (a multiple of 16, at most 512), shared by all query heads.
  * Scores, sums and accumulated values are kept in 32 bits; the weights are rounded to 16 bits for
- * the second product (bf16 for a bf16 cache, else fp16) and the result once to io_type.
+ * the second product (bf16 for a bf16 cache, else fp16) and the result once to io_type. (With K and V
+ * planes and head_dim <= 128 a bf16 weight's rest is used too, i.e. the weight has 16 bits of precision.)
  * Long requests are split between CTAs and joined in a fixed order, through d_workspace: the same
  * arguments give the same bits. At most two kernels are enqueued on `stream`; no allocation, no
  * synchronisation, capturable (the first call for a head size and type on a device raises that
- * kernel's shared-memory limit: make it outside a capture). The workspace holds nothing between calls and needs no
- * initialisation; calls that may run at the same time (other streams, two captured graphs) need
- * one each. TOPKV_FLAG_TABLES_SETTLED is honoured; TOPKV_FLAG_OVERLAP_PREVIOUS is ignored (the call
+ * kernel's shared-memory limit: make it outside a capture). The workspace holds nothing between
+ * calls and needs no initialisation; calls that may run at the same time (other streams, two
+ * captured graphs) need one each. TOPKV_FLAG_TABLES_SETTLED is honoured; TOPKV_FLAG_OVERLAP_PREVIOUS is ignored (the call
  * always waits for the kernels before it). cu_seq_lens and total_tokens are optional; a stated
  * total only bounds the lengths. out and lse must not overlap the inputs. A length outside
  * [0, max_pages_per_req * P] is cut to that range and a page id outside the pool is skipped
