@@ -229,7 +229,7 @@ int launch_latent(const AttendParams& p, int units, cudaStream_t s) {
   if (p.row_tile == 32) return launch_latent2<32, BF16>(p, units, s);
   return launch_latent2<64, BF16>(p, units, s);
 }
-static_assert(sizeof(LatentControl) <= 3072, "the largest layout leaves this much of 227 KiB");
+static_assert(latent_smem(64, kLatentMaxD, kLatentMaxDv).total <= kSmemBudget, "the largest layout fits a CTA");
 
 // ---- page operators -------------------------------------------------------------------------------
 int check_pages(const topkv_layout* lo, const topkv_batch* b, Resolved* rs) {

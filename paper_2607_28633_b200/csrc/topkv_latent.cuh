@@ -205,9 +205,9 @@ struct LatentSmem {
   uint32_t p, p_step;  // weights of the first stage's tile, and from there to the second's
   uint32_t stage;      // bytes of a stage
 };
-__host__ __device__ inline LatentSmem latent_smem(int N, int D, int Dv) {
+__host__ __device__ constexpr LatentSmem latent_smem(int N, int D, int Dv) {
   const int blocks = (D + 63) / 64, vblocks = (Dv + 127) / 128 * 2;
-  LatentSmem s;
+  LatentSmem s = {};
   s.stage = (uint32_t)((blocks > vblocks ? blocks : vblocks) * kLatentBlock);
   s.q = 0;
   s.kv = (uint32_t)(blocks * N * 128);

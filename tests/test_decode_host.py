@@ -242,3 +242,52 @@ def test_oracle_page_operators_by_hand():
     assert od.extend_requests(2, bt, sl, ref, [0, 2, 0]) == od.ERR_PAGES
     assert bt[1].tolist() == [2, 6, -1] and sl.tolist() == [6, 4, 6]
     assert od.extend_requests(2, bt, sl, ref, [0, 3, 0]) == od.ERR_TABLE       # longer than its row
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_entry_points_survive_random_descriptors(seed):
+    """Random, mostly malformed descriptors with fake addresses: a status from the documented set every
+    time, and nothing launched."""
+    rng = np.random.default_rng(seed)
+    known = {tk.TOPKV_OK, INVALID, LAYER, ALIGN, CAP, LAYOUT, CUDA}
+    pick = lambda xs: xs[int(rng.integers(0, len(xs)))]
+    before = tk.topkv_kernel_launch_count()
+    seen = set()
+    for _ in range(100):
+        F, H, D, E = pick([(2, 8, 128, 2), (2, 1, 64, 1), (1, 1, 576, 2), (2, 3, 256, 2), (1, 2, 64, 2), (2, 2, 24, 1)])
+        lo = tk.topkv_layout()
+        try:
+            lo = tk.make_layout(pick([1, 5, 80]), F, H, D, E, pick([1, 16, 64, 1000]), pick([1, 100, 1 << 20]))
+        except tk.TopkvError:
+            pass
+        b = _batch(R=pick([0, 1, 16, 5000]), maxp=pick([0, 1, 64, 5000]), T=pick([-1, 0, 100, 1 << 40]))
+        b.window_tokens = pick([0, 0, 1, 128, -1])
+        narrow = E == 1
+        a = _attention(Hq=H * pick([1, 8, 17]), D=D, cache=3 if narrow else pick([1, 2]), Dv=pick([0, 0, 512, 16, D]),
+                       sink_tokens=pick([0, 4, 0x7fffffff]))
+        a.io_type = a.cache_type if not narrow else pick([1, 2])
+        t = _tables()
+        for _ in range(pick([0, 1, 2])):
+            k = pick(range(10))
+            if k == 0: lo.pool_page_stride += pick([8, 16, -16])
+            elif k == 1: lo.page_tokens = pick([0, 0xffffffff, 7])
+            elif k == 2: lo.num_pool_pages = pick([0, -1, 1 << 33])
+            elif k == 3: a.num_q_heads = pick([0, 7, 65535, 1 << 31])
+            elif k == 4: a.out_head_stride = pick([0, 16, 1 << 50, -16])
+            elif k == 5: a.scale = pick([0.0, -1.0, float("nan")])
+            elif k == 6: b.num_requests = pick([-1, 1 << 30])
+            elif k == 7: b.max_pages_per_req = pick([-1, 1 << 30])
+            elif k == 8: t.ref_counts = pick([None, 3])
+            elif k == 9: lo.head_dim = pick([0, 7, 1 << 20])
+        n, off = pick([0, 1 << 12, 1 << 40]), pick([0, 0, 8])
+        for st in (_attend(lo, b, a, layer=pick([0, 0, 7]), pool=0x7000000 + off, n=n),
+                   min(0, tk.topkv_attend_workspace_bytes(lo, b, a)), min(0, tk.topkv_page_workspace_bytes(lo, b, pick([0, 9, -1]))),
+                   tk.topkv_extend_requests(lo, b, t, 0x70000, 0xA000000 + off, n),
+                   tk.topkv_fork_requests(0x7000000, lo, b, t, 0x70000, 0x80000, pick([0, 5, -1]), 0xA000000, n),
+                   tk.topkv_free_requests(lo, b, t, 0x70000, pick([0, 5, -1])),
+                   tk.topkv_compact_pages(0x7000000, lo, b, t, 0x70000, 0x80000, 0xA000000, n),
+                   tk.topkv_copy_pages(0, 1, 0x7000000 + off, lo, 0x70000, 0x80000, 3)):
+            assert st in known, st
+            seen.add(st)
+    assert tk.topkv_kernel_launch_count() == before
+    assert {INVALID, CAP, LAYOUT, CUDA} <= seen

@@ -832,3 +832,36 @@ def test_page_operators_on_large_tables(dev):
     err = od.free_requests(g.P, bt, sl, ref, range(400))
     s.check(bt, sl, ref, pool, err)
     assert (ref == 0).all()
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_attend_random_cases(dev, seed):
+    """Drawn shapes, types, pools, windows and lengths of both kinds of cache."""
+    rng = np.random.default_rng(1000 + seed)
+    pick = lambda xs: xs[int(rng.integers(0, len(xs)))]
+    R = pick([1, 2, 5, 9])
+    sl = rng.integers(0, pick([3, 70, 300, 900]) + 1, size=R)
+    window, sinks = (pick([1, 33, 64, 200]), pick([0, 3, 70])) if rng.random() < 0.3 else (0, 0)
+    P, style = pick([1, 2, 7, 16, 32, 64, 130]), pick(["page", "padded"])
+    if seed % 3 == 2:
+        D = pick([64, 192, 200, 320])
+        _case(dev, 1, 1, pick([1, 9, 16, 30, 65]), D, P, sl, pick(["bf16", "fp16"]), Dv=pick([16, 64]), window=window, sinks=sinks,
+              style=style, seed=seed, extra_cols=pick([0, 3]))
+    else:
+        kind = pick(["bf16", "fp16", "e4m3"])
+        _case(dev, 2, pick([1, 2, 3]), pick([1, 2, 5, 18]), pick([16, 64, 96, 160]), P, sl, kind, pick(["bf16", "fp16"]) if kind == "e4m3" else kind,
+              window=window, sinks=sinks, style=pick([style, "head", "plane"]), seed=seed, extra_cols=pick([0, 3]),
+              out_order=pick(["rh", "hr"]), T=pick([-1, int(sl.sum())]) if window == 0 else -1)
+
+
+def test_attend_negative_and_zero_scale(dev):
+    rng = np.random.default_rng(4)
+    sl = [300, 17]
+    for F, Dv in ((2, 0), (1, 32)):
+        bt, pages = _table(sl, 16, 1, 0, rng)
+        g = _geom(F, 1, 64, 2, 16, pages)
+        pool_h = _cache(g, bt, sl, "fp16", 0, rng)
+        q = od.decode_elements(od.encode_elements(rng.normal(size=2 * 5 * 64), "fp16"), "fp16").reshape(2, 5, 64)
+        for scale in (-0.3, 0.0):
+            got = _run(dev, g, _layout(g), torch.from_numpy(pool_h).to(dev), bt, sl, q, "fp16", "fp16", scale, Dv)
+            _check(got, od.attend(g, 0, pool_h, bt, sl, q, "fp16", "fp16", scale, Dv))
