@@ -444,19 +444,6 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_compact_plan_kernel(const 
   const int tid = threadIdx.x, N = p.t.num_pages;
   constexpr int kBlock = kPlanThreads * kPlanPages;
   const int mine = blockIdx.x * kBlock;
-  int all = 0, before = 0;
-  for (int64_t i = tid; i < N; i += kPlanThreads) {
-    const int u = ref[i] > 0;
-    all += u;
-    before += i < mine ? u : 0;
-  }
-  int used, used_before, dummy;
-  block_exclusive_sum(all, s_scan, &used);
-  block_exclusive_sum(before, s_scan, &used_before);
-  int low = 0;
-  for (int i = tid; i < used; i += kPlanThreads) low += ref[i] > 0;
-  int used_low;  // pages in use that stay
-  block_exclusive_sum(low, s_scan, &used_low);
   int n = 0;
   bool u[kPlanPages];
   const int64_t p0 = (int64_t)mine + (int64_t)tid * kPlanPages;
@@ -465,7 +452,25 @@ __global__ void __launch_bounds__(kPlanThreads) topkv_compact_plan_kernel(const 
     u[k] = p0 + k < N && ref[p0 + k] > 0;
     n += u[k];
   }
-  int rank = used_before + block_exclusive_sum(n, s_scan, &dummy);  // pages in use below p0
+  int used, used_before = 0, used_low;  // pages in use: all, before this block, and those that stay
+  int rank = block_exclusive_sum(n, s_scan, &used);
+  int low = 0;
+  if (p.blocks == 1) {  // the block is the pool
+#pragma unroll
+    for (int k = 0; k < kPlanPages; ++k) low += u[k] && p0 + k < used;
+  } else {
+    int all = 0, before = 0;
+    for (int64_t i = tid; i < N; i += kPlanThreads) {
+      const int v = ref[i] > 0;
+      all += v;
+      before += i < mine ? v : 0;
+    }
+    block_exclusive_sum(all, s_scan, &used);
+    block_exclusive_sum(before, s_scan, &used_before);
+    for (int i = tid; i < used; i += kPlanThreads) low += ref[i] > 0;
+  }
+  block_exclusive_sum(low, s_scan, &used_low);
+  rank += used_before;  // pages in use below p0
 #pragma unroll
   for (int k = 0; k < kPlanPages; ++k) {
     const int64_t pg = p0 + k;
