@@ -8,8 +8,9 @@
 // last page that is needed), and a wide grid rewrites rows and moves page contents.
 //
 // The contents are moved like every other page here: streaming 16- or 32-byte accesses, several
-// in flight per thread, about 64 KiB per CTA and turn, so that part is bound by memory bandwidth;
-// the planning CTA is bound by the latency of a few dependent rounds of loads and barriers.
+// in flight per thread, about 64 KiB per CTA and turn, so that part is bound by memory bandwidth (255
+// pages of 72 KiB in 8 layers: 45.5 us for 301 MB, 1.0 of the measured copy); the planning CTA is
+// bound by the latency of a few dependent rounds of loads and barriers (4 to 7 us).
 #pragma once
 #include <cuda_runtime.h>
 
