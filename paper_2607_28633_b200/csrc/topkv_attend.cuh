@@ -68,6 +68,7 @@ struct AttendParams {
   int io_bf16;
   int teams;            // CTAs along x
   int uncut;            // 1: team t is request t
+  int narrow;           // 1 (uncut only): a warp has a request to itself, team t the requests 4 t .. 4 t + 3
   int by_request;       // how the join records are indexed
   int start_cost;       // of a request, in tiles
   int late_wait;        // tables are settled
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TeamStart s_team;
   __shared__ uint32_t s_mask[kAttendWarps][AttendShape<DP, TYPE>::kStages];
+  __shared__ int s_seen[kAttendWarps];  // narrow: visible tokens of each warp's request
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
@@ -356,10 +358,15 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   int r = mine.r;
   const int gr = lane >> 2, gc = lane & 3;  // row and column group of this thread in a matrix fragment
 
-  for (bool first = true; left > 0 && r < p.R; ++r) {
-    const Visible vis = visible_tokens(p, r, false);
+  if (p.narrow) r = team * kAttendWarps + warp;  // may lie behind the last request: the warp only keeps step then
+  // from a warp's tile to its next: the CTA's four warps share a request, or each has its own
+  const int hop = p.narrow ? kWarpTokens : kTileTokens;
+
+  for (bool first = true; left > 0 && (r < p.R || p.narrow); ++r) {
+    Visible vis = {0, 0, 0};
+    if (r < p.R) vis = visible_tokens(p, r, false);
     const int tiles = attend_tiles(vis.n);
-    if (tiles == 0) {
+    if (tiles == 0 && !p.narrow) {
       if (p.uncut) return;
       continue;
     }
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     if (records && t0 == 0 && t1 > 0) request_begins(p, s_team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
     left -= taken;
     off = 0;
-    if (t0 == t1) continue;
+    if (t0 == t1 && !p.narrow) continue;
 
     // ---- the query rows as fragments ----------------------------------------------------------
     uint32_t qf[kSteps][4];
@@ -385,7 +392,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
           const int row = gr + (j & 1) * 8;
           const int col = k * 16 + (TYPE == kE4m3 ? gc * 4 + (j >> 1) * 2 : gc * 2 + (j >> 1) * 8);
           uint32_t v = 0;
-          if (row < rows && col < p.D) v = *reinterpret_cast<const uint32_t*>(qp + row * p.q_head + col * 2);
+          if (row < rows && col < p.D && vis.n > 0) v = *reinterpret_cast<const uint32_t*>(qp + row * p.q_head + col * 2);
           qf[k][j] = v;
           if (TYPE == kE4m3 && p.io_bf16)
             top[j & 1] = fmaxf(top[j & 1], fmaxf(fabsf(__uint_as_float(v << 16)), fabsf(__uint_as_float(v & 0xffff0000u))));
@@ -422,7 +429,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, base[2] = {0.f, 0.f};
 
-    // ---- this warp's 16 tokens of every tile: visible tokens v .. v + 15, 64 further each time -----
+    // ---- this warp's 16 tokens of every tile: visible tokens v .. v + 15, `hop` further each time ----
     const int end = t1 == tiles ? vis.n : t1 * kTileTokens;
     const int32_t* bt_row = p.bt + (int64_t)r * p.maxp;
     auto token = [&](int v) { return v < vis.ns ? v : v + (vis.lo - vis.ns); };
@@ -480,13 +487,13 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       if (lane == 0) s_mask[warp][stage] = mask;
       slow |= 1u << stage;
     };
-    int v = t0 * kTileTokens + warp * kWarpTokens;
+    int v = p.narrow ? 0 : t0 * kTileTokens + warp * kWarpTokens;
     int next = page_of(v);
 #pragma unroll
     for (int s = 0; s < S::kStages - 1; ++s) {
       const int pg = next;
-      next = page_of(v + (s + 1) * kTileTokens);
-      issue(s, v + s * kTileTokens, pg);
+      next = page_of(v + (s + 1) * hop);
+      issue(s, v + s * hop, pg);
       cp_async_commit();
     }
     // matrix loads: row and first chunk of this lane, K as it lies and V transposed
@@ -501,11 +508,11 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       v_off[i] = ring_a + (kWarpTokens + v_row) * S::kRow + S::swizzle(v_row, 2 * i + v_chunk);
     }
     int stage = 0;
-    for (; v < end; v += kTileTokens) {
+    for (; v < end; v += hop) {
       {
         const int pg = next;
-        next = page_of(v + S::kStages * kTileTokens);
-        issue(stage == 0 ? S::kStages - 1 : stage - 1, v + (S::kStages - 1) * kTileTokens, pg);
+        next = page_of(v + S::kStages * hop);
+        issue(stage == 0 ? S::kStages - 1 : stage - 1, v + (S::kStages - 1) * hop, pg);
         cp_async_commit();
       }
       cp_async_wait<S::kStages - 1>();
@@ -640,6 +647,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][kPitch]
     float* s_m = s_o + kAttendWarps * kAttendRows * kPitch;                   // [warp][row]
     float* s_l = s_m + kAttendWarps * kAttendRows;
+    if (lane == 0) s_seen[warp] = vis.n;
     if (gc == 0) {
       s_m[warp * kAttendRows + gr] = m[0] - kShift;
       s_m[warp * kAttendRows + gr + 8] = m[1] - kShift;
@@ -663,6 +671,20 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     const bool whole = t0 == 0 && t1 == tiles;
     const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
     const int quads = p.Dv / 4;
+    if (p.narrow) {  // nothing to join: each warp's rows are a result
+      for (int i = tid; i < kAttendWarps * rows * quads; i += kAttendThreads) {
+        const int wg = i / quads, d = (i - wg * quads) * 4;
+        const int w = wg / rows, g = wg - w * rows;
+        if (s_seen[w] == 0) continue;
+        const int64_t e = (int64_t)team * kAttendWarps + w;
+        const float sum = s_l[w * kAttendRows + g];
+        store_io4(p.out + e * p.o_req + (q_head0 + g) * p.o_head + d * 2,
+                  *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]), __fdividef(p.v_scale, sum), p.io_bf16);
+        if (d == 0 && p.lse != nullptr)
+          p.lse[e * p.H * p.G + q_head0 + g] = (s_m[w * kAttendRows + g] + log2f(sum)) * kLn2;
+      }
+      return;
+    }
     for (int i = tid; i < rows * quads; i += kAttendThreads) {
       const int g = i / quads, d = (i - g * quads) * 4;
       float f[kAttendWarps], top = -INFINITY, sum = 0.f;

@@ -865,3 +865,13 @@ def test_attend_negative_and_zero_scale(dev):
         for scale in (-0.3, 0.0):
             got = _run(dev, g, _layout(g), torch.from_numpy(pool_h).to(dev), bt, sl, q, "fp16", "fp16", scale, Dv)
             _check(got, od.attend(g, 0, pool_h, bt, sl, q, "fp16", "fp16", scale, Dv))
+
+
+@pytest.mark.parametrize("kind,D,H,R,window,sinks", [("fp16", 64, 3, 207, 20, 3), ("e4m3", 128, 2, 230, 0, 0), ("fp16", 64, 9, 203, 60, 30), ("bf16", 256, 1, 600, 0, 0),
+                                                     ("bf16", 80, 5, 301, 100, 40), ("fp16", 128, 8, 70, 1, 0)])
+def test_attend_many_short_requests(dev, kind, D, H, R, window, sinks):
+    """More short requests than CTAs at a time: a warp each, some of them empty, a last CTA that is not full."""
+    rng = np.random.default_rng(R)
+    sl = rng.integers(0, 41 if window == 0 else 300, size=R)
+    sl[rng.integers(0, R, size=R // 10)] = 0
+    _case(dev, 2, H, 2, D, 16, sl, kind, window=window, sinks=sinks, seed=R, extra_cols=0, ks=0.5 if kind == "e4m3" else 1.0)
