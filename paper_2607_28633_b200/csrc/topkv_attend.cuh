@@ -21,6 +21,7 @@
 //  * a request that lies inside one team is finished by it. Of one that is cut, each team leaves
 //    its (m, l, sum) in the workspace and topkv_attend_join_kernel joins the parts in their
 //    order, so the result does not depend on which CTA ran when.
+//  * many more short requests than CTAs fit at a time take a warp each: no cut, and nothing to join.
 // Scores, maxima, sums and the accumulated values are 32-bit; the weights exp(x - m) are rounded to
 // the 16-bit type of the values for the second product (to fp16 for an 8-bit cache): half a step of
 // 2^-8 (bf16) or 2^-11 of each weight, which averages out over the tokens and stays at or below the
