@@ -45,6 +45,9 @@ constexpr int kTileTokens = kAttendWarps * kWarpTokens;
 constexpr int kAttendRows = 16;      // query heads per CTA (rows of the matrix instruction)
 constexpr int kUncutTiles = 4;       // requests of at most this many tiles are not cut
 constexpr float kLazy = 8.f;         // a running maximum moves when it is exceeded by more than this (powers of two)
+// Sum of a part none of whose tokens counted (their pages are outside the pool). A sum of zero will not do:
+// tokens that count and score minus infinity have that one, and their result is not zero but 0 / 0.
+constexpr float kNoneSeen = -1.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum AttendType { kBf16 = 1, kFp16 = 2, kE4m3 = 3 };
@@ -329,7 +332,8 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TeamStart s_team;
   __shared__ uint32_t s_mask[kAttendWarps][AttendShape<DP, TYPE>::kStages];
-  __shared__ int s_seen[kAttendWarps];  // narrow: visible tokens of each warp's request
+  __shared__ int s_seen[kAttendWarps];  // kUsable: a token of the warp's share counted; narrow: kVisible as well
+  constexpr int kUsable = 1, kVisible = 2;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
@@ -509,6 +513,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       v_off[i] = ring_a + (kWarpTokens + v_row) * S::kRow + S::swizzle(v_row, 2 * i + v_chunk);
     }
     int stage = 0;
+    bool seen = false;  // a token of this warp's counted (uniform)
     for (; v < end; v += hop) {
       {
         const int pg = next;
@@ -521,6 +526,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       const uint32_t at = stage * S::kStage;
       const uint32_t mask = slow >> stage & 1 ? s_mask[warp][stage] : 0xffffu;
       if (mask != 0) {
+        seen = true;
         float s[2][4] = {};
         if constexpr (TYPE == kE4m3) {
 #pragma unroll
@@ -648,7 +654,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][kPitch]
     float* s_m = s_o + kAttendWarps * kAttendRows * kPitch;                   // [warp][row]
     float* s_l = s_m + kAttendWarps * kAttendRows;
-    if (lane == 0) s_seen[warp] = vis.n;
+    if (lane == 0) s_seen[warp] = (seen ? kUsable : 0) | (vis.n > 0 ? kVisible : 0);
     if (gc == 0) {
       s_m[warp * kAttendRows + gr] = m[0] - kShift;
       s_m[warp * kAttendRows + gr + 8] = m[1] - kShift;
@@ -676,16 +682,19 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       for (int i = tid; i < kAttendWarps * rows * quads; i += kAttendThreads) {
         const int wg = i / quads, d = (i - wg * quads) * 4;
         const int w = wg / rows, g = wg - w * rows;
-        if (s_seen[w] == 0) continue;
+        if (s_seen[w] == 0) continue;  // empty_requests has written it
         const int64_t e = (int64_t)team * kAttendWarps + w;
         const float sum = s_l[w * kAttendRows + g];
         store_io4(p.out + e * p.o_req + (q_head0 + g) * p.o_head + d * 2,
-                  *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]), __fdividef(p.v_scale, sum), p.io_bf16);
+                  *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]),
+                  s_seen[w] & kUsable ? __fdividef(p.v_scale, sum) : 0.f, p.io_bf16);
         if (d == 0 && p.lse != nullptr)
           p.lse[e * p.H * p.G + q_head0 + g] = (s_m[w * kAttendRows + g] + log2f(sum)) * kLn2;
       }
       return;
     }
+    const bool any = (s_seen[0] | s_seen[1] | s_seen[2] | s_seen[3]) & kUsable;
+    static_assert(kAttendWarps == 4, "one flag per warp");
     for (int i = tid; i < rows * quads; i += kAttendThreads) {
       const int g = i / quads, d = (i - g * quads) * 4;
       float f[kAttendWarps], top = -INFINITY, sum = 0.f;
@@ -707,12 +716,12 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
         acc.w += c * v.w;
       }
       if (whole) {
-        const float inv = __fdividef(p.v_scale, sum);
+        const float inv = any ? __fdividef(p.v_scale, sum) : 0.f;
         store_io4(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc, inv, p.io_bf16);
         if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;
       } else {
         *reinterpret_cast<float4*>(&p.part[(slot * p.rows + g) * p.Dv + d]) = acc;
-        if (d == 0) p.ml[slot * p.rows + g] = make_float2(top, sum);
+        if (d == 0) p.ml[slot * p.rows + g] = make_float2(top, any ? sum : kNoneSeen);
       }
     }
     __syncthreads();
@@ -772,14 +781,22 @@ __global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(cons
     constexpr int kHeld = 2;
     float2 held[kHeld];
     float top = -INFINITY, sum = 0.f;
+    bool seen = false;  // a part has a token that counted; one that has none weighs 2^-inf = 0 below
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
       const int k = lane + 32 * j;
-      held[j] = k < parts ? p.ml[slot(k) + g] : make_float2(-INFINITY, 0.f);
+      held[j] = k < parts ? p.ml[slot(k) + g] : make_float2(-INFINITY, kNoneSeen);
     }
 #pragma unroll
-    for (int j = 0; j < kHeld; ++j) top = fmaxf(top, held[j].x);
-    for (int k = lane + 32 * kHeld; k < parts; k += 32) top = fmaxf(top, p.ml[slot(k) + g].x);
+    for (int j = 0; j < kHeld; ++j) {
+      top = fmaxf(top, held[j].x);
+      seen |= held[j].y != kNoneSeen;
+    }
+    for (int k = lane + 32 * kHeld; k < parts; k += 32) {
+      const float2 ml = p.ml[slot(k) + g];
+      top = fmaxf(top, ml.x);
+      seen |= ml.y != kNoneSeen;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float from = top == -INFINITY ? 0.f : top;
@@ -794,7 +811,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) topkv_attend_join_kernel(cons
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float inv = p.v_scale / sum;
+    const float inv = __any_sync(0xffffffffu, seen) ? p.v_scale / sum : 0.f;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
       if (lane + 32 * j < parts) s_w[g][lane + 32 * j] = held[j].x * inv;

@@ -508,6 +508,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         limit[j] = -INFINITY;
       }
       float top = -INFINITY;  // of head c0 + lane (lane < NC)
+      uint32_t usable = 0;    // which of the tokens of this warp's half of the tiles counted, over all tiles
       for (int i = 0; i < count; ++i) {
         const uint32_t k = n + i, st = k & 1;
         wait(b_full + 8 * st, k >> 1);  // for ctl.valid
@@ -515,7 +516,8 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         tcgen05_after_sync();
         uint32_t raw[2 * C];
         tmem_load_half<2 * C>(raw, tmem + lanes + st * N + c0);
-        const uint32_t valid = ctl.valid[st][quarter >> 1] >> ((quarter & 1) * 16 + (lane >> 2));
+        const uint32_t counted = ctl.valid[st][quarter >> 1], valid = counted >> ((quarter & 1) * 16 + (lane >> 2));
+        usable |= counted;
         const bool seen0 = valid & 1, seen1 = valid >> 8 & 1;
         tmem_wait_load();
         float x[2 * C], e[2 * C];
@@ -602,7 +604,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       // tile's writers wait below until this turn has been read
       float* const red = s_red + ((n + count) & 1) * 4 * N;
       red[quarter * N + c0 + mine_col] = total;
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + half), "n"(kSoftmaxWarps * 16) : "memory");
+      const bool seen = bar_any(1 + half, kSoftmaxWarps * 16, usable != 0);  // a token of the segment counted
       if (lane < NC) {  // from here on: of head c0 + lane
         const int c = c0 + lane;
         total = (red[c] + red[N + c]) + (red[2 * N + c] + red[3 * N + c]);
@@ -611,10 +613,10 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
       const bool whole = t0 == 0 && t1 == tiles;
       const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
       const int head = c0 + lane;
-      const float inv = 1.f / total;
+      const float inv = seen ? 1.f / total : 0.f;
       if (quarter == 0 && lane < NC && head < rows) {
         if (!whole)
-          p.ml[slot * p.rows + head] = make_float2(top - kShift, total);
+          p.ml[slot * p.rows + head] = make_float2(top - kShift, seen ? total : kNoneSeen);
         else if (p.lse != nullptr)
           p.lse[(int64_t)r * p.G + g0 + head] = (top - kShift + log2f(total)) * kLn2;
       }

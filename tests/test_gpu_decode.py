@@ -875,3 +875,63 @@ def test_attend_many_short_requests(dev, kind, D, H, R, window, sinks):
     sl = rng.integers(0, 41 if window == 0 else 300, size=R)
     sl[rng.integers(0, R, size=R // 10)] = 0
     _case(dev, 2, H, 2, D, 16, sl, kind, window=window, sinks=sinks, seed=R, extra_cols=0, ks=0.5 if kind == "e4m3" else 1.0)
+
+
+# ------------------------------------------------------------------------- requests all of whose pages are unusable
+
+@pytest.mark.parametrize("F,kind,H,G,D,Dv,sl", [
+    (2, "bf16", 2, 3, 64, 0, [60, 130, 0]),          # finished by one CTA
+    (2, "e4m3", 2, 3, 80, 0, [60, 130, 0]),
+    (2, "bf16", 1, 2, 64, 0, [900, 4000, 70]),       # cut between CTAs and joined
+    (2, "fp16", 2, 18, 256, 0, [900, 4000, 70]),
+    (2, "e4m3", 1, 2, 128, 0, [900, 4000, 70]),
+    (2, "fp16", 2, 2, 16, 0, [40] * 700),            # a warp each
+    (2, "e4m3", 2, 2, 64, 0, [40] * 700),
+    (1, "bf16", 1, 20, 192, 128, [60, 130, 0]),
+    (1, "fp16", 1, 70, 128, 128, [900, 4000, 70]),
+    (1, "bf16", 1, 16, 576, 512, [900, 4000, 70]),
+])
+def test_attend_requests_without_a_usable_page(dev, F, kind, H, G, D, Dv, sl):
+    """A page outside the pool counts as not visible; a request that has no other sees nothing, which is
+    zeros and a log-sum-exp of minus infinity. The others are not touched by it."""
+    rng = np.random.default_rng(31)
+    io = "bf16" if kind == "e4m3" else kind
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(F, H, D, 1 if kind == "e4m3" else 2, 16, pages)
+    pool_h = _cache(g, bt, sl, kind, 0, rng)
+    q = od.decode_elements(od.encode_elements(rng.normal(size=len(sl) * H * G * D), io), io).reshape(len(sl), H * G, D)
+    want = od.attend(g, 0, pool_h, bt, sl, q, kind, io, 0.1, Dv)
+    bad = [1] if len(sl) < 10 else list(range(3, len(sl), 7))
+    broken = bt.copy()
+    broken[bad] = pages + 1
+    out, lse = _run(dev, g, _layout(g), torch.from_numpy(pool_h).to(dev), broken, sl, q, kind, io, 0.1, Dv)
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
+    assert (out[bad] == 0).all() and (lse[bad] == -np.inf).all()
+    good = [r for r in range(len(sl)) if r not in bad]
+    _check((out[good], lse[good]), tuple(x[good] for x in want))
+
+
+@pytest.mark.parametrize("sl", [[70, 40], [3000, 40]])
+def test_attend_infinite_keys_beside_unusable_pages(dev, sl):
+    """Scores of minus infinity are scores: a request that sees nothing else has no finite result, also where
+    some of its pages are unusable, whole or cut between CTAs."""
+    rng = np.random.default_rng(32)
+    for F, Dv in ((2, 0), (1, 16)):
+        bt, pages = _table(sl, 16, 1, 0, rng)
+        g = _geom(F, 1, 16, 2, 16, pages)
+        pool = np.zeros(g.pool_bytes(), np.uint8)
+        ones = od.encode_elements(np.ones(16), "fp16")
+        for p in range(pages):
+            for c in range(F):
+                for t in range(16):
+                    a = od.row_offset(g, 0, p, c, t, 0)
+                    pool[a:a + 32] = ones
+                    if c == 0:
+                        pool[a:a + 2] = od.encode_elements(np.array([-np.inf]), "fp16")
+        broken = bt.copy()
+        broken[0, 1:] = -1                                   # request 0 keeps its first page only
+        out, lse = _run(dev, g, _layout(g), torch.from_numpy(pool).to(dev), broken, sl, np.ones((2, 3, 16)), "fp16", "fp16", 1.0, Dv)
+        assert tk.topkv_device_error_flags() == 2
+        tk.check(tk.topkv_reset_device_error_flags())
+        assert np.isnan(out[..., 0]).all() and (lse == -np.inf).all()
