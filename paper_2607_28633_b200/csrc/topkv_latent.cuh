@@ -225,6 +225,17 @@ __host__ __device__ constexpr LatentSmem latent_smem(int N, int D, int Dv) {
   return s;
 }
 
+// What a load warp waits for before it fills a stage again: the group of its i-th wait, -1 behind the last.
+// A barrier tells its phases apart by parity only, so a wait that lies two phases back passes at once: no
+// warp may wait for a group whose release of the tile before it has not seen. Products end in order, so
+// the release of group 0 implies that of all groups one tile earlier; both lists therefore begin with it.
+__host__ __device__ constexpr int rows_await(int i, int vblocks) {  // ..., then the last: the whole stage is free
+  return i == 0 ? 0 : i == 1 && vblocks > 1 ? vblocks - 1 : -1;
+}
+__host__ __device__ constexpr int pieces_await(int i, int half, int vblocks) {  // ..., then the groups that the warp brings
+  return i == 0 ? 0 : half + 2 * (i - 1) < vblocks ? half + 2 * (i - 1) : -1;
+}
+
 template <int N, bool BF16>
 __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const AttendParams p, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
   constexpr int NC = N / 2;                       // heads per softmax warp
@@ -345,7 +356,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
         const bool pieces = boxes > 0 && __all_sync(0xffffffffu, lane >= boxes || (pg >= 0 && pg < p.num_pages));
         if (pieces) {
           // ctl.valid of the tile before has been read when its products begin
-          if (k >= 2) wait(b_free + 32 * g, (k >> 1) - 1);
+          if (k >= 2) wait(b_free + 32 * g + 8 * pieces_await(0, half, vblocks), (k >> 1) - 1);
           // both warps come to the same answer; each takes every other group
           int own = half == (last & 1) ? max(blocks - 2 * vblocks, 0) : 0;  // blocks that this warp brings
           for (int v = half; v < vblocks; v += 2) own += min(2, blocks - 2 * v);
@@ -357,7 +368,7 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
           }
           __syncwarp();
           const uint32_t dst = base + lay.kv + g * lay.stage;
-          for (int v = half; v < vblocks; v += 2) {
+          for (int w = 1, v; (v = pieces_await(w, half, vblocks)) >= 0; ++w) {
             if (k >= 2) wait(b_free + 32 * g + 8 * v, (k >> 1) - 1);
             for (int e = 0; e < boxes; ++e) {
               const int z = __shfl_sync(0xffffffffu, pg, e), y = __shfl_sync(0xffffffffu, at, e);
@@ -396,7 +407,8 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
             off = (int64_t)page * p.S_page + (int64_t)(tok - j * p.P) * p.S_tok;
         }
         const uint32_t valid = __ballot_sync(0xffffffffu, off >= 0);
-        if (k >= 2) wait(b_free + 32 * g + 8 * last, (k >> 1) - 1);
+        if (k >= 2)
+          for (int w = 0, v; (v = rows_await(w, vblocks)) >= 0; ++w) wait(b_free + 32 * g + 8 * v, (k >> 1) - 1);
         if (lane == 0) ctl.valid[g][half] = valid;
         // a warp-wide copy brings 128 bytes of four rows, so source and destination advance by a
         // constant from one block of 64 columns to the next
