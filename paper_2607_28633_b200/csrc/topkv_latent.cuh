@@ -27,7 +27,9 @@
 // Running maxima move only when a tile exceeds them by more than 2^8, so the accumulator is rescaled
 // a few times per request and not once per tile; the weights are at most 2^8 (fp16: scaled by
 // 2^7, to stay below 2^15), which costs no precision in a floating type.
-// Every wait is bounded; one that runs out raises error bit 1 and lets the CTA finish.
+// Every wait on a barrier is bounded; one that runs out raises error bit 1 and lets the CTA finish. The
+// allocation of TMEM waits for CTAs that hold it, which all end by themselves: the next launch is let in
+// only once every CTA of this one has its share.
 // Measured, 576 / 512 columns in bf16: 32 requests of 1,024 to 8,192 tokens, 128 heads: 77 us, 0.48 Pflop/s
 // (0.68 at 16,384 tokens each), a tile of 64 tokens and 64 heads in 2,930 cycles, of which the tensor core
 // needs 2,070; 16 heads, 32 x 16,384 tokens: 107 us = 5.6 TB/s. What remains is the time from giving up a
@@ -284,12 +286,14 @@ __global__ void __launch_bounds__(kLatentThreads, 1) topkv_latent_kernel(const A
     tcgen05_before_sync();
   }
   if (!p.late_wait) pdl_wait_prior_grid();
-  pdl_release_next_grid();
   const TeamRange mine = team_range<kLatentThreads>(p, team, &ctl.team);
   if (p.late_wait) pdl_wait_prior_grid();
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = ctl.tmem;
+  // Not before this CTA has its TMEM: a CTA of the next launch that found room on this SM would hold some
+  // while it waits for this grid, and a CTA of this grid could ask in vain.
+  pdl_release_next_grid();
   const bool records = !p.uncut && unit == 0 && tid == 0;
   if (records && !p.by_request) write_join(p, 0, team, 0, 0);
   empty_requests<kLatentThreads>(p, team, (int64_t)g0, rows, unit == 0);
