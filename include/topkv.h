@@ -382,7 +382,10 @@ int64_t topkv_page_workspace_bytes(const topkv_layout* layout, const topkv_batch
 /* seq_lens[r] += d_new_tokens[r] (DEVICE int32 [R], >= 0), with the pages that takes. Requests are
  * served in order: r gets its pages if the free ones suffice for it and for every request before
  * it (a request that needs no new page always succeeds). A partly filled last page is filled up
- * where it is: it must be the request's own, as topkv_fork_requests leaves it. */
+ * where it is: it must be the request's own, as topkv_fork_requests leaves it. A request that got
+ * nothing keeps its length, so an unpack of "the last n tokens" would write the new tokens' K/V over
+ * cached ones: leave such requests out of it, by a batch whose seq_lens are 0 for them and whose
+ * cu_seq_lens count the wire rows as they were sent (as session.DecodeCache.append does). */
 int topkv_extend_requests(const topkv_layout* layout, const topkv_batch* batch,
                           const topkv_page_tables* tables, const int32_t* d_new_tokens,
                           void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream);

@@ -7,8 +7,9 @@ layer from the host slab into its own paged pool, checksumming as it goes, and c
 headers when the last layer is in; a mismatch is reported per request so that the caller can
 retry (§3.1). ``DecodeCache`` is what the decode side does next with the pool it has received:
 it gives new tokens their pages, writes their K/V, attends to the cache, forks and frees
-requests and compacts the pool. All of them only issue library calls on the streams they are
-given: no pack / unpack arithmetic happens in Python, and nothing here touches the CPU oracle.
+requests and compacts the pool. All of them only enqueue work on the streams they are given,
+library calls and, for the bookkeeping of new tokens, a few small tensor operations: no pack /
+unpack arithmetic happens in Python, and nothing here touches the CPU oracle.
 """
 from __future__ import annotations
 
@@ -106,13 +107,72 @@ class TransferReceiver(Endpoint):
         return out
 
 
+class _NewTokens:
+    """Which rows of a DecodeCache have tokens whose K/V are still to be written, kept on the device,
+    where alone it is known which requests an extension refused. ``append`` writes a row if its last
+    wish was met and it is longer than what has been written; every row keeps the wire rows that it
+    asked for, so that the caller's slab fits whatever was refused. All methods work on the current
+    stream."""
+
+    def __init__(self, seq_lens: torch.Tensor):
+        self.seq_lens = seq_lens
+        self.row = torch.arange(len(seq_lens), dtype=torch.int32, device=seq_lens.device)
+        self.state = torch.zeros((2, len(seq_lens)), dtype=torch.int32, device=seq_lens.device)
+        self.written, self.asked = self.state       # tokens whose K/V are there, length asked for
+        self.lens = torch.zeros_like(seq_lens)      # append's lengths: 0 leaves a row out
+        self.offsets: dict[int, torch.Tensor] = {}  # tokens of a call -> first wire row of each request
+        self.known = False                          # an extension says what is new ...
+        self.pending = False                        # ... and its appends are not all enqueued yet
+
+    def extending(self, new: torch.Tensor):
+        if self.pending:
+            torch.minimum(self.written, self.seq_lens, out=self.written)
+        else:
+            self.written.copy_(self.seq_lens)
+        torch.add(self.seq_lens, new.clamp(min=0), out=self.asked)
+        self.known = self.pending = True
+
+    def update(self):
+        torch.mul(self.seq_lens, (self.seq_lens == self.asked) & (self.seq_lens > self.written), out=self.lens)
+        for tokens, first in self.offsets.items():
+            torch.cumsum(self.asked.clamp(max=tokens), 0, out=first[1:])
+
+    def first_rows(self, tokens: int) -> torch.Tensor:
+        if tokens not in self.offsets:
+            self.offsets[tokens] = torch.zeros(len(self.seq_lens) + 1, dtype=torch.int64, device=self.seq_lens.device)
+            torch.cumsum(self.asked.clamp(max=tokens), 0, out=self.offsets[tokens][1:])
+        return self.offsets[tokens]
+
+    def all_written(self):
+        torch.maximum(self.written, self.lens, out=self.written)
+        self.pending = False
+
+    def freed(self, rows: torch.Tensor):
+        if self.pending:
+            self.state.masked_fill_((rows[:, None] == self.row).any(0), 0)
+            self.update()
+        else:
+            self.known = False
+
+    def forked(self, parents: torch.Tensor, children: torch.Tensor, before: torch.Tensor | None):
+        if self.pending:  # a row that was forked into (its length says so) is where its parent is
+            n = len(parents)
+            which = torch.where(children[:, None] == self.row, torch.arange(n, device=self.row.device)[:, None], n).amin(0)
+            parent = torch.cat([parents, parents.new_zeros(1)])[which].clamp(0, len(self.row) - 1).long()
+            self.state.copy_(torch.where(self.seq_lens != before, self.state[:, parent], self.state))
+            self.update()
+        else:
+            self.known = False
+
+
 class DecodeCache:
     """The paged cache of a decode worker, from the tables of a receiver (or any pool and tables):
     ``rows`` request slots of ``max_pages`` pages each, of which the first ones hold the requests
     that have arrived. All tables live on the device and are changed in place by the calls below,
     which only enqueue work on ``stream``; calls are ordered by the stream they are given, and one
     object's calls must not run at the same time (they share a workspace). ``max_forks`` bounds
-    the forks of one call."""
+    the forks of one call. In a CUDA graph an extension stands together with its appends, or both are
+    made outside."""
 
     def __init__(self, pool: torch.Tensor, layout: tk.topkv_layout, block_table: torch.Tensor, seq_lens: torch.Tensor,
                  rows: int | None = None, max_pages: int | None = None, max_forks: int = 64):
@@ -136,20 +196,46 @@ class DecodeCache:
         self.num_used = torch.zeros(1, dtype=torch.int32, device=dev)
         self.page_map = torch.zeros(layout.num_pool_pages, dtype=torch.int32, device=dev)
         self._attend_ws = None
+        self._new = _NewTokens(self.seq_lens)
         torch.cuda.current_stream(dev).synchronize()
 
+    def _on(self, stream):
+        """torch's work on the stream that the library's calls are given: a torch stream, a handle or None."""
+        if stream is None or stream == 0:
+            stream = torch.cuda.default_stream(self.pool.device)
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, self.pool.device)
+        return torch.cuda.stream(stream)
+
     def extend(self, new_tokens: torch.Tensor, stream):
-        """Room for new_tokens[r] (device int32 [rows]) more tokens of every request."""
-        tk.check(tk.topkv_extend_requests(self.layout, self.batch, self.tables, new_tokens, self.workspace,
-                                          self.workspace.numel(), stream))
+        """Room for new_tokens[r] (device int32 [rows]) more tokens of every request. A request for which
+        there is no page stays as it is (error bit 8) and is left out by the appends that follow."""
+        with self._on(stream):
+            self._new.extending(new_tokens)
+            tk.check(tk.topkv_extend_requests(self.layout, self.batch, self.tables, new_tokens, self.workspace,
+                                              self.workspace.numel(), stream))
+            self._new.update()
 
     def append(self, layer: int, kv: torch.Tensor, stream, tokens: int = 1):
-        """Writes the K/V of the last ``tokens`` tokens of every request: ``kv`` is a wire slab of
-        min(length, tokens) tokens per request, in request order (empty rows contribute none)."""
-        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens)
+        """Writes the K/V of the last ``tokens`` tokens of every request that has new ones: ``kv`` is a
+        wire slab of min(length, tokens) tokens per request, in request order (empty rows contribute
+        none). The tokens of a request that has not grown since the last append, or that the last
+        ``extend`` refused, are left as they are; it keeps its place in the slab, a refused one the
+        min(length + new_tokens, tokens) tokens that it asked for. Without an ``extend`` since the last
+        fork or free every request is written. ``tokens`` beyond what a request grew by write older
+        tokens again, which must not lie in shared pages. The last layer's append ends the turn."""
+        new = self._new
+        if new.known:
+            with self._on(stream):
+                b = tk.make_batch(self.block_table, new.lens, cu_seq_lens=new.first_rows(tokens), window_tokens=tokens)
+        else:
+            b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens)
         at = layer * self.layout.wire_layer_stride  # the call adds it: kv is this layer's slab alone
         tk.check(tk.topkv_unpack_layer(layer, self.pool, self.layout, b, kv.data_ptr() - at, kv.numel() * kv.element_size() + at,
                                        stream))
+        if new.known and layer == self.layout.num_layers - 1:
+            with self._on(stream):
+                new.all_written()
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
                window_tokens: int = 0, **attention):
@@ -170,11 +256,18 @@ class DecodeCache:
         """Row children[i] becomes a copy of row parents[i] that shares its full pages."""
         if parents.numel() != children.numel() or parents.numel() > self.max_forks:
             raise ValueError("as many parents as children, at most max_forks")
-        tk.check(tk.topkv_fork_requests(self.pool, self.layout, self.batch, self.tables, parents, children, parents.numel(),
-                                        self.workspace, self.workspace.numel(), stream))
+        if parents.numel() == 0:
+            return
+        with self._on(stream):
+            before = self.seq_lens.clone() if self._new.pending else None
+            tk.check(tk.topkv_fork_requests(self.pool, self.layout, self.batch, self.tables, parents, children, parents.numel(),
+                                            self.workspace, self.workspace.numel(), stream))
+            self._new.forked(parents, children, before)
 
     def free(self, rows: torch.Tensor, stream):
-        tk.check(tk.topkv_free_requests(self.layout, self.batch, self.tables, rows, rows.numel(), stream))
+        with self._on(stream):
+            tk.check(tk.topkv_free_requests(self.layout, self.batch, self.tables, rows, rows.numel(), stream))
+            self._new.freed(rows)
 
     def compact(self, stream):
         """Afterwards pages 0 .. num_used - 1 are the ones in use; page_map has every page's new id."""

@@ -935,3 +935,110 @@ def test_attend_infinite_keys_beside_unusable_pages(dev, sl):
         assert tk.topkv_device_error_flags() == 2
         tk.check(tk.topkv_reset_device_error_flags())
         assert np.isnan(out[..., 0]).all() and (lse == -np.inf).all()
+
+
+# ------------------------------------------------------------------------- appends behind refusals
+
+def _append_oracle(g, pool, bt, before, after, new, layer, rows):
+    """One new token per request that asked for one, `rows` in request order; refused ones are skipped."""
+    at, row = 0, rows.reshape(-1, g.F, g.h_kv, g.d_h * g.b_p)
+    for r in range(len(after)):
+        wanted = int(before[r]) + int(new[r])
+        if wanted > 0:
+            if new[r] and after[r] == wanted:
+                i = wanted - 1
+                for c in range(g.F):
+                    for h in range(g.h_kv):
+                        a = od.row_offset(g, layer, int(bt[r, i // g.P]), c, i % g.P, h)
+                        pool[a:a + g.d_h * g.b_p] = row[at, c, h]
+            at += 1
+
+
+@pytest.mark.parametrize("held", [0, 2])   # pages that somebody else has: without them there are enough
+@pytest.mark.parametrize("captured", [False, True])
+def test_decode_cache_with_too_few_pages(dev, captured, held):
+    """Turns in a pool that runs out of pages: requests are refused, freed and extended again, on a side
+    stream, call by call or as a graph that holds the extension and the appends of a turn."""
+    from paper_2607_28633_b200 import session
+    rng = np.random.default_rng(5)
+    g = _geom(2, 2, 64, 2, 4, 9, L=2)
+    bt = np.full((6, 6), -1, np.int32)
+    sl = np.array([4, 8, 3, 6, 0, 0], np.int32)
+    bt[0, 0], bt[1, :2], bt[2, 0], bt[3, :2] = 7, (2, 5), 0, (8, 1)
+    lo = tk.make_layout(2, 2, 2, 64, 2, 4, 9, wire_layer_stride=6 * 512)
+    pool_h = rng.integers(0, 256, g.pool_bytes(), dtype=np.uint8)
+    pool = torch.from_numpy(pool_h).to(dev)
+    cache = session.DecodeCache(pool, lo, torch.from_numpy(bt).to(dev), torch.from_numpy(sl).to(dev))
+    cache.ref_counts[3:3 + held] += 1
+    ref = cache.ref_counts.cpu().numpy().copy()
+    s = torch.cuda.Stream(dev)
+    d_new = torch.zeros(6, dtype=torch.int32, device=dev)
+    d_kv = [torch.zeros(6 * 512, dtype=torch.uint8, device=dev) for _ in range(2)]
+    rows = torch.zeros(1, dtype=torch.int32, device=dev)
+
+    def turn(stream):
+        cache.extend(d_new, stream)
+        for layer in range(2):
+            cache.append(layer, d_kv[layer], stream)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    err = 0
+    for n, (new, ended) in enumerate([([1, 1, 1, 1, 0, 0], 1), ([0, 0, 1, 1, 0, 0], 4), ([1, 0, 1, 2, 1, 0], 3), ([1, 1, 1, 0, 1, 1], 5),
+                                      ([3, 0, 2, 0, 1, 1], 0), ([4, 4, 1, 0, 1, 1], 2), ([1, 1, 1, 1, 1, 1], 5)]):
+        new = np.array(new, np.int32)
+        d_new.copy_(torch.from_numpy(new))
+        kv = [rng.integers(0, 256, 6 * 512, dtype=np.uint8) for _ in range(2)]
+        for d, h in zip(d_kv, kv):
+            d.copy_(torch.from_numpy(h))
+        rows.fill_(ended)
+        torch.cuda.synchronize()
+        if captured and n == 1:
+            with torch.cuda.graph(graph, stream=s):
+                turn(torch.cuda.current_stream())
+        if captured and n >= 1:
+            graph.replay()
+        else:
+            turn(s)
+        torch.cuda.synchronize()
+        before = sl.copy()
+        err |= od.extend_requests(4, bt, sl, ref, new)
+        for layer in range(2):
+            _append_oracle(g, pool_h, bt, before, sl, new, layer, kv[layer])
+        for got, want in ((cache.block_table, bt), (cache.seq_lens, sl), (cache.ref_counts, ref), (pool, pool_h)):
+            assert np.array_equal(got.cpu().numpy(), want), n
+        cache.free(rows, s)
+        err |= od.free_requests(4, bt, sl, ref, [ended])
+    torch.cuda.synchronize()
+    assert err == tk.topkv_device_error_flags() == (8 if held else 0)
+    tk.check(tk.topkv_reset_device_error_flags())
+
+
+def test_decode_cache_frees_and_forks_between_extend_and_append(dev):
+    """A refused request is freed or forked before the appends: places in the slab and tokens stay right."""
+    from paper_2607_28633_b200 import session
+    g = _geom(2, 1, 8, 2, 4, 4)
+    lo = tk.make_layout(1, 2, 1, 8, 2, 4, 4)
+    mark = lambda cache, r, i: {int(x) for c in range(2) for x in cache.pool.cpu().numpy()[
+        od.row_offset(g, 0, int(cache.block_table[r, i // 4]), c, i % 4, 0):][:16]}
+    put = lambda *x: torch.tensor(x, dtype=torch.int32, device=dev)
+    slab = lambda *m: torch.tensor(m, dtype=torch.uint8, device=dev)[:, None].expand(len(m), 32).contiguous()
+
+    def start():
+        cache = session.DecodeCache(torch.full((g.pool_bytes(),), 9, dtype=torch.uint8, device=dev), lo,
+                                    put(0, -1, 1, -1, 2, -1, -1, -1).view(4, 2), put(4, 3, 4, 0))
+        cache.extend(put(1, 1, 1, 0), None)                  # row 2 is refused
+        return cache
+    cache = start()
+    cache.free(put(0, -3, 77), None)
+    cache.append(0, slab(21, 22), None)
+    torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == [0, 4, 4, 0] and mark(cache, 1, 3) == {21} and mark(cache, 2, 3) == {9}
+    cache = start()
+    cache.fork(put(2, 1, 2), put(3, 3, 0), None)             # the refused parent's child is refused as well
+    cache.append(0, slab(31, 32, 33, 34), None)
+    torch.cuda.synchronize()
+    assert cache.seq_lens.tolist() == [5, 4, 4, 4]
+    assert [mark(cache, r, i) for r, i in ((0, 4), (0, 3), (1, 3), (2, 3), (3, 3))] == [{31}, {9}, {32}, {9}, {9}]
+    torch.cuda.synchronize()
+    assert tk.topkv_device_error_flags() == 8 | 2            # pages; rows outside the table, a row named twice
+    tk.check(tk.topkv_reset_device_error_flags())
