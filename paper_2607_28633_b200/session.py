@@ -197,6 +197,7 @@ class DecodeCache:
         self.page_map = torch.zeros(layout.num_pool_pages, dtype=torch.int32, device=dev)
         self._attend_ws = None
         self._new = _NewTokens(self.seq_lens)
+        self._first_rows = None
         torch.cuda.current_stream(dev).synchronize()
 
     def _on(self, stream):
@@ -229,7 +230,14 @@ class DecodeCache:
             with self._on(stream):
                 b = tk.make_batch(self.block_table, new.lens, cu_seq_lens=new.first_rows(tokens), window_tokens=tokens)
         else:
-            b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens)
+            first = None
+            if len(self.seq_lens) > tk.TOPKV_MAX_INLINE_R:  # a copy works the wire rows out itself up to there
+                if self._first_rows is None:
+                    with self._on(stream):
+                        self._first_rows = torch.empty(len(self.seq_lens) + 1, dtype=torch.int64, device=self.pool.device)
+                first = self._first_rows
+                tk.check(tk.topkv_build_plan(tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens), first, stream))
+            b = tk.make_batch(self.block_table, self.seq_lens, cu_seq_lens=first, window_tokens=tokens)
         at = layer * self.layout.wire_layer_stride  # the call adds it: kv is this layer's slab alone
         tk.check(tk.topkv_unpack_layer(layer, self.pool, self.layout, b, kv.data_ptr() - at, kv.numel() * kv.element_size() + at,
                                        stream))

@@ -280,3 +280,21 @@ def test_random_turns(make, seed):
                 for c in range(2):
                     a = od.row_offset(g, 1, int(cache.block_table[r, i // P]), c, i % P, 0)
                     cache.pool[a:a + 16] = m
+
+
+def test_append_to_more_rows_than_a_copy_counts_itself(make):
+    """1,025 rows, before an extension and after one."""
+    g = Geom(num_pages=6, **GEOM)
+    bt, sl = np.full((1025, 2), -1), np.zeros(1025, np.int64)
+    bt[3, 0], bt[1024, 0], sl[3], sl[1024] = 4, 2, 2, 3
+    cache, _ = make(g, bt, sl)
+    cache.append(0, _slab(1, 2), None)
+    assert (_mark(g, cache, 0, 3, 1), _mark(g, cache, 0, 1024, 2)) == (1, 2)
+    new = torch.zeros(1025, dtype=torch.int32)
+    new[1024] = new[7] = 1
+    cache.extend(new, None)
+    cache.append(0, _slab(3, 4, 5), None)
+    assert [_mark(g, cache, 0, r, i) for r, i in ((3, 1), (7, 0), (1024, 2), (1024, 3))] == [1, 4, 2, 5]
+    cache.free(_ints(3), None)
+    cache.append(1, _slab(6, 7), None)
+    assert (_mark(g, cache, 1, 7, 0), _mark(g, cache, 1, 1024, 3)) == (6, 7)

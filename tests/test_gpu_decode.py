@@ -1042,3 +1042,30 @@ def test_decode_cache_frees_and_forks_between_extend_and_append(dev):
     torch.cuda.synchronize()
     assert tk.topkv_device_error_flags() == 8 | 2            # pages; rows outside the table, a row named twice
     tk.check(tk.topkv_reset_device_error_flags())
+
+
+def test_decode_cache_of_more_rows_than_a_copy_counts_itself(dev):
+    from paper_2607_28633_b200 import session
+    g = _geom(1, 1, 16, 2, 4, 6)
+    bt, sl = torch.full((1100, 2), -1, dtype=torch.int32, device=dev), torch.zeros(1100, dtype=torch.int32, device=dev)
+    bt[3, 0], bt[1090, 0], sl[3], sl[1090] = 4, 2, 2, 3
+    lo = tk.make_layout(1, 1, 1, 16, 2, 4, 6)
+    cache = session.DecodeCache(torch.zeros(g.pool_bytes(), dtype=torch.uint8, device=dev), lo, bt, sl)
+    slab = lambda *m: torch.tensor(m, dtype=torch.uint8, device=dev)[:, None].expand(len(m), 32).contiguous()
+    at = lambda page, t: cache.pool.view(6, 4, 32)[page, t].unique().tolist()
+    s = torch.cuda.Stream(dev)
+    kv = slab(1, 2), slab(3, 4, 5), slab(6, 7)
+    new = torch.zeros(1100, dtype=torch.int32, device=dev)
+    new[1090] = new[1050] = 1
+    torch.cuda.synchronize()
+    cache.append(0, kv[0], s)
+    torch.cuda.synchronize()
+    assert at(4, 1) == [1] and at(2, 2) == [2] and at(4, 0) == [0]
+    cache.extend(new, s)                                     # row 1050 takes page 0
+    cache.append(0, kv[1], s)
+    torch.cuda.synchronize()
+    assert [at(4, 1), at(0, 0), at(2, 2), at(2, 3)] == [[1], [4], [2], [5]]
+    cache.free(torch.tensor([3], dtype=torch.int32, device=dev), s)
+    cache.append(0, kv[2], s)
+    torch.cuda.synchronize()
+    assert at(0, 0) == [6] and at(2, 3) == [7]
