@@ -195,7 +195,7 @@ class DecodeCache:
         self.workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
         self.num_used = torch.zeros(1, dtype=torch.int32, device=dev)
         self.page_map = torch.zeros(layout.num_pool_pages, dtype=torch.int32, device=dev)
-        self._attend_ws = None
+        self._attend_ws: dict[int, torch.Tensor] = {}
         self._new = _NewTokens(self.seq_lens)
         self._first_rows = None
         torch.cuda.current_stream(dev).synchronize()
@@ -253,12 +253,13 @@ class DecodeCache:
         att = tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
         b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=window_tokens)
         n = tk.check(tk.topkv_attend_workspace_bytes(self.layout, b, att))
-        if self._attend_ws is None or self._attend_ws.numel() < n:
-            # on its stream, so that the buffer it replaces is not handed out while a call still uses it
-            with torch.cuda.stream(stream):
-                self._attend_ws = torch.empty(max(n, 16), dtype=torch.uint8, device=self.pool.device)
-        tk.check(tk.topkv_attend_layer(layer, self.pool, self.layout, b, att, q, out, self._attend_ws,
-                                       self._attend_ws.numel(), stream))
+        # One per size (a kind of layer has one, whatever the lengths), kept as long as the cache: captured
+        # graphs hold the address, and calls on other streams may still be using it.
+        if n not in self._attend_ws:
+            with self._on(stream):
+                self._attend_ws[n] = torch.empty(max(n, 16), dtype=torch.uint8, device=self.pool.device)
+        ws = self._attend_ws[n]
+        tk.check(tk.topkv_attend_layer(layer, self.pool, self.layout, b, att, q, out, ws, ws.numel(), stream))
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, stream):
         """Row children[i] becomes a copy of row parents[i] that shares its full pages."""

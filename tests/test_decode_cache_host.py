@@ -3,6 +3,8 @@ on the memory that the calls name, so that what the class itself does (order, de
 workspaces, refusals) is followed without a GPU."""
 import contextlib
 import ctypes
+import gc
+import weakref
 
 import numpy as np
 import pytest
@@ -298,3 +300,34 @@ def test_append_to_more_rows_than_a_copy_counts_itself(make):
     cache.free(_ints(3), None)
     cache.append(1, _slab(6, 7), None)
     assert (_mark(g, cache, 1, 7, 0), _mark(g, cache, 1, 1024, 3)) == (6, 7)
+
+
+def _attend(cache, lib, monkeypatch, needs, stream=None):
+    """Attends once per workspace size; returns the workspaces that the calls were given."""
+    seen = []
+    monkeypatch.setattr(tk, "topkv_attend_layer", lambda layer, pool, lo, b, att, q, out, ws, n, stream=None: seen.append((ws, n)) or 0)
+    R = len(cache.seq_lens)
+    for need in needs:
+        monkeypatch.setattr(tk, "topkv_attend_workspace_bytes", lambda lo, b, att, need=need: need)
+        cache.attend(0, torch.zeros(R, 2, 8, dtype=torch.bfloat16), torch.zeros(R, 2, 8, dtype=torch.bfloat16), 1.0, stream)
+    return seen
+
+
+def test_a_workspace_that_a_call_was_given_stays(make, monkeypatch):
+    """A captured graph keeps the address: a later call that needs more must not give that memory back."""
+    g = Geom(num_pages=6, **GEOM)
+    cache, lib = make(g, [[0, -1], [2, 3]], [4, 6])
+    seen = [(weakref.ref(ws), ws.data_ptr(), n) for ws, n in _attend(cache, lib, monkeypatch, [100, 5000, 100, 0, 5000])]
+    gc.collect()
+    assert all(ws() is not None and n >= need for (ws, _, n), need in zip(seen, [100, 5000, 100, 0, 5000]))
+    assert seen[0][1] == seen[2][1] and seen[1][1] == seen[4][1]     # and is the same for the same need
+
+
+@pytest.mark.parametrize("stream", [None, 0, 12345])
+def test_attend_takes_any_kind_of_stream(make, monkeypatch, stream):
+    """A handle, or none, as the other calls do."""
+    g = Geom(num_pages=6, **GEOM)
+    cache, lib = make(g, [[0, -1], [2, 3]], [4, 6])
+    used = []
+    monkeypatch.setattr(session.DecodeCache, "_on", lambda self, s: used.append(s) or contextlib.nullcontext())
+    assert len(_attend(cache, lib, monkeypatch, [100], stream)) == 1 and used == [stream]

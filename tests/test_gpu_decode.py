@@ -1069,3 +1069,37 @@ def test_decode_cache_of_more_rows_than_a_copy_counts_itself(dev):
     cache.append(0, kv[2], s)
     torch.cuda.synchronize()
     assert at(0, 0) == [6] and at(2, 3) == [7]
+
+
+def test_decode_cache_attends_in_a_graph_beside_larger_calls(dev):
+    """A graph that holds an attention is replayed after a call of another kind has asked for a larger
+    workspace and the memory around has been handed out; streams by handle, and none."""
+    from paper_2607_28633_b200 import session
+    rng = np.random.default_rng(14)
+    sl = [900, 40, 2000]
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(2, 2, 64, 2, 16, pages)
+    pool_h = _cache(g, bt, sl, "bf16", 0, rng)
+    cache = session.DecodeCache(torch.from_numpy(pool_h).to(dev), _layout(g), torch.from_numpy(bt).to(dev),
+                                torch.tensor(sl, dtype=torch.int32, device=dev))
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device=dev)
+    wide = torch.randn(3, 32, 64, device=dev).to(torch.bfloat16)
+    out, wide_out, lse = torch.zeros_like(q), torch.zeros_like(wide), torch.zeros(3, 4, device=dev)
+    torch.cuda.synchronize()
+    cache.attend(0, q, out, 0.125, None, lse=lse)
+    side = torch.cuda.Stream(dev)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        cache.attend(0, q, out, 0.125, torch.cuda.current_stream(), lse=lse)
+    cache.attend(0, wide, wide_out, 0.125, side.cuda_stream)
+    torch.cuda.synchronize()
+    others = [torch.full((1 << 18,), 3, dtype=torch.uint8, device=dev) for _ in range(64)]
+    q_h = od.decode_elements(od.encode_elements(rng.normal(size=3 * 4 * 64), "bf16"), "bf16").reshape(3, 4, 64)
+    q.copy_(torch.from_numpy(q_h).to(torch.bfloat16))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    _check((out.double().cpu().numpy(), lse.double().cpu().numpy()), od.attend(g, 0, pool_h, bt, sl, q_h, "bf16", "bf16", 0.125))
+    assert all((x == 3).all() for x in others)
