@@ -151,6 +151,10 @@ def make_attention(q, out, cache_type: int, io_type: int, scale: float, value_di
             raise ValueError("q and out are [requests][heads][elements] of 16-bit elements, the last axis contiguous")
     if q.shape[:2] != out.shape[:2]:
         raise ValueError("q and out differ in requests or heads")
+    if q.dtype != out.dtype or q.device != out.device or (lse is not None and lse.device != q.device):
+        raise ValueError("q and out differ in type, or the tensors in device")
+    if out.shape[2] < (value_dim or q.shape[2]):
+        raise ValueError("out has room for value_dim elements per head, or as many as q")
     if lse is not None and (tuple(lse.shape) != tuple(q.shape[:2]) or lse.element_size() != 4 or not lse.is_contiguous()):
         raise ValueError("lse is a contiguous float32 [requests][heads]")
     a = topkv_attention()

@@ -134,14 +134,13 @@ class _NewTokens:
 
     def update(self):
         torch.mul(self.seq_lens, (self.seq_lens == self.asked) & (self.seq_lens > self.written), out=self.lens)
-        for tokens, first in self.offsets.items():
-            torch.cumsum(self.asked.clamp(max=tokens), 0, out=first[1:])
+        for tokens in self.offsets:
+            self.count_rows(tokens)
 
-    def first_rows(self, tokens: int) -> torch.Tensor:
+    def count_rows(self, tokens: int):
         if tokens not in self.offsets:
             self.offsets[tokens] = torch.zeros(len(self.seq_lens) + 1, dtype=torch.int64, device=self.seq_lens.device)
-            torch.cumsum(self.asked.clamp(max=tokens), 0, out=self.offsets[tokens][1:])
-        return self.offsets[tokens]
+        torch.cumsum(self.asked.clamp(max=tokens), 0, out=self.offsets[tokens][1:])
 
     def all_written(self):
         torch.maximum(self.written, self.lens, out=self.written)
@@ -208,9 +207,16 @@ class DecodeCache:
             stream = torch.cuda.ExternalStream(stream, self.pool.device)
         return torch.cuda.stream(stream)
 
+    def _check_ints(self, name: str, t: torch.Tensor, count: int | None = None):
+        if t.dtype != torch.int32 or t.ndim != 1 or not t.is_contiguous() or t.device != self.pool.device:
+            raise ValueError(f"{name}: a contiguous int32 vector on the pool's device")
+        if count is not None and t.numel() != count:
+            raise ValueError(f"{name}: {count} entries, one per row")
+
     def extend(self, new_tokens: torch.Tensor, stream):
         """Room for new_tokens[r] (device int32 [rows]) more tokens of every request. A request for which
         there is no page stays as it is (error bit 8) and is left out by the appends that follow."""
+        self._check_ints("new_tokens", new_tokens, len(self.seq_lens))
         with self._on(stream):
             self._new.extending(new_tokens)
             tk.check(tk.topkv_extend_requests(self.layout, self.batch, self.tables, new_tokens, self.workspace,
@@ -225,10 +231,14 @@ class DecodeCache:
         min(length + new_tokens, tokens) tokens that it asked for. Without an ``extend`` since the last
         fork or free every request is written. ``tokens`` beyond what a request grew by write older
         tokens again, which must not lie in shared pages. The last layer's append ends the turn."""
+        if tokens < 1 or not kv.is_contiguous() or kv.device != self.pool.device:
+            raise ValueError("a contiguous slab of one or more tokens per request, on the pool's device")
         new = self._new
         if new.known:
-            with self._on(stream):
-                b = tk.make_batch(self.block_table, new.lens, cu_seq_lens=new.first_rows(tokens), window_tokens=tokens)
+            if tokens not in new.offsets:
+                with self._on(stream):
+                    new.count_rows(tokens)
+            b = tk.make_batch(self.block_table, new.lens, cu_seq_lens=new.offsets[tokens], window_tokens=tokens)
         else:
             first = None
             if len(self.seq_lens) > tk.TOPKV_MAX_INLINE_R:  # a copy works the wire rows out itself up to there
@@ -247,8 +257,13 @@ class DecodeCache:
 
     def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
                window_tokens: int = 0, **attention):
-        """Attention of the newest token of every request; see topkv_attend_layer. ``attention`` goes
-        to make_attention (value_dim, sink_tokens, k_scale, v_scale, lse)."""
+        """Attention of the newest token of every request; see topkv_attend_layer. ``q`` and ``out`` have
+        one entry per row, the empty ones included. ``attention`` goes to make_attention (value_dim,
+        sink_tokens, k_scale, v_scale, lse)."""
+        if q.dtype not in (torch.bfloat16, torch.float16) or q.device != self.pool.device:
+            raise ValueError("q and out are bfloat16 or float16 on the pool's device")
+        if q.ndim != 3 or q.shape[0] != len(self.seq_lens) or q.shape[2] != self.layout.head_dim:
+            raise ValueError(f"q is [{len(self.seq_lens)}][heads][{self.layout.head_dim}]")
         io = tk.TOPKV_TYPE_BF16 if q.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
         att = tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
         b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=window_tokens)
@@ -263,6 +278,8 @@ class DecodeCache:
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, stream):
         """Row children[i] becomes a copy of row parents[i] that shares its full pages."""
+        self._check_ints("parents", parents)
+        self._check_ints("children", children)
         if parents.numel() != children.numel() or parents.numel() > self.max_forks:
             raise ValueError("as many parents as children, at most max_forks")
         if parents.numel() == 0:
@@ -274,6 +291,8 @@ class DecodeCache:
             self._new.forked(parents, children, before)
 
     def free(self, rows: torch.Tensor, stream):
+        """The rows (device int32) give their pages back and become empty."""
+        self._check_ints("rows", rows)
         with self._on(stream):
             tk.check(tk.topkv_free_requests(self.layout, self.batch, self.tables, rows, rows.numel(), stream))
             self._new.freed(rows)

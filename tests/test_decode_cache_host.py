@@ -331,3 +331,49 @@ def test_attend_takes_any_kind_of_stream(make, monkeypatch, stream):
     used = []
     monkeypatch.setattr(session.DecodeCache, "_on", lambda self, s: used.append(s) or contextlib.nullcontext())
     assert len(_attend(cache, lib, monkeypatch, [100], stream)) == 1 and used == [stream]
+
+
+def test_tensors_that_do_not_fit_the_cache_are_refused(make, monkeypatch):
+    """The library sees addresses only: too few rows, another type or order would be read past its end
+    or as other numbers."""
+    g = Geom(num_pages=6, **GEOM)
+    cache, lib = make(g, [[0, -1], [2, 3], [-1, -1]], [4, 6, 0])
+    calls = []
+    for name in ("attend_layer", "extend_requests", "free_requests", "fork_requests", "unpack_layer"):
+        monkeypatch.setattr(tk, f"topkv_{name}", lambda *a, name=name: calls.append(name) or 0)
+    new = _ints(1, 1, 1)
+    for bad in (new[:2], new.long(), new.short(), _ints(1, 1, 1, 1), new[:, None].expand(3, 2), _ints(1, 0, 1, 0, 1, 0)[::2],
+                new.float(), torch.zeros(3, dtype=torch.int32, device="meta")):
+        with pytest.raises(ValueError):
+            cache.extend(bad, None)
+    for bad in (new.long(), _ints(1, 0, 1, 0)[::2], new.view(3, 1), torch.zeros(2, dtype=torch.int32, device="meta")):
+        with pytest.raises(ValueError):
+            cache.free(bad, None)
+        with pytest.raises(ValueError):
+            cache.fork(bad, bad, None)
+        with pytest.raises(ValueError):
+            cache.fork(bad.reshape(-1)[:1].int() if bad.device.type == "cpu" else _ints(0), bad.reshape(-1)[:1].long(), None)
+    for kv, tokens in ((_slab(1, 2)[:, ::2], 1), (_slab(1, 2), 0), (_slab(1, 2), -1), (torch.zeros(64, dtype=torch.uint8, device="meta"), 1)):
+        with pytest.raises(ValueError):
+            cache.append(0, kv, None, tokens=tokens)
+    q = lambda *s, dt=torch.bfloat16, dev="cpu": torch.zeros(*s, dtype=dt, device=dev)
+    for a, b in ((q(2, 2, 8), q(2, 2, 8)), (q(4, 2, 8), q(4, 2, 8)), (q(3, 2, 16), q(3, 2, 16)), (q(3, 2, 8), q(3, 2, 4)),
+                 (q(3, 2, 8), q(3, 2, 8, dt=torch.float16)), (q(3, 2, 8, dt=torch.int16), q(3, 2, 8, dt=torch.int16)),
+                 (q(3, 2, 8, dev="meta"), q(3, 2, 8, dev="meta")), (q(3, 2, 8), q(3, 2, 8)[..., :0])):
+        with pytest.raises(ValueError):
+            cache.attend(0, a, b, 1.0, None)
+    assert calls == []
+    cache.extend(new, None), cache.free(_ints(0), None), cache.fork(_ints(0), _ints(2), None), cache.append(0, _slab(1, 2), None)
+    cache.attend(0, q(3, 2, 8), q(3, 2, 8), 1.0, None)
+    assert calls == ["extend_requests", "free_requests", "fork_requests", "unpack_layer", "attend_layer"]
+
+
+def test_make_attention_checks_types_and_sizes():
+    q = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    T = tk.TOPKV_TYPE_BF16
+    for out, kw in ((q.half(), {}), (q[..., :32], {}), (q[..., :32], dict(value_dim=48)),
+                    (q.to("meta"), {}), (q, dict(lse=torch.zeros(3, 8, device="meta")))):
+        with pytest.raises(ValueError):
+            tk.make_attention(q, out, T, T, 1.0, **kw)
+    tk.make_attention(q, q[..., :32], T, T, 1.0, value_dim=32)
+    tk.make_attention(q, torch.zeros_like(q), T, T, 1.0, value_dim=32)          # the rest of a wider row is left alone
