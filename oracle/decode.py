@@ -68,7 +68,8 @@ def rows_of(g: Geom, layer: int, pool: np.ndarray, bt_row: np.ndarray, tokens: n
 
 
 def attend(g: Geom, layer: int, pool: np.ndarray, bt, sl, q: np.ndarray, kind: str, io: str, scale: float,
-           value_dim: int = 0, sinks: int = 0, k_scale: float = 1.0, v_scale: float = 1.0):
+           value_dim: int = 0, sinks: int = 0, k_scale: float = 1.0, v_scale: float = 1.0,
+           weight_step: float | None = None):
     """q float64 [R][Hq][d_h] (values of type io). Returns out and lse in 64 bits, and a bound on how
     far a computation may be off that keeps scores and sums in 32 bits, rounds each weight once to
     16 bits (fp16 where the cache is not bf16) and the result once to ``io``:
@@ -77,7 +78,8 @@ def attend(g: Geom, layer: int, pool: np.ndarray, bt, sl, q: np.ndarray, kind: s
     matrix units may cut instead of round), the scaled score by as much plus two roundings, so the
     weights by the factor e = that, in their sum as in the product with V; the sums over t tokens are
     off by t 2^-23 sum |terms|; a weight's rounding is u |w|, the result's half a step of io.
-    exp and the power of two it is computed by add 2^-20 to a weight's factor."""
+    exp and the power of two it is computed by add 2^-20 to a weight's factor. ``weight_step``: the
+    relative rounding of a weight, if it is not that of one 16-bit value."""
     R, Hq, _ = q.shape
     H = g.h_kv
     G = Hq // H
@@ -85,7 +87,7 @@ def attend(g: Geom, layer: int, pool: np.ndarray, bt, sl, q: np.ndarray, kind: s
     out = np.zeros((R, Hq, dv))
     lse = np.full((R, Hq), -np.inf)
     tol_out, tol_lse = np.zeros_like(out), np.zeros_like(lse)
-    u = HALF_STEP["bf16" if kind == "bf16" else "fp16"]
+    u = HALF_STEP["bf16" if kind == "bf16" else "fp16"] if weight_step is None else weight_step
     ep = 2.0 ** -23
     for r in range(R):
         tok = visible(int(sl[r]), g.window, sinks)

@@ -1103,3 +1103,31 @@ def test_decode_cache_attends_in_a_graph_beside_larger_calls(dev):
     torch.cuda.synchronize()
     _check((out.double().cpu().numpy(), lse.double().cpu().numpy()), od.attend(g, 0, pool_h, bt, sl, q_h, "bf16", "bf16", 0.125))
     assert all((x == 3).all() for x in others)
+
+
+@pytest.mark.parametrize("D,long", [(64, 0), (128, 0), (128, 3000)])
+def test_attend_bf16_weights_keep_sixteen_bits(dev, D, long):
+    """Two values that nearly cancel: half a step of an 8-bit weight would be far more than the result's
+    rounding. A weight is split into two bf16 values, the second of what the first leaves: 2^-8 of 2^-8."""
+    heads = 16
+    n = 2 + long                                             # further tokens weigh nothing
+    bt, pages = _table([n], 16, 1, 0, np.random.default_rng(0))
+    g = _geom(2, 1, D, 2, 16, pages)
+    pool = np.zeros(g.pool_bytes(), np.uint8)
+    q = np.zeros((1, heads, D))
+    q[0, :, 0], q[0, :, 1] = -np.arange(1, heads + 1) / 8, 1.0
+    w = np.exp(q[0, :, 0])
+    k, v = np.zeros((n, D)), np.zeros((n, D))
+    k[1, 0], k[2:, 1] = 1.0, -200.0
+    v[0, :heads], v[1, :heads] = od.decode_elements(od.encode_elements(w, "bf16"), "bf16"), -1.0
+    for i in range(n):
+        for c, x in ((0, k), (1, v)):
+            a = od.row_offset(g, 0, int(bt[0, i // 16]), c, i % 16, 0)
+            pool[a:a + 2 * D] = od.encode_elements(x[i], "bf16")
+    got = _run(dev, g, _layout(g), torch.from_numpy(pool).to(dev), bt, [n], q, "bf16", "bf16", 1.0)
+    want = od.attend(g, 0, pool, bt, [n], q, "bf16", "bf16", 1.0, weight_step=2.0 ** -16)
+    coarse = od.attend(g, 0, pool, bt, [n], q, "bf16", "bf16", 1.0)
+    _check(got, want)
+    own = np.arange(heads)
+    if not long:  # the bound would not let 8 bits through (scores of -200 alone allow 2 * 136 * 2^-23 * 200 = 0.0065)
+        assert (want[2][0, own, own] < coarse[2][0, own, own] / 4).all()
