@@ -763,7 +763,7 @@ const char* topkv_transport_name(int mode);
 /* ---- diagnostics ------------------------------------------------------------------------ */
 
 const char* topkv_strerror(int status);
-int topkv_version(void);
+int topkv_version(void); /* 130 and up: with attention and the page operators */
 /* cudaError_t of the most recent failing CUDA call made by this library on this thread. */
 int topkv_last_cuda_error(void);
 /* Device-side checks. Kernels never trap; when a device table is unusable they skip the

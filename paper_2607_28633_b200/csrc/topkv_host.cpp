@@ -212,6 +212,6 @@ const char* topkv_strerror(int status) {
   }
 }
 
-int topkv_version(void) { return 120; }
+int topkv_version(void) { return 130; }
 
 }  // extern "C"

@@ -291,3 +291,8 @@ def test_entry_points_survive_random_descriptors(seed):
             seen.add(st)
     assert tk.topkv_kernel_launch_count() == before
     assert {INVALID, CAP, LAYOUT, CUDA} <= seen
+
+
+def test_version_tells_the_decode_side_apart():
+    """120 was the library without attention and page operators."""
+    assert tk.topkv_version() >= 130
