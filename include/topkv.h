@@ -302,8 +302,11 @@ int topkv_repage_layer(int layer, const void* src_pool, const topkv_layout* src_
  *     out[r][a][:] = v_scale * sum_i exp(x_i) V[i][h][:] / sum_i exp(x_i)
  *     lse[r][a] = ln sum_i exp(x_i)
  * Visible: all s_r tokens, or in a windowed layer (batch->window_tokens = W > 0) the last
- * min(s_r, W) and the first sink_tokens. A request with no visible token (s_r = 0) gives zeros and
- * lse = -infinity. Table columns that hold no visible token are ignored; what lies in masked places
+ * min(s_r, W) and the first sink_tokens. The first tokens have to be in the cache: the transfer of
+ * a windowed layer brings the last min(s_r, W) tokens only, so a layer that keeps first tokens is sent
+ * as one without a window. (A sink that is a learned logit b per head and no token needs no
+ * sink_tokens: out * 1 / (1 + exp(b - lse)).) A request with no visible token (s_r = 0, or no page
+ * of its visible tokens usable) gives zeros and lse = -infinity. Table columns that hold no visible token are ignored; what lies in masked places
  * (a page's tail, tokens outside the window) is never read.
  *   kv_factor 2: K and V planes, head_dim at most 256 and a multiple of 8 (16 for 8-bit elements).
  *   kv_factor 1 with one head: multi-head latent attention in its absorbed form (§5.3). A row is key
@@ -400,13 +403,15 @@ int topkv_fork_requests(void* pool, const topkv_layout* layout, const topkv_batc
                         int64_t workspace_bytes, topkv_stream_t stream);
 /* The rows d_rows[i] (DEVICE int32 [num_rows]) give back their pages (each count goes down by one),
  * their table entries become -1 and their lengths 0. Empty rows, and a row's second mention, are
- * left alone; a count never goes below 0 (error bit 2). */
+ * left alone; a count never goes below 0 (error bit 2). A negative length becomes 0, a length beyond
+ * the row frees what the row holds (error bit 2). */
 int topkv_free_requests(const topkv_layout* layout, const topkv_batch* batch,
                         const topkv_page_tables* tables, const int32_t* d_rows, int32_t num_rows,
                         topkv_stream_t stream);
 /* Moves the pages in use to ids 0 .. n-1, n = *d_num_used (DEVICE int32 [1]) of them, so that the
  * rest of the pool is one free range: the k-th page in use at or above n goes to the k-th free page
- * below n, with its contents in all layers, its count and every table entry that names it.
+ * below n, with its contents in all layers, its count and every table entry within a request's
+ * length that names it (entries behind that are ignored, here as elsewhere).
  * d_page_map (DEVICE int32 [num_pool_pages]) gets the new id of every page, -1 for free ones, for
  * ids that the caller keeps elsewhere. */
 int topkv_compact_pages(void* pool, const topkv_layout* layout, const topkv_batch* batch,

@@ -10,7 +10,7 @@
 // bits, so for the usual G <= 16 it is memory, far below the tensor rate; the matrix instructions
 // are warp-wide m16n8k16 ones with the G query heads as rows (padded to 16), which need no shared
 // staging of accumulators and keep the tensor pipe 14 % busy. Measured: 16 x 16,384 tokens, 8 KV heads of
-// 128 in bf16, 173 us = 6.2 TB/s (0.95 of the measured copy); 16 x 512 to 4,096, 36 us, of which the
+// 128 in bf16, 176 us = 6.1 TB/s (0.93 of the measured copy); 16 x 512 to 4,096, 34 us, of which the
 // 148 MB take 22.6, the start 2, the spread between the CTAs 4 and the join 4. Layout of the work:
 //  * a CTA has 4 warps and one KV head; each warp takes its own 16 tokens of every 64 and runs its
 //    own ring of cp.async stages, running maximum and sum, so the loop has no CTA barrier at all;

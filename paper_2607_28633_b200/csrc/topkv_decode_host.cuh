@@ -403,7 +403,7 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   p.uncut = plan.uncut;
   p.narrow = plan.narrow;
   // Beginning with a request and writing its result takes a latent CTA, alone on its SM, about as long as
-  // three tiles (32 requests of 1,024 to 8,192 tokens, 128 heads: 79.5 us without, 76.5 with); of
+  // three tiles (32 requests of 1,024 to 8,192 tokens, 128 heads: 77.6 us without, 75.2 with); of
   // grouped-head CTAs others on the SM use that time (1 tile more made no difference)
   p.start_cost = layout->kv_factor == 1 ? 3 : 0;
   p.late_wait = (batch->flags & TOPKV_FLAG_TABLES_SETTLED) ? 1 : 0;

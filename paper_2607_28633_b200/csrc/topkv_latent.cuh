@@ -30,8 +30,9 @@
 // Every wait on a barrier is bounded; one that runs out raises error bit 1 and lets the CTA finish. The
 // allocation of TMEM waits for CTAs that hold it, which all end by themselves: the next launch is let in
 // only once every CTA of this one has its share.
-// Measured, 576 / 512 columns in bf16: 32 requests of 1,024 to 8,192 tokens, 128 heads: 77 us, 0.48 Pflop/s
-// (0.68 at 16,384 tokens each), a tile of 64 tokens and 64 heads in 2,930 cycles, of which the tensor core
+// Measured, 576 / 512 columns in bf16: 32 requests of 1,024 to 8,192 tokens, 128 heads: 75 us in bursts
+// of 200 calls at 1.9 GHz, 80 in a run of seconds, where the power cap holds the clock at 1.78, 0.5 Pflop/s
+// (0.64 at 16,384 tokens each), a tile of 64 tokens and 64 heads in 2,930 cycles, of which the tensor core
 // needs 2,070; 16 heads, 32 x 16,384 tokens: 107 us = 5.6 TB/s. What remains is the time from giving up a
 // stage to having it loaded again (2,000 cycles) in a ring of two: a third does not fit beside Q.
 #pragma once
