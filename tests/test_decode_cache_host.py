@@ -377,3 +377,15 @@ def test_make_attention_checks_types_and_sizes():
             tk.make_attention(q, out, T, T, 1.0, **kw)
     tk.make_attention(q, q[..., :32], T, T, 1.0, value_dim=32)
     tk.make_attention(q, torch.zeros_like(q), T, T, 1.0, value_dim=32)          # the rest of a wider row is left alone
+
+
+def test_more_forks_than_the_workspace_holds_are_refused(make):
+    g = Geom(num_pages=6, **GEOM)
+    cache, lib = make(g, [[0, -1], [-1, -1], [-1, -1], [-1, -1]], [4, 0, 0, 0], max_forks=2)
+    for parents, children in ((_ints(0, 0, 0), _ints(1, 2, 3)), (_ints(0, 0), _ints(1))):
+        with pytest.raises(ValueError):
+            cache.fork(parents, children, None)
+    assert cache.seq_lens.tolist() == [4, 0, 0, 0]
+    cache.fork(_ints(), _ints(), None)
+    cache.fork(_ints(0, 0), _ints(1, 3), None)
+    assert cache.seq_lens.tolist() == [4, 4, 0, 4]

@@ -1131,3 +1131,29 @@ def test_attend_bf16_weights_keep_sixteen_bits(dev, D, long):
     own = np.arange(heads)
     if not long:  # the bound would not let 8 bits through (scores of -200 alone allow 2 * 136 * 2^-23 * 200 = 0.0065)
         assert (want[2][0, own, own] < coarse[2][0, own, own] / 4).all()
+
+
+@pytest.mark.parametrize("kind,window,sinks,rows", [("e4m3", 0, 0, 4), ("e4m3", 33, 5, 4), ("fp16", 64, 4, 6), ("bf16", 1, 0, 4)])
+def test_decode_cache_attends_with_windows_and_eight_bits(dev, kind, window, sinks, rows):
+    """One object for layers of both kinds: all tokens, and a window with first tokens; rows to spare."""
+    from paper_2607_28633_b200 import session
+    rng = np.random.default_rng(window + rows)
+    sl = [700, 40, 0, 1300]
+    io = "bf16" if kind == "e4m3" else kind
+    bt, pages = _table(sl, 16, 1, 0, rng)
+    g = _geom(2, 2, 64, 1 if kind == "e4m3" else 2, 16, pages)
+    pool_h = _cache(g, bt, sl, kind, 0, rng)
+    s = torch.cuda.Stream(dev)
+    cache = session.DecodeCache(torch.from_numpy(pool_h).to(dev), _layout(g), torch.from_numpy(bt).to(dev),
+                                torch.tensor(sl, dtype=torch.int32, device=dev), rows=rows)
+    sl, bt = sl + [0] * (rows - 4), np.concatenate([bt, np.full((rows - 4, bt.shape[1]), -1, np.int32)])
+    q_h = od.decode_elements(od.encode_elements(rng.normal(size=rows * 6 * 64), io), io).reshape(rows, 6, 64)
+    q = torch.from_numpy(q_h).to(dev).to(TORCH[io])
+    ks, vs = (0.5, 2.0) if kind == "e4m3" else (1.0, 1.0)
+    for w, n in ((0, 0), (window, sinks)):
+        out, lse = torch.full_like(q, 7), torch.zeros(rows, 6, device=dev)
+        torch.cuda.synchronize()
+        cache.attend(0, q, out, 0.125, s, cache_type=TYPE[kind], window_tokens=w, sink_tokens=n, k_scale=ks, v_scale=vs, lse=lse)
+        torch.cuda.synchronize()
+        g.window = w
+        _check((out.double().cpu().numpy(), lse.double().cpu().numpy()), od.attend(g, 0, pool_h, bt, sl, q_h, kind, io, 0.125, 0, n, ks, vs))
