@@ -167,8 +167,8 @@ class _NewTokens:
 class DecodeCache:
     """The paged cache of a decode worker, from the tables of a receiver (or any pool and tables):
     ``rows`` request slots of ``max_pages`` pages each, of which the first ones hold the requests
-    that have arrived. All tables live on the device and are changed in place by the calls below,
-    which only enqueue work on ``stream``; calls are ordered by the stream they are given, and one
+    that have arrived. All tables live on the device and are changed in place, by the calls below
+    alone, which only enqueue work on ``stream``; calls are ordered by the stream they are given, and one
     object's calls must not run at the same time (they share a workspace). ``max_forks`` bounds
     the forks of one call. In a CUDA graph an extension stands together with its appends, or both are
     made outside."""
