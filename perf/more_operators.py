@@ -236,7 +236,7 @@ def _prepare_shared(c, seed):
             k = min(n, int(pages[r]))
             bt[r, :k] = common[:k]
             bt[r, k:pages[r]], at = ids[at:at + pages[r] - k], at + int(pages[r]) - k
-    s = dict(case=c, block_table=_int(bt), seq_lens=_int(sl), pages=N, plan=torch.zeros((5, len(sl)), dtype=torch.int32, device="cuda"))
+    s = dict(case=c, block_table=_int(bt), seq_lens=_int(sl), pages=N, plan=torch.zeros((6, len(sl)), dtype=torch.int32, device="cuda"))
     if c["kind"] == "plan":
         return s
     g = torch.Generator(device="cuda")
@@ -345,12 +345,13 @@ def _plain_plan(s):
     leader = torch.where(alike, row[None, :], R).amin(1)
     same = (bt == bt[leader]) & (col[None, :] < torch.minimum(full, full[leader])[:, None])
     common = torch.cumprod(same.long(), 1).sum(1) * P
+    members = alike.sum(1)
     shared = torch.where(alike, common[None, :], 1 << 40).amin(1)
-    shared = torch.where(alike.sum(1) > 1, shared, 0)
+    shared = torch.where(members > 1, shared, 0)
     order = torch.argsort(leader * R + row)
     place = torch.empty_like(order)
     place[order] = row
-    return [torch.stack([leader, common, shared, order, place]).to(torch.int32)]
+    return [torch.stack([leader, common, shared, members, order, place]).to(torch.int32)]
 
 
 def _softmax(score, k_seen, v):
@@ -542,7 +543,7 @@ def work(case):
         rest = sum(int(np.maximum(sl[m] - n * P, 0).sum()) for m, n in zip(rows, prefix))
         entries = 4 * (int((-(-sl // P)).sum()) + len(sl))
         if kind == "plan":
-            return {"bytes": entries + 20 * len(sl), "flops": 0}
+            return {"bytes": entries + 24 * len(sl), "flops": 0}
         return {"bytes": (once + rest) * 2 * H * D * e + len(sl) * Hq * (4 * D + 4) + entries, "flops": 4 * int(sl.sum()) * Hq * D}
     sl, _ = _sparse_lengths(c, 0)
     pages = -(-sl // P)
