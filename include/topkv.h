@@ -425,6 +425,173 @@ int topkv_copy_pages(int first_layer, int num_layers, void* pool, const topkv_la
                      const int32_t* d_src_pages, const int32_t* d_dst_pages, int32_t num_pages,
                      topkv_stream_t stream);
 
+/* ---- new tokens: rotated by their positions and written into the paged cache --------------------
+ * The K/V of a layer's new tokens as its projections leave them, one kernel from there into the pages:
+ * rotary position encoding of K on the way (and of the same tokens' Q, which has no page), conversion
+ * to the cache's type, the place by the block table. With x, y a pair of elements of a head and a the
+ * pair's angle at the token's position,
+ *     x' = scale * (x cos a - y sin a)      y' = scale * (x sin a + y cos a)
+ * in 32 bits, rounded once. A stored element is value / k_scale (V: / v_scale), 8-bit ones kept within
+ * +-448 (NaN stays NaN).
+ * Which tokens: request r brings n_r rows of k, v and q, rows cu_tokens[r] .. cu_tokens[r + 1] - 1 (NULL:
+ * one each, row r): the last n_r of its batch->seq_lens[r] tokens, the new ones included, for which
+ * topkv_extend_requests has made room. A request of length 0 is left out, its rows are skipped; of one
+ * that brings more rows than its length, or whose page ids lie outside the pool, the tokens without a
+ * place are skipped (error bit 2), as are rows at or past num_rows. What is skipped leaves pool and q_out
+ * as they were. The pages written to must be the request's own, as topkv_fork_requests leaves a last page. */
+enum { TOPKV_ROTARY_HALVES = 1, /* element i of the part pairs with element i + count / 2  */
+       TOPKV_ROTARY_PAIRS = 2 };/* element 2 i with element 2 i + 1                        */
+typedef struct topkv_rotary {
+  uint32_t struct_size;   /* = sizeof(topkv_rotary)                                                */
+  uint32_t style;         /* TOPKV_ROTARY_*                                                        */
+  uint32_t first, count;  /* elements first .. first + count - 1 of a head turn, count even; the   */
+                          /* others pass as they are (the rows of MLA: the last 64 of 576)          */
+  float scale;            /* what cos and sin are multiplied by; finite, usually 1                 */
+  uint32_t reserved;      /* must be 0                                                             */
+  const uint64_t* turns;  /* DEVICE [count / 2]: what a pair turns by from one position to the     */
+                          /* next, in units of 2^-64 turns, from topkv_rotary_turns. The product   */
+                          /* with a position, modulo 2^64, is the angle without its full turns: it  */
+                          /* is as exact at position 2^31 as at 1                                   */
+} topkv_rotary;
+typedef struct topkv_new_tokens {
+  uint32_t struct_size;       /* = sizeof(topkv_new_tokens)                                          */
+  uint32_t cache_type;        /* TOPKV_TYPE_*: the pool's elements (elem_bytes 2, 2, 1). 16-bit ones  */
+                              /* are of io_type                                                       */
+  uint32_t io_type;           /* of k, v, q and q_out: BF16 or FP16                                  */
+  uint32_t num_q_heads;       /* 0: there is no q                                                     */
+  int64_t num_rows;           /* rows of k, v and q; without cu_tokens at least num_requests          */
+  float k_scale, v_scale;     /* 8-bit cache: an element stands for itself times this; finite and not */
+                              /* 0. 1 for 16 bits                                                     */
+  const int64_t* cu_tokens;   /* DEVICE int64 [R + 1], not falling, from topkv_build_plan over the    */
+                              /* new tokens' counts; NULL: one row per request                        */
+  const int32_t* positions;   /* DEVICE int32 [num_rows]: positions of the rotation, or NULL:        */
+                              /* a token's number in its request                                      */
+  const topkv_rotary* rotary; /* HOST, or NULL: nothing turns                                         */
+  int64_t k_row_stride, k_head_stride;  /* bytes, multiples of 16; the elements of a head are         */
+  int64_t v_row_stride, v_head_stride;  /* contiguous, so k, v and q may be parts of one buffer. v is */
+  int64_t q_row_stride, q_head_stride;  /* ignored for kv_factor 1, a row of k is the latent row then */
+  int64_t q_out_row_stride, q_out_head_stride;
+} topkv_new_tokens;
+/* d_k, d_v [num_rows][num_kv_heads][head_dim], d_q, d_q_out [num_rows][num_q_heads][head_dim], bases
+ * multiples of 16 bytes, head_dim a multiple of 8. d_q_out may be d_q with the same strides (in place)
+ * and must otherwise overlap nothing. Rows of q_out must not overlap. batch->window_tokens must be 0;
+ * cu_seq_lens and total_tokens are ignored. One kernel on `stream`; no allocation, no synchronisation,
+ * capturable. TOPKV_FLAG_TABLES_SETTLED and TOPKV_FLAG_OVERLAP_PREVIOUS are ignored (the call always waits
+ * for the kernels before it). */
+int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                       const topkv_new_tokens* tokens, const void* d_k, const void* d_v, const void* d_q,
+                       void* d_q_out, topkv_stream_t stream);
+/* Frequencies of rotary position encoding, in radians a position, HOST double [count / 2], count even:
+ * f_j = base^(-2 j / count), changed for contexts longer than those trained on:
+ *   NONE    as they are
+ *   LINEAR  f_j / factor: positions are interpolated
+ *   BASE    base * factor^(count / (count - 2)) in place of base: the slowest pair is divided by factor, the
+ *           fastest stays (count > 2)
+ *   RAMP    by how often a pair turns within original_tokens, n_j = original_tokens * f_j / (2 pi):
+ *           f_j / factor up to `slow` turns, f_j from `fast` turns, between them in the proportion of
+ *           (n_j - slow) / (fast - slow)
+ * factor >= 1, base > 0, 0 <= slow < fast. Returns TOPKV_OK or TOPKV_ERR_INVALID_ARG. */
+enum { TOPKV_STRETCH_NONE = 0, TOPKV_STRETCH_LINEAR = 1, TOPKV_STRETCH_BASE = 2, TOPKV_STRETCH_RAMP = 3 };
+typedef struct topkv_rotary_stretch {
+  uint32_t struct_size;   /* = sizeof(topkv_rotary_stretch)  */
+  uint32_t kind;          /* TOPKV_STRETCH_*                 */
+  double base, factor;
+  double original_tokens, slow, fast; /* RAMP only */
+} topkv_rotary_stretch;
+int topkv_rotary_frequencies(const topkv_rotary_stretch* stretch, uint32_t count, double* h_frequencies);
+/* The turns table (HOST uint64 [n], to be copied to the device) of n frequencies in radians a position,
+ * each finite. */
+int topkv_rotary_turns(const double* h_frequencies, uint32_t n, uint64_t* h_turns);
+
+/* ---- attention behind shared prefixes -------------------------------------------------------------
+ * Requests that were forked from one another, or given the same prompt's pages, begin with the same
+ * block-table entries. topkv_attend_layer reads those pages once per request; the calls below read them
+ * once per group of requests and give the same result (to rounding).
+ * A plan says who shares what; it depends on the block table alone, so it serves all layers and stays
+ * good while requests grow, until a row is freed, forked into or otherwise given other pages (a
+ * compaction changes nothing). d_plan is DEVICE int32 [TOPKV_PLAN_ROWS][R], for request r:
+ *   LEADER   the lowest request that has a full first page with the same id (r itself, if r has no
+ *            full page)
+ *   COMMON   tokens of the leading pages that r and its leader have in common, full in both
+ *   SHARED   the smallest COMMON of the group (all requests with the same leader); 0 in a group of one,
+ *            or where it is below min_tokens: the group shares nothing then
+ *   MEMBERS  requests of the group
+ *   ORDER    the k-th request in the order of (leader, request), at place k
+ *   PLACE    where r stands in that order
+ * One group per first page: where some of its requests share more than all of them do, those tokens are
+ * read by each. A caller that knows better may write a plan of its own: LEADER, SHARED, MEMBERS, ORDER and
+ * PLACE are what attention reads. One that contradicts itself gives results without meaning, but no access
+ * outside the pool and the tensors; a request shorter than SHARED is attended to on its own.
+ * Two kernels on `stream`, no allocation, no synchronisation, capturable; batch->window_tokens must be 0. */
+#define TOPKV_PLAN_ROWS 6
+enum { TOPKV_PLAN_LEADER = 0, TOPKV_PLAN_COMMON = 1, TOPKV_PLAN_SHARED = 2, TOPKV_PLAN_MEMBERS = 3,
+       TOPKV_PLAN_ORDER = 4, TOPKV_PLAN_PLACE = 5 };
+int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, int32_t min_tokens,
+                        int32_t* d_plan, topkv_stream_t stream);
+/* As topkv_attend_layer, with the shared tokens' part formed once per group: the queries of all its
+ * members and heads are the rows of one product. kv_factor 2 only (128 query heads already share a latent
+ * row, which leaves nothing to gain), no window (window_tokens and sink_tokens 0). The weights of shared
+ * tokens are rounded once to 16 bits for the second product (bf16 for a bf16 cache, else fp16), and
+ * bf16 queries over an 8-bit cache become fp16 with a power of two for each row. Three kernels at most;
+ * the workspace holds nothing between calls. TOPKV_FLAG_TABLES_SETTLED covers d_plan too. */
+int64_t topkv_attend_shared_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                            const topkv_attention* attention);
+int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* layout,
+                              const topkv_batch* batch, const topkv_attention* attention,
+                              const int32_t* d_plan, const void* d_q, void* d_out, void* d_workspace,
+                              int64_t workspace_bytes, topkv_stream_t stream);
+
+/* ---- attention over chosen pages -------------------------------------------------------------------
+ * Sparse attention for long contexts: each KV head of a request sees only its first and last pages and
+ * those whose keys can score highest, by a bound kept in 8 bits. Per page p and KV head h, over the keys K
+ * of the tokens it holds, in 32-bit arithmetic, every operation rounded to nearest:
+ *     step = max |K| * c                            c = 1 / 127 rounded to 32 bits
+ *     bounds[p][h][0][d] = floor(min K[d] / step)   bounds[p][h][1][d] = ceil(max K[d] / step)
+ * kept within +-127 (0 where step is 0 or not finite; NaN in a key makes step NaN). For a query head a:
+ *     t = max |q| * c      q8[d] = q[d] / t rounded to the nearest integer, ties to even (0 and t = 0 where
+ *                          t is 0 or not finite)
+ *     dot = sum_d q8[d] * (q8[d] < 0 ? bounds[.][0][d] : bounds[.][1][d])      an exact integer
+ *     score(p, h) = max over the heads a of h of dot * (t * step); a page without a finite step scores highest
+ * Each KV head takes `budget` pages (all, if there are no more): the last `last_pages` before the first
+ * `first_pages` before the rest by falling score, equal scores by rising table column. So a choice is
+ * a function of the inputs alone, and the newest page is always part of it. k_scale must be positive. */
+typedef struct topkv_page_choice {
+  uint32_t struct_size;   /* = sizeof(topkv_page_choice)                                            */
+  uint32_t budget;        /* pages that a query sees, >= 1                                          */
+  uint32_t first_pages;   /* table columns that are always among them ...                           */
+  uint32_t last_pages;    /* ..., >= 1, from the front and the back                                  */
+  const int8_t* bounds;   /* DEVICE int8 [num_pool_pages][num_kv_heads][2][head_dim] of the layer   */
+  const float* steps;     /* DEVICE float [num_pool_pages][num_kv_heads] of the layer               */
+  int32_t* chosen;        /* DEVICE int32 [R][num_kv_heads][budget]: table columns, rising, -1      */
+                          /* behind the last                                                        */
+} topkv_page_choice;
+/* Bounds of every page that holds one of the last batch->window_tokens tokens of a request (0: of
+ * all its pages): after new tokens, of those tokens; after a transfer, a fork or a compaction, of all.
+ * A page outside the pool is skipped (error bit 2); other pages' bounds stay. One kernel, capturable.
+ * kv_factor 2 with head_dim at most 256. d_bounds is a multiple of 16 bytes. Requests that share a page
+ * must agree on how many tokens it holds (as full pages do). */
+int topkv_bound_pages_layer(int layer, const void* pool, const topkv_layout* layout,
+                            const topkv_batch* batch, uint32_t cache_type, int8_t* d_bounds, float* d_steps,
+                            topkv_stream_t stream);
+/* Bytes of d_workspace that either of the calls below needs, whatever the lengths. */
+int64_t topkv_page_choice_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                          const topkv_attention* attention,
+                                          const topkv_page_choice* choice);
+/* Writes choice->chosen for every request and KV head. Queries as for topkv_attend_layer; of `attention` only
+ * io_type, num_q_heads and the strides of q are used beyond its checks. batch->window_tokens must be 0. */
+int topkv_choose_pages_layer(const topkv_layout* layout, const topkv_batch* batch,
+                             const topkv_attention* attention, const topkv_page_choice* choice,
+                             const void* d_q, void* d_workspace, int64_t workspace_bytes,
+                             topkv_stream_t stream);
+/* As topkv_attend_layer over the tokens of the chosen pages alone, choice->chosen being what
+ * topkv_choose_pages_layer wrote for these lengths, or a caller's own: the first min(pages, budget) entries
+ * of a list count and each stands for page_tokens tokens, the last of them for what the request's last
+ * page holds. An entry that is no page of the request is skipped (error bit 2). bounds and steps are not read. */
+int topkv_attend_pages_layer(int layer, const void* pool, const topkv_layout* layout,
+                             const topkv_batch* batch, const topkv_attention* attention,
+                             const topkv_page_choice* choice, const void* d_q, void* d_out,
+                             void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream);
+
 /* ---- integrity: wire header and CRC-64 (§3.4) ------------------------------------------------ */
 
 /* The fixed 128-byte header of §3.4, one per request: magic, request ID, model ID, tensor
@@ -768,7 +935,7 @@ const char* topkv_transport_name(int mode);
 /* ---- diagnostics ------------------------------------------------------------------------ */
 
 const char* topkv_strerror(int status);
-int topkv_version(void); /* 130 and up: with attention and the page operators */
+int topkv_version(void); /* 130 and up: with attention and the page operators; 140: rotation, shared prefixes, chosen pages */
 /* cudaError_t of the most recent failing CUDA call made by this library on this thread. */
 int topkv_last_cuda_error(void);
 /* Device-side checks. Kernels never trap; when a device table is unusable they skip the

@@ -1,0 +1,97 @@
+"""Calls around the decode side's attention written out from their definitions, in 64 bits or as plain
+loops over host lists: rotated new tokens, shared prefixes, chosen pages. Test infrastructure like the rest
+of this package; shares nothing with the library."""
+from __future__ import annotations
+
+import numpy as np
+
+from . import Geom
+from .decode import ERR_TABLE, HALF_STEP, decode_elements, row_offset, rows_of
+
+
+# ---- rotated new tokens -----------------------------------------------------------------------------
+
+def frequencies(count: int, base: float, kind: str = "none", factor: float = 1.0, original: float = 0.0,
+                slow: float = 0.0, fast: float = 0.0) -> np.ndarray:
+    out = []
+    for j in range(count // 2):
+        if kind == "base":
+            f = (base * factor ** (count / (count - 2))) ** (-2 * j / count)
+        else:
+            f = base ** (-2 * j / count)
+        if kind == "linear":
+            f = f / factor
+        if kind == "ramp":
+            turns = original * f / (2 * np.pi)
+            g = min(max((turns - slow) / (fast - slow), 0.0), 1.0)
+            f = (1 - g) * f / factor + g * f
+        out.append(f)
+    return np.array(out)
+
+
+def rotate(x: np.ndarray, position: int, freq: np.ndarray, first: int, pairs: bool, scale: float):
+    """x [..., D] in 64 bits; returns the rotated vectors and, per element, |x| + |y| of its pair (0 outside
+    the rotated part), which the error of the cosines is multiplied by."""
+    y, size = np.array(x, np.float64), np.zeros_like(x)
+    n = 2 * len(freq)
+    for j, f in enumerate(freq):
+        a, b = (first + 2 * j, first + 2 * j + 1) if pairs else (first + j, first + j + n // 2)
+        c, s = np.cos(position * f) * scale, np.sin(position * f) * scale
+        y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., a] * s + x[..., b] * c
+        size[..., a] = size[..., b] = (np.abs(x[..., a]) + np.abs(x[..., b])) * abs(scale)
+    return y, size
+
+
+def stored_step(kind: str) -> tuple[float, float]:
+    """Half a step of one rounding to `kind`, relative, and absolute below the normal numbers."""
+    return HALF_STEP[kind], {"bf16": 2.0 ** -133, "fp16": 2.0 ** -25, "e4m3": 2.0 ** -10}[kind]
+
+
+def places(P: int, num_pages: int, bt, sl, cu, num_rows: int):
+    """For every row: (request, token, page, slot) or None, and the error bits."""
+    R, maxp = bt.shape
+    out, err = [None] * num_rows, 0
+    for r in range(R):
+        begin, end = (r, r + 1) if cu is None else (int(cu[r]), int(cu[r + 1]))
+        s = int(sl[r])
+        for t in range(begin, min(end, num_rows)):
+            i = s - (end - t)
+            if s == 0:
+                continue
+            if s < 0 or s > maxp * P or i < 0 or not 0 <= bt[r, i // P] < num_pages:
+                err |= ERR_TABLE
+                continue
+            out[t] = (r, i, int(bt[r, i // P]), i % P)
+    return out, err
+
+
+def append(g: Geom, layer: int, bt, sl, cu, k, v, q, positions, freq, first, pairs, scale, k_scale, v_scale, kind: str, io: str):
+    """Yields (pool offset or None, row of q, head, expected [D], tolerance [D]): what each written vector
+    holds. k, v, q [rows][heads][D] in 64 bits.
+
+    A cosine in 32 bits is off by the rounding of its angle, up to pi 2^-24, and 2 units of 2^-23; the two
+    products and their sum by 2^-24 each, the division of a stored element by two more roundings: 2^-21 of
+    |x| + |y| holds them all. The result is rounded once."""
+    rows = len(k)
+    where, err = places(g.P, g.num_pages, bt, sl, cu, rows)
+    found = []
+    for t, at in enumerate(where):
+        if at is None:
+            continue
+        r, i, page, slot = at
+        pos = i if positions is None else int(positions[t])
+        for what, x, s in (("q", q, 1.0), ("k", k, k_scale), ("v", v, v_scale)):
+            if x is None:
+                continue
+            y, size = rotate(x[t], pos, freq, first, pairs, scale) if what != "v" else (x[t], np.zeros_like(x[t]))
+            size = np.where(size == 0, np.abs(x[t]) if s != 1.0 else 0.0, size)
+            to = io if what == "q" else kind
+            rel, least = stored_step(to)
+            for h in range(x.shape[1]):
+                e = 2.0 ** -21 * size[h] / abs(s)
+                want = y[h] / s
+                if to == "e4m3":
+                    want = want.clip(-448, 448)
+                off = None if what == "q" else row_offset(g, layer, page, 0 if what == "k" else 1, slot, h)
+                found.append((off, t, h, want, e + rel * (np.abs(want) + e) + least))
+    return found, err

@@ -35,6 +35,9 @@ TOPKV_TYPE_BF16, TOPKV_TYPE_FP16, TOPKV_TYPE_E4M3 = 1, 2, 3
 
 # every symbol include/topkv.h declares
 EXPORTS = (
+    "topkv_append_layer", "topkv_rotary_frequencies", "topkv_rotary_turns", "topkv_plan_prefixes",
+    "topkv_attend_shared_workspace_bytes", "topkv_attend_shared_layer", "topkv_bound_pages_layer",
+    "topkv_page_choice_workspace_bytes", "topkv_choose_pages_layer", "topkv_attend_pages_layer",
     "topkv_pack_layer", "topkv_unpack_layer", "topkv_pack_layer_to_host",
     "topkv_unpack_layer_from_host", "topkv_build_plan", "topkv_validate_batch_host",
     "topkv_layout_default_strides", "topkv_wire_layer_bytes", "topkv_kv_bytes",
@@ -166,6 +169,101 @@ def make_attention(q, out, cache_type: int, io_type: int, scale: float, value_di
     a.lse = _ptr(lse)
     a._keepalive = lse
     return a
+
+
+TOPKV_ROTARY_HALVES, TOPKV_ROTARY_PAIRS = 1, 2
+TOPKV_STRETCH_NONE, TOPKV_STRETCH_LINEAR, TOPKV_STRETCH_BASE, TOPKV_STRETCH_RAMP = 0, 1, 2, 3
+TOPKV_PLAN_ROWS = 6
+(TOPKV_PLAN_LEADER, TOPKV_PLAN_COMMON, TOPKV_PLAN_SHARED, TOPKV_PLAN_MEMBERS, TOPKV_PLAN_ORDER,
+ TOPKV_PLAN_PLACE) = range(TOPKV_PLAN_ROWS)
+
+
+class topkv_rotary(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("style", c_uint32), ("first", c_uint32), ("count", c_uint32),
+                ("scale", c_float), ("reserved", c_uint32), ("turns", c_void_p)]
+
+
+class topkv_rotary_stretch(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("kind", c_uint32), ("base", c_double), ("factor", c_double),
+                ("original_tokens", c_double), ("slow", c_double), ("fast", c_double)]
+
+
+class topkv_new_tokens(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("cache_type", c_uint32), ("io_type", c_uint32), ("num_q_heads", c_uint32),
+                ("num_rows", c_int64), ("k_scale", c_float), ("v_scale", c_float), ("cu_tokens", c_void_p),
+                ("positions", c_void_p), ("rotary", ctypes.POINTER(topkv_rotary)),
+                ("k_row_stride", c_int64), ("k_head_stride", c_int64), ("v_row_stride", c_int64), ("v_head_stride", c_int64),
+                ("q_row_stride", c_int64), ("q_head_stride", c_int64), ("q_out_row_stride", c_int64), ("q_out_head_stride", c_int64)]
+
+
+class topkv_page_choice(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("budget", c_uint32), ("first_pages", c_uint32), ("last_pages", c_uint32),
+                ("bounds", c_void_p), ("steps", c_void_p), ("chosen", c_void_p)]
+
+
+def make_rotary(turns, style: int = TOPKV_ROTARY_HALVES, first: int = 0, scale: float = 1.0) -> topkv_rotary:
+    """turns: contiguous device tensor of 64-bit integers, one per pair, from topkv_rotary_turns."""
+    if turns.ndim != 1 or turns.element_size() != 8 or turns.is_floating_point() or not turns.is_contiguous():
+        raise ValueError("turns is a contiguous vector of 64-bit integers")
+    t = topkv_rotary()
+    t.struct_size = ctypes.sizeof(topkv_rotary)
+    t.style, t.first, t.count, t.scale, t.turns = style, first, 2 * turns.numel(), scale, _ptr(turns)
+    t._keepalive = turns
+    return t
+
+
+def make_new_tokens(k, v, cache_type: int, io_type: int, q=None, q_out=None, rotary: topkv_rotary | None = None,
+                    cu_tokens=None, positions=None, k_scale: float = 1.0, v_scale: float = 1.0) -> topkv_new_tokens:
+    """k, v [rows][kv heads][head_dim] and q, q_out [rows][q heads][head_dim]: device tensors of 16-bit
+    elements (v None for latent rows, q and q_out None for keys alone), whose strides the descriptor takes (the
+    last axis must be contiguous). cu_tokens: device int64 [R + 1] or None; positions: device int32 [rows] or None."""
+    tensors = [t for t in (k, v, q, q_out) if t is not None]
+    for t in tensors:
+        if t.ndim != 3 or t.element_size() != 2 or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError("k, v, q and q_out are [rows][heads][elements] of 16-bit elements, the last axis contiguous")
+        if t.dtype != k.dtype or t.device != k.device or t.shape[0] != k.shape[0] or t.shape[2] != k.shape[2]:
+            raise ValueError("k, v, q and q_out differ in type, device, rows or elements")
+    if (v is not None and v.shape != k.shape) or (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
+        raise ValueError("v is shaped as k, q_out as q")
+    for t, size in ((cu_tokens, 8), (positions, 4)):
+        if t is not None and (t.ndim != 1 or t.element_size() != size or t.is_floating_point() or not t.is_contiguous() or t.device != k.device):
+            raise ValueError("cu_tokens and positions are contiguous vectors of 64- and 32-bit integers on the tensors' device")
+    if positions is not None and positions.numel() < k.shape[0]:
+        raise ValueError("a position for every row")
+    stride = lambda t, i: 2 * t.stride(i) if t.shape[i] > 1 else 0
+    n = topkv_new_tokens()
+    n.struct_size = ctypes.sizeof(topkv_new_tokens)
+    n.cache_type, n.io_type, n.num_q_heads, n.num_rows = cache_type, io_type, q.shape[1] if q is not None else 0, k.shape[0]
+    n.k_scale, n.v_scale, n.cu_tokens, n.positions = k_scale, v_scale, _ptr(cu_tokens), _ptr(positions)
+    if rotary is not None:
+        n.rotary = ctypes.pointer(rotary)
+    n.k_row_stride, n.k_head_stride = stride(k, 0), stride(k, 1)
+    if v is not None:
+        n.v_row_stride, n.v_head_stride = stride(v, 0), stride(v, 1)
+    if q is not None:
+        n.q_row_stride, n.q_head_stride = stride(q, 0), stride(q, 1)
+        n.q_out_row_stride, n.q_out_head_stride = stride(q_out, 0), stride(q_out, 1)
+    n._keepalive = (rotary, cu_tokens, positions)
+    return n
+
+
+def make_page_choice(budget: int, first_pages: int, last_pages: int, bounds, steps, chosen) -> topkv_page_choice:
+    """bounds int8 [pages][kv heads][2][head_dim], steps float32 [pages][kv heads], chosen int32 [requests][kv
+    heads][budget]: contiguous device tensors."""
+    if bounds.ndim != 4 or bounds.element_size() != 1 or bounds.shape[2] != 2 or not bounds.is_contiguous():
+        raise ValueError("bounds is a contiguous int8 [pages][kv heads][2][head_dim]")
+    if tuple(steps.shape) != tuple(bounds.shape[:2]) or steps.element_size() != 4 or not steps.is_contiguous():
+        raise ValueError("steps is a contiguous float32 [pages][kv heads]")
+    if chosen.ndim != 3 or tuple(chosen.shape[1:]) != (bounds.shape[1], budget) or chosen.element_size() != 4 or not chosen.is_contiguous():
+        raise ValueError("chosen is a contiguous int32 [requests][kv heads][budget]")
+    if not (bounds.device == steps.device == chosen.device):
+        raise ValueError("the tensors differ in device")
+    c = topkv_page_choice()
+    c.struct_size = ctypes.sizeof(topkv_page_choice)
+    c.budget, c.first_pages, c.last_pages = budget, first_pages, last_pages
+    c.bounds, c.steps, c.chosen = _ptr(bounds), _ptr(steps), _ptr(chosen)
+    c._keepalive = (bounds, steps, chosen)
+    return c
 
 
 class topkv_page_tables(ctypes.Structure):
@@ -312,6 +410,10 @@ def lib() -> ctypes.CDLL:
         L.topkv_free_requests.argtypes = [lp, bp, pp, c_void_p, c_int32, c_void_p]
         L.topkv_compact_pages.argtypes = [c_void_p, lp, bp, pp, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
         L.topkv_copy_pages.argtypes = [c_int, c_int, c_void_p, lp, c_void_p, c_void_p, c_int32, c_void_p]
+        np_, cp = ctypes.POINTER(topkv_new_tokens), ctypes.POINTER(topkv_page_choice)
+        L.topkv_append_layer.argtypes = [c_int, c_void_p, lp, bp, np_, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.topkv_rotary_frequencies.argtypes = [ctypes.POINTER(topkv_rotary_stretch), c_uint32, c_void_p]
+        L.topkv_rotary_turns.argtypes = [c_void_p, c_uint32, c_void_p]
         ep = ctypes.POINTER(topkv_endpoint)
         L.topkv_select_transport.argtypes = [ep, ep, c_int, c_int]
         L.topkv_planning_rate.argtypes = [c_int]
@@ -637,6 +739,31 @@ def topkv_copy_pages(first_layer, num_layers, pool, layout, d_src_pages, d_dst_p
                      stream=None):
     return lib().topkv_copy_pages(first_layer, num_layers, _ptr(pool), ctypes.byref(layout),
                                   _ptr(d_src_pages), _ptr(d_dst_pages), num_pages, _stream(stream))
+
+
+def topkv_append_layer(layer, pool, layout, batch, tokens, d_k, d_v, d_q, d_q_out, stream=None):
+    return lib().topkv_append_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(tokens),
+                                    _ptr(d_k), _ptr(d_v), _ptr(d_q), _ptr(d_q_out), _stream(stream))
+
+
+def topkv_rotary_frequencies(count, base, kind=TOPKV_STRETCH_NONE, factor=1.0, original_tokens=0.0, slow=0.0, fast=0.0):
+    """numpy float64 [count / 2], radians a position."""
+    import numpy as np
+    s = topkv_rotary_stretch()
+    s.struct_size = ctypes.sizeof(topkv_rotary_stretch)
+    s.kind, s.base, s.factor, s.original_tokens, s.slow, s.fast = kind, base, factor, original_tokens, slow, fast
+    f = np.zeros(count // 2, dtype=np.float64)
+    check(lib().topkv_rotary_frequencies(ctypes.byref(s), count, f.ctypes.data))
+    return f
+
+
+def topkv_rotary_turns(frequencies):
+    """numpy uint64, one per frequency (radians a position)."""
+    import numpy as np
+    f = np.ascontiguousarray(frequencies, dtype=np.float64)
+    turns = np.zeros(f.size, dtype=np.uint64)
+    check(lib().topkv_rotary_turns(f.ctypes.data, f.size, turns.ctypes.data))
+    return turns
 
 
 def topkv_header_fill(header, request_id, model_id, layout, seq_len, crc_k, crc_v):

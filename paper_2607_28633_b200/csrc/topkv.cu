@@ -6,7 +6,9 @@
 // points declared and documented in include/topkv.h. The kernels live in the .cuh files next
 // to it (topkv_vec: vectorised page copy and plan; topkv_bulk: bulk-async ring; topkv_repage:
 // pool to pool; topkv_crc: checksummed copy; topkv_attend: attention over the paged cache;
-// topkv_pages: page operators; the host side of these two is topkv_decode_host.cuh);
+// topkv_pages: page operators; the host side of these two is topkv_decode_host.cuh; topkv_append:
+// new tokens rotated into the cache; topkv_prefix: attention behind shared prefixes; topkv_choose:
+// attention over chosen pages; theirs is topkv_more_host.cuh);
 // topkv_host.cpp holds the CUDA-free helpers.
 // Nothing here ever calls the CPU oracle.
 #include "topkv.h"
@@ -24,6 +26,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <utility>
 #include <vector>
@@ -1695,3 +1698,4 @@ int topkv_set_kernel_variant(int variant) {
 }  // extern "C"
 
 #include "topkv_decode_host.cuh"
+#include "topkv_more_host.cuh"

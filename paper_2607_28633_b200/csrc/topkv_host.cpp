@@ -3,6 +3,7 @@
 #include "topkv.h"
 
 #include <chrono>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <mutex>
@@ -212,6 +213,48 @@ const char* topkv_strerror(int status) {
   }
 }
 
-int topkv_version(void) { return 130; }
+int topkv_version(void) { return 140; }
+
+// f_j = base^(-2 j / count), stretched for contexts longer than those trained on: positions divided by a
+// factor, the base raised ("NTK-aware"), or by how often a pair turns within the trained context, with a ramp
+// between the pairs that stay and those that are divided (YaRN, Peng et al. 2023, §3.2).
+int topkv_rotary_frequencies(const topkv_rotary_stretch* s, uint32_t count, double* f) {
+  if (s == nullptr || s->struct_size != sizeof(topkv_rotary_stretch) || s->kind > TOPKV_STRETCH_RAMP) return TOPKV_ERR_INVALID_ARG;
+  if (count % 2 != 0 || (count > 0 && f == nullptr)) return TOPKV_ERR_INVALID_ARG;
+  if (!(s->base > 0) || !std::isfinite(s->base)) return TOPKV_ERR_INVALID_ARG;
+  if (s->kind != TOPKV_STRETCH_NONE && (!(s->factor >= 1) || !std::isfinite(s->factor))) return TOPKV_ERR_INVALID_ARG;
+  if (s->kind == TOPKV_STRETCH_BASE && count == 2) return TOPKV_ERR_INVALID_ARG;
+  if (s->kind == TOPKV_STRETCH_RAMP &&
+      (!(s->original_tokens > 0) || !std::isfinite(s->original_tokens) || !(s->slow >= 0) || !(s->fast > s->slow) || !std::isfinite(s->fast)))
+    return TOPKV_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  double base = s->base;
+  if (s->kind == TOPKV_STRETCH_BASE && count > 0) base *= std::pow(s->factor, (double)count / ((double)count - 2));
+  for (uint32_t j = 0; j < count / 2; ++j) {
+    double v = std::pow(base, -2.0 * j / count);
+    if (s->kind == TOPKV_STRETCH_LINEAR) v /= s->factor;
+    if (s->kind == TOPKV_STRETCH_RAMP) {
+      double stays = (s->original_tokens * v / two_pi - s->slow) / (s->fast - s->slow);
+      stays = stays < 0 ? 0 : stays > 1 ? 1 : stays;
+      v = stays * v + (1 - stays) * (v / s->factor);
+    }
+    f[j] = v;
+  }
+  return TOPKV_OK;
+}
+
+int topkv_rotary_turns(const double* f, uint32_t n, uint64_t* turns) {
+  if (n > 0 && (f == nullptr || turns == nullptr)) return TOPKV_ERR_INVALID_ARG;
+  for (uint32_t j = 0; j < n; ++j)
+    if (!std::isfinite(f[j])) return TOPKV_ERR_INVALID_ARG;
+  const long double two_pi = 6.28318530717958647692528676655900577L;
+  for (uint32_t j = 0; j < n; ++j) {
+    long double t = f[j] / two_pi;
+    t -= std::floor(t);  // 0 <= t <= 1; with 64 bits of mantissa the fraction keeps 2^-64 of a turn
+    const long double scaled = std::floor(t * 18446744073709551616.0L + 0.5L);
+    turns[j] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+  }
+  return TOPKV_OK;
+}
 
 }  // extern "C"

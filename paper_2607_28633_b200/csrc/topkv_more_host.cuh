@@ -1,0 +1,144 @@
+// Host side of the calls that stand around the decode side's attention: new tokens on their way into the
+// cache, shared prefixes, chosen pages. Included by topkv.cu behind topkv_decode_host.cuh, whose checks
+// and launches it shares.
+#pragma once
+#include "topkv_append.cuh"
+
+namespace {
+
+inline bool mult8p(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7) == 0; }
+constexpr int64_t kFarStride = 1ll << 40;  // no stride is longer: sums of a few stay within 64 bits
+
+// Whether [rows][heads] vectors of `bytes` at these strides do not overlap.
+bool apart(int64_t rows, int64_t heads, int64_t row, int64_t head, int64_t bytes) {
+  const __int128 R = rows, H = heads, sr = row, sh = head;
+  const bool heads_in = (H == 1 || sh >= bytes) && (R <= 1 || sr >= (H - 1) * sh + bytes);
+  const bool rows_in = (R <= 1 || sr >= bytes) && (H == 1 || sh >= (R - 1) * sr + bytes);
+  return heads_in || rows_in;
+}
+int check_strides(std::initializer_list<int64_t> strides) {
+  for (const int64_t s : strides)
+    if (s < 0 || s > kFarStride) return TOPKV_ERR_INVALID_ARG;
+  for (const int64_t s : strides)
+    if (!mult16(s)) return TOPKV_ERR_ALIGNMENT;
+  return TOPKV_OK;
+}
+
+// ---- new tokens ---------------------------------------------------------------------------------
+int check_new_tokens(const topkv_layout* lo, const topkv_batch* b, const topkv_new_tokens* n) {
+  Resolved rs;
+  int st = check_layout(lo, &rs);
+  if (st != TOPKV_OK) return st;
+  st = check_tables_batch(lo, b);
+  if (st != TOPKV_OK) return st;
+  if (b->window_tokens != 0) return TOPKV_ERR_INVALID_ARG;
+  if (n == nullptr || n->struct_size != sizeof(topkv_new_tokens)) return TOPKV_ERR_INVALID_ARG;
+  if (n->cache_type < TOPKV_TYPE_BF16 || n->cache_type > TOPKV_TYPE_E4M3) return TOPKV_ERR_INVALID_ARG;
+  if (n->io_type != TOPKV_TYPE_BF16 && n->io_type != TOPKV_TYPE_FP16) return TOPKV_ERR_INVALID_ARG;
+  const bool narrow = n->cache_type == TOPKV_TYPE_E4M3;
+  if (!narrow && (n->io_type != n->cache_type || n->k_scale != 1.f || n->v_scale != 1.f)) return TOPKV_ERR_INVALID_ARG;
+  for (const float s : {n->k_scale, n->v_scale})
+    if (!std::isfinite(s) || s == 0.f || !std::isfinite(1.f / s)) return TOPKV_ERR_INVALID_ARG;
+  if (lo->elem_bytes != (narrow ? 1u : 2u) || lo->head_dim % 8 != 0 || lo->head_dim > 2048) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (n->num_rows < 0 || n->num_rows > 0x7fffffffll || n->num_q_heads > 65535) return TOPKV_ERR_INVALID_ARG;
+  if (lo->num_kv_heads > 65535) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (n->cu_tokens == nullptr && n->num_rows < b->num_requests) return TOPKV_ERR_INVALID_ARG;
+  st = check_strides({n->k_row_stride, n->k_head_stride, n->q_row_stride, n->q_head_stride, n->q_out_row_stride, n->q_out_head_stride});
+  if (st == TOPKV_OK && lo->kv_factor == 2) st = check_strides({n->v_row_stride, n->v_head_stride});
+  if (st != TOPKV_OK) return st;
+  if (!mult8p(n->cu_tokens) || !mult4p(n->positions)) return TOPKV_ERR_ALIGNMENT;
+  if (n->num_q_heads > 0 && !apart(n->num_rows, n->num_q_heads, n->q_out_row_stride, n->q_out_head_stride, 2ll * lo->head_dim))
+    return TOPKV_ERR_INVALID_ARG;
+  if (const topkv_rotary* t = n->rotary) {
+    if (t->struct_size != sizeof(topkv_rotary) || t->reserved != 0) return TOPKV_ERR_INVALID_ARG;
+    if (t->style != TOPKV_ROTARY_HALVES && t->style != TOPKV_ROTARY_PAIRS) return TOPKV_ERR_INVALID_ARG;
+    if (t->count % 2 != 0 || t->count > lo->head_dim || t->first > lo->head_dim - t->count || !std::isfinite(t->scale))
+      return TOPKV_ERR_INVALID_ARG;
+    if (t->count > 0 && t->turns == nullptr) return TOPKV_ERR_INVALID_ARG;
+    if (!mult8p(t->turns)) return TOPKV_ERR_ALIGNMENT;
+  }
+  return TOPKV_OK;
+}
+
+template <bool BF16, bool E8>
+int launch_append(const AppendParams& p, bool chunks, dim3 grid, cudaStream_t s) {
+  return launched(chunks ? launch_pdl(topkv_append_kernel<BF16, E8, true>, grid, dim3(kAppendThreads), 0, s, p)
+                         : launch_pdl(topkv_append_kernel<BF16, E8, false>, grid, dim3(kAppendThreads), 0, s, p), 1);
+}
+
+}  // namespace
+
+extern "C" {
+
+int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                       const topkv_new_tokens* tokens, const void* d_k, const void* d_v, const void* d_q,
+                       void* d_q_out, topkv_stream_t stream) {
+  const int st = check_new_tokens(layout, batch, tokens);
+  if (st != TOPKV_OK) return st;
+  if (layer < 0 || (uint32_t)layer >= layout->num_layers) return TOPKV_ERR_LAYER_RANGE;
+  const bool values = layout->kv_factor == 2, queries = tokens->num_q_heads > 0;
+  if (tokens->num_rows == 0) return TOPKV_OK;  // tensors without rows may have no address
+  if (pool == nullptr || d_k == nullptr || (values && d_v == nullptr) || (queries && (d_q == nullptr || d_q_out == nullptr)))
+    return TOPKV_ERR_INVALID_ARG;
+  if (!mult16p(pool) || !mult16p(d_k) || (values && !mult16p(d_v)) || (queries && (!mult16p(d_q) || !mult16p(d_q_out))))
+    return TOPKV_ERR_ALIGNMENT;
+  if (queries && d_q == d_q_out && (tokens->q_row_stride != tokens->q_out_row_stride || tokens->q_head_stride != tokens->q_out_head_stride))
+    return TOPKV_ERR_INVALID_ARG;
+  if (batch->num_requests == 0 || batch->max_pages_per_req == 0) return TOPKV_OK;
+  AppendParams p = {};
+  p.pool = static_cast<uint8_t*>(pool) + (int64_t)layer * layout->pool_layer_stride;
+  p.bt = batch->block_table;
+  p.sl = batch->seq_lens;
+  p.cu = tokens->cu_tokens;
+  p.positions = tokens->positions;
+  const void* in[3] = {d_q, d_k, d_v};
+  const int64_t row[3] = {tokens->q_row_stride, tokens->k_row_stride, tokens->v_row_stride};
+  const int64_t head[3] = {tokens->q_head_stride, tokens->k_head_stride, tokens->v_head_stride};
+  for (int i = 0; i < 3; ++i) {
+    p.in[i] = static_cast<const uint8_t*>(in[i]);
+    p.in_row[i] = row[i];
+    p.in_head[i] = head[i];
+  }
+  p.q_out = static_cast<uint8_t*>(d_q_out);
+  p.out_row = tokens->q_out_row_stride;
+  p.out_head = tokens->q_out_head_stride;
+  p.S_page = layout->pool_page_stride;
+  p.S_kv = values ? layout->pool_kv_stride : 0;
+  p.S_tok = layout->page_tokens > 1 ? layout->pool_token_stride : 0;
+  p.S_head = layout->num_kv_heads > 1 ? layout->pool_head_stride : 0;
+  p.num_pages = layout->num_pool_pages;
+  // rows behind the last request's are spare: without offsets there is one row per request
+  p.num_rows = tokens->cu_tokens == nullptr ? batch->num_requests : tokens->num_rows;
+  p.R = batch->num_requests;
+  p.maxp = batch->max_pages_per_req;
+  p.P = (int)layout->page_tokens;
+  p.Hq = (int)tokens->num_q_heads;
+  p.H = (int)layout->num_kv_heads;
+  p.rows = p.Hq + p.H * (values ? 2 : 1);
+  p.D = (int)layout->head_dim;
+  p.inv_scale[0] = 1.f / tokens->k_scale;
+  p.inv_scale[1] = 1.f / tokens->v_scale;
+  if (const topkv_rotary* t = tokens->rotary) {
+    p.first = (int)t->first;
+    p.half = (int)t->count / 2;
+    p.pairs = t->style == TOPKV_ROTARY_PAIRS;
+    p.turns = t->turns;
+    p.scale = t->scale;
+  }
+  const bool chunks = p.first % 8 == 0 && (p.pairs ? 2 * p.half : p.half) % 8 == 0;
+  // Few tokens a CTA, so that there are several CTAs per SM; where there are not enough tokens for that
+  // the heads of a token are shared out too, two rows of heads a thread.
+  const int most = std::min(kAppendThreads, p.half > 0 ? kAppendPairs / p.half : kAppendThreads);
+  p.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({p.num_rows / (8 * 148), most, 8}));
+  const int64_t ctas = (p.num_rows + p.tokens - 1) / p.tokens;
+  const int items = chunks ? (p.pairs ? p.half / 4 : p.half / 8) + p.D / 8 - p.half / 4 : p.D - p.half;
+  const int64_t passes = ((int64_t)p.rows * items + 2 * kAppendThreads - 1) / (2 * kAppendThreads);
+  const unsigned y = (unsigned)std::max<int64_t>(1, std::min<int64_t>({(2 * 148 + ctas - 1) / ctas, passes, 65535}));
+  const dim3 grid((unsigned)ctas, y);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const bool bf16 = tokens->io_type == TOPKV_TYPE_BF16, narrow = tokens->cache_type == TOPKV_TYPE_E4M3;
+  if (bf16) return narrow ? launch_append<true, true>(p, chunks, grid, s) : launch_append<true, false>(p, chunks, grid, s);
+  return narrow ? launch_append<false, true>(p, chunks, grid, s) : launch_append<false, false>(p, chunks, grid, s);
+}
+
+}  // extern "C"
