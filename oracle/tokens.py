@@ -95,3 +95,27 @@ def append(g: Geom, layer: int, bt, sl, cu, k, v, q, positions, freq, first, pai
                 off = None if what == "q" else row_offset(g, layer, page, 0 if what == "k" else 1, slot, h)
                 found.append((off, t, h, want, e + rel * (np.abs(want) + e) + least))
     return found, err
+
+
+# ---- shared prefixes ----------------------------------------------------------------------------------
+
+def plan_prefixes(P: int, num_pages: int, bt, sl, min_tokens: int = 0) -> np.ndarray:
+    """int32 [6][R]: leader, common, shared, members, order, place."""
+    R, maxp = bt.shape
+    full = [min(max(int(s), 0) // P, maxp) for s in sl]
+    leader, common = [], []
+    for r in range(R):
+        lead = r
+        if full[r] and 0 <= bt[r, 0] < num_pages:
+            lead = next(x for x in range(r + 1) if full[x] and bt[x, 0] == bt[r, 0])
+        n = 0
+        while n < min(full[r], full[lead]) and bt[r, n] == bt[lead, n]:
+            n += 1
+        leader.append(lead)
+        common.append(n * P)
+    members = [leader.count(x) for x in leader]
+    shared = [min(c for c, x in zip(common, leader) if x == leader[r]) for r in range(R)]
+    shared = [s if m > 1 and s >= min_tokens else 0 for s, m in zip(shared, members)]
+    order = sorted(range(R), key=lambda r: (leader[r], r))
+    place = [order.index(r) for r in range(R)]
+    return np.array([leader, common, shared, members, order, place], np.int32).reshape(6, R)

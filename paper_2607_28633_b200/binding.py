@@ -414,6 +414,10 @@ def lib() -> ctypes.CDLL:
         L.topkv_append_layer.argtypes = [c_int, c_void_p, lp, bp, np_, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
         L.topkv_rotary_frequencies.argtypes = [ctypes.POINTER(topkv_rotary_stretch), c_uint32, c_void_p]
         L.topkv_rotary_turns.argtypes = [c_void_p, c_uint32, c_void_p]
+        L.topkv_plan_prefixes.argtypes = [lp, bp, c_int32, c_void_p, c_void_p]
+        L.topkv_attend_shared_workspace_bytes.argtypes = [lp, bp, ap]
+        L.topkv_attend_shared_workspace_bytes.restype = c_int64
+        L.topkv_attend_shared_layer.argtypes = [c_int, c_void_p, lp, bp, ap, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
         ep = ctypes.POINTER(topkv_endpoint)
         L.topkv_select_transport.argtypes = [ep, ep, c_int, c_int]
         L.topkv_planning_rate.argtypes = [c_int]
@@ -764,6 +768,21 @@ def topkv_rotary_turns(frequencies):
     turns = np.zeros(f.size, dtype=np.uint64)
     check(lib().topkv_rotary_turns(f.ctypes.data, f.size, turns.ctypes.data))
     return turns
+
+
+def topkv_plan_prefixes(layout, batch, min_tokens, d_plan, stream=None):
+    return lib().topkv_plan_prefixes(ctypes.byref(layout), ctypes.byref(batch), min_tokens, _ptr(d_plan), _stream(stream))
+
+
+def topkv_attend_shared_workspace_bytes(layout, batch, attention):
+    return lib().topkv_attend_shared_workspace_bytes(ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(attention))
+
+
+def topkv_attend_shared_layer(layer, pool, layout, batch, attention, d_plan, d_q, d_out, d_workspace, workspace_bytes,
+                              stream=None):
+    return lib().topkv_attend_shared_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
+                                           ctypes.byref(attention), _ptr(d_plan), _ptr(d_q), _ptr(d_out),
+                                           _ptr(d_workspace), workspace_bytes, _stream(stream))
 
 
 def topkv_header_fill(header, request_id, model_id, layout, seq_len, crc_k, crc_v):

@@ -52,6 +52,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum AttendType { kBf16 = 1, kFp16 = 2, kE4m3 = 3 };
 
+// Which tokens a request sees: all (or a window and first tokens); those behind the prefix that it shares with
+// others, whose part is formed elsewhere; those of the pages that were chosen for it.
+enum AttendMode { kAllTokens = 0, kBehindPrefix = 1, kChosenPages = 2 };
+
 struct AttendParams {
   const uint8_t* pool;  // this layer's slab
   const int32_t* bt;
@@ -84,12 +88,32 @@ struct AttendParams {
   int4* joins;          // which requests were cut, see JoinRecord: [R] if by_request, else [teams]
   float2* ml;           // [teams][2][H * gtiles][rows]
   float* part;          // [teams][2][H * gtiles][rows][Dv]
+  // kBehindPrefix: every request leaves parts, slot (r + team) of [R + teams] (uncut: r of [R]), and its
+  // join record is {r, first slot, parts, 0}
+  const int32_t* plan;  // [rows of a plan][R]
+  // kChosenPages
+  const int32_t* chosen;  // [R][H][budget] table columns
+  int budget;
 };
+
+// Tokens that request r, s long, shares with others under a plan; 0 if it is on its own. Everything that the
+// product over the prefix takes for granted is checked here, so that both agree on who takes part.
+__device__ __forceinline__ int shared_tokens(const AttendParams& p, int r, int s) {
+  const int n = p.plan[TOPKV_PLAN_SHARED * p.R + r], lead = p.plan[TOPKV_PLAN_LEADER * p.R + r];
+  if (n <= 0 || n > s || lead < 0 || lead >= p.R) return 0;
+  const int rank = p.plan[TOPKV_PLAN_PLACE * p.R + r] - p.plan[TOPKV_PLAN_PLACE * p.R + lead];
+  const int members = p.plan[TOPKV_PLAN_MEMBERS * p.R + lead];
+  if (p.plan[TOPKV_PLAN_LEADER * p.R + lead] != lead || p.plan[TOPKV_PLAN_SHARED * p.R + lead] != n || p.sl[lead] < n ||
+      members < 2 || rank < 0 || rank >= members)
+    return 0;
+  return n;
+}
 
 // Visible tokens of a request: 0 .. n-1 stand for tokens 0 .. ns-1 and lo, lo+1, ..
 struct Visible {
   int n, ns, lo;
 };
+template <int MODE = kAllTokens>
 __device__ __forceinline__ Visible visible_tokens(const AttendParams& p, int r, bool complain) {
   int s = p.sl[r];
   const int64_t row = (int64_t)p.maxp * p.P;
@@ -98,6 +122,19 @@ __device__ __forceinline__ Visible visible_tokens(const AttendParams& p, int r, 
     s = s < 0 ? 0 : (int)row;
   }
   Visible v;
+  if constexpr (MODE == kBehindPrefix) {
+    v.lo = shared_tokens(p, r, s);
+    v.ns = 0;
+    v.n = s - v.lo;
+    return v;
+  }
+  if constexpr (MODE == kChosenPages) {  // lo: the request's pages; the last of the list's holds what its last page holds
+    v.lo = s / p.P + (s % p.P != 0);
+    v.ns = 0;
+    const int listed = min(v.lo, p.budget);
+    v.n = listed > 0 ? (listed - 1) * p.P + s - (v.lo - 1) * p.P : 0;
+    return v;
+  }
   v.lo = p.window > 0 ? max(s - p.window, 0) : 0;
   v.ns = min(p.sinks, v.lo);
   v.n = v.ns + s - v.lo;
@@ -136,7 +173,7 @@ __device__ __forceinline__ int team_of(const TeamStart& t, int64_t x) {
   const int64_t wide = t.more * (t.each + 1);
   return x < wide ? (int)(x / (t.each + 1)) : t.more + (int)((x - wide) / t.each);
 }
-template <int THREADS>
+template <int THREADS, int MODE = kAllTokens>
 __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team, TeamStart* s) {
   TeamRange out = {team, 0, 0x7fffffff};
   if (p.uncut) return out;
@@ -147,7 +184,7 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
   const int r0 = (int)min((int64_t)tid * per, (int64_t)p.R), r1 = min(r0 + per, p.R);
   int64_t mine = 0;
   auto length = [&](int i) {
-    const int n = attend_tiles(visible_tokens(p, i, false).n);
+    const int n = attend_tiles(visible_tokens<MODE>(p, i, false).n);
     return n > 0 ? n + p.start_cost : 0;
   };
   for (int i = r0; i < r1; ++i) mine += length(i);
@@ -266,12 +303,16 @@ __device__ __forceinline__ void store_io4(uint8_t* p, const float4& v, float f, 
 }
 // Requests with nothing to see get zeros and a log-sum-exp of minus infinity, `rows` heads from head0. Every
 // lane looks at one request of the team's share, a warp writes what it finds.
-template <int THREADS>
+template <int THREADS, int MODE = kAllTokens>
 __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, int64_t head0, int rows, bool complain) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t first = team + (int64_t)p.teams * 32 * warp; first < p.R; first += (int64_t)p.teams * THREADS) {
     const int64_t e = first + (int64_t)p.teams * lane;
-    const bool empty = e < p.R && visible_tokens(p, (int)e, complain).n == 0;
+    const bool empty = e < p.R && visible_tokens<MODE>(p, (int)e, complain).n == 0;
+    if constexpr (MODE == kBehindPrefix) {  // the join writes the result
+      if (empty && complain) write_join(p, (int)e, 0, 0, 0);
+      continue;
+    }
     if (empty && complain && !p.uncut && p.by_request) write_join(p, (int)e, 0, 0, 0);
     for (uint32_t left = __ballot_sync(0xffffffffu, empty); left != 0; left &= left - 1) {
       const int64_t r = first + (int64_t)p.teams * (__ffs(left) - 1);
@@ -319,7 +360,7 @@ __host__ __device__ inline int attend_ctas_per_sm(int D, int type) {
   return D <= 64 ? 4 : D <= 128 ? 3 : type == kE4m3 ? 2 : 1;
 }
 
-template <int DP, int TYPE>
+template <int DP, int TYPE, int MODE>
 __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) topkv_attend_kernel(const AttendParams p) {
   using S = AttendShape<DP, TYPE>;
   constexpr bool kMmaBf16 = TYPE == kBf16;
@@ -339,15 +380,23 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
   const int h = unit / p.gtiles, g0 = (unit - h * p.gtiles) * kAttendRows;
   const int rows = min(p.G - g0, kAttendRows);
-  if (!p.late_wait) pdl_wait_prior_grid();
+  // The kernel that forms the shared prefixes' part is enqueued just before and independent of this one. It lets
+  // this one in only behind its own wait, so everything earlier has ended; one more CTA sees to it that this
+  // one does not end before it.
+  constexpr bool kWaits = MODE != kBehindPrefix;
+  if (kWaits && !p.late_wait) pdl_wait_prior_grid();
   pdl_release_next_grid();
+  if (MODE == kBehindPrefix && team == p.teams) {
+    if (unit == 0 && tid == 0) pdl_wait_prior_grid();
+    return;
+  }
 
-  const TeamRange mine = team_range<kAttendThreads>(p, team, &s_team);
-  if (p.late_wait) pdl_wait_prior_grid();
+  const TeamRange mine = team_range<kAttendThreads, MODE>(p, team, &s_team);
+  if (kWaits && p.late_wait) pdl_wait_prior_grid();
   const int64_t q_head0 = (int64_t)h * p.G + g0;
-  empty_requests<kAttendThreads>(p, team, q_head0, rows, unit == 0);
-  const bool records = !p.uncut && unit == 0 && tid == 0;
-  if (records && !p.by_request) write_join(p, 0, team, 0, 0);
+  empty_requests<kAttendThreads, MODE>(p, team, q_head0, rows, unit == 0);
+  const bool records = (MODE == kBehindPrefix || !p.uncut) && unit == 0 && tid == 0;
+  if (MODE != kBehindPrefix && records && !p.by_request) write_join(p, 0, team, 0, 0);
   if (mine.left == 0) return;
 
   uint8_t* ring = smem + warp * S::kStages * S::kStage;
@@ -369,7 +418,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
 
   for (bool first = true; left > 0 && (r < p.R || p.narrow); ++r) {
     Visible vis = {0, 0, 0};
-    if (r < p.R) vis = visible_tokens(p, r, false);
+    if (r < p.R) vis = visible_tokens<MODE>(p, r, false);
     const int tiles = attend_tiles(vis.n);
     if (tiles == 0 && !p.narrow) {
       if (p.uncut) return;
@@ -377,7 +426,16 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     }
     int t0, t1;
     const int64_t taken = tiles_in_range(p, tiles, off, left, &t0, &t1);
-    if (records && t0 == 0 && t1 > 0) request_begins(p, s_team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
+    if constexpr (MODE == kBehindPrefix) {
+      if (p.narrow) {
+        if (unit == 0 && lane == 0 && tiles > 0) write_join(p, r, r, 1, 0);
+      } else if (records && t0 == 0 && t1 > 0) {
+        const int64_t last = s_team.pos + mine.left - left - off + tiles - 1;
+        write_join(p, r, p.uncut ? r : r + team, t1 == tiles ? 1 : team_of(s_team, last) - team + 1, 0);
+      }
+    } else {
+      if (records && t0 == 0 && t1 > 0) request_begins(p, s_team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
+    }
     left -= taken;
     off = 0;
     if (t0 == t1 && !p.narrow) continue;
@@ -437,10 +495,20 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     // ---- this warp's 16 tokens of every tile: visible tokens v .. v + 15, `hop` further each time ----
     const int end = t1 == tiles ? vis.n : t1 * kTileTokens;
     const int32_t* bt_row = p.bt + (int64_t)r * p.maxp;
-    auto token = [&](int v) { return v < vis.ns ? v : v + (vis.lo - vis.ns); };
+    auto token = [&](int v) { return MODE == kChosenPages || v < vis.ns ? v : v + (vis.lo - vis.ns); };
     auto page_column = [&](int i) { return p.page_shift >= 0 ? i >> p.page_shift : i / p.P; };
+    // The page that holds place i of the tokens: the table's, or by way of the list of chosen columns.
+    const int32_t* list = MODE == kChosenPages ? p.chosen + ((int64_t)r * p.H + h) * p.budget : nullptr;
+    auto page_at = [&](int i) {
+      int j = page_column(i);
+      if constexpr (MODE == kChosenPages) {
+        j = list[j];
+        if (j < 0 || j >= vis.lo) return -1;
+      }
+      return bt_row[j];
+    };
     // The page of the tile's first token, one tile ahead of its use.
-    auto page_of = [&](int v) { return v < end ? bt_row[page_column(token(v))] : 0; };
+    auto page_of = [&](int v) { return v < end ? page_at(token(v)) : 0; };
     constexpr int kRows = 32 / S::kChunks;   // rows that one warp-wide copy brings
     static_assert(kRows >= 1, "a row is at most 512 bytes");
     constexpr int kCopies = kWarpTokens * S::kChunks / 32;
@@ -471,7 +539,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       // a window, a page outside the pool: every row for itself
       int64_t off = -1;
       if (v + (lane & 15) < end) {
-        const int i = token(v + (lane & 15)), j = page_column(i), page = bt_row[j];
+        const int i = token(v + (lane & 15)), j = page_column(i), page = page_at(i);
         if (page < 0 || page >= p.num_pages)
           raise_error(kErrTable);
         else
@@ -676,7 +744,8 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     }
     __syncthreads();
     const bool whole = t0 == 0 && t1 == tiles;
-    const int64_t slot = ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
+    const int64_t slot = MODE == kBehindPrefix ? (p.uncut ? (int64_t)r : (int64_t)r + team) * gridDim.y + unit
+                                               : ((int64_t)team * 2 + (first ? 0 : 1)) * gridDim.y + unit;
     const int quads = p.Dv / 4;
     if (p.narrow) {  // nothing to join: each warp's rows are a result
       for (int i = tid; i < kAttendWarps * rows * quads; i += kAttendThreads) {
@@ -684,6 +753,12 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
         const int w = wg / rows, g = wg - w * rows;
         if (s_seen[w] == 0) continue;  // empty_requests has written it
         const int64_t e = (int64_t)team * kAttendWarps + w;
+        if constexpr (MODE == kBehindPrefix) {
+          const int64_t row = (e * gridDim.y + unit) * p.rows + g;
+          *reinterpret_cast<float4*>(&p.part[row * p.Dv + d]) = *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]);
+          if (d == 0) p.ml[row] = make_float2(s_m[w * kAttendRows + g], s_seen[w] & kUsable ? s_l[w * kAttendRows + g] : kNoneSeen);
+          continue;
+        }
         const float sum = s_l[w * kAttendRows + g];
         store_io4(p.out + e * p.o_req + (q_head0 + g) * p.o_head + d * 2,
                   *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]),
@@ -715,7 +790,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
         acc.z += c * v.z;
         acc.w += c * v.w;
       }
-      if (whole) {
+      if (MODE != kBehindPrefix && whole) {
         const float inv = any ? __fdividef(p.v_scale, sum) : 0.f;
         store_io4(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc, inv, p.io_bf16);
         if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;

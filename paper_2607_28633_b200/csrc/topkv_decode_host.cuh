@@ -153,19 +153,25 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   return TOPKV_OK;
 }
 
-template <int DP, int TYPE>
+template <int DP, int TYPE, int MODE>
 int launch_attend(const AttendParams& p, int units, cudaStream_t s) {
   using S = AttendShape<DP, TYPE>;
   static std::atomic<uint64_t> done{0};
-  const int st = raise_smem(topkv_attend_kernel<DP, TYPE>, S::kSmem, &done);
+  const int st = raise_smem(topkv_attend_kernel<DP, TYPE, MODE>, S::kSmem, &done);
   if (st != TOPKV_OK) return st;
-  return launched(launch_pdl(topkv_attend_kernel<DP, TYPE>, dim3(p.teams, units), dim3(kAttendThreads), S::kSmem, s, p), 1);
+  return launched(launch_pdl(topkv_attend_kernel<DP, TYPE, MODE>, dim3(p.teams + (MODE == kBehindPrefix ? 1 : 0), units), dim3(kAttendThreads), S::kSmem, s, p), 1);
 }
-template <int TYPE>
+template <int TYPE, int MODE>
 int launch_attend_dim(const AttendParams& p, int units, cudaStream_t s) {
-  if (p.D <= 64) return launch_attend<64, TYPE>(p, units, s);
-  if (p.D <= 128) return launch_attend<128, TYPE>(p, units, s);
-  return launch_attend<256, TYPE>(p, units, s);
+  if (p.D <= 64) return launch_attend<64, TYPE, MODE>(p, units, s);
+  if (p.D <= 128) return launch_attend<128, TYPE, MODE>(p, units, s);
+  return launch_attend<256, TYPE, MODE>(p, units, s);
+}
+template <int MODE>
+int launch_attend_type(const AttendParams& p, uint32_t type, int units, cudaStream_t s) {
+  if (type == TOPKV_TYPE_BF16) return launch_attend_dim<kBf16, MODE>(p, units, s);
+  if (type == TOPKV_TYPE_FP16) return launch_attend_dim<kFp16, MODE>(p, units, s);
+  return launch_attend_dim<kE4m3, MODE>(p, units, s);
 }
 
 // Tensor map of one layer's rows, [page][token][column], for boxes of p->box tokens x 64 columns in the
@@ -237,6 +243,64 @@ int launch_latent(const AttendParams& p, int units, cudaStream_t s) {
   return launch_latent2<64, BF16>(p, units, s);
 }
 static_assert(latent_smem(64, kLatentMaxD, kLatentMaxDv).total <= kSmemBudget, "the largest layout fits a CTA");
+
+int check_attend_pointers(int layer, const topkv_layout* layout, const void* pool, const void* d_q, const void* d_out,
+                          const void* d_workspace, int64_t workspace_bytes, int64_t needed) {
+  if (layer < 0 || (uint32_t)layer >= layout->num_layers) return TOPKV_ERR_LAYER_RANGE;
+  if (pool == nullptr || d_q == nullptr || d_out == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult16p(pool) || !mult16p(d_q) || !mult16p(d_out)) return TOPKV_ERR_ALIGNMENT;
+  if (needed > 0) {
+    if (d_workspace == nullptr) return TOPKV_ERR_INVALID_ARG;
+    if (!mult16p(d_workspace)) return TOPKV_ERR_ALIGNMENT;
+    if (workspace_bytes < needed) return TOPKV_ERR_CAPACITY;
+  }
+  return TOPKV_OK;
+}
+// What every form of the attention takes from its descriptors.
+AttendParams attend_params(int layer, const void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                           const topkv_attention* attention, const AttendPlan& plan, const void* d_q, void* d_out) {
+  AttendParams p = {};
+  p.pool = static_cast<const uint8_t*>(pool) + (int64_t)layer * layout->pool_layer_stride;
+  p.bt = batch->block_table;
+  p.sl = batch->seq_lens;
+  p.q = static_cast<const uint8_t*>(d_q);
+  p.out = static_cast<uint8_t*>(d_out);
+  p.lse = attention->lse;
+  p.S_page = layout->pool_page_stride;
+  p.S_kv = layout->kv_factor > 1 ? layout->pool_kv_stride : 0;
+  p.S_tok = layout->page_tokens > 1 ? layout->pool_token_stride : 0;
+  p.S_head = layout->num_kv_heads > 1 ? layout->pool_head_stride : 0;
+  p.q_req = attention->q_request_stride;
+  p.q_head = attention->q_head_stride;
+  p.o_req = attention->out_request_stride;
+  p.o_head = attention->out_head_stride;
+  p.num_pages = layout->num_pool_pages;
+  p.R = batch->num_requests;
+  p.maxp = batch->max_pages_per_req;
+  p.P = (int)layout->page_tokens;
+  p.page_shift = (p.P & (p.P - 1)) == 0 ? __builtin_ctz((unsigned)p.P) : -1;
+  p.H = (int)layout->num_kv_heads;
+  p.G = (int)(attention->num_q_heads / layout->num_kv_heads);
+  p.gtiles = plan.units / p.H;
+  p.D = (int)layout->head_dim;
+  p.Dv = plan.dv;
+  p.window = batch->window_tokens;
+  p.sinks = (int)attention->sink_tokens;
+  p.qk_scale = attention->scale * attention->k_scale * kLog2e;
+  p.v_scale = attention->v_scale;
+  p.io_bf16 = attention->io_type == TOPKV_TYPE_BF16;
+  p.teams = plan.teams;
+  p.uncut = plan.uncut;
+  p.narrow = plan.narrow;
+  // Beginning with a request and writing its result takes a latent CTA, alone on its SM, about as long as
+  // three tiles (32 requests of 1,024 to 8,192 tokens, 128 heads: 77.6 us without, 75.2 with); of
+  // grouped-head CTAs others on the SM use that time (1 tile more made no difference)
+  p.start_cost = layout->kv_factor == 1 ? 3 : 0;
+  p.late_wait = (batch->flags & TOPKV_FLAG_TABLES_SETTLED) ? 1 : 0;
+  p.rows = plan.rows;
+  p.row_tile = plan.row_tile;
+  return p;
+}
 
 // ---- page operators -------------------------------------------------------------------------------
 int check_pages(const topkv_layout* lo, const topkv_batch* b, Resolved* rs) {
@@ -360,55 +424,10 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   AttendPlan plan;
   int st = check_attention(layout, batch, attention, &plan);
   if (st != TOPKV_OK) return st;
-  if (layer < 0 || (uint32_t)layer >= layout->num_layers) return TOPKV_ERR_LAYER_RANGE;
-  if (pool == nullptr || d_q == nullptr || d_out == nullptr) return TOPKV_ERR_INVALID_ARG;
-  if (!mult16p(pool) || !mult16p(d_q) || !mult16p(d_out)) return TOPKV_ERR_ALIGNMENT;
-  if (plan.bytes > 0) {
-    if (d_workspace == nullptr) return TOPKV_ERR_INVALID_ARG;
-    if (!mult16p(d_workspace)) return TOPKV_ERR_ALIGNMENT;
-    if (workspace_bytes < plan.bytes) return TOPKV_ERR_CAPACITY;
-  }
+  st = check_attend_pointers(layer, layout, pool, d_q, d_out, d_workspace, workspace_bytes, plan.bytes);
+  if (st != TOPKV_OK) return st;
   if (batch->num_requests == 0) return TOPKV_OK;
-  AttendParams p = {};
-  p.pool = static_cast<const uint8_t*>(pool) + (int64_t)layer * layout->pool_layer_stride;
-  p.bt = batch->block_table;
-  p.sl = batch->seq_lens;
-  p.q = static_cast<const uint8_t*>(d_q);
-  p.out = static_cast<uint8_t*>(d_out);
-  p.lse = attention->lse;
-  p.S_page = layout->pool_page_stride;
-  p.S_kv = layout->kv_factor > 1 ? layout->pool_kv_stride : 0;
-  p.S_tok = layout->page_tokens > 1 ? layout->pool_token_stride : 0;
-  p.S_head = layout->num_kv_heads > 1 ? layout->pool_head_stride : 0;
-  p.q_req = attention->q_request_stride;
-  p.q_head = attention->q_head_stride;
-  p.o_req = attention->out_request_stride;
-  p.o_head = attention->out_head_stride;
-  p.num_pages = layout->num_pool_pages;
-  p.R = batch->num_requests;
-  p.maxp = batch->max_pages_per_req;
-  p.P = (int)layout->page_tokens;
-  p.page_shift = (p.P & (p.P - 1)) == 0 ? __builtin_ctz((unsigned)p.P) : -1;
-  p.H = (int)layout->num_kv_heads;
-  p.G = (int)(attention->num_q_heads / layout->num_kv_heads);
-  p.gtiles = plan.units / p.H;
-  p.D = (int)layout->head_dim;
-  p.Dv = plan.dv;
-  p.window = batch->window_tokens;
-  p.sinks = (int)attention->sink_tokens;
-  p.qk_scale = attention->scale * attention->k_scale * kLog2e;
-  p.v_scale = attention->v_scale;
-  p.io_bf16 = attention->io_type == TOPKV_TYPE_BF16;
-  p.teams = plan.teams;
-  p.uncut = plan.uncut;
-  p.narrow = plan.narrow;
-  // Beginning with a request and writing its result takes a latent CTA, alone on its SM, about as long as
-  // three tiles (32 requests of 1,024 to 8,192 tokens, 128 heads: 77.6 us without, 75.2 with); of
-  // grouped-head CTAs others on the SM use that time (1 tile more made no difference)
-  p.start_cost = layout->kv_factor == 1 ? 3 : 0;
-  p.late_wait = (batch->flags & TOPKV_FLAG_TABLES_SETTLED) ? 1 : 0;
-  p.rows = plan.rows;
-  p.row_tile = plan.row_tile;
+  AttendParams p = attend_params(layer, pool, layout, batch, attention, plan, d_q, d_out);
   if (!plan.uncut) {
     uint8_t* w = static_cast<uint8_t*>(d_workspace);
     const int64_t slots = 2ll * plan.teams * plan.units * plan.rows;
@@ -421,12 +440,8 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (layout->kv_factor == 1)
     st = p.io_bf16 ? launch_latent<true>(p, plan.units, s) : launch_latent<false>(p, plan.units, s);
-  else if (attention->cache_type == TOPKV_TYPE_BF16)
-    st = launch_attend_dim<kBf16>(p, plan.units, s);
-  else if (attention->cache_type == TOPKV_TYPE_FP16)
-    st = launch_attend_dim<kFp16>(p, plan.units, s);
   else
-    st = launch_attend_dim<kE4m3>(p, plan.units, s);
+    st = launch_attend_type<kAllTokens>(p, attention->cache_type, plan.units, s);
   if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
   // about eight CTAs per SM for the requests that can be cut
   const int64_t cuts = (int64_t)plan.joins * plan.units;

@@ -3,6 +3,7 @@
 // and launches it shares.
 #pragma once
 #include "topkv_append.cuh"
+#include "topkv_prefix.cuh"
 
 namespace {
 
@@ -66,9 +67,127 @@ int launch_append(const AppendParams& p, bool chunks, dim3 grid, cudaStream_t s)
                          : launch_pdl(topkv_append_kernel<BF16, E8, false>, grid, dim3(kAppendThreads), 0, s, p), 1);
 }
 
+// ---- shared prefixes ------------------------------------------------------------------------------
+struct SharedPlan {
+  AttendPlan attend;      // of the tokens behind the prefixes
+  int tiles, tokens;      // of the prefix kernel's shape
+  int64_t own_rows, rows; // rows of parts: of the tokens behind the prefixes, of the prefixes
+  int64_t bytes;
+};
+int64_t aligned16(int64_t x) { return (x + 15) / 16 * 16; }
+
+int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, SharedPlan* plan) {
+  const int st = check_attention(lo, b, at, &plan->attend);
+  if (st != TOPKV_OK) return st;
+  if (lo->kv_factor != 2) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (b->window_tokens != 0 || at->sink_tokens != 0) return TOPKV_ERR_INVALID_ARG;
+  const AttendPlan& a = plan->attend;
+  plan->tiles = lo->head_dim <= 128 ? 2 : 1;
+  plan->tokens = lo->head_dim <= 128 ? 128 : 64;
+  const int64_t R = b->num_requests, q_rows = (int64_t)at->num_q_heads * R;
+  plan->own_rows = (R + (a.uncut ? 0 : a.teams)) * a.units * a.rows;
+  plan->rows = plan->tiles * (q_rows + (int64_t)kPrefixCtas * kPrefixRows);
+  plan->bytes = R == 0 ? 0
+                       : R * 16 + (int64_t)sizeof(PrefixHeader) + aligned16(R * 8) + aligned16((plan->own_rows + plan->rows) * 8) +
+                             (plan->own_rows + plan->rows) * a.dv * 4;
+  plan->bytes = (plan->bytes + 255) / 256 * 256;
+  return TOPKV_OK;
+}
+
+template <int DP, int TYPE>
+int launch_prefix(const PrefixParams& p, cudaStream_t s) {
+  using S = PrefixShape<DP, TYPE>;
+  static std::atomic<uint64_t> done{0};
+  const int st = raise_smem(topkv_prefix_kernel<DP, TYPE>, S::kSmem, &done);
+  if (st != TOPKV_OK) return st;
+  return launched(launch_pdl(topkv_prefix_kernel<DP, TYPE>, dim3(kPrefixCtas), dim3(S::kThreads), S::kSmem, s, p), 1);
+}
+template <int TYPE>
+int launch_prefix_dim(const PrefixParams& p, cudaStream_t s) {
+  if (p.a.D <= 64) return launch_prefix<64, TYPE>(p, s);
+  if (p.a.D <= 128) return launch_prefix<128, TYPE>(p, s);
+  return launch_prefix<256, TYPE>(p, s);
+}
+
 }  // namespace
 
 extern "C" {
+
+int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, int32_t min_tokens, int32_t* d_plan,
+                        topkv_stream_t stream) {
+  Resolved rs;
+  const int st = check_pages(layout, batch, &rs);
+  if (st != TOPKV_OK) return st;
+  if (min_tokens < 0) return TOPKV_ERR_INVALID_ARG;
+  if (batch->num_requests == 0) return TOPKV_OK;
+  if (d_plan == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult4p(d_plan)) return TOPKV_ERR_ALIGNMENT;
+  if ((int64_t)batch->num_requests * TOPKV_PLAN_ROWS > 0x7fffffffll) return TOPKV_ERR_INVALID_ARG;
+  PrefixPlanParams p;
+  p.bt = batch->block_table;
+  p.sl = batch->seq_lens;
+  p.plan = d_plan;
+  p.num_pages = layout->num_pool_pages;
+  p.R = batch->num_requests;
+  p.maxp = batch->max_pages_per_req;
+  p.P = (int)layout->page_tokens;
+  p.min_tokens = min_tokens;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)((p.R + kPrefixPlanThreads / 32 - 1) / (kPrefixPlanThreads / 32)));
+  const int first = launched(launch_pdl(topkv_plan_leaders_kernel, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);
+  if (first != TOPKV_OK) return first;
+  return launched(launch_pdl(topkv_plan_groups_kernel, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);
+}
+
+int64_t topkv_attend_shared_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                            const topkv_attention* attention) {
+  SharedPlan plan;
+  const int st = check_shared(layout, batch, attention, &plan);
+  return st != TOPKV_OK ? st : plan.bytes;
+}
+
+int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                              const topkv_attention* attention, const int32_t* d_plan, const void* d_q, void* d_out,
+                              void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream) {
+  SharedPlan plan;
+  int st = check_shared(layout, batch, attention, &plan);
+  if (st != TOPKV_OK) return st;
+  st = check_attend_pointers(layer, layout, pool, d_q, d_out, d_workspace, workspace_bytes, plan.bytes);
+  if (st != TOPKV_OK) return st;
+  if (batch->num_requests == 0) return TOPKV_OK;
+  if (d_plan == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult4p(d_plan)) return TOPKV_ERR_ALIGNMENT;
+  if ((int64_t)batch->num_requests * TOPKV_PLAN_ROWS > 0x7fffffffll) return TOPKV_ERR_INVALID_ARG;
+  PrefixParams p = {};
+  p.a = attend_params(layer, pool, layout, batch, attention, plan.attend, d_q, d_out);
+  p.a.plan = d_plan;
+  p.tiles = plan.tiles;
+  p.tokens = plan.tokens;
+  uint8_t* w = static_cast<uint8_t*>(d_workspace);
+  auto part = [&](int64_t bytes) {
+    uint8_t* at = w;
+    w += aligned16(bytes);
+    return at;
+  };
+  const int64_t R = p.a.R;
+  p.a.joins = reinterpret_cast<int4*>(part(R * 16));
+  p.a.by_request = 1;
+  p.header = reinterpret_cast<PrefixHeader*>(part(sizeof(PrefixHeader)));
+  p.begin = reinterpret_cast<int64_t*>(part(R * 8));
+  p.a.ml = reinterpret_cast<float2*>(part((plan.own_rows + plan.rows) * 8));
+  p.ml = p.a.ml + plan.own_rows;
+  p.a.part = reinterpret_cast<float*>(w);
+  p.part = p.a.part + plan.own_rows * p.a.Dv;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const uint32_t type = attention->cache_type;
+  st = type == TOPKV_TYPE_BF16 ? launch_prefix_dim<kBf16>(p, s) : type == TOPKV_TYPE_FP16 ? launch_prefix_dim<kFp16>(p, s) : launch_prefix_dim<kE4m3>(p, s);
+  if (st != TOPKV_OK) return st;
+  st = launch_attend_type<kBehindPrefix>(p.a, type, plan.attend.units, s);
+  if (st != TOPKV_OK) return st;
+  const int64_t ctas = R * plan.attend.units;
+  const unsigned z = (unsigned)std::max<int64_t>((plan.attend.rows + kJoinRows - 1) / kJoinRows, std::min<int64_t>(plan.attend.rows, 4 * 148 / ctas));
+  return launched(launch_pdl(topkv_prefix_join_kernel, dim3((unsigned)R, plan.attend.units, z), dim3(kPrefixJoinThreads), 0, s, p), 1);
+}
 
 int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const topkv_batch* batch,
                        const topkv_new_tokens* tokens, const void* d_k, const void* d_v, const void* d_q,

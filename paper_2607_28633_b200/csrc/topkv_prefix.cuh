@@ -1,0 +1,827 @@
+// Attention of one new token per request where groups of requests share their first tokens: the plan of who
+// shares what, the shared tokens' part, and the join with what each request has for itself.
+//
+//   part over the tokens i of a range:  m = max x_i, l = sum exp(x_i - m), o = sum exp(x_i - m) V[i]
+//   parts join by  out = sum_k exp(m_k - m) o_k / sum_k exp(m_k - m) l_k,  m = max m_k
+//
+// The queries of a group's members and of a KV head's G query heads are the rows of one product with the
+// prefix: members * G rows, 2 * members * G flops a byte at 16 bits, so with 128 rows the tensor rate (254
+// flop a byte of this memory) is about reached: the product runs on the tensor memory path (tcgen05), 128 rows to a
+// tile, rows in TMEM lanes, one thread a row, so that maxima and sums need no exchange:
+//
+//   S [128 x tokens] = Q [128 x D] K^T         both K-major in shared memory
+//   O [128 x D]     += P [128 x tokens] V      P in TMEM, over the scores it was made of; V N-major
+//
+// A CTA, alone on its SM, has two accumulators that work by turns, the softmax of one under the products of the
+// other: with more than 128 rows they are two tiles of rows over the same tokens, else the same rows over every
+// other tile of tokens. (256 columns: one accumulator, two buffers of scores, 64 tokens a tile.) Roles:
+//   warps 0-7    softmax: four per accumulator, one thread a row; also Q and the result
+//   warps 8-11   load K and V through the block table into a ring (16-byte copies; 8-bit values become fp16)
+//   warp 12      one thread issues the products
+// The (group, KV head, 256 rows) units laid end to end, as long as their tiles, are cut into equal ranges, one
+// per CTA; each leaves its part in 32 bits in the workspace, and the joining kernel adds them to those of the
+// tokens behind the prefix, in order, so that results do not depend on timing.
+// Waits are bounded and TMEM is held as in the latent-row kernel.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "topkv_attend.cuh"
+#include "topkv_common.cuh"
+#include "topkv_latent.cuh"
+
+namespace topkv {
+
+// ---- the plan -------------------------------------------------------------------------------------
+constexpr int kPrefixPlanThreads = 256;
+struct PrefixPlanParams {
+  const int32_t* bt;
+  const int32_t* sl;
+  int32_t* plan;
+  int64_t num_pages;
+  int R, maxp, P, min_tokens;
+};
+// Full pages of a row, as far as its table goes.
+__device__ __forceinline__ int full_pages(const PrefixPlanParams& p, int r) {
+  return min(max(p.sl[r], 0) / p.P, p.maxp);
+}
+// A warp per row: the lowest row that begins with the same page, and how many pages both have in common.
+__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_leaders_kernel(const PrefixPlanParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
+  if (r >= p.R) return;
+  const int32_t* mine = p.bt + (int64_t)r * p.maxp;
+  int full = full_pages(p, r), lead = r;
+  const int page = full > 0 ? mine[0] : -1;
+  if (p.sl[r] < 0 || p.sl[r] > (int64_t)p.maxp * p.P) {
+    if (lane == 0) raise_error(kErrTable);
+  }
+  if (page >= 0 && page < p.num_pages) {
+    constexpr int kAhead = 4;
+    for (int q0 = 0; q0 < r; q0 += 32 * kAhead) {
+      bool same[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int q = q0 + u * 32 + lane;
+        same[u] = q < r && full_pages(p, q) > 0 && p.bt[(int64_t)q * p.maxp] == page;
+      }
+#pragma unroll
+      for (int u = kAhead - 1; u >= 0; --u) {
+        const uint32_t found = __ballot_sync(0xffffffffu, same[u]);
+        if (found != 0) lead = q0 + u * 32 + __ffs(found) - 1;
+      }
+      if (lead != r) break;
+    }
+  }
+  const int32_t* first = p.bt + (int64_t)lead * p.maxp;
+  full = min(full, full_pages(p, lead));
+  int common = full;
+  if (lead != r) {
+    constexpr int kAhead = 4;
+    for (int j0 = 0; j0 < full; j0 += 32 * kAhead) {
+      bool differ[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int j = j0 + u * 32 + lane;
+        differ[u] = j < full && first[j] != mine[j];
+      }
+      int at = full;
+#pragma unroll
+      for (int u = kAhead - 1; u >= 0; --u) {
+        const uint32_t found = __ballot_sync(0xffffffffu, differ[u]);
+        if (found != 0) at = j0 + u * 32 + __ffs(found) - 1;
+      }
+      if (at < full) {
+        common = at;
+        break;
+      }
+    }
+  }
+  if (lane == 0) {
+    p.plan[TOPKV_PLAN_LEADER * p.R + r] = lead;
+    p.plan[TOPKV_PLAN_COMMON * p.R + r] = common * p.P;
+  }
+}
+// A warp per row: over all rows, what its group shares, its size, and the row's place in the order.
+__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(const PrefixPlanParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
+  if (r >= p.R) return;
+  const int32_t* leader = p.plan + TOPKV_PLAN_LEADER * p.R;
+  const int32_t* common = p.plan + TOPKV_PLAN_COMMON * p.R;
+  const int lead = leader[r];
+  int shared = 0x7fffffff, members = 0, place = 0;
+#pragma unroll 4
+  for (int q = lane; q < p.R; q += 32) {
+    const int l = leader[q];
+    if (l == lead) {
+      shared = min(shared, common[q]);
+      ++members;
+    }
+    place += l < lead || (l == lead && q < r);
+  }
+  shared = __reduce_min_sync(0xffffffffu, shared);
+  members = __reduce_add_sync(0xffffffffu, members);
+  place = __reduce_add_sync(0xffffffffu, place);
+  if (lane == 0) {
+    p.plan[TOPKV_PLAN_SHARED * p.R + r] = members > 1 && shared >= p.min_tokens ? shared : 0;
+    p.plan[TOPKV_PLAN_MEMBERS * p.R + r] = members;
+    p.plan[TOPKV_PLAN_PLACE * p.R + r] = place;
+    p.plan[TOPKV_PLAN_ORDER * p.R + place] = r;
+  }
+}
+
+// ---- the shared tokens' part ------------------------------------------------------------------------
+constexpr int kPrefixRows = 128;    // rows of a tile
+constexpr int kPrefixLoadWarps = 4;
+constexpr int kPrefixMaxStages = 8;
+constexpr int kPrefixCtas = 148;    // at most
+
+struct PrefixControl {
+  uint64_t bar[2 * kPrefixMaxStages + 7];
+  int64_t scan[16];
+  int64_t off;
+  int lead;
+  uint32_t tmem;
+  volatile int dead;
+  float row_scale[2 * kPrefixRows];
+};
+template <int DP, int TYPE>
+struct PrefixShape {
+  static constexpr int kTiles = DP <= 128 ? 2 : 1;        // accumulators
+  static constexpr int kTokens = DP <= 128 ? 128 : 64;    // per tile
+  static constexpr int kQ = kPrefixRows * DP * 2;         // bytes of a tile of Q
+  static constexpr int kStage = kTokens * DP * 2;         // ... of K or V
+  static constexpr int kRoom = (227 * 1024 - kTiles * kQ - (int)sizeof(PrefixControl)) / kStage;
+  static constexpr int kStages = kRoom < kPrefixMaxStages ? kRoom : kPrefixMaxStages;
+  static constexpr int kControl = kTiles * kQ + kStages * kStage;
+  static constexpr int kSmem = kControl + (int)sizeof(PrefixControl);
+  static constexpr int kSoftmaxWarps = 4 * kTiles;
+  static constexpr int kThreads = (kSoftmaxWarps + kPrefixLoadWarps + 1) * 32;
+  static constexpr uint32_t kScores = 0, kSums = 2 * kTokens;  // TMEM columns: two buffers of scores, the accumulators
+  static_assert(2 * kTokens + kTiles * DP <= 512, "TMEM");
+  static_assert(kStages >= 5, "a ring shorter than five entries could wait for itself");
+};
+// What the joining kernel has to know, in the workspace.
+struct PrefixHeader {
+  int64_t each;  // length of a range ...
+  int more;      // ... and how many are one longer
+  int teams;
+};
+struct PrefixParams {
+  AttendParams a;          // teams is that of the tokens behind the prefix
+  PrefixHeader* header;
+  int64_t* begin;          // [R], of leaders: where the group's units begin on the line
+  float2* ml;              // [rows of parts]
+  float* part;             // [rows of parts][Dv]
+  int tiles;               // accumulators, tokens per tile: those of the kernel's shape
+  int tokens;
+};
+// A group: its leader, and the geometry of its units.
+struct PrefixGroup {
+  int lead, place;   // its first row's place in the plan's order
+  int tokens, n;     // shared tokens, tiles of them
+  int rows;          // members * G
+  int units;         // per KV head
+  int full;          // length of a unit of all rows
+  int64_t length;    // of a KV head's units
+};
+__device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int lead) {
+  const AttendParams& a = p.a;
+  PrefixGroup g;
+  g.lead = lead;
+  g.tokens = shared_tokens(a, lead, a.sl[lead]);
+  if (a.plan[TOPKV_PLAN_LEADER * a.R + lead] != lead) g.tokens = 0;
+  g.tokens = (int)min((int64_t)g.tokens, (int64_t)a.maxp * a.P);
+  if (g.tokens == 0) return g;
+  g.n = (g.tokens - 1) / p.tokens + 1;
+  g.place = min(max(a.plan[TOPKV_PLAN_PLACE * a.R + lead], 0), a.R - 1);
+  g.rows = min(a.plan[TOPKV_PLAN_MEMBERS * a.R + lead], a.R - g.place) * a.G;
+  const int tall = kPrefixRows * p.tiles, rest = (g.rows - 1) % tall + 1;
+  g.units = (g.rows - 1) / tall + 1;
+  g.full = g.n * p.tiles;
+  g.length = (int64_t)(g.units - 1) * g.full + (rest > kPrefixRows ? g.full : g.n);
+  return g;
+}
+// One unit: rows first_row .. first_row + rows - 1 of a group with one KV head.
+struct PrefixUnit {
+  int h, first_row, rows;
+  bool both;       // the accumulators hold different rows; a tile of tokens is as long as both
+  int length;
+  int64_t slot;    // row of parts where the unit's parts of team 0 would lie
+};
+__device__ __forceinline__ PrefixUnit prefix_unit(const PrefixParams& p, const PrefixGroup& g, int h, int i) {
+  PrefixUnit u;
+  const int tall = kPrefixRows * p.tiles;
+  u.h = h;
+  u.first_row = i * tall;
+  u.rows = min(tall, g.rows - u.first_row);
+  u.both = u.rows > kPrefixRows;
+  u.length = u.both ? g.full : g.n;
+  u.slot = p.tiles * ((int64_t)p.a.H * p.a.G * g.place + (int64_t)h * g.rows + u.first_row);
+  return u;
+}
+__device__ __forceinline__ int prefix_team_of(const PrefixHeader& t, int64_t x) {
+  const int64_t wide = t.more * (t.each + 1);
+  return x < wide ? (int)(x / (t.each + 1)) : t.more + (int)((x - wide) / t.each);
+}
+// The next leader of a group that shares, from row r on (a whole warp asks); R if there is none.
+__device__ __forceinline__ int next_group(const PrefixParams& p, int r, int lane) {
+  for (; r < p.a.R; r += 32) {
+    const int mine = r + lane;
+    const uint32_t found = __ballot_sync(0xffffffffu, mine < p.a.R && prefix_group(p, mine).tokens > 0);
+    if (found != 0) return r + __ffs(found) - 1;
+  }
+  return p.a.R;
+}
+
+__device__ __forceinline__ void tcgen05_mma_ta(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 db; mov.b64 db, {%2, %3}; setp.ne.u32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p; }" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+
+template <int DP, int TYPE>
+__global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_prefix_kernel(const PrefixParams p) {
+  using S = PrefixShape<DP, TYPE>;
+  constexpr bool kBf = TYPE == kBf16;
+  constexpr float kShift = kBf ? 0.f : 7.f;
+  constexpr int kTokens = S::kTokens, kTiles = S::kTiles, kStages = S::kStages;
+  constexpr int kLoadWarp = S::kSoftmaxWarps, kIssueWarp = kLoadWarp + kPrefixLoadWarps;
+  constexpr int kSoftmaxThreads = S::kSoftmaxWarps * 32;
+  constexpr int kBlock = kTokens * 128, kQBlock = kPrefixRows * 128;  // bytes of 64 columns
+  extern __shared__ __align__(128) uint8_t smem[];
+  const AttendParams& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, team = blockIdx.x;
+  const uint32_t base = smem_addr(smem);
+  if (base & 1023) {
+    if (tid == 0) raise_error(kErrWait);
+    return;
+  }
+  PrefixControl& ctl = *reinterpret_cast<PrefixControl*>(smem + S::kControl);
+  volatile int& s_dead = ctl.dead;
+  const uint32_t b_full = smem_addr(ctl.bar), b_free = b_full + 8 * kStages, b_score = b_free + 8 * kStages;
+  const uint32_t b_weight = b_score + 16, b_sum = b_score + 32, b_query = b_score + 48;
+  if (tid == 0) {
+    s_dead = 0;
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(b_full + 8 * i, kPrefixLoadWarps * 32);
+      mbar_init(b_free + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(b_score + 8 * i, 1);
+      mbar_init(b_weight + 8 * i, 128);
+      mbar_init(b_sum + 8 * i, 1);
+    }
+    mbar_init(b_query, kSoftmaxThreads);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kIssueWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "n"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    tcgen05_before_sync();
+  }
+  if (!a.late_wait) pdl_wait_prior_grid();
+
+  // ---- this CTA's range of the line --------------------------------------------------------------------
+  int64_t pos, left = 0;
+  {
+    const int per = (a.R + S::kThreads - 1) / S::kThreads;
+    const int r0 = (int)min((int64_t)tid * per, (int64_t)a.R), r1 = min(r0 + per, a.R);
+    auto length = [&](int r) {
+      const PrefixGroup g = prefix_group(p, r);
+      return g.tokens > 0 ? a.H * g.length : 0;
+    };
+    int64_t mine = 0;
+    for (int r = r0; r < r1; ++r) mine += length(r);
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    if (lane == 31) ctl.scan[warp] = incl;
+    if (tid == 0) ctl.lead = -1;
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < S::kThreads / 32; ++w) {
+      if (w < warp) incl += ctl.scan[w];
+      total += ctl.scan[w];
+    }
+    // a range is two tiles long at least: what a CTA costs to begin is about that
+    const int teams = (int)min((int64_t)gridDim.x, max((total + 1) / 2, (int64_t)1));
+    PrefixHeader t;
+    t.each = total / teams;
+    t.more = (int)(total - t.each * teams);
+    t.teams = teams;
+    pos = t.each * team + min(team, t.more);
+    if (team < teams) left = t.each + (team < t.more ? 1 : 0);
+    if (a.late_wait) pdl_wait_prior_grid();  // the join of the call before reads the workspace until then
+    int64_t at = incl - mine;
+    const bool begins = left > 0 && pos >= at && pos < incl;  // exactly one thread
+    if (begins || team == 0) {
+      for (int r = r0; r < r1; ++r) {
+        const int64_t n = length(r);
+        if (team == 0) p.begin[r] = at;
+        if (begins && pos >= at && pos < at + n) {
+          ctl.lead = r;
+          ctl.off = pos - at;
+        }
+        at += n;
+      }
+    }
+    if (team == 0 && tid == 0) *p.header = t;
+  }
+  __syncthreads();
+  tcgen05_after_sync();
+  const uint32_t tmem = ctl.tmem;
+  pdl_release_next_grid();  // every CTA has its TMEM, and has waited for what came before
+
+  auto wait = [&](uint32_t bar, uint32_t phase) {
+    if (mbar_try_wait(bar, phase & 1)) return;
+    const long long began = clock64();
+    while (!mbar_try_wait(bar, phase & 1)) {
+      if (s_dead) break;
+      if (clock64() - began > kWaitClocks) {
+        s_dead = 1;
+        raise_error(kErrWait);
+        break;
+      }
+    }
+  };
+
+  constexpr uint32_t kType = 1u << 4 | (kBf ? 1u : 0u) << 7 | (kBf ? 1u : 0u) << 10 | 8u << 24;  // M = 128
+  constexpr uint32_t kScore = kType | (uint32_t)(kTokens >> 3) << 17;
+  const uint32_t kValue = kType | 1u << 16 | (uint32_t)((a.D + 15) / 16 * 2) << 17;  // V is N-major
+  const int ksteps = (a.D + 15) / 16;
+  uint32_t seq = 0;                 // tiles of tokens before the current segment, in this CTA
+  uint32_t done[2] = {0, 0};        // jobs before, by the buffer of scores they use
+  uint32_t seg = 0;
+  uint32_t issued = 0;              // load: entries whose copies are enqueued
+  PrefixGroup g = {};
+  int64_t off = ctl.off;
+  int lead = ctl.lead;
+  if (left > 0 && lead >= 0) g = prefix_group(p, lead);
+  while (left > 0 && lead >= 0 && lead < a.R) {
+    // the unit, and the tiles [t0, t1) of it that are this CTA's
+    const int h = (int)(off / g.length);
+    const int64_t in_head = off - h * g.length;
+    const int i = (int)min(in_head / g.full, (int64_t)g.units - 1);
+    const PrefixUnit u = prefix_unit(p, g, h, i);
+    const int from = (int)(in_head - (int64_t)i * g.full);
+    const int take = (int)min(left, (int64_t)(u.length - from));
+    const int scale = u.both ? kTiles : 1;
+    const int t0 = (from + scale - 1) / scale, t1 = (from + take + scale - 1) / scale, count = t1 - t0;
+    const int jobs = count * scale;
+    const int64_t slot = u.slot + (int64_t)team * (kPrefixRows * kTiles);
+    auto page_column = [&](int x) { return a.page_shift >= 0 ? x >> a.page_shift : x / a.P; };
+    const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
+
+    if (warp >= kLoadWarp && warp < kIssueWarp) {
+      // ---- load ---------------------------------------------------------------------------------------
+      constexpr int kRows = kTokens / kPrefixLoadWarps;  // rows of this warp
+      const int w = warp - kLoadWarp;
+      const uint8_t* head = a.pool + (int64_t)h * a.S_head;
+      auto page_of = [&](int t) {
+        const int x = t * kTokens + w * kRows + lane;
+        return t < t1 && lane < kRows && x < g.tokens ? bt_row[page_column(x)] : -1;
+      };
+      int pg = page_of(t0);
+      for (int t = t0; t < t1; ++t) {
+        if (__any_sync(0xffffffffu, s_dead)) break;
+        int64_t o = -1;
+        const int x = t * kTokens + w * kRows + lane;
+        if (lane < kRows && x < g.tokens) {
+          if (pg < 0 || pg >= a.num_pages)
+            raise_error(kErrTable);
+          else
+            o = (int64_t)pg * a.S_page + (int64_t)(x - page_column(x) * a.P) * a.S_tok;
+        }
+        pg = page_of(t + 1);
+#pragma unroll 1
+        for (int plane = 0; plane < 2; ++plane) {
+          const uint32_t entry = issued, stage = entry % kStages;
+          const uint32_t dst = base + kTiles * S::kQ + stage * S::kStage + w * kRows * 128;
+          const uint8_t* src0 = head + plane * a.S_kv;
+          if constexpr (TYPE == kE4m3) {
+            constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kCopies = kRows / kPer;
+            const int c = lane % kChunks, sub = lane / kChunks;
+            uint4 v[kCopies];
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const int64_t ro = __shfl_sync(0xffffffffu, o, k * kPer + sub);
+              v[k] = make_uint4(0, 0, 0, 0);
+              if (ro >= 0 && c * 16 < a.D) v[k] = *reinterpret_cast<const uint4*>(src0 + ro + c * 16);
+            }
+            if (entry >= kStages) wait(b_free + 8 * stage, entry / kStages - 1);
+            if (c * 16 < a.D) {
+#pragma unroll
+              for (int k = 0; k < kCopies; ++k) {
+                const int row = k * kPer + sub;
+                uint32_t x8[8];
+                e4m3x4_to_f16(v[k].x, &x8[0], &x8[1]);
+                e4m3x4_to_f16(v[k].y, &x8[2], &x8[3]);
+                e4m3x4_to_f16(v[k].z, &x8[4], &x8[5]);
+                e4m3x4_to_f16(v[k].w, &x8[6], &x8[7]);
+                uint8_t* to = smem + (dst - base) + (c >> 2) * kBlock + row * 128;
+                const int ch = (c & 3) * 2;
+                *reinterpret_cast<uint4*>(to + ((ch ^ (row & 7)) << 4)) = make_uint4(x8[0], x8[1], x8[2], x8[3]);
+                *reinterpret_cast<uint4*>(to + (((ch + 1) ^ (row & 7)) << 4)) = make_uint4(x8[4], x8[5], x8[6], x8[7]);
+              }
+            }
+            proxy_fence_smem();
+            bar_arrive(b_full + 8 * stage);
+          } else {
+            if (entry >= kStages) wait(b_free + 8 * stage, entry / kStages - 1);
+            const int chunks = a.D / 8, padded = ksteps * 2, full = chunks / 8;
+            const int c = lane & 7, sub = lane >> 3;
+#pragma unroll 2
+            for (int rg = 0; rg < kRows / 4; ++rg) {
+              const int row = rg * 4 + sub;
+              const int64_t ro = __shfl_sync(0xffffffffu, o, row);
+              const uint8_t* src = (ro < 0 ? a.pool : src0 + ro) + c * 16;
+              uint32_t to = dst + row * 128 + ((c ^ (row & 7)) << 4);
+#pragma unroll
+              for (int b = 0; b < DP / 64; ++b, to += kBlock) {
+                if (b < full)
+                  cp_async16(to, ro < 0 ? a.pool : src + b * 128, ro >= 0);
+                else if (b * 8 + c < padded)
+                  cp_async16(to, ro >= 0 && b * 8 + c < chunks ? src + b * 128 : a.pool, ro >= 0 && b * 8 + c < chunks);
+              }
+            }
+            cp_async_commit();
+            // the entry before has arrived, now that this one is under way
+            if (entry > 0) {
+              cp_async_wait<1>();
+              proxy_fence_smem();
+              bar_arrive(b_full + 8 * ((entry - 1) % kStages));
+            }
+          }
+          ++issued;
+        }
+      }
+    } else if (warp == kIssueWarp) {
+      // ---- products -----------------------------------------------------------------------------------
+      if (jobs > 0) wait(b_query, seg);
+      const uint32_t q0 = operand_lo(base, 16);
+      const uint32_t kv0 = operand_lo(base + kTiles * S::kQ, 16), v00 = operand_lo(base + kTiles * S::kQ, kBlock);
+      for (int j = 0; j < jobs + 2; ++j) {
+        if (__any_sync(0xffffffffu, s_dead)) break;
+        if (j >= 2) {
+          const int jj = j - 2, b = jj & 1, t = u.both ? jj >> 1 : jj;
+          const uint32_t entry = 2 * (seq + t) + 1, stage = entry % kStages;
+          wait(b_weight + 8 * b, done[b] + (jj >> 1));
+          wait(b_full + 8 * stage, entry / kStages);
+          tcgen05_after_sync();
+          const uint32_t d = tmem + S::kSums + (kTiles == 2 ? b * DP : 0), w = tmem + b * kTokens, v0 = v00 + stage * (S::kStage >> 4);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < kTokens / 16; ++k)
+              tcgen05_mma_ta(d, w + 8 * k, v0 + 128 * k, kOperandHi, kValue, jj >= kTiles || k > 0);
+            tcgen05_commit(b_sum + 8 * b);
+            if (!u.both || b == 1) tcgen05_commit(b_free + 8 * stage);
+          }
+          __syncwarp();
+        }
+        if (j < jobs) {
+          const int b = j & 1, t = u.both ? j >> 1 : j;
+          const uint32_t entry = 2 * (seq + t), stage = entry % kStages;
+          wait(b_full + 8 * stage, entry / kStages);
+          tcgen05_after_sync();
+          const uint32_t d = tmem + b * kTokens, k0 = kv0 + stage * (S::kStage >> 4), qa = q0 + (u.both ? b * (S::kQ >> 4) : 0);
+          if (elect_one()) {
+            for (int k = 0; k < ksteps; ++k)
+              tcgen05_mma(d, qa + (k >> 2) * (kQBlock >> 4) + 2 * (k & 3), k0 + (k >> 2) * (kBlock >> 4) + 2 * (k & 3), kOperandHi, kScore, k > 0);
+            tcgen05_commit(b_score + 8 * b);
+            if (!u.both || b == 1) tcgen05_commit(b_free + 8 * stage);
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp < kLoadWarp) {
+      // ---- softmax ------------------------------------------------------------------------------------
+      const int acc = warp >> 2, row = (warp & 3) * 32 + lane;        // accumulator, TMEM lane
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+      const int my_row = u.both ? acc * kPrefixRows + row : row;      // of the unit
+      const bool live = my_row < u.rows;
+      float row_scale = a.qk_scale;
+      if (jobs > 0) {
+        // Q of the segment before is done with: both accumulators' last products have been waited for
+        asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+        if (u.both || acc == 0) {
+          const int gr = u.first_row + my_row, member = gr / a.G;
+          const uint8_t* src = nullptr;
+          if (live) {
+            int r = a.plan[TOPKV_PLAN_ORDER * a.R + g.place + member];
+            r = min(max(r, 0), a.R - 1);
+            src = a.q + r * a.q_req + ((int64_t)h * a.G + gr - member * a.G) * a.q_head;
+          }
+          const int chunks = a.D / 8, padded = ksteps * 2;
+          float up = 1.f, rest = 1.f;
+          if (TYPE == kE4m3 && a.io_bf16) {
+            // bf16 queries become fp16 ones after a power of two for the row; see the kernel of the other tokens
+            float top = 0.f;
+            for (int c = 0; c < chunks; ++c) {
+              const uint4 v = live ? *reinterpret_cast<const uint4*>(src + c * 16) : make_uint4(0, 0, 0, 0);
+              const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u))));
+            }
+            int e = 0;
+            if (top > 0.f && top < INFINITY) e = ilogbf(top);
+            up = exp2f((float)(-(e / 2)));
+            rest = exp2f((float)(-(e - e / 2)));
+            row_scale = a.qk_scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
+          }
+          ctl.row_scale[my_row] = row_scale;
+          for (int c = 0; c < padded; ++c) {
+            uint4 v = live && c < chunks ? *reinterpret_cast<const uint4*>(src + c * 16) : make_uint4(0, 0, 0, 0);
+            if (TYPE == kE4m3 && a.io_bf16) {
+              uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                x[e] = pack2<false>(__uint_as_float(x[e] << 16) * up * rest, __uint_as_float(x[e] & 0xffff0000u) * up * rest);
+              v = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+            *reinterpret_cast<uint4*>(smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+          }
+          proxy_fence_smem();
+        }
+        tcgen05_before_sync();
+        asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+        row_scale = ctl.row_scale[my_row];
+        bar_arrive(b_query);
+      }
+      // Pages outside the pool are not visible. They are looked for once for the segment; only if there are
+      // any does every tile ask which of its tokens count.
+      bool odd = false;
+      for (int t = page_column(t0 * kTokens) + lane; count > 0 && t <= page_column(min(t1 * kTokens, g.tokens) - 1); t += 32) {
+        const int page = bt_row[t];
+        odd |= page < 0 || page >= a.num_pages;
+      }
+      odd = __any_sync(0xffffffffu, odd);
+      const bool some = __any_sync(0xffffffffu, live);  // a row of this warp counts
+      float m = -INFINITY, l = 0.f;
+      bool seen = false;
+      int last = -1;  // this accumulator's last job
+      for (int j = kTiles == 2 ? acc : 0; j < jobs; j += kTiles) {
+        const int b = j & 1, t = t0 + (u.both ? j >> 1 : j);
+        const uint32_t s_col = tmem + lanes + b * kTokens;
+        wait(b_score + 8 * b, done[b] + (j >> 1));
+        // no phase of a barrier is left out, since a wait tells them apart by parity alone
+        if (j >= 2) wait(b_sum + 8 * b, done[b] + (j >> 1) - 1);
+        if (__any_sync(0xffffffffu, s_dead)) break;
+        tcgen05_after_sync();
+        last = j;
+        if (some) {
+          // which of the tile's tokens count, 32 to a word
+          uint32_t valid[kTokens / 32];
+          const int visible = g.tokens - t * kTokens;
+#pragma unroll
+          for (int c = 0; c < kTokens / 32; ++c) {
+            const int n = visible - c * 32;
+            valid[c] = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+          }
+          if (odd) {
+#pragma unroll
+            for (int c = 0; c < kTokens / 32; ++c) {
+              const int x = t * kTokens + c * 32 + lane;
+              const int page = x < g.tokens ? bt_row[page_column(x)] : -1;
+              valid[c] &= __ballot_sync(0xffffffffu, page >= 0 && page < a.num_pages);
+            }
+          }
+          const bool partial = odd || visible < kTokens;
+          float top = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < kTokens / 32; ++c) {
+            uint32_t raw[32];
+            tmem_load<32>(raw, s_col + c * 32);
+            tmem_wait_load();
+            seen |= valid[c] != 0;
+            if (partial) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (valid[c] >> e & 1) top = fmaxf(top, __uint_as_float(raw[e]) * row_scale);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(raw[e]) * row_scale);
+            }
+          }
+          if (__any_sync(0xffffffffu, top > m + kLazy)) {
+            float alpha = 1.f;
+            if (top > m) {
+              alpha = exp2_approx(m - top);
+              m = top;
+            }
+            l *= alpha;
+            if (j >= kTiles) {
+              // With two accumulators the scores' arrival says that this one's products have ended, with one
+              // those of the job before may still be running.
+              if (kTiles == 1) {
+                wait(b_sum + 8 * (b ^ 1), done[b ^ 1] + ((j - 1) >> 1));
+                tcgen05_after_sync();
+              }
+              for (int c = 0; c < DP / 32; ++c) {
+                if (c * 32 >= a.D) break;
+                uint32_t o[32];
+                tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
+                tmem_wait_load();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_store<32>(tmem + lanes + S::kSums + acc * DP + c * 32, o);
+              }
+            }
+          }
+          const float sub = m == -INFINITY ? 0.f : m - kShift;
+#pragma unroll
+          for (int c = 0; c < kTokens / 32; ++c) {
+            uint32_t raw[32], w[16];
+            tmem_load<32>(raw, s_col + c * 32);
+            tmem_wait_load();
+            float e[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) e[k] = exp2_approx(fmaf(__uint_as_float(raw[k]), row_scale, -sub));
+            if (partial) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (!(valid[c] >> k & 1)) e[k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              l += e[k] + e[k + 1];
+              w[k / 2] = pack2<kBf>(e[k], e[k + 1]);
+            }
+            tmem_store<16>(s_col + c * 16, w);  // over scores that have been read
+          }
+          tmem_wait_store();
+        }
+        tcgen05_before_sync();
+        bar_arrive(b_weight + 8 * b);
+      }
+      // ---- the segment's part --------------------------------------------------------------------------
+      // Every accumulator of the unit leaves one: of its rows, or of the same rows and other tokens.
+      if (last >= 0) {
+        if (kTiles == 1 && last > 0) wait(b_sum + 8 * ((last - 1) & 1), done[(last - 1) & 1] + ((last - 1) >> 1));
+        wait(b_sum + 8 * (last & 1), done[last & 1] + (last >> 1));
+        tcgen05_after_sync();
+      }
+      const int64_t to = slot + (u.both || acc == 0 ? my_row : u.rows + my_row);
+      if (live) p.ml[to] = make_float2(m - kShift, seen ? l : kNoneSeen);
+      if (last >= 0 && some) {
+        for (int c = 0; c < DP / 32; ++c) {
+          if (c * 32 >= a.D) break;
+          uint32_t o[32];
+          tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
+          tmem_wait_load();
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              if (c * 32 + e < a.D)
+                *reinterpret_cast<float4*>(&p.part[to * a.Dv + c * 32 + e]) =
+                    make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+          }
+        }
+      }
+      tcgen05_before_sync();
+    }
+    seq += count;
+    done[0] += (jobs + 1) / 2;
+    done[1] += jobs / 2;
+    if (jobs > 0) ++seg;
+    left -= take;
+    off += take;
+    if (off == a.H * g.length && left > 0) {
+      off = 0;
+      lead = next_group(p, lead + 1, lane);
+      if (lead < a.R) g = prefix_group(p, lead);
+    }
+  }
+  if constexpr (TYPE != kE4m3) {
+    if (warp >= kLoadWarp && warp < kIssueWarp && issued > 0) {
+      cp_async_wait<0>();
+      proxy_fence_smem();
+      bar_arrive(b_full + 8 * ((issued - 1) % kStages));
+    }
+  }
+  if (s_dead) {  // give the copies and products that are in flight a millisecond to end
+    const long long began = clock64();
+    while (clock64() - began < 2000000) __nanosleep(1000);
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  if (warp == kIssueWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// ---- join -------------------------------------------------------------------------------------------
+// A CTA takes up to kJoinRows heads of a request and KV head: parts of the tokens behind the prefix, then those
+// of the prefix, in order. First a warp per row turns the parts' maxima and sums into weights, then each
+// thread adds up four columns of a row.
+constexpr int kPrefixJoinThreads = 256;
+constexpr int kPrefixJoinParts = kJoinParts + 2 * kPrefixCtas;
+__global__ void __launch_bounds__(kPrefixJoinThreads) topkv_prefix_join_kernel(const PrefixParams p) {
+  __shared__ float s_w[kJoinRows][kPrefixJoinParts];
+  __shared__ int64_t s_first[kJoinRows];
+  __shared__ int s_n[kJoinRows], s_step[kJoinRows];
+  const AttendParams& a = p.a;
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int r = blockIdx.x, unit = blockIdx.y;
+  const int h = unit / a.gtiles, g0 = (unit - h * a.gtiles) * a.row_tile;
+  const int per = (a.rows + gridDim.z - 1) / gridDim.z, row0 = blockIdx.z * per;
+  const int rows = min(per, min(a.G - g0, a.row_tile) - row0);
+  if (rows <= 0) return;
+  const int s = (int)min((int64_t)max(a.sl[r], 0), (int64_t)a.maxp * a.P);
+  const int4 rec = a.joins[r];
+  const int behind = rec.z, units = gridDim.y;
+  const int64_t q_head0 = (int64_t)h * a.G + g0 + row0;
+  const int64_t b_first = ((int64_t)rec.y * units + unit) * a.rows + row0, b_step = (int64_t)units * a.rows;
+  // where the prefix parts of each row lie: kTiles to a team unless the accumulators hold different rows
+  const bool shares = shared_tokens(a, r, s) > 0;
+  if (tid < rows) {
+    int n = 0, step = 0;
+    int64_t first = 0;
+    if (shares) {
+      const int lead = a.plan[TOPKV_PLAN_LEADER * a.R + r];
+      const PrefixGroup g = prefix_group(p, lead);
+      const int row = (a.plan[TOPKV_PLAN_PLACE * a.R + r] - a.plan[TOPKV_PLAN_PLACE * a.R + lead]) * a.G + g0 + row0 + tid;
+      if (g.tokens > 0 && row < g.rows) {
+        const int i = row / (kPrefixRows * p.tiles);
+        const PrefixUnit u = prefix_unit(p, g, h, i);
+        const PrefixHeader t = *p.header;
+        const int64_t pos = p.begin[lead] + h * g.length + (int64_t)i * g.full;
+        const int t0 = prefix_team_of(t, pos), t1 = prefix_team_of(t, pos + u.length - 1);
+        first = u.slot + (int64_t)t0 * (kPrefixRows * p.tiles) + row - u.first_row;
+        step = u.both || p.tiles == 1 ? 0 : u.rows;  // from one part of a team to its other
+        n = (t1 - t0 + 1) * (step > 0 ? 2 : 1);
+      }
+    }
+    s_n[tid] = n;
+    s_step[tid] = step;
+    s_first[tid] = first;
+  }
+  __syncthreads();
+  // rows of parts: of part k >= behind of row g
+  auto prefix_part = [&](int g, int k) -> int64_t {
+    const int step = s_step[g];
+    return s_first[g] + (step > 0 ? (int64_t)(k >> 1) * (kPrefixRows * p.tiles) + (k & 1) * step : (int64_t)k * (kPrefixRows * p.tiles));
+  };
+  for (int g = warp; g < rows; g += kPrefixJoinThreads / 32) {
+    const int parts = behind + s_n[g];
+    auto ml_of = [&](int k) { return k < behind ? a.ml[b_first + g + k * b_step] : p.ml[prefix_part(g, k - behind)]; };
+    float top = -INFINITY, sum = 0.f;
+    bool seen = false;
+    for (int k = lane; k < parts; k += 32) {
+      const float2 ml = ml_of(k);
+      if (ml.y != kNoneSeen) {
+        seen = true;
+        top = fmaxf(top, ml.x);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float from = top == -INFINITY ? 0.f : top;
+    for (int k = lane; k < parts; k += 32) {
+      const float2 ml = ml_of(k);
+      const float w = ml.y != kNoneSeen ? exp2_approx(ml.x - from) : 0.f;
+      sum += w * ml.y;
+      s_w[g][k] = w;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    seen = __any_sync(0xffffffffu, seen);
+    const float inv = seen ? a.v_scale / sum : 0.f;
+    __syncwarp();
+    for (int k = lane; k < parts; k += 32) s_w[g][k] *= inv;
+    if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)r * a.H * a.G + q_head0 + g] = seen ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  }
+  __syncthreads();
+  const int quads = a.Dv / 4, items = rows * quads;
+  for (int i = tid; i < items; i += kPrefixJoinThreads) {
+    const int g = i / quads, d = (i - g * quads) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float* from, float f) {
+      const float4 v = *reinterpret_cast<const float4*>(from);
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
+    };
+#pragma unroll 4
+    for (int k = 0; k < behind; ++k)
+      add(a.part + (b_first + g + k * b_step) * a.Dv + d, s_w[g][k]);
+#pragma unroll 4
+    for (int k = 0; k < s_n[g]; ++k)
+      if (s_w[g][behind + k] != 0.f) add(p.part + prefix_part(g, k) * a.Dv + d, s_w[g][behind + k]);
+    store_io4(a.out + r * a.o_req + (q_head0 + g) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
+  }
+}
+
+}  // namespace topkv

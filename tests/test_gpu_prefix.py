@@ -1,0 +1,282 @@
+"""GPU tests of attention behind shared prefixes: the plan against plain loops, integer for integer, and the
+attention against the oracle in 64 bits over all tokens (tolerances derived in oracle.decode.attend)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import decode as od, tokens as ot
+from paper_2607_28633_b200 import binding as tk
+from test_gpu_decode import NAN, TORCH, TYPE, _check, _geom, _layout
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    import __graft_entry__ as entry
+    entry.build()
+    return torch.device("cuda:0")
+
+
+@pytest.fixture(autouse=True)
+def clean(dev):
+    tk.check(tk.topkv_reset_device_error_flags())
+    yield
+    assert tk.topkv_device_error_flags() == 0
+
+
+def _tables(groups, P, rng, extra_cols=1, shuffle=True):
+    """groups: (prefix pages, [tokens behind the prefix of each member]). Rows of all groups, mixed."""
+    rows = []
+    total = sum(n + sum(-(-t // P) for t in tails) for n, tails in groups) + 3
+    ids, at = rng.permutation(total), 0
+    for n, tails in groups:
+        common, at = list(ids[at:at + n]), at + n
+        for t in tails:
+            k = -(-t // P)
+            rows.append((n * P + t, common + list(ids[at:at + k])))
+            at += k
+    if shuffle:
+        rows = [rows[i] for i in rng.permutation(len(rows))]
+    bt = np.full((len(rows), max(len(x) for _, x in rows) + extra_cols), -1, np.int32)
+    for r, (_, pages) in enumerate(rows):
+        bt[r, :len(pages)] = pages
+    return bt, np.array([s for s, _ in rows]), total
+
+
+def _filled(g, bt, sl, kind, rng, layer=0):
+    """NaN patterns everywhere but in the tokens that some request holds."""
+    pool = np.empty(g.L * g.S_layer, np.uint8)
+    pool[0::2], pool[1::2] = NAN[kind]
+    n, done = g.d_h * g.b_p, set()
+    for r, s in enumerate(sl):
+        for i in range(max(int(s), 0)):
+            where = (int(bt[r, i // g.P]), i % g.P)
+            if where in done or not 0 <= where[0] < g.num_pages:
+                continue
+            done.add(where)
+            for c in range(2):
+                for h in range(g.h_kv):
+                    a = od.row_offset(g, layer, where[0], c, where[1], h)
+                    pool[a:a + n] = od.encode_elements(rng.normal(size=g.d_h), kind)
+    return pool
+
+
+class Case:
+    def __init__(self, dev, groups, H=2, G=2, D=64, P=16, kind="bf16", io=None, style="page", L=1, layer=0, seed=0, ks=1.0, vs=1.0, tables=None,
+                 q_size=1.0, scale=None):
+        rng = np.random.default_rng(seed)
+        self.dev, self.kind, self.layer, self.ks, self.vs = dev, kind, layer, ks, vs
+        self.io = io or (kind if kind != "e4m3" else "bf16")
+        self.bt, self.sl, pages = _tables(groups, P, rng) if tables is None else tables
+        self.g = _geom(2, H, D, 1 if kind == "e4m3" else 2, P, pages, style, L)
+        self.lo = _layout(self.g)
+        self.pool_h = _filled(self.g, self.bt, self.sl, kind, rng, layer)
+        self.pool = torch.from_numpy(self.pool_h).to(dev)
+        R = len(self.sl)
+        self.q_h = od.decode_elements(od.encode_elements(q_size * rng.normal(size=R * H * G * D), self.io), self.io).reshape(R, H * G, D)
+        self.q = torch.from_numpy(self.q_h).to(dev).to(TORCH[self.io])
+        self.out = torch.full_like(self.q, 7.0)
+        self.lse = torch.full((R, H * G), 3.0, device=dev)
+        self.d_bt = torch.from_numpy(self.bt).to(dev)
+        self.d_sl = torch.from_numpy(self.sl.astype(np.int32)).to(dev)
+        self.batch = tk.make_batch(self.d_bt, self.d_sl)
+        self.scale = D ** -0.5 if scale is None else scale
+        self.att = tk.make_attention(self.q, self.out, TYPE[kind], TYPE[self.io], self.scale, k_scale=ks, v_scale=vs, lse=self.lse)
+        self.n = tk.check(tk.topkv_attend_shared_workspace_bytes(self.lo, self.batch, self.att))
+        self.ws = torch.full((self.n + 32,), 0xFF, dtype=torch.uint8, device=dev)  # NaN patterns: nothing is assumed
+        self.plan = torch.full((6, R), -7, dtype=torch.int32, device=dev)
+        torch.cuda.synchronize()
+
+    def make_plan(self, min_tokens=0, stream=None):
+        tk.check(tk.topkv_plan_prefixes(self.lo, self.batch, min_tokens, self.plan, stream))
+
+    def attend(self, stream=None):
+        tk.check(tk.topkv_attend_shared_layer(self.layer, self.pool, self.lo, self.batch, self.att, self.plan, self.q, self.out, self.ws, self.n, stream))
+
+    def result(self):
+        torch.cuda.synchronize()
+        assert (self.ws[self.n:] == 0xFF).all() and np.array_equal(self.pool.cpu().numpy(), self.pool_h)
+        return self.out.double().cpu().numpy(), self.lse.double().cpu().numpy()
+
+    def want(self):
+        return od.attend(self.g, self.layer, self.pool_h, self.bt, self.sl, self.q_h, self.kind, self.io, self.scale, k_scale=self.ks, v_scale=self.vs)
+
+    def check(self, min_tokens=0):
+        self.make_plan(min_tokens)
+        self.attend()
+        got = self.result()
+        assert np.array_equal(self.plan.cpu().numpy(), ot.plan_prefixes(self.g.P, self.g.num_pages, self.bt, self.sl, min_tokens))
+        _check(got, self.want())
+
+
+@pytest.mark.parametrize("groups, kw", [
+    ([(3, [5, 9])], dict()),
+    ([(1, [1] * 4)], dict()),
+    ([(8, [5, 9, 0, 33])], dict()),                                   # one has nothing of its own; a whole tile
+    ([(9, [20] * 70)], dict(G=2, H=1)),                               # 140 rows: two tiles of rows
+    ([(9, [3] * 300)], dict(G=1, H=1)),                               # 300 rows: two units, the second of one tile
+    ([(20, [3] * 129)], dict(G=1, H=2)),
+    ([(40, [30, 700])], dict(P=24)),
+    ([(0, [5, 70]), (4, [3, 3]), (30, [1, 2, 3, 200, 500]), (0, [0]), (2, [0, 0])], dict()),
+    ([(0, [5, 70, 0])], dict()),                                      # nothing is shared
+    ([(33, [3, 40])], dict(D=128, kind="fp16", style="head")),
+    ([(33, [3, 40])], dict(D=128, kind="e4m3", ks=0.5, vs=1.5)),
+    ([(33, [3, 40] * 40)], dict(D=128, kind="e4m3", io="fp16", H=1, style="padded")),
+    ([(33, [3, 40])], dict(D=80, G=7)), ([(33, [3, 40])], dict(D=72, kind="fp16")), ([(33, [3, 40])], dict(D=96, kind="e4m3")),
+    ([(33, [3, 40] * 5)], dict(D=256, H=1, G=16)), ([(33, [3, 40] * 5)], dict(D=192, H=1, G=24, kind="fp16")),
+    ([(33, [3, 40] * 5)], dict(D=256, H=1, G=4, kind="e4m3", ks=0.25)), ([(50, [3] * 100)], dict(D=200, H=1, G=2)),
+    ([(300, [3, 40])], dict(P=1, style="head")), ([(5, [3, 40])], dict(P=256, style="plane")),
+    ([(7, [3, 40])], dict(D=8, H=5, G=1)), ([(7, [3, 40])], dict(D=16, H=5, G=3, kind="e4m3")),
+    ([(300, [3, 900, 5])], dict(H=1, G=4, seed=3)),                   # many CTAs a unit
+    ([(40, [3, 40])], dict(L=3, layer=2, style="padded")),
+    ([(40, [3, 40])], dict(q_size=30.0)), ([(40, [3, 40])], dict(q_size=30.0, kind="fp16")),   # maxima that move
+    ([(40, [3, 40])], dict(q_size=3e4, scale=1e-5, kind="e4m3")),
+    ([(40, [3, 40])], dict(scale=-0.2)), ([(40, [3, 40])], dict(scale=0.0)),
+    ([(1, [3] * 2)] * 30, dict(H=1)),                                 # many small groups
+])
+def test_against_the_oracle(dev, groups, kw):
+    Case(dev, groups, **kw).check()
+
+
+def test_long_prefix_over_all_ctas(dev):
+    Case(dev, [(260, [9, 1000] + [3] * 5)], H=1, G=8, D=128, P=32).check()
+    Case(dev, [(520, [9] + [3] * 7)], H=1, G=8, D=128, P=16, kind="e4m3").check()
+    Case(dev, [(260, [9, 100])], H=1, G=4, D=256, P=16).check()
+
+
+def test_a_plan_with_a_lower_limit_shares_less(dev):
+    for least in (48, 49, 1000):
+        Case(dev, [(3, [5, 9]), (6, [4, 3, 2])]).check(least)
+
+
+def test_groups_within_a_group_share_what_all_of_it_shares(dev):
+    bt = np.array([[4, 1, 2, 3, -1], [4, 1, 5, 6, -1], [4, 1, 2, 7, -1], [8, 1, 2, 9, -1], [-1] * 5], np.int32)
+    sl = np.array([60, 50, 64, 60, 0])
+    c = Case(dev, None, tables=(bt, sl, 10))
+    c.check()
+    assert c.plan[2].tolist() == [32, 32, 32, 0, 0]
+
+
+def test_the_plan_stays_good_while_requests_grow(dev):
+    c = Case(dev, [(9, [40, 70, 33]), (3, [20, 30])])
+    whole = c.sl.copy()
+    c.d_sl.copy_(torch.from_numpy(whole - 15))
+    c.make_plan()
+    c.d_sl.copy_(torch.from_numpy(whole))
+    c.attend()
+    _check(c.result(), c.want())
+
+
+def test_a_freed_row_is_attended_to_on_its_own(dev):
+    c = Case(dev, [(9, [40, 70, 33, 5])])
+    c.make_plan()
+    for r in (0, 2):
+        c.sl[r] = 0
+        c.d_sl[r] = 0
+        c.attend()
+        _check(c.result(), c.want())
+
+
+def test_contradicting_plans_reach_nothing_outside(dev):
+    """Every field by turns holds what no plan says: results are numbers of some kind, error bits may be raised."""
+    c = Case(dev, [(9, [40, 70, 33]), (3, [20, 30]), (0, [17])])
+    c.make_plan()
+    torch.cuda.synchronize()
+    good, rng = c.plan.clone(), np.random.default_rng(5)
+    R = len(c.sl)
+    for trial in range(40):
+        bad = good.clone()
+        for row in ([trial % 6] if trial < 24 else range(6)):
+            bad[row] = torch.from_numpy(rng.integers(*[(-3, R + 3), (-2 ** 31, 2 ** 31 - 1), (0, 200), (0, R)][trial // 6 % 4], size=R).astype(np.int32)).to(dev)
+        c.plan.copy_(bad)
+        c.attend()
+        c.result()
+        tk.check(tk.topkv_reset_device_error_flags())
+    c.plan.copy_(good)
+    c.attend()
+    _check(c.result(), c.want())
+
+
+def test_pages_outside_the_pool_are_not_visible(dev):
+    c = Case(dev, [(20, [40, 70, 33])], H=1, P=8)
+    c.make_plan()
+    torch.cuda.synchronize()
+    alone = c.bt.copy()
+    bad = c.bt.copy()
+    bad[:, [3, 11]] = [[-5, c.g.num_pages]]
+    c.d_bt.copy_(torch.from_numpy(bad))
+    c.attend()
+    torch.cuda.synchronize()
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
+    # the same without these pages
+    keep = [j for j in range(c.bt.shape[1]) if j not in (3, 11)]
+    c.bt, c.sl = np.ascontiguousarray(alone[:, keep]), c.sl - 16
+    _check(c.result(), c.want())
+    # no usable page at all in the prefix
+    bad[:, :20] = -1
+    c.bt, c.sl = np.ascontiguousarray(alone[:, 20:]), c.sl - 18 * 8
+    c.d_bt.copy_(torch.from_numpy(bad))
+    c.attend()
+    torch.cuda.synchronize()
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
+    _check(c.result(), c.want())
+
+
+def test_same_bits_again_and_equal_to_graphs_and_other_streams(dev):
+    c = Case(dev, [(40, [30, 700, 9]), (7, [1] * 9)], D=128)
+    c.make_plan()
+    c.attend()
+    first = [x.copy() for x in c.result()]
+    for stream in (None, torch.cuda.Stream(dev)):
+        c.out.fill_(7.0)
+        c.lse.fill_(3.0)
+        torch.cuda.synchronize()
+        c.make_plan(stream=stream)
+        c.attend(stream)
+        assert all(np.array_equal(a, b) for a, b in zip(first, c.result()))
+    c.out.fill_(7.0)
+    c.plan.fill_(-1)
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        s = torch.cuda.current_stream()
+        c.make_plan(stream=s)
+        c.attend(s)
+        c.attend(s)
+    for _ in range(3):
+        gr.replay()
+    assert all(np.array_equal(a, b) for a, b in zip(first, c.result()))
+
+
+def test_scores_of_minus_infinity_and_nan_stay_with_their_rows(dev):
+    c = Case(dev, [(9, [20, 30, 40])], H=1, G=2)
+    c.make_plan()
+    c.q[1, 0, 0] = float("nan")
+    c.q[2, 1, 3] = float("inf")
+    c.attend()
+    out, lse = c.result()
+    ref, ref_lse, tol, tol_lse = c.want()
+    bad = np.zeros(lse.shape, bool)
+    bad[1, 0] = bad[2, 1] = True
+    assert np.isnan(out[bad]).all()
+    assert (np.abs(out - ref) <= tol)[~bad].all() and (np.abs(lse - ref_lse) <= tol_lse)[~bad].all()
+
+
+def test_large_plan(dev):
+    rng = np.random.default_rng(1)
+    R, maxp = 1500, 200
+    bt = rng.integers(0, 9, size=(R, 1)).astype(np.int32) * 1000 + np.arange(maxp, dtype=np.int32)
+    for r in range(R):
+        bt[r, rng.integers(50, maxp):] = rng.integers(0, 10000)
+    bt[7, 0], bt[9, 0] = -1, 10 ** 6
+    sl = rng.integers(0, maxp * 4, size=R)
+    plan = torch.full((6, R), -7, dtype=torch.int32, device=dev)
+    b = tk.make_batch(torch.from_numpy(bt).to(dev), torch.from_numpy(sl.astype(np.int32)).to(dev))
+    tk.check(tk.topkv_plan_prefixes(tk.make_layout(1, 2, 1, 64, 2, 4, 10000), b, 8, plan))
+    torch.cuda.synchronize()
+    assert np.array_equal(plan.cpu().numpy(), ot.plan_prefixes(4, 10000, bt, sl, 8))
