@@ -119,3 +119,73 @@ def plan_prefixes(P: int, num_pages: int, bt, sl, min_tokens: int = 0) -> np.nda
     order = sorted(range(R), key=lambda r: (leader[r], r))
     place = [order.index(r) for r in range(R)]
     return np.array([leader, common, shared, members, order, place], np.int32).reshape(6, R)
+
+
+# ---- chosen pages ---------------------------------------------------------------------------------------
+# Every operation below is one rounding to 32 bits, as the definition says, so the results are exact.
+
+C127 = np.float32(1) / np.float32(127)
+
+
+def bound_pages(g: Geom, layer: int, pool: np.ndarray, bt, sl, window: int, kind: str, bounds: np.ndarray, steps: np.ndarray) -> int:
+    """Writes int8 bounds [pages][H][2][D] and float32 steps [pages][H]; returns error bits."""
+    err = 0
+    R, maxp = bt.shape
+    for r in range(R):
+        s = int(sl[r])
+        if not 0 <= s <= maxp * g.P:
+            err, s = err | ERR_TABLE, min(max(s, 0), maxp * g.P)
+        for j in range(max(s - window, 0) // g.P if window else 0, -(-s // g.P)):
+            page = int(bt[r, j])
+            if not 0 <= page < g.num_pages:
+                err |= ERR_TABLE
+                continue
+            tok = np.arange(j * g.P, min(s, (j + 1) * g.P))
+            for h in range(g.h_kv):
+                k = rows_of(g, layer, pool, bt[r], tok, 0, h, kind).astype(np.float32)
+                step = (np.nan if np.isnan(k).any() else np.abs(k).max()) * C127
+                steps[page, h] = step
+                if not (step > 0 and np.isfinite(step)):
+                    bounds[page, h] = 0
+                    continue
+                bounds[page, h, 0] = np.clip(np.floor(k.min(0) / step), -127, 127)
+                bounds[page, h, 1] = np.clip(np.ceil(k.max(0) / step), -127, 127)
+    return err
+
+
+def choose_pages(P: int, bt, sl, q: np.ndarray, H: int, bounds, steps, budget: int, firsts: int, lasts: int) -> np.ndarray:
+    """int32 [R][H][budget]."""
+    R, maxp = bt.shape
+    G = q.shape[1] // H
+    out = np.full((R, H, budget), -1, np.int32)
+    for r in range(R):
+        pages = -(-min(max(int(sl[r]), 0), maxp * P) // P)
+        for h in range(H):
+            score = np.full(pages, -np.inf, np.float32)
+            for a in range(h * G, (h + 1) * G):
+                x = q[r, a].astype(np.float32)
+                t = np.abs(x).max() * C127
+                if not (t > 0 and np.isfinite(t)):
+                    t, q8 = np.float32(0), np.zeros(len(x), np.int64)
+                else:
+                    q8 = np.clip(np.rint(x / t), -127, 127).astype(np.int64)
+                ids = np.clip(bt[r, :pages], 0, len(steps) - 1)
+                b = bounds[ids, h].astype(np.int64)                              # [pages][2][D]
+                dot = (np.minimum(q8, 0) * b[:, 0] + np.maximum(q8, 0) * b[:, 1]).sum(1)
+                with np.errstate(all="ignore"):
+                    by = np.minimum(t * steps[ids, h], np.finfo(np.float32).max)
+                    one = dot.astype(np.float32) * by
+                    score = np.maximum(score, np.where(np.isfinite(steps[ids, h]), one, np.float32(np.inf)))
+            last = range(max(pages - lasts, 0), pages)
+            rank = sorted(range(pages), key=lambda j: (0, -j) if j in last else (1, j) if j < firsts else (2, -score[j], j))
+            best = sorted(rank[:budget])
+            out[r, h, :len(best)] = best
+    return out
+
+
+def of_chosen(P: int, bt_row, s: int, columns) -> tuple[np.ndarray, int]:
+    """The table row and length of a request that has the chosen pages alone."""
+    columns = [j for j in columns if j >= 0]
+    pages = -(-s // P)
+    n = (len(columns) - 1) * P + s - (pages - 1) * P if columns else 0
+    return np.array([bt_row[j] for j in columns] or [-1], np.int32), n

@@ -418,6 +418,11 @@ def lib() -> ctypes.CDLL:
         L.topkv_attend_shared_workspace_bytes.argtypes = [lp, bp, ap]
         L.topkv_attend_shared_workspace_bytes.restype = c_int64
         L.topkv_attend_shared_layer.argtypes = [c_int, c_void_p, lp, bp, ap, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
+        L.topkv_bound_pages_layer.argtypes = [c_int, c_void_p, lp, bp, c_uint32, c_void_p, c_void_p, c_void_p]
+        L.topkv_page_choice_workspace_bytes.argtypes = [lp, bp, ap, cp]
+        L.topkv_page_choice_workspace_bytes.restype = c_int64
+        L.topkv_choose_pages_layer.argtypes = [lp, bp, ap, cp, c_void_p, c_void_p, c_int64, c_void_p]
+        L.topkv_attend_pages_layer.argtypes = [c_int, c_void_p, lp, bp, ap, cp, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
         ep = ctypes.POINTER(topkv_endpoint)
         L.topkv_select_transport.argtypes = [ep, ep, c_int, c_int]
         L.topkv_planning_rate.argtypes = [c_int]
@@ -783,6 +788,28 @@ def topkv_attend_shared_layer(layer, pool, layout, batch, attention, d_plan, d_q
     return lib().topkv_attend_shared_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
                                            ctypes.byref(attention), _ptr(d_plan), _ptr(d_q), _ptr(d_out),
                                            _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def topkv_bound_pages_layer(layer, pool, layout, batch, cache_type, d_bounds, d_steps, stream=None):
+    return lib().topkv_bound_pages_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch), cache_type,
+                                         _ptr(d_bounds), _ptr(d_steps), _stream(stream))
+
+
+def topkv_page_choice_workspace_bytes(layout, batch, attention, choice):
+    return lib().topkv_page_choice_workspace_bytes(ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(attention),
+                                                   ctypes.byref(choice))
+
+
+def topkv_choose_pages_layer(layout, batch, attention, choice, d_q, d_workspace, workspace_bytes, stream=None):
+    return lib().topkv_choose_pages_layer(ctypes.byref(layout), ctypes.byref(batch), ctypes.byref(attention),
+                                          ctypes.byref(choice), _ptr(d_q), _ptr(d_workspace), workspace_bytes, _stream(stream))
+
+
+def topkv_attend_pages_layer(layer, pool, layout, batch, attention, choice, d_q, d_out, d_workspace, workspace_bytes,
+                             stream=None):
+    return lib().topkv_attend_pages_layer(layer, _ptr(pool), ctypes.byref(layout), ctypes.byref(batch),
+                                          ctypes.byref(attention), ctypes.byref(choice), _ptr(d_q), _ptr(d_out),
+                                          _ptr(d_workspace), workspace_bytes, _stream(stream))
 
 
 def topkv_header_fill(header, request_id, model_id, layout, seq_len, crc_k, crc_v):

@@ -1,0 +1,437 @@
+// Which pages a query looks at: bounds of each page's keys in 8 bits, and the choice of the pages that can
+// score highest.
+//
+//   step = max |K| c, c = 1/127    lo[d] = floor(min K[d] / step)    hi[d] = ceil(max K[d] / step)
+//   t = max |q| c                  q8[d] = rint(q[d] / t)
+//   score = max over the heads of (sum_d q8[d] < 0 ? q8[d] lo[d] : q8[d] hi[d]) * (t * step)
+//
+// The sum is of whole numbers, and what is left are two roundings, so the choice does not depend on any order
+// of summation. With q8 split into its negative and its positive part the sum is one product over 2 D
+// elements, [negative | positive] . [lo | hi], formed by the warp-wide 8-bit matrix instruction: 16 heads by 8
+// pages by 32 elements. Elements may be paired in any order, so a thread brings 16 consecutive bytes of a page's bounds
+// at a time and keeps its queries in the matching order.
+//
+// What bounds it: the bounds, 2 D + 4 bytes a page and head (1/32 of a cache of 16-token pages), read once; in
+// small calls the chain table -> bounds -> keys -> four passes of 8 bits each over the keys -> list.
+// A cluster of 1 to 8 CTAs has one request and KV head, each CTA an equal share of its pages; histograms and
+// counts are added up through the cluster's shared memory.
+#pragma once
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include <cfloat>
+#include <cstdint>
+
+#include "topkv_append.cuh"
+#include "topkv_attend.cuh"
+#include "topkv_common.cuh"
+
+namespace topkv {
+
+constexpr float k127th = 1.f / 127.f;
+
+// ---- bounds ---------------------------------------------------------------------------------------
+constexpr int kBoundThreads = 256;
+struct BoundParams {
+  const uint8_t* pool;  // this layer's slab
+  const int32_t* bt;
+  const int32_t* sl;
+  int8_t* bounds;       // [pages][H][2][D]
+  float* steps;         // [pages][H]
+  int64_t S_page, S_tok, S_head;
+  int64_t num_pages;
+  int64_t items;        // R * columns * H
+  int maxp, P, H, D;
+  int window;
+  int columns;          // that the window can touch
+};
+template <int TYPE>
+struct BoundElements {
+  static constexpr int kN = TYPE == kE4m3 ? 16 : 8;  // of 16 bytes
+};
+template <int TYPE>
+__device__ __forceinline__ void elements_of(const uint4& v, float (&x)[BoundElements<TYPE>::kN]) {
+  if constexpr (TYPE == kE4m3) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t h[2];
+      e4m3x4_to_f16(w[i], &h[0], &h[1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[j]));
+        x[4 * i + 2 * j] = f.x;
+        x[4 * i + 2 * j + 1] = f.y;
+      }
+    }
+  } else {
+    unpack8<TYPE == kBf16>(v, x);
+  }
+}
+// A warp per page and head: lanes over the 16-byte chunks of a key, groups of them over the tokens.
+template <int TYPE>
+__global__ void __launch_bounds__(kBoundThreads) topkv_bound_pages_kernel(const BoundParams p) {
+  constexpr int N = BoundElements<TYPE>::kN;
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31;
+  const int64_t item = (int64_t)blockIdx.x * (kBoundThreads / 32) + (threadIdx.x >> 5);
+  if (item >= p.items) return;
+  const int64_t at = item / p.H;
+  const int h = (int)(item - at * p.H), r = (int)(at / p.columns);
+  int s = p.sl[r];
+  const int64_t row = (int64_t)p.maxp * p.P;
+  if (s < 0 || s > row) {
+    if (lane == 0) raise_error(kErrTable);
+    s = s < 0 ? 0 : (int)row;
+  }
+  const int first = p.window > 0 ? max(s - p.window, 0) / p.P : 0;
+  const int64_t j = first + (at - (int64_t)r * p.columns);
+  if (j * p.P >= s) return;
+  const int page = p.bt[(int64_t)r * p.maxp + j], held = min(p.P, s - (int)j * p.P);
+  if (page < 0 || page >= p.num_pages) {
+    if (lane == 0) raise_error(kErrTable);
+    return;
+  }
+  const int chunks = p.D / N, groups = 32 / chunks, group = lane / chunks, c = lane - group * chunks;
+  const uint8_t* src = p.pool + (int64_t)page * p.S_page + (int64_t)h * p.S_head + c * 16;
+  float lo[N], hi[N];
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    lo[i] = INFINITY;
+    hi[i] = -INFINITY;
+  }
+  auto take = [&](const uint4& v) {
+    float x[N];
+    elements_of<TYPE>(v, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      nan |= x[i] != x[i];
+      lo[i] = fminf(lo[i], x[i]);
+      hi[i] = fmaxf(hi[i], x[i]);
+    }
+  };
+  if (group < groups) {
+    constexpr int kAhead = 8;
+    for (int t = group; t < held; t += groups * kAhead) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (t + u * groups < held) v[u] = *reinterpret_cast<const uint4*>(src + (int64_t)(t + u * groups) * p.S_tok);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (t + u * groups < held) take(v[u]);
+    }
+  }
+  for (int k = 1; k < groups; ++k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      lo[i] = fminf(lo[i], __shfl_sync(0xffffffffu, lo[i], (c + k * chunks) & 31));
+      hi[i] = fmaxf(hi[i], __shfl_sync(0xffffffffu, hi[i], (c + k * chunks) & 31));
+    }
+  }
+  // the first group has them all from here on
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (group == 0) most = fmaxf(most, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (__any_sync(0xffffffffu, nan)) most = NAN;
+  const float step = __fmul_rn(most, k127th);
+  const bool usable = step > 0.f && step < INFINITY;
+  const int64_t to = (int64_t)page * p.H + h;
+  if (lane == 0) p.steps[to] = step;
+  if (group == 0) {
+    uint32_t w[2][N / 4] = {};
+    if (usable) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int a = (int)fminf(fmaxf(floorf(__fdiv_rn(lo[i], step)), -127.f), 127.f);
+        const int b = (int)fminf(fmaxf(ceilf(__fdiv_rn(hi[i], step)), -127.f), 127.f);
+        w[0][i / 4] |= (uint32_t)(a & 255) << (i % 4 * 8);
+        w[1][i / 4] |= (uint32_t)(b & 255) << (i % 4 * 8);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      int8_t* out = p.bounds + (to * 2 + k) * p.D + c * N;
+      if constexpr (N == 16)
+        *reinterpret_cast<uint4*>(out) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+      else
+        *reinterpret_cast<uint2*>(out) = make_uint2(w[k][0], w[k][1]);
+    }
+  }
+}
+
+// ---- choice ---------------------------------------------------------------------------------------
+constexpr int kChooseThreads = 256;
+constexpr int kChooseWarps = kChooseThreads / 32;
+constexpr int kChooseCluster = 8;
+constexpr int kChooseRows = 16;  // heads of one matrix instruction
+struct ChooseParams {
+  const int32_t* bt;
+  const int32_t* sl;
+  const uint8_t* q;
+  const int8_t* bounds;
+  const float* steps;
+  int32_t* chosen;
+  uint32_t* keys;       // workspace [R][H][maxp], or nullptr: they fit in shared memory
+  int64_t q_req, q_head;
+  int64_t num_pages;
+  int maxp, P, H, G, D;
+  int budget, firsts, lasts;
+  int pitch;            // bytes of a head's queries in shared memory
+};
+__device__ __forceinline__ void mma16832(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Rising floats as rising unsigned numbers.
+__device__ __forceinline__ uint32_t score_key(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+struct ChooseShared {
+  uint32_t histogram[2][256];
+  uint32_t count[2];                 // pages above the threshold, pages at it, of this CTA
+  uint32_t sum[2][kChooseWarps];
+  uint32_t found[2];                 // the passes' digit, and how many of its pages are still wanted
+};
+
+// Dynamic shared memory: q8 [heads, a multiple of 16][pitch], t [heads], keys of this CTA's pages.
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(const ChooseParams p) {
+  namespace cg = cooperative_groups;
+  constexpr int kSets = DP / 32;  // four 16-byte chunks each, of 2 D bytes
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ ChooseShared sh;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int unit = blockIdx.x / ctas, r = unit / p.H, h = unit - r * p.H;
+  const int tiles = (p.G + kChooseRows - 1) / kChooseRows, heads = tiles * kChooseRows;
+  float* const s_t = reinterpret_cast<float*>(smem + heads * p.pitch);
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  int s = p.sl[r];
+  const int64_t row = (int64_t)p.maxp * p.P;
+  if (s < 0 || s > row) {
+    if (tid == 0 && h == 0) raise_error(kErrTable);
+    s = s < 0 ? 0 : (int)row;
+  }
+  const int pages = s / p.P + (s % p.P != 0);
+  int32_t* const out = p.chosen + (int64_t)unit * p.budget;
+  const int listed = min(pages, p.budget);
+  for (int i = listed + rank * kChooseThreads + tid; i < p.budget; i += ctas * kChooseThreads) out[i] = -1;
+  if (pages <= p.budget) {  // all of them; every CTA of the cluster comes here
+    for (int i = rank * kChooseThreads + tid; i < pages; i += ctas * kChooseThreads) out[i] = i;
+    return;
+  }
+  const int lasts = min(p.lasts, p.budget), firsts = min(p.firsts, p.budget - lasts);
+  const int wanted = p.budget - lasts - firsts, end = pages - lasts;  // of the pages firsts .. end - 1
+  if (rank == 0) {
+    for (int i = tid; i < firsts; i += kChooseThreads) out[i] = i;
+    for (int i = tid; i < lasts; i += kChooseThreads) out[p.budget - lasts + i] = end + i;
+  }
+  if (wanted == 0) return;
+  // this CTA's pages
+  const int each = ((end - firsts + ctas - 1) / ctas + 7) / 8 * 8;
+  const int j0 = min(firsts + rank * each, end), n = min(each, end - j0);
+  const int32_t* bt_row = p.bt + (int64_t)r * p.maxp + j0;
+  uint32_t* const keys = p.keys != nullptr ? p.keys + (int64_t)unit * p.maxp + j0 : reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
+
+  // ---- the queries in 8 bits, negative part before positive part ------------------------------------
+  for (int g = warp; g < heads; g += kChooseWarps) {
+    uint8_t* to = smem + g * p.pitch;
+    const uint8_t* src = p.q + r * p.q_req + ((int64_t)h * p.G + g) * p.q_head;
+    float x[8], most = 0.f;
+    bool nan = false;
+    const bool mine = g < p.G && lane < p.D / 8;  // D is at most 256
+    if (mine) {
+      unpack8<BF16>(*reinterpret_cast<const uint4*>(src + lane * 16), x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        most = fmaxf(most, fabsf(x[i]));
+        nan |= x[i] != x[i];
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float t = __fmul_rn(most, k127th);
+    if (__any_sync(0xffffffffu, nan) || !(t > 0.f && t < INFINITY)) t = 0.f;
+    if (lane == 0) s_t[g] = t;
+    uint32_t neg[2] = {0, 0}, pos[2] = {0, 0};
+    if (mine && t > 0.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int v = (int)fminf(fmaxf(rintf(__fdiv_rn(x[i], t)), -127.f), 127.f);
+        neg[i / 4] |= (uint32_t)(min(v, 0) & 255) << (i % 4 * 8);
+        pos[i / 4] |= (uint32_t)(max(v, 0) & 255) << (i % 4 * 8);
+      }
+    }
+    if (lane < p.D / 8) {
+      *reinterpret_cast<uint2*>(to + lane * 8) = make_uint2(neg[0], neg[1]);
+      *reinterpret_cast<uint2*>(to + p.D + lane * 8) = make_uint2(pos[0], pos[1]);
+    }
+    for (int i = 2 * p.D + lane * 8; i < kSets * 64; i += 32 * 8) *reinterpret_cast<uint2*>(to + i) = make_uint2(0, 0);
+  }
+  for (int i = tid; i < 256; i += kChooseThreads) sh.histogram[0][i] = sh.histogram[1][i] = 0;
+  __syncthreads();
+
+  // ---- scores: a warp takes eight pages at a time ----------------------------------------------------
+  const int gr = lane >> 2, gc = lane & 3;
+  const int chunks = p.D / 8;  // of 16 bytes, of 2 D bytes
+  uint32_t qa[kSets][8];
+  auto queries = [&](int tile) {
+    const uint8_t* from = smem + (tile * kChooseRows + gr) * p.pitch + gc * 16;
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) {
+      const uint4 a = *reinterpret_cast<const uint4*>(from + k * 64), b = *reinterpret_cast<const uint4*>(from + 8 * p.pitch + k * 64);
+      qa[k][0] = a.x;
+      qa[k][1] = b.x;
+      qa[k][2] = a.y;
+      qa[k][3] = b.y;
+      qa[k][4] = a.z;
+      qa[k][5] = b.z;
+      qa[k][6] = a.w;
+      qa[k][7] = b.w;
+    }
+  };
+  queries(0);
+  auto page_of = [&](int i) { return i + gr < n ? bt_row[i + gr] : -1; };
+  int page = page_of(warp * 8);
+  for (int i = warp * 8; i < n; i += kChooseWarps * 8) {
+    const bool ok = page >= 0 && page < p.num_pages;
+    if (!ok && i + gr < n && gc == 0) raise_error(kErrTable);
+    const int64_t at = ((int64_t)(ok ? page : 0) * p.H + h);
+    const float step = ok ? p.steps[at] : 0.f;
+    const int8_t* from = p.bounds + at * 2 * p.D + gc * 16;
+    uint4 v[kSets];
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) {
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (ok && k * 4 + gc < chunks) v[k] = *reinterpret_cast<const uint4*>(from + k * 64);
+    }
+    page = page_of(i + kChooseWarps * 8);
+    float best[2] = {-INFINITY, -INFINITY};  // of pages 2 gc and 2 gc + 1
+    const float step2[2] = {__shfl_sync(0xffffffffu, step, gc * 8), __shfl_sync(0xffffffffu, step, gc * 8 + 4)};
+    for (int tile = 0; tile < tiles; ++tile) {
+      if (tiles > 1) queries(tile);
+      int c[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < kSets; ++k) {
+        mma16832(c, qa[k][0], qa[k][1], qa[k][2], qa[k][3], v[k].x, v[k].y);
+        mma16832(c, qa[k][4], qa[k][5], qa[k][6], qa[k][7], v[k].z, v[k].w);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int g = tile * kChooseRows + gr + (e >> 1) * 8;
+        // kept finite, so that a sum of 0 stays 0
+        if (g < p.G) best[e & 1] = fmaxf(best[e & 1], __fmul_rn((float)c[e], fminf(__fmul_rn(s_t[g], step2[e & 1]), FLT_MAX)));
+      }
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
+      best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
+    }
+    if (gr < 2) {
+      const int j = i + 2 * gc + gr;
+      const float st = gr ? step2[1] : step2[0];
+      if (j < n) {
+        const uint32_t key = st < INFINITY ? score_key(__fadd_rn(gr ? best[1] : best[0], 0.f)) : 0xffffffffu;
+        keys[j] = key;
+        atomicAdd(&sh.histogram[0][key >> 24], 1u);
+      }
+    }
+  }
+
+  // ---- the key of the last page that is taken, 8 bits a pass ---------------------------------------
+  uint32_t prefix = 0, need = (uint32_t)wanted;
+#pragma unroll 1
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass, b = pass & 1;
+    if (ctas > 1) cluster.sync(); else __syncthreads();
+    // the whole cluster's histogram, summed by a thread per bin, and how many pages lie above each bin
+    uint32_t mine = 0;
+    for (int k = 0; k < ctas; ++k) mine += (ctas > 1 ? cluster.map_shared_rank(sh.histogram[b], k) : sh.histogram[b])[255 - tid];
+    uint32_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    if (lane == 31) sh.sum[0][warp] = incl;
+    sh.histogram[b ^ 1][tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kChooseWarps; ++w)
+      if (w < warp) incl += sh.sum[0][w];
+    if (incl >= need && incl - mine < need) {  // exactly one thread
+      sh.found[0] = 255 - tid;
+      sh.found[1] = need - (incl - mine);
+    }
+    __syncthreads();
+    prefix |= sh.found[0] << shift;
+    need = sh.found[1];
+    if (pass < 3) {
+      for (int i = tid; i < n; i += kChooseThreads) {
+        const uint32_t key = keys[i];
+        if ((key ^ prefix) >> shift == 0) atomicAdd(&sh.histogram[b ^ 1][key >> (shift - 8) & 255], 1u);
+      }
+    }
+  }
+
+  // ---- the list: pages above that key, and the first `need` at it, in order of their columns ------------
+  const int per = (n + kChooseThreads - 1) / kChooseThreads;
+  const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
+  uint32_t mine[2] = {0, 0};
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t key = keys[i];
+    mine[0] += key > prefix;
+    mine[1] += key == prefix;
+  }
+  uint32_t incl[2] = {mine[0], mine[1]};
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl[k], o);
+      if (lane >= o) incl[k] += up;
+    }
+  if (lane == 31) {
+    sh.sum[0][warp] = incl[0];
+    sh.sum[1][warp] = incl[1];
+  }
+  __syncthreads();
+  uint32_t before[2] = {incl[0] - mine[0], incl[1] - mine[1]}, total[2] = {0, 0};
+#pragma unroll
+  for (int w = 0; w < kChooseWarps; ++w)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (w < warp) before[k] += sh.sum[k][w];
+      total[k] += sh.sum[k][w];
+    }
+  if (ctas > 1) {
+    if (tid < 2) sh.count[tid] = total[tid];
+    cluster.sync();
+    for (int k = 0; k < rank; ++k) {
+      const uint32_t* there = cluster.map_shared_rank(sh.count, k);
+      before[0] += there[0];
+      before[1] += there[1];
+    }
+    cluster.sync();  // nobody leaves while its counts are read
+  }
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t key = keys[i];
+    const bool above = key > prefix, at = key == prefix;
+    if (above || (at && before[1] < need)) out[firsts + before[0] + min(before[1], need)] = j0 + i;
+    before[0] += above;
+    before[1] += at;
+  }
+}
+
+}  // namespace topkv

@@ -69,7 +69,8 @@ struct AttendPlan {
   int64_t bytes;    // of the workspace
 };
 
-int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, AttendPlan* plan) {
+// `budget`: how many pages a request is attended to at most, 0 = all.
+int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, AttendPlan* plan, uint32_t budget = 0) {
   Resolved rs;
   int st = check_layout(lo, &rs);
   if (st != TOPKV_OK) return st;
@@ -125,6 +126,7 @@ int check_attention(const topkv_layout* lo, const topkv_batch* b, const topkv_at
   if (plan->units > 65535) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   int64_t most = (int64_t)b->max_pages_per_req * lo->page_tokens;
   if (most > 0x7ffff000ll) return TOPKV_ERR_INVALID_ARG;  // token numbers a few tiles further still fit an int
+  if (budget > 0) most = std::min(most, (int64_t)budget * lo->page_tokens);
   if (b->window_tokens > 0) most = std::min(most, (int64_t)b->window_tokens + at->sink_tokens);
   if (b->total_tokens >= 0) most = std::min(most, b->total_tokens);
   const int64_t tiles = (most + kTileTokens - 1) / kTileTokens;
@@ -302,6 +304,30 @@ AttendParams attend_params(int layer, const void* pool, const topkv_layout* layo
   return p;
 }
 
+// The attention and, if a request can be cut, the kernel that joins its parts.
+template <int MODE>
+int attend_and_join(AttendParams p, const AttendPlan& plan, bool latent, uint32_t type, void* d_workspace, cudaStream_t s) {
+  if (!plan.uncut) {
+    uint8_t* w = static_cast<uint8_t*>(d_workspace);
+    const int64_t slots = 2ll * plan.teams * plan.units * plan.rows;
+    p.joins = reinterpret_cast<int4*>(w);
+    p.by_request = plan.joins == p.R;
+    w += (int64_t)plan.joins * 16;
+    p.ml = reinterpret_cast<float2*>(w);
+    p.part = reinterpret_cast<float*>(w + slots * 8);
+  }
+  int st;
+  if (latent)
+    st = p.io_bf16 ? launch_latent<true>(p, plan.units, s) : launch_latent<false>(p, plan.units, s);
+  else
+    st = launch_attend_type<MODE>(p, type, plan.units, s);
+  if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
+  // about eight CTAs per SM for the requests that can be cut
+  const int64_t cuts = (int64_t)plan.joins * plan.units;
+  const unsigned z = (unsigned)std::max((plan.rows + kJoinRows - 1) / kJoinRows, (int)std::min<int64_t>(plan.rows, 8 * 148 / cuts));
+  return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.joins, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
+}
+
 // ---- page operators -------------------------------------------------------------------------------
 int check_pages(const topkv_layout* lo, const topkv_batch* b, Resolved* rs) {
   int st = check_layout(lo, rs);
@@ -427,26 +453,8 @@ int topkv_attend_layer(int layer, const void* pool, const topkv_layout* layout, 
   st = check_attend_pointers(layer, layout, pool, d_q, d_out, d_workspace, workspace_bytes, plan.bytes);
   if (st != TOPKV_OK) return st;
   if (batch->num_requests == 0) return TOPKV_OK;
-  AttendParams p = attend_params(layer, pool, layout, batch, attention, plan, d_q, d_out);
-  if (!plan.uncut) {
-    uint8_t* w = static_cast<uint8_t*>(d_workspace);
-    const int64_t slots = 2ll * plan.teams * plan.units * plan.rows;
-    p.joins = reinterpret_cast<int4*>(w);
-    p.by_request = plan.joins == p.R;
-    w += (int64_t)plan.joins * 16;
-    p.ml = reinterpret_cast<float2*>(w);
-    p.part = reinterpret_cast<float*>(w + slots * 8);
-  }
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (layout->kv_factor == 1)
-    st = p.io_bf16 ? launch_latent<true>(p, plan.units, s) : launch_latent<false>(p, plan.units, s);
-  else
-    st = launch_attend_type<kAllTokens>(p, attention->cache_type, plan.units, s);
-  if (st != TOPKV_OK || plan.uncut || plan.teams < 2) return st;
-  // about eight CTAs per SM for the requests that can be cut
-  const int64_t cuts = (int64_t)plan.joins * plan.units;
-  const unsigned z = (unsigned)std::max((plan.rows + kJoinRows - 1) / kJoinRows, (int)std::min<int64_t>(plan.rows, 8 * 148 / cuts));
-  return launched(launch_pdl(topkv_attend_join_kernel, dim3(plan.joins, plan.units, z), dim3(kJoinThreads), 0, s, p), 1);
+  const AttendParams p = attend_params(layer, pool, layout, batch, attention, plan, d_q, d_out);
+  return attend_and_join<kAllTokens>(p, plan, layout->kv_factor == 1, attention->cache_type, d_workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int64_t topkv_page_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch, int32_t num_forks) {

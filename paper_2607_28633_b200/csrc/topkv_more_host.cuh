@@ -3,6 +3,7 @@
 // and launches it shares.
 #pragma once
 #include "topkv_append.cuh"
+#include "topkv_choose.cuh"
 #include "topkv_prefix.cuh"
 
 namespace {
@@ -109,9 +110,185 @@ int launch_prefix_dim(const PrefixParams& p, cudaStream_t s) {
   return launch_prefix<256, TYPE>(p, s);
 }
 
+// ---- chosen pages -----------------------------------------------------------------------------------
+constexpr uint32_t kChooseMaxHeads = 128;     // query heads per KV head: they are held in shared memory
+constexpr int64_t kChooseMaxKeys = 24 * 1024;  // pages of a CTA whose keys are
+struct ChoosePlan {
+  AttendPlan attend;
+  int ctas;          // of a cluster
+  int64_t cap;       // pages of a CTA at most
+  int64_t key_bytes; // of the workspace, where shared memory does not hold the keys
+  int pitch, smem;
+};
+int choose_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+int check_choice(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, const topkv_page_choice* c, ChoosePlan* plan) {
+  if (c == nullptr || c->struct_size != sizeof(topkv_page_choice)) return TOPKV_ERR_INVALID_ARG;
+  if (c->budget == 0 || c->budget > 0x7fffffffu || c->last_pages == 0 || c->first_pages > 0x7fffffffu || c->last_pages > 0x7fffffffu)
+    return TOPKV_ERR_INVALID_ARG;
+  const int st = check_attention(lo, b, at, &plan->attend, c->budget);
+  if (st != TOPKV_OK) return st;
+  if (lo->kv_factor != 2) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (b->window_tokens != 0 || at->sink_tokens != 0 || !(at->k_scale > 0.f)) return TOPKV_ERR_INVALID_ARG;
+  const uint32_t G = at->num_q_heads / lo->num_kv_heads;
+  if (G > kChooseMaxHeads) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  const int64_t units = (int64_t)b->num_requests * lo->num_kv_heads;
+  if (units * kChooseCluster > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (!mult16p(c->bounds) || !mult4p(c->steps) || !mult4p(c->chosen)) return TOPKV_ERR_ALIGNMENT;
+  // Two CTAs per SM are wanted, but none with fewer than 256 pages.
+  plan->ctas = 1;
+  while (plan->ctas < kChooseCluster && units * plan->ctas < 2 * 148 && b->max_pages_per_req / plan->ctas > 256) plan->ctas *= 2;
+  plan->cap = (b->max_pages_per_req + plan->ctas - 1) / plan->ctas + 8;
+  const bool inside = plan->cap <= kChooseMaxKeys;
+  plan->key_bytes = inside ? 0 : units * b->max_pages_per_req * 4;
+  plan->pitch = choose_columns((int)lo->head_dim) * 2 + 16;
+  const int heads = (int)(G + kChooseRows - 1) / kChooseRows * kChooseRows;
+  plan->smem = heads * (plan->pitch + 4) + (inside ? (int)plan->cap * 4 : 0);
+  return TOPKV_OK;
+}
+
+template <int DP, bool BF16>
+int launch_choose2(const ChooseParams& p, const ChoosePlan& plan, int64_t units, cudaStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  constexpr int kMost = (int)kChooseMaxHeads * (DP * 2 + 20) + (int)kChooseMaxKeys * 4;
+  static_assert(kMost + (int)sizeof(ChooseShared) <= kSmemBudget, "queries and keys fit a CTA");
+  const int st = raise_smem(topkv_choose_pages_kernel<DP, BF16>, kMost, &done);
+  if (st != TOPKV_OK) return st;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * plan.ctas));
+  cfg.blockDim = dim3(kChooseThreads);
+  cfg.dynamicSmemBytes = (size_t)plan.smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)plan.ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return launched(cudaLaunchKernelEx(&cfg, topkv_choose_pages_kernel<DP, BF16>, p), 1);
+}
+template <int DP>
+int launch_choose(const ChooseParams& p, const ChoosePlan& plan, int64_t units, bool bf16, cudaStream_t s) {
+  return bf16 ? launch_choose2<DP, true>(p, plan, units, s) : launch_choose2<DP, false>(p, plan, units, s);
+}
+
+int check_choice_workspace(const void* ws, int64_t bytes, int64_t needed) {
+  if (needed == 0) return TOPKV_OK;
+  if (ws == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult16p(ws)) return TOPKV_ERR_ALIGNMENT;
+  return bytes < needed ? TOPKV_ERR_CAPACITY : TOPKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int topkv_bound_pages_layer(int layer, const void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                            uint32_t cache_type, int8_t* d_bounds, float* d_steps, topkv_stream_t stream) {
+  Resolved rs;
+  int st = check_layout(layout, &rs);
+  if (st == TOPKV_OK) st = check_tables_batch(layout, batch);
+  if (st != TOPKV_OK) return st;
+  if (cache_type < TOPKV_TYPE_BF16 || cache_type > TOPKV_TYPE_E4M3) return TOPKV_ERR_INVALID_ARG;
+  const bool narrow = cache_type == TOPKV_TYPE_E4M3;
+  if (layout->kv_factor != 2 || layout->elem_bytes != (narrow ? 1u : 2u) || layout->head_dim > 256 ||
+      !mult16((int64_t)layout->head_dim * layout->elem_bytes))
+    return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  if (layer < 0 || (uint32_t)layer >= layout->num_layers) return TOPKV_ERR_LAYER_RANGE;
+  if (layout->num_kv_heads > 1 && !mult16(layout->pool_head_stride)) return TOPKV_ERR_ALIGNMENT;
+  if (pool == nullptr || d_bounds == nullptr || d_steps == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult16p(pool) || !mult16p(d_bounds) || !mult4p(d_steps)) return TOPKV_ERR_ALIGNMENT;
+  if (batch->num_requests == 0 || batch->max_pages_per_req == 0) return TOPKV_OK;
+  BoundParams p = {};
+  p.pool = static_cast<const uint8_t*>(pool) + (int64_t)layer * layout->pool_layer_stride;
+  p.bt = batch->block_table;
+  p.sl = batch->seq_lens;
+  p.bounds = d_bounds;
+  p.steps = d_steps;
+  p.S_page = layout->pool_page_stride;
+  p.S_tok = layout->page_tokens > 1 ? layout->pool_token_stride : 0;
+  p.S_head = layout->num_kv_heads > 1 ? layout->pool_head_stride : 0;
+  p.num_pages = layout->num_pool_pages;
+  p.maxp = batch->max_pages_per_req;
+  p.P = (int)layout->page_tokens;
+  p.H = (int)layout->num_kv_heads;
+  p.D = (int)layout->head_dim;
+  p.window = batch->window_tokens;
+  p.columns = p.maxp;
+  if (p.window > 0) p.columns = (int)std::min<int64_t>(p.maxp, ((int64_t)p.window + p.P - 2) / p.P + 1);
+  p.items = (int64_t)batch->num_requests * p.columns * p.H;
+  const int64_t ctas = (p.items + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
+  if (ctas > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)ctas), block(kBoundThreads);
+  return launched(cache_type == TOPKV_TYPE_BF16   ? launch_pdl(topkv_bound_pages_kernel<kBf16>, grid, block, 0, s, p)
+                  : cache_type == TOPKV_TYPE_FP16 ? launch_pdl(topkv_bound_pages_kernel<kFp16>, grid, block, 0, s, p)
+                                                  : launch_pdl(topkv_bound_pages_kernel<kE4m3>, grid, block, 0, s, p), 1);
+}
+
+int64_t topkv_page_choice_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
+                                          const topkv_attention* attention, const topkv_page_choice* choice) {
+  ChoosePlan plan;
+  const int st = check_choice(layout, batch, attention, choice, &plan);
+  return st != TOPKV_OK ? st : std::max(plan.attend.bytes, (plan.key_bytes + 255) / 256 * 256);
+}
+
+int topkv_choose_pages_layer(const topkv_layout* layout, const topkv_batch* batch, const topkv_attention* attention,
+                             const topkv_page_choice* choice, const void* d_q, void* d_workspace, int64_t workspace_bytes,
+                             topkv_stream_t stream) {
+  ChoosePlan plan;
+  int st = check_choice(layout, batch, attention, choice, &plan);
+  if (st != TOPKV_OK) return st;
+  if (d_q == nullptr || choice->bounds == nullptr || choice->steps == nullptr || choice->chosen == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (!mult16p(d_q)) return TOPKV_ERR_ALIGNMENT;
+  st = check_choice_workspace(d_workspace, workspace_bytes, plan.key_bytes);
+  if (st != TOPKV_OK) return st;
+  if (batch->num_requests == 0) return TOPKV_OK;
+  ChooseParams p = {};
+  p.bt = batch->block_table;
+  p.sl = batch->seq_lens;
+  p.q = static_cast<const uint8_t*>(d_q);
+  p.bounds = choice->bounds;
+  p.steps = choice->steps;
+  p.chosen = choice->chosen;
+  p.keys = plan.key_bytes > 0 ? static_cast<uint32_t*>(d_workspace) : nullptr;
+  p.q_req = attention->q_request_stride;
+  p.q_head = attention->q_head_stride;
+  p.num_pages = layout->num_pool_pages;
+  p.maxp = batch->max_pages_per_req;
+  p.P = (int)layout->page_tokens;
+  p.H = (int)layout->num_kv_heads;
+  p.G = (int)(attention->num_q_heads / layout->num_kv_heads);
+  p.D = (int)layout->head_dim;
+  p.budget = (int)choice->budget;
+  p.firsts = (int)choice->first_pages;
+  p.lasts = (int)choice->last_pages;
+  p.pitch = plan.pitch;
+  const int64_t units = (int64_t)batch->num_requests * p.H;
+  const bool bf16 = attention->io_type == TOPKV_TYPE_BF16;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (p.D <= 64) return launch_choose<64>(p, plan, units, bf16, s);
+  if (p.D <= 128) return launch_choose<128>(p, plan, units, bf16, s);
+  return launch_choose<256>(p, plan, units, bf16, s);
+}
+
+int topkv_attend_pages_layer(int layer, const void* pool, const topkv_layout* layout, const topkv_batch* batch,
+                             const topkv_attention* attention, const topkv_page_choice* choice, const void* d_q, void* d_out,
+                             void* d_workspace, int64_t workspace_bytes, topkv_stream_t stream) {
+  ChoosePlan plan;
+  int st = check_choice(layout, batch, attention, choice, &plan);
+  if (st != TOPKV_OK) return st;
+  st = check_attend_pointers(layer, layout, pool, d_q, d_out, d_workspace, workspace_bytes, plan.attend.bytes);
+  if (st != TOPKV_OK) return st;
+  if (choice->chosen == nullptr) return TOPKV_ERR_INVALID_ARG;
+  if (batch->num_requests == 0) return TOPKV_OK;
+  AttendParams p = attend_params(layer, pool, layout, batch, attention, plan.attend, d_q, d_out);
+  p.chosen = choice->chosen;
+  p.budget = (int)choice->budget;
+  return attend_and_join<kChosenPages>(p, plan.attend, false, attention->cache_type, d_workspace, reinterpret_cast<cudaStream_t>(stream));
+}
 
 int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, int32_t min_tokens, int32_t* d_plan,
                         topkv_stream_t stream) {
