@@ -206,7 +206,7 @@ template <int DP, bool BF16>
 __global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(const ChooseParams p) {
   namespace cg = cooperative_groups;
   constexpr int kSets = DP / 32;  // four 16-byte chunks each, of 2 D bytes
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem[];
   __shared__ ChooseShared sh;
   cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();

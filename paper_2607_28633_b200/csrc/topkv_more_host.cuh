@@ -95,13 +95,37 @@ int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   return TOPKV_OK;
 }
 
+// Tensor map of a layer's keys and values, [page][plane][head][token][column], for boxes of p->box tokens x 64
+// columns in the swizzled order of the operands; box 0 where there is none: pieces of 8 to `tokens` tokens that
+// never straddle a page need page sizes that are multiples of 8, 8-bit values are converted on the way.
+CUtensorMap prefix_map(AttendParams* p, uint32_t type, int tokens) {
+  CUtensorMap map = {};
+  p->box = 0;
+  const int box = std::min(tokens, p->P & -p->P);
+  const int64_t head = p->H > 1 ? p->S_head : 16;
+  if (type == TOPKV_TYPE_E4M3 || box < 8 || p->D < 64 || p->num_pages > 0x7ffffff0ll) return map;
+  for (const int64_t s : {p->S_page, p->S_kv, p->S_tok, head})
+    if (s <= 0 || s >= (1ll << 40)) return map;
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return map;
+  const cuuint64_t dims[5] = {(cuuint64_t)p->D, (cuuint64_t)p->P, (cuuint64_t)p->H, 2, (cuuint64_t)p->num_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)p->S_tok, (cuuint64_t)head, (cuuint64_t)p->S_kv, (cuuint64_t)p->S_page};
+  const cuuint32_t sizes[5] = {64, (cuuint32_t)box, 1, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
+  const CUresult r = encode(&map, type == TOPKV_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+                            const_cast<uint8_t*>(p->pool), dims, strides, sizes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) p->box = box;
+  return map;
+}
+
 template <int DP, int TYPE>
-int launch_prefix(const PrefixParams& p, cudaStream_t s) {
+int launch_prefix(PrefixParams p, cudaStream_t s) {
   using S = PrefixShape<DP, TYPE>;
   static std::atomic<uint64_t> done{0};
   const int st = raise_smem(topkv_prefix_kernel<DP, TYPE>, S::kSmem, &done);
   if (st != TOPKV_OK) return st;
-  return launched(launch_pdl(topkv_prefix_kernel<DP, TYPE>, dim3(kPrefixCtas), dim3(S::kThreads), S::kSmem, s, p), 1);
+  const CUtensorMap map = prefix_map(&p.a, TYPE, S::kTokens);
+  return launched(launch_pdl(topkv_prefix_kernel<DP, TYPE>, dim3(kPrefixCtas), dim3(S::kThreads), S::kSmem, s, p, map), 1);
 }
 template <int TYPE>
 int launch_prefix_dim(const PrefixParams& p, cudaStream_t s) {

@@ -16,8 +16,9 @@
 // other: with more than 128 rows they are two tiles of rows over the same tokens, else the same rows over every
 // other tile of tokens. (256 columns: one accumulator, two buffers of scores, 64 tokens a tile.) Roles:
 //   warps 0-7    softmax: four per accumulator, one thread a row; also Q and the result
-//   warps 8-11   load K and V through the block table into a ring (16-byte copies; 8-bit values become fp16)
-//   warp 12      one thread issues the products
+//   warps 8, 9   load K and V through the block table into a ring: tensor copies of page pieces, or 16-byte
+//                copies (any page size and stride); 8-bit values become fp16 on the way
+//   warp 10      one thread issues the products
 // The (group, KV head, 256 rows) units laid end to end, as long as their tiles, are cut into equal ranges, one
 // per CTA; each leaves its part in 32 bits in the workspace, and the joining kernel adds them to those of the
 // tokens behind the prefix, in order, so that results do not depend on timing.
@@ -26,6 +27,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "topkv_attend.cuh"
 #include "topkv_common.cuh"
@@ -136,7 +138,7 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(c
 
 // ---- the shared tokens' part ------------------------------------------------------------------------
 constexpr int kPrefixRows = 128;    // rows of a tile
-constexpr int kPrefixLoadWarps = 4;
+constexpr int kPrefixLoadWarps = 2;
 constexpr int kPrefixMaxStages = 8;
 constexpr int kPrefixCtas = 148;    // at most
 
@@ -238,6 +240,40 @@ __device__ __forceinline__ int next_group(const PrefixParams& p, int r, int lane
   return p.a.R;
 }
 
+// Two products and sums at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z; mov.b64 {%0, %1}, x; }"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// What has been loaded is used only behind this, by name.
+__device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
+                 "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
+                 "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+// Arrives at the barrier once this thread's copies so far are there.
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load5(uint32_t dst, const CUtensorMap* map, int x, int token, int head, int plane, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(token), "r"(head), "r"(plane), "r"(page), "r"(bar)
+      : "memory");
+}
+
 __device__ __forceinline__ void tcgen05_mma_ta(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool accumulate) {
   asm volatile(
       "{ .reg .pred p; .reg .b64 db; mov.b64 db, {%2, %3}; setp.ne.u32 p, %5, 0;\n\t"
@@ -247,7 +283,7 @@ __device__ __forceinline__ void tcgen05_mma_ta(uint32_t d, uint32_t a, uint32_t 
 }
 
 template <int DP, int TYPE>
-__global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_prefix_kernel(const PrefixParams p) {
+__global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_prefix_kernel(const PrefixParams p, const __grid_constant__ CUtensorMap map) {
   using S = PrefixShape<DP, TYPE>;
   constexpr bool kBf = TYPE == kBf16;
   constexpr float kShift = kBf ? 0.f : 7.f;
@@ -384,28 +420,68 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
 
     if (warp >= kLoadWarp && warp < kIssueWarp) {
       // ---- load ---------------------------------------------------------------------------------------
-      constexpr int kRows = kTokens / kPrefixLoadWarps;  // rows of this warp
       const int w = warp - kLoadWarp;
       const uint8_t* head = a.pool + (int64_t)h * a.S_head;
-      auto page_of = [&](int t) {
-        const int x = t * kTokens + w * kRows + lane;
-        return t < t1 && lane < kRows && x < g.tokens ? bt_row[page_column(x)] : -1;
+      constexpr int kRows = kTokens / kPrefixLoadWarps, kGroups = kRows / 32;  // rows of this warp
+      static_assert(kRows % 32 == 0, "a lane per row");
+      const int chunks = a.D / 8, padded = ksteps * 2, full = chunks / 8;
+      // Whole page pieces come by tensor copies, those outside the pool and behind the prefix as zeros from
+      // outside the tensor. A prefix that ends inside a piece has its last tile copied row by row.
+      const int box = a.box, boxes = box > 0 ? kTokens / box : 0;
+      auto piece = [&](int t) {  // page of piece `lane` of a tile
+        const int x = t * kTokens + lane * box;
+        return t < t1 && lane < boxes && x < g.tokens ? bt_row[page_column(x)] : -1;
       };
-      int pg = page_of(t0);
+      int pg = boxes > 0 ? piece(t0) : -1;
       for (int t = t0; t < t1; ++t) {
         if (__any_sync(0xffffffffu, s_dead)) break;
-        int64_t o = -1;
-        const int x = t * kTokens + w * kRows + lane;
-        if (lane < kRows && x < g.tokens) {
-          if (pg < 0 || pg >= a.num_pages)
+        if (TYPE != kE4m3 && boxes > 0 && (g.tokens >= (t + 1) * kTokens || g.tokens % box == 0)) {
+          const int x = t * kTokens + lane * box;
+          bool ok = lane < boxes && x < g.tokens;
+          if (ok && (pg < 0 || pg >= a.num_pages)) {
             raise_error(kErrTable);
-          else
-            o = (int64_t)pg * a.S_page + (int64_t)(x - page_column(x) * a.P) * a.S_tok;
-        }
-        pg = page_of(t + 1);
+            ok = false;
+          }
+          const int z = ok ? pg : (int)a.num_pages, y = ok ? x - page_column(x) * a.P : 0;
+          pg = piece(t + 1);
 #pragma unroll 1
-        for (int plane = 0; plane < 2; ++plane) {
-          const uint32_t entry = issued, stage = entry % kStages;
+          for (int plane = 0; plane < 2; ++plane, ++issued) {
+            const uint32_t stage = issued % kStages, bar = b_full + 8 * stage;
+            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
+            const uint32_t dst = base + kTiles * S::kQ + stage * S::kStage;
+            const int blocks = (a.D + 63) / 64;
+            if (lane == 0)
+              mbar_expect_tx(bar, (uint32_t)((boxes + 1 - w) / 2 * blocks * box * 128));
+            else
+              bar_arrive(bar);
+            __syncwarp();
+            for (int e = w; e < boxes; e += kPrefixLoadWarps) {
+              const int ze = __shfl_sync(0xffffffffu, z, e), ye = __shfl_sync(0xffffffffu, y, e);
+              if (elect_one()) {
+                for (int b = 0; b < blocks; ++b) tma_load5(dst + b * kBlock + e * box * 128, &map, b * 64, ye, h, plane, ze, bar);
+              }
+              __syncwarp();
+            }
+          }
+          continue;
+        }
+        if (boxes > 0) pg = piece(t + 1);
+        int64_t o[kGroups];
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+          const int x = t * kTokens + w * kRows + k * 32 + lane;
+          o[k] = -1;
+          if (x < g.tokens) {
+            const int j = page_column(x), page = bt_row[j];
+            if (page < 0 || page >= a.num_pages)
+              raise_error(kErrTable);
+            else
+              o[k] = (int64_t)page * a.S_page + (int64_t)(x - j * a.P) * a.S_tok;
+          }
+        }
+#pragma unroll 1
+        for (int plane = 0; plane < 2; ++plane, ++issued) {
+          const uint32_t stage = issued % kStages;
           const uint32_t dst = base + kTiles * S::kQ + stage * S::kStage + w * kRows * 128;
           const uint8_t* src0 = head + plane * a.S_kv;
           if constexpr (TYPE == kE4m3) {
@@ -414,11 +490,11 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             uint4 v[kCopies];
 #pragma unroll
             for (int k = 0; k < kCopies; ++k) {
-              const int64_t ro = __shfl_sync(0xffffffffu, o, k * kPer + sub);
+              const int64_t ro = __shfl_sync(0xffffffffu, o[k * kPer / 32], (k * kPer + sub) & 31);
               v[k] = make_uint4(0, 0, 0, 0);
               if (ro >= 0 && c * 16 < a.D) v[k] = *reinterpret_cast<const uint4*>(src0 + ro + c * 16);
             }
-            if (entry >= kStages) wait(b_free + 8 * stage, entry / kStages - 1);
+            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
             if (c * 16 < a.D) {
 #pragma unroll
               for (int k = 0; k < kCopies; ++k) {
@@ -434,35 +510,29 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 *reinterpret_cast<uint4*>(to + (((ch + 1) ^ (row & 7)) << 4)) = make_uint4(x8[4], x8[5], x8[6], x8[7]);
               }
             }
-            proxy_fence_smem();
             bar_arrive(b_full + 8 * stage);
           } else {
-            if (entry >= kStages) wait(b_free + 8 * stage, entry / kStages - 1);
-            const int chunks = a.D / 8, padded = ksteps * 2, full = chunks / 8;
+            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
             const int c = lane & 7, sub = lane >> 3;
-#pragma unroll 2
-            for (int rg = 0; rg < kRows / 4; ++rg) {
-              const int row = rg * 4 + sub;
-              const int64_t ro = __shfl_sync(0xffffffffu, o, row);
-              const uint8_t* src = (ro < 0 ? a.pool : src0 + ro) + c * 16;
-              uint32_t to = dst + row * 128 + ((c ^ (row & 7)) << 4);
 #pragma unroll
-              for (int b = 0; b < DP / 64; ++b, to += kBlock) {
-                if (b < full)
-                  cp_async16(to, ro < 0 ? a.pool : src + b * 128, ro >= 0);
-                else if (b * 8 + c < padded)
-                  cp_async16(to, ro >= 0 && b * 8 + c < chunks ? src + b * 128 : a.pool, ro >= 0 && b * 8 + c < chunks);
+            for (int k = 0; k < kGroups; ++k) {
+#pragma unroll 2
+              for (int rg = 0; rg < 8; ++rg) {
+                const int row = rg * 4 + sub;
+                const int64_t ro = __shfl_sync(0xffffffffu, o[k], row);
+                const uint8_t* src = (ro < 0 ? a.pool : src0 + ro) + c * 16;
+                uint32_t to = dst + (k * 32 + row) * 128 + ((c ^ (row & 7)) << 4);
+#pragma unroll
+                for (int b = 0; b < DP / 64; ++b, to += kBlock) {
+                  if (b < full)
+                    cp_async16(to, ro < 0 ? a.pool : src + b * 128, ro >= 0);
+                  else if (b * 8 + c < padded)
+                    cp_async16(to, ro >= 0 && b * 8 + c < chunks ? src + b * 128 : a.pool, ro >= 0 && b * 8 + c < chunks);
+                }
               }
             }
-            cp_async_commit();
-            // the entry before has arrived, now that this one is under way
-            if (entry > 0) {
-              cp_async_wait<1>();
-              proxy_fence_smem();
-              bar_arrive(b_full + 8 * ((entry - 1) % kStages));
-            }
+            cp_async_arrive(b_full + 8 * stage);
           }
-          ++issued;
         }
       }
     } else if (warp == kIssueWarp) {
@@ -477,6 +547,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           const uint32_t entry = 2 * (seq + t) + 1, stage = entry % kStages;
           wait(b_weight + 8 * b, done[b] + (jj >> 1));
           wait(b_full + 8 * stage, entry / kStages);
+          proxy_fence_smem();  // what threads wrote and the barrier has shown, before the products read it
           tcgen05_after_sync();
           const uint32_t d = tmem + S::kSums + (kTiles == 2 ? b * DP : 0), w = tmem + b * kTokens, v0 = v00 + stage * (S::kStage >> 4);
           if (elect_one()) {
@@ -492,11 +563,13 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           const int b = j & 1, t = u.both ? j >> 1 : j;
           const uint32_t entry = 2 * (seq + t), stage = entry % kStages;
           wait(b_full + 8 * stage, entry / kStages);
+          proxy_fence_smem();
           tcgen05_after_sync();
           const uint32_t d = tmem + b * kTokens, k0 = kv0 + stage * (S::kStage >> 4), qa = q0 + (u.both ? b * (S::kQ >> 4) : 0);
           if (elect_one()) {
-            for (int k = 0; k < ksteps; ++k)
-              tcgen05_mma(d, qa + (k >> 2) * (kQBlock >> 4) + 2 * (k & 3), k0 + (k >> 2) * (kBlock >> 4) + 2 * (k & 3), kOperandHi, kScore, k > 0);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+              if (k < ksteps) tcgen05_mma(d, qa + (k >> 2) * (kQBlock >> 4) + 2 * (k & 3), k0 + (k >> 2) * (kBlock >> 4) + 2 * (k & 3), kOperandHi, kScore, k > 0);
             tcgen05_commit(b_score + 8 * b);
             if (!u.both || b == 1) tcgen05_commit(b_free + 8 * stage);
           }
@@ -539,7 +612,8 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             rest = exp2f((float)(-(e - e / 2)));
             row_scale = a.qk_scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
           }
-          ctl.row_scale[my_row] = row_scale;
+          ctl.row_scale[my_row] = fabsf(row_scale);
+          const uint32_t flip = row_scale < 0.f ? 0x80008000u : 0u;  // scores times a factor that is not negative
           for (int c = 0; c < padded; ++c) {
             uint4 v = live && c < chunks ? *reinterpret_cast<const uint4*>(src + c * 16) : make_uint4(0, 0, 0, 0);
             if (TYPE == kE4m3 && a.io_bf16) {
@@ -549,6 +623,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 x[e] = pack2<false>(__uint_as_float(x[e] << 16) * up * rest, __uint_as_float(x[e] & 0xffff0000u) * up * rest);
               v = make_uint4(x[0], x[1], x[2], x[3]);
             }
+            v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
             *reinterpret_cast<uint4*>(smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
           }
           proxy_fence_smem();
@@ -567,7 +642,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       }
       odd = __any_sync(0xffffffffu, odd);
       const bool some = __any_sync(0xffffffffu, live);  // a row of this warp counts
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, sub = 0.f;  // sub: what is subtracted from a score
       bool seen = false;
       int last = -1;  // this accumulator's last job
       for (int j = kTiles == 2 ? acc : 0; j < jobs; j += kTiles) {
@@ -597,27 +672,56 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             }
           }
           const bool partial = odd || visible < kTokens;
-          float top = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < kTokens / 32; ++c) {
-            uint32_t raw[32];
-            tmem_load<32>(raw, s_col + c * 32);
-            tmem_wait_load();
-            seen |= valid[c] != 0;
-            if (partial) {
+          for (int c = 0; c < kTokens / 32; ++c) seen |= valid[c] != 0;
+          // One pass as a rule: weights from the maximum so far, which stay in registers while the tile's own
+          // maximum is looked at; only if that exceeds it by more than 2^kLazy, or there is none yet, a second.
+          uint32_t w[kTokens / 2];
+          float2 sum;
+          float top;
+          auto pass = [&](auto exps, auto masked) {
+            constexpr bool kExps = decltype(exps)::value, kMasked = decltype(masked)::value;
+            const float2 by = make_float2(row_scale, row_scale), less = make_float2(-sub, -sub);
+            top = -INFINITY;
+            float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            uint32_t raw[2][32];
+            tmem_load<32>(raw[0], s_col);
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (valid[c] >> e & 1) top = fmaxf(top, __uint_as_float(raw[e]) * row_scale);
-            } else {
+            for (int c = 0; c < kTokens / 32; ++c) {
+              uint32_t(&x)[32] = raw[c & 1];
+              tmem_loaded(x);
+              if (c + 1 < kTokens / 32) tmem_load<32>(raw[(c + 1) & 1], s_col + (c + 1) * 32);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(raw[e]) * row_scale);
+              for (int k = 0; k < 32; k += 2) {
+                float2 s = make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                const bool v0 = !kMasked || (valid[c] >> k & 1), v1 = !kMasked || (valid[c] >> (k + 1) & 1);
+                top = fmaxf(top, fmaxf(v0 ? s.x : -INFINITY, v1 ? s.y : -INFINITY));
+                if constexpr (kExps) {
+                  s = fma2(s, by, less);
+                  s.x = v0 ? exp2_approx(s.x) : 0.f;
+                  s.y = v1 ? exp2_approx(s.y) : 0.f;
+                  part[k / 2 & 1] = add2(part[k / 2 & 1], s);
+                  w[c * 16 + k / 2] = pack2<kBf>(s.x, s.y);
+                }
+              }
             }
+            top = top == -INFINITY ? top : top * row_scale;
+            sum = add2(part[0], part[1]);
+          };
+          auto exps = [&] {
+            if (partial) pass(std::true_type{}, std::true_type{}); else pass(std::true_type{}, std::false_type{});
+          };
+          if (j < kTiles) {
+            if (partial) pass(std::false_type{}, std::true_type{}); else pass(std::false_type{}, std::false_type{});
+          } else {
+            exps();
           }
-          if (__any_sync(0xffffffffu, top > m + kLazy)) {
+          if (__any_sync(0xffffffffu, top > m + kLazy) || j < kTiles) {
             float alpha = 1.f;
             if (top > m) {
               alpha = exp2_approx(m - top);
               m = top;
+              sub = m - kShift;
             }
             l *= alpha;
             if (j >= kTiles) {
@@ -631,34 +735,18 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 if (c * 32 >= a.D) break;
                 uint32_t o[32];
                 tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
-                tmem_wait_load();
+                tmem_loaded(o);
 #pragma unroll
                 for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
                 tmem_store<32>(tmem + lanes + S::kSums + acc * DP + c * 32, o);
               }
             }
+            exps();
           }
-          const float sub = m == -INFINITY ? 0.f : m - kShift;
+          l += sum.x + sum.y;
 #pragma unroll
-          for (int c = 0; c < kTokens / 32; ++c) {
-            uint32_t raw[32], w[16];
-            tmem_load<32>(raw, s_col + c * 32);
-            tmem_wait_load();
-            float e[32];
-#pragma unroll
-            for (int k = 0; k < 32; ++k) e[k] = exp2_approx(fmaf(__uint_as_float(raw[k]), row_scale, -sub));
-            if (partial) {
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (!(valid[c] >> k & 1)) e[k] = 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              l += e[k] + e[k + 1];
-              w[k / 2] = pack2<kBf>(e[k], e[k + 1]);
-            }
-            tmem_store<16>(s_col + c * 16, w);  // over scores that have been read
-          }
+          for (int c = 0; c < kTokens / 64; ++c)  // over the scores, which have been read
+            tmem_store<32>(s_col + c * 32, *reinterpret_cast<const uint32_t(*)[32]>(&w[c * 32]));
           tmem_wait_store();
         }
         tcgen05_before_sync();
@@ -678,7 +766,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           if (c * 32 >= a.D) break;
           uint32_t o[32];
           tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
-          tmem_wait_load();
+          tmem_loaded(o);
           if (live) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
@@ -702,13 +790,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (lead < a.R) g = prefix_group(p, lead);
     }
   }
-  if constexpr (TYPE != kE4m3) {
-    if (warp >= kLoadWarp && warp < kIssueWarp && issued > 0) {
-      cp_async_wait<0>();
-      proxy_fence_smem();
-      bar_arrive(b_full + 8 * ((issued - 1) % kStages));
-    }
-  }
+  cp_async_wait<0>();
   if (s_dead) {  // give the copies and products that are in flight a millisecond to end
     const long long began = clock64();
     while (clock64() - began < 2000000) __nanosleep(1000);
