@@ -95,25 +95,29 @@ int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   return TOPKV_OK;
 }
 
-// Tensor map of a layer's keys and values, [page][plane][head][token][column], for boxes of p->box tokens x 64
-// columns in the swizzled order of the operands; box 0 where there is none: pieces of 8 to `tokens` tokens that
-// never straddle a page need page sizes that are multiples of 8, 8-bit values are converted on the way.
+// Tensor map of a layer's keys and values, [page][plane][head][token][column], for boxes of p->box tokens: x 64
+// columns in the swizzled order of the operands, or whole rows of 8-bit values as they lie. Box 0 where there is
+// none: pieces of 8 to `tokens` tokens that never straddle a page need page sizes that are multiples of 8.
 CUtensorMap prefix_map(AttendParams* p, uint32_t type, int tokens) {
   CUtensorMap map = {};
   p->box = 0;
+  const bool narrow = type == TOPKV_TYPE_E4M3;
   const int box = std::min(tokens, p->P & -p->P);
   const int64_t head = p->H > 1 ? p->S_head : 16;
-  if (type == TOPKV_TYPE_E4M3 || box < 8 || p->D < 64 || p->num_pages > 0x7ffffff0ll) return map;
+  if (box < 8 || (!narrow && p->D < 64) || p->num_pages > 0x7ffffff0ll) return map;
   for (const int64_t s : {p->S_page, p->S_kv, p->S_tok, head})
-    if (s <= 0 || s >= (1ll << 40)) return map;
+    if (s <= 0 || s >= (1ll << 40) || !mult16(s)) return map;
   const EncodeTiled encode = encode_tiled();
   if (encode == nullptr) return map;
   const cuuint64_t dims[5] = {(cuuint64_t)p->D, (cuuint64_t)p->P, (cuuint64_t)p->H, 2, (cuuint64_t)p->num_pages};
   const cuuint64_t strides[4] = {(cuuint64_t)p->S_tok, (cuuint64_t)head, (cuuint64_t)p->S_kv, (cuuint64_t)p->S_page};
-  const cuuint32_t sizes[5] = {64, (cuuint32_t)box, 1, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
-  const CUresult r = encode(&map, type == TOPKV_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+  const cuuint32_t sizes[5] = {narrow ? (cuuint32_t)p->D : 64, (cuuint32_t)box, 1, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
+  const CUresult r = encode(&map, narrow                     ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                  : type == TOPKV_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
                             const_cast<uint8_t*>(p->pool), dims, strides, sizes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                            narrow ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r == CUDA_SUCCESS) p->box = box;
   return map;
 }

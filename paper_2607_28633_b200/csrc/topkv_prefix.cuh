@@ -16,9 +16,9 @@
 // other: with more than 128 rows they are two tiles of rows over the same tokens, else the same rows over every
 // other tile of tokens. (256 columns: one accumulator, two buffers of scores, 64 tokens a tile.) Roles:
 //   warps 0-7    softmax: four per accumulator, one thread a row; also Q and the result
-//   warps 8, 9   load K and V through the block table into a ring: tensor copies of page pieces, or 16-byte
-//                copies (any page size and stride); 8-bit values become fp16 on the way
-//   warp 10      one thread issues the products
+//   two warps    load K and V through the block table into a ring: tensor copies of page pieces, or 16-byte
+//                copies (any page size and stride). Of an 8-bit cache one warp loads and two make fp16 of it
+//   one warp     one thread issues the products
 // The (group, KV head, 256 rows) units laid end to end, as long as their tiles, are cut into equal ranges, one
 // per CTA; each leaves its part in 32 bits in the workspace, and the joining kernel adds them to those of the
 // tokens behind the prefix, in order, so that results do not depend on timing.
@@ -140,15 +140,19 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(c
 constexpr int kPrefixRows = 128;    // rows of a tile
 constexpr int kPrefixLoadWarps = 2;
 constexpr int kPrefixMaxStages = 8;
+constexpr int kPrefixMaxRaw = 4;    // buffers of 8-bit tiles that wait to be converted
 constexpr int kPrefixCtas = 148;    // at most
 
+struct PrefixGroup;
 struct PrefixControl {
-  uint64_t bar[2 * kPrefixMaxStages + 7];
+  uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
   int64_t scan[16];
   int64_t off;
-  int lead;
+  int64_t length;  // of the first group's units per KV head ...
+  int group[7];    // ... and the rest of what is known of it; leader -1: nothing to do
   uint32_t tmem;
   volatile int dead;
+  volatile int odd;   // a page outside the pool has been met
   float row_scale[2 * kPrefixRows];
 };
 template <int DP, int TYPE>
@@ -157,15 +161,19 @@ struct PrefixShape {
   static constexpr int kTokens = DP <= 128 ? 128 : 64;    // per tile
   static constexpr int kQ = kPrefixRows * DP * 2;         // bytes of a tile of Q
   static constexpr int kStage = kTokens * DP * 2;         // ... of K or V
-  static constexpr int kRoom = (227 * 1024 - kTiles * kQ - (int)sizeof(PrefixControl)) / kStage;
+  static constexpr bool kConvert = TYPE == kE4m3;
+  static constexpr int kRaws = !kConvert ? 0 : DP == 64 ? 4 : 2;
+  static constexpr int kRaw = kTokens * DP;               // bytes of a tile of 8-bit values
+  static constexpr int kRoom = (227 * 1024 - kTiles * kQ - kRaws * kRaw - (int)sizeof(PrefixControl)) / kStage;
   static constexpr int kStages = kRoom < kPrefixMaxStages ? kRoom : kPrefixMaxStages;
-  static constexpr int kControl = kTiles * kQ + kStages * kStage;
+  static constexpr int kRawAt = kTiles * kQ + kStages * kStage;
+  static constexpr int kControl = kRawAt + kRaws * kRaw;
   static constexpr int kSmem = kControl + (int)sizeof(PrefixControl);
   static constexpr int kSoftmaxWarps = 4 * kTiles;
-  static constexpr int kThreads = (kSoftmaxWarps + kPrefixLoadWarps + 1) * 32;
+  static constexpr int kThreads = (kSoftmaxWarps + kPrefixLoadWarps + (kConvert ? 1 : 0) + 1) * 32;
   static constexpr uint32_t kScores = 0, kSums = 2 * kTokens;  // TMEM columns: two buffers of scores, the accumulators
   static_assert(2 * kTokens + kTiles * DP <= 512, "TMEM");
-  static_assert(kStages >= 5, "a ring shorter than five entries could wait for itself");
+  static_assert(kStages >= 4, "the ring holds K of two tiles and V of the first");
 };
 // What the joining kernel has to know, in the workspace.
 struct PrefixHeader {
@@ -195,13 +203,14 @@ __device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int l
   const AttendParams& a = p.a;
   PrefixGroup g;
   g.lead = lead;
-  g.tokens = shared_tokens(a, lead, a.sl[lead]);
-  if (a.plan[TOPKV_PLAN_LEADER * a.R + lead] != lead) g.tokens = 0;
-  g.tokens = (int)min((int64_t)g.tokens, (int64_t)a.maxp * a.P);
+  // as shared_tokens() has it for the leader; all loads at once
+  const int leader = a.plan[TOPKV_PLAN_LEADER * a.R + lead], shared = a.plan[TOPKV_PLAN_SHARED * a.R + lead];
+  const int members = a.plan[TOPKV_PLAN_MEMBERS * a.R + lead], place = a.plan[TOPKV_PLAN_PLACE * a.R + lead], s = a.sl[lead];
+  g.tokens = leader == lead && members >= 2 && shared > 0 && shared <= s ? (int)min((int64_t)shared, (int64_t)a.maxp * a.P) : 0;
   if (g.tokens == 0) return g;
   g.n = (g.tokens - 1) / p.tokens + 1;
-  g.place = min(max(a.plan[TOPKV_PLAN_PLACE * a.R + lead], 0), a.R - 1);
-  g.rows = min(a.plan[TOPKV_PLAN_MEMBERS * a.R + lead], a.R - g.place) * a.G;
+  g.place = min(max(place, 0), a.R - 1);
+  g.rows = min(members, a.R - g.place) * a.G;
   const int tall = kPrefixRows * p.tiles, rest = (g.rows - 1) % tall + 1;
   g.units = (g.rows - 1) / tall + 1;
   g.full = g.n * p.tiles;
@@ -263,6 +272,11 @@ __device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
                  "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
                  "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
 }
+__device__ __forceinline__ void tmem_loaded(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
 // Arrives at the barrier once this thread's copies so far are there.
 __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
@@ -288,7 +302,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   constexpr bool kBf = TYPE == kBf16;
   constexpr float kShift = kBf ? 0.f : 7.f;
   constexpr int kTokens = S::kTokens, kTiles = S::kTiles, kStages = S::kStages;
-  constexpr int kLoadWarp = S::kSoftmaxWarps, kIssueWarp = kLoadWarp + kPrefixLoadWarps;
+  // 8-bit values: a warp brings them, two convert
+  constexpr int kRawWarp = S::kConvert ? S::kSoftmaxWarps : -1, kLoadWarp = S::kSoftmaxWarps + (S::kConvert ? 1 : 0);
+  constexpr int kIssueWarp = kLoadWarp + kPrefixLoadWarps;
   constexpr int kSoftmaxThreads = S::kSoftmaxWarps * 32;
   constexpr int kBlock = kTokens * 128, kQBlock = kPrefixRows * 128;  // bytes of 64 columns
   extern __shared__ __align__(128) uint8_t smem[];
@@ -303,8 +319,10 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   volatile int& s_dead = ctl.dead;
   const uint32_t b_full = smem_addr(ctl.bar), b_free = b_full + 8 * kStages, b_score = b_free + 8 * kStages;
   const uint32_t b_weight = b_score + 16, b_sum = b_score + 32, b_query = b_score + 48;
+  const uint32_t b_raw = b_query + 8, b_raw_free = b_raw + 8 * S::kRaws;
   if (tid == 0) {
     s_dead = 0;
+    ctl.odd = 0;
     for (int i = 0; i < kStages; ++i) {
       mbar_init(b_full + 8 * i, kPrefixLoadWarps * 32);
       mbar_init(b_free + 8 * i, 1);
@@ -315,6 +333,10 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       mbar_init(b_sum + 8 * i, 1);
     }
     mbar_init(b_query, kSoftmaxThreads);
+    for (int i = 0; i < S::kRaws; ++i) {
+      mbar_init(b_raw + 8 * i, 32);
+      mbar_init(b_raw_free + 8 * i, kPrefixLoadWarps * 32);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kIssueWarp) {
@@ -329,8 +351,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   {
     const int per = (a.R + S::kThreads - 1) / S::kThreads;
     const int r0 = (int)min((int64_t)tid * per, (int64_t)a.R), r1 = min(r0 + per, a.R);
+    PrefixGroup g = {};
     auto length = [&](int r) {
-      const PrefixGroup g = prefix_group(p, r);
+      if (per > 1 || g.n == 0) g = prefix_group(p, r);
       return g.tokens > 0 ? a.H * g.length : 0;
     };
     int64_t mine = 0;
@@ -342,7 +365,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (lane >= o) incl += up;
     }
     if (lane == 31) ctl.scan[warp] = incl;
-    if (tid == 0) ctl.lead = -1;
+    if (tid == 0) ctl.group[0] = -1;
     __syncthreads();
     int64_t total = 0;
     for (int w = 0; w < S::kThreads / 32; ++w) {
@@ -365,8 +388,11 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         const int64_t n = length(r);
         if (team == 0) p.begin[r] = at;
         if (begins && pos >= at && pos < at + n) {
-          ctl.lead = r;
           ctl.off = pos - at;
+          ctl.length = g.length;
+          const int known[7] = {r, g.place, g.tokens, g.n, g.rows, g.units, g.full};
+#pragma unroll
+          for (int i = 0; i < 7; ++i) ctl.group[i] = known[i];
         }
         at += n;
       }
@@ -401,8 +427,8 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   uint32_t issued = 0;              // load: entries whose copies are enqueued
   PrefixGroup g = {};
   int64_t off = ctl.off;
-  int lead = ctl.lead;
-  if (left > 0 && lead >= 0) g = prefix_group(p, lead);
+  int lead = ctl.group[0];
+  g = PrefixGroup{lead, ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], ctl.length};
   while (left > 0 && lead >= 0 && lead < a.R) {
     // the unit, and the tiles [t0, t1) of it that are this CTA's
     const int h = (int)(off / g.length);
@@ -418,16 +444,22 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     auto page_column = [&](int x) { return a.page_shift >= 0 ? x >> a.page_shift : x / a.P; };
     const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
 
-    if (warp >= kLoadWarp && warp < kIssueWarp) {
-      // ---- load ---------------------------------------------------------------------------------------
-      const int w = warp - kLoadWarp;
+    if (warp == kRawWarp || (!S::kConvert && warp >= kLoadWarp && warp < kIssueWarp)) {
+      // ---- load: 16-bit tiles into the ring, 8-bit tiles into buffers of their own ------------------------
+      constexpr int kWarps = S::kConvert ? 1 : kPrefixLoadWarps, kElem = S::kConvert ? 1 : 2;
+      constexpr int kDepth = S::kConvert ? S::kRaws : kStages, kBytes = S::kConvert ? S::kRaw : S::kStage;
+      const int w = S::kConvert ? 0 : warp - kLoadWarp;
+      const uint32_t b_there = S::kConvert ? b_raw : b_full, b_room = S::kConvert ? b_raw_free : b_free;
+      const uint32_t to0 = base + (S::kConvert ? S::kRawAt : kTiles * S::kQ);
       const uint8_t* head = a.pool + (int64_t)h * a.S_head;
-      constexpr int kRows = kTokens / kPrefixLoadWarps, kGroups = kRows / 32;  // rows of this warp
+      constexpr int kRows = kTokens / kWarps, kGroups = kRows / 32;  // rows of this warp
       static_assert(kRows % 32 == 0, "a lane per row");
-      const int chunks = a.D / 8, padded = ksteps * 2, full = chunks / 8;
+      const int chunks = a.D * kElem / 16, padded = S::kConvert ? chunks : ksteps * 2;  // of 16 bytes
+      const int blocks = S::kConvert ? 1 : (a.D + 63) / 64;
       // Whole page pieces come by tensor copies, those outside the pool and behind the prefix as zeros from
       // outside the tensor. A prefix that ends inside a piece has its last tile copied row by row.
       const int box = a.box, boxes = box > 0 ? kTokens / box : 0;
+      const uint32_t box_bytes = (uint32_t)(box * (S::kConvert ? a.D : 128));
       auto piece = [&](int t) {  // page of piece `lane` of a tile
         const int x = t * kTokens + lane * box;
         return t < t1 && lane < boxes && x < g.tokens ? bt_row[page_column(x)] : -1;
@@ -435,30 +467,44 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       int pg = boxes > 0 ? piece(t0) : -1;
       for (int t = t0; t < t1; ++t) {
         if (__any_sync(0xffffffffu, s_dead)) break;
-        if (TYPE != kE4m3 && boxes > 0 && (g.tokens >= (t + 1) * kTokens || g.tokens % box == 0)) {
+        if (boxes > 0 && (g.tokens >= (t + 1) * kTokens || g.tokens % box == 0)) {
           const int x = t * kTokens + lane * box;
           bool ok = lane < boxes && x < g.tokens;
           if (ok && (pg < 0 || pg >= a.num_pages)) {
             raise_error(kErrTable);
+            ctl.odd = 1;
             ok = false;
           }
           const int z = ok ? pg : (int)a.num_pages, y = ok ? x - page_column(x) * a.P : 0;
           pg = piece(t + 1);
 #pragma unroll 1
           for (int plane = 0; plane < 2; ++plane, ++issued) {
-            const uint32_t stage = issued % kStages, bar = b_full + 8 * stage;
-            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
-            const uint32_t dst = base + kTiles * S::kQ + stage * S::kStage;
-            const int blocks = (a.D + 63) / 64;
+            const uint32_t stage = issued % kDepth, bar = b_there + 8 * stage;
+            if (issued >= kDepth) wait(b_room + 8 * stage, issued / kDepth - 1);
+            const uint32_t dst = to0 + stage * kBytes;
             if (lane == 0)
-              mbar_expect_tx(bar, (uint32_t)((boxes + 1 - w) / 2 * blocks * box * 128));
+              mbar_expect_tx(bar, (uint32_t)((boxes + kWarps - 1 - w) / kWarps) * blocks * box_bytes);
             else
               bar_arrive(bar);
             __syncwarp();
-            for (int e = w; e < boxes; e += kPrefixLoadWarps) {
-              const int ze = __shfl_sync(0xffffffffu, z, e), ye = __shfl_sync(0xffffffffu, y, e);
+            // the pieces' places are gathered by the whole warp, so that one thread's instructions follow each other
+#pragma unroll 1
+            for (int e0 = w; e0 < boxes; e0 += 4 * kWarps) {
+              int ze[4], ye[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                ze[k] = __shfl_sync(0xffffffffu, z, (e0 + kWarps * k) & 31);
+                ye[k] = __shfl_sync(0xffffffffu, y, (e0 + kWarps * k) & 31);
+              }
               if (elect_one()) {
-                for (int b = 0; b < blocks; ++b) tma_load5(dst + b * kBlock + e * box * 128, &map, b * 64, ye, h, plane, ze, bar);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const int e = e0 + kWarps * k;
+                  if (e >= boxes) break;
+#pragma unroll
+                  for (int b = 0; b < (S::kConvert ? 1 : DP / 64); ++b)
+                    if (b < blocks) tma_load5(dst + b * kBlock + e * box_bytes, &map, b * 64, ye[k], h, plane, ze[k], bar);
+                }
               }
               __syncwarp();
             }
@@ -473,67 +519,72 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           o[k] = -1;
           if (x < g.tokens) {
             const int j = page_column(x), page = bt_row[j];
-            if (page < 0 || page >= a.num_pages)
+            if (page < 0 || page >= a.num_pages) {
               raise_error(kErrTable);
-            else
+              ctl.odd = 1;
+            } else {
               o[k] = (int64_t)page * a.S_page + (int64_t)(x - j * a.P) * a.S_tok;
+            }
           }
         }
 #pragma unroll 1
         for (int plane = 0; plane < 2; ++plane, ++issued) {
-          const uint32_t stage = issued % kStages;
-          const uint32_t dst = base + kTiles * S::kQ + stage * S::kStage + w * kRows * 128;
+          const uint32_t stage = issued % kDepth;
+          if (issued >= kDepth) wait(b_room + 8 * stage, issued / kDepth - 1);
+          const uint32_t dst = to0 + stage * kBytes;
           const uint8_t* src0 = head + plane * a.S_kv;
-          if constexpr (TYPE == kE4m3) {
-            constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kCopies = kRows / kPer;
-            const int c = lane % kChunks, sub = lane / kChunks;
-            uint4 v[kCopies];
+          const int c = lane & 7, sub = lane >> 3;
 #pragma unroll
-            for (int k = 0; k < kCopies; ++k) {
-              const int64_t ro = __shfl_sync(0xffffffffu, o[k * kPer / 32], (k * kPer + sub) & 31);
-              v[k] = make_uint4(0, 0, 0, 0);
-              if (ro >= 0 && c * 16 < a.D) v[k] = *reinterpret_cast<const uint4*>(src0 + ro + c * 16);
-            }
-            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
-            if (c * 16 < a.D) {
-#pragma unroll
-              for (int k = 0; k < kCopies; ++k) {
-                const int row = k * kPer + sub;
-                uint32_t x8[8];
-                e4m3x4_to_f16(v[k].x, &x8[0], &x8[1]);
-                e4m3x4_to_f16(v[k].y, &x8[2], &x8[3]);
-                e4m3x4_to_f16(v[k].z, &x8[4], &x8[5]);
-                e4m3x4_to_f16(v[k].w, &x8[6], &x8[7]);
-                uint8_t* to = smem + (dst - base) + (c >> 2) * kBlock + row * 128;
-                const int ch = (c & 3) * 2;
-                *reinterpret_cast<uint4*>(to + ((ch ^ (row & 7)) << 4)) = make_uint4(x8[0], x8[1], x8[2], x8[3]);
-                *reinterpret_cast<uint4*>(to + (((ch + 1) ^ (row & 7)) << 4)) = make_uint4(x8[4], x8[5], x8[6], x8[7]);
-              }
-            }
-            bar_arrive(b_full + 8 * stage);
-          } else {
-            if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
-            const int c = lane & 7, sub = lane >> 3;
-#pragma unroll
-            for (int k = 0; k < kGroups; ++k) {
+          for (int k = 0; k < kGroups; ++k) {
 #pragma unroll 2
-              for (int rg = 0; rg < 8; ++rg) {
-                const int row = rg * 4 + sub;
-                const int64_t ro = __shfl_sync(0xffffffffu, o[k], row);
-                const uint8_t* src = (ro < 0 ? a.pool : src0 + ro) + c * 16;
-                uint32_t to = dst + (k * 32 + row) * 128 + ((c ^ (row & 7)) << 4);
+            for (int rg = 0; rg < 8; ++rg) {
+              const int row = rg * 4 + sub, in_tile = w * kRows + k * 32 + row;
+              const int64_t ro = __shfl_sync(0xffffffffu, o[k], row);
 #pragma unroll
-                for (int b = 0; b < DP / 64; ++b, to += kBlock) {
-                  if (b < full)
-                    cp_async16(to, ro < 0 ? a.pool : src + b * 128, ro >= 0);
-                  else if (b * 8 + c < padded)
-                    cp_async16(to, ro >= 0 && b * 8 + c < chunks ? src + b * 128 : a.pool, ro >= 0 && b * 8 + c < chunks);
-                }
+              for (int b = 0; b < DP * kElem / 128; ++b) {
+                const int ch = b * 8 + c;
+                const uint32_t to = S::kConvert ? dst + in_tile * a.D + ch * 16 : dst + b * kBlock + in_tile * 128 + ((c ^ (row & 7)) << 4);
+                const bool ok = ro >= 0 && ch < chunks;
+                if (ch < padded) cp_async16(to, ok ? src0 + ro + ch * 16 : a.pool, ok);
+              }
+              if (DP * kElem < 128 && c < padded) {  // 64 columns of 8 bits
+                const bool ok = ro >= 0;
+                cp_async16(dst + in_tile * a.D + c * 16, ok ? src0 + ro + c * 16 : a.pool, ok);
               }
             }
-            cp_async_arrive(b_full + 8 * stage);
+          }
+          cp_async_arrive(b_there + 8 * stage);
+        }
+      }
+    } else if (S::kConvert && warp >= kLoadWarp && warp < kIssueWarp) {
+      // ---- convert: 16 bytes of a row at a time, half of the rows each ----------------------------------
+      constexpr int kRaws = S::kRaws > 0 ? S::kRaws : 1;
+      constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kRows = kTokens / kPrefixLoadWarps;
+      const int c = lane % kChunks, sub = lane / kChunks, row0 = (warp - kLoadWarp) * kRows;
+      for (int e = 0; e < 2 * count; ++e, ++issued) {
+        const uint32_t stage = issued % kStages, raw = issued % kRaws;
+        wait(b_raw + 8 * raw, issued / kRaws);
+        if (issued >= kStages) wait(b_free + 8 * stage, issued / kStages - 1);
+        if (__any_sync(0xffffffffu, s_dead)) break;
+        const uint8_t* from = smem + S::kRawAt + raw * S::kRaw + c * 16;
+        uint8_t* const to = smem + kTiles * S::kQ + stage * S::kStage + (c >> 2) * kBlock;
+        const int ch = (c & 3) * 2;
+        if (c * 16 < a.D) {
+#pragma unroll 4
+          for (int k = 0; k < kRows; k += kPer) {
+            const int row = row0 + k + sub;
+            const uint4 v = *reinterpret_cast<const uint4*>(from + row * a.D);
+            uint32_t x8[8];
+            e4m3x4_to_f16(v.x, &x8[0], &x8[1]);
+            e4m3x4_to_f16(v.y, &x8[2], &x8[3]);
+            e4m3x4_to_f16(v.z, &x8[4], &x8[5]);
+            e4m3x4_to_f16(v.w, &x8[6], &x8[7]);
+            *reinterpret_cast<uint4*>(to + row * 128 + ((ch ^ (row & 7)) << 4)) = make_uint4(x8[0], x8[1], x8[2], x8[3]);
+            *reinterpret_cast<uint4*>(to + row * 128 + (((ch + 1) ^ (row & 7)) << 4)) = make_uint4(x8[4], x8[5], x8[6], x8[7]);
           }
         }
+        bar_arrive(b_raw_free + 8 * raw);
+        bar_arrive(b_full + 8 * stage);
       }
     } else if (warp == kIssueWarp) {
       // ---- products -----------------------------------------------------------------------------------
@@ -576,7 +627,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           __syncwarp();
         }
       }
-    } else if (warp < kLoadWarp) {
+    } else if (warp < S::kSoftmaxWarps) {
       // ---- softmax ------------------------------------------------------------------------------------
       const int acc = warp >> 2, row = (warp & 3) * 32 + lane;        // accumulator, TMEM lane
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;
@@ -587,44 +638,54 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         // Q of the segment before is done with: both accumulators' last products have been waited for
         asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
         if (u.both || acc == 0) {
-          const int gr = u.first_row + my_row, member = gr / a.G;
-          const uint8_t* src = nullptr;
+          const uint8_t* mine = nullptr;
           if (live) {
+            const int gr = u.first_row + my_row, member = gr / a.G;
             int r = a.plan[TOPKV_PLAN_ORDER * a.R + g.place + member];
             r = min(max(r, 0), a.R - 1);
-            src = a.q + r * a.q_req + ((int64_t)h * a.G + gr - member * a.G) * a.q_head;
+            mine = a.q + r * a.q_req + ((int64_t)h * a.G + gr - member * a.G) * a.q_head;
           }
-          const int chunks = a.D / 8, padded = ksteps * 2;
-          float up = 1.f, rest = 1.f;
-          if (TYPE == kE4m3 && a.io_bf16) {
-            // bf16 queries become fp16 ones after a power of two for the row; see the kernel of the other tokens
-            float top = 0.f;
-            for (int c = 0; c < chunks; ++c) {
-              const uint4 v = live ? *reinterpret_cast<const uint4*>(src + c * 16) : make_uint4(0, 0, 0, 0);
-              const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+          // kLanes lanes bring a row, so that a warp's accesses cover whole rows
+          constexpr int kLanes = DP / 8, kPer = 32 / kLanes, kAhead = 8;
+          const int chunks = a.D / 8, padded = ksteps * 2, c = lane % kLanes, sub = lane / kLanes;
+          uint8_t* const to = smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + (warp & 3) * 32 * 128;
+          const uint32_t flip = a.qk_scale < 0.f ? 0x80008000u : 0u;  // scores times a factor that is not negative
+#pragma unroll 1
+          for (int k0 = 0; k0 < 32; k0 += kPer * kAhead) {
+            uint4 v[kAhead];
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u))));
+            for (int k = 0; k < kAhead; ++k) {
+              const uint8_t* src = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), k0 + k * kPer + sub));
+              v[k] = make_uint4(0, 0, 0, 0);
+              if (src != nullptr && c < chunks) v[k] = *reinterpret_cast<const uint4*>(src + c * 16);
             }
-            int e = 0;
-            if (top > 0.f && top < INFINITY) e = ilogbf(top);
-            up = exp2f((float)(-(e / 2)));
-            rest = exp2f((float)(-(e - e / 2)));
-            row_scale = a.qk_scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
-          }
-          ctl.row_scale[my_row] = fabsf(row_scale);
-          const uint32_t flip = row_scale < 0.f ? 0x80008000u : 0u;  // scores times a factor that is not negative
-          for (int c = 0; c < padded; ++c) {
-            uint4 v = live && c < chunks ? *reinterpret_cast<const uint4*>(src + c * 16) : make_uint4(0, 0, 0, 0);
-            if (TYPE == kE4m3 && a.io_bf16) {
-              uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[e] = pack2<false>(__uint_as_float(x[e] << 16) * up * rest, __uint_as_float(x[e] & 0xffff0000u) * up * rest);
-              v = make_uint4(x[0], x[1], x[2], x[3]);
+            for (int k = 0; k < kAhead; ++k) {
+              const int rw = k0 + k * kPer + sub;
+              float scale = fabsf(a.qk_scale);
+              if (TYPE == kE4m3 && a.io_bf16) {
+                // bf16 queries become fp16 ones after a power of two for the row; see the kernel of the other tokens
+                uint32_t x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+                float top = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u))));
+#pragma unroll
+                for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                int e = 0;
+                if (top > 0.f && top < INFINITY) e = ilogbf(top);
+                // in two steps: a single factor of 2^-e may itself leave the range of a float
+                const float up = exp2f((float)(-(e / 2))), rest = exp2f((float)(-(e - e / 2)));
+                scale = scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  x[i] = pack2<false>(__uint_as_float(x[i] << 16) * up * rest, __uint_as_float(x[i] & 0xffff0000u) * up * rest);
+                v[k] = make_uint4(x[0], x[1], x[2], x[3]);
+              }
+              if (c == 0) ctl.row_scale[(u.both ? acc * kPrefixRows : 0) + (warp & 3) * 32 + rw] = scale;
+              v[k] = make_uint4(v[k].x ^ flip, v[k].y ^ flip, v[k].z ^ flip, v[k].w ^ flip);
+              if (c < padded) *reinterpret_cast<uint4*>(to + rw * 128 + (((c & 7) ^ (rw & 7)) << 4)) = v[k];
             }
-            v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
-            *reinterpret_cast<uint4*>(smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
           }
           proxy_fence_smem();
         }
@@ -633,14 +694,6 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         row_scale = ctl.row_scale[my_row];
         bar_arrive(b_query);
       }
-      // Pages outside the pool are not visible. They are looked for once for the segment; only if there are
-      // any does every tile ask which of its tokens count.
-      bool odd = false;
-      for (int t = page_column(t0 * kTokens) + lane; count > 0 && t <= page_column(min(t1 * kTokens, g.tokens) - 1); t += 32) {
-        const int page = bt_row[t];
-        odd |= page < 0 || page >= a.num_pages;
-      }
-      odd = __any_sync(0xffffffffu, odd);
       const bool some = __any_sync(0xffffffffu, live);  // a row of this warp counts
       float m = -INFINITY, l = 0.f, sub = 0.f;  // sub: what is subtracted from a score
       bool seen = false;
@@ -658,6 +711,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           // which of the tile's tokens count, 32 to a word
           uint32_t valid[kTokens / 32];
           const int visible = g.tokens - t * kTokens;
+          const bool odd = ctl.odd;  // pages outside the pool are not visible: from the first one on every tile asks
 #pragma unroll
           for (int c = 0; c < kTokens / 32; ++c) {
             const int n = visible - c * 32;
@@ -684,24 +738,25 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             const float2 by = make_float2(row_scale, row_scale), less = make_float2(-sub, -sub);
             top = -INFINITY;
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            uint32_t raw[2][32];
-            tmem_load<32>(raw[0], s_col);
+            uint32_t raw[2][16];
+            tmem_load<16>(raw[0], s_col);
 #pragma unroll
-            for (int c = 0; c < kTokens / 32; ++c) {
-              uint32_t(&x)[32] = raw[c & 1];
+            for (int c = 0; c < kTokens / 16; ++c) {
+              uint32_t(&x)[16] = raw[c & 1];
               tmem_loaded(x);
-              if (c + 1 < kTokens / 32) tmem_load<32>(raw[(c + 1) & 1], s_col + (c + 1) * 32);
+              if (c + 1 < kTokens / 16) tmem_load<16>(raw[(c + 1) & 1], s_col + (c + 1) * 16);
 #pragma unroll
-              for (int k = 0; k < 32; k += 2) {
+              for (int k = 0; k < 16; k += 2) {
                 float2 s = make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-                const bool v0 = !kMasked || (valid[c] >> k & 1), v1 = !kMasked || (valid[c] >> (k + 1) & 1);
+                const uint32_t bits = kMasked ? valid[c / 2] >> (c % 2 * 16 + k) : 3u;
+                const bool v0 = bits & 1, v1 = bits & 2;
                 top = fmaxf(top, fmaxf(v0 ? s.x : -INFINITY, v1 ? s.y : -INFINITY));
                 if constexpr (kExps) {
                   s = fma2(s, by, less);
                   s.x = v0 ? exp2_approx(s.x) : 0.f;
                   s.y = v1 ? exp2_approx(s.y) : 0.f;
                   part[k / 2 & 1] = add2(part[k / 2 & 1], s);
-                  w[c * 16 + k / 2] = pack2<kBf>(s.x, s.y);
+                  w[c * 8 + k / 2] = pack2<kBf>(s.x, s.y);
                 }
               }
             }
@@ -761,19 +816,37 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       }
       const int64_t to = slot + (u.both || acc == 0 ? my_row : u.rows + my_row);
       if (live) p.ml[to] = make_float2(m - kShift, seen ? l : kNoneSeen);
+      // Rows leave by way of shared memory, where Q is not needed any more once both accumulators have come here:
+      // a warp's 32 rows of kWide columns, 16-byte chunks permuted by row, then whole rows at a time. (A row per
+      // thread straight to memory: 8,000 cycles a segment.)
+      if (jobs > 0) asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
       if (last >= 0 && some) {
-        for (int c = 0; c < DP / 32; ++c) {
-          if (c * 32 >= a.D) break;
-          uint32_t o[32];
-          tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
-          tmem_loaded(o);
-          if (live) {
+        constexpr int kWide = DP / 2, kChunks = kWide / 4, kPer = 32 / kChunks;  // columns, their chunks, rows per access
+        uint8_t* const mine = smem + (acc * 4 + (warp & 3)) * (32 * kWide * 4);
+        const int rows_here = min(32, u.rows - (u.both ? acc * kPrefixRows : 0) - (warp & 3) * 32);
+        const int c = lane % kChunks, sub = lane / kChunks;
+#pragma unroll 1
+        for (int half = 0; half < 2 && half * kWide < a.D; ++half) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              if (c * 32 + e < a.D)
-                *reinterpret_cast<float4*>(&p.part[to * a.Dv + c * 32 + e]) =
-                    make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+          for (int k = 0; k < kWide / 32; ++k) {
+            uint32_t o[32];
+            tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + half * kWide + k * 32);
+            tmem_loaded(o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              *reinterpret_cast<uint4*>(mine + lane * (kWide * 4) + (((k * 8 + e) ^ (lane & (kChunks - 1))) << 4)) =
+                  make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
+          __syncwarp();
+          float* const out = p.part + (to - lane) * a.Dv + half * kWide;
+#pragma unroll 8
+          for (int r0 = 0; r0 < 32; r0 += kPer) {
+            const int rw = r0 + sub, at = c ^ (rw & (kChunks - 1));
+            const uint4 v = *reinterpret_cast<const uint4*>(mine + rw * (kWide * 4) + (c << 4));
+            if (rw < rows_here && half * kWide + at * 4 < a.D)
+              *reinterpret_cast<uint4*>(out + (int64_t)rw * a.Dv + at * 4) = v;
+          }
+          __syncwarp();
         }
       }
       tcgen05_before_sync();
