@@ -541,6 +541,14 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
                               const int32_t* d_plan, const void* d_q, void* d_out, void* d_workspace,
                               int64_t workspace_bytes, topkv_stream_t stream);
 
+/* A group's shared tokens are formed once only if that saves reading at least this many bytes of a layer, (members -
+ * 1) * shared tokens of K and V of all heads; smaller groups are attended to request by request, which is
+ * faster then (the default is the time of the additional kernel's start). Returns the previous value, or
+ * TOPKV_ERR_INVALID_ARG for a negative one. Process-wide; takes effect for calls made after it returns.
+ * Results differ by rounding only. */
+#define TOPKV_DEFAULT_SHARING_BYTES (4 * 1024 * 1024)
+int64_t topkv_set_sharing_bytes(int64_t bytes);
+
 /* ---- attention over chosen pages -------------------------------------------------------------------
  * Sparse attention for long contexts: each KV head of a request sees only its first and last pages and
  * those whose keys can score highest, by a bound kept in 8 bits. Per page p and KV head h, over the keys K

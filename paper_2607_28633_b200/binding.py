@@ -36,7 +36,7 @@ TOPKV_TYPE_BF16, TOPKV_TYPE_FP16, TOPKV_TYPE_E4M3 = 1, 2, 3
 # every symbol include/topkv.h declares
 EXPORTS = (
     "topkv_append_layer", "topkv_rotary_frequencies", "topkv_rotary_turns", "topkv_plan_prefixes",
-    "topkv_attend_shared_workspace_bytes", "topkv_attend_shared_layer", "topkv_bound_pages_layer",
+    "topkv_attend_shared_workspace_bytes", "topkv_attend_shared_layer", "topkv_set_sharing_bytes", "topkv_bound_pages_layer",
     "topkv_page_choice_workspace_bytes", "topkv_choose_pages_layer", "topkv_attend_pages_layer",
     "topkv_pack_layer", "topkv_unpack_layer", "topkv_pack_layer_to_host",
     "topkv_unpack_layer_from_host", "topkv_build_plan", "topkv_validate_batch_host",
@@ -174,6 +174,7 @@ def make_attention(q, out, cache_type: int, io_type: int, scale: float, value_di
 TOPKV_ROTARY_HALVES, TOPKV_ROTARY_PAIRS = 1, 2
 TOPKV_STRETCH_NONE, TOPKV_STRETCH_LINEAR, TOPKV_STRETCH_BASE, TOPKV_STRETCH_RAMP = 0, 1, 2, 3
 TOPKV_PLAN_ROWS = 6
+TOPKV_DEFAULT_SHARING_BYTES = 4 * 1024 * 1024
 (TOPKV_PLAN_LEADER, TOPKV_PLAN_COMMON, TOPKV_PLAN_SHARED, TOPKV_PLAN_MEMBERS, TOPKV_PLAN_ORDER,
  TOPKV_PLAN_PLACE) = range(TOPKV_PLAN_ROWS)
 
@@ -415,6 +416,8 @@ def lib() -> ctypes.CDLL:
         L.topkv_rotary_frequencies.argtypes = [ctypes.POINTER(topkv_rotary_stretch), c_uint32, c_void_p]
         L.topkv_rotary_turns.argtypes = [c_void_p, c_uint32, c_void_p]
         L.topkv_plan_prefixes.argtypes = [lp, bp, c_int32, c_void_p, c_void_p]
+        L.topkv_set_sharing_bytes.argtypes = [c_int64]
+        L.topkv_set_sharing_bytes.restype = c_int64
         L.topkv_attend_shared_workspace_bytes.argtypes = [lp, bp, ap]
         L.topkv_attend_shared_workspace_bytes.restype = c_int64
         L.topkv_attend_shared_layer.argtypes = [c_int, c_void_p, lp, bp, ap, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
@@ -777,6 +780,10 @@ def topkv_rotary_turns(frequencies):
 
 def topkv_plan_prefixes(layout, batch, min_tokens, d_plan, stream=None):
     return lib().topkv_plan_prefixes(ctypes.byref(layout), ctypes.byref(batch), min_tokens, _ptr(d_plan), _stream(stream))
+
+
+def topkv_set_sharing_bytes(nbytes):
+    return lib().topkv_set_sharing_bytes(nbytes)
 
 
 def topkv_attend_shared_workspace_bytes(layout, batch, attention):

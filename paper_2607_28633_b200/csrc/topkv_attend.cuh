@@ -88,9 +88,10 @@ struct AttendParams {
   int4* joins;          // which requests were cut, see JoinRecord: [R] if by_request, else [teams]
   float2* ml;           // [teams][2][H * gtiles][rows]
   float* part;          // [teams][2][H * gtiles][rows][Dv]
-  // kBehindPrefix: every request leaves parts, slot (r + team) of [R + teams] (uncut: r of [R]), and its
-  // join record is {r, first slot, parts, 0}
+  // kBehindPrefix: requests that share or are cut leave parts, slot (r + team) of [R + teams] (uncut: r of
+  // [R]), and a join record {r, first slot, parts, 0}; parts -1: the result is written
   const int32_t* plan;  // [rows of a plan][R]
+  int64_t least_saved;  // tokens of a group that need not be read again, from which on it is worth the work
   // kChosenPages
   const int32_t* chosen;  // [R][H][budget] table columns
   int budget;
@@ -104,7 +105,7 @@ __device__ __forceinline__ int shared_tokens(const AttendParams& p, int r, int s
   const int rank = p.plan[TOPKV_PLAN_PLACE * p.R + r] - p.plan[TOPKV_PLAN_PLACE * p.R + lead];
   const int members = p.plan[TOPKV_PLAN_MEMBERS * p.R + lead];
   if (p.plan[TOPKV_PLAN_LEADER * p.R + lead] != lead || p.plan[TOPKV_PLAN_SHARED * p.R + lead] != n || p.sl[lead] < n ||
-      members < 2 || rank < 0 || rank >= members)
+      members < 2 || rank < 0 || rank >= members || (members - 1ll) * n < p.least_saved)
     return 0;
   return n;
 }
@@ -243,6 +244,18 @@ __device__ __forceinline__ TeamRange team_range(const AttendParams& p, int team,
 __device__ __forceinline__ void write_join(const AttendParams& p, int r, int team, int slot, int parts) {
   p.joins[p.by_request ? r : team] = make_int4(r, team, slot, parts);
 }
+// kBehindPrefix: ... with whom the request shares, and its rank among them.
+__device__ __forceinline__ void write_part_join(const AttendParams& p, int r, const Visible& v, int slot, int parts) {
+  int lead = -1, rank = 0;
+  if (v.lo > 0) {
+    lead = p.plan[TOPKV_PLAN_LEADER * p.R + r];
+    rank = p.plan[TOPKV_PLAN_PLACE * p.R + r] - p.plan[TOPKV_PLAN_PLACE * p.R + lead];
+    parts = max(parts, 0);
+  } else if (parts <= 1) {
+    parts = -1;  // the result is written by the CTA that has the whole request
+  }
+  p.joins[r] = make_int4(lead, slot, parts, rank);
+}
 // `begin`: where the request begins, from the start of the team's range (before it, if negative).
 __device__ __forceinline__ void request_begins(const AttendParams& p, const TeamStart& s, int team, int r, bool first, int64_t begin,
                                                int tiles, bool whole) {
@@ -308,12 +321,15 @@ __device__ __forceinline__ void empty_requests(const AttendParams& p, int team, 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t first = team + (int64_t)p.teams * 32 * warp; first < p.R; first += (int64_t)p.teams * THREADS) {
     const int64_t e = first + (int64_t)p.teams * lane;
-    const bool empty = e < p.R && visible_tokens<MODE>(p, (int)e, complain).n == 0;
-    if constexpr (MODE == kBehindPrefix) {  // the join writes the result
-      if (empty && complain) write_join(p, (int)e, 0, 0, 0);
-      continue;
+    Visible vis = {1, 0, 0};
+    if (e < p.R) vis = visible_tokens<MODE>(p, (int)e, complain);
+    bool empty = vis.n == 0;
+    if constexpr (MODE == kBehindPrefix) {  // of one that shares all it has the join writes the result
+      if (empty && complain) write_part_join(p, (int)e, vis, 0, 0);
+      empty = empty && vis.lo == 0;
+    } else {
+      if (empty && complain && !p.uncut && p.by_request) write_join(p, (int)e, 0, 0, 0);
     }
-    if (empty && complain && !p.uncut && p.by_request) write_join(p, (int)e, 0, 0, 0);
     for (uint32_t left = __ballot_sync(0xffffffffu, empty); left != 0; left &= left - 1) {
       const int64_t r = first + (int64_t)p.teams * (__ffs(left) - 1);
       for (int i = lane; i < rows * p.Dv; i += 32) {
@@ -374,7 +390,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
   __shared__ TeamStart s_team;
   __shared__ uint32_t s_mask[kAttendWarps][AttendShape<DP, TYPE>::kStages];
   __shared__ int s_seen[kAttendWarps];  // kUsable: a token of the warp's share counted; narrow: kVisible as well
-  constexpr int kUsable = 1, kVisible = 2;
+  constexpr int kUsable = 1, kVisible = 2, kPart = 4;  // kPart: the rest of the request is elsewhere
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int team = blockIdx.x, unit = blockIdx.y;  // unit: KV head and group of 16 query heads
@@ -428,10 +444,10 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     const int64_t taken = tiles_in_range(p, tiles, off, left, &t0, &t1);
     if constexpr (MODE == kBehindPrefix) {
       if (p.narrow) {
-        if (unit == 0 && lane == 0 && tiles > 0) write_join(p, r, r, 1, 0);
+        if (unit == 0 && lane == 0 && tiles > 0) write_part_join(p, r, vis, r, 1);
       } else if (records && t0 == 0 && t1 > 0) {
         const int64_t last = s_team.pos + mine.left - left - off + tiles - 1;
-        write_join(p, r, p.uncut ? r : r + team, t1 == tiles ? 1 : team_of(s_team, last) - team + 1, 0);
+        write_part_join(p, r, vis, p.uncut ? r : r + team, t1 < tiles ? team_of(s_team, last) - team + 1 : 1);
       }
     } else {
       if (records && t0 == 0 && t1 > 0) request_begins(p, s_team, team, r, first, mine.left - left - off, tiles, t1 == tiles);
@@ -722,7 +738,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
     float* s_o = reinterpret_cast<float*>(smem);                              // [warp][row][kPitch]
     float* s_m = s_o + kAttendWarps * kAttendRows * kPitch;                   // [warp][row]
     float* s_l = s_m + kAttendWarps * kAttendRows;
-    if (lane == 0) s_seen[warp] = (seen ? kUsable : 0) | (vis.n > 0 ? kVisible : 0);
+    if (lane == 0) s_seen[warp] = (seen ? kUsable : 0) | (vis.n > 0 ? kVisible : 0) | (MODE == kBehindPrefix && vis.lo > 0 ? kPart : 0);
     if (gc == 0) {
       s_m[warp * kAttendRows + gr] = m[0] - kShift;
       s_m[warp * kAttendRows + gr + 8] = m[1] - kShift;
@@ -751,9 +767,9 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
       for (int i = tid; i < kAttendWarps * rows * quads; i += kAttendThreads) {
         const int wg = i / quads, d = (i - wg * quads) * 4;
         const int w = wg / rows, g = wg - w * rows;
-        if (s_seen[w] == 0) continue;  // empty_requests has written it
+        if (!(s_seen[w] & kVisible)) continue;  // empty_requests has written it
         const int64_t e = (int64_t)team * kAttendWarps + w;
-        if constexpr (MODE == kBehindPrefix) {
+        if (MODE == kBehindPrefix && (s_seen[w] & kPart)) {
           const int64_t row = (e * gridDim.y + unit) * p.rows + g;
           *reinterpret_cast<float4*>(&p.part[row * p.Dv + d]) = *reinterpret_cast<const float4*>(&s_o[(w * kAttendRows + g) * kPitch + d]);
           if (d == 0) p.ml[row] = make_float2(s_m[w * kAttendRows + g], s_seen[w] & kUsable ? s_l[w * kAttendRows + g] : kNoneSeen);
@@ -790,7 +806,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<DP, TYPE>::kCtas) 
         acc.z += c * v.z;
         acc.w += c * v.w;
       }
-      if (MODE != kBehindPrefix && whole) {
+      if (whole && !(MODE == kBehindPrefix && vis.lo > 0)) {
         const float inv = any ? __fdividef(p.v_scale, sum) : 0.f;
         store_io4(p.out + r * p.o_req + (q_head0 + g) * p.o_head + d * 2, acc, inv, p.io_bf16);
         if (d == 0 && p.lse != nullptr) p.lse[(int64_t)r * p.H * p.G + q_head0 + g] = (top + log2f(sum)) * kLn2;

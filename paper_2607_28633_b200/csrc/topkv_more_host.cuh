@@ -75,6 +75,7 @@ struct SharedPlan {
   int64_t own_rows, rows; // rows of parts: of the tokens behind the prefixes, of the prefixes
   int64_t bytes;
 };
+std::atomic<int64_t> g_sharing_bytes{TOPKV_DEFAULT_SHARING_BYTES};
 int64_t aligned16(int64_t x) { return (x + 15) / 16 * 16; }
 
 int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, SharedPlan* plan) {
@@ -89,7 +90,7 @@ int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   plan->own_rows = (R + (a.uncut ? 0 : a.teams)) * a.units * a.rows;
   plan->rows = plan->tiles * (q_rows + (int64_t)kPrefixCtas * kPrefixRows);
   plan->bytes = R == 0 ? 0
-                       : R * 16 + (int64_t)sizeof(PrefixHeader) + aligned16(R * 8) + aligned16((plan->own_rows + plan->rows) * 8) +
+                       : R * 16 + (int64_t)sizeof(PrefixHeader) + R * (int64_t)sizeof(PrefixGroup) + aligned16((plan->own_rows + plan->rows) * 8) +
                              (plan->own_rows + plan->rows) * a.dv * 4;
   plan->bytes = (plan->bytes + 255) / 256 * 256;
   return TOPKV_OK;
@@ -344,6 +345,10 @@ int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, in
   return launched(launch_pdl(topkv_plan_groups_kernel, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);
 }
 
+int64_t topkv_set_sharing_bytes(int64_t bytes) {
+  return bytes < 0 ? TOPKV_ERR_INVALID_ARG : g_sharing_bytes.exchange(bytes, std::memory_order_relaxed);
+}
+
 int64_t topkv_attend_shared_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
                                             const topkv_attention* attention) {
   SharedPlan plan;
@@ -366,6 +371,7 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
   PrefixParams p = {};
   p.a = attend_params(layer, pool, layout, batch, attention, plan.attend, d_q, d_out);
   p.a.plan = d_plan;
+  p.a.least_saved = g_sharing_bytes.load(std::memory_order_relaxed) / (2ll * p.a.H * p.a.D * (int64_t)layout->elem_bytes);
   p.tiles = plan.tiles;
   p.tokens = plan.tokens;
   uint8_t* w = static_cast<uint8_t*>(d_workspace);
@@ -378,7 +384,7 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
   p.a.joins = reinterpret_cast<int4*>(part(R * 16));
   p.a.by_request = 1;
   p.header = reinterpret_cast<PrefixHeader*>(part(sizeof(PrefixHeader)));
-  p.begin = reinterpret_cast<int64_t*>(part(R * 8));
+  p.groups = reinterpret_cast<PrefixGroup*>(part(R * (int64_t)sizeof(PrefixGroup)));
   p.a.ml = reinterpret_cast<float2*>(part((plan.own_rows + plan.rows) * 8));
   p.ml = p.a.ml + plan.own_rows;
   p.a.part = reinterpret_cast<float*>(w);

@@ -142,8 +142,8 @@ constexpr int kPrefixLoadWarps = 2;
 constexpr int kPrefixMaxStages = 8;
 constexpr int kPrefixMaxRaw = 4;    // buffers of 8-bit tiles that wait to be converted
 constexpr int kPrefixCtas = 148;    // at most
+constexpr int kMixedPairs = 3;      // of eight pairs of weights, those on the multiply-add units
 
-struct PrefixGroup;
 struct PrefixControl {
   uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
   int64_t scan[16];
@@ -175,21 +175,6 @@ struct PrefixShape {
   static_assert(2 * kTokens + kTiles * DP <= 512, "TMEM");
   static_assert(kStages >= 4, "the ring holds K of two tiles and V of the first");
 };
-// What the joining kernel has to know, in the workspace.
-struct PrefixHeader {
-  int64_t each;  // length of a range ...
-  int more;      // ... and how many are one longer
-  int teams;
-};
-struct PrefixParams {
-  AttendParams a;          // teams is that of the tokens behind the prefix
-  PrefixHeader* header;
-  int64_t* begin;          // [R], of leaders: where the group's units begin on the line
-  float2* ml;              // [rows of parts]
-  float* part;             // [rows of parts][Dv]
-  int tiles;               // accumulators, tokens per tile: those of the kernel's shape
-  int tokens;
-};
 // A group: its leader, and the geometry of its units.
 struct PrefixGroup {
   int lead, place;   // its first row's place in the plan's order
@@ -197,7 +182,24 @@ struct PrefixGroup {
   int rows;          // members * G
   int units;         // per KV head
   int full;          // length of a unit of all rows
+  int pad;
   int64_t length;    // of a KV head's units
+  int64_t begin;     // where the group's units begin on the line
+};
+// How the line is cut.
+struct PrefixHeader {
+  int64_t each;  // length of a range ...
+  int more;      // ... and how many are one longer
+  int teams;
+};
+struct PrefixParams {
+  AttendParams a;          // teams is that of the tokens behind the prefix
+  PrefixHeader* header;    // for the joining kernel, as are
+  PrefixGroup* groups;     // [R], of leaders
+  float2* ml;              // [rows of parts]
+  float* part;             // [rows of parts][Dv]
+  int tiles;               // accumulators, tokens per tile: those of the kernel's shape
+  int tokens;
 };
 __device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int lead) {
   const AttendParams& a = p.a;
@@ -206,7 +208,7 @@ __device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int l
   // as shared_tokens() has it for the leader; all loads at once
   const int leader = a.plan[TOPKV_PLAN_LEADER * a.R + lead], shared = a.plan[TOPKV_PLAN_SHARED * a.R + lead];
   const int members = a.plan[TOPKV_PLAN_MEMBERS * a.R + lead], place = a.plan[TOPKV_PLAN_PLACE * a.R + lead], s = a.sl[lead];
-  g.tokens = leader == lead && members >= 2 && shared > 0 && shared <= s ? (int)min((int64_t)shared, (int64_t)a.maxp * a.P) : 0;
+  g.tokens = leader == lead && members >= 2 && shared > 0 && shared <= s && (members - 1ll) * shared >= a.least_saved ? (int)min((int64_t)shared, (int64_t)a.maxp * a.P) : 0;
   if (g.tokens == 0) return g;
   g.n = (g.tokens - 1) / p.tokens + 1;
   g.place = min(max(place, 0), a.R - 1);
@@ -262,6 +264,30 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// 2^x of two numbers on the multiply-add units, whose time is free while the other elements' exponentials keep the
+// special ones busy: x = n + f with |f| <= 1/2, a polynomial of degree 4 for 2^f (the one with the least
+// largest relative error, 2.6e-6, found by exchange), n added to the exponent. Below 2^-126 it stays there.
+// NaN does not survive it: callers use exp2_approx for tiles that hold any.
+__device__ __forceinline__ float2 exp2_multiply(float2 x) {
+  constexpr float kRound = 12582912.f;  // 1.5 * 2^23: sums with it are rounded to whole numbers
+  x.x = fmaxf(x.x, -126.f);
+  x.y = fmaxf(x.y, -126.f);
+  const float2 t = add2(x, make_float2(kRound, kRound));
+  const float2 f = fma2(add2(t, make_float2(-kRound, -kRound)), make_float2(-1.f, -1.f), x);
+  float2 y = fma2(f, make_float2(0x1.3997d6p-7f, 0x1.3997d6p-7f), make_float2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
+  y = fma2(y, f, make_float2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
+  y = fma2(y, f, make_float2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
+  y = fma2(y, f, make_float2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
+  y.x = __int_as_float(__float_as_int(y.x) + (__float_as_int(t.x) << 23));
+  y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(t.y) << 23));
+  return y;
+}
+// The larger of two, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
 // What has been loaded is used only behind this, by name.
@@ -339,12 +365,17 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // The kernel behind this one does not wait for it: it may run once this one has waited. (It holds no TMEM, and
+  // what comes after it starts when all its CTAs have, which is after this kernel's.)
+  if (!a.late_wait) {
+    pdl_wait_prior_grid();
+    pdl_release_next_grid();
+  }
   if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "n"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     tcgen05_before_sync();
   }
-  if (!a.late_wait) pdl_wait_prior_grid();
 
   // ---- this CTA's range of the line --------------------------------------------------------------------
   int64_t pos, left = 0;
@@ -380,13 +411,19 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     t.teams = teams;
     pos = t.each * team + min(team, t.more);
     if (team < teams) left = t.each + (team < t.more ? 1 : 0);
-    if (a.late_wait) pdl_wait_prior_grid();  // the join of the call before reads the workspace until then
+    if (a.late_wait) {  // the join of the call before reads the workspace until then
+      pdl_wait_prior_grid();
+      pdl_release_next_grid();
+    }
     int64_t at = incl - mine;
     const bool begins = left > 0 && pos >= at && pos < incl;  // exactly one thread
     if (begins || team == 0) {
       for (int r = r0; r < r1; ++r) {
         const int64_t n = length(r);
-        if (team == 0) p.begin[r] = at;
+        if (team == 0 && n > 0) {
+          g.begin = at;
+          p.groups[r] = g;
+        }
         if (begins && pos >= at && pos < at + n) {
           ctl.off = pos - at;
           ctl.length = g.length;
@@ -402,7 +439,6 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   __syncthreads();
   tcgen05_after_sync();
   const uint32_t tmem = ctl.tmem;
-  pdl_release_next_grid();  // every CTA has its TMEM, and has waited for what came before
 
   auto wait = [&](uint32_t bar, uint32_t phase) {
     if (mbar_try_wait(bar, phase & 1)) return;
@@ -428,7 +464,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   PrefixGroup g = {};
   int64_t off = ctl.off;
   int lead = ctl.group[0];
-  g = PrefixGroup{lead, ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], ctl.length};
+  g = PrefixGroup{lead, ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], 0, ctl.length, 0};
   while (left > 0 && lead >= 0 && lead < a.R) {
     // the unit, and the tiles [t0, t1) of it that are this CTA's
     const int h = (int)(off / g.length);
@@ -646,7 +682,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             mine = a.q + r * a.q_req + ((int64_t)h * a.G + gr - member * a.G) * a.q_head;
           }
           // kLanes lanes bring a row, so that a warp's accesses cover whole rows
-          constexpr int kLanes = DP / 8, kPer = 32 / kLanes, kAhead = 8;
+          constexpr int kLanes = DP / 8, kPer = 32 / kLanes, kAhead = 32 / kPer < 16 ? 32 / kPer : 16;
           const int chunks = a.D / 8, padded = ksteps * 2, c = lane % kLanes, sub = lane / kLanes;
           uint8_t* const to = smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + (warp & 3) * 32 * 128;
           const uint32_t flip = a.qk_scale < 0.f ? 0x80008000u : 0u;  // scores times a factor that is not negative
@@ -733,8 +769,8 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           uint32_t w[kTokens / 2];
           float2 sum;
           float top;
-          auto pass = [&](auto exps, auto masked) {
-            constexpr bool kExps = decltype(exps)::value, kMasked = decltype(masked)::value;
+          auto pass = [&](auto exps, auto masked, auto mixed) {
+            constexpr bool kExps = decltype(exps)::value, kMasked = decltype(masked)::value, kMixed = decltype(mixed)::value;
             const float2 by = make_float2(row_scale, row_scale), less = make_float2(-sub, -sub);
             top = -INFINITY;
             float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -750,11 +786,15 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 float2 s = make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
                 const uint32_t bits = kMasked ? valid[c / 2] >> (c % 2 * 16 + k) : 3u;
                 const bool v0 = bits & 1, v1 = bits & 2;
-                top = fmaxf(top, fmaxf(v0 ? s.x : -INFINITY, v1 ? s.y : -INFINITY));
+                top = max_nan(top, max_nan(v0 ? s.x : -INFINITY, v1 ? s.y : -INFINITY));
                 if constexpr (kExps) {
                   s = fma2(s, by, less);
-                  s.x = v0 ? exp2_approx(s.x) : 0.f;
-                  s.y = v1 ? exp2_approx(s.y) : 0.f;
+                  if (kMixed && (k / 2) % 8 < kMixedPairs) {
+                    s = exp2_multiply(s);
+                  } else {
+                    s.x = v0 ? exp2_approx(s.x) : 0.f;
+                    s.y = v1 ? exp2_approx(s.y) : 0.f;
+                  }
                   part[k / 2 & 1] = add2(part[k / 2 & 1], s);
                   w[c * 8 + k / 2] = pack2<kBf>(s.x, s.y);
                 }
@@ -763,15 +803,14 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             top = top == -INFINITY ? top : top * row_scale;
             sum = add2(part[0], part[1]);
           };
-          auto exps = [&] {
-            if (partial) pass(std::true_type{}, std::true_type{}); else pass(std::true_type{}, std::false_type{});
-          };
+          constexpr std::true_type yes{};
+          constexpr std::false_type no{};
           if (j < kTiles) {
-            if (partial) pass(std::false_type{}, std::true_type{}); else pass(std::false_type{}, std::false_type{});
+            if (partial) pass(no, yes, no); else pass(no, no, no);
           } else {
-            exps();
+            if (partial) pass(yes, yes, no); else pass(yes, no, yes);
           }
-          if (__any_sync(0xffffffffu, top > m + kLazy) || j < kTiles) {
+          if (j < kTiles || __any_sync(0xffffffffu, !(top <= m + kLazy))) {
             float alpha = 1.f;
             if (top > m) {
               alpha = exp2_approx(m - top);
@@ -796,7 +835,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 tmem_store<32>(tmem + lanes + S::kSums + acc * DP + c * 32, o);
               }
             }
-            exps();
+            if (partial) pass(yes, yes, no); else pass(yes, no, no);
           }
           l += sum.x + sum.y;
 #pragma unroll
@@ -880,60 +919,58 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
 // thread adds up four columns of a row.
 constexpr int kPrefixJoinThreads = 256;
 constexpr int kPrefixJoinParts = kJoinParts + 2 * kPrefixCtas;
-__global__ void __launch_bounds__(kPrefixJoinThreads) topkv_prefix_join_kernel(const PrefixParams p) {
+__global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kernel(const PrefixParams p) {
   __shared__ float s_w[kJoinRows][kPrefixJoinParts];
-  __shared__ int64_t s_first[kJoinRows];
-  __shared__ int s_n[kJoinRows], s_step[kJoinRows];
   const AttendParams& a = p.a;
   pdl_wait_prior_grid();
   pdl_release_next_grid();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x, unit = blockIdx.y;
+  const int4 rec = a.joins[r];
+  const PrefixHeader t = *p.header;
+  const int lead = rec.x, behind = rec.z, units = gridDim.y;
+  if (behind < 0) return;  // written
   const int h = unit / a.gtiles, g0 = (unit - h * a.gtiles) * a.row_tile;
   const int per = (a.rows + gridDim.z - 1) / gridDim.z, row0 = blockIdx.z * per;
   const int rows = min(per, min(a.G - g0, a.row_tile) - row0);
   if (rows <= 0) return;
-  const int s = (int)min((int64_t)max(a.sl[r], 0), (int64_t)a.maxp * a.P);
-  const int4 rec = a.joins[r];
-  const int behind = rec.z, units = gridDim.y;
+  PrefixGroup g = {};
+  if (lead >= 0) g = p.groups[lead];
   const int64_t q_head0 = (int64_t)h * a.G + g0 + row0;
-  const int64_t b_first = ((int64_t)rec.y * units + unit) * a.rows + row0, b_step = (int64_t)units * a.rows;
-  // where the prefix parts of each row lie: kTiles to a team unless the accumulators hold different rows
-  const bool shares = shared_tokens(a, r, s) > 0;
-  if (tid < rows) {
-    int n = 0, step = 0;
-    int64_t first = 0;
-    if (shares) {
-      const int lead = a.plan[TOPKV_PLAN_LEADER * a.R + r];
-      const PrefixGroup g = prefix_group(p, lead);
-      const int row = (a.plan[TOPKV_PLAN_PLACE * a.R + r] - a.plan[TOPKV_PLAN_PLACE * a.R + lead]) * a.G + g0 + row0 + tid;
-      if (g.tokens > 0 && row < g.rows) {
-        const int i = row / (kPrefixRows * p.tiles);
-        const PrefixUnit u = prefix_unit(p, g, h, i);
-        const PrefixHeader t = *p.header;
-        const int64_t pos = p.begin[lead] + h * g.length + (int64_t)i * g.full;
-        const int t0 = prefix_team_of(t, pos), t1 = prefix_team_of(t, pos + u.length - 1);
-        first = u.slot + (int64_t)t0 * (kPrefixRows * p.tiles) + row - u.first_row;
-        step = u.both || p.tiles == 1 ? 0 : u.rows;  // from one part of a team to its other
-        n = (t1 - t0 + 1) * (step > 0 ? 2 : 1);
-      }
-    }
-    s_n[tid] = n;
-    s_step[tid] = step;
-    s_first[tid] = first;
-  }
-  __syncthreads();
-  // rows of parts: of part k >= behind of row g
-  auto prefix_part = [&](int g, int k) -> int64_t {
-    const int step = s_step[g];
-    return s_first[g] + (step > 0 ? (int64_t)(k >> 1) * (kPrefixRows * p.tiles) + (k & 1) * step : (int64_t)k * (kPrefixRows * p.tiles));
+  // Where the parts of row `row` lie: those behind the prefix at a constant stride; of the prefix one to a team, or
+  // two, `half` rows apart, where the accumulators hold the same rows.
+  const int64_t b_first = ((int64_t)rec.y * units + unit) * a.rows + row0;
+  const int b_step = units * a.rows, p_step = kPrefixRows * p.tiles;
+  auto prefix_parts = [&](int row, int64_t* first, int* half) {
+    *first = 0;
+    *half = 0;
+    const int at = rec.w * a.G + g0 + row0 + row;
+    if (lead < 0 || at < 0 || at >= g.rows) return 0;
+    const int i = at / p_step;
+    const PrefixUnit u = prefix_unit(p, g, h, i);
+    const int64_t pos = g.begin + h * g.length + (int64_t)i * g.full;
+    const int t0 = prefix_team_of(t, pos), t1 = prefix_team_of(t, pos + u.length - 1);
+    *first = u.slot + (int64_t)t0 * p_step + at - u.first_row;
+    *half = u.both || p.tiles == 1 ? 0 : u.rows;
+    return t1 - t0 + 1;
   };
-  for (int g = warp; g < rows; g += kPrefixJoinThreads / 32) {
-    const int parts = behind + s_n[g];
-    auto ml_of = [&](int k) { return k < behind ? a.ml[b_first + g + k * b_step] : p.ml[prefix_part(g, k - behind)]; };
-    float top = -INFINITY, sum = 0.f;
-    bool seen = false;
-    for (int k = lane; k < parts; k += 32) {
+  const int quads = a.Dv / 4, items = rows * quads;
+  for (int row = warp; row < rows; row += kPrefixJoinThreads / 32) {
+    int64_t first;
+    int half;
+    const int teams = prefix_parts(row, &first, &half), parts = behind + teams * (half > 0 ? 2 : 1);
+    // parts in the order: behind the prefix, the teams' first, the teams' second
+    auto ml_of = [&](int k) {
+      if (k < behind) return a.ml[b_first + row + (int64_t)k * b_step];
+      k -= behind;
+      return k < teams ? p.ml[first + (int64_t)k * p_step] : p.ml[first + half + (int64_t)(k - teams) * p_step];
+    };
+    // the first 32 parts are held by the lanes, the others read twice
+    float2 held = make_float2(-INFINITY, kNoneSeen);
+    if (lane < parts) held = ml_of(lane);
+    float top = held.y != kNoneSeen ? held.x : -INFINITY, sum = 0.f;
+    bool seen = held.y != kNoneSeen;
+    for (int k = lane + 32; k < parts; k += 32) {
       const float2 ml = ml_of(k);
       if (ml.y != kNoneSeen) {
         seen = true;
@@ -943,39 +980,47 @@ __global__ void __launch_bounds__(kPrefixJoinThreads) topkv_prefix_join_kernel(c
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float from = top == -INFINITY ? 0.f : top;
-    for (int k = lane; k < parts; k += 32) {
+    const float mine = held.y != kNoneSeen ? exp2_approx(held.x - from) : 0.f;
+    if (held.y != kNoneSeen) sum = mine * held.y;
+    for (int k = lane + 32; k < parts; k += 32) {
       const float2 ml = ml_of(k);
       const float w = ml.y != kNoneSeen ? exp2_approx(ml.x - from) : 0.f;
-      sum += w * ml.y;
-      s_w[g][k] = w;
+      if (ml.y != kNoneSeen) sum += w * ml.y;
+      s_w[row][k] = w;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     seen = __any_sync(0xffffffffu, seen);
     const float inv = seen ? a.v_scale / sum : 0.f;
-    __syncwarp();
-    for (int k = lane; k < parts; k += 32) s_w[g][k] *= inv;
-    if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)r * a.H * a.G + q_head0 + g] = seen ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    if (lane < parts) s_w[row][lane] = mine * inv;
+    for (int k = lane + 32; k < parts; k += 32) s_w[row][k] *= inv;
+    if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)r * a.H * a.G + q_head0 + row] = seen ? (top + log2f(sum)) * kLn2 : -INFINITY;
   }
   __syncthreads();
-  const int quads = a.Dv / 4, items = rows * quads;
   for (int i = tid; i < items; i += kPrefixJoinThreads) {
-    const int g = i / quads, d = (i - g * quads) * 4;
+    const int row = i / quads, d = (i - row * quads) * 4;
+    int64_t first;
+    int half;
+    const int teams = prefix_parts(row, &first, &half);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float* from, float f) {
-      const float4 v = *reinterpret_cast<const float4*>(from);
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
+    const float* w = s_w[row];
+    auto add = [&](const float* from, int64_t step, int n) {  // n parts at a constant stride
+#pragma unroll 8
+      for (int k = 0; k < n; ++k, from += step) {
+        const float f = w[k];
+        if (f == 0.f) continue;  // nothing was written where nothing was seen
+        const float4 v = *reinterpret_cast<const float4*>(from);
+        acc.x += f * v.x;
+        acc.y += f * v.y;
+        acc.z += f * v.z;
+        acc.w += f * v.w;
+      }
+      w += n;
     };
-#pragma unroll 4
-    for (int k = 0; k < behind; ++k)
-      add(a.part + (b_first + g + k * b_step) * a.Dv + d, s_w[g][k]);
-#pragma unroll 4
-    for (int k = 0; k < s_n[g]; ++k)
-      if (s_w[g][behind + k] != 0.f) add(p.part + prefix_part(g, k) * a.Dv + d, s_w[g][behind + k]);
-    store_io4(a.out + r * a.o_req + (q_head0 + g) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
+    add(a.part + (b_first + row) * a.Dv + d, (int64_t)b_step * a.Dv, behind);
+    add(p.part + first * a.Dv + d, (int64_t)p_step * a.Dv, teams);
+    if (half > 0) add(p.part + (first + half) * a.Dv + d, (int64_t)p_step * a.Dv, teams);
+    store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
   }
 }
 

@@ -23,8 +23,11 @@ def dev():
 
 @pytest.fixture(autouse=True)
 def clean(dev):
+    """However little is shared, it is formed once: these cases are small."""
     tk.check(tk.topkv_reset_device_error_flags())
+    before = tk.topkv_set_sharing_bytes(0)
     yield
+    tk.topkv_set_sharing_bytes(before)
     assert tk.topkv_device_error_flags() == 0
 
 
@@ -280,3 +283,30 @@ def test_large_plan(dev):
     tk.check(tk.topkv_plan_prefixes(tk.make_layout(1, 2, 1, 64, 2, 4, 10000), b, 8, plan))
     torch.cuda.synchronize()
     assert np.array_equal(plan.cpu().numpy(), ot.plan_prefixes(4, 10000, bt, sl, 8))
+
+
+def test_small_groups_are_left_to_their_requests(dev):
+    """The default limit: nothing here saves that much, alone or mixed with a group that does."""
+    groups = [(9, [40, 70, 0]), (3, [20, 30]), (0, [0, 17])]
+    for limit in (tk.TOPKV_DEFAULT_SHARING_BYTES, 2 * 9 * 16 * 2 * 2 * 64 * 2, 2 * 9 * 16 * 2 * 2 * 64 * 2 + 512):
+        tk.topkv_set_sharing_bytes(limit)
+        Case(dev, groups).check()
+    tk.topkv_set_sharing_bytes(tk.TOPKV_DEFAULT_SHARING_BYTES)
+    c = Case(dev, groups)
+    c.make_plan()
+    c.attend()
+    out, lse = c.result()
+    n = tk.check(tk.topkv_attend_workspace_bytes(c.lo, c.batch, c.att))
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+    tk.check(tk.topkv_attend_layer(0, c.pool, c.lo, c.batch, c.att, c.q, c.out, ws, n))
+    again, lse2 = c.result()
+    assert np.array_equal(out, again) and np.array_equal(lse, lse2)
+    # many short requests, a warp each
+    tk.topkv_set_sharing_bytes(0)
+    Case(dev, [(1, [1, 5] * 60), (0, [3] * 400)], H=8, G=1, D=16).check()
+    tk.topkv_set_sharing_bytes(tk.TOPKV_DEFAULT_SHARING_BYTES)
+    Case(dev, [(1, [1, 5] * 60), (0, [3, 0] * 200)], H=8, G=1, D=16).check()
+
+
+def test_sharing_limit_refuses_negative_values(dev):
+    assert tk.topkv_set_sharing_bytes(-1) == tk.TOPKV_ERR_INVALID_ARG and tk.topkv_set_sharing_bytes(0) == 0
