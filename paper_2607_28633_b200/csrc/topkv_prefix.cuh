@@ -142,7 +142,6 @@ constexpr int kPrefixLoadWarps = 2;
 constexpr int kPrefixMaxStages = 8;
 constexpr int kPrefixMaxRaw = 4;    // buffers of 8-bit tiles that wait to be converted
 constexpr int kPrefixCtas = 148;    // at most
-constexpr int kMixedPairs = 3;      // of eight pairs of weights, those on the multiply-add units
 
 struct PrefixControl {
   uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
@@ -266,30 +265,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
-// 2^x of two numbers on the multiply-add units, whose time is free while the other elements' exponentials keep the
-// special ones busy: x = n + f with |f| <= 1/2, a polynomial of degree 4 for 2^f (the one with the least
-// largest relative error, 2.6e-6, found by exchange), n added to the exponent. Below 2^-126 it stays there.
-// NaN does not survive it: callers use exp2_approx for tiles that hold any.
-__device__ __forceinline__ float2 exp2_multiply(float2 x) {
-  constexpr float kRound = 12582912.f;  // 1.5 * 2^23: sums with it are rounded to whole numbers
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
-  const float2 t = add2(x, make_float2(kRound, kRound));
-  const float2 f = fma2(add2(t, make_float2(-kRound, -kRound)), make_float2(-1.f, -1.f), x);
-  float2 y = fma2(f, make_float2(0x1.3997d6p-7f, 0x1.3997d6p-7f), make_float2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
-  y = fma2(y, f, make_float2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
-  y = fma2(y, f, make_float2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
-  y = fma2(y, f, make_float2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
-  y.x = __int_as_float(__float_as_int(y.x) + (__float_as_int(t.x) << 23));
-  y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(t.y) << 23));
-  return y;
-}
-// The larger of two, NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
 // What has been loaded is used only behind this, by name.
 __device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -297,11 +272,6 @@ __device__ __forceinline__ void tmem_loaded(uint32_t (&v)[32]) {
                  "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
                  "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
                  "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
-}
-__device__ __forceinline__ void tmem_loaded(uint32_t (&v)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
-                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 // Arrives at the barrier once this thread's copies so far are there.
 __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
@@ -461,26 +431,42 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   uint32_t done[2] = {0, 0};        // jobs before, by the buffer of scores they use
   uint32_t seg = 0;
   uint32_t issued = 0;              // load: entries whose copies are enqueued
-  PrefixGroup g = {};
-  int64_t off = ctl.off;
-  int lead = ctl.group[0];
-  g = PrefixGroup{lead, ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], 0, ctl.length, 0};
-  while (left > 0 && lead >= 0 && lead < a.R) {
-    // the unit, and the tiles [t0, t1) of it that are this CTA's
-    const int h = (int)(off / g.length);
-    const int64_t in_head = off - h * g.length;
-    const int i = (int)min(in_head / g.full, (int64_t)g.units - 1);
-    const PrefixUnit u = prefix_unit(p, g, h, i);
-    const int from = (int)(in_head - (int64_t)i * g.full);
-    const int take = (int)min(left, (int64_t)(u.length - from));
-    const int scale = u.both ? kTiles : 1;
-    const int t0 = (from + scale - 1) / scale, t1 = (from + take + scale - 1) / scale, count = t1 - t0;
-    const int jobs = count * scale;
-    const int64_t slot = u.slot + (int64_t)team * (kPrefixRows * kTiles);
-    auto page_column = [&](int x) { return a.page_shift >= 0 ? x >> a.page_shift : x / a.P; };
-    const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
+  auto page_column = [&](int x) { return a.page_shift >= 0 ? x >> a.page_shift : x / a.P; };
+  // Hands out what is this CTA's: tiles [t0, t1) of a unit at a time. Every role walks by itself, so that each has
+  // registers of its own.
+  auto walk = [&](auto body) {
+    PrefixGroup g{ctl.group[0], ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], 0, ctl.length, 0};
+    int64_t off = ctl.off, rest = left;
+    int lead = g.lead;
+    while (rest > 0 && lead >= 0 && lead < a.R) {
+      const int h = (int)(off / g.length);
+      const int64_t in_head = off - h * g.length;
+      const int i = (int)min(in_head / g.full, (int64_t)g.units - 1);
+      const PrefixUnit u = prefix_unit(p, g, h, i);
+      const int from = (int)(in_head - (int64_t)i * g.full);
+      const int take = (int)min(rest, (int64_t)(u.length - from));
+      const int scale = u.both ? kTiles : 1;
+      const int t0 = (from + scale - 1) / scale, t1 = (from + take + scale - 1) / scale, count = t1 - t0, jobs = count * scale;
+      body(g, u, t0, t1, jobs);
+      seq += count;
+      done[0] += (jobs + 1) / 2;
+      done[1] += jobs / 2;
+      if (jobs > 0) ++seg;
+      rest -= take;
+      off += take;
+      if (off == a.H * g.length && rest > 0) {
+        off = 0;
+        lead = next_group(p, lead + 1, lane);
+        if (lead < a.R) g = prefix_group(p, lead);
+      }
+    }
+  };
 
+  if (warp >= S::kSoftmaxWarps) {
     if (warp == kRawWarp || (!S::kConvert && warp >= kLoadWarp && warp < kIssueWarp)) {
+     walk([&](const PrefixGroup& g, const PrefixUnit& u, int t0, int t1, int jobs) {
+      const int h = u.h;
+      const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
       // ---- load: 16-bit tiles into the ring, 8-bit tiles into buffers of their own ------------------------
       constexpr int kWarps = S::kConvert ? 1 : kPrefixLoadWarps, kElem = S::kConvert ? 1 : 2;
       constexpr int kDepth = S::kConvert ? S::kRaws : kStages, kBytes = S::kConvert ? S::kRaw : S::kStage;
@@ -592,7 +578,10 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           cp_async_arrive(b_there + 8 * stage);
         }
       }
+     });
     } else if (S::kConvert && warp >= kLoadWarp && warp < kIssueWarp) {
+     walk([&](const PrefixGroup& g, const PrefixUnit& u, int t0, int t1, int jobs) {
+      const int count = t1 - t0;
       // ---- convert: 16 bytes of a row at a time, half of the rows each ----------------------------------
       constexpr int kRaws = S::kRaws > 0 ? S::kRaws : 1;
       constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kRows = kTokens / kPrefixLoadWarps;
@@ -620,21 +609,27 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           }
         }
         bar_arrive(b_raw_free + 8 * raw);
+        proxy_fence_smem();
         bar_arrive(b_full + 8 * stage);
       }
+     });
     } else if (warp == kIssueWarp) {
+     walk([&](const PrefixGroup& g, const PrefixUnit& u, int t0, int t1, int jobs) {
       // ---- products -----------------------------------------------------------------------------------
+      // 16-byte copies are a thread's own writes, which the products see only behind a fence; a loader's own would
+      // wait for all copies that it has under way. The first tile that comes so:
+      const int rows_from = S::kConvert ? t1 : a.box == 0 ? t0 : g.tokens % a.box == 0 ? t1 : g.tokens / kTokens;
       if (jobs > 0) wait(b_query, seg);
       const uint32_t q0 = operand_lo(base, 16);
       const uint32_t kv0 = operand_lo(base + kTiles * S::kQ, 16), v00 = operand_lo(base + kTiles * S::kQ, kBlock);
       for (int j = 0; j < jobs + 2; ++j) {
-        if (__any_sync(0xffffffffu, s_dead)) break;
+        if (s_dead) break;
         if (j >= 2) {
           const int jj = j - 2, b = jj & 1, t = u.both ? jj >> 1 : jj;
           const uint32_t entry = 2 * (seq + t) + 1, stage = entry % kStages;
           wait(b_weight + 8 * b, done[b] + (jj >> 1));
           wait(b_full + 8 * stage, entry / kStages);
-          proxy_fence_smem();  // what threads wrote and the barrier has shown, before the products read it
+          if (t0 + t >= rows_from) proxy_fence_smem();  // what threads wrote and the barrier has shown, before the products read it
           tcgen05_after_sync();
           const uint32_t d = tmem + S::kSums + (kTiles == 2 ? b * DP : 0), w = tmem + b * kTokens, v0 = v00 + stage * (S::kStage >> 4);
           if (elect_one()) {
@@ -650,7 +645,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           const int b = j & 1, t = u.both ? j >> 1 : j;
           const uint32_t entry = 2 * (seq + t), stage = entry % kStages;
           wait(b_full + 8 * stage, entry / kStages);
-          proxy_fence_smem();
+          if (t0 + t >= rows_from) proxy_fence_smem();
           tcgen05_after_sync();
           const uint32_t d = tmem + b * kTokens, k0 = kv0 + stage * (S::kStage >> 4), qa = q0 + (u.both ? b * (S::kQ >> 4) : 0);
           if (elect_one()) {
@@ -663,13 +658,18 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           __syncwarp();
         }
       }
-    } else if (warp < S::kSoftmaxWarps) {
+     });
+    }
+  } else {
+    walk([&](const PrefixGroup& g, const PrefixUnit& u, int t0, int t1, int jobs) {
+      const int h = u.h;
+      const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
+      const int64_t slot = u.slot + (int64_t)team * (kPrefixRows * kTiles);
       // ---- softmax ------------------------------------------------------------------------------------
       const int acc = warp >> 2, row = (warp & 3) * 32 + lane;        // accumulator, TMEM lane
       const uint32_t lanes = (uint32_t)(warp & 3) << 21;
       const int my_row = u.both ? acc * kPrefixRows + row : row;      // of the unit
       const bool live = my_row < u.rows;
-      float row_scale = a.qk_scale;
       if (jobs > 0) {
         // Q of the segment before is done with: both accumulators' last products have been waited for
         asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
@@ -682,56 +682,67 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
             mine = a.q + r * a.q_req + ((int64_t)h * a.G + gr - member * a.G) * a.q_head;
           }
           // kLanes lanes bring a row, so that a warp's accesses cover whole rows
-          constexpr int kLanes = DP / 8, kPer = 32 / kLanes, kAhead = 32 / kPer < 16 ? 32 / kPer : 16;
+          constexpr int kLanes = DP / 8, kPer = 32 / kLanes;
           const int chunks = a.D / 8, padded = ksteps * 2, c = lane % kLanes, sub = lane / kLanes;
-          uint8_t* const to = smem + (u.both ? acc * S::kQ : 0) + (c >> 3) * kQBlock + (warp & 3) * 32 * 128;
-          const uint32_t flip = a.qk_scale < 0.f ? 0x80008000u : 0u;  // scores times a factor that is not negative
+          const uint32_t tile = base + (u.both ? acc * S::kQ : 0) + (warp & 3) * 32 * 128;
+#pragma unroll 4
+          for (int k = 0; k < 32; k += kPer) {
+            const int rw = k + sub;
+            const uint8_t* src = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), rw));
+            const bool ok = src != nullptr && c < chunks;
+            if (c < padded) cp_async16(tile + (c >> 3) * kQBlock + rw * 128 + (((c & 7) ^ (rw & 7)) << 4), ok ? src + c * 16 : a.q, ok);
+          }
+          cp_async_commit();
+          cp_async_wait<0>();
+          __syncwarp();
+          // Scores times a factor that is not negative (a sign goes into Q) nor zero; bf16 queries over 8-bit keys
+          // become fp16 ones after a power of two for the row, see the kernel of the other tokens. A row a thread.
+          float row_scale = fmaxf(fabsf(a.qk_scale), 1e-30f);
+          const uint32_t flip = a.qk_scale < 0.f ? 0x80008000u : 0u;
+          const bool halves = TYPE == kE4m3 && a.io_bf16;
+          if (halves || flip) {
+            uint8_t* const at = smem + (tile - base) + lane * 128;
+            float up = 1.f, rest = 1.f;
+            if (halves) {
+              float top = 0.f;
 #pragma unroll 1
-          for (int k0 = 0; k0 < 32; k0 += kPer * kAhead) {
-            uint4 v[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-              const uint8_t* src = reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), k0 + k * kPer + sub));
-              v[k] = make_uint4(0, 0, 0, 0);
-              if (src != nullptr && c < chunks) v[k] = *reinterpret_cast<const uint4*>(src + c * 16);
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-              const int rw = k0 + k * kPer + sub;
-              float scale = fabsf(a.qk_scale);
-              if (TYPE == kE4m3 && a.io_bf16) {
-                // bf16 queries become fp16 ones after a power of two for the row; see the kernel of the other tokens
-                uint32_t x[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-                float top = 0.f;
+              for (int k = 0; k < chunks; ++k) {
+                const uint4 v = *reinterpret_cast<const uint4*>(at + (k >> 3) * kQBlock + (((k & 7) ^ (lane & 7)) << 4));
+                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                   top = fmaxf(top, fmaxf(fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u))));
-#pragma unroll
-                for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                int e = 0;
-                if (top > 0.f && top < INFINITY) e = ilogbf(top);
-                // in two steps: a single factor of 2^-e may itself leave the range of a float
-                const float up = exp2f((float)(-(e / 2))), rest = exp2f((float)(-(e - e / 2)));
-                scale = scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  x[i] = pack2<false>(__uint_as_float(x[i] << 16) * up * rest, __uint_as_float(x[i] & 0xffff0000u) * up * rest);
-                v[k] = make_uint4(x[0], x[1], x[2], x[3]);
               }
-              if (c == 0) ctl.row_scale[(u.both ? acc * kPrefixRows : 0) + (warp & 3) * 32 + rw] = scale;
-              v[k] = make_uint4(v[k].x ^ flip, v[k].y ^ flip, v[k].z ^ flip, v[k].w ^ flip);
-              if (c < padded) *reinterpret_cast<uint4*>(to + rw * 128 + (((c & 7) ^ (rw & 7)) << 4)) = v[k];
+              int e = 0;
+              if (top > 0.f && top < INFINITY) e = ilogbf(top);
+              // in two steps: a single factor of 2^-e may itself leave the range of a float
+              up = exp2f((float)(-(e / 2)));
+              rest = exp2f((float)(-(e - e / 2)));
+              row_scale = row_scale * exp2f((float)(e / 2)) * exp2f((float)(e - e / 2));
+            }
+#pragma unroll 1
+            for (int k = 0; k < chunks; ++k) {
+              uint4* const v = reinterpret_cast<uint4*>(at + (k >> 3) * kQBlock + (((k & 7) ^ (lane & 7)) << 4));
+              uint32_t x[4] = {v->x, v->y, v->z, v->w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (halves)
+                  x[e] = pack2<false>(__uint_as_float(x[e] << 16) * up * rest, __uint_as_float(x[e] & 0xffff0000u) * up * rest);
+                x[e] ^= flip;
+              }
+              *v = make_uint4(x[0], x[1], x[2], x[3]);
             }
           }
+          ctl.row_scale[my_row] = row_scale;
           proxy_fence_smem();
         }
         tcgen05_before_sync();
         asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
-        row_scale = ctl.row_scale[my_row];
         bar_arrive(b_query);
       }
+      const float row_scale = ctl.row_scale[my_row];
       const bool some = __any_sync(0xffffffffu, live);  // a row of this warp counts
-      float m = -INFINITY, l = 0.f, sub = 0.f;  // sub: what is subtracted from a score
+      float m = -INFINITY, l = 0.f, sub = 0.f;          // sub: what is subtracted from a score
       bool seen = false;
       int last = -1;  // this accumulator's last job
       for (int j = kTiles == 2 ? acc : 0; j < jobs; j += kTiles) {
@@ -744,73 +755,53 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         tcgen05_after_sync();
         last = j;
         if (some) {
-          // which of the tile's tokens count, 32 to a word
-          uint32_t valid[kTokens / 32];
+          // which of 32 tokens count; pages outside the pool are not visible, from the first one on every tile asks
           const int visible = g.tokens - t * kTokens;
-          const bool odd = ctl.odd;  // pages outside the pool are not visible: from the first one on every tile asks
-#pragma unroll
-          for (int c = 0; c < kTokens / 32; ++c) {
+          const bool odd = ctl.odd, partial = odd || visible < kTokens;
+          auto valid = [&](int c) {
             const int n = visible - c * 32;
-            valid[c] = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
-          }
-          if (odd) {
-#pragma unroll
-            for (int c = 0; c < kTokens / 32; ++c) {
+            uint32_t bits = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+            if (odd) {
               const int x = t * kTokens + c * 32 + lane;
               const int page = x < g.tokens ? bt_row[page_column(x)] : -1;
-              valid[c] &= __ballot_sync(0xffffffffu, page >= 0 && page < a.num_pages);
+              bits &= __ballot_sync(0xffffffffu, page >= 0 && page < a.num_pages);
             }
-          }
-          const bool partial = odd || visible < kTokens;
+            return bits;
+          };
+          // Two passes over the scores, whose code is kept short: it is fetched anew at every launch, at 9 cycles an
+          // instruction (unrolled over the whole row, in variants, the first tiles took 9,000 cycles each).
+          auto mask = [&](uint32_t (&x)[32], uint32_t bits) {
 #pragma unroll
-          for (int c = 0; c < kTokens / 32; ++c) seen |= valid[c] != 0;
-          // One pass as a rule: weights from the maximum so far, which stay in registers while the tile's own
-          // maximum is looked at; only if that exceeds it by more than 2^kLazy, or there is none yet, a second.
-          uint32_t w[kTokens / 2];
-          float2 sum;
-          float top;
-          auto pass = [&](auto exps, auto masked, auto mixed) {
-            constexpr bool kExps = decltype(exps)::value, kMasked = decltype(masked)::value, kMixed = decltype(mixed)::value;
-            const float2 by = make_float2(row_scale, row_scale), less = make_float2(-sub, -sub);
-            top = -INFINITY;
-            float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-            uint32_t raw[2][16];
-            tmem_load<16>(raw[0], s_col);
+            for (int k = 0; k < 32; ++k)
+              if (!(bits >> k & 1)) x[k] = 0xff800000u;  // minus infinity
+          };
+          float top = -INFINITY;
+          uint32_t counted = 0;
+          {
+            uint32_t x[2][32];
+            tmem_load<32>(x[0], s_col);
+#pragma unroll 1
+            for (int c = 0; c < kTokens / 32; c += 2) {
 #pragma unroll
-            for (int c = 0; c < kTokens / 16; ++c) {
-              uint32_t(&x)[16] = raw[c & 1];
-              tmem_loaded(x);
-              if (c + 1 < kTokens / 16) tmem_load<16>(raw[(c + 1) & 1], s_col + (c + 1) * 16);
-#pragma unroll
-              for (int k = 0; k < 16; k += 2) {
-                float2 s = make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-                const uint32_t bits = kMasked ? valid[c / 2] >> (c % 2 * 16 + k) : 3u;
-                const bool v0 = bits & 1, v1 = bits & 2;
-                top = max_nan(top, max_nan(v0 ? s.x : -INFINITY, v1 ? s.y : -INFINITY));
-                if constexpr (kExps) {
-                  s = fma2(s, by, less);
-                  if (kMixed && (k / 2) % 8 < kMixedPairs) {
-                    s = exp2_multiply(s);
-                  } else {
-                    s.x = v0 ? exp2_approx(s.x) : 0.f;
-                    s.y = v1 ? exp2_approx(s.y) : 0.f;
-                  }
-                  part[k / 2 & 1] = add2(part[k / 2 & 1], s);
-                  w[c * 8 + k / 2] = pack2<kBf>(s.x, s.y);
+              for (int i = 0; i < 2; ++i) {
+                tmem_loaded(x[i]);
+                if (i == 0 || c + 2 < kTokens / 32) tmem_load<32>(x[i ^ 1], s_col + (c + i + 1) * 32);
+                if (partial) {
+                  const uint32_t bits = valid(c + i);
+                  counted |= bits;
+                  if (bits != 0xffffffffu) mask(x[i], bits);
                 }
+                float part[2] = {top, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < 32; ++k) part[k & 1] = fmaxf(part[k & 1], __uint_as_float(x[i][k]));
+                top = fmaxf(part[0], part[1]);
               }
             }
-            top = top == -INFINITY ? top : top * row_scale;
-            sum = add2(part[0], part[1]);
-          };
-          constexpr std::true_type yes{};
-          constexpr std::false_type no{};
-          if (j < kTiles) {
-            if (partial) pass(no, yes, no); else pass(no, no, no);
-          } else {
-            if (partial) pass(yes, yes, no); else pass(yes, no, yes);
           }
-          if (j < kTiles || __any_sync(0xffffffffu, !(top <= m + kLazy))) {
+          seen |= !partial || counted != 0;
+          top = top == -INFINITY ? top : top * row_scale;
+          // The reference moves only when it is exceeded by more than 2^kLazy.
+          if (__any_sync(0xffffffffu, top > m + kLazy)) {
             float alpha = 1.f;
             if (top > m) {
               alpha = exp2_approx(m - top);
@@ -825,8 +816,8 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 wait(b_sum + 8 * (b ^ 1), done[b ^ 1] + ((j - 1) >> 1));
                 tcgen05_after_sync();
               }
-              for (int c = 0; c < DP / 32; ++c) {
-                if (c * 32 >= a.D) break;
+#pragma unroll 1
+              for (int c = 0; c * 32 < a.D; ++c) {
                 uint32_t o[32];
                 tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + c * 32);
                 tmem_loaded(o);
@@ -835,12 +826,37 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 tmem_store<32>(tmem + lanes + S::kSums + acc * DP + c * 32, o);
               }
             }
-            if (partial) pass(yes, yes, no); else pass(yes, no, no);
           }
-          l += sum.x + sum.y;
+          const float2 by = make_float2(row_scale, row_scale), less = make_float2(-sub, -sub);
+          float2 sum[2] = {make_float2(l, 0.f), make_float2(0.f, 0.f)};
+          {
+            uint32_t x[2][32];
+            tmem_load<32>(x[0], s_col);
+#pragma unroll 1
+            for (int c = 0; c < kTokens / 32; c += 2) {
 #pragma unroll
-          for (int c = 0; c < kTokens / 64; ++c)  // over the scores, which have been read
-            tmem_store<32>(s_col + c * 32, *reinterpret_cast<const uint32_t(*)[32]>(&w[c * 32]));
+              for (int i = 0; i < 2; ++i) {
+                tmem_loaded(x[i]);
+                if (i == 0 || c + 2 < kTokens / 32) tmem_load<32>(x[i ^ 1], s_col + (c + i + 1) * 32);
+                if (partial) {
+                  const uint32_t bits = valid(c + i);
+                  if (bits != 0xffffffffu) mask(x[i], bits);
+                }
+                uint32_t w[16];
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                  float2 e = fma2(make_float2(__uint_as_float(x[i][k]), __uint_as_float(x[i][k + 1])), by, less);
+                  e.x = exp2_approx(e.x);
+                  e.y = exp2_approx(e.y);
+                  sum[k / 2 & 1] = add2(sum[k / 2 & 1], e);
+                  w[k / 2] = pack2<kBf>(e.x, e.y);
+                }
+                tmem_store<16>(s_col + (c + i) * 16, w);  // over scores that have been read
+              }
+            }
+          }
+          sum[0] = add2(sum[0], sum[1]);
+          l = sum[0].x + sum[0].y;
           tmem_wait_store();
         }
         tcgen05_before_sync();
@@ -866,7 +882,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         const int c = lane % kChunks, sub = lane / kChunks;
 #pragma unroll 1
         for (int half = 0; half < 2 && half * kWide < a.D; ++half) {
-#pragma unroll
+#pragma unroll 1
           for (int k = 0; k < kWide / 32; ++k) {
             uint32_t o[32];
             tmem_load<32>(o, tmem + lanes + S::kSums + acc * DP + half * kWide + k * 32);
@@ -878,7 +894,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           }
           __syncwarp();
           float* const out = p.part + (to - lane) * a.Dv + half * kWide;
-#pragma unroll 8
+#pragma unroll 4
           for (int r0 = 0; r0 < 32; r0 += kPer) {
             const int rw = r0 + sub, at = c ^ (rw & (kChunks - 1));
             const uint4 v = *reinterpret_cast<const uint4*>(mine + rw * (kWide * 4) + (c << 4));
@@ -889,18 +905,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
         }
       }
       tcgen05_before_sync();
-    }
-    seq += count;
-    done[0] += (jobs + 1) / 2;
-    done[1] += jobs / 2;
-    if (jobs > 0) ++seg;
-    left -= take;
-    off += take;
-    if (off == a.H * g.length && left > 0) {
-      off = 0;
-      lead = next_group(p, lead + 1, lane);
-      if (lead < a.R) g = prefix_group(p, lead);
-    }
+    });
   }
   cp_async_wait<0>();
   if (s_dead) {  // give the copies and products that are in flight a millisecond to end
