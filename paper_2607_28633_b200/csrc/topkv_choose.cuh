@@ -13,8 +13,10 @@
 //
 // What bounds it: the bounds, 2 D + 4 bytes a page and head (1/32 of a cache of 16-token pages), read once; in
 // small calls the chain table -> bounds -> keys -> four passes of 8 bits each over the keys -> list.
-// A cluster of 1 to 8 CTAs has one request and KV head, each CTA an equal share of its pages; histograms and
-// counts are added up through the cluster's shared memory.
+// A cluster of 1 to 8 CTAs has one request and KV head, each CTA an equal share of its pages. The keys go to the
+// first CTA's shared memory, which then selects alone (passes of the whole cluster, 1.5 us each for its
+// barrier and eight remote histograms, took 4 x 8,192 pages from 27 to 33 us); where they are more than it holds, each
+// keeps its own, and histograms and counts are added up through the cluster's shared memory.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -45,33 +47,33 @@ struct BoundParams {
   int window;
   int columns;          // that the window can touch
 };
-template <int TYPE>
-struct BoundElements {
-  static constexpr int kN = TYPE == kE4m3 ? 16 : 8;  // of 16 bytes
-};
-template <int TYPE>
-__device__ __forceinline__ void elements_of(const uint4& v, float (&x)[BoundElements<TYPE>::kN]) {
-  if constexpr (TYPE == kE4m3) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t h[2];
-      e4m3x4_to_f16(w[i], &h[0], &h[1]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[j]));
-        x[4 * i + 2 * j] = f.x;
-        x[4 * i + 2 * j + 1] = f.y;
-      }
-    }
-  } else {
-    unpack8<TYPE == kBf16>(v, x);
-  }
+// Pairs of 16-bit values; 8-bit ones are held as fp16, exactly. NaN wins.
+template <bool BF16>
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  if constexpr (BF16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
-// A warp per page and head: lanes over the 16-byte chunks of a key, groups of them over the tokens.
+template <bool BF16>
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  if constexpr (BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 both(uint32_t v) {
+  if constexpr (BF16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+// A warp per page and head: lanes over the 16-byte chunks of a key, groups of them over the tokens. Minima and
+// maxima stay in 16 bits, two to an instruction, which leaves registers for four CTAs of eight warps an SM with eight
+// accesses under way each.
 template <int TYPE>
-__global__ void __launch_bounds__(kBoundThreads) topkv_bound_pages_kernel(const BoundParams p) {
-  constexpr int N = BoundElements<TYPE>::kN;
+__global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bound_pages_kernel(const BoundParams p) {
+  constexpr bool kBf = TYPE == kBf16;
+  constexpr int N = TYPE == kE4m3 ? 16 : 8, kPairs = N / 2;  // elements of 16 bytes
   pdl_wait_prior_grid();
   pdl_release_next_grid();
   const int lane = threadIdx.x & 31;
@@ -95,22 +97,15 @@ __global__ void __launch_bounds__(kBoundThreads) topkv_bound_pages_kernel(const 
   }
   const int chunks = p.D / N, groups = 32 / chunks, group = lane / chunks, c = lane - group * chunks;
   const uint8_t* src = p.pool + (int64_t)page * p.S_page + (int64_t)h * p.S_head + c * 16;
-  float lo[N], hi[N];
-  bool nan = false;
+  uint32_t lo[kPairs], hi[kPairs];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    lo[i] = INFINITY;
-    hi[i] = -INFINITY;
+  for (int i = 0; i < kPairs; ++i) {
+    lo[i] = kBf ? 0x7f807f80u : 0x7c007c00u;  // infinity
+    hi[i] = kBf ? 0xff80ff80u : 0xfc00fc00u;
   }
-  auto take = [&](const uint4& v) {
-    float x[N];
-    elements_of<TYPE>(v, x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      nan |= x[i] != x[i];
-      lo[i] = fminf(lo[i], x[i]);
-      hi[i] = fmaxf(hi[i], x[i]);
-    }
+  auto take = [&](int i, uint32_t v) {
+    lo[i] = min2<kBf>(lo[i], v);
+    hi[i] = max2<kBf>(hi[i], v);
   };
   if (group < groups) {
     constexpr int kAhead = 8;
@@ -120,22 +115,42 @@ __global__ void __launch_bounds__(kBoundThreads) topkv_bound_pages_kernel(const 
       for (int u = 0; u < kAhead; ++u)
         if (t + u * groups < held) v[u] = *reinterpret_cast<const uint4*>(src + (int64_t)(t + u * groups) * p.S_tok);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (t + u * groups < held) take(v[u]);
+      for (int u = 0; u < kAhead; ++u) {
+        if (t + u * groups >= held) continue;
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (TYPE == kE4m3) {
+            uint32_t x, y;
+            e4m3x4_to_f16(w[i], &x, &y);
+            take(2 * i, x);
+            take(2 * i + 1, y);
+          } else {
+            take(i, w[i]);
+          }
+        }
+      }
     }
   }
   for (int k = 1; k < groups; ++k) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      lo[i] = fminf(lo[i], __shfl_sync(0xffffffffu, lo[i], (c + k * chunks) & 31));
-      hi[i] = fmaxf(hi[i], __shfl_sync(0xffffffffu, hi[i], (c + k * chunks) & 31));
+    for (int i = 0; i < kPairs; ++i) {
+      const uint32_t a = __shfl_sync(0xffffffffu, lo[i], (c + k * chunks) & 31), b = __shfl_sync(0xffffffffu, hi[i], (c + k * chunks) & 31);
+      lo[i] = min2<kBf>(lo[i], a);
+      hi[i] = max2<kBf>(hi[i], b);
     }
   }
   // the first group has them all from here on
   float most = 0.f;
+  bool nan = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (group == 0) most = fmaxf(most, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
+  for (int i = 0; i < kPairs; ++i) {
+    const float2 a = both<kBf>(lo[i]), b = both<kBf>(hi[i]);
+    if (group == 0) {
+      most = fmaxf(most, fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))));
+      nan |= a.x != a.x || a.y != a.y;
+    }
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
   if (__any_sync(0xffffffffu, nan)) most = NAN;
@@ -147,11 +162,12 @@ __global__ void __launch_bounds__(kBoundThreads) topkv_bound_pages_kernel(const 
     uint32_t w[2][N / 4] = {};
     if (usable) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int a = (int)fminf(fmaxf(floorf(__fdiv_rn(lo[i], step)), -127.f), 127.f);
-        const int b = (int)fminf(fmaxf(ceilf(__fdiv_rn(hi[i], step)), -127.f), 127.f);
-        w[0][i / 4] |= (uint32_t)(a & 255) << (i % 4 * 8);
-        w[1][i / 4] |= (uint32_t)(b & 255) << (i % 4 * 8);
+      for (int i = 0; i < kPairs; ++i) {
+        const float2 a = both<kBf>(lo[i]), b = both<kBf>(hi[i]);
+        auto low = [&](float x) { return (uint32_t)((int)fminf(fmaxf(floorf(__fdiv_rn(x, step)), -127.f), 127.f) & 255); };
+        auto high = [&](float x) { return (uint32_t)((int)fminf(fmaxf(ceilf(__fdiv_rn(x, step)), -127.f), 127.f) & 255); };
+        w[0][i / 2] |= (low(a.x) | low(a.y) << 8) << (i % 2 * 16);
+        w[1][i / 2] |= (high(b.x) | high(b.y) << 8) << (i % 2 * 16);
       }
     }
 #pragma unroll
@@ -194,6 +210,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
   const uint32_t u = __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr int kGatherKeys = 24 * 1024;  // pages of a request up to which one CTA of the cluster selects
 struct ChooseShared {
   uint32_t histogram[2][256];
   uint32_t count[2];                 // pages above the threshold, pages at it, of this CTA
@@ -202,14 +219,14 @@ struct ChooseShared {
 };
 
 // Dynamic shared memory: q8 [heads, a multiple of 16][pitch], t [heads], keys of this CTA's pages.
-template <int DP, bool BF16>
-__global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(const ChooseParams p) {
+template <int DP, bool BF16, bool GATHER>
+__global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(const ChooseParams p) {
   namespace cg = cooperative_groups;
-  constexpr int kSets = DP / 32;  // four 16-byte chunks each, of 2 D bytes
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ ChooseShared sh;
   cg::cluster_group cluster = cg::this_cluster();
-  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  int ctas = (int)cluster.num_blocks();
+  const int rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x / ctas, r = unit / p.H, h = unit - r * p.H;
   const int tiles = (p.G + kChooseRows - 1) / kChooseRows, heads = tiles * kChooseRows;
@@ -239,9 +256,46 @@ __global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(cons
   if (wanted == 0) return;
   // this CTA's pages
   const int each = ((end - firsts + ctas - 1) / ctas + 7) / 8 * 8;
-  const int j0 = min(firsts + rank * each, end), n = min(each, end - j0);
+  int j0 = min(firsts + rank * each, end), n = min(each, end - j0);
   const int32_t* bt_row = p.bt + (int64_t)r * p.maxp + j0;
-  uint32_t* const keys = p.keys != nullptr ? p.keys + (int64_t)unit * p.maxp + j0 : reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
+  uint32_t* keys = p.keys != nullptr ? p.keys + (int64_t)unit * p.maxp + j0 : reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
+  for (int i = tid; i < 256; i += kChooseThreads) sh.histogram[0][i] = sh.histogram[1][i] = 0;
+  if (GATHER && ctas > 1) {  // keys go to the first CTA, which has to have begun
+    cluster.sync();
+    keys = cluster.map_shared_rank(keys, 0) + (j0 - firsts);
+  }
+  // A warp has kAhead groups of eight pages under way at a time, the first ones while the queries are made.
+  constexpr int kSets = DP / 32;  // four 16-byte chunks each, of 2 D bytes
+  constexpr int kAhead = 16 / kSets < 4 ? 16 / kSets : 4;
+  constexpr int kHop = kChooseWarps * 8 * kAhead;
+  const int gr = lane >> 2, gc = lane & 3;
+  const int chunks = p.D / 8;  // of 16 bytes, of 2 D bytes
+  int page[kAhead];
+  uint4 v[kAhead][kSets];
+  float step[kAhead];
+  auto pages_of = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) page[u] = i + u * 8 + gr < n ? bt_row[i + u * 8 + gr] : -1;
+  };
+  auto bring = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const bool ok = page[u] >= 0 && page[u] < p.num_pages;
+      if (!ok && i + u * 8 + gr < n && gc == 0) raise_error(kErrTable);
+      const int64_t at = (int64_t)(ok ? page[u] : 0) * p.H + h;
+      step[u] = ok ? p.steps[at] : 0.f;
+      const int8_t* from = p.bounds + at * 2 * p.D + gc * 16;
+#pragma unroll
+      for (int k = 0; k < kSets; ++k) {
+        v[u][k] = make_uint4(0, 0, 0, 0);
+        if (ok && k * 4 + gc < chunks) v[u][k] = *reinterpret_cast<const uint4*>(from + k * 64);
+      }
+    }
+  };
+  const int i_first = warp * 8 * kAhead;
+  pages_of(i_first);
+  bring(i_first);
+  pages_of(i_first + kHop);
 
   // ---- the queries in 8 bits, negative part before positive part ------------------------------------
   for (int g = warp; g < heads; g += kChooseWarps) {
@@ -278,12 +332,9 @@ __global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(cons
     }
     for (int i = 2 * p.D + lane * 8; i < kSets * 64; i += 32 * 8) *reinterpret_cast<uint2*>(to + i) = make_uint2(0, 0);
   }
-  for (int i = tid; i < 256; i += kChooseThreads) sh.histogram[0][i] = sh.histogram[1][i] = 0;
   __syncthreads();
 
   // ---- scores: a warp takes eight pages at a time ----------------------------------------------------
-  const int gr = lane >> 2, gc = lane & 3;
-  const int chunks = p.D / 8;  // of 16 bytes, of 2 D bytes
   uint32_t qa[kSets][8];
   auto queries = [&](int tile) {
     const uint8_t* from = smem + (tile * kChooseRows + gr) * p.pitch + gc * 16;
@@ -301,52 +352,60 @@ __global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(cons
     }
   };
   queries(0);
-  auto page_of = [&](int i) { return i + gr < n ? bt_row[i + gr] : -1; };
-  int page = page_of(warp * 8);
-  for (int i = warp * 8; i < n; i += kChooseWarps * 8) {
-    const bool ok = page >= 0 && page < p.num_pages;
-    if (!ok && i + gr < n && gc == 0) raise_error(kErrTable);
-    const int64_t at = ((int64_t)(ok ? page : 0) * p.H + h);
-    const float step = ok ? p.steps[at] : 0.f;
-    const int8_t* from = p.bounds + at * 2 * p.D + gc * 16;
-    uint4 v[kSets];
+#pragma unroll 1
+  for (int i0 = i_first; i0 < n; i0 += kHop) {
 #pragma unroll
-    for (int k = 0; k < kSets; ++k) {
-      v[k] = make_uint4(0, 0, 0, 0);
-      if (ok && k * 4 + gc < chunks) v[k] = *reinterpret_cast<const uint4*>(from + k * 64);
-    }
-    page = page_of(i + kChooseWarps * 8);
-    float best[2] = {-INFINITY, -INFINITY};  // of pages 2 gc and 2 gc + 1
-    const float step2[2] = {__shfl_sync(0xffffffffu, step, gc * 8), __shfl_sync(0xffffffffu, step, gc * 8 + 4)};
-    for (int tile = 0; tile < tiles; ++tile) {
-      if (tiles > 1) queries(tile);
-      int c[4] = {0, 0, 0, 0};
+    for (int u = 0; u < kAhead; ++u) {
+      float best[2] = {-INFINITY, -INFINITY};  // of pages 2 gc and 2 gc + 1
+      const float step2[2] = {__shfl_sync(0xffffffffu, step[u], gc * 8), __shfl_sync(0xffffffffu, step[u], gc * 8 + 4)};
+#pragma unroll 1
+      for (int tile = 0; tile < tiles; ++tile) {
+        if (tiles > 1) queries(tile);
+        int c[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int k = 0; k < kSets; ++k) {
-        mma16832(c, qa[k][0], qa[k][1], qa[k][2], qa[k][3], v[k].x, v[k].y);
-        mma16832(c, qa[k][4], qa[k][5], qa[k][6], qa[k][7], v[k].z, v[k].w);
+        for (int k = 0; k < kSets; ++k) {
+          mma16832(c, qa[k][0], qa[k][1], qa[k][2], qa[k][3], v[u][k].x, v[u][k].y);
+          mma16832(c, qa[k][4], qa[k][5], qa[k][6], qa[k][7], v[u][k].z, v[u][k].w);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int g = tile * kChooseRows + gr + (e >> 1) * 8;
+          // kept finite, so that a sum of 0 stays 0
+          if (g < p.G) best[e & 1] = fmaxf(best[e & 1], __fmul_rn((float)c[e], fminf(__fmul_rn(s_t[g], step2[e & 1]), FLT_MAX)));
+        }
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int g = tile * kChooseRows + gr + (e >> 1) * 8;
-        // kept finite, so that a sum of 0 stays 0
-        if (g < p.G) best[e & 1] = fmaxf(best[e & 1], __fmul_rn((float)c[e], fminf(__fmul_rn(s_t[g], step2[e & 1]), FLT_MAX)));
+      for (int o = 4; o < 32; o <<= 1) {
+        best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
+        best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
+      }
+      if (gr < 2) {
+        const int j = i0 + u * 8 + 2 * gc + gr;
+        const float st = gr ? step2[1] : step2[0];
+        if (j < n) {
+          const uint32_t key = st < INFINITY ? score_key(__fadd_rn(gr ? best[1] : best[0], 0.f)) : 0xffffffffu;
+          keys[j] = key;
+          atomicAdd(&sh.histogram[0][key >> 24], 1u);
+        }
       }
     }
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
-      best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
+    if (i0 + kHop < n) {
+      bring(i0 + kHop);
+      pages_of(i0 + 2 * kHop);
     }
-    if (gr < 2) {
-      const int j = i + 2 * gc + gr;
-      const float st = gr ? step2[1] : step2[0];
-      if (j < n) {
-        const uint32_t key = st < INFINITY ? score_key(__fadd_rn(gr ? best[1] : best[0], 0.f)) : 0xffffffffu;
-        keys[j] = key;
-        atomicAdd(&sh.histogram[0][key >> 24], 1u);
-      }
+  }
+  if (GATHER && ctas > 1) {
+    __syncthreads();
+    if (rank > 0) {
+      const uint32_t mine = sh.histogram[0][tid];
+      if (mine > 0) atomicAdd(cluster.map_shared_rank(sh.histogram[0], 0) + tid, mine);
     }
+    cluster.sync();
+    if (rank > 0) return;
+    ctas = 1;
+    j0 = firsts;
+    n = end - firsts;
+    keys = reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
   }
 
   // ---- the key of the last page that is taken, 8 bits a pass ---------------------------------------
@@ -386,7 +445,7 @@ __global__ void __launch_bounds__(kChooseThreads) topkv_choose_pages_kernel(cons
   }
 
   // ---- the list: pages above that key, and the first `need` at it, in order of their columns ------------
-  const int per = (n + kChooseThreads - 1) / kChooseThreads;
+  const int per = (n + kChooseThreads - 1) / kChooseThreads | 1;  // odd: the threads' runs begin in different banks
   const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
   uint32_t mine[2] = {0, 0};
   for (int i = i0; i < i1; ++i) {

@@ -141,11 +141,12 @@ int launch_prefix_dim(const PrefixParams& p, cudaStream_t s) {
 
 // ---- chosen pages -----------------------------------------------------------------------------------
 constexpr uint32_t kChooseMaxHeads = 128;     // query heads per KV head: they are held in shared memory
-constexpr int64_t kChooseMaxKeys = 24 * 1024;  // pages of a CTA whose keys are
+constexpr int64_t kChooseMaxKeys = kGatherKeys;  // pages whose keys a CTA's are
 struct ChoosePlan {
   AttendPlan attend;
   int ctas;          // of a cluster
-  int64_t cap;       // pages of a CTA at most
+  bool gather;       // its first CTA has all keys
+  int64_t cap;       // keys of a CTA at most
   int64_t key_bytes; // of the workspace, where shared memory does not hold the keys
   int pitch, smem;
 };
@@ -167,7 +168,8 @@ int check_choice(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   // Two CTAs per SM are wanted, but none with fewer than 256 pages.
   plan->ctas = 1;
   while (plan->ctas < kChooseCluster && units * plan->ctas < 2 * 148 && b->max_pages_per_req / plan->ctas > 256) plan->ctas *= 2;
-  plan->cap = (b->max_pages_per_req + plan->ctas - 1) / plan->ctas + 8;
+  plan->gather = b->max_pages_per_req <= kGatherKeys;
+  plan->cap = plan->gather ? b->max_pages_per_req : (b->max_pages_per_req + plan->ctas - 1) / plan->ctas + 8;
   const bool inside = plan->cap <= kChooseMaxKeys;
   plan->key_bytes = inside ? 0 : units * b->max_pages_per_req * 4;
   plan->pitch = choose_columns((int)lo->head_dim) * 2 + 16;
@@ -176,12 +178,12 @@ int check_choice(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   return TOPKV_OK;
 }
 
-template <int DP, bool BF16>
+template <int DP, bool BF16, bool GATHER>
 int launch_choose2(const ChooseParams& p, const ChoosePlan& plan, int64_t units, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   constexpr int kMost = (int)kChooseMaxHeads * (DP * 2 + 20) + (int)kChooseMaxKeys * 4;
   static_assert(kMost + (int)sizeof(ChooseShared) <= kSmemBudget, "queries and keys fit a CTA");
-  const int st = raise_smem(topkv_choose_pages_kernel<DP, BF16>, kMost, &done);
+  const int st = raise_smem(topkv_choose_pages_kernel<DP, BF16, GATHER>, kMost, &done);
   if (st != TOPKV_OK) return st;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * plan.ctas));
@@ -196,11 +198,12 @@ int launch_choose2(const ChooseParams& p, const ChoosePlan& plan, int64_t units,
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return launched(cudaLaunchKernelEx(&cfg, topkv_choose_pages_kernel<DP, BF16>, p), 1);
+  return launched(cudaLaunchKernelEx(&cfg, topkv_choose_pages_kernel<DP, BF16, GATHER>, p), 1);
 }
 template <int DP>
 int launch_choose(const ChooseParams& p, const ChoosePlan& plan, int64_t units, bool bf16, cudaStream_t s) {
-  return bf16 ? launch_choose2<DP, true>(p, plan, units, s) : launch_choose2<DP, false>(p, plan, units, s);
+  if (plan.gather) return bf16 ? launch_choose2<DP, true, true>(p, plan, units, s) : launch_choose2<DP, false, true>(p, plan, units, s);
+  return bf16 ? launch_choose2<DP, true, false>(p, plan, units, s) : launch_choose2<DP, false, false>(p, plan, units, s);
 }
 
 int check_choice_workspace(const void* ws, int64_t bytes, int64_t needed) {
