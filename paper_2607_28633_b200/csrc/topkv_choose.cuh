@@ -7,16 +7,16 @@
 //
 // The sum is of whole numbers, and what is left are two roundings, so the choice does not depend on any order
 // of summation. With q8 split into its negative and its positive part the sum is one product over 2 D
-// elements, [negative | positive] . [lo | hi], formed by the warp-wide 8-bit matrix instruction: 16 heads by 8
-// pages by 32 elements. Elements may be paired in any order, so a thread brings 16 consecutive bytes of a page's bounds
-// at a time and keeps its queries in the matching order.
+// elements, [negative | positive] . [lo | hi], formed four 8-bit products and sums at an instruction; four threads
+// share a page, 16 consecutive bytes each at a time. (The warp-wide matrix instruction for 8-bit integers is
+// no help: 100 cycles each, 26,000 for 1,024 pages a CTA.)
 //
 // What bounds it: the bounds, 2 D + 4 bytes a page and head (1/32 of a cache of 16-token pages), read once; in
-// small calls the chain table -> bounds -> keys -> four passes of 8 bits each over the keys -> list.
+// small calls the chain table -> bounds -> keys -> three passes over the keys -> list.
 // A cluster of 1 to 8 CTAs has one request and KV head, each CTA an equal share of its pages. The keys go to the
-// first CTA's shared memory, which then selects alone (passes of the whole cluster, 1.5 us each for its
-// barrier and eight remote histograms, took 4 x 8,192 pages from 27 to 33 us); where they are more than it holds, each
-// keeps its own, and histograms and counts are added up through the cluster's shared memory.
+// first CTA's shared memory, which then selects alone (a pass of the whole cluster takes 1.5 us for its barrier and
+// the remote histograms); where they are more than it holds, each keeps its own, and histograms and counts are
+// added up through the cluster's shared memory.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -185,7 +185,6 @@ __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bo
 constexpr int kChooseThreads = 256;
 constexpr int kChooseWarps = kChooseThreads / 32;
 constexpr int kChooseCluster = 8;
-constexpr int kChooseRows = 16;  // heads of one matrix instruction
 struct ChooseParams {
   const int32_t* bt;
   const int32_t* sl;
@@ -200,25 +199,22 @@ struct ChooseParams {
   int budget, firsts, lasts;
   int pitch;            // bytes of a head's queries in shared memory
 };
-__device__ __forceinline__ void mma16832(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 // Rising floats as rising unsigned numbers.
 __device__ __forceinline__ uint32_t score_key(float x) {
   const uint32_t u = __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr int kChooseBits = 8, kChooseBins = 1 << kChooseBits;
 constexpr int kGatherKeys = 24 * 1024;  // pages of a request up to which one CTA of the cluster selects
 struct ChooseShared {
-  uint32_t histogram[2][256];
+  uint32_t histogram[2][kChooseBins];
+  uint32_t range[2];                 // the smallest and the largest key
   uint32_t count[2];                 // pages above the threshold, pages at it, of this CTA
   uint32_t sum[2][kChooseWarps];
-  uint32_t found[2];                 // the passes' digit, and how many of its pages are still wanted
+  uint32_t found[2];                 // the pass's digit, and how many of its pages are still wanted
 };
 
-// Dynamic shared memory: q8 [heads, a multiple of 16][pitch], t [heads], keys of this CTA's pages.
+// Dynamic shared memory: q8 [heads][pitch], t [heads], keys.
 template <int DP, bool BF16, bool GATHER>
 __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(const ChooseParams p) {
   namespace cg = cooperative_groups;
@@ -229,7 +225,7 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
   const int rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x / ctas, r = unit / p.H, h = unit - r * p.H;
-  const int tiles = (p.G + kChooseRows - 1) / kChooseRows, heads = tiles * kChooseRows;
+  const int heads = p.G;
   float* const s_t = reinterpret_cast<float*>(smem + heads * p.pitch);
   pdl_wait_prior_grid();
   pdl_release_next_grid();
@@ -259,10 +255,16 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
   int j0 = min(firsts + rank * each, end), n = min(each, end - j0);
   const int32_t* bt_row = p.bt + (int64_t)r * p.maxp + j0;
   uint32_t* keys = p.keys != nullptr ? p.keys + (int64_t)unit * p.maxp + j0 : reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
-  for (int i = tid; i < 256; i += kChooseThreads) sh.histogram[0][i] = sh.histogram[1][i] = 0;
+  for (int i = tid; i < kChooseBins; i += kChooseThreads) sh.histogram[0][i] = sh.histogram[1][i] = 0;
+  if (tid == 0) {
+    sh.range[0] = 0xffffffffu;
+    sh.range[1] = 0;
+  }
+  uint32_t* range = sh.range;
   if (GATHER && ctas > 1) {  // keys go to the first CTA, which has to have begun
     cluster.sync();
     keys = cluster.map_shared_rank(keys, 0) + (j0 - firsts);
+    range = cluster.map_shared_rank(range, 0);
   }
   // A warp has kAhead groups of eight pages under way at a time, the first ones while the queries are made.
   constexpr int kSets = DP / 32;  // four 16-byte chunks each, of 2 D bytes
@@ -335,57 +337,45 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
   __syncthreads();
 
   // ---- scores: a warp takes eight pages at a time ----------------------------------------------------
-  uint32_t qa[kSets][8];
-  auto queries = [&](int tile) {
-    const uint8_t* from = smem + (tile * kChooseRows + gr) * p.pitch + gc * 16;
-#pragma unroll
-    for (int k = 0; k < kSets; ++k) {
-      const uint4 a = *reinterpret_cast<const uint4*>(from + k * 64), b = *reinterpret_cast<const uint4*>(from + 8 * p.pitch + k * 64);
-      qa[k][0] = a.x;
-      qa[k][1] = b.x;
-      qa[k][2] = a.y;
-      qa[k][3] = b.y;
-      qa[k][4] = a.z;
-      qa[k][5] = b.z;
-      qa[k][6] = a.w;
-      qa[k][7] = b.w;
-    }
-  };
-  queries(0);
+  uint32_t least = 0xffffffffu, most = 0;
 #pragma unroll 1
   for (int i0 = i_first; i0 < n; i0 += kHop) {
+    float best[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      float best[2] = {-INFINITY, -INFINITY};  // of pages 2 gc and 2 gc + 1
-      const float step2[2] = {__shfl_sync(0xffffffffu, step[u], gc * 8), __shfl_sync(0xffffffffu, step[u], gc * 8 + 4)};
+    for (int u = 0; u < kAhead; ++u) best[u] = -INFINITY;
 #pragma unroll 1
-      for (int tile = 0; tile < tiles; ++tile) {
-        if (tiles > 1) queries(tile);
-        int c[4] = {0, 0, 0, 0};
+    for (int g = 0; g < heads; ++g) {
+      int dot[kAhead] = {};
+      const uint8_t* from = smem + g * p.pitch + gc * 16;
 #pragma unroll
-        for (int k = 0; k < kSets; ++k) {
-          mma16832(c, qa[k][0], qa[k][1], qa[k][2], qa[k][3], v[u][k].x, v[u][k].y);
-          mma16832(c, qa[k][4], qa[k][5], qa[k][6], qa[k][7], v[u][k].z, v[u][k].w);
-        }
+      for (int k = 0; k < kSets; ++k) {
+        const uint4 q = *reinterpret_cast<const uint4*>(from + k * 64);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int g = tile * kChooseRows + gr + (e >> 1) * 8;
-          // kept finite, so that a sum of 0 stays 0
-          if (g < p.G) best[e & 1] = fmaxf(best[e & 1], __fmul_rn((float)c[e], fminf(__fmul_rn(s_t[g], step2[e & 1]), FLT_MAX)));
+        for (int u = 0; u < kAhead; ++u) {
+          dot[u] = __dp4a((int)v[u][k].x, (int)q.x, dot[u]);
+          dot[u] = __dp4a((int)v[u][k].y, (int)q.y, dot[u]);
+          dot[u] = __dp4a((int)v[u][k].z, (int)q.z, dot[u]);
+          dot[u] = __dp4a((int)v[u][k].w, (int)q.w, dot[u]);
         }
       }
+      const float t = s_t[g];
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) {
-        best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
-        best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
+      for (int u = 0; u < kAhead; ++u) {
+        dot[u] += __shfl_xor_sync(0xffffffffu, dot[u], 1);
+        dot[u] += __shfl_xor_sync(0xffffffffu, dot[u], 2);
+        // kept finite, so that a sum of 0 stays 0
+        best[u] = fmaxf(best[u], __fmul_rn((float)dot[u], fminf(__fmul_rn(t, step[u]), FLT_MAX)));
       }
-      if (gr < 2) {
-        const int j = i0 + u * 8 + 2 * gc + gr;
-        const float st = gr ? step2[1] : step2[0];
+    }
+    if (gc == 0) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int j = i0 + u * 8 + gr;
         if (j < n) {
-          const uint32_t key = st < INFINITY ? score_key(__fadd_rn(gr ? best[1] : best[0], 0.f)) : 0xffffffffu;
+          const uint32_t key = step[u] < INFINITY ? score_key(__fadd_rn(best[u], 0.f)) : 0xffffffffu;
           keys[j] = key;
-          atomicAdd(&sh.histogram[0][key >> 24], 1u);
+          least = min(least, key);
+          most = max(most, key);
         }
       }
     }
@@ -394,13 +384,14 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
       pages_of(i0 + 2 * kHop);
     }
   }
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) {
+    atomicMin(range, least);
+    atomicMax(range + 1, most);
+  }
+  if (ctas > 1) cluster.sync(); else __syncthreads();
   if (GATHER && ctas > 1) {
-    __syncthreads();
-    if (rank > 0) {
-      const uint32_t mine = sh.histogram[0][tid];
-      if (mine > 0) atomicAdd(cluster.map_shared_rank(sh.histogram[0], 0) + tid, mine);
-    }
-    cluster.sync();
     if (rank > 0) return;
     ctas = 1;
     j0 = firsts;
@@ -408,15 +399,38 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
     keys = reinterpret_cast<uint32_t*>(smem + heads * (p.pitch + 4));
   }
 
-  // ---- the key of the last page that is taken, 8 bits a pass ---------------------------------------
-  uint32_t prefix = 0, need = (uint32_t)wanted;
+  // ---- the key of the last page that is taken, kChooseBits bits a pass --------------------------------
+  // The first pass begins at the highest bit in which keys differ, so that they spread over its bins.
+  least = sh.range[0];
+  most = sh.range[1];
+  for (int k = 0; k < ctas && ctas > 1; ++k) {
+    const uint32_t* there = cluster.map_shared_rank(sh.range, k);
+    least = min(least, there[0]);
+    most = max(most, there[1]);
+  }
+  int top = 32 - __clz((int)(least ^ most));  // bits below `top` are not known yet
+  uint32_t prefix = top < 32 ? most >> top << top : 0, need = (uint32_t)wanted;
 #pragma unroll 1
-  for (int pass = 0; pass < 4; ++pass) {
-    const int shift = 24 - 8 * pass, b = pass & 1;
+  for (int b = 0; top > 0; b ^= 1) {
+    const int shift = max(top - kChooseBits, 0);
+    const uint32_t digits = (1u << (top - shift)) - 1;
+#pragma unroll 8
+    for (int i = tid; i < n; i += kChooseThreads) {
+      const uint32_t key = keys[i];
+      if (top == 32 || (key ^ prefix) >> top == 0) atomicAdd(&sh.histogram[b][key >> shift & digits], 1u);
+    }
     if (ctas > 1) cluster.sync(); else __syncthreads();
-    // the whole cluster's histogram, summed by a thread per bin, and how many pages lie above each bin
-    uint32_t mine = 0;
-    for (int k = 0; k < ctas; ++k) mine += (ctas > 1 ? cluster.map_shared_rank(sh.histogram[b], k) : sh.histogram[b])[255 - tid];
+    // the whole cluster's histogram, a few bins a thread from the highest down, and how many pages lie above them
+    constexpr int kBins = kChooseBins / kChooseThreads;
+    const int bin0 = kChooseBins - 1 - tid * kBins;
+    uint32_t bin[kBins] = {}, mine = 0;
+    for (int k = 0; k < ctas; ++k) {
+      const uint32_t* there = ctas > 1 ? cluster.map_shared_rank(sh.histogram[b], k) : sh.histogram[b];
+#pragma unroll
+      for (int i = 0; i < kBins; ++i) bin[i] += there[bin0 - i];
+    }
+#pragma unroll
+    for (int i = 0; i < kBins; ++i) mine += bin[i];
     uint32_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -424,34 +438,51 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
       if (lane >= o) incl += up;
     }
     if (lane == 31) sh.sum[0][warp] = incl;
-    sh.histogram[b ^ 1][tid] = 0;
+    // the other buffer: read by all before the barrier above, filled behind the one below
+#pragma unroll
+    for (int i = 0; i < kBins; ++i) sh.histogram[b ^ 1][tid + i * kChooseThreads] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kChooseWarps; ++w)
       if (w < warp) incl += sh.sum[0][w];
-    if (incl >= need && incl - mine < need) {  // exactly one thread
-      sh.found[0] = 255 - tid;
-      sh.found[1] = need - (incl - mine);
+    uint32_t above = incl - mine;
+    if (incl >= need && above < need) {  // exactly one thread
+#pragma unroll
+      for (int i = 0; i < kBins; ++i) {
+        if (above < need && above + bin[i] >= need) {
+          sh.found[0] = bin0 - i;
+          sh.found[1] = need - above;
+          above = need;  // none of the bins below
+        } else {
+          above += bin[i];
+        }
+      }
     }
     __syncthreads();
     prefix |= sh.found[0] << shift;
     need = sh.found[1];
-    if (pass < 3) {
-      for (int i = tid; i < n; i += kChooseThreads) {
-        const uint32_t key = keys[i];
-        if ((key ^ prefix) >> shift == 0) atomicAdd(&sh.histogram[b ^ 1][key >> (shift - 8) & 255], 1u);
-      }
-    }
+    top = shift;
   }
 
   // ---- the list: pages above that key, and the first `need` at it, in order of their columns ------------
   const int per = (n + kChooseThreads - 1) / kChooseThreads | 1;  // odd: the threads' runs begin in different banks
   const int i0 = min(tid * per, n), i1 = min(i0 + per, n);
-  uint32_t mine[2] = {0, 0};
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = keys[i];
-    mine[0] += key > prefix;
-    mine[1] += key == prefix;
+  // which of up to 32 keys from i on are above, which at the threshold
+  auto look = [&](int i, uint32_t* above, uint32_t* at) {
+    *above = *at = 0;
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) {
+      if (i + k >= i1) break;
+      const uint32_t key = keys[i + k];
+      *above |= (uint32_t)(key > prefix) << k;
+      *at |= (uint32_t)(key == prefix) << k;
+    }
+  };
+  uint32_t mine[2] = {0, 0}, seen[2] = {0, 0};
+  for (int i = i0; i < i1; i += 32) {
+    look(i, &seen[0], &seen[1]);
+    mine[0] += __popc(seen[0]);
+    mine[1] += __popc(seen[1]);
   }
   uint32_t incl[2] = {mine[0], mine[1]};
 #pragma unroll
@@ -484,12 +515,15 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
     }
     cluster.sync();  // nobody leaves while its counts are read
   }
-  for (int i = i0; i < i1; ++i) {
-    const uint32_t key = keys[i];
-    const bool above = key > prefix, at = key == prefix;
-    if (above || (at && before[1] < need)) out[firsts + before[0] + min(before[1], need)] = j0 + i;
-    before[0] += above;
-    before[1] += at;
+  for (int i = i0; i < i1; i += 32) {
+    if (i1 - i0 > 32) look(i, &seen[0], &seen[1]);
+    for (uint32_t any = seen[0] | seen[1]; any != 0; any &= any - 1) {
+      const int k = __ffs(any) - 1;
+      const bool above = seen[0] >> k & 1;
+      if (above || before[1] < need) out[firsts + before[0] + min(before[1], need)] = j0 + i + k;
+      before[0] += above;
+      before[1] += !above;
+    }
   }
 }
 

@@ -173,8 +173,7 @@ int check_choice(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   const bool inside = plan->cap <= kChooseMaxKeys;
   plan->key_bytes = inside ? 0 : units * b->max_pages_per_req * 4;
   plan->pitch = choose_columns((int)lo->head_dim) * 2 + 16;
-  const int heads = (int)(G + kChooseRows - 1) / kChooseRows * kChooseRows;
-  plan->smem = heads * (plan->pitch + 4) + (inside ? (int)plan->cap * 4 : 0);
+  plan->smem = (int)G * (plan->pitch + 4) + (inside ? (int)plan->cap * 4 : 0);
   return TOPKV_OK;
 }
 
