@@ -116,8 +116,8 @@ __device__ __forceinline__ void append_store1(const AppendTo& to, int d, float x
 // CHUNKS: the rotated part begins, ends and is halved at multiples of eight elements (any rotation of
 // neighbours that begins and ends at such); otherwise elements are handled one pair at a time.
 template <bool BF16, bool E8, bool CHUNKS>
-__global__ void __launch_bounds__(kAppendThreads) topkv_append_kernel(const AppendParams p) {
-  __shared__ float2 s_turn[kAppendPairs];
+__global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const AppendParams p) {
+  __shared__ __align__(16) float2 s_turn[kAppendPairs];
   __shared__ int64_t s_place[kAppendThreads];  // offset of the token's page row in the slab, -1: left out
   __shared__ int s_position[kAppendThreads];
   const int tid = threadIdx.x;
@@ -125,17 +125,20 @@ __global__ void __launch_bounds__(kAppendThreads) topkv_append_kernel(const Appe
   pdl_release_next_grid();
   const int64_t t0 = (int64_t)blockIdx.x * p.tokens;
   const int n = (int)min((int64_t)p.tokens, p.num_rows - t0);
+  // The request of the CTA's first row: all offsets are looked at side by side, which takes one access where a
+  // search by halves takes one after the other.
+  int r0 = (int)min(t0, (int64_t)p.R);
+  if (p.cu != nullptr) {
+    r0 = 0;
+    for (int i = 0; i < p.R; i += kAppendThreads)
+      r0 += __syncthreads_count(i + tid < p.R && p.cu[min(i + tid, p.R - 1) + 1] <= t0);
+  }
   if (tid < n) {
     const int64_t t = t0 + tid;
-    int r = (int)min(t, (int64_t)p.R);
+    int r = p.cu != nullptr ? r0 : (int)min(t, (int64_t)p.R);
     int64_t behind = 1;  // rows of the request from this one on
     if (p.cu != nullptr) {
-      int lo = 0, hi = p.R;  // the last request that begins at or before t and holds it
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu[mid + 1] > t) hi = mid; else lo = mid + 1;
-      }
-      r = lo;
+      while (r < p.R && p.cu[r + 1] <= t) ++r;
       behind = r < p.R ? p.cu[r + 1] - t : 0;
       if (r < p.R && p.cu[r] > t) r = p.R;  // before the first request's rows
     }
@@ -154,8 +157,6 @@ __global__ void __launch_bounds__(kAppendThreads) topkv_append_kernel(const Appe
           place = (int64_t)page * p.S_page + ((int)i - j * p.P) * p.S_tok;
         position = p.positions != nullptr ? p.positions[t] : (int)i;
       }
-    } else if (p.cu != nullptr && t >= p.cu[p.R]) {
-      place = -1;  // spare rows
     }
     s_place[tid] = place;
     s_position[tid] = position;
@@ -188,55 +189,65 @@ __global__ void __launch_bounds__(kAppendThreads) topkv_append_kernel(const Appe
     }
     const bool two = turns && !p.pairs;
     const int by = step * gridDim.y;
-    row0 += blockIdx.y * step;
-    for (int k = 0; k < n; ++k) {
-      if (s_place[k] < 0) continue;
-      const float2* turn = s_turn + k * p.half + (p.pairs ? item * 4 : item * 8);
-      float2 cs[8];
-      if (turns) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (two || i < 4) cs[i] = turn[i];
+    // Rows of all the CTA's tokens behind each other, kAhead of them at a time, so that their loads run together.
+    constexpr int kAhead = 2;
+    int k = 0, row = row0 + blockIdx.y * step;
+    auto settle = [&] {  // to a row that exists, of a token that has a place; k == n: none is left
+      for (;;) {
+        while (k < n && row >= p.rows) {
+          row -= p.rows;
+          ++k;
+        }
+        if (k >= n || s_place[k] >= 0) return;
+        row += by;
       }
-      // two rows at a time, so that their loads run together
-      for (int row = row0; row < p.rows; row += 2 * by) {
-        const bool more = row + by < p.rows;
-        uint4 a[2], b[2];
+    };
+    settle();
+    while (k < n) {
+      uint4 a[kAhead], b[kAhead];
+      int at_k[kAhead], at_row[kAhead];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u && !more) break;
-          const uint8_t* src = append_from(p, t0 + k, row + u * by);
+      for (int u = 0; u < kAhead; ++u) {
+        at_k[u] = k;
+        at_row[u] = row;
+        if (k < n) {
+          const uint8_t* src = append_from(p, t0 + k, row);
           a[u] = *reinterpret_cast<const uint4*>(src + c0 * 16);
           if (two) b[u] = *reinterpret_cast<const uint4*>(src + c1 * 16);
+          row += by;
+          settle();
         }
+      }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u && !more) break;
-          const AppendTo to = append_to<E8>(p, t0 + k, row + u * by, s_place[k]);
-          const bool keys = row + u * by < p.Hq + p.H;
-          float x[8], y[8];
-          unpack8<BF16>(a[u], x);
-          if (two) {
-            unpack8<BF16>(b[u], y);
-            if (keys) {
+      for (int u = 0; u < kAhead; ++u) {
+        if (at_k[u] >= n) break;
+        const AppendTo to = append_to<E8>(p, t0 + at_k[u], at_row[u], s_place[at_k[u]]);
+        const bool keys = at_row[u] < p.Hq + p.H;
+        const float2* cs = s_turn + at_k[u] * p.half + (p.pairs ? item * 4 : item * 8);
+        float x[8], y[8];
+        unpack8<BF16>(a[u], x);
+        if (two) {
+          unpack8<BF16>(b[u], y);
+          if (keys) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float v = x[i] * cs[i].x - y[i] * cs[i].y;
-                y[i] = x[i] * cs[i].y + y[i] * cs[i].x;
-                x[i] = v;
-              }
-            }
-            append_store8<BF16, E8>(to, c1 * 8, y);
-          } else if (turns && keys) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float v = x[2 * i] * cs[i].x - x[2 * i + 1] * cs[i].y;
-              x[2 * i + 1] = x[2 * i] * cs[i].y + x[2 * i + 1] * cs[i].x;
-              x[2 * i] = v;
+            for (int i = 0; i < 8; ++i) {
+              const float2 c = cs[i];
+              const float v = x[i] * c.x - y[i] * c.y;
+              y[i] = x[i] * c.y + y[i] * c.x;
+              x[i] = v;
             }
           }
-          append_store8<BF16, E8>(to, c0 * 8, x);
+          append_store8<BF16, E8>(to, c1 * 8, y);
+        } else if (turns && keys) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 c = cs[i];
+            const float v = x[2 * i] * c.x - x[2 * i + 1] * c.y;
+            x[2 * i + 1] = x[2 * i] * c.y + x[2 * i + 1] * c.x;
+            x[2 * i] = v;
+          }
         }
+        append_store8<BF16, E8>(to, c0 * 8, x);
       }
     }
   } else {

@@ -465,7 +465,7 @@ int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const 
   const int64_t ctas = (p.num_rows + p.tokens - 1) / p.tokens;
   const int items = chunks ? (p.pairs ? p.half / 4 : p.half / 8) + p.D / 8 - p.half / 4 : p.D - p.half;
   const int64_t passes = ((int64_t)p.rows * items + 2 * kAppendThreads - 1) / (2 * kAppendThreads);
-  const unsigned y = (unsigned)std::max<int64_t>(1, std::min<int64_t>({(2 * 148 + ctas - 1) / ctas, passes, 65535}));
+  const unsigned y = (unsigned)std::max<int64_t>(1, std::min<int64_t>({(8 * 148 + ctas - 1) / ctas, passes, 65535}));
   const dim3 grid((unsigned)ctas, y);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool bf16 = tokens->io_type == TOPKV_TYPE_BF16, narrow = tokens->cache_type == TOPKV_TYPE_E4M3;
