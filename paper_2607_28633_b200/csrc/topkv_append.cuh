@@ -113,9 +113,10 @@ __device__ __forceinline__ void append_store1(const AppendTo& to, int d, float x
     store_io(to.p + 2 * d, x, BF16);
 }
 
-// CHUNKS: the rotated part begins, ends and is halved at multiples of eight elements (any rotation of
-// neighbours that begins and ends at such); otherwise elements are handled one pair at a time.
-template <bool BF16, bool E8, bool CHUNKS>
+// By chunks of eight elements if the rotated part begins, ends and is halved at multiples of eight (a rotation of
+// neighbours: begins and ends), otherwise one pair at a time.
+enum AppendWay { kByElements = 0, kByHalves = 1, kByNeighbours = 2 };
+template <bool BF16, bool E8, int WAY>
 __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const AppendParams p) {
   __shared__ __align__(16) float2 s_turn[kAppendPairs];
   __shared__ int64_t s_place[kAppendThreads];  // offset of the token's page row in the slab, -1: left out
@@ -171,8 +172,9 @@ __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const A
   }
   __syncthreads();
 
-  if constexpr (CHUNKS) {
-    const int chunks = p.D / 8, first = p.first / 8, turned = p.pairs ? p.half / 4 : p.half / 8;
+  if constexpr (WAY != kByElements) {
+    constexpr bool kPairs = WAY == kByNeighbours;
+    const int chunks = p.D / 8, first = p.first / 8, turned = kPairs ? p.half / 4 : p.half / 8;
     // items of a row: chunks of pairs that turn (halves: two chunks each), then the others
     const int items = turned + chunks - p.half / 4;
     const int step = kAppendThreads / items, item = tid % items;
@@ -187,10 +189,10 @@ __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const A
       c0 = item - turned;
       if (c0 >= first) c0 += p.half / 4;
     }
-    const bool two = turns && !p.pairs;
+    const bool two = turns && !kPairs;
     const int by = step * gridDim.y;
     // Rows of all the CTA's tokens behind each other, kAhead of them at a time, so that their loads run together.
-    constexpr int kAhead = 2;
+    constexpr int kAhead = kPairs ? 4 : 2;
     int k = 0, row = row0 + blockIdx.y * step;
     auto settle = [&] {  // to a row that exists, of a token that has a place; k == n: none is left
       for (;;) {
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const A
         if (k < n) {
           const uint8_t* src = append_from(p, t0 + k, row);
           a[u] = *reinterpret_cast<const uint4*>(src + c0 * 16);
-          if (two) b[u] = *reinterpret_cast<const uint4*>(src + c1 * 16);
+          if (!kPairs && two) b[u] = *reinterpret_cast<const uint4*>(src + c1 * 16);
           row += by;
           settle();
         }
@@ -223,10 +225,10 @@ __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const A
         if (at_k[u] >= n) break;
         const AppendTo to = append_to<E8>(p, t0 + at_k[u], at_row[u], s_place[at_k[u]]);
         const bool keys = at_row[u] < p.Hq + p.H;
-        const float2* cs = s_turn + at_k[u] * p.half + (p.pairs ? item * 4 : item * 8);
+        const float2* cs = s_turn + at_k[u] * p.half + (kPairs ? item * 4 : item * 8);
         float x[8], y[8];
         unpack8<BF16>(a[u], x);
-        if (two) {
+        if (!kPairs && two) {
           unpack8<BF16>(b[u], y);
           if (keys) {
 #pragma unroll

@@ -26,6 +26,25 @@ int check_strides(std::initializer_list<int64_t> strides) {
   return TOPKV_OK;
 }
 
+// launch_pdl with clusters of `ctas` CTAs.
+template <typename... K, typename... P>
+cudaError_t launch_cluster(void (*kernel)(K...), unsigned ctas, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const P&... params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, params...);
+}
+
 // ---- new tokens ---------------------------------------------------------------------------------
 int check_new_tokens(const topkv_layout* lo, const topkv_batch* b, const topkv_new_tokens* n) {
   Resolved rs;
@@ -64,8 +83,10 @@ int check_new_tokens(const topkv_layout* lo, const topkv_batch* b, const topkv_n
 
 template <bool BF16, bool E8>
 int launch_append(const AppendParams& p, bool chunks, dim3 grid, cudaStream_t s) {
-  return launched(chunks ? launch_pdl(topkv_append_kernel<BF16, E8, true>, grid, dim3(kAppendThreads), 0, s, p)
-                         : launch_pdl(topkv_append_kernel<BF16, E8, false>, grid, dim3(kAppendThreads), 0, s, p), 1);
+  const dim3 block(kAppendThreads);
+  return launched(!chunks ? launch_pdl(topkv_append_kernel<BF16, E8, kByElements>, grid, block, 0, s, p)
+                  : p.pairs ? launch_pdl(topkv_append_kernel<BF16, E8, kByNeighbours>, grid, block, 0, s, p)
+                            : launch_pdl(topkv_append_kernel<BF16, E8, kByHalves>, grid, block, 0, s, p), 1);
 }
 
 // ---- shared prefixes ------------------------------------------------------------------------------
@@ -87,6 +108,10 @@ int check_shared(const topkv_layout* lo, const topkv_batch* b, const topkv_atten
   plan->tiles = lo->head_dim <= 128 ? 2 : 1;
   plan->tokens = lo->head_dim <= 128 ? 128 : 64;
   const int64_t R = b->num_requests, q_rows = (int64_t)at->num_q_heads * R;
+  // the line on which all units lie, tiles long, is counted in 32 bits
+  const __int128 units = q_rows / (kPrefixRows * plan->tiles) + lo->num_kv_heads * (R / 2 + 1);
+  const __int128 line = units * plan->tiles * (((int64_t)b->max_pages_per_req * lo->page_tokens) / plan->tokens + 1);
+  if (line > 0x7fffffff) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
   plan->own_rows = (R + (a.uncut ? 0 : a.teams)) * a.units * a.rows;
   plan->rows = plan->tiles * (q_rows + (int64_t)kPrefixCtas * kPrefixRows);
   plan->bytes = R == 0 ? 0
@@ -184,20 +209,8 @@ int launch_choose2(const ChooseParams& p, const ChoosePlan& plan, int64_t units,
   static_assert(kMost + (int)sizeof(ChooseShared) <= kSmemBudget, "queries and keys fit a CTA");
   const int st = raise_smem(topkv_choose_pages_kernel<DP, BF16, GATHER>, kMost, &done);
   if (st != TOPKV_OK) return st;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * plan.ctas));
-  cfg.blockDim = dim3(kChooseThreads);
-  cfg.dynamicSmemBytes = (size_t)plan.smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)plan.ctas;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return launched(cudaLaunchKernelEx(&cfg, topkv_choose_pages_kernel<DP, BF16, GATHER>, p), 1);
+  return launched(launch_cluster(topkv_choose_pages_kernel<DP, BF16, GATHER>, plan.ctas, dim3((unsigned)(units * plan.ctas)),
+                                 dim3(kChooseThreads), plan.smem, s, p), 1);
 }
 template <int DP>
 int launch_choose(const ChooseParams& p, const ChoosePlan& plan, int64_t units, bool bf16, cudaStream_t s) {
@@ -342,6 +355,7 @@ int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, in
   p.min_tokens = min_tokens;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const dim3 grid((unsigned)((p.R + kPrefixPlanThreads / 32 - 1) / (kPrefixPlanThreads / 32)));
+  if (p.R <= kPrefixPlanRows) return launched(launch_cluster(topkv_plan_cluster_kernel, grid.x, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);
   const int first = launched(launch_pdl(topkv_plan_leaders_kernel, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);
   if (first != TOPKV_OK) return first;
   return launched(launch_pdl(topkv_plan_groups_kernel, grid, dim3(kPrefixPlanThreads), 0, s, p), 1);

@@ -24,10 +24,10 @@
 // tokens behind the prefix, in order, so that results do not depend on timing.
 // Waits are bounded and TMEM is held as in the latent-row kernel.
 #pragma once
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
-#include <type_traits>
 
 #include "topkv_attend.cuh"
 #include "topkv_common.cuh"
@@ -36,7 +36,7 @@
 namespace topkv {
 
 // ---- the plan -------------------------------------------------------------------------------------
-constexpr int kPrefixPlanThreads = 256;
+constexpr int kPrefixPlanThreads = 1024;
 struct PrefixPlanParams {
   const int32_t* bt;
   const int32_t* sl;
@@ -48,21 +48,16 @@ struct PrefixPlanParams {
 __device__ __forceinline__ int full_pages(const PrefixPlanParams& p, int r) {
   return min(max(p.sl[r], 0) / p.P, p.maxp);
 }
-// A warp per row: the lowest row that begins with the same page, and how many pages both have in common.
-__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_leaders_kernel(const PrefixPlanParams p) {
-  pdl_wait_prior_grid();
-  pdl_release_next_grid();
-  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
-  if (r >= p.R) return;
+// A warp looks at a row: the lowest row that begins with the same page, and how many pages both have in common.
+__device__ __forceinline__ void plan_leader(const PrefixPlanParams& p, int r, int lane) {
   const int32_t* mine = p.bt + (int64_t)r * p.maxp;
   int full = full_pages(p, r), lead = r;
   const int page = full > 0 ? mine[0] : -1;
-  if (p.sl[r] < 0 || p.sl[r] > (int64_t)p.maxp * p.P) {
-    if (lane == 0) raise_error(kErrTable);
-  }
+  if (lane == 0 && (p.sl[r] < 0 || p.sl[r] > (int64_t)p.maxp * p.P)) raise_error(kErrTable);
+  constexpr int kAhead = 8;
   if (page >= 0 && page < p.num_pages) {
-    constexpr int kAhead = 4;
-    for (int q0 = 0; q0 < r; q0 += 32 * kAhead) {
+#pragma unroll 1
+    for (int q0 = 0; q0 < r && lead == r; q0 += 32 * kAhead) {
       bool same[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
@@ -74,31 +69,23 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_leaders_kernel(
         const uint32_t found = __ballot_sync(0xffffffffu, same[u]);
         if (found != 0) lead = q0 + u * 32 + __ffs(found) - 1;
       }
-      if (lead != r) break;
     }
   }
   const int32_t* first = p.bt + (int64_t)lead * p.maxp;
   full = min(full, full_pages(p, lead));
   int common = full;
-  if (lead != r) {
-    constexpr int kAhead = 4;
-    for (int j0 = 0; j0 < full; j0 += 32 * kAhead) {
-      bool differ[kAhead];
+#pragma unroll 1
+  for (int j0 = 0; lead != r && j0 < common; j0 += 32 * kAhead) {
+    bool differ[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int j = j0 + u * 32 + lane;
-        differ[u] = j < full && first[j] != mine[j];
-      }
-      int at = full;
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * 32 + lane;
+      differ[u] = j < full && first[j] != mine[j];
+    }
 #pragma unroll
-      for (int u = kAhead - 1; u >= 0; --u) {
-        const uint32_t found = __ballot_sync(0xffffffffu, differ[u]);
-        if (found != 0) at = j0 + u * 32 + __ffs(found) - 1;
-      }
-      if (at < full) {
-        common = at;
-        break;
-      }
+    for (int u = kAhead - 1; u >= 0; --u) {
+      const uint32_t found = __ballot_sync(0xffffffffu, differ[u]);
+      if (found != 0) common = j0 + u * 32 + __ffs(found) - 1;
     }
   }
   if (lane == 0) {
@@ -106,21 +93,18 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_leaders_kernel(
     p.plan[TOPKV_PLAN_COMMON * p.R + r] = common * p.P;
   }
 }
-// A warp per row: over all rows, what its group shares, its size, and the row's place in the order.
-__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(const PrefixPlanParams p) {
-  pdl_wait_prior_grid();
-  pdl_release_next_grid();
-  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
-  if (r >= p.R) return;
+// ... and, over all rows, what its group shares, its size, and the row's place in the order.
+__device__ __forceinline__ void plan_group(const PrefixPlanParams& p, int r, int lane) {
+  // written by other CTAs of the cluster, or by the launch before: read from L2
   const int32_t* leader = p.plan + TOPKV_PLAN_LEADER * p.R;
   const int32_t* common = p.plan + TOPKV_PLAN_COMMON * p.R;
-  const int lead = leader[r];
+  const int lead = __ldcg(leader + r);
   int shared = 0x7fffffff, members = 0, place = 0;
 #pragma unroll 4
   for (int q = lane; q < p.R; q += 32) {
-    const int l = leader[q];
+    const int l = __ldcg(leader + q), c = __ldcg(common + q);
     if (l == lead) {
-      shared = min(shared, common[q]);
+      shared = min(shared, c);
       ++members;
     }
     place += l < lead || (l == lead && q < r);
@@ -135,6 +119,30 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(c
     p.plan[TOPKV_PLAN_ORDER * p.R + place] = r;
   }
 }
+// A warp per row. Up to kPrefixPlanRows rows fit one cluster, whose barrier separates the two steps; more take a
+// launch each.
+constexpr int kPrefixPlanCluster = 8, kPrefixPlanRows = kPrefixPlanCluster * kPrefixPlanThreads / 32;
+__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_cluster_kernel(const PrefixPlanParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
+  if (r < p.R) plan_leader(p, r, lane);
+  __threadfence();
+  cooperative_groups::this_cluster().sync();
+  if (r < p.R) plan_group(p, r, lane);
+}
+__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_leaders_kernel(const PrefixPlanParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
+  if (r < p.R) plan_leader(p, r, lane);
+}
+__global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(const PrefixPlanParams p) {
+  pdl_wait_prior_grid();
+  pdl_release_next_grid();
+  const int lane = threadIdx.x & 31, r = blockIdx.x * (kPrefixPlanThreads / 32) + (threadIdx.x >> 5);
+  if (r < p.R) plan_group(p, r, lane);
+}
 
 // ---- the shared tokens' part ------------------------------------------------------------------------
 constexpr int kPrefixRows = 128;    // rows of a tile
@@ -145,10 +153,9 @@ constexpr int kPrefixCtas = 148;    // at most
 
 struct PrefixControl {
   uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
-  int64_t scan[16];
-  int64_t off;
-  int64_t length;  // of the first group's units per KV head ...
-  int group[7];    // ... and the rest of what is known of it; leader -1: nothing to do
+  int scan[16];
+  int off;
+  int group[8];    // what is known of the first group; leader -1: nothing to do
   uint32_t tmem;
   volatile int dead;
   volatile int odd;   // a page outside the pool has been met
@@ -181,15 +188,15 @@ struct PrefixGroup {
   int rows;          // members * G
   int units;         // per KV head
   int full;          // length of a unit of all rows
-  int pad;
-  int64_t length;    // of a KV head's units
-  int64_t begin;     // where the group's units begin on the line
+  int length;        // of a KV head's units
+  int begin;         // where the group's units begin on the line (the host has seen to it that this fits)
+  int pad[3];
 };
 // How the line is cut.
 struct PrefixHeader {
-  int64_t each;  // length of a range ...
+  int each;      // length of a range ...
   int more;      // ... and how many are one longer
-  int teams;
+  int teams, pad;
 };
 struct PrefixParams {
   AttendParams a;          // teams is that of the tokens behind the prefix
@@ -215,7 +222,7 @@ __device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int l
   const int tall = kPrefixRows * p.tiles, rest = (g.rows - 1) % tall + 1;
   g.units = (g.rows - 1) / tall + 1;
   g.full = g.n * p.tiles;
-  g.length = (int64_t)(g.units - 1) * g.full + (rest > kPrefixRows ? g.full : g.n);
+  g.length = (g.units - 1) * g.full + (rest > kPrefixRows ? g.full : g.n);
   return g;
 }
 // One unit: rows first_row .. first_row + rows - 1 of a group with one KV head.
@@ -236,9 +243,9 @@ __device__ __forceinline__ PrefixUnit prefix_unit(const PrefixParams& p, const P
   u.slot = p.tiles * ((int64_t)p.a.H * p.a.G * g.place + (int64_t)h * g.rows + u.first_row);
   return u;
 }
-__device__ __forceinline__ int prefix_team_of(const PrefixHeader& t, int64_t x) {
-  const int64_t wide = t.more * (t.each + 1);
-  return x < wide ? (int)(x / (t.each + 1)) : t.more + (int)((x - wide) / t.each);
+__device__ __forceinline__ int prefix_team_of(const PrefixHeader& t, int x) {
+  const int wide = t.more * (t.each + 1), past = x >= wide;
+  return (x - past * wide) / (t.each + 1 - past) + past * t.more;
 }
 // The next leader of a group that shares, from row r on (a whole warp asks); R if there is none.
 __device__ __forceinline__ int next_group(const PrefixParams& p, int r, int lane) {
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   }
 
   // ---- this CTA's range of the line --------------------------------------------------------------------
-  int64_t pos, left = 0;
+  int pos, left = 0;
   {
     const int per = (a.R + S::kThreads - 1) / S::kThreads;
     const int r0 = (int)min((int64_t)tid * per, (int64_t)a.R), r1 = min(r0 + per, a.R);
@@ -357,27 +364,27 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (per > 1 || g.n == 0) g = prefix_group(p, r);
       return g.tokens > 0 ? a.H * g.length : 0;
     };
-    int64_t mine = 0;
+    int mine = 0;
     for (int r = r0; r < r1; ++r) mine += length(r);
-    int64_t incl = mine;
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
     if (lane == 31) ctl.scan[warp] = incl;
     if (tid == 0) ctl.group[0] = -1;
     __syncthreads();
-    int64_t total = 0;
+    int total = 0;
     for (int w = 0; w < S::kThreads / 32; ++w) {
       if (w < warp) incl += ctl.scan[w];
       total += ctl.scan[w];
     }
     // a range is two tiles long at least: what a CTA costs to begin is about that
-    const int teams = (int)min((int64_t)gridDim.x, max((total + 1) / 2, (int64_t)1));
+    const int teams = min((int)gridDim.x, max((total + 1) / 2, 1));
     PrefixHeader t;
     t.each = total / teams;
-    t.more = (int)(total - t.each * teams);
+    t.more = total - t.each * teams;
     t.teams = teams;
     pos = t.each * team + min(team, t.more);
     if (team < teams) left = t.each + (team < t.more ? 1 : 0);
@@ -385,21 +392,20 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       pdl_wait_prior_grid();
       pdl_release_next_grid();
     }
-    int64_t at = incl - mine;
+    int at = incl - mine;
     const bool begins = left > 0 && pos >= at && pos < incl;  // exactly one thread
     if (begins || team == 0) {
       for (int r = r0; r < r1; ++r) {
-        const int64_t n = length(r);
+        const int n = length(r);
         if (team == 0 && n > 0) {
           g.begin = at;
           p.groups[r] = g;
         }
         if (begins && pos >= at && pos < at + n) {
           ctl.off = pos - at;
-          ctl.length = g.length;
-          const int known[7] = {r, g.place, g.tokens, g.n, g.rows, g.units, g.full};
+          const int known[8] = {r, g.place, g.tokens, g.n, g.rows, g.units, g.full, g.length};
 #pragma unroll
-          for (int i = 0; i < 7; ++i) ctl.group[i] = known[i];
+          for (int i = 0; i < 8; ++i) ctl.group[i] = known[i];
         }
         at += n;
       }
@@ -435,16 +441,13 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   // Hands out what is this CTA's: tiles [t0, t1) of a unit at a time. Every role walks by itself, so that each has
   // registers of its own.
   auto walk = [&](auto body) {
-    PrefixGroup g{ctl.group[0], ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], 0, ctl.length, 0};
-    int64_t off = ctl.off, rest = left;
+    PrefixGroup g{ctl.group[0], ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], ctl.group[7]};
+    int off = ctl.off, rest = left;
     int lead = g.lead;
     while (rest > 0 && lead >= 0 && lead < a.R) {
-      const int h = (int)(off / g.length);
-      const int64_t in_head = off - h * g.length;
-      const int i = (int)min(in_head / g.full, (int64_t)g.units - 1);
+      const int h = off / g.length, in_head = off - h * g.length, i = min(in_head / g.full, g.units - 1);
       const PrefixUnit u = prefix_unit(p, g, h, i);
-      const int from = (int)(in_head - (int64_t)i * g.full);
-      const int take = (int)min(rest, (int64_t)(u.length - from));
+      const int from = in_head - i * g.full, take = min(rest, u.length - from);
       const int scale = u.both ? kTiles : 1;
       const int t0 = (from + scale - 1) / scale, t1 = (from + take + scale - 1) / scale, count = t1 - t0, jobs = count * scale;
       body(g, u, t0, t1, jobs);
@@ -926,6 +929,8 @@ constexpr int kPrefixJoinThreads = 256;
 constexpr int kPrefixJoinParts = kJoinParts + 2 * kPrefixCtas;
 __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kernel(const PrefixParams p) {
   __shared__ float s_w[kJoinRows][kPrefixJoinParts];
+  __shared__ int64_t s_first[kJoinRows];
+  __shared__ int s_half[kJoinRows], s_teams[kJoinRows];
   const AttendParams& a = p.a;
   pdl_wait_prior_grid();
   pdl_release_next_grid();
@@ -946,24 +951,25 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
   // two, `half` rows apart, where the accumulators hold the same rows.
   const int64_t b_first = ((int64_t)rec.y * units + unit) * a.rows + row0;
   const int b_step = units * a.rows, p_step = kPrefixRows * p.tiles;
-  auto prefix_parts = [&](int row, int64_t* first, int* half) {
-    *first = 0;
-    *half = 0;
-    const int at = rec.w * a.G + g0 + row0 + row;
-    if (lead < 0 || at < 0 || at >= g.rows) return 0;
-    const int i = at / p_step;
-    const PrefixUnit u = prefix_unit(p, g, h, i);
-    const int64_t pos = g.begin + h * g.length + (int64_t)i * g.full;
-    const int t0 = prefix_team_of(t, pos), t1 = prefix_team_of(t, pos + u.length - 1);
-    *first = u.slot + (int64_t)t0 * p_step + at - u.first_row;
-    *half = u.both || p.tiles == 1 ? 0 : u.rows;
-    return t1 - t0 + 1;
-  };
   const int quads = a.Dv / 4, items = rows * quads;
   for (int row = warp; row < rows; row += kPrefixJoinThreads / 32) {
-    int64_t first;
-    int half;
-    const int teams = prefix_parts(row, &first, &half), parts = behind + teams * (half > 0 ? 2 : 1);
+    int64_t first = 0;
+    int half = 0, teams = 0;
+    const int mine_at = rec.w * a.G + g0 + row0 + row;
+    if (lead >= 0 && mine_at >= 0 && mine_at < g.rows) {
+      const int i = mine_at / p_step;
+      const PrefixUnit u = prefix_unit(p, g, h, i);
+      const int pos = g.begin + h * g.length + i * g.full, t0 = prefix_team_of(t, pos);
+      teams = prefix_team_of(t, pos + u.length - 1) - t0 + 1;
+      first = u.slot + (int64_t)t0 * p_step + mine_at - u.first_row;
+      half = u.both || p.tiles == 1 ? 0 : u.rows;
+    }
+    if (lane == 0) {
+      s_first[row] = first;
+      s_half[row] = half;
+      s_teams[row] = teams;
+    }
+    const int parts = behind + teams * (half > 0 ? 2 : 1);
     // parts in the order: behind the prefix, the teams' first, the teams' second
     auto ml_of = [&](int k) {
       if (k < behind) return a.ml[b_first + row + (int64_t)k * b_step];
@@ -1004,27 +1010,27 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
   __syncthreads();
   for (int i = tid; i < items; i += kPrefixJoinThreads) {
     const int row = i / quads, d = (i - row * quads) * 4;
-    int64_t first;
-    int half;
-    const int teams = prefix_parts(row, &first, &half);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* w = s_w[row];
-    auto add = [&](const float* from, int64_t step, int n) {  // n parts at a constant stride
+    const float* from = a.part + (b_first + row) * a.Dv + d;
+    int64_t step = (int64_t)b_step * a.Dv;
+    int n = behind;
+#pragma unroll 1
+    for (int range = 0; range < 3; ++range) {  // parts at a constant stride: behind the prefix, of it, and its other half
 #pragma unroll 8
       for (int k = 0; k < n; ++k, from += step) {
         const float f = w[k];
-        if (f == 0.f) continue;  // nothing was written where nothing was seen
-        const float4 v = *reinterpret_cast<const float4*>(from);
+        const float4 v = f != 0.f ? *reinterpret_cast<const float4*>(from) : make_float4(0.f, 0.f, 0.f, 0.f);  // 0: not written
         acc.x += f * v.x;
         acc.y += f * v.y;
         acc.z += f * v.z;
         acc.w += f * v.w;
       }
       w += n;
-    };
-    add(a.part + (b_first + row) * a.Dv + d, (int64_t)b_step * a.Dv, behind);
-    add(p.part + first * a.Dv + d, (int64_t)p_step * a.Dv, teams);
-    if (half > 0) add(p.part + (first + half) * a.Dv + d, (int64_t)p_step * a.Dv, teams);
+      n = range == 0 || s_half[row] > 0 ? s_teams[row] : 0;
+      step = (int64_t)p_step * a.Dv;
+      from = p.part + (s_first[row] + (range == 0 ? 0 : s_half[row])) * a.Dv + d;
+    }
     store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
   }
 }
