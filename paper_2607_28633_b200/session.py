@@ -6,8 +6,9 @@ layer's slab to pinned host memory with the checksummed host leg, and at the end
 layer from the host slab into its own paged pool, checksumming as it goes, and checks the
 headers when the last layer is in; a mismatch is reported per request so that the caller can
 retry (§3.1). ``DecodeCache`` is what the decode side does next with the pool it has received:
-it gives new tokens their pages, writes their K/V, attends to the cache, forks and frees
-requests and compacts the pool. All of them only enqueue work on the streams they are given,
+it gives new tokens their pages, writes their K/V (rotating them on the way), attends to the cache
+(to all of it, to shared prefixes once for all, or to chosen pages), forks and frees requests and
+compacts the pool. All of them only enqueue work on the streams they are given,
 library calls and, for the bookkeeping of new tokens, a few small tensor operations: no pack /
 unpack arithmetic happens in Python, and nothing here touches the CPU oracle.
 """
@@ -197,6 +198,10 @@ class DecodeCache:
         self._attend_ws: dict[int, torch.Tensor] = {}
         self._new = _NewTokens(self.seq_lens)
         self._first_rows = None
+        self.plan = torch.zeros((tk.TOPKV_PLAN_ROWS, rows), dtype=torch.int32, device=dev)
+        self._planned = False
+        self.bounds = self.steps = None
+        self._bounded: set[int] = set()  # layers whose pages all have bounds
         torch.cuda.current_stream(dev).synchronize()
 
     def _on(self, stream):
@@ -255,26 +260,107 @@ class DecodeCache:
             with self._on(stream):
                 new.all_written()
 
-    def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
-               window_tokens: int = 0, **attention):
-        """Attention of the newest token of every request; see topkv_attend_layer. ``q`` and ``out`` have
-        one entry per row, the empty ones included. ``attention`` goes to make_attention (value_dim,
-        sink_tokens, k_scale, v_scale, lse)."""
+    def append_rotated(self, layer: int, k: torch.Tensor, v: torch.Tensor | None, stream, rotary: tk.topkv_rotary | None = None,
+                       q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, cu_tokens: torch.Tensor | None = None,
+                       positions: torch.Tensor | None = None, cache_type: int | None = None, k_scale: float = 1.0, v_scale: float = 1.0):
+        """Writes the K/V of new tokens as a layer's projections leave them, K (and the queries, to ``q_out``)
+        rotated by the tokens' positions; see topkv_append_layer. ``k``, ``v``, ``q`` are [rows][heads][elements]: one
+        row per request, the empty ones included, or, with ``cu_tokens`` (device int64 [rows + 1]), the
+        rows that cu_tokens gives each. What is written follows ``append``: requests that have grown as far as
+        they asked. The rows of the others are skipped, in q_out too. The last layer's append ends the turn."""
+        if k.dtype not in (torch.bfloat16, torch.float16) or k.device != self.pool.device:
+            raise ValueError("k, v and q are bfloat16 or float16 on the pool's device")
+        if cu_tokens is None and k.shape[0] != len(self.seq_lens):
+            raise ValueError(f"{len(self.seq_lens)} rows, one per request, or cu_tokens")
+        if cu_tokens is not None and cu_tokens.numel() != len(self.seq_lens) + 1:
+            raise ValueError(f"cu_tokens has {len(self.seq_lens) + 1} entries")
+        if k.shape[1:] != (self.layout.num_kv_heads, self.layout.head_dim) or (v is None) != (self.layout.kv_factor == 1):
+            raise ValueError("k (and v, unless rows are latent) have the layout's heads and elements")
+        io = tk.TOPKV_TYPE_BF16 if k.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
+        new = self._new
+        n = tk.make_new_tokens(k, v, io if cache_type is None else cache_type, io, q=q, q_out=q_out, rotary=rotary, cu_tokens=cu_tokens,
+                               positions=positions, k_scale=k_scale, v_scale=v_scale)
+        b = tk.make_batch(self.block_table, new.lens if new.known else self.seq_lens)
+        tk.check(tk.topkv_append_layer(layer, self.pool, self.layout, b, n, k, v, q, q_out, stream))
+        if new.known and layer == self.layout.num_layers - 1:
+            with self._on(stream):
+                new.all_written()
+
+    def _attention(self, q: torch.Tensor, out: torch.Tensor, scale: float, cache_type: int | None, attention) -> tk.topkv_attention:
         if q.dtype not in (torch.bfloat16, torch.float16) or q.device != self.pool.device:
             raise ValueError("q and out are bfloat16 or float16 on the pool's device")
         if q.ndim != 3 or q.shape[0] != len(self.seq_lens) or q.shape[2] != self.layout.head_dim:
             raise ValueError(f"q is [{len(self.seq_lens)}][heads][{self.layout.head_dim}]")
         io = tk.TOPKV_TYPE_BF16 if q.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
-        att = tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
-        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=window_tokens)
-        n = tk.check(tk.topkv_attend_workspace_bytes(self.layout, b, att))
+        return tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
+
+    def _workspace(self, n: int, stream) -> torch.Tensor:
         # One per size (a kind of layer has one, whatever the lengths), kept as long as the cache: captured
         # graphs hold the address, and calls on other streams may still be using it.
         if n not in self._attend_ws:
             with self._on(stream):
                 self._attend_ws[n] = torch.empty(max(n, 16), dtype=torch.uint8, device=self.pool.device)
-        ws = self._attend_ws[n]
+        return self._attend_ws[n]
+
+    def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
+               window_tokens: int = 0, **attention):
+        """Attention of the newest token of every request; see topkv_attend_layer. ``q`` and ``out`` have
+        one entry per row, the empty ones included. ``attention`` goes to make_attention (value_dim,
+        sink_tokens, k_scale, v_scale, lse)."""
+        att = self._attention(q, out, scale, cache_type, attention)
+        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=window_tokens)
+        ws = self._workspace(tk.check(tk.topkv_attend_workspace_bytes(self.layout, b, att)), stream)
         tk.check(tk.topkv_attend_layer(layer, self.pool, self.layout, b, att, q, out, ws, ws.numel(), stream))
+
+    def plan_prefixes(self, stream, min_tokens: int = 0):
+        """Finds out which requests begin with the same pages, for ``attend_shared`` of all layers, until the next
+        fork or free. In a CUDA graph a plan stands together with the attention that uses it, or both are
+        made outside."""
+        tk.check(tk.topkv_plan_prefixes(self.layout, self.batch, min_tokens, self.plan, stream))
+        self._planned = True
+
+    def attend_shared(self, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream, cache_type: int | None = None,
+                      **attention):
+        """``attend``, with the tokens that requests share (forks, common prompts) read once for all of them; see
+        topkv_attend_shared_layer."""
+        if not self._planned:
+            raise ValueError("plan_prefixes comes first, and again after a fork or a free")
+        att = self._attention(q, out, scale, cache_type, attention)
+        ws = self._workspace(tk.check(tk.topkv_attend_shared_workspace_bytes(self.layout, self.batch, att)), stream)
+        tk.check(tk.topkv_attend_shared_layer(layer, self.pool, self.layout, self.batch, att, self.plan, q, out, ws, ws.numel(), stream))
+
+    def bound_pages(self, layer: int, stream, tokens: int = 0, cache_type: int | None = None):
+        """Bounds of the keys of the pages that hold the last ``tokens`` tokens of each request (0: of all pages), for
+        ``attend_chosen``. The first call for a layer, and the first after a fork or a compaction, takes all pages
+        whatever ``tokens`` says. cache_type: what the pool's 16-bit elements are, bfloat16 unless given."""
+        lo = self.layout
+        if cache_type is None:
+            cache_type = tk.TOPKV_TYPE_E4M3 if lo.elem_bytes == 1 else tk.TOPKV_TYPE_BF16
+        if not 0 <= layer < lo.num_layers or tokens < 0:
+            raise ValueError("a layer of the layout and a number of tokens")
+        if self.bounds is None:
+            shape = (lo.num_layers, lo.num_pool_pages, lo.num_kv_heads)
+            with self._on(stream):
+                self.bounds = torch.zeros((*shape, 2, lo.head_dim), dtype=torch.int8, device=self.pool.device)
+                self.steps = torch.zeros(shape, dtype=torch.float32, device=self.pool.device)
+        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens if layer in self._bounded else 0)
+        tk.check(tk.topkv_bound_pages_layer(layer, self.pool, lo, b, cache_type, self.bounds[layer], self.steps[layer], stream))
+        self._bounded.add(layer)
+
+    def attend_chosen(self, layer: int, q: torch.Tensor, out: torch.Tensor, chosen: torch.Tensor, scale: float, stream, first_pages: int = 1,
+                      last_pages: int = 1, cache_type: int | None = None, **attention):
+        """Attention to the pages that can score highest: ``chosen`` (device int32 [rows][kv heads][budget]) gets
+        their table columns; see topkv_choose_pages_layer and topkv_attend_pages_layer. ``bound_pages`` must have
+        seen the newest tokens."""
+        if layer not in self._bounded:
+            raise ValueError("bound_pages comes first, and again after a fork or a compaction")
+        if chosen.ndim != 3 or tuple(chosen.shape[:2]) != (len(self.seq_lens), self.layout.num_kv_heads) or chosen.dtype != torch.int32:
+            raise ValueError(f"chosen is int32 [{len(self.seq_lens)}][{self.layout.num_kv_heads}][budget]")
+        att = self._attention(q, out, scale, cache_type, attention)
+        choice = tk.make_page_choice(chosen.shape[2], first_pages, last_pages, self.bounds[layer], self.steps[layer], chosen)
+        ws = self._workspace(tk.check(tk.topkv_page_choice_workspace_bytes(self.layout, self.batch, att, choice)), stream)
+        tk.check(tk.topkv_choose_pages_layer(self.layout, self.batch, att, choice, q, ws, ws.numel(), stream))
+        tk.check(tk.topkv_attend_pages_layer(layer, self.pool, self.layout, self.batch, att, choice, q, out, ws, ws.numel(), stream))
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, stream):
         """Row children[i] becomes a copy of row parents[i] that shares its full pages."""
@@ -289,6 +375,8 @@ class DecodeCache:
             tk.check(tk.topkv_fork_requests(self.pool, self.layout, self.batch, self.tables, parents, children, parents.numel(),
                                             self.workspace, self.workspace.numel(), stream))
             self._new.forked(parents, children, before)
+        self._planned = False
+        self._bounded.clear()  # the last pages of children are new
 
     def free(self, rows: torch.Tensor, stream):
         """The rows (device int32) give their pages back and become empty."""
@@ -296,11 +384,13 @@ class DecodeCache:
         with self._on(stream):
             tk.check(tk.topkv_free_requests(self.layout, self.batch, self.tables, rows, rows.numel(), stream))
             self._new.freed(rows)
+        self._planned = False
 
     def compact(self, stream):
         """Afterwards pages 0 .. num_used - 1 are the ones in use; page_map has every page's new id."""
         tk.check(tk.topkv_compact_pages(self.pool, self.layout, self.batch, self.tables, self.num_used, self.page_map,
                                         self.workspace, self.workspace.numel(), stream))
+        self._bounded.clear()  # pages have other ids
 
 
 def transfer(sender: TransferSender, receiver: TransferReceiver, h_wire: torch.Tensor,
