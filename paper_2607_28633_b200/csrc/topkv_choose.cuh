@@ -42,10 +42,12 @@ struct BoundParams {
   float* steps;         // [pages][H]
   int64_t S_page, S_tok, S_head;
   int64_t num_pages;
-  int64_t items;        // R * columns * H
-  int maxp, P, H, D;
+  uint32_t items;       // R * columns * H
+  int maxp, P;
+  uint32_t H;
+  int D;
   int window;
-  int columns;          // that the window can touch
+  uint32_t columns;          // that the window can touch
 };
 // Pairs of 16-bit values; 8-bit ones are held as fp16, exactly. NaN wins.
 template <bool BF16>
@@ -77,20 +79,22 @@ __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bo
   pdl_wait_prior_grid();
   pdl_release_next_grid();
   const int lane = threadIdx.x & 31;
-  const int64_t item = (int64_t)blockIdx.x * (kBoundThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t item = blockIdx.x * (kBoundThreads / 32) + (threadIdx.x >> 5);
   if (item >= p.items) return;
-  const int64_t at = item / p.H;
-  const int h = (int)(item - at * p.H), r = (int)(at / p.columns);
+  const uint32_t at = item / p.H;
+  const int h = (int)(item - at * p.H), r = (int)(at / p.columns), column = (int)(at - (uint32_t)r * p.columns);
+  const int32_t* bt_row = p.bt + (int64_t)r * p.maxp;
+  int page = p.window > 0 ? 0 : bt_row[column];  // under way beside the length
   int s = p.sl[r];
   const int64_t row = (int64_t)p.maxp * p.P;
   if (s < 0 || s > row) {
     if (lane == 0) raise_error(kErrTable);
     s = s < 0 ? 0 : (int)row;
   }
-  const int first = p.window > 0 ? max(s - p.window, 0) / p.P : 0;
-  const int64_t j = first + (at - (int64_t)r * p.columns);
-  if (j * p.P >= s) return;
-  const int page = p.bt[(int64_t)r * p.maxp + j], held = min(p.P, s - (int)j * p.P);
+  const int j = (p.window > 0 ? max(s - p.window, 0) / p.P : 0) + column;
+  if ((int64_t)j * p.P >= s) return;
+  if (p.window > 0) page = bt_row[j];
+  const int held = min(p.P, s - j * p.P);
   if (page < 0 || page >= p.num_pages) {
     if (lane == 0) raise_error(kErrTable);
     return;

@@ -257,14 +257,15 @@ int topkv_bound_pages_layer(int layer, const void* pool, const topkv_layout* lay
   p.num_pages = layout->num_pool_pages;
   p.maxp = batch->max_pages_per_req;
   p.P = (int)layout->page_tokens;
-  p.H = (int)layout->num_kv_heads;
+  p.H = layout->num_kv_heads;
   p.D = (int)layout->head_dim;
   p.window = batch->window_tokens;
-  p.columns = p.maxp;
-  if (p.window > 0) p.columns = (int)std::min<int64_t>(p.maxp, ((int64_t)p.window + p.P - 2) / p.P + 1);
-  p.items = (int64_t)batch->num_requests * p.columns * p.H;
-  const int64_t ctas = (p.items + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
-  if (ctas > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  p.columns = (uint32_t)p.maxp;
+  if (p.window > 0) p.columns = (uint32_t)std::min<int64_t>(p.maxp, ((int64_t)p.window + p.P - 2) / p.P + 1);
+  const int64_t items = (int64_t)batch->num_requests * p.columns * p.H;
+  if (items > 0x7fffffffll) return TOPKV_ERR_UNSUPPORTED_LAYOUT;
+  p.items = (uint32_t)items;
+  const int64_t ctas = (items + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const dim3 grid((unsigned)ctas), block(kBoundThreads);
   return launched(cache_type == TOPKV_TYPE_BF16   ? launch_pdl(topkv_bound_pages_kernel<kBf16>, grid, block, 0, s, p)
