@@ -226,6 +226,11 @@ __global__ void __launch_bounds__(kAppendThreads, 4) topkv_append_kernel(const A
         const AppendTo to = append_to<E8>(p, t0 + at_k[u], at_row[u], s_place[at_k[u]]);
         const bool keys = at_row[u] < p.Hq + p.H;
         const float2* cs = s_turn + at_k[u] * p.half + (kPairs ? item * 4 : item * 8);
+        if (!(turns && keys) && !(E8 && to.narrow)) {  // as it is
+          *reinterpret_cast<uint4*>(to.p + c0 * 16) = a[u];
+          if (!kPairs && two) *reinterpret_cast<uint4*>(to.p + c1 * 16) = b[u];
+          continue;
+        }
         float x[8], y[8];
         unpack8<BF16>(a[u], x);
         if (!kPairs && two) {

@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bo
       }
     }
   }
-  for (int k = 1; k < groups; ++k) {
+  for (int k = 0; k < groups; ++k) {  // all groups' into each
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       const uint32_t a = __shfl_sync(0xffffffffu, lo[i], (c + k * chunks) & 31), b = __shfl_sync(0xffffffffu, hi[i], (c + k * chunks) & 31);
@@ -144,7 +144,6 @@ __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bo
       hi[i] = max2<kBf>(hi[i], b);
     }
   }
-  // the first group has them all from here on
   float most = 0.f;
   bool nan = false;
 #pragma unroll
@@ -162,26 +161,25 @@ __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bo
   const bool usable = step > 0.f && step < INFINITY;
   const int64_t to = (int64_t)page * p.H + h;
   if (lane == 0) p.steps[to] = step;
-  if (group == 0) {
-    uint32_t w[2][N / 4] = {};
+  // The first group divides the minima, the second the maxima (their negatives, rounded down as well): divisions are
+  // most of what this kernel computes.
+#pragma unroll 1
+  for (int e = group; group < groups && e < 2; e += groups) {
+    const float sign = e == 0 ? 1.f : -1.f;
+    uint32_t w[N / 4] = {};
     if (usable) {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
-        const float2 a = both<kBf>(lo[i]), b = both<kBf>(hi[i]);
-        auto low = [&](float x) { return (uint32_t)((int)fminf(fmaxf(floorf(__fdiv_rn(x, step)), -127.f), 127.f) & 255); };
-        auto high = [&](float x) { return (uint32_t)((int)fminf(fmaxf(ceilf(__fdiv_rn(x, step)), -127.f), 127.f) & 255); };
-        w[0][i / 2] |= (low(a.x) | low(a.y) << 8) << (i % 2 * 16);
-        w[1][i / 2] |= (high(b.x) | high(b.y) << 8) << (i % 2 * 16);
+        const float2 a = both<kBf>(e == 0 ? lo[i] : hi[i]);
+        auto whole = [&](float x) { return (uint32_t)((int)(sign * fminf(fmaxf(floorf(__fdiv_rn(sign * x, step)), -127.f), 127.f)) & 255); };
+        w[i / 2] |= (whole(a.x) | whole(a.y) << 8) << (i % 2 * 16);
       }
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      int8_t* out = p.bounds + (to * 2 + k) * p.D + c * N;
-      if constexpr (N == 16)
-        *reinterpret_cast<uint4*>(out) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-      else
-        *reinterpret_cast<uint2*>(out) = make_uint2(w[k][0], w[k][1]);
-    }
+    int8_t* out = p.bounds + (to * 2 + e) * p.D + c * N;
+    if constexpr (N == 16)
+      *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    else
+      *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
   }
 }
 
