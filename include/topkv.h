@@ -520,9 +520,10 @@ int topkv_rotary_turns(const double* h_frequencies, uint32_t n, uint64_t* h_turn
  *   PLACE    where r stands in that order
  * One group per first page: where some of its requests share more than all of them do, those tokens are
  * read by each. A caller that knows better may write a plan of its own: LEADER, SHARED, MEMBERS, ORDER and
- * PLACE are what attention reads. One that contradicts itself gives results without meaning, but no access
- * outside the pool and the tensors; a request shorter than SHARED is attended to on its own.
- * Two kernels on `stream`, no allocation, no synchronisation, capturable; batch->window_tokens must be 0. */
+ * PLACE are what attention reads. One that contradicts itself gives results without meaning (and may raise
+ * error bit 2), but no access outside the pool and the tensors; a request shorter than SHARED is attended to on its own.
+ * One or two kernels on `stream`, no allocation, no synchronisation, capturable; batch->window_tokens must be 0.
+ * Every row looks at every other one: fine for thousands of requests, not for a hundred thousand. */
 #define TOPKV_PLAN_ROWS 6
 enum { TOPKV_PLAN_LEADER = 0, TOPKV_PLAN_COMMON = 1, TOPKV_PLAN_SHARED = 2, TOPKV_PLAN_MEMBERS = 3,
        TOPKV_PLAN_ORDER = 4, TOPKV_PLAN_PLACE = 5 };
@@ -533,7 +534,10 @@ int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, in
  * row, which leaves nothing to gain), no window (window_tokens and sink_tokens 0). The weights of shared
  * tokens are rounded once to 16 bits for the second product (bf16 for a bf16 cache, else fp16), and
  * bf16 queries over an 8-bit cache become fp16 with a power of two for each row. Three kernels at most;
- * the workspace holds nothing between calls. TOPKV_FLAG_TABLES_SETTLED covers d_plan too. */
+ * the workspace holds nothing between calls, and calls that may run at the same time need one each.
+ * Capturable (the first call for a head size and type on a device raises the kernels' shared-memory limits: make
+ * it outside a capture). TOPKV_FLAG_TABLES_SETTLED covers d_plan too. TOPKV_ERR_UNSUPPORTED_LAYOUT also for batches
+ * whose prefixes could amount to more than 2^31 tiles of 128 tokens and rows. */
 int64_t topkv_attend_shared_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
                                             const topkv_attention* attention);
 int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* layout,
@@ -565,7 +569,7 @@ int64_t topkv_set_sharing_bytes(int64_t bytes);
  * a function of the inputs alone, and the newest page is always part of it. k_scale must be positive. */
 typedef struct topkv_page_choice {
   uint32_t struct_size;   /* = sizeof(topkv_page_choice)                                            */
-  uint32_t budget;        /* pages that a query sees, >= 1                                          */
+  uint32_t budget;        /* pages that a query sees, 1 .. 2^31 - 2^12                              */
   uint32_t first_pages;   /* table columns that are always among them ...                           */
   uint32_t last_pages;    /* ..., >= 1, from the front and the back                                  */
   const int8_t* bounds;   /* DEVICE int8 [num_pool_pages][num_kv_heads][2][head_dim] of the layer   */
@@ -581,7 +585,8 @@ typedef struct topkv_page_choice {
 int topkv_bound_pages_layer(int layer, const void* pool, const topkv_layout* layout,
                             const topkv_batch* batch, uint32_t cache_type, int8_t* d_bounds, float* d_steps,
                             topkv_stream_t stream);
-/* Bytes of d_workspace that either of the calls below needs, whatever the lengths. */
+/* Bytes of d_workspace that either of the calls below needs, whatever the lengths. Both are capturable, except
+ * for the first call for a head size and type on a device; at most 128 query heads per KV head. */
 int64_t topkv_page_choice_workspace_bytes(const topkv_layout* layout, const topkv_batch* batch,
                                           const topkv_attention* attention,
                                           const topkv_page_choice* choice);

@@ -179,7 +179,7 @@ int choose_columns(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
 int check_choice(const topkv_layout* lo, const topkv_batch* b, const topkv_attention* at, const topkv_page_choice* c, ChoosePlan* plan) {
   if (c == nullptr || c->struct_size != sizeof(topkv_page_choice)) return TOPKV_ERR_INVALID_ARG;
-  if (c->budget == 0 || c->budget > 0x7fffffffu || c->last_pages == 0 || c->first_pages > 0x7fffffffu || c->last_pages > 0x7fffffffu)
+  if (c->budget == 0 || c->budget > 0x7ffff000u || c->last_pages == 0 || c->first_pages > 0x7fffffffu || c->last_pages > 0x7fffffffu)
     return TOPKV_ERR_INVALID_ARG;
   const int st = check_attention(lo, b, at, &plan->attend, c->budget);
   if (st != TOPKV_OK) return st;

@@ -153,7 +153,7 @@ constexpr int kPrefixCtas = 148;    // at most
 
 struct PrefixControl {
   uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
-  int scan[16];
+  int64_t scan[16];
   int off;
   int group[8];    // what is known of the first group; leader -1: nothing to do
   uint32_t tmem;
@@ -265,6 +265,11 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 d;
   asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
@@ -364,26 +369,30 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (per > 1 || g.n == 0) g = prefix_group(p, r);
       return g.tokens > 0 ? a.H * g.length : 0;
     };
-    int mine = 0;
+    int64_t mine = 0;
     for (int r = r0; r < r1; ++r) mine += length(r);
-    int incl = mine;
+    int64_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
     if (lane == 31) ctl.scan[warp] = incl;
     if (tid == 0) ctl.group[0] = -1;
     __syncthreads();
-    int total = 0;
+    int64_t sum = 0;
     for (int w = 0; w < S::kThreads / 32; ++w) {
       if (w < warp) incl += ctl.scan[w];
-      total += ctl.scan[w];
+      sum += ctl.scan[w];
     }
+    // A plan whose groups overlap can come to more than the line counts: it has no work then (the host has seen to
+    // it that no other can).
+    const int total = sum <= 0x7fffffff ? (int)sum : 0;
+    if (sum > 0x7fffffff && tid == 0) raise_error(kErrTable);
     // a range is two tiles long at least: what a CTA costs to begin is about that
-    const int teams = min((int)gridDim.x, max((total + 1) / 2, 1));
+    const int teams = min((int)gridDim.x, (total + 1) / 2);
     PrefixHeader t;
-    t.each = total / teams;
+    t.each = total / max(teams, 1);
     t.more = total - t.each * teams;
     t.teams = teams;
     pos = t.each * team + min(team, t.more);
@@ -392,9 +401,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       pdl_wait_prior_grid();
       pdl_release_next_grid();
     }
-    int at = incl - mine;
+    int at = (int)(incl - mine);
     const bool begins = left > 0 && pos >= at && pos < incl;  // exactly one thread
-    if (begins || team == 0) {
+    if (begins || (team == 0 && total > 0)) {
       for (int r = r0; r < r1; ++r) {
         const int n = length(r);
         if (team == 0 && n > 0) {
@@ -796,7 +805,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
                 }
                 float part[2] = {top, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < 32; ++k) part[k & 1] = fmaxf(part[k & 1], __uint_as_float(x[i][k]));
+                for (int k = 0; k < 32; k += 2) part[k / 2 & 1] = max3(part[k / 2 & 1], __uint_as_float(x[i][k]), __uint_as_float(x[i][k + 1]));
                 top = fmaxf(part[0], part[1]);
               }
             }
@@ -952,11 +961,11 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
   const int64_t b_first = ((int64_t)rec.y * units + unit) * a.rows + row0;
   const int b_step = units * a.rows, p_step = kPrefixRows * p.tiles;
   const int quads = a.Dv / 4, items = rows * quads;
-  for (int row = warp; row < rows; row += kPrefixJoinThreads / 32) {
+  if (tid < rows) {
     int64_t first = 0;
     int half = 0, teams = 0;
-    const int mine_at = rec.w * a.G + g0 + row0 + row;
-    if (lead >= 0 && mine_at >= 0 && mine_at < g.rows) {
+    const int mine_at = rec.w * a.G + g0 + row0 + tid;
+    if (lead >= 0 && t.teams > 0 && mine_at >= 0 && mine_at < g.rows) {
       const int i = mine_at / p_step;
       const PrefixUnit u = prefix_unit(p, g, h, i);
       const int pos = g.begin + h * g.length + i * g.full, t0 = prefix_team_of(t, pos);
@@ -964,12 +973,30 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
       first = u.slot + (int64_t)t0 * p_step + mine_at - u.first_row;
       half = u.both || p.tiles == 1 ? 0 : u.rows;
     }
-    if (lane == 0) {
-      s_first[row] = first;
-      s_half[row] = half;
-      s_teams[row] = teams;
-    }
-    const int parts = behind + teams * (half > 0 ? 2 : 1);
+    s_first[tid] = first;
+    s_half[tid] = half;
+    s_teams[tid] = teams;
+  }
+  __syncthreads();
+  // part k of a row's columns d ..
+  auto part_of = [&](int row, int d, int k) {
+    if (k < behind) return reinterpret_cast<const float4*>(a.part + (b_first + row + (int64_t)k * b_step) * a.Dv + d);
+    const int teams = s_teams[row], second = k - behind >= teams;
+    return reinterpret_cast<const float4*>(p.part + (s_first[row] + second * s_half[row] + (int64_t)(k - behind - second * teams) * p_step) * a.Dv + d);
+  };
+  auto parts_of = [&](int row) { return behind + (s_half[row] > 0 ? 2 : 1) * s_teams[row]; };
+  // the first parts of a thread's first item are under way while the weights are formed
+  constexpr int kAhead = 6;
+  float4 ahead[kAhead];
+  {
+    const int row = tid / quads, d = (tid - row * quads) * 4, parts = tid < items ? parts_of(row) : 0;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (k < parts) ahead[k] = *part_of(row, d, k);
+  }
+  for (int row = warp; row < rows; row += kPrefixJoinThreads / 32) {
+    const int64_t first = s_first[row];
+    const int half = s_half[row], teams = s_teams[row], parts = parts_of(row);
     // parts in the order: behind the prefix, the teams' first, the teams' second
     auto ml_of = [&](int k) {
       if (k < behind) return a.ml[b_first + row + (int64_t)k * b_step];
@@ -1012,25 +1039,23 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
     const int row = i / quads, d = (i - row * quads) * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* w = s_w[row];
-    const float* from = a.part + (b_first + row) * a.Dv + d;
-    int64_t step = (int64_t)b_step * a.Dv;
-    int n = behind;
-#pragma unroll 1
-    for (int range = 0; range < 3; ++range) {  // parts at a constant stride: behind the prefix, of it, and its other half
-#pragma unroll 8
-      for (int k = 0; k < n; ++k, from += step) {
-        const float f = w[k];
-        const float4 v = f != 0.f ? *reinterpret_cast<const float4*>(from) : make_float4(0.f, 0.f, 0.f, 0.f);  // 0: not written
-        acc.x += f * v.x;
-        acc.y += f * v.y;
-        acc.z += f * v.z;
-        acc.w += f * v.w;
-      }
-      w += n;
-      n = range == 0 || s_half[row] > 0 ? s_teams[row] : 0;
-      step = (int64_t)p_step * a.Dv;
-      from = p.part + (s_first[row] + (range == 0 ? 0 : s_half[row])) * a.Dv + d;
+    const int parts = parts_of(row);
+    auto add = [&](const float4& v, float f) {
+      if (f == 0.f) return;  // not written where nothing was seen
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
+    };
+    int k = 0;
+    if (i == tid) {
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e)
+        if (e < parts) add(ahead[e], w[e]);
+      k = kAhead;
     }
+#pragma unroll 4
+    for (; k < parts; ++k) add(*part_of(row, d, k), w[k]);
     store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
   }
 }

@@ -310,3 +310,23 @@ def test_small_groups_are_left_to_their_requests(dev):
 
 def test_sharing_limit_refuses_negative_values(dev):
     assert tk.topkv_set_sharing_bytes(-1) == tk.TOPKV_ERR_INVALID_ARG and tk.topkv_set_sharing_bytes(0) == 0
+
+
+def test_a_plan_with_more_work_than_its_line_counts(dev):
+    """Every row its own leader of all rows behind it, a million tokens each: refused on the device."""
+    R, maxp, P = 2400, 4096, 256
+    lo = tk.make_layout(1, 2, 1, 16, 2, P, 1)
+    pool = torch.zeros(2 * P * 16, dtype=torch.bfloat16, device=dev)
+    bt, sl = torch.zeros((R, maxp), dtype=torch.int32, device=dev), torch.full((R,), maxp * P, dtype=torch.int32, device=dev)
+    row = torch.arange(R, dtype=torch.int32, device=dev)
+    plan = torch.stack([row, sl, sl, torch.full_like(row, R), row, row]).contiguous()
+    q = torch.zeros((R, 16, 16), dtype=torch.bfloat16, device=dev)
+    out = torch.full_like(q, 7.0)
+    b, att = tk.make_batch(bt, sl), tk.make_attention(q, out, TYPE["bf16"], TYPE["bf16"], 0.25)
+    n = tk.check(tk.topkv_attend_shared_workspace_bytes(lo, b, att))
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=dev)
+    torch.cuda.synchronize()
+    tk.check(tk.topkv_attend_shared_layer(0, pool, lo, b, att, plan, q, out, ws, n))
+    torch.cuda.synchronize()
+    assert tk.topkv_device_error_flags() == 2 and (out == 0).all()
+    tk.check(tk.topkv_reset_device_error_flags())
