@@ -547,10 +547,11 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
 
 /* A group's shared tokens are formed once only if that saves reading at least this many bytes of a layer, (members -
  * 1) * shared tokens of K and V of all heads; smaller groups are attended to request by request, which is
- * faster then (the default is the time of the additional kernel's start). Returns the previous value, or
+ * faster then (the default is the time of the additional kernel's start). For 8-bit caches, whose shared tokens are
+ * converted first, (members - 3) counts, but with 0 each group's are formed once. Returns the previous value, or
  * TOPKV_ERR_INVALID_ARG for a negative one. Process-wide; takes effect for calls made after it returns.
  * Results differ by rounding only. */
-#define TOPKV_DEFAULT_SHARING_BYTES (4 * 1024 * 1024)
+#define TOPKV_DEFAULT_SHARING_BYTES (8 * 1024 * 1024)
 int64_t topkv_set_sharing_bytes(int64_t bytes);
 
 /* ---- attention over chosen pages -------------------------------------------------------------------

@@ -174,7 +174,7 @@ def make_attention(q, out, cache_type: int, io_type: int, scale: float, value_di
 TOPKV_ROTARY_HALVES, TOPKV_ROTARY_PAIRS = 1, 2
 TOPKV_STRETCH_NONE, TOPKV_STRETCH_LINEAR, TOPKV_STRETCH_BASE, TOPKV_STRETCH_RAMP = 0, 1, 2, 3
 TOPKV_PLAN_ROWS = 6
-TOPKV_DEFAULT_SHARING_BYTES = 4 * 1024 * 1024
+TOPKV_DEFAULT_SHARING_BYTES = 8 * 1024 * 1024
 (TOPKV_PLAN_LEADER, TOPKV_PLAN_COMMON, TOPKV_PLAN_SHARED, TOPKV_PLAN_MEMBERS, TOPKV_PLAN_ORDER,
  TOPKV_PLAN_PLACE) = range(TOPKV_PLAN_ROWS)
 

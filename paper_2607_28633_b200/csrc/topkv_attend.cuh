@@ -91,7 +91,8 @@ struct AttendParams {
   // kBehindPrefix: requests that share or are cut leave parts, slot (r + team) of [R + teams] (uncut: r of
   // [R]), and a join record {r, first slot, parts, 0}; parts -1: the result is written
   const int32_t* plan;  // [rows of a plan][R]
-  int64_t least_saved;  // tokens of a group that need not be read again, from which on it is worth the work
+  int64_t least_saved;  // tokens of a group that need not be read again, from which on it is worth the work: (members -
+  int spent;            // spent) * shared ones; 3 for an 8-bit cache, see topkv_attend_shared_layer()
   // kChosenPages
   const int32_t* chosen;  // [R][H][budget] table columns
   int budget;
@@ -105,7 +106,7 @@ __device__ __forceinline__ int shared_tokens(const AttendParams& p, int r, int s
   const int rank = p.plan[TOPKV_PLAN_PLACE * p.R + r] - p.plan[TOPKV_PLAN_PLACE * p.R + lead];
   const int members = p.plan[TOPKV_PLAN_MEMBERS * p.R + lead];
   if (p.plan[TOPKV_PLAN_LEADER * p.R + lead] != lead || p.plan[TOPKV_PLAN_SHARED * p.R + lead] != n || p.sl[lead] < n ||
-      members < 2 || rank < 0 || rank >= members || (members - 1ll) * n < p.least_saved)
+      members < 2 || rank < 0 || rank >= members || (int64_t)(members - p.spent) * n < p.least_saved)
     return 0;
   return n;
 }

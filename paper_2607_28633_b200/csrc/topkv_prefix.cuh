@@ -214,7 +214,7 @@ __device__ __forceinline__ PrefixGroup prefix_group(const PrefixParams& p, int l
   // as shared_tokens() has it for the leader; all loads at once
   const int leader = a.plan[TOPKV_PLAN_LEADER * a.R + lead], shared = a.plan[TOPKV_PLAN_SHARED * a.R + lead];
   const int members = a.plan[TOPKV_PLAN_MEMBERS * a.R + lead], place = a.plan[TOPKV_PLAN_PLACE * a.R + lead], s = a.sl[lead];
-  g.tokens = leader == lead && members >= 2 && shared > 0 && shared <= s && (members - 1ll) * shared >= a.least_saved ? (int)min((int64_t)shared, (int64_t)a.maxp * a.P) : 0;
+  g.tokens = leader == lead && members >= 2 && shared > 0 && shared <= s && (int64_t)(members - a.spent) * shared >= a.least_saved ? (int)min((int64_t)shared, (int64_t)a.maxp * a.P) : 0;
   if (g.tokens == 0) return g;
   g.n = (g.tokens - 1) / p.tokens + 1;
   g.place = min(max(place, 0), a.R - 1);
@@ -932,14 +932,15 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
 
 // ---- join -------------------------------------------------------------------------------------------
 // A CTA takes up to kJoinRows heads of a request and KV head: parts of the tokens behind the prefix, then those
-// of the prefix, in order. First a warp per row turns the parts' maxima and sums into weights, then each
-// thread adds up four columns of a row.
+// of the prefix, in order. First a warp per row turns the parts' maxima and sums into weights, then threads add up
+// four columns of a row each, several of them a row's parts in turns where they would have nothing to do.
 constexpr int kPrefixJoinThreads = 256;
 constexpr int kPrefixJoinParts = kJoinParts + 2 * kPrefixCtas;
 __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kernel(const PrefixParams p) {
   __shared__ float s_w[kJoinRows][kPrefixJoinParts];
   __shared__ int64_t s_first[kJoinRows];
   __shared__ int s_half[kJoinRows], s_teams[kJoinRows];
+  __shared__ float4 s_sum[kPrefixJoinThreads];
   const AttendParams& a = p.a;
   pdl_wait_prior_grid();
   pdl_release_next_grid();
@@ -985,14 +986,19 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
     return reinterpret_cast<const float4*>(p.part + (s_first[row] + second * s_half[row] + (int64_t)(k - behind - second * teams) * p_step) * a.Dv + d);
   };
   auto parts_of = [&](int row) { return behind + (s_half[row] > 0 ? 2 : 1) * s_teams[row]; };
-  // the first parts of a thread's first item are under way while the weights are formed
+  // Where there are more threads than items, several share an item's parts: part k goes to thread k % split. The first
+  // parts of a thread's first item are under way while the weights are formed.
   constexpr int kAhead = 6;
+  const int split = max(1, kPrefixJoinThreads / items), turn = split > 1 ? tid / items : 0;
   float4 ahead[kAhead];
-  {
-    const int row = tid / quads, d = (tid - row * quads) * 4, parts = tid < items ? parts_of(row) : 0;
+  auto fetch = [&](int row, int d, int from, int parts) {  // parts from, from + split, ..; behind the last one the last one again
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (k < parts) ahead[k] = *part_of(row, d, k);
+    for (int e = 0; e < kAhead; ++e) ahead[e] = *part_of(row, d, min(from + e * split, parts - 1));
+  };
+  const int item = tid - turn * items;
+  if (item < items && turn < split) {
+    const int row = item / quads, parts = parts_of(row);
+    if (turn < parts) fetch(row, (item - row * quads) * 4, turn, parts);
   }
   for (int row = warp; row < rows; row += kPrefixJoinThreads / 32) {
     const int64_t first = s_first[row];
@@ -1035,29 +1041,42 @@ __global__ void __launch_bounds__(kPrefixJoinThreads, 4) topkv_prefix_join_kerne
     if (lane == 0 && a.lse != nullptr) a.lse[(int64_t)r * a.H * a.G + q_head0 + row] = seen ? (top + log2f(sum)) * kLn2 : -INFINITY;
   }
   __syncthreads();
-  for (int i = tid; i < items; i += kPrefixJoinThreads) {
+  for (int i = item; i < items && turn < split; i += kPrefixJoinThreads) {
     const int row = i / quads, d = (i - row * quads) * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* w = s_w[row];
     const int parts = parts_of(row);
-    auto add = [&](const float4& v, float f) {
-      if (f == 0.f) return;  // not written where nothing was seen
-      acc.x += f * v.x;
-      acc.y += f * v.y;
-      acc.z += f * v.z;
-      acc.w += f * v.w;
-    };
-    int k = 0;
-    if (i == tid) {
+    for (int k = turn; k < parts; k += kAhead * split) {
+      if (k != turn || i != item) fetch(row, d, k, parts);
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e)
-        if (e < parts) add(ahead[e], w[e]);
-      k = kAhead;
+      for (int e = 0; e < kAhead; ++e) {
+        // a part without weight may not have been written; no branch, so that the loads stay together
+        const float f = k + e * split < parts ? w[k + e * split] : 0.f;
+        acc.x = f != 0.f ? acc.x + f * ahead[e].x : acc.x;
+        acc.y = f != 0.f ? acc.y + f * ahead[e].y : acc.y;
+        acc.z = f != 0.f ? acc.z + f * ahead[e].z : acc.z;
+        acc.w = f != 0.f ? acc.w + f * ahead[e].w : acc.w;
+      }
     }
-#pragma unroll 4
-    for (; k < parts; ++k) add(*part_of(row, d, k), w[k]);
-    store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
+    if (split > 1) {
+      s_sum[tid] = acc;
+    } else {
+      store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + d * 2, acc, 1.f, a.io_bf16);
+    }
   }
+  if (split == 1) return;
+  __syncthreads();
+  if (tid >= items) return;
+  float4 acc = s_sum[tid];
+  for (int k = 1; k < split; ++k) {
+    const float4 v = s_sum[tid + k * items];
+    acc.x += v.x;
+    acc.y += v.y;
+    acc.z += v.z;
+    acc.w += v.w;
+  }
+  const int row = tid / quads;
+  store_io4(a.out + r * a.o_req + (q_head0 + row) * a.o_head + (tid - row * quads) * 8, acc, 1.f, a.io_bf16);
 }
 
 }  // namespace topkv

@@ -308,6 +308,26 @@ def test_small_groups_are_left_to_their_requests(dev):
     Case(dev, [(1, [1, 5] * 60), (0, [3, 0] * 200)], H=8, G=1, D=16).check()
 
 
+@pytest.mark.parametrize("limit", [1, 2 * 9 * 16 * 2 * 2 * 64, 1 << 40])
+def test_small_groups_of_an_8_bit_cache(dev, limit):
+    """Two and three members are left to their requests at any limit but 0, four and more by what they save."""
+    tk.topkv_set_sharing_bytes(limit)
+    Case(dev, [(9, [40, 70]), (8, [5, 0, 30]), (9, [1, 2, 3, 4]), (9, [9, 8, 7, 6, 5]), (0, [17, 0])], kind="e4m3", vs=0.5).check()
+
+
+@pytest.mark.parametrize("tails, kw", [
+    ([0], dict(H=8)),  # a request alone: nothing to join but its own parts
+    ([9, 100, 0, 2000], dict(H=8, D=128)),
+    ([3, 1], dict(H=1, D=64, G=1)),
+    ([3, 700, 0], dict(H=1, G=16, D=256)),
+    ([5, 60], dict(H=1, G=3, D=16, kind="e4m3")),
+    ([2] * 40, dict(H=2, G=8, D=128)),
+])
+def test_prefix_of_many_parts(dev, tails, kw):
+    """A long prefix of few heads is cut into many ranges: the join's threads share a row's parts, or have several rows."""
+    Case(dev, [(500, tails)], **kw).check()
+
+
 def test_sharing_limit_refuses_negative_values(dev):
     assert tk.topkv_set_sharing_bytes(-1) == tk.TOPKV_ERR_INVALID_ARG and tk.topkv_set_sharing_bytes(0) == 0
 
