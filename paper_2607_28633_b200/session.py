@@ -331,8 +331,10 @@ class DecodeCache:
 
     def bound_pages(self, layer: int, stream, tokens: int = 0, cache_type: int | None = None):
         """Bounds of the keys of the pages that hold the last ``tokens`` tokens of each request (0: of all pages), for
-        ``attend_chosen``: as many as any request has got since the call before for this layer. The first call for a layer, and the first after a fork or a compaction, takes all pages
-        whatever ``tokens`` says. cache_type: what the pool's 16-bit elements are, bfloat16 unless given."""
+        ``attend_chosen``: as many as any request has got since the call before for this layer. The first call for a
+        layer, and the first after a fork or a compaction, takes all pages whatever ``tokens`` says; make it outside a
+        CUDA graph, which repeats what it was captured with. cache_type: what the pool's 16-bit elements are, bfloat16
+        unless given."""
         lo = self.layout
         if cache_type is None:
             cache_type = tk.TOPKV_TYPE_E4M3 if lo.elem_bytes == 1 else tk.TOPKV_TYPE_BF16

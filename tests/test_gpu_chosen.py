@@ -285,3 +285,43 @@ def test_all_pages_chosen_is_plain_attention(dev):
     tk.check(tk.topkv_attend_layer(0, c.pool, c.lo, c.batch, c.att, c.q, c.out, ws, n))
     torch.cuda.synchronize()
     assert torch.equal(out, c.out) and np.array_equal(sparse[1], c.lse.double().cpu().numpy())
+
+
+def test_settled_tables_and_known_totals(dev):
+    c = Case(dev, [2000, 300, 0, 1], D=128, budget=40, firsts=2, lasts=3)
+    c.check()
+    lists, want = c.chosen.cpu().numpy(), None
+    for flags in (0, tk.TOPKV_FLAG_TABLES_SETTLED):
+        c.batch = tk.make_batch(c.d_bt, c.d_sl, total_tokens=2301, flags=flags)
+        c.n = tk.check(tk.topkv_page_choice_workspace_bytes(c.lo, c.batch, c.att, c.choice))
+        c.ws = torch.full((c.n + 32,), 0xFF, dtype=torch.uint8, device=dev)
+        for _ in range(4):
+            c.out.fill_(7.0)
+            c.chosen.fill_(-9)
+            c.choose()
+            c.attend()
+        assert np.array_equal(c.chosen.cpu().numpy(), lists)
+        want = want or c.want(lists)
+        _check(c.result(), want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_offsets_beyond_32_bits(dev, kind):
+    """Pages far apart: the bits of the same pages side by side."""
+    c = Case(dev, [150, 20], kind=kind, budget=5)
+    c.check()
+    near = [x.copy() for x in c.result()] + [c.chosen.cpu().numpy()]
+    far = 700_000_000
+    big = torch.zeros(c.g.num_pages * far, dtype=torch.uint8, device=dev)
+    big.view(c.g.num_pages, far)[:, :c.g.S_page] = c.pool.view(c.g.num_pages, c.g.S_page)
+    c.lo.pool_page_stride, c.lo.pool_layer_stride = far, c.g.num_pages * far
+    for t in (c.out, c.chosen):
+        t.fill_(7)
+    bounds, steps = c.bounds.clone(), c.steps.clone()
+    c.bounds.fill_(99)
+    c.steps.fill_(5)
+    tk.check(tk.topkv_bound_pages_layer(0, big, c.lo, c.batch, TYPE[kind], c.bounds, c.steps))
+    c.choose()
+    tk.check(tk.topkv_attend_pages_layer(0, big, c.lo, c.batch, c.att, c.choice, c.q, c.out, c.ws, c.n))
+    assert all(np.array_equal(a, b) for a, b in zip(near, list(c.result()) + [c.chosen.cpu().numpy()])) and c.g.num_pages * far > 1 << 32
+    assert torch.equal(bounds, c.bounds) and torch.equal(steps, c.steps)

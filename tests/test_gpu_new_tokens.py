@@ -187,3 +187,27 @@ def test_gradient_free_inverse(dev):
     # two roundings to fp16, each half a step of at most the pair's size
     assert ((back - x).float().abs() <= pair * 2 * 2.0 ** -11 * 1.01).all()
     assert not torch.equal(there, x) and torch.equal(pool.view(4, 8, D)[2, 5], back[0, 0])
+
+
+@pytest.mark.parametrize("kind, count", [("bf16", 64), ("e4m3", 64), ("bf16", 6)])
+def test_offsets_beyond_32_bits(dev, kind, count):
+    """Pages far apart get the bits that the same pages get side by side, and nothing around them."""
+    rng = np.random.default_rng(3)
+    sl, H, D, P = np.array([17, 64, 40]), 2, 64, 16
+    bt, pages = _table(sl, P, 2, 1, rng)
+    g = _geom(2, H, D, 1 if kind == "e4m3" else 2, P, pages)
+    lo = _layout(g)
+    k, v = (torch.from_numpy(_values(rng, (3, H, D), "bf16")).to(dev).to(torch.bfloat16) for _ in range(2))
+    turns = torch.from_numpy(tk.topkv_rotary_turns(ot.frequencies(count, 10000.0)).view(np.int64)).to(dev)
+    n = tk.make_new_tokens(k, v, TYPE[kind], TYPE["bf16"], rotary=tk.make_rotary(turns, tk.TOPKV_ROTARY_HALVES, 0, 1.0))
+    b = tk.make_batch(torch.from_numpy(bt).to(dev), torch.from_numpy(sl.astype(np.int32)).to(dev))
+    near = torch.zeros(pages * g.S_page, dtype=torch.uint8, device=dev)
+    tk.check(tk.topkv_append_layer(0, near, lo, b, n, k, v, None, None))
+    far = 700_000_000
+    big = torch.zeros(pages * far, dtype=torch.uint8, device=dev)
+    lo.pool_page_stride, lo.pool_layer_stride = far, pages * far
+    tk.check(tk.topkv_append_layer(0, big, lo, b, n, k, v, None, None))
+    torch.cuda.synchronize()
+    assert torch.equal(big.view(pages, far)[:, :g.S_page], near.view(pages, g.S_page)) and near.any() and pages * far > 1 << 32
+    for page in big.view(pages, far):
+        assert not page[g.S_page:].any()

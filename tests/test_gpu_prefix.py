@@ -350,3 +350,61 @@ def test_a_plan_with_more_work_than_its_line_counts(dev):
     torch.cuda.synchronize()
     assert tk.topkv_device_error_flags() == 2 and (out == 0).all()
     tk.check(tk.topkv_reset_device_error_flags())
+
+
+def test_settled_tables_and_known_totals(dev):
+    """Tables and plan that stay as they are, calls behind each other, lengths' sum known or not."""
+    c = Case(dev, [(40, [30, 700, 9]), (7, [1] * 9), (0, [1, 0, 300])], D=128)
+    c.make_plan()
+    c.attend()
+    first = [x.copy() for x in c.result()]
+    plain = c.batch
+    c.batch = tk.make_batch(c.d_bt, c.d_sl, flags=tk.TOPKV_FLAG_TABLES_SETTLED)
+    for _ in range(5):
+        c.out.fill_(7.0)
+        for _ in range(3):
+            c.attend()
+        assert all(np.array_equal(a, b) for a, b in zip(first, c.result()))
+    for flags in (0, tk.TOPKV_FLAG_TABLES_SETTLED):
+        c.batch = tk.make_batch(c.d_bt, c.d_sl, total_tokens=int(sum(c.sl)), flags=flags)
+        c.out.fill_(7.0)
+        c.n = tk.check(tk.topkv_attend_shared_workspace_bytes(c.lo, c.batch, c.att))
+        c.ws = torch.full((c.n + 32,), 0xFF, dtype=torch.uint8, device=dev)
+        c.attend()
+        c.attend()
+        _check(c.result(), c.want())
+    assert plain.flags == 0
+
+
+def test_two_calls_at_once(dev):
+    cases = [Case(dev, [(40, [30, 700, 9]), (7, [1] * 9)], D=128), Case(dev, [(130, [30, 7, 9, 1])], D=64, P=24, kind="e4m3")]
+    first = []
+    for c in cases:
+        c.make_plan()
+        c.attend()
+        first.append([x.copy() for x in c.result()])
+        c.out.fill_(7.0)
+    streams = [torch.cuda.Stream(dev) for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s in zip(cases, streams):
+            c.make_plan(stream=s)
+            c.attend(s)
+    for c, want in zip(cases, first):
+        assert all(np.array_equal(a, b) for a, b in zip(want, c.result()))
+
+
+@pytest.mark.parametrize("P, kind", [(16, "bf16"), (12, "fp16"), (16, "e4m3"), (12, "e4m3")])
+def test_offsets_beyond_32_bits(dev, P, kind):
+    """Pages far apart, which come by tensor copies (P 16) or row by row: the bits of the same pages side by side."""
+    c = Case(dev, [(4, [5, 30])], P=P, kind=kind)
+    c.make_plan()
+    c.attend()
+    near = [x.copy() for x in c.result()]
+    far = 800_000_000
+    big = torch.zeros(c.g.num_pages * far, dtype=torch.uint8, device=dev)
+    big.view(c.g.num_pages, far)[:, :c.g.S_page] = c.pool.view(c.g.num_pages, c.g.S_page)
+    c.lo.pool_page_stride, c.lo.pool_layer_stride = far, c.g.num_pages * far
+    c.out.fill_(7.0)
+    tk.check(tk.topkv_attend_shared_layer(0, big, c.lo, c.batch, c.att, c.plan, c.q, c.out, c.ws, c.n))
+    assert all(np.array_equal(a, b) for a, b in zip(near, c.result())) and c.g.num_pages * far > 1 << 32
