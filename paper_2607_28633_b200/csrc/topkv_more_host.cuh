@@ -480,15 +480,31 @@ int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const 
     p.scale = t->scale;
   }
   const bool chunks = p.first % 8 == 0 && (p.pairs ? 2 * p.half : p.half) % 8 == 0;
-  // Few tokens a CTA, so that there are several CTAs per SM; where there are not enough tokens for that
-  // the heads of a token are shared out too, two rows of heads a thread.
-  const int most = std::min(kAppendThreads, p.half > 0 ? kAppendPairs / p.half : kAppendThreads);
-  p.tokens = (int)std::max<int64_t>(1, std::min<int64_t>({p.num_rows / (8 * 148), most, 8}));
-  const int64_t ctas = (p.num_rows + p.tokens - 1) / p.tokens;
+  // A CTA has a few tokens, or a share of a token's heads. All take about as long, so they are cut such that the rounds of
+  // 4 x 148, which are on the GPU at a time, come out short: a CTA costs half a pass (two rows a thread) to begin. With 128
+  // heads of 576: 64 tokens in 576 CTAs 5.5 us, in 1,216 8.2; 256 tokens in 512 CTAs 18.8 us, in 1,280 21.6, in 768 22.0; 600
+  // tokens in 3,600 41.6, in 600 53. With 80 rows of 128: 1,000 tokens two a CTA 11.6 us, one 13.8, four 13.1; 2,000 four a
+  // CTA 19.1, one 24.1. More than eight are slower (13,312 tokens 61 us, sixteen a CTA 67).
+  constexpr int kResident = 4 * 148;
+  const int most = std::min(8, p.half > 0 ? kAppendPairs / p.half : 8);
   const int items = chunks ? (p.pairs ? p.half / 4 : p.half / 8) + p.D / 8 - p.half / 4 : p.D - p.half;
-  const int64_t passes = ((int64_t)p.rows * items + 2 * kAppendThreads - 1) / (2 * kAppendThreads);
-  const unsigned y = (unsigned)std::max<int64_t>(1, std::min<int64_t>({(8 * 148 + ctas - 1) / ctas, passes, 65535}));
-  const dim3 grid((unsigned)ctas, y);
+  const double passes = (double)p.rows * items / (2 * kAppendThreads);
+  const int64_t shares = std::min<int64_t>(65535, (int64_t)std::ceil(passes));
+  double least = std::numeric_limits<double>::infinity();
+  int64_t ctas = 0, y = 1;
+  auto weigh = [&](int tokens, int64_t parts) {
+    const int64_t n = (p.num_rows + tokens - 1) / tokens, rounds = (n * parts + kResident - 1) / kResident;
+    const double cost = rounds * (0.5 + passes * tokens / parts);
+    if (cost >= least) return;
+    least = cost;
+    p.tokens = tokens;
+    ctas = n;
+    y = parts;
+  };
+  for (int t = 1; t <= most; ++t) weigh(t, 1);
+  for (int64_t k = 2; k <= std::min<int64_t>(shares, 8); ++k) weigh(1, k);
+  if (p.num_rows < kResident) weigh(1, std::min(shares, kResident / p.num_rows));
+  const dim3 grid((unsigned)ctas, (unsigned)y);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool bf16 = tokens->io_type == TOPKV_TYPE_BF16, narrow = tokens->cache_type == TOPKV_TYPE_E4M3;
   if (bf16) return narrow ? launch_append<true, true>(p, chunks, grid, s) : launch_append<true, false>(p, chunks, grid, s);
