@@ -391,8 +391,8 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
   // Whether a group's tokens are formed once. 8 KV heads of 128, both ways after other work has been through L2,
   // once / by each request: 16-bit, 40 pairs of 4,096 tokens 165 / 236 us, 8 fours of 1,024 42 / 42, 20 pairs of 1,024
   // 56 / 50, eight of 8,192 40 / 53: worth it from 8 MB on. 8-bit tokens are converted tile by tile, at a rate that does
-  // not depend on the rows: 40 pairs of 4,096 214 / 151, 40 fours of 1,024 122 / 102, 8 eights of 4,096 84 / 121, 8
-  // sixteens of 1,024 78 / 87, as if two more members had to read them.
+  // not depend on the rows: 40 pairs of 4,096 198 / 151, 40 fours of 1,024 120 / 102, 8 eights of 4,096 81 / 122, 8
+  // sixteens of 1,024 79 / 87, as if two more members had to read them.
   const int64_t least = g_sharing_bytes.load(std::memory_order_relaxed);
   p.a.least_saved = least / (2ll * p.a.H * p.a.D * (int64_t)layout->elem_bytes);
   p.a.spent = layout->elem_bytes == 1 && least > 0 ? 3 : 1;

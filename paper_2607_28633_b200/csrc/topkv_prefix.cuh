@@ -17,7 +17,8 @@
 // other tile of tokens. (256 columns: one accumulator, two buffers of scores, 64 tokens a tile.) Roles:
 //   warps 0-7    softmax: four per accumulator, one thread a row; also Q and the result
 //   two warps    load K and V through the block table into a ring: tensor copies of page pieces, or 16-byte
-//                copies (any page size and stride). Of an 8-bit cache one warp loads and two make fp16 of it
+//                copies (any page size and stride). Of an 8-bit cache one warp loads and four make fp16 of it (8 groups
+//                of eight behind 4,096 tokens 81 us, 85 with two warps)
 //   one warp     one thread issues the products
 // The (group, KV head, 256 rows) units laid end to end, as long as their tiles, are cut into equal ranges, one
 // per CTA; each leaves its part in 32 bits in the workspace, and the joining kernel adds them to those of the
@@ -151,7 +152,6 @@ __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_groups_kernel(c
 
 // ---- the shared tokens' part ------------------------------------------------------------------------
 constexpr int kPrefixRows = 128;    // rows of a tile
-constexpr int kPrefixLoadWarps = 2;
 constexpr int kPrefixMaxStages = 8;
 constexpr int kPrefixMaxRaw = 4;    // buffers of 8-bit tiles that wait to be converted
 constexpr int kPrefixCtas = 148;    // at most
@@ -181,7 +181,8 @@ struct PrefixShape {
   static constexpr int kControl = kRawAt + kRaws * kRaw;
   static constexpr int kSmem = kControl + (int)sizeof(PrefixControl);
   static constexpr int kSoftmaxWarps = 4 * kTiles;
-  static constexpr int kThreads = (kSoftmaxWarps + kPrefixLoadWarps + (kConvert ? 1 : 0) + 1) * 32;
+  static constexpr int kLoadWarps = kConvert ? 4 : 2;     // that fill the ring
+  static constexpr int kThreads = (kSoftmaxWarps + kLoadWarps + (kConvert ? 1 : 0) + 1) * 32;
   static constexpr uint32_t kScores = 0, kSums = 2 * kTokens;  // TMEM columns: two buffers of scores, the accumulators
   static_assert(2 * kTokens + kTiles * DP <= 512, "TMEM");
   static_assert(kStages >= 4, "the ring holds K of two tiles and V of the first");
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   constexpr int kTokens = S::kTokens, kTiles = S::kTiles, kStages = S::kStages;
   // 8-bit values: a warp brings them, two convert
   constexpr int kRawWarp = S::kConvert ? S::kSoftmaxWarps : -1, kLoadWarp = S::kSoftmaxWarps + (S::kConvert ? 1 : 0);
-  constexpr int kIssueWarp = kLoadWarp + kPrefixLoadWarps;
+  constexpr int kIssueWarp = kLoadWarp + S::kLoadWarps;
   constexpr int kSoftmaxThreads = S::kSoftmaxWarps * 32;
   constexpr int kBlock = kTokens * 128, kQBlock = kPrefixRows * 128;  // bytes of 64 columns
   extern __shared__ __align__(128) uint8_t smem[];
@@ -337,7 +338,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     s_dead = 0;
     ctl.odd = 0;
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(b_full + 8 * i, kPrefixLoadWarps * 32);
+      mbar_init(b_full + 8 * i, S::kLoadWarps * 32);
       mbar_init(b_free + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     mbar_init(b_query, kSoftmaxThreads);
     for (int i = 0; i < S::kRaws; ++i) {
       mbar_init(b_raw + 8 * i, 32);
-      mbar_init(b_raw_free + 8 * i, kPrefixLoadWarps * 32);
+      mbar_init(b_raw_free + 8 * i, S::kLoadWarps * 32);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -485,7 +486,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       const int h = u.h;
       const int32_t* bt_row = a.bt + (int64_t)g.lead * a.maxp;
       // ---- load: 16-bit tiles into the ring, 8-bit tiles into buffers of their own ------------------------
-      constexpr int kWarps = S::kConvert ? 1 : kPrefixLoadWarps, kElem = S::kConvert ? 1 : 2;
+      constexpr int kWarps = S::kConvert ? 1 : S::kLoadWarps, kElem = S::kConvert ? 1 : 2;
       constexpr int kDepth = S::kConvert ? S::kRaws : kStages, kBytes = S::kConvert ? S::kRaw : S::kStage;
       const int w = S::kConvert ? 0 : warp - kLoadWarp;
       const uint32_t b_there = S::kConvert ? b_raw : b_full, b_room = S::kConvert ? b_raw_free : b_free;
@@ -599,9 +600,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
     } else if (S::kConvert && warp >= kLoadWarp && warp < kIssueWarp) {
      walk([&](const PrefixGroup& g, const PrefixUnit& u, int t0, int t1, int jobs) {
       const int count = t1 - t0;
-      // ---- convert: 16 bytes of a row at a time, half of the rows each ----------------------------------
+      // ---- convert: 16 bytes of a row at a time, a share of the rows each ----------------------------------
       constexpr int kRaws = S::kRaws > 0 ? S::kRaws : 1;
-      constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kRows = kTokens / kPrefixLoadWarps;
+      constexpr int kChunks = DP / 16, kPer = 32 / kChunks, kRows = kTokens / S::kLoadWarps;
       const int c = lane % kChunks, sub = lane / kChunks, row0 = (warp - kLoadWarp) * kRows;
       for (int e = 0; e < 2 * count; ++e, ++issued) {
         const uint32_t stage = issued % kStages, raw = issued % kRaws;
