@@ -484,8 +484,7 @@ def _handle(s):
     elif kind in ("shared", "sparse"):
         h["att"] = tk.make_attention(s["q"], s["out"], types[c["type"]], types[c["io"]], s["scale"], k_scale=s["scales"][0], v_scale=s["scales"][1],
                                      lse=s["lse"])
-    if kind == "shared":  # once a turn, for all layers
-        tk.check(tk.topkv_plan_prefixes(lo, h["batch"], 0, s["plan"], torch.cuda.current_stream().cuda_stream))
+    if kind == "shared":
         n = tk.check(tk.topkv_attend_shared_workspace_bytes(lo, h["batch"], h["att"]))
     elif kind == "sparse":
         h["pick"] = tk.make_page_choice(c["budget"], c["firsts"], c["lasts"], s["bounds"], s["steps"], s["picked"])
@@ -512,7 +511,8 @@ def _own(s):
         tk.check(tk.topkv_bound_pages_layer(0, s["flat"], lo, batch, tk.TOPKV_TYPE_E4M3 if s["case"]["type"] == "e4m3" else
                                             tk.TOPKV_TYPE_BF16 if s["case"]["type"] == "bf16" else tk.TOPKV_TYPE_FP16, s["bounds"], s["steps"], stream))
         return [s["bounds"], s["steps"]]
-    if kind == "shared":
+    if kind == "shared":  # a plan serves all layers of a turn: a turn of one layer, which reads the table that it is given
+        tk.check(tk.topkv_plan_prefixes(lo, batch, 0, s["plan"], stream))
         tk.check(tk.topkv_attend_shared_layer(0, s["flat"], lo, batch, h["att"], s["plan"], s["q"], s["out"], h["ws"], h["ws"].numel(), stream))
         return [s["out"], s["lse"]]
     tk.check(tk.topkv_choose_pages_layer(lo, batch, h["att"], h["pick"], s["q"], h["ws"], h["ws"].numel(), stream))
