@@ -477,9 +477,9 @@ def _handle(s):
         if c["count"]:
             turns = torch.from_numpy(tk.topkv_rotary_turns(s["frequencies"]).view(np.int64)).cuda()
             rotary = tk.make_rotary(turns, tk.TOPKV_ROTARY_PAIRS if c["pairs"] else tk.TOPKV_ROTARY_HALVES, c["first"], s["turn"])
-        # decode steps of one token a request need no offsets, and where tokens count as they lie no positions
+        # decode steps of one token a request need no offsets
         h["new"] = tk.make_new_tokens(s["k"], s["v"], types[c["type"]], types[c["io"]], q=s["q"], q_out=s["q_out"], rotary=rotary,
-                                      cu_tokens=None if s["one"] else s["cu"], positions=s["positions"] if c["far"] else None,
+                                      cu_tokens=None if s["one"] else s["cu"], positions=s["positions"],
                                       k_scale=s["scales"][0], v_scale=s["scales"][1])
     elif kind in ("shared", "sparse"):
         h["att"] = tk.make_attention(s["q"], s["out"], types[c["type"]], types[c["io"]], s["scale"], k_scale=s["scales"][0], v_scale=s["scales"][1],
