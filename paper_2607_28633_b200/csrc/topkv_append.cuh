@@ -49,7 +49,8 @@ struct AppendParams {
   int pairs;                  // neighbours, not halves
   int tokens;                 // per CTA
   float scale;
-  float inv_scale[2];         // of K, V
+  float by[2];                // of K, V: what stored elements are multiplied by, or divided by
+  int divide[2];
 };
 
 // Eight 16-bit elements as floats, and back.
@@ -76,27 +77,31 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {  // saturati
   return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
 // Where row `row` of a token goes: q_out, or a plane of its page. E: bytes of an element there.
+// Elements of an 8-bit plane are quotients: value / scale, rounded to 32 bits, then to 8. The product with the reciprocal is
+// the same number only where the reciprocal has no rounding, i.e. for powers of two; with other scales it leaves ties
+// (1.5625 = 0.01068115234375 / (7 / 1024)) and comes out a step apart. So other scales divide.
 struct AppendTo {
   uint8_t* p;
-  bool narrow;
-  float inv;
+  bool narrow, divide;
+  float by;
 };
 template <bool E8>
 __device__ __forceinline__ AppendTo append_to(const AppendParams& p, int64_t token, int row, int64_t place) {
-  if (row < p.Hq) return {p.q_out + token * p.out_row + row * p.out_head, false, 1.f};
+  if (row < p.Hq) return {p.q_out + token * p.out_row + row * p.out_head, false, false, 1.f};
   const int h = row - p.Hq, plane = h >= p.H;
-  return {p.pool + place + plane * p.S_kv + (h - plane * p.H) * p.S_head, E8, E8 ? p.inv_scale[plane] : 1.f};
+  return {p.pool + place + plane * p.S_kv + (h - plane * p.H) * p.S_head, E8, E8 && p.divide[plane] != 0, E8 ? p.by[plane] : 1.f};
 }
 __device__ __forceinline__ const uint8_t* append_from(const AppendParams& p, int64_t token, int row) {
   const int kind = row < p.Hq ? 0 : row < p.Hq + p.H ? 1 : 2;
   const int h = row - (kind == 0 ? 0 : kind == 1 ? p.Hq : p.Hq + p.H);
   return p.in[kind] + token * p.in_row[kind] + h * p.in_head[kind];
 }
+__device__ __forceinline__ float append_scaled(const AppendTo& to, float x) { return to.divide ? __fdiv_rn(x, to.by) : x * to.by; }
 template <bool BF16, bool E8>
 __device__ __forceinline__ void append_store8(const AppendTo& to, int d, float (&x)[8]) {
   if (E8 && to.narrow) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= to.inv;
+    for (int i = 0; i < 8; ++i) x[i] = append_scaled(to, x[i]);
     *reinterpret_cast<uint2*>(to.p + d) = make_uint2(to_e4m3x2(x[0], x[1]) | to_e4m3x2(x[2], x[3]) << 16,
                                                      to_e4m3x2(x[4], x[5]) | to_e4m3x2(x[6], x[7]) << 16);
   } else {
@@ -111,7 +116,7 @@ __device__ __forceinline__ float load_io(const uint8_t* p) {
 template <bool BF16, bool E8>
 __device__ __forceinline__ void append_store1(const AppendTo& to, int d, float x) {
   if (E8 && to.narrow)
-    to.p[d] = (uint8_t)__nv_cvt_float_to_fp8(x * to.inv, __NV_SATFINITE, __NV_E4M3);
+    to.p[d] = (uint8_t)__nv_cvt_float_to_fp8(append_scaled(to, x), __NV_SATFINITE, __NV_E4M3);
   else
     store_io(to.p + 2 * d, x, BF16);
 }

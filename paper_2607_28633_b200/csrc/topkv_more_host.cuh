@@ -470,8 +470,12 @@ int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const 
   p.H = (int)layout->num_kv_heads;
   p.rows = p.Hq + p.H * (values ? 2 : 1);
   p.D = (int)layout->head_dim;
-  p.inv_scale[0] = 1.f / tokens->k_scale;
-  p.inv_scale[1] = 1.f / tokens->v_scale;
+  const float scales[2] = {tokens->k_scale, tokens->v_scale};
+  for (int i = 0; i < 2; ++i) {
+    int exponent;
+    p.divide[i] = std::fabs(std::frexp(scales[i], &exponent)) != 0.5f;  // no power of two
+    p.by[i] = p.divide[i] ? scales[i] : 1.f / scales[i];
+  }
   if (const topkv_rotary* t = tokens->rotary) {
     p.first = (int)t->first;
     p.half = (int)t->count / 2;

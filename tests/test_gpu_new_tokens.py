@@ -211,3 +211,33 @@ def test_offsets_beyond_32_bits(dev, kind, count):
     assert torch.equal(big.view(pages, far)[:, :g.S_page], near.view(pages, g.S_page)) and near.any() and pages * far > 1 << 32
     for page in big.view(pages, far):
         assert not page[g.S_page:].any()
+
+
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("count, pairs", [(0, False), (64, False), (64, True), (6, False)])
+@pytest.mark.parametrize("scale", [7 / 1024, 0.3, 0.9, -1.1, 3.0, 0.5, 2.0 ** -126, 1e-38, 3e38])
+def test_stored_elements_are_quotients(dev, io, count, pairs, scale):
+    """Every value of 16 bits as an element of V, and of the part of K that does not turn: divided in 32 bits and
+    rounded once, bit for bit (a quotient between two 8-bit values goes to the even one)."""
+    D, rows = 256, 256
+    bits = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(rows, 1, D)
+    x = bits.view(TORCH[io]).to(dev)
+    lo = tk.make_layout(1, 2, 1, D, 1, 1, rows)
+    pool = torch.zeros(rows * 2 * D, dtype=torch.uint8, device=dev)
+    bt, sl = torch.arange(rows, dtype=torch.int32, device=dev).view(rows, 1), torch.ones(rows, dtype=torch.int32, device=dev)
+    rotary = None
+    if count:
+        turns = torch.from_numpy(tk.topkv_rotary_turns(ot.frequencies(count, 10000.0)).view(np.int64)).to(dev)
+        rotary = tk.make_rotary(turns, tk.TOPKV_ROTARY_PAIRS if pairs else tk.TOPKV_ROTARY_HALVES, D - count)
+    n = tk.make_new_tokens(x, x, TYPE["e4m3"], TYPE[io], rotary=rotary, k_scale=scale, v_scale=scale)
+    tk.check(tk.topkv_append_layer(0, pool, lo, tk.make_batch(bt, sl), n, x, x, None, None))
+    torch.cuda.synchronize()
+    got = pool.cpu().numpy().reshape(rows, 2, D)
+    with np.errstate(over="ignore"):
+        quotient = x.float().cpu().numpy()[:, 0] / np.float32(scale)  # one operation in 32 bits
+    nan = np.isnan(quotient)
+    want = od.encode_elements(np.where(nan, 0, quotient).astype(np.float64).clip(-448, 448).reshape(-1), "e4m3").reshape(rows, D)
+    for plane, columns in ((0, D - count), (1, D)):
+        have, same = got[:, plane, :columns], np.where(nan, 0x7F, want)[:, :columns]
+        bad = np.where(nan[:, :columns], have & 0x7F, have) != same
+        assert not bad.any(), (plane, np.argwhere(bad)[:4], quotient[:, :columns][bad][:4], have[bad][:4], same[bad][:4])
