@@ -394,7 +394,8 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
   // not depend on the rows: 40 pairs of 4,096 198 / 151, 40 fours of 1,024 120 / 102, 8 eights of 4,096 81 / 122, 8
   // sixteens of 1,024 79 / 87, as if two more members had to read them.
   const int64_t least = g_sharing_bytes.load(std::memory_order_relaxed);
-  p.a.least_saved = least / (2ll * p.a.H * p.a.D * (int64_t)layout->elem_bytes);
+  const int64_t token_bytes = 2ll * p.a.H * p.a.D * (int64_t)layout->elem_bytes;
+  p.a.least_saved = least / token_bytes + (least % token_bytes != 0);  // rounded up: at least that many bytes
   p.a.spent = layout->elem_bytes == 1 && least > 0 ? 3 : 1;
   p.tiles = plan.tiles;
   p.tokens = plan.tokens;

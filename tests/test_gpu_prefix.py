@@ -408,3 +408,47 @@ def test_offsets_beyond_32_bits(dev, P, kind):
     c.out.fill_(7.0)
     tk.check(tk.topkv_attend_shared_layer(0, big, c.lo, c.batch, c.att, c.plan, c.q, c.out, c.ws, c.n))
     assert all(np.array_equal(a, b) for a, b in zip(near, c.result())) and c.g.num_pages * far > 1 << 32
+
+
+def _formed(c):
+    """Leaders of the groups whose shared tokens were formed once: their records in the workspace are written."""
+    R = len(c.sl)
+    at = 16 * R + 16  # behind the join records and the line's header
+    records = c.ws[at:at + 48 * R].view(R, 48).cpu()
+    return [r for r in range(R) if not (records[r] == 0xFF).all()]
+
+
+def _alone(c):
+    """The same requests, each attended to on its own."""
+    n = tk.check(tk.topkv_attend_workspace_bytes(c.lo, c.batch, c.att))
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=c.dev)
+    tk.check(tk.topkv_attend_layer(c.layer, c.pool, c.lo, c.batch, c.att, c.q, c.out, ws, n))
+    return c.result()
+
+
+@pytest.mark.parametrize("kind, members, counted", [("bf16", 2, 1), ("fp16", 5, 4), ("e4m3", 4, 1), ("e4m3", 6, 3)])
+def test_a_group_is_formed_from_the_limit_on(dev, kind, members, counted):
+    """The limit is a number of bytes that the group has to save at least, whatever a token's bytes are."""
+    saved = counted * 9 * 16 * 2 * 2 * 64 * (1 if kind == "e4m3" else 2)
+    for limit, formed in [(1, True), (saved - 1, True), (saved, True), (saved + 1, False), (saved + 511, False), (2 ** 63 - 1, False)]:
+        tk.topkv_set_sharing_bytes(limit)
+        c = Case(dev, [(9, [40, 70, 5, 0, 9, 1][:members])], kind=kind)
+        c.check()
+        assert _formed(c) == ([0] if formed else []), limit
+        if not formed:
+            got = [x.copy() for x in c.result()]
+            assert all(np.array_equal(a, b) for a, b in zip(got, _alone(c)))
+
+
+def test_two_and_three_members_of_an_8_bit_cache_are_left_to_their_requests(dev):
+    """... at any limit but 0: converting a tile costs as much as two more members' reading."""
+    groups = [(9, [40, 70]), (8, [5, 0, 30]), (9, [1, 2, 3, 4]), (9, [9, 8, 7, 6, 5]), (0, [17, 0])]
+    for limit, sizes in [(0, [2, 3, 4, 5]), (1, [4, 5]), (2 * 2 * 64 - 1, [4, 5]), (1 << 40, [])]:
+        tk.topkv_set_sharing_bytes(limit)
+        c = Case(dev, groups, kind="e4m3", vs=0.5)
+        c.check()
+        plan = c.plan.cpu().numpy()
+        assert sorted(plan[tk.TOPKV_PLAN_MEMBERS][r] for r in _formed(c)) == sizes, limit
+    out, lse = [x.copy() for x in c.result()]
+    again, lse2 = _alone(c)
+    assert np.array_equal(out, again) and np.array_equal(lse, lse2)
