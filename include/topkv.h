@@ -592,7 +592,9 @@ int64_t topkv_page_choice_workspace_bytes(const topkv_layout* layout, const topk
                                           const topkv_attention* attention,
                                           const topkv_page_choice* choice);
 /* Writes choice->chosen for every request and KV head. Queries as for topkv_attend_layer; of `attention` only
- * io_type, num_q_heads and the strides of q are used beyond its checks. batch->window_tokens must be 0. */
+ * io_type, num_q_heads and the strides of q are used beyond its checks. The bounds are those of the largest
+ * products, so a negative scale, under which the smallest ones count, is refused (TOPKV_ERR_INVALID_ARG; attention to a
+ * caller's own lists takes it). batch->window_tokens must be 0. */
 int topkv_choose_pages_layer(const topkv_layout* layout, const topkv_batch* batch,
                              const topkv_attention* attention, const topkv_page_choice* choice,
                              const void* d_q, void* d_workspace, int64_t workspace_bytes,

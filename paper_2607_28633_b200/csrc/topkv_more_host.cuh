@@ -286,6 +286,7 @@ int topkv_choose_pages_layer(const topkv_layout* layout, const topkv_batch* batc
   ChoosePlan plan;
   int st = check_choice(layout, batch, attention, choice, &plan);
   if (st != TOPKV_OK) return st;
+  if (attention->scale < 0.f) return TOPKV_ERR_INVALID_ARG;  // the pages with the smallest products would count
   if (d_q == nullptr || choice->bounds == nullptr || choice->steps == nullptr || choice->chosen == nullptr) return TOPKV_ERR_INVALID_ARG;
   if (!mult16p(d_q)) return TOPKV_ERR_ALIGNMENT;
   st = check_choice_workspace(d_workspace, workspace_bytes, plan.key_bytes);

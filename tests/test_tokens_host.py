@@ -243,6 +243,14 @@ def test_chosen_pages_refusals():
     assert _choose(lo, wide, a, few, ws=None) == INVALID and _choose(lo, wide, a, few, ws=0xA000008) == ALIGN
 
 
+def test_a_choice_refuses_negative_scales():
+    """They turn the order of the scores round; a caller's own list has no order."""
+    lo, b, c = _gqa(), _batch(), _choice()
+    for scale, status in [(-0.1, INVALID), (-1e-45, INVALID), (0.0, CUDA), (-0.0, CUDA), (0.1, CUDA)]:
+        assert _choose(lo, b, _attention(scale=scale), c) == status and _sparse(lo, b, _attention(scale=scale), c) == CUDA
+    assert tk.topkv_page_choice_workspace_bytes(lo, b, _attention(scale=-0.1), c) >= 0
+
+
 def test_bounds_refusals():
     lo, b = _gqa(), _batch()
     call = lambda lo=lo, b=b, kind=BF16, layer=0, pool=0x7000000, bounds=0xB000000, steps=0xC000000: tk.topkv_bound_pages_layer(layer, pool, lo, b, kind, bounds, steps)
