@@ -33,6 +33,7 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
+#include <cfloat>
 #include <cstdint>
 
 #include "topkv_attend.cuh"
@@ -713,9 +714,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
           cp_async_commit();
           cp_async_wait<0>();
           __syncwarp();
-          // Scores times a factor that is not negative (a sign goes into Q) nor zero; bf16 queries over 8-bit keys
+          // Scores times a factor that is not negative (a sign goes into Q); bf16 queries over 8-bit keys
           // become fp16 ones after a power of two for the row, see the kernel of the other tokens. A row a thread.
-          float row_scale = fmaxf(fabsf(a.qk_scale), 1e-30f);
+          float row_scale = fabsf(a.qk_scale);
           const uint32_t flip = a.qk_scale < 0.f ? 0x80008000u : 0u;
           const bool halves = TYPE == kE4m3 && a.io_bf16;
           if (halves || flip) {
@@ -751,7 +752,8 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
               *v = make_uint4(x[0], x[1], x[2], x[3]);
             }
           }
-          ctl.row_scale[my_row] = row_scale;
+          // Nor zero, as a product of small factors may be: masked scores are minus infinity before it is applied.
+          ctl.row_scale[my_row] = fmaxf(row_scale, FLT_MIN);
           proxy_fence_smem();
         }
         tcgen05_before_sync();

@@ -452,3 +452,11 @@ def test_two_and_three_members_of_an_8_bit_cache_are_left_to_their_requests(dev)
     out, lse = [x.copy() for x in c.result()]
     again, lse2 = _alone(c)
     assert np.array_equal(out, again) and np.array_equal(lse, lse2)
+
+
+@pytest.mark.parametrize("q_size, scale, ks", [(1e-18, 0.0, 1.0), (1e-37, 0.125, 1e-9), (1e-37, -0.125, 1e-9), (1e-30, 1e-12, 0.5), (0.0, 0.0, 1.0)])
+@pytest.mark.parametrize("kind, io", [("e4m3", "bf16"), ("e4m3", "fp16"), ("bf16", "bf16")])
+def test_factors_of_scores_below_the_range_of_32_bits(dev, kind, io, q_size, scale, ks):
+    """A prefix that ends inside a tile, of which a row's factor is zero or rounds to it: all tokens weigh the same."""
+    c = Case(dev, [(3, [5, 9]), (11, [1, 0, 2])], kind=kind, io=io, q_size=q_size, scale=scale, ks=ks if kind == "e4m3" else 1.0)
+    c.check()
