@@ -475,8 +475,10 @@ int topkv_append_layer(int layer, void* pool, const topkv_layout* layout, const 
   const float scales[2] = {tokens->k_scale, tokens->v_scale};
   for (int i = 0; i < 2; ++i) {
     int exponent;
-    p.divide[i] = std::fabs(std::frexp(scales[i], &exponent)) != 0.5f;  // no power of two
-    p.by[i] = p.divide[i] ? scales[i] : 1.f / scales[i];
+    const bool exact = std::fabs(std::frexp(scales[i], &exponent)) == 0.5f;  // a power of two
+    p.stored[i] = exact ? 0.f : scales[i];
+    p.inv[i] = 1.f / scales[i];
+    if (!exact && !std::isnormal(p.inv[i])) p.inv[i] = 0.f;  // has lost bits: products of zero are all looked at
   }
   if (const topkv_rotary* t = tokens->rotary) {
     p.first = (int)t->first;
