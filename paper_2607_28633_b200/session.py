@@ -201,7 +201,7 @@ class DecodeCache:
         self.plan = torch.zeros((tk.TOPKV_PLAN_ROWS, rows), dtype=torch.int32, device=dev)
         self._planned = False
         self.bounds = self.steps = None
-        self._bounded: set[int] = set()  # layers whose pages all have bounds
+        self._bounded: dict[int, int] = {}  # layers whose pages all have bounds -> the type that they were formed of
         torch.cuda.current_stream(dev).synchronize()
 
     def _on(self, stream):
@@ -217,6 +217,12 @@ class DecodeCache:
             raise ValueError(f"{name}: a contiguous int32 vector on the pool's device")
         if count is not None and t.numel() != count:
             raise ValueError(f"{name}: {count} entries, one per row")
+
+    def _cache_type(self, dtype: torch.dtype, cache_type: int | None) -> int:
+        """What the pool's elements are: as told, or 8-bit ones by their size, 16-bit ones as the tensors beside them."""
+        if cache_type is not None:
+            return cache_type
+        return tk.TOPKV_TYPE_E4M3 if self.layout.elem_bytes == 1 else tk.TOPKV_TYPE_FP16 if dtype == torch.float16 else tk.TOPKV_TYPE_BF16
 
     def extend(self, new_tokens: torch.Tensor, stream):
         """Room for new_tokens[r] (device int32 [rows]) more tokens of every request. A request for which
@@ -278,7 +284,7 @@ class DecodeCache:
             raise ValueError("k (and v, unless rows are latent) have the layout's heads and elements")
         io = tk.TOPKV_TYPE_BF16 if k.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
         new = self._new
-        n = tk.make_new_tokens(k, v, io if cache_type is None else cache_type, io, q=q, q_out=q_out, rotary=rotary, cu_tokens=cu_tokens,
+        n = tk.make_new_tokens(k, v, self._cache_type(k.dtype, cache_type), io, q=q, q_out=q_out, rotary=rotary, cu_tokens=cu_tokens,
                                positions=positions, k_scale=k_scale, v_scale=v_scale)
         b = tk.make_batch(self.block_table, new.lens if new.known else self.seq_lens)
         tk.check(tk.topkv_append_layer(layer, self.pool, self.layout, b, n, k, v, q, q_out, stream))
@@ -292,7 +298,7 @@ class DecodeCache:
         if q.ndim != 3 or q.shape[0] != len(self.seq_lens) or q.shape[2] != self.layout.head_dim:
             raise ValueError(f"q is [{len(self.seq_lens)}][heads][{self.layout.head_dim}]")
         io = tk.TOPKV_TYPE_BF16 if q.dtype == torch.bfloat16 else tk.TOPKV_TYPE_FP16
-        return tk.make_attention(q, out, io if cache_type is None else cache_type, io, scale, **attention)
+        return tk.make_attention(q, out, self._cache_type(q.dtype, cache_type), io, scale, **attention)
 
     def _workspace(self, n: int, stream) -> torch.Tensor:
         # One per size (a kind of layer has one, whatever the lengths), kept as long as the cache: captured
@@ -333,11 +339,10 @@ class DecodeCache:
         """Bounds of the keys of the pages that hold the last ``tokens`` tokens of each request (0: of all pages), for
         ``attend_chosen``: as many as any request has got since the call before for this layer. The first call for a
         layer, and the first after a fork or a compaction, takes all pages whatever ``tokens`` says; make it outside a
-        CUDA graph, which repeats what it was captured with. cache_type: what the pool's 16-bit elements are, bfloat16
-        unless given."""
-        lo = self.layout
-        if cache_type is None:
-            cache_type = tk.TOPKV_TYPE_E4M3 if lo.elem_bytes == 1 else tk.TOPKV_TYPE_BF16
+        CUDA graph, which repeats what it was captured with. cache_type: what the pool's 16-bit elements are; unless given,
+        what the pool tensor's are, or bfloat16 if that one holds bytes. ``attend_chosen`` refuses bounds of another type
+        than its own."""
+        lo, cache_type = self.layout, self._cache_type(self.pool.dtype, cache_type)
         if not 0 <= layer < lo.num_layers or tokens < 0:
             raise ValueError("a layer of the layout and a number of tokens")
         if self.bounds is None:
@@ -345,9 +350,9 @@ class DecodeCache:
             with self._on(stream):
                 self.bounds = torch.zeros((*shape, 2, lo.head_dim), dtype=torch.int8, device=self.pool.device)
                 self.steps = torch.zeros(shape, dtype=torch.float32, device=self.pool.device)
-        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens if layer in self._bounded else 0)
+        b = tk.make_batch(self.block_table, self.seq_lens, window_tokens=tokens if self._bounded.get(layer) == cache_type else 0)
         tk.check(tk.topkv_bound_pages_layer(layer, self.pool, lo, b, cache_type, self.bounds[layer], self.steps[layer], stream))
-        self._bounded.add(layer)
+        self._bounded[layer] = cache_type
 
     def attend_chosen(self, layer: int, q: torch.Tensor, out: torch.Tensor, chosen: torch.Tensor, scale: float, stream, first_pages: int = 1,
                       last_pages: int = 1, cache_type: int | None = None, **attention):
@@ -359,6 +364,8 @@ class DecodeCache:
         if chosen.ndim != 3 or tuple(chosen.shape[:2]) != (len(self.seq_lens), self.layout.num_kv_heads) or chosen.dtype != torch.int32:
             raise ValueError(f"chosen is int32 [{len(self.seq_lens)}][{self.layout.num_kv_heads}][budget]")
         att = self._attention(q, out, scale, cache_type, attention)
+        if att.cache_type != self._bounded[layer]:
+            raise ValueError("bound_pages took the pool's elements for another type: give it cache_type")
         choice = tk.make_page_choice(chosen.shape[2], first_pages, last_pages, self.bounds[layer], self.steps[layer], chosen)
         ws = self._workspace(tk.check(tk.topkv_page_choice_workspace_bytes(self.layout, self.batch, att, choice)), stream)
         tk.check(tk.topkv_choose_pages_layer(self.layout, self.batch, att, choice, q, ws, ws.numel(), stream))

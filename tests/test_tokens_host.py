@@ -379,6 +379,42 @@ def test_class_bounds_all_pages_where_it_must(cache):
             c.bound_pages(stream=None, **bad)
 
 
+def test_class_keeps_to_one_type_of_elements(cache):
+    """Bounds of one type are not used with another; a type that is not given is what the tensors' are."""
+    c, calls = cache
+    q, chosen = torch.zeros((3, 4, 16), dtype=torch.float16), torch.zeros((3, 2, 2), dtype=torch.int32)
+    bounds = lambda: [(a[3].window_tokens, a[4]) for n, a in calls if n == "bound_pages_layer"]
+    c.bound_pages(0, None)
+    with pytest.raises(ValueError):
+        c.attend_chosen(0, q, q.clone(), chosen, 1.0, None)                # fp16 queries of a bfloat16 pool
+    c.bound_pages(0, None, tokens=1, cache_type=FP16)                      # the pages' bounds were those of the other type
+    c.attend_chosen(0, q, q.clone(), chosen, 1.0, None)
+    c.bound_pages(0, None, tokens=1, cache_type=FP16)
+    with pytest.raises(ValueError):
+        c.attend_chosen(0, q.bfloat16(), q.bfloat16(), chosen, 1.0, None)
+    c.pool = c.pool.half()
+    c.bound_pages(1, None)
+    c.pool = c.pool.view(torch.uint8)
+    c.bound_pages(1, None, tokens=1)
+    assert bounds() == [(0, BF16), (0, FP16), (1, FP16), (0, FP16), (0, BF16)]
+
+
+def test_class_knows_8_bit_pools(monkeypatch, cache):
+    c, calls = cache
+    monkeypatch.setattr(c, "layout", tk.make_layout(2, 2, 2, 16, 1, 4, 8))
+    k, q, chosen = torch.zeros((3, 2, 16), dtype=torch.float16), torch.zeros((3, 4, 16), dtype=torch.float16), torch.zeros((3, 2, 2), dtype=torch.int32)
+    c.append_rotated(0, k, k, None, k_scale=0.5)
+    assert calls[-1][1][4].cache_type == E4M3 and calls[-1][1][4].io_type == FP16
+    c.bound_pages(0, None)
+    c.plan_prefixes(None)
+    monkeypatch.setattr(tk, "topkv_attend_layer", lambda *a: calls.append(("attend_layer", a)) or 0)
+    for call in (c.attend, c.attend_shared):
+        call(0, q, q.clone(), 1.0, None, k_scale=0.5)
+        assert calls[-1][1][4].cache_type == E4M3 and calls[-1][1][4].io_type == FP16
+    c.attend_chosen(0, q, q.clone(), chosen, 1.0, None, k_scale=0.5)
+    assert calls[-1][0] == "attend_pages_layer" and calls[-1][1][4].cache_type == E4M3
+
+
 def test_class_appends_what_has_grown(cache):
     c, calls = cache
     ints = lambda *x: torch.tensor(x, dtype=torch.int32)
