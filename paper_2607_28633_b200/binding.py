@@ -229,6 +229,8 @@ def make_new_tokens(k, v, cache_type: int, io_type: int, q=None, q_out=None, rot
     for t, size in ((cu_tokens, 8), (positions, 4)):
         if t is not None and (t.ndim != 1 or t.element_size() != size or t.is_floating_point() or not t.is_contiguous() or t.device != k.device):
             raise ValueError("cu_tokens and positions are contiguous vectors of 64- and 32-bit integers on the tensors' device")
+    if rotary is not None and getattr(rotary, "_keepalive", None) is not None and rotary._keepalive.device != k.device:
+        raise ValueError("the rotary turns are on another device than the tensors")
     if positions is not None and positions.numel() < k.shape[0]:
         raise ValueError("a position for every row")
     stride = lambda t, i: 2 * t.stride(i) if t.shape[i] > 1 else 0

@@ -315,6 +315,18 @@ def test_binding_refuses_tensors_that_do_not_fit():
     assert one.k_row_stride == 0 and one.k_head_stride == 0 and one.num_q_heads == 0
 
 
+def test_binding_refuses_turns_of_another_device():
+    """A table left on the host would be an address that the kernel cannot read."""
+    k, turns = torch.zeros((4, 2, 16), dtype=torch.bfloat16), torch.zeros(8, dtype=torch.int64)
+    assert tk.make_new_tokens(k, k, BF16, BF16, rotary=tk.make_rotary(turns)).rotary.contents.count == 16
+    with pytest.raises(ValueError):
+        tk.make_new_tokens(k, k, BF16, BF16, rotary=tk.make_rotary(turns.to("meta")))
+    with pytest.raises(ValueError):
+        tk.make_new_tokens(k.to("meta"), None, BF16, BF16, rotary=tk.make_rotary(turns))
+    bare = tk.topkv_rotary()  # a descriptor of the caller's own says nothing of devices
+    assert tk.make_new_tokens(k, k, BF16, BF16, rotary=bare).rotary
+
+
 @pytest.fixture
 def cache(monkeypatch):
     """A cache whose library calls are noted, not made."""
