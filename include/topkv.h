@@ -531,8 +531,8 @@ int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, in
                         int32_t* d_plan, topkv_stream_t stream);
 /* As topkv_attend_layer, with the shared tokens' part formed once per group: the queries of all its
  * members and heads are the rows of one product. kv_factor 2 only (128 query heads already share a latent
- * row, which leaves nothing to gain), no window (window_tokens and sink_tokens 0). The weights of shared
- * tokens are rounded once to 16 bits for the second product (bf16 for a bf16 cache, else fp16), and
+ * row, which leaves nothing to gain), no window (window_tokens and sink_tokens 0). Weights are rounded as
+ * topkv_attend_layer rounds them (to fp16; of a bf16 cache with head_dim <= 128 to two bf16 values, beyond that to one), and
  * bf16 queries over an 8-bit cache become fp16 with a power of two for each row. Three kernels at most;
  * the workspace holds nothing between calls, and calls that may run at the same time need one each.
  * Capturable (the first call for a head size and type on a device raises the kernels' shared-memory limits: make

@@ -460,3 +460,47 @@ def test_factors_of_scores_below_the_range_of_32_bits(dev, kind, io, q_size, sca
     """A prefix that ends inside a tile, of which a row's factor is zero or rounds to it: all tokens weigh the same."""
     c = Case(dev, [(3, [5, 9]), (11, [1, 0, 2])], kind=kind, io=io, q_size=q_size, scale=scale, ks=ks if kind == "e4m3" else 1.0)
     c.check()
+
+
+@pytest.mark.parametrize("D, pages", [(64, 1), (128, 1), (128, 9), (40, 20)])
+def test_bf16_weights_of_shared_tokens_keep_sixteen_bits(dev, D, pages):
+    """Two values that nearly cancel, as for attention to each request's own tokens: a weight is split into two bf16
+    values, the second of what the first leaves, 2^-8 of 2^-8. The other tokens have values of zero."""
+    G = 16
+    c = Case(dev, [(pages, [0, 1, 3])], H=1, G=G, D=D)
+    q = np.zeros((3, G, D))
+    q[:, :, 0] = -np.arange(1, G + 1) / 8
+    w = np.exp(q[0, :, 0])
+    k, v = np.zeros((16 * pages + 3, D)), np.zeros((16 * pages + 3, D))
+    k[1, 0] = 1.0
+    v[0, :G], v[1, :G] = od.decode_elements(od.encode_elements(w, "bf16"), "bf16"), -1.0
+    for r, s in enumerate(c.sl):
+        for i in range(int(s)):
+            for plane, x in ((0, k), (1, v)):
+                a = od.row_offset(c.g, 0, int(c.bt[r, i // 16]), plane, i % 16, 0)
+                c.pool_h[a:a + 2 * D] = od.encode_elements(x[i], "bf16")
+    c.pool.copy_(torch.from_numpy(c.pool_h))
+    c.q.copy_(torch.from_numpy(q))
+    c.scale = c.att.scale = 1.0
+    c.make_plan()
+    c.attend()
+    got = c.result()
+    want = od.attend(c.g, 0, c.pool_h, c.bt, c.sl, q, "bf16", "bf16", 1.0, weight_step=2.0 ** -16)
+    coarse = od.attend(c.g, 0, c.pool_h, c.bt, c.sl, q, "bf16", "bf16", 1.0)
+    assert _formed(c) == [0]
+    _check(got, want)
+    own = np.arange(G)  # the bound would not let 8 bits through
+    assert (want[2][:, own, own] < coarse[2][:, own, own] / 4).all()
+
+
+def test_a_shared_prefix_is_as_exact_as_reading_it_again(dev):
+    """The same cache both ways: results differ by the rounding of the output."""
+    c = Case(dev, [(64, [9, 40, 0, 17])], D=128, H=2, G=4, seed=4)
+    c.make_plan()
+    c.attend()
+    once, lse = [x.copy() for x in c.result()]
+    each, lse_each = _alone(c)
+    want = od.attend(c.g, 0, c.pool_h, c.bt, c.sl, c.q_h, "bf16", "bf16", c.scale, weight_step=2.0 ** -16)
+    for got in ((once, lse), (each, lse_each)):
+        _check(got, want)
+    assert (np.abs(once - each) <= 2 * want[2]).all()
