@@ -520,7 +520,8 @@ int topkv_rotary_turns(const double* h_frequencies, uint32_t n, uint64_t* h_turn
  *   PLACE    where r stands in that order
  * One group per first page: where some of its requests share more than all of them do, those tokens are
  * read by each. A caller that knows better may write a plan of its own: LEADER, SHARED, MEMBERS, ORDER and
- * PLACE are what attention reads. One that contradicts itself gives results without meaning (and may raise
+ * PLACE are what attention reads. The groups may stand in any order there, each with its leader (any of its requests) first and
+ * the others right behind it, and share any number of tokens that all of its requests have in common. One that contradicts itself gives results without meaning (and may raise
  * error bit 2), but no access outside the pool and the tensors; a request shorter than SHARED is attended to on its own.
  * One or two kernels on `stream`, no allocation, no synchronisation, capturable; batch->window_tokens must be 0.
  * Every row looks at every other one: fine for thousands of requests, not for a hundred thousand. */

@@ -160,9 +160,9 @@ constexpr int kPrefixCtas = 148;    // at most
 
 struct PrefixControl {
   uint64_t bar[2 * kPrefixMaxStages + 7 + 2 * kPrefixMaxRaw];
-  int64_t scan[16];
+  int64_t scan[2][16];
   int off;
-  int group[8];    // what is known of the first group; leader -1: nothing to do
+  int group[9];    // what is known of the first group; leader -1: nothing to do
   uint32_t tmem;
   volatile int dead;
   volatile int odd;   // a page outside the pool has been met
@@ -198,7 +198,8 @@ struct PrefixGroup {
   int full;          // length of a unit of all rows
   int length;        // of a KV head's units
   int begin;         // where the group's units begin on the line (the host has seen to it that this fits)
-  int pad[3];
+  int first;         // rows of the groups before it on the line, where its parts lie
+  int pad[2];
 };
 // How the line is cut.
 struct PrefixHeader {
@@ -248,7 +249,7 @@ __device__ __forceinline__ PrefixUnit prefix_unit(const PrefixParams& p, const P
   u.rows = min(tall, g.rows - u.first_row);
   u.both = u.rows > kPrefixRows;
   u.length = u.both ? g.full : g.n;
-  u.slot = p.tiles * ((int64_t)p.a.H * p.a.G * g.place + (int64_t)h * g.rows + u.first_row);
+  u.slot = p.tiles * ((int64_t)p.a.H * g.first + (int64_t)h * g.rows + u.first_row);
   return u;
 }
 __device__ __forceinline__ int prefix_team_of(const PrefixHeader& t, int x) {
@@ -381,26 +382,41 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (per > 1 || g.n == 0) g = prefix_group(p, r);
       return g.tokens > 0 ? a.H * g.length : 0;
     };
-    int64_t mine = 0;
-    for (int r = r0; r < r1; ++r) mine += length(r);
-    int64_t incl = mine;
+    int64_t mine = 0, mine_rows = 0;
+    for (int r = r0; r < r1; ++r) {
+      const int n = length(r);
+      mine += n;
+      mine_rows += n > 0 ? g.rows : 0;
+    }
+    int64_t incl = mine, incl_rows = mine_rows;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
+      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o), up_rows = __shfl_up_sync(0xffffffffu, incl_rows, o);
+      if (lane >= o) {
+        incl += up;
+        incl_rows += up_rows;
+      }
     }
-    if (lane == 31) ctl.scan[warp] = incl;
+    if (lane == 31) {
+      ctl.scan[0][warp] = incl;
+      ctl.scan[1][warp] = incl_rows;
+    }
     if (tid == 0) ctl.group[0] = -1;
     __syncthreads();
-    int64_t sum = 0;
+    int64_t sum = 0, sum_rows = 0;
     for (int w = 0; w < S::kThreads / 32; ++w) {
-      if (w < warp) incl += ctl.scan[w];
-      sum += ctl.scan[w];
+      if (w < warp) {
+        incl += ctl.scan[0][w];
+        incl_rows += ctl.scan[1][w];
+      }
+      sum += ctl.scan[0][w];
+      sum_rows += ctl.scan[1][w];
     }
-    // A plan whose groups overlap can come to more than the line counts: it has no work then (the host has seen to
-    // it that no other can).
-    const int total = sum <= 0x7fffffff ? (int)sum : 0;
-    if (sum > 0x7fffffff && tid == 0) raise_error(kErrTable);
+    // A plan whose groups overlap can come to more than the line counts, or than there is room for: it has no work then
+    // (the host has seen to it that no other can).
+    const bool fits = sum <= 0x7fffffff && sum_rows <= (int64_t)a.R * a.G;
+    const int total = fits ? (int)sum : 0;
+    if (!fits && tid == 0) raise_error(kErrTable);
     // a range is two tiles long at least: what a CTA costs to begin is about that
     const int teams = min((int)gridDim.x, (total + 1) / 2);
     PrefixHeader t;
@@ -413,22 +429,24 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       pdl_wait_prior_grid();
       pdl_release_next_grid();
     }
-    int at = (int)(incl - mine);
+    int at = (int)(incl - mine), rows_at = (int)(incl_rows - mine_rows);
     const bool begins = left > 0 && pos >= at && pos < incl;  // exactly one thread
     if (begins || (team == 0 && total > 0)) {
       for (int r = r0; r < r1; ++r) {
         const int n = length(r);
         if (team == 0 && n > 0) {
           g.begin = at;
+          g.first = rows_at;
           p.groups[r] = g;
         }
         if (begins && pos >= at && pos < at + n) {
           ctl.off = pos - at;
-          const int known[8] = {r, g.place, g.tokens, g.n, g.rows, g.units, g.full, g.length};
+          const int known[9] = {r, g.place, g.tokens, g.n, g.rows, g.units, g.full, g.length, rows_at};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) ctl.group[i] = known[i];
+          for (int i = 0; i < 9; ++i) ctl.group[i] = known[i];
         }
         at += n;
+        rows_at += n > 0 ? g.rows : 0;
       }
     }
     if (team == 0 && tid == 0) *p.header = t;
@@ -463,6 +481,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   // registers of its own.
   auto walk = [&](auto body) {
     PrefixGroup g{ctl.group[0], ctl.group[1], ctl.group[2], ctl.group[3], ctl.group[4], ctl.group[5], ctl.group[6], ctl.group[7]};
+    g.first = ctl.group[8];
     int off = ctl.off, rest = left;
     int lead = g.lead;
     while (rest > 0 && lead >= 0 && lead < a.R) {
@@ -481,7 +500,9 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
       if (off == a.H * g.length && rest > 0) {
         off = 0;
         lead = next_group(p, lead + 1, lane);
+        const int first = g.first + g.rows;
         if (lead < a.R) g = prefix_group(p, lead);
+        g.first = first;
       }
     }
   };

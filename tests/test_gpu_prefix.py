@@ -504,3 +504,40 @@ def test_a_shared_prefix_is_as_exact_as_reading_it_again(dev):
     for got in ((once, lse), (each, lse_each)):
         _check(got, want)
     assert (np.abs(once - each) <= 2 * want[2]).all()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(D=128, G=4, kind="e4m3"), dict(D=256, H=1, G=16), dict(H=8, G=8, D=64, kind="fp16", style="head")])
+def test_a_callers_plan_has_its_groups_in_any_order(dev, kw):
+    """Groups stand in ORDER last first, or mixed, members behind a leader that is not the lowest of them, and share
+    fewer tokens than they could, down to parts of a page."""
+    groups = [(9, [40, 70, 33]), (30, [20, 30] * 9), (12, [1, 0, 5, 9]), (0, [17, 3]), (50, [2, 3])]
+    for seed in range(4):
+        c = Case(dev, groups, seed=seed, **kw)
+        c.make_plan()
+        torch.cuda.synchronize()
+        auto, rng = c.plan.cpu().numpy(), np.random.default_rng(seed)
+        plan, place = np.zeros_like(auto), 0
+        leaders = sorted(set(auto[tk.TOPKV_PLAN_LEADER].tolist()), reverse=True)
+        for lead in leaders if seed == 0 else rng.permutation(leaders):
+            members = rng.permutation(np.flatnonzero(auto[tk.TOPKV_PLAN_LEADER] == lead))
+            shared = int(auto[tk.TOPKV_PLAN_SHARED][lead])
+            shared = shared if seed < 2 else int(rng.integers(0, shared + 1))
+            for r in members:
+                plan[tk.TOPKV_PLAN_LEADER, r], plan[tk.TOPKV_PLAN_SHARED, r] = members[0], shared
+                plan[tk.TOPKV_PLAN_MEMBERS, r], plan[tk.TOPKV_PLAN_PLACE, r], plan[tk.TOPKV_PLAN_ORDER, place] = len(members), place, r
+                place += 1
+        c.plan.copy_(torch.from_numpy(plan))
+        c.attend()
+        _check(c.result(), c.want())
+
+
+def test_a_plan_whose_groups_overlap_is_reported(dev):
+    """More rows in all groups than there are: no room for their parts, so nothing is formed."""
+    c = Case(dev, [(9, [40, 70, 33]), (4, [3, 9, 5])])
+    c.make_plan()
+    c.plan[tk.TOPKV_PLAN_MEMBERS] = 6
+    c.plan[tk.TOPKV_PLAN_PLACE] = torch.where(c.plan[tk.TOPKV_PLAN_LEADER] == 0, c.plan[tk.TOPKV_PLAN_PLACE], c.plan[tk.TOPKV_PLAN_PLACE] - 3)
+    c.attend()
+    c.result()
+    assert tk.topkv_device_error_flags() == 2
+    tk.check(tk.topkv_reset_device_error_flags())
