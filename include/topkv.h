@@ -565,7 +565,7 @@ int64_t topkv_set_sharing_bytes(int64_t bytes);
  *     t = max |q| * c      q8[d] = q[d] / t rounded to the nearest integer, ties to even (0 and t = 0 where
  *                          t is 0 or not finite)
  *     dot = sum_d q8[d] * (q8[d] < 0 ? bounds[.][0][d] : bounds[.][1][d])      an exact integer
- *     score(p, h) = max over the heads a of h of dot * (t * step); a page without a finite step scores highest
+ *     score(p, h) = max over the heads a of h of dot * (t * step); a page without a finite step scores +infinity
  * Each KV head takes `budget` pages (all, if there are no more): the last `last_pages` before the first
  * `first_pages` before the rest by falling score, equal scores by rising table column. So a choice is
  * a function of the inputs alone, and the newest page is always part of it. k_scale must be positive. */

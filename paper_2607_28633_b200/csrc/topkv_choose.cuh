@@ -379,7 +379,8 @@ __global__ void __launch_bounds__(kChooseThreads, 2) topkv_choose_pages_kernel(c
       for (int u = 0; u < kAhead; ++u) {
         const int j = i0 + u * 8 + gr;
         if (j < n) {
-          const uint32_t key = step[u] < INFINITY ? score_key(__fadd_rn(best[u], 0.f)) : 0xffffffffu;
+          // infinity without a finite step, as a score that has left the range is: such pages are equal
+          const uint32_t key = score_key(step[u] < INFINITY ? __fadd_rn(best[u], 0.f) : INFINITY);
           keys[j] = key;
           least = min(least, key);
           most = max(most, key);

@@ -325,3 +325,21 @@ def test_offsets_beyond_32_bits(dev, kind):
     tk.check(tk.topkv_attend_pages_layer(0, big, c.lo, c.batch, c.att, c.choice, c.q, c.out, c.ws, c.n))
     assert all(np.array_equal(a, b) for a, b in zip(near, list(c.result()) + [c.chosen.cpu().numpy()])) and c.g.num_pages * far > 1 << 32
     assert torch.equal(bounds, c.bounds) and torch.equal(steps, c.steps)
+
+
+def test_scores_beyond_the_range_equal_those_without_a_finite_step(dev):
+    """Both are infinite, so the lower columns win, whichever they are."""
+    c = Case(dev, [640], H=1, G=2, D=16, budget=4, firsts=0, lasts=1)
+    c.bound()
+    torch.cuda.synchronize()
+    c.bounds_h[:], c.steps_h[:] = 100, 1.0
+    for column, step in ((7, 3e38), (11, np.inf), (5, 3e38), (20, np.nan), (3, 2.0)):
+        c.steps_h[c.bt[0, column]] = step
+    c.bounds_h[c.bt[0, 30], :, 0] = -100
+    c.q.copy_(c.q.abs() * 1000)
+    c.q_h = c.q.double().cpu().numpy()
+    c.bounds.copy_(torch.from_numpy(c.bounds_h))
+    c.steps.copy_(torch.from_numpy(c.steps_h))
+    c.choose()
+    c.check_choice()
+    assert c.chosen.tolist() == [[[5, 7, 11, 39]]]
