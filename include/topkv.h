@@ -519,10 +519,13 @@ int topkv_rotary_turns(const double* h_frequencies, uint32_t n, uint64_t* h_turn
  *   ORDER    the k-th request in the order of (leader, request), at place k
  *   PLACE    where r stands in that order
  * One group per first page: where some of its requests share more than all of them do, those tokens are
- * read by each. A caller that knows better may write a plan of its own: LEADER, SHARED, MEMBERS, ORDER and
- * PLACE are what attention reads. The groups may stand in any order there, each with its leader (any of its requests) first and
- * the others right behind it, and share any number of tokens that all of its requests have in common. One that contradicts itself gives results without meaning (and may raise
- * error bit 2), but no access outside the pool and the tensors; a request shorter than SHARED is attended to on its own.
+ * read by each, and a request that has little more than the first page in common with the others leaves
+ * them little to share. A caller that knows better may write a plan of its own: LEADER, SHARED, MEMBERS,
+ * ORDER and PLACE are what attention reads. The groups may stand in any order there, each with its leader
+ * (any of its requests) first and the others right behind it, and share any number of tokens that all of
+ * its requests have in common. A plan that contradicts itself gives results without meaning (and may raise
+ * error bit 2), but no access outside the pool and the tensors; a request shorter than SHARED is attended
+ * to on its own.
  * One or two kernels on `stream`, no allocation, no synchronisation, capturable; batch->window_tokens must be 0.
  * Every row looks at every other one: fine for thousands of requests, not for a hundred thousand. */
 #define TOPKV_PLAN_ROWS 6
@@ -532,10 +535,11 @@ int topkv_plan_prefixes(const topkv_layout* layout, const topkv_batch* batch, in
                         int32_t* d_plan, topkv_stream_t stream);
 /* As topkv_attend_layer, with the shared tokens' part formed once per group: the queries of all its
  * members and heads are the rows of one product. kv_factor 2 only (128 query heads already share a latent
- * row, which leaves nothing to gain), no window (window_tokens and sink_tokens 0). Weights are rounded as
- * topkv_attend_layer rounds them (to fp16; of a bf16 cache with head_dim <= 128 to two bf16 values, beyond that to one), and
- * bf16 queries over an 8-bit cache become fp16 with a power of two for each row. Three kernels at most;
- * the workspace holds nothing between calls, and calls that may run at the same time need one each.
+ * row and leave little to gain; for fewer heads it is not built), no window (window_tokens and sink_tokens
+ * 0). Weights are rounded as topkv_attend_layer rounds them (to fp16; of a bf16 cache with head_dim <= 128
+ * to two bf16 values, beyond that to one), and bf16 queries over an 8-bit cache become fp16 with a power of
+ * two for each row. Three kernels at most; the workspace holds nothing between calls, and calls that may
+ * run at the same time need one each.
  * Capturable (the first call for a head size and type on a device raises the kernels' shared-memory limits: make
  * it outside a capture). TOPKV_FLAG_TABLES_SETTLED covers d_plan too. TOPKV_ERR_UNSUPPORTED_LAYOUT also for batches
  * whose prefixes could amount to more than 2^31 tiles of 128 tokens and rows. */

@@ -17,9 +17,10 @@
 // first CTA's shared memory, which then selects alone (a pass of the whole cluster takes 1.5 us for its barrier and
 // the remote histograms); where they are more than it holds, each keeps its own, and histograms and counts are
 // added up through the cluster's shared memory.
-// Measured: 4 requests of 65,537 to 131,071 tokens, 128 of up to 8,192 pages a head, 8 x 8 heads of 128: bounds read
-// at 5.4 TB/s in 10 us, 8 for the selection, attention over the chosen 34 MB and its join 14, 49 with both calls; two
-// of 2,000 to 3,001 tokens 17 us, the calls.
+// Measured: 4 requests of 65,537 to 131,071 tokens, 128 of up to 8,192 pages a head, 8 x 4 heads of 128: 28 us here, of
+// which the bounds are read at 5.4 TB/s in 10 and the selection takes 8, attention over the chosen 34 MB 16, its join 4: 49
+// with both calls; two of 2,000 to 3,001 tokens 17 us, the calls (24 in a table of 65,536 columns, where the keys stay with
+// their CTAs).
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>

@@ -390,10 +390,10 @@ int topkv_attend_shared_layer(int layer, const void* pool, const topkv_layout* l
   p.a = attend_params(layer, pool, layout, batch, attention, plan.attend, d_q, d_out);
   p.a.plan = d_plan;
   // Whether a group's tokens are formed once. 8 KV heads of 128, both ways after other work has been through L2,
-  // once / by each request: 16-bit, 40 pairs of 4,096 tokens 165 / 236 us, 8 fours of 1,024 42 / 42, 20 pairs of 1,024
-  // 56 / 50, eight of 8,192 40 / 53: worth it from 8 MB on. 8-bit tokens are converted tile by tile, at a rate that does
-  // not depend on the rows: 40 pairs of 4,096 198 / 151, 40 fours of 1,024 120 / 102, 8 eights of 4,096 81 / 122, 8
-  // sixteens of 1,024 79 / 87, as if two more members had to read them.
+  // once / by each request: 16-bit, 40 pairs of 4,096 tokens 170 / 236 us, 40 fours of 1,024 105 / 118, 20 pairs of 1,024
+  // 60 / 51, eight of 8,192 42 / 55: worth it from 8 MB on. 8-bit tokens are converted tile by tile, at a rate that does
+  // not depend on the rows: 40 pairs of 4,096 197 / 152, 40 fours of 1,024 118 / 101, 8 eights of 4,096 79 / 122, 8
+  // sixteens of 1,024 76 / 87, as if two more members had to read them.
   const int64_t least = g_sharing_bytes.load(std::memory_order_relaxed);
   const int64_t token_bytes = 2ll * p.a.H * p.a.D * (int64_t)layout->elem_bytes;
   p.a.least_saved = least / token_bytes + (least % token_bytes != 0);  // rounded up: at least that many bytes

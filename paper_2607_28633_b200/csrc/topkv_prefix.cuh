@@ -5,9 +5,10 @@
 //   parts join by  out = sum_k exp(m_k - m) o_k / sum_k exp(m_k - m) l_k,  m = max m_k
 //
 // The queries of a group's members and of a KV head's G query heads are the rows of one product with the
-// prefix: members * G rows, 2 * members * G flops a byte at 16 bits, so with 128 rows the tensor rate (254
-// flop a byte of this memory) is about reached: the product runs on the tensor memory path (tcgen05), 128 rows to a
-// tile, rows in TMEM lanes, one thread a row, so that maxima and sums need no exchange:
+// prefix: members * G rows, and as many flops a byte at 16 bits (4 rows flops for 2 + 2 bytes of K and V), twice as
+// many at 8. The tensor rate is 254 flop a byte of this memory, so 254 rows of 16 bits balance both and 128 leave the
+// memory as the bound: the product runs on the tensor memory path (tcgen05), 128 rows to a tile and up to two tiles over
+// the same tokens, rows in TMEM lanes, one thread a row, so that maxima and sums need no exchange:
 //
 //   S [128 x tokens] = Q [128 x D] K^T         both K-major in shared memory
 //   O [128 x D]     += P [128 x tokens] V      P in TMEM, over the scores it was made of; V N-major. Of a bf16 cache P is
@@ -25,11 +26,12 @@
 // per CTA; each leaves its part in 32 bits in the workspace, and the joining kernel adds them to those of the
 // tokens behind the prefix, in order, so that results do not depend on timing.
 // Waits are bounded and TMEM is held as in the latent-row kernel.
-// What bounds it: with many rows the steps from one tile's scores to the next (a tile of 128 tokens and 256 rows takes 4,400
-// cycles, of which the tensor core is busy 2,200 and a softmax job 2,600); with few rows a tile takes as long, and memory is
-// at about half its rate. Measured, with the plan made before: 64 requests behind 16,384 tokens with 100 to 1,000 of
-// their own, 8 x 8 heads of 128, bf16: 96 us, of which 40 are the product, 860 Tflop/s (126 in the first form); 78
-// requests in 6 groups behind 500 to 4,000 tokens, e4m3: 67 us (79).
+// What bounds it: with many rows the steps from one tile's scores to the next (with one bf16 value a weight a tile of 128
+// tokens and 256 rows takes 4,400 cycles, of which the tensor core is busy 2,200 and a softmax job 2,600; the second value
+// adds 1,100 to the tensor core's); with few rows a tile takes as long, and memory is at about half its rate. Measured, with
+// the plan made before: 64 requests behind 16,384 tokens with 100 to 1,000 of their own, 8 x 8 heads of 128, bf16: 103 us,
+// 61 in this kernel, 30 behind it, 11 in the join; 78 requests in 6 groups behind 500 to 4,000 tokens, e4m3: 68 us, 31 + 26 +
+// 10. 32 requests behind 8,192 tokens, plan included: 4 x 8 heads of 256 72 us (floor 15), e4m3 84 (8); 8 x 8 heads of 64 50 (8).
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -128,7 +130,8 @@ __device__ __forceinline__ void plan_group(const PrefixPlanParams& p, int r, int
   }
 }
 // A warp per row. Up to kPrefixPlanRows rows fit one cluster, whose barrier separates the two steps; more take a
-// launch each. (7 rows: 7.8 us with the cluster, 10.0 with two launches; 253 rows of up to 410 pages 9.6.)
+// launch each. (7 rows: 7.8 us with the cluster, 10.0 with two launches; 253 rows of up to 410 pages 9.6; by two launches
+// 1,000 rows 23.5, 3,000 63: every row looks at all others, twice.)
 constexpr int kPrefixPlanCluster = 8, kPrefixPlanRows = kPrefixPlanCluster * kPrefixPlanThreads / 32;
 __global__ void __launch_bounds__(kPrefixPlanThreads) topkv_plan_cluster_kernel(const PrefixPlanParams p) {
   pdl_wait_prior_grid();
@@ -323,7 +326,7 @@ __global__ void __launch_bounds__(PrefixShape<DP, TYPE>::kThreads, 1) topkv_pref
   // to 0.0017, the output's rounding, for half as many products again (64 requests 104 -> 112 us, the plan included).
   constexpr bool kSecond = kBf && DP <= 128;
   constexpr int kTokens = S::kTokens, kTiles = S::kTiles, kStages = S::kStages;
-  // 8-bit values: a warp brings them, two convert
+  // 8-bit values: a warp brings them, four convert
   constexpr int kRawWarp = S::kConvert ? S::kSoftmaxWarps : -1, kLoadWarp = S::kSoftmaxWarps + (S::kConvert ? 1 : 0);
   constexpr int kIssueWarp = kLoadWarp + S::kLoadWarps;
   constexpr int kSoftmaxThreads = S::kSoftmaxWarps * 32;
